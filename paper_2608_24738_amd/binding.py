@@ -85,6 +85,23 @@ def load() -> ctypes.CDLL:
             lib.tm_selftest_host.argtypes = []
             lib.tm_mask_nonzero.restype = i32
             lib.tm_mask_nonzero.argtypes = [vp, i32, i32, vp, vp, vp, vp]
+            # the operators of a training step (module training)
+            size = ctypes.c_size_t
+            labels = [vp, i32, i64, i64, i64, vp, vp, i32, vp, vp]
+            lib.tm_label_logp.argtypes = labels + [i32, vp, vp, vp, vp, vp, vp, vp, size, vp]
+            lib.tm_label_logp_workspace_size.argtypes = [i32, i64, i64, i64, vp, i32]
+            lib.tm_label_logp_grad.argtypes = labels + [vp] * 8 + [vp]
+            grid = [i32, vp, vp, vp, i32, vp, i64]
+            lib.tm_distance_bias.argtypes = [vp, i32, i64, i64, vp, i32, i32, i64, vp, vp, vp, i32, vp]
+            lib.tm_relative_bias.argtypes = grid + [vp, i32, i32, i64, vp, vp, vp, i32, vp]
+            lib.tm_distance_bias_grad.argtypes = [vp, i32, i64, i64, vp, i32, i32, i64, vp, vp, i32, vp, size, vp]
+            lib.tm_relative_bias_grad.argtypes = grid + [vp, i32, i32, i64, vp, vp, i32, vp, size, vp]
+            lib.tm_bias_grad_workspace_size.argtypes = [i64, i64, i32, i64]
+            for name in ("tm_label_logp", "tm_label_logp_grad", "tm_distance_bias", "tm_relative_bias",
+                         "tm_distance_bias_grad", "tm_relative_bias_grad"):
+                getattr(lib, name).restype = i32
+            lib.tm_label_logp_workspace_size.restype = size
+            lib.tm_bias_grad_workspace_size.restype = size
             _lib = lib
     return _lib
 

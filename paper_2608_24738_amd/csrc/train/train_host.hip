@@ -1,0 +1,395 @@
+// train_host.hip -- C-ABI of the training operators: argument checks, choice
+// of kernel and launches (declared in include/tm_train.h).
+
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+
+#include "../../../include/tm_train.h"
+#include "bias.h"
+#include "label.h"
+
+using namespace tmtrain;
+
+namespace {
+
+constexpr uint64_t kLimit = uint64_t(1) << 31;
+
+bool float_type(int dtype) { return dtype == TM_DTYPE_F32 || dtype == TM_DTYPE_F16 || dtype == TM_DTYPE_BF16; }
+uint64_t float_bytes(int dtype) { return dtype == TM_DTYPE_F32 ? 4 : 2; }
+
+struct Range {
+    const void *at;
+    uint64_t bytes;
+};
+bool meet(const Range &a, const Range &b) {
+    if (!a.at || !b.at || !a.bytes || !b.bytes) return false;
+    const uintptr_t x = uintptr_t(a.at), y = uintptr_t(b.at);
+    return x < y + b.bytes && y < x + a.bytes;
+}
+// No output may overlap an input or another output.
+template <int NI, int NO>
+bool aliased(const Range (&in)[NI], const Range (&out)[NO]) {
+    for (int o = 0; o < NO; ++o) {
+        for (int i = 0; i < NI; ++i)
+            if (meet(out[o], in[i])) return true;
+        for (int p = 0; p < o; ++p)
+            if (meet(out[o], out[p])) return true;
+    }
+    return false;
+}
+
+template <typename Args>
+int launch(void (*kernel)(Args), dim3 grid, dim3 block, hipStream_t s, const Args &args) {
+    hipLaunchKernelGGL(kernel, grid, block, 0, s, args);
+    return hipGetLastError() == hipSuccess ? TM_OK : TM_ERR_HIP;
+}
+
+// fn(T{}) with T the storage type of dtype.
+template <typename F>
+int by_type(int dtype, F fn) {
+    if (dtype == TM_DTYPE_F32) return fn(float{});
+    if (dtype == TM_DTYPE_BF16) return fn(bf16{});
+    return fn(f16{});
+}
+
+// ---------------------------------------------------------------------------
+// Labels.
+// ---------------------------------------------------------------------------
+
+// Elements from a view's first to the end of its last, or 0 if a stride is
+// negative or the view is too long to address.
+uint64_t view_span(const uint64_t (&n)[3], const int64_t *strides) {
+    uint64_t span = 1;
+    for (int a = 0; a < 3; ++a) {
+        if (strides[a] < 0) return 0;
+        if (n[a] > 1 && uint64_t(strides[a]) > (uint64_t(1) << 58) / n[a]) return 0;
+        span += (n[a] - 1) * uint64_t(strides[a]);
+    }
+    return span;
+}
+
+// Whether two elements of a view share an address.
+bool self_overlap(const uint64_t (&n)[3], const int64_t *strides) {
+    int order[3] = {0, 1, 2};
+    for (int a = 1; a < 3; ++a)
+        for (int b = a; b > 0 && strides[order[b]] < strides[order[b - 1]]; --b) {
+            const int t = order[b];
+            order[b] = order[b - 1];
+            order[b - 1] = t;
+        }
+    uint64_t reach = 0;         // from the first to the last element of the axes so far
+    for (int a : order) {
+        if (n[a] < 2) continue;
+        if (uint64_t(strides[a]) <= reach) return true;
+        reach += (n[a] - 1) * uint64_t(strides[a]);
+    }
+    return false;
+}
+
+struct LabelShape {
+    uint64_t n[3];              // outer, classes, inner
+    uint64_t positions;
+    uint64_t x_bytes, field_bytes, label_bytes;
+};
+
+int check_labels(const void *logits, int dtype, int64_t outer, int64_t classes, int64_t inner, const int64_t *strides,
+                 const void *labels, int label_dtype, const float *field, const int64_t *field_strides,
+                 LabelShape &s) {
+    if (outer < 0 || inner < 0 || classes < 1 || !strides || (field && !field_strides)) return TM_ERR_SHAPE;
+    for (int a = 0; a < 3; ++a)
+        if (strides[a] < 0 || (field && field_strides[a] < 0)) return TM_ERR_SHAPE;
+    if (!float_type(dtype)) return TM_ERR_DTYPE;
+    if (labels && label_dtype != TM_DTYPE_U8 && label_dtype != TM_DTYPE_I32 && label_dtype != TM_DTYPE_I64)
+        return TM_ERR_DTYPE;
+    if (uint64_t(classes) >= kLimit || uint64_t(outer) >= kLimit || uint64_t(inner) >= kLimit ||
+        uint64_t(outer) * uint64_t(inner) >= kLimit)
+        return TM_ERR_TOO_LARGE;
+    s.n[0] = uint64_t(outer);
+    s.n[1] = uint64_t(classes);
+    s.n[2] = uint64_t(inner);
+    s.positions = s.n[0] * s.n[2];
+    if (s.positions == 0) return TM_OK;
+    if (!logits) return TM_ERR_NULL;
+    const uint64_t span = view_span(s.n, strides), fspan = field ? view_span(s.n, field_strides) : 1;
+    if (!span || !fspan) return TM_ERR_TOO_LARGE;
+    s.x_bytes = span * float_bytes(dtype);
+    s.field_bytes = field ? fspan * 4 : 0;
+    s.label_bytes = label_dtype == TM_DTYPE_U8 ? 1 : label_dtype == TM_DTYPE_I32 ? 4 : 8;
+    return TM_OK;
+}
+
+}  // namespace
+
+extern "C" size_t tm_label_logp_workspace_size(int, int64_t, int64_t, int64_t, const int64_t *, int) { return 0; }
+
+extern "C" int tm_label_logp(const void *logits, int dtype, int64_t outer, int64_t classes, int64_t inner,
+                             const int64_t *strides, const void *labels, int label_dtype, const float *field,
+                             const int64_t *field_strides, int top_k, float *out_logp, float *out_entropy,
+                             float *out_mean, float *out_top, int32_t *out_index, float *out_stats, void *workspace,
+                             size_t workspace_bytes, hipStream_t stream) {
+    LabelShape s{};
+    const int rc = check_labels(logits, dtype, outer, classes, inner, strides, labels, label_dtype, field,
+                                field_strides, s);
+    if (rc != TM_OK) return rc;
+    if (top_k < 0 || top_k > TM_LABEL_MAX_TOP || top_k > classes) return TM_ERR_UNSUPPORTED;
+    if (s.positions == 0) return TM_OK;
+    if ((out_logp && !labels) || (out_mean && !field)) return TM_ERR_NULL;
+    if (!out_logp && !out_entropy && !out_mean && !out_stats && !top_k) return TM_ERR_NO_OUTPUT;
+    if (top_k > 0 && (!out_top || !out_index)) return TM_ERR_NO_OUTPUT;
+    const size_t need = tm_label_logp_workspace_size(dtype, outer, classes, inner, strides, top_k);
+    if (need && (!workspace || workspace_bytes < need || uintptr_t(workspace) % 8)) return TM_ERR_WORKSPACE;
+    const uint64_t n4 = s.positions * 4;
+    const Range in[] = {{logits, s.x_bytes}, {labels, s.positions * s.label_bytes}, {field, s.field_bytes}};
+    const Range out[] = {{out_logp, n4}, {out_entropy, n4}, {out_mean, n4}, {out_stats, 2 * n4},
+                         {top_k ? out_top : nullptr, n4 * uint64_t(top_k)},
+                         {top_k ? out_index : nullptr, n4 * uint64_t(top_k)}, {need ? workspace : nullptr, need}};
+    if (aliased(in, out)) return TM_ERR_ALIAS;
+    LabelArgs a{};
+    a.x = logits;
+    a.label = labels;
+    a.field = out_mean ? field : nullptr;
+    a.logp = out_logp;
+    a.entropy = out_entropy;
+    a.mean = out_mean;
+    a.top = out_top;
+    a.index = out_index;
+    a.stats = out_stats;
+    for (int i = 0; i < 3; ++i) {
+        a.xs[i] = strides[i];
+        a.fs[i] = a.field ? field_strides[i] : 0;
+    }
+    a.outer = uint32_t(outer);
+    a.classes = uint32_t(classes);
+    a.inner = uint32_t(inner);
+    a.k = uint32_t(top_k);
+    a.label_bytes = int32_t(s.label_bytes);
+    a.n = uint32_t(s.positions);
+    a.div_inner = Div32::make(uint32_t(inner));
+    return by_type(dtype, [&](auto t) {
+        return launch(k_label_logp<decltype(t)>, dim3((a.n + 255) / 256), dim3(256), stream, a);
+    });
+}
+
+extern "C" int tm_label_logp_grad(const void *logits, int dtype, int64_t outer, int64_t classes, int64_t inner,
+                                  const int64_t *strides, const void *labels, int label_dtype, const float *field,
+                                  const int64_t *field_strides, const float *stats, const float *entropy,
+                                  const float *mean, const float *up_logp, const float *up_entropy,
+                                  const float *up_mean, void *out_grad, const int64_t *grad_strides,
+                                  hipStream_t stream) {
+    LabelShape s{};
+    const int rc = check_labels(logits, dtype, outer, classes, inner, strides, labels, label_dtype, field,
+                                field_strides, s);
+    if (rc != TM_OK) return rc;
+    if (!grad_strides) return TM_ERR_SHAPE;
+    for (int a = 0; a < 3; ++a)
+        if (grad_strides[a] < 0) return TM_ERR_SHAPE;
+    if (s.positions == 0) return TM_OK;
+    if (!up_logp && !up_entropy && !up_mean) return TM_ERR_NULL;
+    if ((up_logp && !labels) || (up_mean && !field)) return TM_ERR_NULL;
+    if (!stats && classes > TM_LABEL_MAX_RECOMPUTE) return TM_ERR_NULL;
+    if (stats && ((up_entropy && !entropy) || (up_mean && !mean))) return TM_ERR_NULL;
+    if (!out_grad) return TM_ERR_NO_OUTPUT;
+    const uint64_t span = view_span(s.n, grad_strides);
+    if (!span) return TM_ERR_TOO_LARGE;
+    if (self_overlap(s.n, grad_strides)) return TM_ERR_ALIAS;
+    const uint64_t n4 = s.positions * 4;
+    const Range in[] = {{logits, s.x_bytes}, {labels, s.positions * s.label_bytes}, {field, s.field_bytes},
+                        {stats, 2 * n4}, {entropy, n4}, {mean, n4}, {up_logp, n4}, {up_entropy, n4}, {up_mean, n4}};
+    const Range out[] = {{out_grad, span * float_bytes(dtype)}};
+    if (aliased(in, out)) return TM_ERR_ALIAS;
+    LabelGradArgs a{};
+    a.x = logits;
+    a.label = labels;
+    a.field = up_mean ? field : nullptr;
+    a.stats = stats;
+    a.entropy = entropy;
+    a.mean = mean;
+    a.up_logp = up_logp;
+    a.up_entropy = up_entropy;
+    a.up_mean = up_mean;
+    a.grad = out_grad;
+    for (int i = 0; i < 3; ++i) {
+        a.xs[i] = strides[i];
+        a.fs[i] = a.field ? field_strides[i] : 0;
+        a.gs[i] = grad_strides[i];
+    }
+    a.outer = uint32_t(outer);
+    a.classes = uint32_t(classes);
+    a.inner = uint32_t(inner);
+    a.label_bytes = int32_t(s.label_bytes);
+    a.n = uint32_t(s.positions);
+    a.div_inner = Div32::make(uint32_t(inner));
+    return by_type(dtype, [&](auto t) {
+        return launch(k_label_logp_grad<decltype(t)>, dim3((a.n + 255) / 256), dim3(256), stream, a);
+    });
+}
+
+// ---------------------------------------------------------------------------
+// Biases.
+// ---------------------------------------------------------------------------
+namespace {
+
+struct BiasShape {
+    BiasSource src;
+    uint64_t batch, field_batch;
+    uint64_t field_bytes;       // of the distances
+    uint64_t elements;          // batch * heads * positions
+};
+
+int check_field(const void *distances, int distance_dtype, int64_t batch, int64_t positions, BiasShape &s) {
+    if (batch < 0 || positions < 0) return TM_ERR_SHAPE;
+    if (distance_dtype != TM_DTYPE_F32 && distance_dtype != TM_DTYPE_I32) return TM_ERR_DTYPE;
+    if (uint64_t(batch) >= kLimit || uint64_t(positions) >= kLimit) return TM_ERR_TOO_LARGE;
+    s.src.source = distance_dtype == TM_DTYPE_F32 ? kFieldF32 : kFieldI32;
+    s.src.field = distances;
+    s.src.positions = uint32_t(positions);
+    s.batch = s.field_batch = uint64_t(batch);
+    s.field_bytes = s.batch * uint64_t(positions) * 4;
+    if (!distances && s.field_bytes) return TM_ERR_NULL;
+    return TM_OK;
+}
+
+int check_grid(int ndim, const int64_t *query_shape, const int64_t *key_shape, const int64_t *query_offset, int metric,
+               const double *sampling, int64_t batch, BiasShape &s) {
+    if (ndim < 1 || ndim > kBiasMaxDim) return TM_ERR_NDIM;
+    if (!query_shape || !key_shape || batch < 0) return TM_ERR_SHAPE;
+    if (metric < TM_METRIC_EUCLIDEAN || metric > TM_METRIC_OFFSET || (metric == TM_METRIC_OFFSET && ndim != 1))
+        return TM_ERR_METRIC;
+    uint64_t nq = 1, nk = 1;
+    for (int a = 0; a < ndim; ++a) {
+        if (query_shape[a] < 0 || key_shape[a] < 0) return TM_ERR_SHAPE;
+        const int64_t off = query_offset ? query_offset[a] : 0, lim = int64_t(1) << 30;
+        if (query_shape[a] > lim || key_shape[a] > lim || off > lim || off < -lim) return TM_ERR_TOO_LARGE;
+        const double sp = sampling ? sampling[a] : 1.0;
+        if (!std::isfinite(sp) || !(sp > 0.0) || !std::isfinite(float(sp)) || !(float(sp) > 0.0f))
+            return TM_ERR_SAMPLING;
+        s.src.offset[a] = int32_t(off);
+        s.src.sampling[a] = float(sp);
+        s.src.div_q[a] = Div32::make(uint32_t(query_shape[a] ? query_shape[a] : 1));
+        s.src.div_k[a] = Div32::make(uint32_t(key_shape[a] ? key_shape[a] : 1));
+        nq *= uint64_t(query_shape[a]);
+        nk *= uint64_t(key_shape[a]);
+        if (nq >= kLimit || nk >= kLimit) return TM_ERR_TOO_LARGE;
+    }
+    if (nq * nk >= kLimit || uint64_t(batch) >= kLimit) return TM_ERR_TOO_LARGE;
+    if (metric == TM_METRIC_OFFSET && s.src.sampling[0] != 1.0f) return TM_ERR_SAMPLING;
+    s.src.source = metric == TM_METRIC_OFFSET ? kOffset : metric == TM_METRIC_EUCLIDEAN ? kEuclid
+                   : metric == TM_METRIC_TAXICAB ? kTaxicab : kChess;
+    s.src.ndim = ndim;
+    s.src.positions = uint32_t(nq * nk);
+    s.src.div_key = Div32::make(uint32_t(nk ? nk : 1));
+    s.batch = uint64_t(batch);
+    s.field_batch = 1;
+    return TM_OK;
+}
+
+int check_table(int buckets, int64_t heads, const float *edges, int table_dtype, int value_dtype, BiasShape &s) {
+    if (buckets < 1 || buckets > int(kMaxBuckets) || heads < 1) return TM_ERR_SHAPE;
+    if (!float_type(table_dtype) || !float_type(value_dtype)) return TM_ERR_DTYPE;
+    if (uint64_t(heads) >= kLimit / kMaxBuckets) return TM_ERR_TOO_LARGE;
+    if (!edges && buckets > 1) return TM_ERR_NULL;
+    const uint64_t lim = uint64_t(1) << 58;
+    const uint64_t bh = s.batch * uint64_t(heads);          // below 2^54
+    if (s.src.positions && bh > lim / s.src.positions) return TM_ERR_TOO_LARGE;
+    s.src.edges = edges;
+    s.src.buckets = uint32_t(buckets);
+    s.elements = bh * s.src.positions;
+    return TM_OK;
+}
+
+int run_bias(const BiasShape &s, const void *table, int table_dtype, int64_t heads, const void *add, void *out,
+             int out_dtype, hipStream_t stream) {
+    if (s.elements == 0) return TM_OK;
+    if (!table) return TM_ERR_NULL;
+    if (!out) return TM_ERR_NO_OUTPUT;
+    const uint64_t bytes = s.elements * float_bytes(out_dtype);
+    const Range in[] = {{s.src.field, s.field_bytes}, {table, s.src.buckets * uint64_t(heads) * float_bytes(table_dtype)},
+                        {s.src.edges, 4 * uint64_t(s.src.buckets - 1)}, {add, bytes}};
+    const Range outs[] = {{out, bytes}};
+    if (aliased(in, outs)) return TM_ERR_ALIAS;
+    BiasArgs a{};
+    a.src = s.src;
+    a.table = table;
+    a.table_type = table_dtype;
+    a.add = add;
+    a.out = out;
+    a.heads = uint32_t(heads);
+    a.batch = uint32_t(s.batch);
+    a.field_batch = uint32_t(s.field_batch);
+    return by_type(out_dtype, [&](auto t) {
+        return launch(k_bias<decltype(t)>, dim3((s.src.positions + 255u) / 256u), dim3(256), stream, a);
+    });
+}
+
+int run_bias_grad(const BiasShape &s, const void *grad, int grad_dtype, int64_t heads, void *out, int table_dtype,
+                  void *workspace, size_t workspace_bytes, hipStream_t stream) {
+    if (!out) return TM_ERR_NO_OUTPUT;
+    if (!grad && s.elements) return TM_ERR_NULL;
+    const size_t need = tm_bias_grad_workspace_size(int64_t(s.field_batch), s.src.positions, int(s.src.buckets), heads);
+    if (need && (!workspace || workspace_bytes < need || uintptr_t(workspace) % 16)) return TM_ERR_WORKSPACE;
+    const Range in[] = {{s.src.field, s.field_bytes}, {s.src.edges, 4 * uint64_t(s.src.buckets - 1)},
+                        {grad, s.elements * float_bytes(grad_dtype)}};
+    const Range outs[] = {{out, s.src.buckets * uint64_t(heads) * float_bytes(table_dtype)},
+                          {need ? workspace : nullptr, need}};
+    if (aliased(in, outs)) return TM_ERR_ALIAS;
+    BiasGradArgs a{};
+    a.src = s.src;
+    a.grad = grad;
+    a.out = out;
+    a.partial = static_cast<float *>(workspace);
+    a.heads = uint32_t(heads);
+    a.batch = uint32_t(s.batch);
+    a.field_batch = uint32_t(s.field_batch);
+    a.table_type = table_dtype;
+    return by_type(grad_dtype, [&](auto t) {
+        return launch(k_bias_grad<decltype(t)>, dim3(s.src.buckets * a.heads), dim3(256), stream, a);
+    });
+}
+
+}  // namespace
+
+extern "C" int tm_distance_bias(const void *distances, int distance_dtype, int64_t batch, int64_t positions,
+                                const void *table, int table_dtype, int buckets, int64_t heads, const float *edges,
+                                const void *add, void *out, int out_dtype, hipStream_t stream) {
+    BiasShape s{};
+    int rc = check_field(distances, distance_dtype, batch, positions, s);
+    if (rc == TM_OK) rc = check_table(buckets, heads, edges, table_dtype, out_dtype, s);
+    return rc == TM_OK ? run_bias(s, table, table_dtype, heads, add, out, out_dtype, stream) : rc;
+}
+
+extern "C" int tm_relative_bias(int ndim, const int64_t *query_shape, const int64_t *key_shape,
+                                const int64_t *query_offset, int metric, const double *sampling, int64_t batch,
+                                const void *table, int table_dtype, int buckets, int64_t heads, const float *edges,
+                                const void *add, void *out, int out_dtype, hipStream_t stream) {
+    BiasShape s{};
+    int rc = check_grid(ndim, query_shape, key_shape, query_offset, metric, sampling, batch, s);
+    if (rc == TM_OK && !add && batch > 1) rc = TM_ERR_SHAPE;
+    if (rc == TM_OK) rc = check_table(buckets, heads, edges, table_dtype, out_dtype, s);
+    return rc == TM_OK ? run_bias(s, table, table_dtype, heads, add, out, out_dtype, stream) : rc;
+}
+
+extern "C" size_t tm_bias_grad_workspace_size(int64_t, int64_t, int, int64_t) { return 0; }
+
+extern "C" int tm_distance_bias_grad(const void *distances, int distance_dtype, int64_t batch, int64_t positions,
+                                     const void *grad, int grad_dtype, int buckets, int64_t heads, const float *edges,
+                                     void *out_grad, int table_dtype, void *workspace, size_t workspace_bytes,
+                                     hipStream_t stream) {
+    BiasShape s{};
+    int rc = check_field(distances, distance_dtype, batch, positions, s);
+    if (rc == TM_OK) rc = check_table(buckets, heads, edges, table_dtype, grad_dtype, s);
+    return rc == TM_OK ? run_bias_grad(s, grad, grad_dtype, heads, out_grad, table_dtype, workspace, workspace_bytes,
+                                       stream) : rc;
+}
+
+extern "C" int tm_relative_bias_grad(int ndim, const int64_t *query_shape, const int64_t *key_shape,
+                                     const int64_t *query_offset, int metric, const double *sampling, int64_t batch,
+                                     const void *grad, int grad_dtype, int buckets, int64_t heads, const float *edges,
+                                     void *out_grad, int table_dtype, void *workspace, size_t workspace_bytes,
+                                     hipStream_t stream) {
+    BiasShape s{};
+    int rc = check_grid(ndim, query_shape, key_shape, query_offset, metric, sampling, batch, s);
+    if (rc == TM_OK) rc = check_table(buckets, heads, edges, table_dtype, grad_dtype, s);
+    return rc == TM_OK ? run_bias_grad(s, grad, grad_dtype, heads, out_grad, table_dtype, workspace, workspace_bytes,
+                                       stream) : rc;
+}

@@ -1,0 +1,391 @@
+"""The operators of a training step on distances, over torch tensors.
+
+``label_log_probs``  log-probabilities of given labels, with the entropy, the
+                     likeliest classes and the expected value of a field under
+                     the softmax (the boundary loss, for the signed distance
+                     field of each class)
+``relative_bias``    a learned bias by buckets of the distance between a
+                     query's and a key's position
+``distance_bias``    the same bias from a distance field
+
+All three run in the HIP kernels of ``libtm_edt.so`` (``include/tm_train.h``)
+on the current stream, take part in autograd, and raise where the library
+refuses a request; there is no fallback.
+"""
+from __future__ import annotations
+
+import ctypes
+import functools
+import math
+from typing import NamedTuple, Optional
+
+import torch
+
+from .binding import METRICS, _call, _sampling_array, _shape_array, load
+
+FLOATS = {torch.float16: 4, torch.bfloat16: 5, torch.float32: 6}
+LABELS = {torch.uint8: 0, torch.int32: 2, torch.int64: 3}
+DISTANCES = {torch.int32: 2, torch.float32: 6}
+BIAS_METRICS = dict(METRICS, offset=3)
+MAX_TOP = 32
+MAX_RECOMPUTE = 16           # classes whose gradient needs no saved statistics
+MAX_BUCKETS = 256
+
+
+class LabelLogProbs(NamedTuple):
+    """What ``label_log_probs`` gives; None for what was not asked for."""
+    log_probs: Optional[torch.Tensor]
+    entropy: Optional[torch.Tensor]
+    field_mean: Optional[torch.Tensor]
+    top_log_probs: Optional[torch.Tensor]
+    top_indices: Optional[torch.Tensor]
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _collapse(sizes, strides):
+    """One axis (extent, stride) that visits the elements of these axes in
+    order, or None where no single stride does."""
+    extent, step = 1, 0
+    for n, st in zip(reversed(sizes), reversed(strides)):
+        if n == 1:
+            continue
+        if extent == 1:
+            step = st
+        elif st != extent * step:
+            return None
+        extent *= n
+    return extent, step
+
+
+@functools.lru_cache(maxsize=1024)
+def _view(shape, strides, dim):
+    """((outer, classes, inner), their strides as a C array) of a tensor whose
+    class axis is ``dim``, or None where three strides cannot describe it."""
+    if 0 in shape:
+        return (math.prod(shape[:dim]), shape[dim], math.prod(shape[dim + 1:])), (ctypes.c_int64 * 3)(0, 0, 0)
+    outer = _collapse(shape[:dim], strides[:dim])
+    inner = _collapse(shape[dim + 1:], strides[dim + 1:])
+    if outer is None or inner is None:
+        return None
+    return (outer[0], shape[dim], inner[0]), (ctypes.c_int64 * 3)(outer[1], strides[dim], inner[1])
+
+
+def _viewed(t, dim):
+    """(tensor, extents, strides): ``t``, or a contiguous copy of it where its
+    strides are too many."""
+    view = _view(tuple(t.shape), t.stride(), dim)
+    if view is None:
+        t = t.contiguous()
+        view = _view(tuple(t.shape), t.stride(), dim)
+    return t, view[0], view[1]
+
+
+@functools.lru_cache(maxsize=1024)
+def _label_workspace(dtype, extents, strides, top_k):
+    return int(load().tm_label_logp_workspace_size(dtype, *extents, (ctypes.c_int64 * 3)(*strides), top_k))
+
+
+def _label_forward(logits, labels, field, dim, entropy, top_k, stats):
+    """Runs tm_label_logp; returns (logits, field) as they were read and the outputs."""
+    dev = logits.device
+    logits, extents, strides = _viewed(logits, dim)
+    shape = logits.shape[:dim] + logits.shape[dim + 1:]
+    field_strides = None
+    if field is not None:
+        field, _, field_strides = _viewed(field, dim)
+    logp = torch.empty(shape, dtype=torch.float32, device=dev) if labels is not None else None
+    ent = torch.empty(shape, dtype=torch.float32, device=dev) if entropy else None
+    mean = torch.empty(shape, dtype=torch.float32, device=dev) if field is not None else None
+    top = index = kept = workspace = None
+    if top_k:
+        shape_k = logits.shape[:dim] + (top_k,) + logits.shape[dim + 1:]
+        top = torch.empty(shape_k, dtype=torch.float32, device=dev)
+        index = torch.empty(shape_k, dtype=torch.int32, device=dev)
+    if stats:
+        kept = torch.empty(tuple(shape) + (2,), dtype=torch.float32, device=dev)
+    nbytes = _label_workspace(FLOATS[logits.dtype], extents, tuple(strides), top_k)
+    if nbytes:
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    _call("tm_label_logp", dev, None, logits.data_ptr(), FLOATS[logits.dtype], *extents, strides, _ptr(labels),
+          LABELS[labels.dtype] if labels is not None else 0, _ptr(field), field_strides, top_k, _ptr(logp), _ptr(ent),
+          _ptr(mean), _ptr(top), _ptr(index), _ptr(kept), _ptr(workspace), nbytes)
+    return logits, field, (logp, ent, mean, top, index), kept
+
+
+def _upstream(grad):
+    return None if grad is None else grad.to(torch.float32).contiguous()
+
+
+class _LabelLogProbs(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, labels, field, dim, entropy, top_k):
+        stats = logits.shape[dim] > MAX_RECOMPUTE
+        logits, field, out, kept = _label_forward(logits, labels, field, dim, entropy, top_k, stats)
+        ctx.dim = dim
+        ctx.set_materialize_grads(False)
+        ctx.mark_non_differentiable(*[t for t in out[3:] if t is not None])
+        ctx.save_for_backward(logits, labels, field, kept, out[1] if stats else None, out[2] if stats else None)
+        return out
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, up_logp, up_entropy, up_mean, _top, _index):
+        logits, labels, field, kept, entropy, mean = ctx.saved_tensors
+        if up_logp is None and up_entropy is None and up_mean is None:
+            return None, None, None, None, None, None
+        up_logp, up_entropy, up_mean = _upstream(up_logp), _upstream(up_entropy), _upstream(up_mean)
+        grad = torch.empty_like(logits)
+        _, extents, strides = _viewed(logits, ctx.dim)
+        grad, _, grad_strides = _viewed(grad, ctx.dim)
+        field_strides = _viewed(field, ctx.dim)[2] if field is not None else None
+        _call("tm_label_logp_grad", logits.device, None, logits.data_ptr(), FLOATS[logits.dtype], *extents, strides,
+              _ptr(labels), LABELS[labels.dtype] if labels is not None else 0, _ptr(field), field_strides, _ptr(kept),
+              _ptr(entropy), _ptr(mean), _ptr(up_logp), _ptr(up_entropy), _ptr(up_mean), grad.data_ptr(), grad_strides)
+        return grad, None, None, None, None, None
+
+
+def label_log_probs(logits: torch.Tensor, labels: Optional[torch.Tensor] = None, *, dim: int = 1,
+                    entropy: bool = False, top_k: int = 0, field: Optional[torch.Tensor] = None) -> LabelLogProbs:
+    """Log-probabilities of given labels under the softmax of ``logits`` over
+    axis ``dim``: (B, C, *spatial) maps, or rows (N, C).
+
+    ``logits``  float32, float16 or bfloat16, any strides.
+    ``labels``  their shape without ``dim``; uint8, bool, int32 or int64.  A
+                label outside [0, C) marks an element without one: log-probability
+                0, and no gradient through it.  None: no ``log_probs``.
+    ``entropy`` also the entropy of each element's classes.
+    ``top_k``   also the largest log-probabilities and their classes (at most
+                32), along ``dim`` in falling order, equal logits by rising class.
+    ``field``   float32, the logits' shape (or broadcastable to it): also
+                ``field_mean``, the sum over classes of probability x field.
+
+    Results are float32 (indices int32).  Gradients flow to ``logits`` from
+    ``log_probs``, ``entropy`` and ``field_mean``; labels, field and the top
+    classes are constants of the step.
+    """
+    if not logits.is_cuda:
+        raise ValueError("logits must be a ROCm (cuda) tensor")
+    if logits.dtype not in FLOATS:
+        raise TypeError("logits must be float32, float16 or bfloat16, got %s" % logits.dtype)
+    if not -logits.dim() <= dim < logits.dim():
+        raise ValueError("logits of %d dimensions have no axis %d" % (logits.dim(), dim))
+    dim %= logits.dim()
+    classes = logits.shape[dim]
+    if classes < 1:
+        raise ValueError("logits have no classes along axis %d" % dim)
+    if labels is not None:
+        if labels.device != logits.device:
+            raise ValueError("labels are on %s, the logits on %s" % (labels.device, logits.device))
+        if labels.dtype == torch.bool:
+            labels = labels.contiguous().view(torch.uint8)
+        if labels.dtype not in LABELS:
+            raise TypeError("labels must be uint8, bool, int32 or int64, got %s" % labels.dtype)
+        if labels.shape != logits.shape[:dim] + logits.shape[dim + 1:]:
+            raise ValueError("labels of shape %s do not fit logits of shape %s with classes along axis %d"
+                             % (tuple(labels.shape), tuple(logits.shape), dim))
+        labels = labels.contiguous()
+    if not 0 <= top_k <= min(classes, MAX_TOP):
+        raise ValueError("top_k must be between 0 and %d, got %d" % (min(classes, MAX_TOP), top_k))
+    if field is not None:
+        if field.device != logits.device:
+            raise ValueError("field is on %s, the logits on %s" % (field.device, logits.device))
+        if field.dtype != torch.float32:
+            raise TypeError("field must be float32, got %s" % field.dtype)
+        if field.requires_grad and torch.is_grad_enabled():
+            raise ValueError("field is a constant of the step; detach it")
+        if field.shape != logits.shape:
+            field = field.expand(logits.shape)
+    if labels is None and field is None and not entropy and not top_k:
+        raise ValueError("nothing to compute: give labels or a field, or ask for the entropy or top_k")
+    entropy, top_k = bool(entropy), int(top_k)
+    if logits.requires_grad and torch.is_grad_enabled():
+        return LabelLogProbs(*_LabelLogProbs.apply(logits, labels, field, dim, entropy, top_k))
+    return LabelLogProbs(*_label_forward(logits, labels, field, dim, entropy, top_k, False)[2])
+
+
+def distance_edges(buckets: int, reach: float, *, signed: bool = False, device=None) -> torch.Tensor:
+    """``buckets`` - 1 ascending edges for ``relative_bias`` and ``distance_bias``:
+    one bucket a unit for the nearer half, then buckets growing by a constant
+    factor up to ``reach``; ``signed`` splits them between both signs (of
+    metric "offset").  Any other ascending edges do as well."""
+    if not 1 <= buckets <= MAX_BUCKETS:
+        raise ValueError("buckets must be between 1 and %d, got %d" % (MAX_BUCKETS, buckets))
+
+    def half(count):
+        exact = (count + 1) // 2
+        far = count - exact
+        span = max(float(reach), 2.0 * exact)
+        return [0.5 + i for i in range(exact)] + [
+            0.5 + exact * (span / max(exact, 1)) ** ((i + 1) / (far + 1)) for i in range(far)]
+    if signed:
+        near = half((buckets - 1) // 2)
+        edges = [-e for e in reversed(near)] + near
+        if len(edges) < buckets - 1:
+            edges.append(2.0 * near[-1] if near else 0.5)
+    else:
+        edges = half(buckets - 1)
+    return torch.tensor(edges, dtype=torch.float32, device=device)
+
+
+class _Bias(torch.autograd.Function):
+    """A bias whose table learns.  ``source`` is what the entry points take
+    before the table: ("tm_distance_bias", args, keep) with ``keep`` the
+    distances, or ("tm_relative_bias", args, None)."""
+
+    @staticmethod
+    def forward(ctx, table, edges, add, source, shape, sizes):
+        ctx.source, ctx.sizes = source, sizes
+        ctx.table_dtype, ctx.table_shape = table.dtype, tuple(table.shape)
+        ctx.has_add = add is not None
+        ctx.save_for_backward(edges, source[2])
+        return _bias_forward(table, edges, add, source, shape)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, up):
+        edges, distances = ctx.saved_tensors
+        name, args, _ = ctx.source
+        grad = None
+        if ctx.needs_input_grad[0]:
+            up = up.contiguous()
+            buckets, heads = ctx.table_shape
+            dev = edges.device
+            grad = torch.empty(ctx.table_shape, dtype=ctx.table_dtype, device=dev)
+            nbytes = _bias_workspace(*ctx.sizes, buckets, heads)
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
+            if distances is not None:
+                args = (distances.data_ptr(),) + args[1:]
+            _call(name + "_grad", dev, None, *args, up.data_ptr(), FLOATS[up.dtype], buckets, heads, edges.data_ptr(),
+                  grad.data_ptr(), FLOATS[ctx.table_dtype], _ptr(workspace), nbytes)
+        return grad, None, up if ctx.has_add and ctx.needs_input_grad[2] else None, None, None, None
+
+
+@functools.lru_cache(maxsize=1024)
+def _bias_workspace(batch, positions, buckets, heads):
+    return int(load().tm_bias_grad_workspace_size(batch, positions, buckets, heads))
+
+
+def _bias_forward(table, edges, add, source, shape):
+    name, args, _ = source
+    out = torch.empty(shape, dtype=table.dtype if add is None else add.dtype, device=table.device)
+    _call(name, table.device, None, *args, table.data_ptr(), FLOATS[table.dtype], table.shape[0], table.shape[1],
+          edges.data_ptr(), _ptr(add), out.data_ptr(), FLOATS[out.dtype])
+    return out
+
+
+def _run_bias(table, edges, add, source, shape, sizes):
+    if torch.is_grad_enabled() and (table.requires_grad or (add is not None and add.requires_grad)):
+        return _Bias.apply(table, edges, add, source, shape, sizes)
+    return _bias_forward(table, edges, add, source, shape)
+
+
+def _check_bias(table, edges, add):
+    if not table.is_cuda:
+        raise ValueError("table must be a ROCm (cuda) tensor")
+    if table.dtype not in FLOATS:
+        raise TypeError("table must be float32, float16 or bfloat16, got %s" % table.dtype)
+    if table.dim() != 2 or not 1 <= table.shape[0] <= MAX_BUCKETS or table.shape[1] < 1:
+        raise ValueError("table must be (buckets, heads) with 1 to %d buckets, got %s"
+                         % (MAX_BUCKETS, tuple(table.shape)))
+    if edges.dtype != torch.float32 or edges.device != table.device:
+        raise TypeError("edges must be float32 on %s" % table.device)
+    if tuple(edges.shape) != (table.shape[0] - 1,):
+        raise ValueError("a table of %d buckets needs %d edges, got %s"
+                         % (table.shape[0], table.shape[0] - 1, tuple(edges.shape)))
+    if add is not None:
+        if add.dtype not in FLOATS:
+            raise TypeError("add must be float32, float16 or bfloat16, got %s" % add.dtype)
+        if add.device != table.device:
+            raise ValueError("add is on %s, the table on %s" % (add.device, table.device))
+        add = add.contiguous()
+    return table.contiguous(), edges.contiguous(), add
+
+
+def distance_bias(distances: torch.Tensor, table: torch.Tensor, edges: torch.Tensor, *,
+                  add: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """A learned bias by buckets of a distance field: from ``distances`` (B,
+    *spatial), float32 or int32, to (B, heads, *spatial) with
+
+        out[b, h, x] = table[number of edges <= distances[b, x], h]  (+ add[b, h, x])
+
+    ``table``  (buckets, heads) float32, float16 or bfloat16.
+    ``edges``  buckets - 1 ascending float32 values on the same device.
+    ``add``    (B, heads, *spatial), such as logits: the sum is made in float32
+               and rounded once to its type; alone, the bias has the table's.
+
+    Gradients flow to ``table`` and ``add``; distances are constants of the step.
+    """
+    table, edges, add = _check_bias(table, edges, add)
+    if distances.dtype not in DISTANCES:
+        raise TypeError("distances must be float32 or int32, got %s" % distances.dtype)
+    if distances.device != table.device:
+        raise ValueError("distances are on %s, the table on %s" % (distances.device, table.device))
+    if distances.dim() < 1:
+        raise ValueError("distances must be (B, *spatial)")
+    if distances.requires_grad and torch.is_grad_enabled():
+        raise ValueError("distances are constants of the step; detach them")
+    distances = distances.contiguous()
+    shape = (distances.shape[0], table.shape[1]) + tuple(distances.shape[1:])
+    if add is not None and tuple(add.shape) != shape:
+        raise ValueError("add must have shape %s, got %s" % (shape, tuple(add.shape)))
+    sizes = (distances.shape[0], math.prod(distances.shape[1:]))
+    source = ("tm_distance_bias", (distances.data_ptr(), DISTANCES[distances.dtype]) + sizes, distances)
+    return _run_bias(table, edges, add, source, shape, sizes)
+
+
+def _extents(value, what):
+    extents = (value,) if isinstance(value, int) else tuple(int(n) for n in value)
+    if not 1 <= len(extents) <= 8:
+        raise ValueError("%s must have 1 to 8 axes" % what)
+    return extents
+
+
+def relative_bias(table: torch.Tensor, edges: torch.Tensor, query_shape, key_shape, *, query_offset=0,
+                  metric: str = "euclidean", sampling=None, add: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """A learned bias by buckets of the distance between a query's and a key's
+    position, for attention over a sequence, an image or a volume:
+
+        out[h, q, k] = table[number of edges <= D(q, k), h]  (+ add[..., h, q, k])
+
+    ``query_shape``, ``key_shape``  extents of the grids of queries and keys (an
+                int for a sequence); positions run in row-major order.
+    ``query_offset``  coordinates of the first query (an int: along the first
+                axis), as for one new token at the end of its sequence.
+    ``metric``  "offset": the signed difference key - query of a sequence;
+                "euclidean", "taxicab" or "chessboard": the library's distances,
+                with ``sampling`` the spacing along each axis.
+    ``table``, ``edges``  as for ``distance_bias``.
+    ``add``     (*batch, heads, queries, keys), such as attention scores.
+
+    Returns (heads, queries, keys) of the table's type, or the shape and type
+    of ``add``.  Gradients flow to ``table`` (summed over the batch) and ``add``.
+    """
+    table, edges, add = _check_bias(table, edges, add)
+    query, key = _extents(query_shape, "query_shape"), _extents(key_shape, "key_shape")
+    ndim = len(query)
+    if len(key) != ndim:
+        raise ValueError("query_shape has %d axes, key_shape %d" % (ndim, len(key)))
+    offset = (query_offset,) + (0,) * (ndim - 1) if isinstance(query_offset, int) else tuple(query_offset)
+    if len(offset) != ndim:
+        raise ValueError("query_offset must have %d coordinates, got %d" % (ndim, len(offset)))
+    if metric not in BIAS_METRICS:
+        raise ValueError("metric must be one of %s" % sorted(BIAS_METRICS))
+    if metric == "offset" and (ndim != 1 or sampling is not None):
+        raise ValueError("metric 'offset' is for sequences, without sampling")
+    if sampling is not None:
+        sampling = [float(sampling)] * ndim if isinstance(sampling, (int, float)) else [float(s) for s in sampling]
+        if len(sampling) != ndim:
+            raise RuntimeError("sequence argument must have length equal to input rank")
+    tail = (table.shape[1], math.prod(query), math.prod(key))
+    shape, batch = tail, 1
+    if add is not None:
+        if tuple(add.shape[-3:]) != tail:
+            raise ValueError("add must have shape (..., %d, %d, %d), got %s" % (tail + (tuple(add.shape),)))
+        shape = tuple(add.shape)
+        batch = math.prod(shape[:-3])
+    args = (ndim, _shape_array(query), _shape_array(key), _shape_array(offset), BIAS_METRICS[metric],
+            _sampling_array(sampling, ndim), batch)
+    return _run_bias(table, edges, add, ("tm_relative_bias", args, None), shape, (1, tail[1] * tail[2]))

@@ -1,0 +1,298 @@
+"""relative_bias, distance_bias and the gradient of their table against the definitions in float64.
+
+Bounds.  A forward value is a table entry, widened exactly, plus at most one float32 addition and one
+rounding to the output's type.  A gradient is a float32 sum in some fixed order: n terms of magnitudes
+summing to S, whose roundings are independent, stay within u S (8 + 8 sqrt n) / n^(1/2) ... bounded here by
+u S 16 (each partial sum is at most S and the error of a sum of n random roundings of partial sums growing
+to S is about u S sqrt(n) / n^(1/2)); the worst case of a short chain, u S n for n <= 16, is below it.
+"""
+import numpy as np
+import pytest
+
+import bias_reference as ref
+from gpu_util import announce
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"f32": "float32", "f16": "float16", "bf16": "bfloat16"}
+U = 2.0 ** -24
+
+
+def check_all(call, table, bucket, add, dtype, table_type, up, what, heads):
+    """call(table, add) -> bias; forward and gradient against the reference.  bucket: (B or 1, P)."""
+    import torch
+    announce("bias " + what)
+    table = table.detach().requires_grad_(up is not None)
+    bias = call(table, add)
+    grad = None
+    if up is not None:
+        wants = [table]
+        if add is not None:
+            add = add.detach().requires_grad_(True)
+            bias = call(table, add)
+            wants.append(add)
+        got = torch.autograd.grad([bias], wants, [up])
+        grad = got[0]
+        if add is not None:
+            assert torch.equal(got[1].nan_to_num(), up.nan_to_num())
+    torch.cuda.synchronize()
+    p = bucket.shape[1]
+    lead = bias.numel() // (heads * p)
+    value = bias.detach().reshape(lead, heads, p).double().cpu().numpy()
+    t = table.detach().double().cpu().numpy()
+    a = None if add is None else add.detach().reshape(lead, heads, p).double().cpu().numpy()
+    want = ref.forward(t, np.broadcast_to(bucket, (lead, p)), a)
+    ref.check(value, want, 0.0 if a is None else U * np.abs(want), dtype, what + " forward")
+    if up is not None:
+        assert grad.dtype == table.dtype and grad.shape == table.shape
+        total, size, _ = ref.gradient(up.reshape(lead, heads, p).double().cpu().numpy(), bucket, table.shape[0])
+        ref.check(grad.double().cpu().numpy(), total, 16 * U * np.where(np.isfinite(size), size, 0), table_type,
+                  what + " gradient")
+    return bias, grad
+
+
+def relative(query, key, heads, count, metric, dtype="f32", table_type=None, offset=0, sampling=None, batch=None,
+             train=True, seed=0, edges=None):
+    import torch
+    from paper_2608_24738_amd import training
+    gen = torch.Generator().manual_seed(seed)
+    dev = "cuda:0"
+    table_type = table_type or (dtype if batch is None else "f32")
+    kind = getattr(torch, TYPES[dtype])
+    off = (offset,) + (0,) * (len(query) - 1) if isinstance(offset, int) else offset
+    if edges is None:
+        edges = training.distance_edges(count, max(key), signed=metric == "offset")
+    table = torch.randn((count, heads), generator=gen).to(getattr(torch, TYPES[table_type])).to(dev)
+    tail = (heads, int(np.prod(query)), int(np.prod(key)))
+    shape = tail if batch is None else tuple(batch) + tail
+    add = None if batch is None else (torch.randn(shape, generator=gen) * 3).to(kind).to(dev)
+    up = torch.randn(shape, generator=gen).to(kind).to(dev) if train else None
+    bucket = ref.buckets(ref.grid_distances(query, key, off, metric, sampling), edges.numpy()).reshape(1, -1)
+    on = edges.to(dev)
+    what = "relative %s x %s heads=%d buckets=%d %s %s batch=%s" % (query, key, heads, count, metric, dtype, batch)
+
+    def call(t, a):
+        return training.relative_bias(t, on, query, key, query_offset=offset, metric=metric, sampling=sampling, add=a)
+    return check_all(call, table, bucket, add, dtype, table_type, up, what, heads)
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("query,key,heads,count,offset", [
+    (1, 1, 1, 1, 0), (1, 1, 2, 2, 5), (1, 2, 3, 3, 1), (3, 5, 4, 8, 0), (1, 4099, 16, 32, 4098), (1, 64, 33, 32, 63),
+    (65, 65, 5, 31, 0), (7, 1030, 2, 33, 100), (129, 63, 17, 64, -3), (300, 301, 16, 32, 0), (33, 31, 3, 255, 0),
+    (31, 47, 48, 16, 0), (64, 64, 1, 256, 0)])
+def test_sequence(query, key, heads, count, offset, dtype):
+    relative((query,), (key,), heads, count, "offset", dtype, offset=offset)
+    relative((query,), (key,), heads, count, "offset", dtype, offset=offset, batch=(3,), seed=1)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("metric", ["euclidean", "taxicab", "chessboard"])
+@pytest.mark.parametrize("query,key,offset", [
+    ((5,), (9,), 2), ((4, 6), (4, 6), 0), ((1, 1), (17, 19), (16, 18)), ((3, 5), (7, 2), (0, 1)),
+    ((2, 3, 4), (5, 4, 3), (1, 0, -2)), ((9, 1, 2), (3, 3, 3), 0), ((2, 2, 2, 2), (3, 1, 2, 2), 0),
+    ((1, 2, 1, 2, 1, 2, 1, 2), (2, 1, 2, 1, 2, 1, 2, 1), 0), ((16, 16), (16, 16), 0)])
+def test_grids(query, key, offset, metric, dtype):
+    relative(query, key, 3, 12, metric, dtype, offset=offset)
+    relative(query, key, 5, 12, metric, dtype, offset=offset, batch=(2, 2), seed=2)
+    if len(query) == 3:
+        relative(query, key, 4, 20, metric, dtype, offset=offset, sampling=(2.5, 0.8, 0.8))
+
+
+def test_edges_on_distances():
+    """Edges that equal distances, repeated edges, edges far out and infinite."""
+    import torch
+    inf = float("inf")
+    for edges in ([0.0], [1.0, 2.0, 5.0], [1.0, 1.0, 1.0, 3.0], [-inf, 0.0, 2.0, inf], [2.0 ** 0.5, 5.0 ** 0.5]):
+        e = torch.tensor(edges, dtype=torch.float32)
+        for metric in ("euclidean", "taxicab", "chessboard"):
+            relative((6, 7), (6, 7), 2, len(edges) + 1, metric, edges=e)
+    e = torch.tensor([-3.0, 0.0, 0.0, 4.0])
+    relative((9,), (12,), 2, 5, "offset", edges=e)
+
+
+def distance(batch, shape, heads, count, dtype="f32", kind="float32", add=False, table_type=None, train=True, seed=0,
+             values=None, edges=None):
+    import torch
+    from paper_2608_24738_amd import training
+    gen = torch.Generator().manual_seed(seed)
+    dev = "cuda:0"
+    table_type = table_type or ("f32" if add else dtype)
+    if values is None:
+        values = torch.rand((batch,) + shape, generator=gen) ** 2 * 60
+        values = values.round().to(torch.int32) if kind == "int32" else values
+    if edges is None:
+        edges = training.distance_edges(count, 40)
+    out = getattr(torch, TYPES[dtype])
+    table = torch.randn((count, heads), generator=gen).to(getattr(torch, TYPES[table_type])).to(dev)
+    full = (batch, heads) + shape
+    extra = (torch.randn(full, generator=gen) * 3).to(out).to(dev) if add else None
+    up = torch.randn(full, generator=gen).to(out).to(dev) if train else None
+    bucket = ref.buckets(values.numpy(), edges.numpy()).reshape(batch, -1)
+    d, on = values.to(dev), edges.to(dev)
+    what = "distance %d x %s heads=%d buckets=%d %s %s add=%s" % (batch, shape, heads, count, dtype, kind, add)
+    return check_all(lambda t, a: training.distance_bias(d, t, on, add=a), table, bucket, extra, dtype, table_type, up,
+                     what, heads)
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("batch,shape,heads,count", [
+    (1, (1,), 1, 1), (1, (5,), 1, 2), (2, (63,), 3, 8), (3, (8, 8), 4, 24), (2, (31, 33), 16, 32), (1, (1023,), 17, 40),
+    (4, (5, 6, 7), 2, 64), (1, (40, 50), 21, 128), (2, (9, 10), 5, 256), (1, (70, 71), 33, 16), (7, (3,), 1, 9)])
+def test_fields(batch, shape, heads, count, dtype):
+    distance(batch, shape, heads, count, dtype)
+    distance(batch, shape, heads, count, dtype, kind="int32", add=True, seed=1)
+
+
+@pytest.mark.parametrize("count", [1, 15, 16, 17, 32, 33, 64, 65, 128, 129, 256])
+def test_bucket_counts(count):
+    distance(1, (3000,), 3, count)
+    relative((50,), (60,), 18, count, "offset", "bf16")
+
+
+def test_larger():
+    distance(3, (200, 211), 4, 24, "bf16", add=True)
+    distance(2, (61, 62, 63), 1, 64, "f32")
+    relative((512,), (513,), 8, 32, "offset", "bf16", batch=(2,))
+    relative((12, 13), (12, 13), 6, 40, "euclidean", "f16", batch=(3,))
+
+
+def test_one_bucket_of_many_positions():
+    """Every position in one bucket: a sum over all, and zeros elsewhere."""
+    import torch
+    values = torch.full((2, 70000), 7.0)
+    _, grad = distance(2, (70000,), 2, 24, "f32", values=values)
+    assert int((grad != 0).any(1).sum()) == 1
+
+
+def test_odd_distances():
+    """NaN, infinities and huge integers have a bucket."""
+    import torch
+    inf = float("inf")
+    values = torch.tensor([[0.0, -0.0, float("nan"), inf, -inf, 1e30, -5.0, 3.0]])
+    distance(1, (8,), 3, 12, values=values)
+    huge = torch.tensor([[0, 2 ** 31 - 1, -2 ** 31, 2 ** 24 + 1, 7]], dtype=torch.int32)
+    distance(1, (5,), 3, 12, kind="int32", values=huge)
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+def test_not_finite(dtype):
+    """Infinities and NaN in gradients reach their own bucket and head alone."""
+    import torch
+    from paper_2608_24738_amd import training
+    gen = torch.Generator().manual_seed(5)
+    dev = "cuda:0"
+    d = (torch.rand((2, 900), generator=gen) * 30)
+    edges = training.distance_edges(20, 30)
+    for heads in (1, 5, 20):
+        table = torch.randn((20, heads), generator=gen).to(dev).requires_grad_(True)
+        up = torch.randn((2, heads, 900), generator=gen)
+        up[0, 0, 5], up[1, heads - 1, 700], up[1, 0, 899] = float("inf"), float("nan"), float("-inf")
+        up = up.to(getattr(torch, TYPES[dtype]))
+        announce("gradients that are not finite, heads=%d %s" % (heads, dtype))
+        bias = training.distance_bias(d.to(dev), table, edges.to(dev), add=up.to(dev))
+        grad, = torch.autograd.grad([bias], [table], [up.to(dev)])
+        total, size, _ = ref.gradient(up.double().numpy(), ref.buckets(d.numpy(), edges.numpy()), 20)
+        ref.check(grad.cpu().double().numpy(), total, 16 * U * np.where(np.isfinite(size), size, 0), "f32", "not finite")
+
+
+def test_cancelling_and_wide_values():
+    """Gradients of very different sizes in one bucket keep 24 bits of the largest."""
+    import torch
+    from paper_2608_24738_amd import training
+    dev = "cuda:0"
+    gen = torch.Generator().manual_seed(1)
+    d = torch.rand((1, 4096), generator=gen) * 30
+    edges = training.distance_edges(16, 30)
+    up = torch.randn((1, 3, 4096), generator=gen) * torch.pow(10.0, torch.rand((1, 3, 4096), generator=gen) * 12 - 6)
+    table = torch.zeros((16, 3), device=dev, requires_grad=True)
+    bias = training.distance_bias(d.to(dev), table, edges.to(dev))
+    grad, = torch.autograd.grad([bias], [table], [up.to(dev)])
+    total, size, _ = ref.gradient(up.double().numpy(), ref.buckets(d.numpy(), edges.numpy()), 16)
+    ref.check(grad.cpu().double().numpy(), total, 16 * U * size, "f32", "wide values")
+
+
+def test_differences():
+    """The table's gradient against differences of the forward pass: the bias is linear in it, so one step is exact
+    but for rounding."""
+    import torch
+    from paper_2608_24738_amd import training
+    dev = "cuda:0"
+    gen = torch.Generator().manual_seed(3)
+    edges = training.distance_edges(9, 20).to(dev)
+    table = torch.randn((9, 2), generator=gen).to(dev).requires_grad_(True)
+    up = torch.randn((2, 30, 30), generator=gen).to(dev)
+
+    def loss(t):
+        return (training.relative_bias(t, edges, (5, 6), (5, 6)).double() * up.double()).sum()
+    grad, = torch.autograd.grad([training.relative_bias(table, edges, (5, 6), (5, 6))], [table], [up])
+    with torch.no_grad():
+        for k in range(9):
+            for h in range(2):
+                step = torch.zeros_like(table)
+                step[k, h] = 1.0
+                slope = float(loss(table + step) - loss(table - step)) / 2
+                # up to 900 entries of magnitude 3 rounded to u each
+                assert abs(slope - float(grad[k, h])) < 900 * 3 * 4 * U * 4
+
+
+def test_strides_and_alignment():
+    import torch
+    from paper_2608_24738_amd import training
+    dev = "cuda:0"
+    gen = torch.Generator().manual_seed(7)
+    edges = training.distance_edges(16, 30).to(dev)
+    for dtype in (torch.float32, torch.bfloat16):
+        d = (torch.rand((2, 40, 41), generator=gen) * 30).to(dev)
+        add = torch.randn((2, 3, 40, 41), generator=gen).to(dtype).to(dev)
+        wide = torch.randn((16, 8), generator=gen).to(dev)
+        base = training.distance_bias(d, wide[:, :3].contiguous(), edges, add=add)
+        announce("strides and alignment %s" % dtype)
+        assert torch.equal(base, training.distance_bias(d, wide[:, :3], edges, add=add))
+        assert torch.equal(base, training.distance_bias(
+            d.transpose(1, 2).contiguous().transpose(1, 2), wide[:, :3], edges,
+            add=add.to(memory_format=torch.channels_last)))
+        for shift in (1, 2, 3, 5):
+            room = torch.zeros(add.numel() + 8, dtype=dtype, device=dev)
+            moved = room[shift:shift + add.numel()].view(add.shape)
+            moved.copy_(add)
+            far = torch.zeros(d.numel() + 8, device=dev)
+            near = far[shift:shift + d.numel()].view(d.shape)
+            near.copy_(d)
+            table = wide[:, :3].clone().requires_grad_(True)
+            got = training.distance_bias(near, table, edges, add=moved)
+            assert torch.equal(base, got)
+            one, = torch.autograd.grad([got], [table], [moved])
+            table2 = wide[:, :3].clone().requires_grad_(True)
+            two, = torch.autograd.grad([training.distance_bias(d, table2, edges, add=add)], [table2], [add])
+            assert torch.allclose(one, two, rtol=1e-5, atol=1e-4)
+
+
+def test_repeatable():
+    import torch
+    from paper_2608_24738_amd import training
+    dev = "cuda:0"
+    gen = torch.Generator().manual_seed(9)
+    edges = training.distance_edges(32, 500, signed=True).to(dev)
+    up = torch.randn((2, 16, 400, 400), generator=gen).to(torch.bfloat16).to(dev)
+    grads = []
+    for _ in range(3):
+        table = torch.zeros((32, 16), device=dev, requires_grad=True)
+        bias = training.relative_bias(table, edges, 400, 400, metric="offset", add=up)
+        grads.append(torch.autograd.grad([bias], [table], [up])[0])
+    assert torch.equal(grads[0], grads[1]) and torch.equal(grads[0], grads[2])
+
+
+def test_empty():
+    import torch
+    from paper_2608_24738_amd import training
+    dev = "cuda:0"
+    table = torch.ones((4, 2), device=dev, requires_grad=True)
+    edges = training.distance_edges(4, 5).to(dev)
+    for d in (torch.zeros((0, 3), device=dev), torch.zeros((2, 0), device=dev)):
+        bias = training.distance_bias(d, table, edges)
+        grad, = torch.autograd.grad([bias], [table], [torch.zeros_like(bias)])
+        assert bias.numel() == 0 and torch.equal(grad, torch.zeros_like(table))
+    add = torch.zeros((0, 2, 3, 4), device=dev)
+    assert training.relative_bias(table, edges, 3, 4, add=add).shape == (0, 2, 3, 4)
+    assert training.relative_bias(table, edges, 0, 4).shape == (2, 0, 4)

@@ -1,0 +1,277 @@
+"""label_log_probs and its gradient against the definitions in float64."""
+import numpy as np
+import pytest
+
+import label_reference as ref
+from gpu_util import announce
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"f32": "float32", "f16": "float16", "bf16": "bfloat16"}
+
+
+def run(x, labels, dim=1, field=None, top_k=0, entropy=True, ups=None, what="", dtype="f32"):
+    """Runs forward and (ups given) backward on torch inputs; checks everything against float64."""
+    import torch
+    from paper_2608_24738_amd import training
+    announce("label_log_probs %s %s dim=%d top_k=%d field=%s train=%s" % (
+        what, tuple(x.shape), dim, top_k, field is not None, ups is not None))
+    x = x.detach().requires_grad_(ups is not None)
+    got = training.label_log_probs(x, labels, dim=dim, entropy=entropy, top_k=top_k, field=field)
+    grad = None
+    if ups is not None:
+        ups = [u if o is not None else None for o, u in zip((got.log_probs, got.entropy, got.field_mean), ups)]
+        outs = [o for o, u in zip((got.log_probs, got.entropy, got.field_mean), ups) if u is not None]
+        grad, = torch.autograd.grad(outs, [x], [u for u in ups if u is not None])
+    torch.cuda.synchronize()
+
+    def flat(t):                       # (N, classes or k), elements in order
+        t = t.detach().movedim(dim, -1)
+        return t.reshape(-1, t.shape[-1]).double().cpu().numpy()
+
+    lab = labels.reshape(-1).long().cpu().numpy()
+    up = None if ups is None else [None if u is None else u.reshape(-1).double().cpu().numpy() for u in ups]
+    want = ref.exact(flat(x), lab, None if field is None else flat(field.expand(x.shape)), top_k, up)
+    ref.check(got.log_probs.detach().reshape(-1).cpu(), want["logp"], want["tol_logp"], what + " log_probs")
+    if entropy:
+        ref.check(got.entropy.detach().reshape(-1).cpu(), want["entropy"], want["tol_entropy"], what + " entropy")
+    if field is not None:
+        ref.check(got.field_mean.detach().reshape(-1).cpu(), want["mean"], want["tol_mean"], what + " field_mean")
+    if top_k:
+        assert np.array_equal(flat(got.top_indices), want["index"]), what + " top_indices"
+        ref.check(flat(got.top_log_probs), want["top"], want["tol_top"], what + " top_log_probs")
+    if grad is not None:
+        assert grad.dtype == x.dtype and grad.shape == x.shape
+        ref.check(flat(grad), want["grad"], want["tol_grad"], what + " gradient", dtype)
+    return got, grad
+
+
+def case(shape, dtype, seed=0, dim=1, label="int64", scale=3.0, field=False, spread_labels=True):
+    import torch
+    gen = torch.Generator().manual_seed(seed)
+    x = (torch.randn(shape, generator=gen) * scale).to(getattr(torch, TYPES[dtype]))
+    rest = shape[:dim] + shape[dim + 1:]
+    classes = shape[dim]
+    y = torch.randint(0, classes, rest, generator=gen)
+    if spread_labels:
+        gone = torch.rand(rest, generator=gen) < 0.1
+        y = torch.where(gone, torch.full_like(y, 255 if label == "uint8" else -100), y)
+    phi = torch.randn(shape, generator=gen) * 20 if field else None
+    ups = [torch.randn(rest, generator=gen) for _ in range(3)]
+    dev = "cuda:0"
+    return (x.to(dev), y.to(getattr(torch, label)).to(dev), None if phi is None else phi.to(dev),
+            [u.to(dev) for u in ups])
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("shape", [
+    (1, 1), (1, 2), (3, 5), (2, 63), (5, 64), (4, 65), (3, 127), (2, 257), (7, 1000), (1, 1023), (2, 2049), (1, 4097),
+    (3, 8191), (2, 20011), (1, 65537), (70, 33), (1000, 16), (513, 17)])
+def test_rows(shape, dtype):
+    k = min(shape[1], 5)
+    x, y, phi, ups = case(shape, dtype, seed=shape[1], field=True)
+    run(x, y, field=phi, top_k=k, ups=ups, what="rows " + dtype, dtype=dtype)
+    run(x, y, entropy=False, top_k=0, what="rows, log-probabilities alone " + dtype, dtype=dtype)
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("shape", [
+    (1, 2, 1), (2, 3, 5), (1, 4, 63), (2, 4, 64, 3), (3, 8, 9, 7), (2, 5, 6, 7, 11), (1, 16, 129), (2, 17, 67),
+    (2, 21, 13, 17), (1, 150, 8, 9), (1, 1, 40), (2, 64, 33), (1, 300, 3), (1, 2000, 5), (2, 4, 4099)])
+def test_maps(shape, dtype):
+    k = min(shape[1], 3)
+    x, y, phi, ups = case(shape, dtype, seed=sum(shape), label="uint8" if shape[1] < 200 else "int32", field=True)
+    run(x, y, field=phi, top_k=k, ups=ups, what="maps " + dtype, dtype=dtype)
+    run(x, y, entropy=False, top_k=1, what="maps, no field " + dtype, dtype=dtype)
+    run(x, y, entropy=False, ups=[ups[0], None, None], what="maps, one gradient " + dtype, dtype=dtype)
+
+
+@pytest.mark.parametrize("label", ["uint8", "int32", "int64"])
+@pytest.mark.parametrize("parts", [(1, 0, 0), (0, 1, 0), (0, 0, 1), (1, 1, 0), (1, 0, 1), (0, 1, 1)])
+@pytest.mark.parametrize("shape", [(3, 4, 50), (3, 40, 50), (5, 700)])
+def test_parts_of_the_gradient(shape, parts, label):
+    x, y, phi, ups = case(shape, "f32", seed=3, label=label, field=True, spread_labels=label != "uint8")
+    if label == "uint8":
+        y = y.clamp(max=250)
+    run(x, y, field=phi, ups=[u if on else None for u, on in zip(ups, parts)], what="parts %s %s" % (parts, label))
+
+
+@pytest.mark.parametrize("k", [1, 2, 4, 7, 8, 16, 31, 32])
+@pytest.mark.parametrize("shape", [(3, 32), (2, 1500), (1, 70001), (2, 40, 61)])
+def test_top_k(shape, k):
+    x, y, _, _ = case(shape, "bf16", seed=k)
+    run(x, y, top_k=k, entropy=False, what="top", dtype="bf16")
+
+
+@pytest.mark.parametrize("order", ["equal", "rising", "falling", "steps", "zeros"])
+@pytest.mark.parametrize("shape", [(2, 100), (1, 3001), (1, 50000), (2, 12, 37), (1, 90, 21)])
+def test_top_ties(shape, order):
+    import torch
+    classes = shape[1]
+    c = torch.arange(classes, dtype=torch.float32)
+    values = {"equal": torch.full((classes,), 1.5), "rising": c / classes, "falling": -c / classes,
+              "steps": (c % 7).floor(), "zeros": torch.where(c % 2 == 0, -0.0, 0.0)}[order]
+    x = values.reshape((1, -1) + (1,) * (len(shape) - 2)).expand(shape).contiguous().to("cuda:0")
+    y = torch.zeros(shape[:1] + shape[2:], dtype=torch.int64, device="cuda:0")
+    run(x, y, top_k=12, what="ties " + order)
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("shape", [(6, 9), (6, 300), (6, 33000), (6, 9, 40), (6, 40, 41)])
+def test_masks(shape, dtype):
+    """-inf and the type's lowest value in some classes, in all but one, in all."""
+    import torch
+    x, y, phi, ups = case(shape, dtype, seed=8, field=True)
+    low = torch.finfo(x.dtype).min
+    cut = torch.rand(x.shape, device=x.device) < 0.5
+    x[0] = torch.where(cut[0], -torch.inf, x[0])
+    x[1] = torch.where(cut[1], low, x[1])
+    x[2] = -torch.inf
+    x[2][3] = x[5][3]
+    x[3] = -torch.inf
+    x[4] = low
+    x[5][::2] = -torch.inf
+    phi = torch.where(torch.isneginf(x), torch.where(cut, torch.inf, torch.nan), phi)
+    run(x, y, field=phi, top_k=8, ups=ups, what="masks " + dtype, dtype=dtype)
+
+
+@pytest.mark.parametrize("shape", [(4, 9), (4, 30000), (4, 9, 40), (4, 40, 41)])
+def test_not_finite(shape):
+    """NaN and +inf make a position's floats NaN and leave the others alone."""
+    import torch
+    x, y, phi, ups = case(shape, "f32", seed=9, field=True, spread_labels=False)
+    clean, _ = run(x, y, field=phi, top_k=2, ups=ups, what="clean")
+    x[1][5] = torch.nan
+    x[2][4] = torch.inf
+    from paper_2608_24738_amd import training
+    x = x.requires_grad_(True)
+    got = training.label_log_probs(x, y, entropy=True, field=phi, top_k=2)
+    grad, = torch.autograd.grad([got.log_probs, got.entropy, got.field_mean], [x], ups)
+    for a, b in zip(got[:3], clean[:3]):
+        assert torch.isnan(a[1:3]).all()
+        assert torch.equal(a[0], b[0]) and torch.equal(a[3], b[3])
+    assert torch.isnan(grad[1:3]).all() and torch.isfinite(grad[0]).all() and torch.isfinite(grad[3]).all()
+    inside = got.top_indices
+    assert ((inside >= 0) & (inside < shape[1])).all()
+
+
+@pytest.mark.parametrize("offset", [1.0e4, -3.0e4, 1.0e6])
+@pytest.mark.parametrize("shape", [(5, 20), (3, 5000), (2, 20, 30)])
+def test_large_logits(shape, offset):
+    """A shift of every logit changes nothing but their rounding, which the reference reads too."""
+    x, y, phi, ups = case(shape, "f32", seed=2, field=True)
+    run(x + offset, y, field=phi, top_k=3, ups=ups, what="shift %g" % offset)
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+def test_strides(dtype):
+    import torch
+    x, y, phi, ups = case((4, 70, 6, 10), dtype, seed=4, field=True)
+    # channels last: the class axis contiguous
+    run(x.to(memory_format=torch.channels_last), y, field=phi, top_k=4, ups=ups, what="channels last", dtype=dtype)
+    run(x, y, field=phi.to(memory_format=torch.channels_last), top_k=4, ups=ups, what="field channels last", dtype=dtype)
+    # last axis
+    last = x.movedim(1, -1).contiguous()
+    run(last, y, dim=-1, field=phi.movedim(1, -1), ups=ups, what="last axis", dtype=dtype)
+    # a view that three strides cannot describe, rows of a wider buffer, every other class
+    run(x[:, :, 1:5, 2:9], y[:, 1:5, 2:9], field=phi[:, :, 1:5, 2:9], top_k=2, ups=[u[:, 1:5, 2:9] for u in ups],
+        what="window", dtype=dtype)
+    wide, label, field, up = case((9, 1203), dtype, seed=5, field=True)
+    run(wide[:, 1:1002], label.clamp(max=1000), field=field[:, 1:1002], top_k=3, ups=up, what="padded rows", dtype=dtype)
+    run(wide[:, ::3], label.clamp(max=400), field=field[:, ::3], top_k=3, ups=up, what="every third class", dtype=dtype)
+    run(wide.t()[:500], label[:1].expand(500).clamp(max=8), dim=1, ups=[u[:1].expand(500) for u in up],
+        what="transposed", dtype=dtype)
+    # one field for all classes but a constant: broadcast
+    run(x, y, field=phi[:, :, :1, :1], ups=ups, what="broadcast field", dtype=dtype)
+    run(x[:1].expand(3, 70, 6, 10), y[:3], field=phi[:3], ups=[u[:3] for u in ups], what="expanded logits", dtype=dtype)
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("shift", [1, 2, 3, 5, 7])
+def test_alignment(shift, dtype):
+    """Logits, labels, field and gradients that begin off a 16-byte line."""
+    import torch
+    for shape in [(3, 4, 137), (2, 30, 77), (3, 2051), (300, 7)]:
+        x, y, phi, ups = case(shape, dtype, seed=shift, label="uint8" if shape[1] < 200 else "int32", field=True)
+
+        def moved(t):
+            room = torch.zeros(t.numel() + 8, dtype=t.dtype, device=t.device)
+            view = room[shift:shift + t.numel()].view(t.shape)
+            view.copy_(t)
+            return view
+        run(moved(x), moved(y), field=moved(phi), top_k=2, ups=[moved(u) for u in ups], what="shift %d" % shift,
+            dtype=dtype)
+
+
+def test_differences():
+    """The gradient against central differences of the float64 definition."""
+    import torch
+    for shape in [(2, 6, 3), (3, 50)]:
+        x, y, phi, ups = case(shape, "f32", seed=6, field=True, scale=1.0)
+        _, grad = run(x, y, field=phi, ups=ups, what="differences")
+        flat = x.detach().movedim(1, -1).reshape(-1, shape[1]).double().cpu().numpy()
+        lab = y.reshape(-1).cpu().numpy()
+        fld = phi.movedim(1, -1).reshape(-1, shape[1]).double().cpu().numpy()
+        up = [u.reshape(-1).double().cpu().numpy() for u in ups]
+
+        def loss(z):
+            r = ref.exact(z, lab, fld)
+            return up[0] * r["logp"] + up[1] * r["entropy"] + up[2] * r["mean"]
+        got = grad.movedim(1, -1).reshape(-1, shape[1]).double().cpu().numpy()
+        step = 1e-4
+        for c in range(shape[1]):
+            hi, lo = flat.copy(), flat.copy()
+            hi[:, c] += step
+            lo[:, c] -= step
+            # third derivatives of these are of the order of the field; step^2 of that, and float32's rounding
+            slope = (loss(hi) - loss(lo)) / (2 * step)
+            assert np.allclose(got[:, c], slope, rtol=1e-5, atol=1e-5 * np.abs(fld).max())
+
+
+def test_repeatable_and_streams():
+    import torch
+    from paper_2608_24738_amd import training
+    x, y, phi, ups = case((2, 50001), "bf16", seed=1, field=True)
+    first = training.label_log_probs(x, y, entropy=True, top_k=5, field=phi)
+    torch.cuda.synchronize()
+    other = torch.cuda.Stream()
+    other.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(other):
+        second = training.label_log_probs(x, y, entropy=True, top_k=5, field=phi)
+    torch.cuda.synchronize()
+    for a, b in zip(first, second):
+        assert torch.equal(a, b)
+
+
+def test_empty():
+    import torch
+    from paper_2608_24738_amd import training
+    for shape in [(0, 5), (3, 5, 0), (0, 5, 4)]:
+        x = torch.zeros(shape, device="cuda:0", requires_grad=True)
+        y = torch.zeros(shape[:1] + shape[2:], dtype=torch.int64, device="cuda:0")
+        got = training.label_log_probs(x, y, entropy=True, top_k=2, field=torch.zeros(shape, device="cuda:0"))
+        assert got.log_probs.shape == y.shape and got.top_indices.shape == shape[:1] + (2,) + shape[2:]
+        grad, = torch.autograd.grad(got.log_probs.sum(), [x])
+        assert grad.shape == shape
+
+
+def test_graph_replays():
+    """Forward and backward calls captured in a graph and replayed with other inputs."""
+    import torch
+    from paper_2608_24738_amd import training
+    for shape in [(2, 40000), (2, 5, 300)]:
+        x, y, phi, _ = case(shape, "f32", seed=3, field=True)
+        training.label_log_probs(x, y, entropy=True, top_k=3, field=phi)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            got = training.label_log_probs(x, y, entropy=True, top_k=3, field=phi)
+        for seed in range(4):
+            fresh = case(shape, "f32", seed=20 + seed)[0]
+            x.copy_(fresh)
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            want = training.label_log_probs(fresh, y, entropy=True, top_k=3, field=phi)
+            for a, b in zip(got, want):
+                assert torch.equal(a, b)

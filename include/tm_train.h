@@ -114,7 +114,7 @@ int tm_label_logp_grad(const void *logits, int dtype, int64_t outer, int64_t cla
  * table_dtype and out_dtype: TM_DTYPE_F32, _F16 or _BF16.
  * Errors: TM_ERR_SHAPE (buckets outside [1, TM_BIAS_MAX_BUCKETS], heads < 1,
  * negative extents), TM_ERR_NULL, TM_ERR_NO_OUTPUT, TM_ERR_DTYPE,
- * TM_ERR_TOO_LARGE (2^31 positions, heads or samples), TM_ERR_ALIAS, TM_ERR_HIP.
+ * TM_ERR_TOO_LARGE (2^31 positions or samples, more than 2^16 heads), TM_ERR_ALIAS, TM_ERR_HIP.
  */
 int tm_distance_bias(const void *distances, int distance_dtype, int64_t batch, int64_t positions, const void *table,
                      int table_dtype, int buckets, int64_t heads, const float *edges, const void *add, void *out,
@@ -161,9 +161,7 @@ int tm_relative_bias_grad(int ndim, const int64_t *query_shape, const int64_t *k
                           const void *grad, int grad_dtype, int buckets, int64_t heads, const float *edges,
                           void *out_grad, int table_dtype, void *workspace, size_t workspace_bytes,
                           hipStream_t stream);
-/* positions: those of one sample (query positions x key positions); batch: samples with a field of their own
- * (tm_distance_bias_grad), or 1 (tm_relative_bias_grad, whose samples share the buckets). */
-size_t tm_bias_grad_workspace_size(int64_t batch, int64_t positions, int buckets, int64_t heads);
+size_t tm_bias_grad_workspace_size(int buckets, int64_t heads);
 
 #ifdef __cplusplus
 }

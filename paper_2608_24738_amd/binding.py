@@ -96,7 +96,7 @@ def load() -> ctypes.CDLL:
             lib.tm_relative_bias.argtypes = grid + [vp, i32, i32, i64, vp, vp, vp, i32, vp]
             lib.tm_distance_bias_grad.argtypes = [vp, i32, i64, i64, vp, i32, i32, i64, vp, vp, i32, vp, size, vp]
             lib.tm_relative_bias_grad.argtypes = grid + [vp, i32, i32, i64, vp, vp, i32, vp, size, vp]
-            lib.tm_bias_grad_workspace_size.argtypes = [i64, i64, i32, i64]
+            lib.tm_bias_grad_workspace_size.argtypes = [i32, i64]
             for name in ("tm_label_logp", "tm_label_logp_grad", "tm_distance_bias", "tm_relative_bias",
                          "tm_distance_bias_grad", "tm_relative_bias_grad"):
                 getattr(lib, name).restype = i32

@@ -17,10 +17,10 @@ struct BiasSource {
     const void *field;
     const float *edges;
     int32_t source, ndim;
-    uint32_t buckets;
+    uint32_t buckets, span;                // span: buckets rounded up to a power of two
     uint32_t positions;                    // of one sample
     Div32 div_key;                         // key positions
-    Div32 div_q[kBiasMaxDim], div_k[kBiasMaxDim];
+    Div32 div_q[kBiasMaxDim], div_k[kBiasMaxDim];   // positions of the axes behind each axis
     int32_t offset[kBiasMaxDim];           // first query's coordinates
     float sampling[kBiasMaxDim];
 };
@@ -32,15 +32,22 @@ struct BiasArgs {
     void *out;
     uint32_t heads, batch, field_batch;    // field_batch: samples with buckets of their own
     int32_t table_type;                    // tm_dtype
+    uint32_t head_share, row;              // heads of a workgroup, and their floats per bucket in LDS
+    uint32_t batch_share, batch_shares;    // samples of a workgroup (relative)
+    Div32 div_tiles;                       // workgroups along the positions of one sample
 };
 
 struct BiasGradArgs {
     BiasSource src;
     const void *grad;
     void *out;
-    float *partial;
+    float *partial;                        // [splits][heads / 16][tile_rows][16]
     uint32_t heads, batch, field_batch;
     int32_t table_type;
+    uint32_t splits, tile_rows;
+    uint32_t units;                        // shares of the batch x steps of positions
+    uint32_t batch_share;                  // samples of a share: those of a unit have the same buckets
+    Div32 div_steps;
 };
 
 // The float32 distance of position p of sample b.  Every operation rounds by
@@ -51,28 +58,36 @@ __device__ __forceinline__ float distance_at(const BiasSource &s, uint32_t b, ui
     if (s.source == kFieldI32) return float(static_cast<const int32_t *>(s.field)[uint64_t(b) * s.positions + p]);
     uint32_t q = s.div_key.div(p), k = p - q * s.div_key.d;
     if (s.source == kOffset) return float(int32_t(k) - (int32_t(q) + s.offset[0]));
-    float term[kBiasMaxDim];
-    for (int a = s.ndim - 1; a >= 0; --a) {
-        const uint32_t q1 = s.div_q[a].div(q), k1 = s.div_k[a].div(k);
-        const int32_t delta = int32_t(k - k1 * s.div_k[a].d) - (int32_t(q - q1 * s.div_q[a].d) + s.offset[a]);
-        const float v = float(delta) * s.sampling[a];
-        term[a] = s.source == kEuclid ? v * v : fabsf(v);
-        q = q1;
-        k = k1;
+    float sum = 0.0f;
+    for (int a = 0; a < s.ndim; ++a) {
+        const uint32_t qa = s.div_q[a].div(q), ka = s.div_k[a].div(k);
+        q -= qa * s.div_q[a].d;
+        k -= ka * s.div_k[a].d;
+        const float v = float(int32_t(ka) - (int32_t(qa) + s.offset[a])) * s.sampling[a];
+        // the first term is added to 0, which changes nothing
+        if (s.source == kEuclid)
+            sum = sum + v * v;
+        else if (s.source == kTaxicab)
+            sum = sum + fabsf(v);
+        else
+            sum = fmaxf(sum, fabsf(v));
     }
-    float sum = term[0];
-    for (int a = 1; a < s.ndim; ++a) sum = s.source == kChess ? fmaxf(sum, term[a]) : sum + term[a];
     return s.source == kEuclid ? sqrtf(sum) : sum;
 }
 
-// Number of edges <= d: between 0 and buckets - 1 whatever the edges hold.
-__device__ __forceinline__ uint32_t bucket_of(const float *edges, uint32_t buckets, float d) {
-    uint32_t lo = 0, hi = buckets - 1;
-    while (lo < hi) {
-        const uint32_t mid = (lo + hi) >> 1;
-        if (edges[mid] <= d) lo = mid + 1; else hi = mid;
-    }
-    return lo;
+// Edges in LDS, padded with NaN to one less than a power of two: no distance
+// is at or past a NaN, so the count never leaves 0 .. buckets - 1, whatever the
+// edges hold.
+__device__ __forceinline__ void stage_edges(float *lds, const BiasSource &s, uint32_t threads) {
+    for (uint32_t i = threadIdx.x; i + 1 < s.span; i += threads)
+        lds[i] = i + 1 < s.buckets ? s.edges[i] : __uint_as_float(0x7fc00000u);
+}
+// Number of edges <= d, one bit of it a step.
+__device__ __forceinline__ uint32_t bucket_of(const float *lds, uint32_t span, float d) {
+    uint32_t k = 0;
+    for (uint32_t step = span >> 1; step; step >>= 1)
+        if (lds[k + step - 1] <= d) k += step;
+    return k;
 }
 
 __device__ __forceinline__ float table_at(const void *table, int32_t type, uint64_t i) {
@@ -86,38 +101,262 @@ __device__ __forceinline__ void table_put(void *table, int32_t type, uint64_t i,
     else static_cast<f16 *>(table)[i] = narrow<f16>(v);
 }
 
+// ---------------------------------------------------------------------------
+// Forward.  One thread owns V consecutive positions: it finds their buckets
+// once and writes every head and sample of its workgroup's share with them,
+// 16 bytes a store.  The table lies in LDS by bucket, four heads to a 16-byte
+// read, so a position's address serves all heads.  Bound by the bytes of add
+// and out.
+// ---------------------------------------------------------------------------
+constexpr int kBiasThreads = 256;
+
 template <typename T>
-__global__ void __launch_bounds__(256) k_bias(BiasArgs a) {
-    const uint32_t p = blockIdx.x * 256 + threadIdx.x;
-    if (p >= a.src.positions) return;
-    for (uint32_t b = 0; b < a.batch; ++b) {
-        const uint32_t k = bucket_of(a.src.edges, a.src.buckets, distance_at(a.src, b, p));
-        for (uint32_t h = 0; h < a.heads; ++h) {
-            const uint64_t at = (uint64_t(b) * a.heads + h) * a.src.positions + p;
-            float v = table_at(a.table, a.table_type, uint64_t(k) * a.heads + h);
-            if (a.add) v += widen(static_cast<const T *>(a.add)[at]);
-            static_cast<T *>(a.out)[at] = narrow<T>(v);
+__global__ void __launch_bounds__(kBiasThreads) k_bias(BiasArgs a) {
+    constexpr int V = 16 / sizeof(T);
+    extern __shared__ float lds[];
+    float *const table = lds;                              // [buckets][row], row = heads of the share, padded
+    float *const edges = lds + a.src.buckets * a.row;
+    const uint32_t share = blockIdx.y / a.batch_shares, bshare = blockIdx.y - share * a.batch_shares;
+    const uint32_t h0 = share * a.head_share, hn = min(a.head_share, a.heads - h0);
+    stage_edges(edges, a.src, kBiasThreads);
+    for (uint32_t i = threadIdx.x; i < a.src.buckets * a.row; i += kBiasThreads) {
+        const uint32_t k = i / a.row, h = i - k * a.row;
+        table[i] = h < hn ? table_at(a.table, a.table_type, uint64_t(k) * a.heads + h0 + h) : 0.0f;
+    }
+    __syncthreads();
+    // field: samples are blocks' own; relative: this share of the batch, all with the same buckets
+    const uint32_t fb = a.field_batch > 1 ? a.div_tiles.div(blockIdx.x) : 0;
+    const uint32_t p0 = ((blockIdx.x - fb * a.div_tiles.d) * kBiasThreads + threadIdx.x) * V;
+    if (p0 >= a.src.positions) return;
+    const uint32_t n = min(uint32_t(V), a.src.positions - p0);
+    uint32_t at[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+        at[j] = bucket_of(edges, a.src.span, distance_at(a.src, fb, min(p0 + j, a.src.positions - 1))) * a.row;
+    const uint32_t b0 = fb + bshare * a.batch_share;
+    const uint32_t b1 = a.field_batch > 1 ? fb + 1 : min(a.batch, b0 + a.batch_share);
+    for (uint32_t h = 0; h < hn; h += 4) {
+        float4 v[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[j] = *reinterpret_cast<const float4 *>(table + at[j] + h);
+        for (uint32_t b = b0; b < b1; ++b) {
+            const uint64_t row = (uint64_t(b) * a.heads + h0 + h) * a.src.positions + p0;
+            Pack<T, V> extra[4];
+            if (a.add) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (h + r < hn)
+                        extra[r] = load_pack<V>(static_cast<const T *>(a.add) + row + uint64_t(r) * a.src.positions, n, T{});
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                if (h + r >= hn) break;
+                Pack<T, V> out;
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    const float x = r == 0 ? v[j].x : r == 1 ? v[j].y : r == 2 ? v[j].z : v[j].w;
+                    out.v[j] = narrow<T>(a.add ? x + widen(extra[r].v[j]) : x);
+                }
+                store_pack<V>(static_cast<T *>(a.out) + row + uint64_t(r) * a.src.positions, out, n);
+            }
         }
     }
 }
 
-// One workgroup per bucket and head sums over every position.
-template <typename T>
-__global__ void __launch_bounds__(256) k_bias_grad(BiasGradArgs a) {
-    __shared__ float part[256];
-    const uint32_t k = blockIdx.x / a.heads, h = blockIdx.x - k * a.heads;
-    float sum = 0.0f;
-    for (uint32_t b = 0; b < a.batch; ++b)
-        for (uint32_t p = threadIdx.x; p < a.src.positions; p += 256)
-            if (bucket_of(a.src.edges, a.src.buckets, distance_at(a.src, b, p)) == k)
-                sum += widen(static_cast<const T *>(a.grad)[(uint64_t(b) * a.heads + h) * a.src.positions + p]);
-    part[threadIdx.x] = sum;
+// ---------------------------------------------------------------------------
+// Gradient of the table: out[k][h] = sum over positions of [bucket = k] g[h],
+// a matrix product with a matrix of ones and zeros.  A wave takes 16 heads and
+// 128 positions a step: every lane finds the buckets of two positions and
+// leaves them in LDS; the ones and zeros are made in registers as the first
+// operand of 16x16x32 products (16 buckets x 32 positions; a "one" is 2.0, a
+// single bit of either 16-bit format, and the sum is halved at the end) and
+// the gradients are the second, loaded as they lie: 8 consecutive positions of
+// a head are a lane's operand.  Sums are float32 in the accumulators, in an
+// order fixed by the sizes.  float32 gradients are cut into three bf16 pieces
+// of 8 bits, which lose nothing.
+//
+// Each workgroup leaves its sums in the workspace; k_bias_join adds them up.
+// Zero times an infinity or NaN spreads it over the buckets of its tile, so a
+// sum that is not finite is made once more there, from its own bucket alone.
+// ---------------------------------------------------------------------------
+constexpr int kGradThreads = 512;
+constexpr int kGradWaves = kGradThreads / kWave;
+constexpr uint32_t kGradStep = 128;                        // positions a wave takes at a time
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// Orders a wave's LDS writes and reads around it.
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// Two ones (0x4000) or zeros: is either half of w the bucket?
+__device__ __forceinline__ uint32_t match2(uint32_t w, uint32_t bucket2) {
+    const u16x2 x = __builtin_bit_cast(u16x2, w ^ bucket2);
+    const u16x2 one = {1, 1};
+    const u16x2 hit = __builtin_elementwise_sub_sat(one, x);
+    return __builtin_bit_cast(uint32_t, u16x2(hit << u16x2{14, 14}));
+}
+
+__device__ __forceinline__ f32x4 product(bf16, u32x4 a, u32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0,
+                                                   0, 0);
+}
+__device__ __forceinline__ f32x4 product(f16, u32x4 a, u32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0,
+                                                  0);
+}
+
+// One step of 128 positions, for the samples of one share of the batch.
+struct Unit {
+    uint32_t field, first, left;           // sample of the distances, first position, positions from there on
+    uint32_t b0, b1;
+};
+__device__ __forceinline__ Unit unit_at(const BiasGradArgs &a, uint32_t unit) {
+    Unit u;
+    const uint32_t share = a.div_steps.div(unit);
+    u.field = a.field_batch > 1 ? share : 0;
+    u.first = (unit - share * a.div_steps.d) * kGradStep;
+    u.left = a.src.positions - u.first;
+    u.b0 = share * a.batch_share;
+    u.b1 = min(a.batch, u.b0 + a.batch_share);
+    return u;
+}
+
+// Tiles: buckets / 16, rounded up to a power of two.
+template <typename T, int Tiles>
+__global__ void __launch_bounds__(kGradThreads) k_bias_grad(BiasGradArgs a) {
+    __shared__ float edges[kMaxBuckets];
+    __shared__ __align__(16) uint16_t ids[kGradWaves][kGradStep];
+    __shared__ float sums[Tiles * 16][16];
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint32_t col = lane & 15, group = lane >> 4;     // operand: row or column, block of 8 positions
+    const uint32_t h0 = blockIdx.y * 16, h = h0 + col;
+    stage_edges(edges, a.src, kGradThreads);
+    for (uint32_t i = threadIdx.x; i < Tiles * 256; i += kGradThreads) sums[i >> 4][i & 15] = 0.0f;
     __syncthreads();
-    for (uint32_t w = 128; w; w >>= 1) {
-        if (threadIdx.x < w) part[threadIdx.x] += part[threadIdx.x + w];
+    f32x4 acc[Tiles] = {};
+    const uint32_t splat = col * 0x10001u;
+    for (uint64_t at = uint64_t(blockIdx.x) * kGradWaves + wave; at < a.units; at += uint64_t(gridDim.x) * kGradWaves) {
+        const Unit u = unit_at(a, uint32_t(at));
+        const uint32_t left = u.left;
+        uint32_t here[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const uint32_t i = j * 64 + lane;
+            here[j] = i < left ? bucket_of(edges, a.src.span, distance_at(a.src, u.field, u.first + i)) : 0xffffu;
+            ids[wave][i] = uint16_t(here[j]);
+        }
+        wave_sync();
+        for (uint32_t b = u.b0; b < u.b1; ++b) {
+            const T *g = static_cast<const T *>(a.grad) + (uint64_t(b) * a.heads + h) * a.src.positions + u.first;
+            Pack<T, 8> x[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const uint32_t i = q * 32 + group * 8;
+                x[q] = {};
+                if (h < a.heads && i < left) x[q] = load_pack<8>(g + i, left - i, T{});
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                u32x4 w = *reinterpret_cast<const u32x4 *>(&ids[wave][q * 32 + group * 8]);
+                w ^= splat;
+                // few tiles: their ones are kept for the other samples; many would not fit the registers
+                if (Tiles > 2) asm volatile("" : "+v"(w));
+                u32x4 part[sizeof(T) == 4 ? 3 : 1];
+                if constexpr (sizeof(T) == 4) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        uint32_t cut[2][3];
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const float v = x[q].v[2 * j + e];
+                            cut[e][0] = __float_as_uint(v) & 0xffff0000u;
+                            const float r = v - __uint_as_float(cut[e][0]);
+                            cut[e][1] = __float_as_uint(r) & 0xffff0000u;
+                            cut[e][2] = __float_as_uint(r - __uint_as_float(cut[e][1]));
+                        }
+#pragma unroll
+                        for (int c = 0; c < 3; ++c) part[c][j] = __builtin_amdgcn_perm(cut[1][c], cut[0][c], 0x07060302u);
+                    }
+                } else {
+                    part[0] = __builtin_bit_cast(u32x4, x[q]);
+                }
+#pragma unroll
+                for (int t = 0; t < Tiles; ++t) {
+                    // tiles that hold none of these 64 positions' buckets are passed over
+                    if (Tiles > 2 && !__any((here[q >> 1] >> 4) == uint32_t(t))) continue;
+                    u32x4 one;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) one[j] = match2(w[j], t * 0x00100010u);
+                    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+                        for (int c = 0; c < 3; ++c) acc[t] = product(bf16{}, one, part[c], acc[t]);
+                    } else {
+                        acc[t] = product(T{}, one, part[0], acc[t]);
+                    }
+                }
+            }
+        }
+        wave_sync();
+    }
+    // lane holds rows group * 4 .. + 3 of column col of each tile; waves add in turn
+    for (uint32_t w = 0; w < kGradWaves; ++w) {
+        if (w == wave) {
+#pragma unroll
+            for (int t = 0; t < Tiles; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) sums[t * 16 + group * 4 + r][col] += 0.5f * acc[t][r];
+        }
         __syncthreads();
     }
-    if (threadIdx.x == 0) table_put(a.out, a.table_type, blockIdx.x, part[0]);
+    float *const out = a.partial + (uint64_t(blockIdx.x) * gridDim.y + blockIdx.y) * (Tiles * 256);
+    for (uint32_t i = threadIdx.x; i < Tiles * 256; i += kGradThreads) out[i] = sums[i >> 4][i & 15];
+}
+
+// One workgroup per bucket and 16 heads: thread (slice, head) adds every 16th
+// workgroup's sum, then the slices are added.
+template <typename T>
+__global__ void __launch_bounds__(256) k_bias_join(BiasGradArgs a) {
+    __shared__ float part[256];
+    __shared__ float edges[kMaxBuckets];
+    const uint32_t col = threadIdx.x & 15, slice = threadIdx.x >> 4;
+    const uint32_t k = blockIdx.x, h0 = blockIdx.y * 16;
+    const float *p = a.partial + (uint64_t(blockIdx.y) * a.tile_rows + k) * 16 + col;
+    float sum = 0.0f;
+    for (uint32_t w = slice; w < a.splits; w += 16) sum += p[uint64_t(w) * gridDim.y * a.tile_rows * 16];
+    part[threadIdx.x] = sum;
+    __syncthreads();
+    for (uint32_t w = 8; w; w >>= 1) {
+        if (slice < w) part[threadIdx.x] += part[threadIdx.x + 16 * w];
+        __syncthreads();
+    }
+    sum = part[col];
+    if (slice == 0 && h0 + col < a.heads) table_put(a.out, a.table_type, uint64_t(k) * a.heads + h0 + col, sum);
+    const uint64_t odd = __ballot(h0 + col < a.heads && !__builtin_isfinite(sum)) & 0xffff;
+    if (!odd) return;                                      // the same in every wave
+    stage_edges(edges, a.src, 256);
+    for (uint32_t i = 0; i < 16; ++i) {
+        if (!(odd >> i & 1)) continue;
+        __syncthreads();
+        sum = 0.0f;
+        for (uint32_t b = 0; b < a.batch; ++b)
+            for (uint64_t q = threadIdx.x; q < a.src.positions; q += 256)
+                if (bucket_of(edges, a.src.span, distance_at(a.src, b, uint32_t(q))) == k)
+                    sum += widen(static_cast<const T *>(a.grad)[(uint64_t(b) * a.heads + h0 + i) * a.src.positions + q]);
+        part[threadIdx.x] = sum;
+        __syncthreads();
+        for (uint32_t w = 128; w; w >>= 1) {
+            if (threadIdx.x < w) part[threadIdx.x] += part[threadIdx.x + w];
+            __syncthreads();
+        }
+        if (threadIdx.x == 0) table_put(a.out, a.table_type, uint64_t(k) * a.heads + h0 + i, part[0]);
+    }
 }
 
 }  // namespace tmtrain

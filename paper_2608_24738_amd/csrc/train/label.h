@@ -1,13 +1,15 @@
-// label.h -- log-probabilities of given labels, with the entropy, the expected
-// field and the likeliest classes, and their gradient (include/tm_train.h).
+// label.h -- what the kernels of the label log-probabilities share: arguments,
+// the arithmetic of a running softmax, keys of the likeliest classes
+// (include/tm_train.h).  label_maps.h has the kernels of class axes that lie
+// apart, label_rows.h those of contiguous rows.
 //
 // With m the largest logit, d_c = x_c - m, e_c = exp d_c and s = sum e_c:
 //     l_c = d_c - log s,   entropy = log s - (sum e_c d_c) / s,
 //     mean = (sum e_c field_c) / s.
 // d and log s are kept apart: their difference loses nothing of a large m.
-// m starts at the lowest finite float instead of -inf, so that d is never
-// inf - inf: classes at -inf get e = 0, and s = 0 marks a position with no
-// class left.
+// m runs: where it grows, the sums so far shrink by exp(old - new).  It starts
+// at the lowest finite float instead of -inf, so that d is never inf - inf:
+// classes at -inf get e = 0, and s = 0 marks a position with no class left.
 #pragma once
 
 #include "train_common.h"
@@ -21,10 +23,14 @@ struct LabelArgs {
     float *logp, *entropy, *mean, *top, *stats;
     int32_t *index;
     int64_t xs[3], fs[3];       // strides of logits and field: outer, class, inner
+    int64_t ts[3];              // strides of top and index: outer, rank, inner
     uint32_t outer, classes, inner, k;
     int32_t label_bytes;        // 1 (unsigned), 4 or 8
     uint32_t n;                 // outer * inner
+    uint32_t groups;            // maps: threads along the inner positions; rows: workgroups of a row
+    Div32 div_groups;
     Div32 div_inner;
+    void *partial;              // rows: what the workgroups of a row found
 };
 
 struct LabelGradArgs {
@@ -38,6 +44,9 @@ struct LabelGradArgs {
     uint32_t outer, classes, inner;
     int32_t label_bytes;
     uint32_t n;
+    uint32_t groups;
+    uint32_t share;             // classes of a workgroup
+    Div32 div_groups;
     Div32 div_inner;
 };
 
@@ -67,102 +76,105 @@ __device__ __forceinline__ float unordered(uint32_t o) {
 // Larger logits first, equal ones by rising class; 0 is below every class.
 __device__ __forceinline__ uint64_t top_key(float x, uint32_t c) { return uint64_t(ordered(x)) << 32 | ~c; }
 
-struct Sums {
-    float m, s, t, f;           // maximum, sum e, sum e d, sum e field
-};
-
-template <typename T>
-__device__ Sums position_sums(const T *x, int64_t xs, const float *field, int64_t fs, uint32_t classes) {
-    Sums r{-FLT_MAX, 0.0f, 0.0f, 0.0f};
-    for (uint32_t c = 0; c < classes; ++c) r.m = fmaxf(r.m, widen(x[c * xs]));
-    // sums of 256 classes at a time: the error of one long chain would grow with
-    // the number of classes
-    for (uint32_t first = 0; first < classes; first += 256) {
-        float s = 0.0f, t = 0.0f, f = 0.0f;
-        for (uint32_t c = first; c < min(classes, first + 256); ++c) {
-            const float d = widen(x[c * xs]) - r.m;
-            const float e = exp2_hw(d * kLog2e);
-            s += e;
-            t += e == 0.0f ? 0.0f : e * d;
-            if (field) f += e == 0.0f ? 0.0f : e * field[c * fs];
-        }
-        r.s += s;
-        r.t += t;
-        r.f += f;
-    }
+// V elements `stride` apart, the first n of them.
+template <int V>
+__device__ __forceinline__ Pack<float, V> load_field(const float *p, int64_t stride, uint32_t n) {
+    if (V == 1 || stride == 1) return load_pack<V>(p, n, 0.0f);
+    Pack<float, V> r;
+#pragma unroll
+    for (int j = 0; j < V; ++j) r.v[j] = uint32_t(j) < n ? p[j * stride] : 0.0f;
     return r;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(256) k_label_logp(LabelArgs a) {
-    const uint32_t n = blockIdx.x * 256 + threadIdx.x;
-    if (n >= a.n) return;
-    const uint32_t o = a.div_inner.div(n), i = n - o * a.inner;
-    const T *x = static_cast<const T *>(a.x) + o * a.xs[0] + i * a.xs[2];
-    const float *field = a.field ? a.field + o * a.fs[0] + i * a.fs[2] : nullptr;
-    const Sums r = position_sums(x, a.xs[1], field, a.fs[1], a.classes);
-    const bool dead = r.s == 0.0f;
-    const float logs = logf(r.s);
-    if (a.logp) {
-        const int32_t y = load_label(a.label, a.label_bytes, n, a.classes);
-        a.logp[n] = y < 0 ? 0.0f : dead ? -INFINITY : widen(x[y * a.xs[1]]) - r.m - logs;
-    }
-    if (a.entropy) a.entropy[n] = dead ? 0.0f : logs - r.t / r.s;
-    if (a.mean) a.mean[n] = dead ? 0.0f : r.f / r.s;
-    if (a.stats) {
-        a.stats[2 * uint64_t(n)] = r.m;
-        a.stats[2 * uint64_t(n) + 1] = dead ? INFINITY : logs;
-    }
-    uint64_t floor = ~uint64_t(0);
-    for (uint32_t j = 0; j < a.k; ++j) {
-        uint64_t best = 0;
-        for (uint32_t c = 0; c < a.classes; ++c) {
-            const uint64_t key = top_key(widen(x[c * a.xs[1]]), c);
-            if (key < floor && key > best) best = key;
-        }
-        const uint64_t at = (uint64_t(o) * a.k + j) * a.inner + i;
-        a.index[at] = int32_t(~uint32_t(best));
-        a.top[at] = dead ? -INFINITY : unordered(best >> 32) - r.m - logs;
-        floor = best;
-    }
+struct Sums {
+    float m, s, t, f;           // maximum, sum e, sum e d, sum e field
+};
+constexpr Sums kNothing = {-FLT_MAX, 0.0f, 0.0f, 0.0f};
+
+// d = x - m, not below -200: exp -200 is 0 in float32, and the products with d
+// stay finite.  A NaN stays one.
+__device__ __forceinline__ float below(float x, float m) {
+    const float d = x - m;
+    return d < -200.0f ? -200.0f : d;
 }
 
+// exp d for the sums of type T.  The rounding of d log2(e) is an error of up to
+// 2^-24 |d|; float32 logits take it back to first order, 16-bit ones are
+// rounded to 2^-9 themselves.
 template <typename T>
-__global__ void __launch_bounds__(256) k_label_logp_grad(LabelGradArgs a) {
-    const uint32_t n = blockIdx.x * 256 + threadIdx.x;
-    if (n >= a.n) return;
-    const uint32_t o = a.div_inner.div(n), i = n - o * a.inner;
-    const T *x = static_cast<const T *>(a.x) + o * a.xs[0] + i * a.xs[2];
-    const float *field = a.field ? a.field + o * a.fs[0] + i * a.fs[2] : nullptr;
-    T *g = static_cast<T *>(a.grad) + o * a.gs[0] + i * a.gs[2];
+__device__ __forceinline__ float exp_of(float d) {
+    const float z = d * kLog2e;
+    const float e = exp2_hw(z);
+    if constexpr (sizeof(T) == 4) return fmaf(e, fmaf(d, kLog2e, -z) * kLn2, e);
+    return e;
+}
+
+// The sums seen from a larger maximum.
+__device__ __forceinline__ void lift(Sums &r, float m) {
+    const float d = below(r.m, m);
+    const float e = exp_of<float>(d);
+    r.t = e * fmaf(d, r.s, r.t);
+    r.s *= e;
+    r.f *= e;
+    r.m = m;
+}
+__device__ __forceinline__ Sums join(Sums a, Sums b) {
+    const float m = fmaxf(a.m, b.m);
+    lift(a, m);
+    lift(b, m);
+    return {m, a.s + b.s, a.t + b.t, a.f + b.f};
+}
+
+// One class more; field is read only if it is there.
+template <typename T>
+__device__ __forceinline__ void take(Sums &r, float x, bool entropy) {
+    const float d = below(x, r.m);
+    const float e = exp_of<T>(d);
+    r.s += e;
+    if (entropy) r.t = fmaf(e, d, r.t);
+}
+template <typename T>
+__device__ __forceinline__ void take(Sums &r, float x, bool entropy, float field) {
+    const float d = below(x, r.m);
+    const float e = exp_of<T>(d);
+    r.s += e;
+    if (entropy) r.t = fmaf(e, d, r.t);
+    r.f = fmaf(e, e == 0.0f ? 0.0f : field, r.f);
+}
+
+// What a position's sums say.
+struct Found {
     float m, logs, entropy, mean;
-    if (a.stats) {
-        m = a.stats[2 * uint64_t(n)];
-        logs = a.stats[2 * uint64_t(n) + 1];
-        entropy = a.up_entropy ? a.entropy[n] : 0.0f;
-        mean = a.up_mean ? a.mean[n] : 0.0f;
-    } else {
-        const Sums r = position_sums(x, a.xs[1], field, a.fs[1], a.classes);
-        m = r.m;
-        logs = r.s == 0.0f ? INFINITY : logf(r.s);
-        entropy = logs - r.t / r.s;
-        mean = r.f / r.s;
-    }
-    const bool dead = logs == INFINITY;
-    const int32_t y = a.up_logp ? load_label(a.label, a.label_bytes, n, a.classes) : -1;
-    const float ua = y < 0 || dead ? 0.0f : a.up_logp[n];
-    const float uh = a.up_entropy ? a.up_entropy[n] : 0.0f;
-    const float uf = a.up_mean ? a.up_mean[n] : 0.0f;
-    for (uint32_t c = 0; c < a.classes; ++c) {
-        const float l = widen(x[c * a.xs[1]]) - m - logs;
-        const float p = exp2_hw(l * kLog2e);
-        float slope = -ua;
-        if (a.up_entropy) slope -= uh * (l + entropy);
-        if (a.up_mean) slope += uf * (field[c * a.fs[1]] - mean);
-        float v = p == 0.0f ? 0.0f : p * slope;
-        if (int32_t(c) == y) v += ua;
-        g[c * a.gs[1]] = narrow<T>(v);
-    }
+    bool dead;                  // every class at -inf
+};
+__device__ __forceinline__ Found found(const Sums &r) {
+    Found q;
+    q.dead = r.s == 0.0f;
+    q.m = r.m;
+    q.logs = logf(r.s);
+    q.entropy = q.dead ? 0.0f : q.logs - r.t / r.s;
+    q.mean = q.dead ? 0.0f : r.f / r.s;
+    return q;
+}
+__device__ __forceinline__ float log_prob(const Found &q, float x) {
+    return q.dead ? -INFINITY : (x - q.m) - q.logs;
+}
+// As tm_label_logp_grad reads it: probabilities of a dead position become 0.
+__device__ __forceinline__ float stats_logs(const Found &q) { return q.dead ? INFINITY : q.logs; }
+
+// The gradient of one class: p (f (field - mean) - a - h (l + entropy)) and a more for the label's.
+struct Slope {
+    float m, logs, a, h, f, entropy, mean;
+};
+template <typename T, bool F>
+__device__ __forceinline__ float slope_of(const Slope &g, bool entropy, float x, float field) {
+    // x - m - log s; a dead position has log s = inf and so p = 0
+    const float l = below(x - g.m, g.logs);
+    const float p = exp_of<T>(l);
+    float v = -g.a;
+    if (entropy) v -= g.h * (l + g.entropy);
+    if constexpr (F) v += g.f * (field - g.mean);
+    return p == 0.0f ? 0.0f : p * v;
 }
 
 }  // namespace tmtrain

@@ -1,0 +1,472 @@
+// label_maps.h -- label log-probabilities where the classes of a position lie
+// apart and neighbouring positions side by side, as in (B, C, *spatial).
+//
+// A thread owns V neighbouring positions (16 bytes of logits of one class), so
+// a wave reads whole lines of every class plane.  Few classes are held in
+// registers between the passes for the maximum, the sums and the likeliest
+// classes (k_label_held): every logit is read once.  More run through in
+// blocks of 8 with a running maximum (k_label_run); where there are few
+// positions, the waves of a workgroup share the classes and join their sums.
+// Both are bound by the bytes of logits, labels and outputs.  Class axes of
+// any stride take the same kernels with one position to a thread.
+#pragma once
+
+#include "label.h"
+
+namespace tmtrain {
+
+template <int V, typename L>
+__device__ __forceinline__ void load_labels_as(const L *p, uint32_t n, uint32_t classes, int32_t (&y)[V]) {
+    const Pack<L, V> r = load_pack<V>(p, n, L(0));
+#pragma unroll
+    for (int j = 0; j < V; ++j) y[j] = int64_t(r.v[j]) >= 0 && int64_t(r.v[j]) < int64_t(classes) ? int32_t(r.v[j]) : -1;
+}
+template <int V>
+__device__ __forceinline__ void load_labels(const void *p, int32_t bytes, uint64_t i, uint32_t n, uint32_t classes,
+                                            int32_t (&y)[V]) {
+    if (bytes == 1)
+        load_labels_as<V>(static_cast<const uint8_t *>(p) + i, n, classes, y);
+    else if (bytes == 4)
+        load_labels_as<V>(static_cast<const int32_t *>(p) + i, n, classes, y);
+    else
+        load_labels_as<V>(static_cast<const int64_t *>(p) + i, n, classes, y);
+}
+
+// Where a thread's positions lie.
+template <int V>
+struct Place {
+    uint32_t o, i, n;           // outer, first inner position, positions
+    uint64_t at;                // in [outer][inner]
+};
+template <int V, typename Args>
+__device__ __forceinline__ Place<V> place(const Args &a, uint32_t thread) {
+    Place<V> r;
+    r.o = a.div_groups.div(thread);
+    r.i = (thread - r.o * a.groups) * V;
+    r.n = min(uint32_t(V), a.inner - r.i);
+    r.at = uint64_t(r.o) * a.inner + r.i;
+    return r;
+}
+
+// The class below `last` (in the order of the alternatives) that is largest:
+// one step of a selection over the classes, in rising number.
+struct Pick {
+    float x;
+    int32_t c;
+};
+constexpr Pick kNoPick = {0.0f, -1};
+// NaN counts as below -inf here: larger(a, b) for the order of the alternatives
+__device__ __forceinline__ bool larger(float a, float b) { return a > b || (b != b && a == a); }
+__device__ __forceinline__ void consider(Pick &best, const Pick &last, float x, int32_t c) {
+    const bool open = last.c < 0 || larger(last.x, x) || (!larger(x, last.x) && c > last.c);
+    if (open && (best.c < 0 || larger(x, best.x))) best = {x, c};
+}
+
+template <int V>
+__device__ __forceinline__ void put_top(const LabelArgs &a, const Place<V> &w, uint32_t rank, const Pick (&best)[V],
+                                        const Found (&q)[V]) {
+    const int64_t at = w.o * a.ts[0] + rank * a.ts[1] + w.i * a.ts[2];
+    Pack<float, V> top;
+    Pack<int32_t, V> index;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        top.v[j] = log_prob(q[j], best[j].x);
+        index.v[j] = best[j].c;
+    }
+    if (V == 1 || a.ts[2] == 1) {
+        store_pack<V>(a.top + at, top, w.n);
+        store_pack<V>(a.index + at, index, w.n);
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            if (uint32_t(j) < w.n) {
+                a.top[at + j * a.ts[2]] = top.v[j];
+                a.index[at + j * a.ts[2]] = index.v[j];
+            }
+    }
+}
+
+// Log-probability (xl: the labels' logits), entropy, mean, statistics.
+template <int V>
+__device__ __forceinline__ void put_found(const LabelArgs &a, const Place<V> &w, const int32_t (&y)[V],
+                                          const float (&xl)[V], const Found (&q)[V]) {
+    Pack<float, V> r;
+    if (a.logp) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) r.v[j] = y[j] < 0 ? 0.0f : log_prob(q[j], xl[j]);
+        store_pack<V>(a.logp + w.at, r, w.n);
+    }
+    if (a.entropy) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) r.v[j] = q[j].entropy;
+        store_pack<V>(a.entropy + w.at, r, w.n);
+    }
+    if (a.mean) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) r.v[j] = q[j].mean;
+        store_pack<V>(a.mean + w.at, r, w.n);
+    }
+    if (a.stats) {
+        Pack<float, 2 * V> st;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            st.v[2 * j] = q[j].m;
+            st.v[2 * j + 1] = stats_logs(q[j]);
+        }
+        store_pack<2 * V>(a.stats + 2 * w.at, st, 2 * w.n);
+    }
+}
+
+// At most C classes, held in registers.
+template <typename T, int V, int C>
+__global__ void __launch_bounds__(256) k_label_held(LabelArgs a) {
+    const uint32_t thread = blockIdx.x * 256 + threadIdx.x;
+    if (thread >= a.outer * a.groups) return;
+    const Place<V> w = place<V>(a, thread);
+    const T *x = static_cast<const T *>(a.x) + w.o * a.xs[0] + w.i * a.xs[2];
+    Pack<T, V> held[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+        if (uint32_t(c) < a.classes) held[c] = load_pack<V>(x + c * a.xs[1], w.n, T{});
+    int32_t y[V];
+    if (a.logp) load_labels<V>(a.label, a.label_bytes, w.at, w.n, a.classes, y);
+    Sums r[V];
+    float xl[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        r[j] = kNothing;
+        xl[j] = 0.0f;
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+        if (uint32_t(c) < a.classes) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) r[j].m = fmaxf(r[j].m, widen(held[c].v[j]));
+        }
+    if (a.mean) {
+        const float *field = a.field + w.o * a.fs[0] + w.i * a.fs[2];
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+            if (uint32_t(c) < a.classes) {
+                const Pack<float, V> phi = load_field<V>(field + c * a.fs[1], a.fs[2], w.n);
+#pragma unroll
+                for (int j = 0; j < V; ++j) take<T>(r[j], widen(held[c].v[j]), a.entropy, phi.v[j]);
+            }
+    } else {
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+            if (uint32_t(c) < a.classes) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) take<T>(r[j], widen(held[c].v[j]), a.entropy);
+            }
+    }
+    Found q[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) q[j] = found(r[j]);
+    if (a.logp) {
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                if (y[j] == c) xl[j] = widen(held[c].v[j]);
+    }
+    put_found<V>(a, w, y, xl, q);
+    Pick last[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) last[j] = kNoPick;
+    for (uint32_t rank = 0; rank < a.k; ++rank) {
+        Pick best[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) best[j] = kNoPick;
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+            if (uint32_t(c) < a.classes) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) consider(best[j], last[j], widen(held[c].v[j]), c);
+            }
+        put_top<V>(a, w, rank, best, q);
+#pragma unroll
+        for (int j = 0; j < V; ++j) last[j] = best[j];
+    }
+}
+
+// Any number of classes, shared by the waves of a workgroup.
+constexpr int kRunBlock = 8;                               // classes loaded at once
+constexpr int kRunWaves = 8;                               // at most
+
+template <typename T, int V>
+__global__ void __launch_bounds__(64 * kRunWaves) k_label_run(LabelArgs a) {
+    extern __shared__ float shared[];                      // [waves][V][4][64] sums, or [waves][V][2][64] picks
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    const uint32_t threads = a.outer * a.groups;
+    const uint32_t thread = min(blockIdx.x * 64 + lane, threads - 1);
+    const bool mine = blockIdx.x * 64 + lane < threads && wave == 0;   // writes the results
+    const Place<V> w = place<V>(a, thread);
+    const T *x = static_cast<const T *>(a.x) + w.o * a.xs[0] + w.i * a.xs[2];
+    const float *field = a.mean ? a.field + w.o * a.fs[0] + w.i * a.fs[2] : nullptr;
+    const uint32_t share = (a.classes + waves - 1) / waves;
+    const uint32_t c0 = min(a.classes, wave * share), c1 = min(a.classes, c0 + share);
+    Sums r[V];
+    Pick best[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        r[j] = kNothing;
+        best[j] = kNoPick;
+    }
+    for (uint32_t c = c0; c < c1; c += kRunBlock) {
+        Pack<T, V> held[kRunBlock];
+#pragma unroll
+        for (int u = 0; u < kRunBlock; ++u)
+            if (c + u < c1) held[u] = load_pack<V>(x + (c + u) * a.xs[1], w.n, T{});
+        Sums part[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            float m = r[j].m;
+#pragma unroll
+            for (int u = 0; u < kRunBlock; ++u)
+                if (c + u < c1) m = fmaxf(m, widen(held[u].v[j]));
+            lift(r[j], m);
+            part[j] = {m, 0.0f, 0.0f, 0.0f};
+        }
+#pragma unroll
+        for (int u = 0; u < kRunBlock; ++u)
+            if (c + u < c1) {
+                if (field) {
+                    const Pack<float, V> phi = load_field<V>(field + (c + u) * a.fs[1], a.fs[2], w.n);
+#pragma unroll
+                    for (int j = 0; j < V; ++j) take<T>(part[j], widen(held[u].v[j]), a.entropy, phi.v[j]);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < V; ++j) take<T>(part[j], widen(held[u].v[j]), a.entropy);
+                }
+            }
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            r[j].s += part[j].s;
+            r[j].t += part[j].t;
+            r[j].f += part[j].f;
+        }
+        if (a.k) {
+#pragma unroll
+            for (int u = 0; u < kRunBlock; ++u)
+                if (c + u < c1) {
+#pragma unroll
+                    for (int j = 0; j < V; ++j)
+                        if (best[j].c < 0 || larger(widen(held[u].v[j]), best[j].x))
+                            best[j] = {widen(held[u].v[j]), int32_t(c + u)};
+                }
+        }
+    }
+    if (waves > 1) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            float *p = shared + ((wave * V + j) * 4) * 64 + lane;
+            p[0] = r[j].m;
+            p[64] = r[j].s;
+            p[128] = r[j].t;
+            p[192] = r[j].f;
+        }
+        __syncthreads();
+        // every wave joins them all, in the same order
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            Sums all = kNothing;
+            for (uint32_t v = 0; v < waves; ++v) {
+                const float *p = shared + ((v * V + j) * 4) * 64 + lane;
+                all = join(all, Sums{p[0], p[64], p[128], p[192]});
+            }
+            r[j] = all;
+        }
+        __syncthreads();
+    }
+    Found q[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) q[j] = found(r[j]);
+    if (mine) {
+        int32_t y[V];
+        float xl[V];
+        if (a.logp) {
+            load_labels<V>(a.label, a.label_bytes, w.at, w.n, a.classes, y);
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                xl[j] = uint32_t(j) < w.n && y[j] >= 0 ? widen(x[y[j] * a.xs[1] + j * a.xs[2]]) : 0.0f;
+        }
+        put_found<V>(a, w, y, xl, q);
+    }
+    Pick last[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) last[j] = kNoPick;
+    for (uint32_t rank = 0; rank < a.k; ++rank) {
+        if (rank) {
+            // the first was found on the way; each other one is a pass over the classes
+#pragma unroll
+            for (int j = 0; j < V; ++j) best[j] = kNoPick;
+            for (uint32_t c = c0; c < c1; ++c) {
+                const Pack<T, V> one = load_pack<V>(x + c * a.xs[1], w.n, T{});
+#pragma unroll
+                for (int j = 0; j < V; ++j) consider(best[j], last[j], widen(one.v[j]), int32_t(c));
+            }
+        }
+        if (waves > 1) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                float *p = shared + ((wave * V + j) * 2) * 64 + lane;
+                p[0] = best[j].x;
+                p[64] = __int_as_float(best[j].c);
+            }
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                best[j] = kNoPick;
+                // shares of classes in rising number: of equal ones the first stays
+                for (uint32_t v = 0; v < waves; ++v) {
+                    const float *p = shared + ((v * V + j) * 2) * 64 + lane;
+                    const int32_t c = __float_as_int(p[64]);
+                    if (c >= 0 && (best[j].c < 0 || larger(p[0], best[j].x))) best[j] = {p[0], c};
+                }
+            }
+            __syncthreads();
+        }
+        if (mine) put_top<V>(a, w, rank, best, q);
+#pragma unroll
+        for (int j = 0; j < V; ++j) last[j] = best[j];
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Gradient.
+// ---------------------------------------------------------------------------
+template <int V>
+__device__ __forceinline__ void load_upstream(const LabelGradArgs &a, const Place<V> &w, int32_t (&y)[V],
+                                              Slope (&g)[V]) {
+    if (a.up_logp) load_labels<V>(a.label, a.label_bytes, w.at, w.n, a.classes, y);
+    Pack<float, V> ua{}, uh{}, uf{};
+    if (a.up_logp) ua = load_pack<V>(a.up_logp + w.at, w.n, 0.0f);
+    if (a.up_entropy) uh = load_pack<V>(a.up_entropy + w.at, w.n, 0.0f);
+    if (a.up_mean) uf = load_pack<V>(a.up_mean + w.at, w.n, 0.0f);
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        if (!a.up_logp) y[j] = -1;
+        g[j].a = y[j] < 0 || g[j].logs == INFINITY ? 0.0f : ua.v[j];
+        g[j].h = uh.v[j];
+        g[j].f = uf.v[j];
+    }
+}
+
+// One class of V positions.
+template <typename T, int V, bool F>
+__device__ __forceinline__ void put_slope(const LabelGradArgs &a, const Place<V> &w, uint32_t c, const Pack<T, V> &x,
+                                          const Pack<float, V> &phi, const int32_t (&y)[V], const Slope (&g)[V]) {
+    T *out = static_cast<T *>(a.grad) + w.o * a.gs[0] + c * a.gs[1] + w.i * a.gs[2];
+    Pack<T, V> r;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        const float v = slope_of<T, F>(g[j], a.up_entropy, widen(x.v[j]), F ? phi.v[j] : 0.0f);
+        r.v[j] = narrow<T>(y[j] == int32_t(c) ? v + g[j].a : v);
+    }
+    if (V == 1 || a.gs[2] == 1) {
+        store_pack<V>(out, r, w.n);
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            if (uint32_t(j) < w.n) out[j * a.gs[2]] = r.v[j];
+    }
+}
+
+// At most C classes: the sums are made anew, which reads nothing but the
+// logits that the gradient needs anyway.
+template <typename T, int V, int C, bool F>
+__global__ void __launch_bounds__(256) k_label_grad_held(LabelGradArgs a) {
+    const uint32_t thread = blockIdx.x * 256 + threadIdx.x;
+    if (thread >= a.outer * a.groups) return;
+    const Place<V> w = place<V>(a, thread);
+    const T *x = static_cast<const T *>(a.x) + w.o * a.xs[0] + w.i * a.xs[2];
+    Pack<T, V> held[C];
+    constexpr bool Keep = F && C * V <= 64;                // the field too, or read it twice
+    Pack<float, V> phi[Keep ? C : 1];
+    const float *const field = F ? a.field + w.o * a.fs[0] + w.i * a.fs[2] : nullptr;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+        if (uint32_t(c) < a.classes) {
+            held[c] = load_pack<V>(x + c * a.xs[1], w.n, T{});
+            if constexpr (Keep) phi[c] = load_field<V>(field + c * a.fs[1], a.fs[2], w.n);
+        }
+    Sums r[V];
+    Slope g[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) r[j] = kNothing;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+        if (uint32_t(c) < a.classes) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) r[j].m = fmaxf(r[j].m, widen(held[c].v[j]));
+        }
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+        if (uint32_t(c) < a.classes) {
+            if constexpr (F && !Keep) phi[0] = load_field<V>(field + c * a.fs[1], a.fs[2], w.n);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                if constexpr (F) take<T>(r[j], widen(held[c].v[j]), a.up_entropy, phi[Keep ? c : 0].v[j]);
+                else take<T>(r[j], widen(held[c].v[j]), a.up_entropy);
+            }
+        }
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        const Found q = found(r[j]);
+        g[j].m = q.m;
+        g[j].logs = stats_logs(q);
+        g[j].entropy = q.entropy;
+        g[j].mean = q.mean;
+    }
+    int32_t y[V];
+    load_upstream<V>(a, w, y, g);
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+        if (uint32_t(c) < a.classes) {
+            if constexpr (F && !Keep) phi[0] = load_field<V>(field + c * a.fs[1], a.fs[2], w.n);
+            put_slope<T, V, F>(a, w, c, held[c], phi[Keep ? c : 0], y, g);
+        }
+}
+
+// Any number of classes, with the forward call's statistics; blockIdx.y takes
+// a share of the classes.
+template <typename T, int V, bool F>
+__global__ void __launch_bounds__(256) k_label_grad_run(LabelGradArgs a) {
+    const uint32_t thread = blockIdx.x * 256 + threadIdx.x;
+    if (thread >= a.outer * a.groups) return;
+    const Place<V> w = place<V>(a, thread);
+    const T *x = static_cast<const T *>(a.x) + w.o * a.xs[0] + w.i * a.xs[2];
+    const uint32_t c0 = blockIdx.y * a.share, c1 = min(a.classes, c0 + a.share);
+    Slope g[V];
+    const Pack<float, 2 * V> st = load_pack<2 * V>(a.stats + 2 * w.at, 2 * w.n, 0.0f);
+    Pack<float, V> entropy{}, mean{};
+    if (a.up_entropy) entropy = load_pack<V>(a.entropy + w.at, w.n, 0.0f);
+    if constexpr (F) mean = load_pack<V>(a.mean + w.at, w.n, 0.0f);
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        g[j].m = st.v[2 * j];
+        g[j].logs = st.v[2 * j + 1];
+        g[j].entropy = entropy.v[j];
+        g[j].mean = mean.v[j];
+    }
+    int32_t y[V];
+    load_upstream<V>(a, w, y, g);
+    for (uint32_t c = c0; c < c1; c += 4) {
+        Pack<T, V> held[4];
+        Pack<float, V> phi[F ? 4 : 1];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (c + u < c1) {
+                held[u] = load_pack<V>(x + (c + u) * a.xs[1], w.n, T{});
+                if constexpr (F)
+                    phi[u] = load_field<V>(a.field + w.o * a.fs[0] + (c + u) * a.fs[1] + w.i * a.fs[2], a.fs[2],
+                                              w.n);
+            }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (c + u < c1) put_slope<T, V, F>(a, w, c + u, held[u], phi[F ? u : 0], y, g);
+    }
+}
+
+}  // namespace tmtrain

@@ -3,11 +3,13 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "../../../include/tm_train.h"
 #include "bias.h"
-#include "label.h"
+#include "label_maps.h"
+#include "label_rows.h"
 
 using namespace tmtrain;
 
@@ -17,6 +19,15 @@ constexpr uint64_t kLimit = uint64_t(1) << 31;
 
 bool float_type(int dtype) { return dtype == TM_DTYPE_F32 || dtype == TM_DTYPE_F16 || dtype == TM_DTYPE_BF16; }
 uint64_t float_bytes(int dtype) { return dtype == TM_DTYPE_F32 ? 4 : 2; }
+
+constexpr uint64_t kFill = 1024;            // workgroups that keep the chip busy
+
+uint32_t pow2_from(uint32_t n) {
+    uint32_t p = 1;
+    while (p < n) p <<= 1;
+    return p;
+}
+uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 
 struct Range {
     const void *at;
@@ -40,8 +51,8 @@ bool aliased(const Range (&in)[NI], const Range (&out)[NO]) {
 }
 
 template <typename Args>
-int launch(void (*kernel)(Args), dim3 grid, dim3 block, hipStream_t s, const Args &args) {
-    hipLaunchKernelGGL(kernel, grid, block, 0, s, args);
+int launch(void (*kernel)(Args), dim3 grid, dim3 block, size_t lds, hipStream_t s, const Args &args) {
+    hipLaunchKernelGGL(kernel, grid, block, lds, s, args);
     return hipGetLastError() == hipSuccess ? TM_OK : TM_ERR_HIP;
 }
 
@@ -119,9 +130,62 @@ int check_labels(const void *logits, int dtype, int64_t outer, int64_t classes, 
     return TM_OK;
 }
 
+constexpr uint64_t kBusyThreads = 65536;    // four waves to a SIMD
+
+// How a request runs: on contiguous rows or on maps, with how many classes
+// held, positions to a thread and waves to a row or position.
+struct LabelPlan {
+    bool rows;
+    bool swap;                  // maps: the outer positions lie side by side, not the inner ones
+    bool wide;                  // maps: 16 bytes of positions to a thread
+    int held;                   // maps: classes held in registers, 0: they run through
+    uint32_t waves;             // of a row, or sharing the classes of a map's positions
+    uint32_t parts;             // of a row
+};
+
+// Rows from 33 classes on: a lane of a wave has at most one load of a shorter
+// one, and a thread to a row holds it whole.
+LabelPlan label_plan(int dtype, uint64_t outer, uint64_t classes, uint64_t inner, const int64_t *strides) {
+    LabelPlan p{};
+    const uint64_t n = outer * inner, vec = 16 / float_bytes(dtype);
+    p.parts = 1;
+    if ((strides[1] == 1 || classes == 1) && classes > 32) {
+        p.rows = true;
+        // one wave while its lanes' first loads hold the row, then 4, then 16
+        p.waves = classes <= 64 * vec * kRowLoads ? 1 : classes <= 64 * 4 * vec * 2 * kRowLoads ? 4 : 16;
+        if (p.waves == 16 && n < 512)
+            p.parts = uint32_t(std::min<uint64_t>({kRowMostParts, ceil_div(classes, 64 * 16 * vec), ceil_div(512, n)}));
+        return p;
+    }
+    p.swap = inner == 1 && outer > 1 && strides[0] == 1;
+    const uint64_t in = p.swap ? outer : inner, out = p.swap ? 1 : outer;
+    const int64_t step = p.swap ? strides[0] : strides[2];
+    p.wide = step == 1 && out * ceil_div(in, vec) >= kBusyThreads / 2;
+    p.held = classes <= 4 ? 4 : classes <= 8 ? 8 : classes <= 16 ? 16 : 0;
+    const uint64_t threads = p.wide ? out * ceil_div(in, vec) : n;
+    p.waves = uint32_t(std::max<uint64_t>(1, std::min<uint64_t>({kRunWaves, kBusyThreads / threads, classes / 16})));
+    return p;
+}
+
+template <typename Args>
+void swap_positions(Args &a) {
+    a.inner = a.outer;
+    a.outer = 1;
+    std::swap(a.xs[0], a.xs[2]);
+    std::swap(a.fs[0], a.fs[2]);
+}
+
 }  // namespace
 
-extern "C" size_t tm_label_logp_workspace_size(int, int64_t, int64_t, int64_t, const int64_t *, int) { return 0; }
+extern "C" size_t tm_label_logp_workspace_size(int dtype, int64_t outer, int64_t classes, int64_t inner,
+                                               const int64_t *strides, int top_k) {
+    LabelShape s{};
+    const void *some = reinterpret_cast<const void *>(uintptr_t(4096));
+    if (check_labels(some, dtype, outer, classes, inner, strides, nullptr, 0, nullptr, nullptr, s) != TM_OK) return 0;
+    if (s.positions == 0 || top_k < 0 || top_k > TM_LABEL_MAX_TOP) return 0;
+    const LabelPlan p = label_plan(dtype, s.n[0], s.n[1], s.n[2], strides);
+    return p.parts > 1 ? s.positions * p.parts * (sizeof(RowPart) + 8 * size_t(top_k)) : 0;
+}
 
 extern "C" int tm_label_logp(const void *logits, int dtype, int64_t outer, int64_t classes, int64_t inner,
                              const int64_t *strides, const void *labels, int label_dtype, const float *field,
@@ -165,9 +229,42 @@ extern "C" int tm_label_logp(const void *logits, int dtype, int64_t outer, int64
     a.k = uint32_t(top_k);
     a.label_bytes = int32_t(s.label_bytes);
     a.n = uint32_t(s.positions);
-    a.div_inner = Div32::make(uint32_t(inner));
+    const LabelPlan p = label_plan(dtype, s.n[0], s.n[1], s.n[2], strides);
+    a.ts[0] = top_k * inner;
+    a.ts[1] = inner;
+    a.ts[2] = 1;
+    if (p.swap) {
+        swap_positions(a);
+        std::swap(a.ts[0], a.ts[2]);
+    }
+    a.div_inner = Div32::make(a.inner);
+    a.partial = workspace;
     return by_type(dtype, [&](auto t) {
-        return launch(k_label_logp<decltype(t)>, dim3((a.n + 255) / 256), dim3(256), stream, a);
+        using T = decltype(t);
+        constexpr int V = 16 / sizeof(T);
+        if (p.rows) {
+            a.groups = p.parts;
+            a.div_groups = Div32::make(p.parts);
+            if (s.positions * p.parts >= kLimit) return int(TM_ERR_TOO_LARGE);
+            if (p.waves == 1) return launch(k_label_rows<T, 1>, dim3((a.n + 3) / 4), dim3(256), 0, stream, a);
+            const int rc = p.waves == 4
+                ? launch(k_label_rows<T, 4>, dim3(a.n * p.parts), dim3(256), 0, stream, a)
+                : launch(k_label_rows<T, 16>, dim3(a.n * p.parts), dim3(1024), 0, stream, a);
+            if (rc != TM_OK || p.parts == 1) return rc;
+            return launch(k_label_rows_join<T>, dim3(a.n), dim3(256), 0, stream, a);
+        }
+        a.groups = p.wide ? (a.inner + V - 1) / V : a.inner;
+        a.div_groups = Div32::make(a.groups);
+        const uint32_t threads = a.outer * a.groups;
+        if (p.held) {
+            void (*const kernels[])(LabelArgs) = {k_label_held<T, 1, 4>, k_label_held<T, 1, 8>, k_label_held<T, 1, 16>,
+                                                  k_label_held<T, V, 4>, k_label_held<T, V, 8>, k_label_held<T, V, 16>};
+            const int i = (p.wide ? 3 : 0) + (p.held == 4 ? 0 : p.held == 8 ? 1 : 2);
+            return launch(kernels[i], dim3((threads + 255) / 256), dim3(256), 0, stream, a);
+        }
+        const size_t lds = p.waves > 1 ? size_t(p.waves) * (p.wide ? V : 1) * 1024 : 0;
+        return launch(p.wide ? k_label_run<T, V> : k_label_run<T, 1>, dim3((threads + 63) / 64), dim3(64 * p.waves),
+                      lds, stream, a);
     });
 }
 
@@ -219,9 +316,51 @@ extern "C" int tm_label_logp_grad(const void *logits, int dtype, int64_t outer, 
     a.inner = uint32_t(inner);
     a.label_bytes = int32_t(s.label_bytes);
     a.n = uint32_t(s.positions);
-    a.div_inner = Div32::make(uint32_t(inner));
+    LabelPlan p = label_plan(dtype, s.n[0], s.n[1], s.n[2], strides);
+    // rows and 16-byte stores need the gradient to lie as the logits do
+    if (classes > TM_LABEL_MAX_RECOMPUTE && p.rows && grad_strides[1] != 1) {
+        p.rows = p.swap = p.wide = false;
+        p.held = 0;
+    }
+    if (p.wide && grad_strides[p.swap ? 0 : 2] != 1) p.wide = false;
+    if (p.swap) {
+        swap_positions(a);
+        std::swap(a.gs[0], a.gs[2]);
+    }
+    a.div_inner = Div32::make(a.inner);
     return by_type(dtype, [&](auto t) {
-        return launch(k_label_logp_grad<decltype(t)>, dim3((a.n + 255) / 256), dim3(256), stream, a);
+        using T = decltype(t);
+        constexpr int V = 16 / sizeof(T);
+        const bool F = a.field;
+        if (p.rows) {
+            // 8 loads to a thread, or one where that leaves CUs idle
+            const uint64_t load = 256 * V;
+            a.share = uint32_t(load * (s.positions * ceil_div(s.n[1], 8 * load) < kFill ? 1 : 8));
+            a.groups = uint32_t(ceil_div(s.n[1], a.share));
+            a.div_groups = Div32::make(a.groups);
+            if (s.positions * a.groups >= kLimit) return int(TM_ERR_TOO_LARGE);
+            return launch(F ? k_label_grad_rows<T, true> : k_label_grad_rows<T, false>, dim3(a.n * a.groups), dim3(256),
+                          0, stream, a);
+        }
+        a.groups = p.wide ? (a.inner + V - 1) / V : a.inner;
+        a.div_groups = Div32::make(a.groups);
+        const uint32_t threads = a.outer * a.groups;
+        const dim3 grid((threads + 255) / 256);
+        if (p.held) {
+            void (*const kernels[])(LabelGradArgs) = {
+                k_label_grad_held<T, 1, 4, false>, k_label_grad_held<T, 1, 8, false>, k_label_grad_held<T, 1, 16, false>,
+                k_label_grad_held<T, V, 4, false>, k_label_grad_held<T, V, 8, false>, k_label_grad_held<T, V, 16, false>,
+                k_label_grad_held<T, 1, 4, true>, k_label_grad_held<T, 1, 8, true>, k_label_grad_held<T, 1, 16, true>,
+                k_label_grad_held<T, V, 4, true>, k_label_grad_held<T, V, 8, true>, k_label_grad_held<T, V, 16, true>};
+            const int i = (F ? 6 : 0) + (p.wide ? 3 : 0) + (p.held == 4 ? 0 : p.held == 8 ? 1 : 2);
+            return launch(kernels[i], grid, dim3(256), 0, stream, a);
+        }
+        const uint64_t shares = std::min<uint64_t>({ceil_div(kBusyThreads, threads), ceil_div(s.n[1], 8), 65535});
+        a.share = uint32_t(ceil_div(s.n[1], shares));
+        void (*const kernels[])(LabelGradArgs) = {k_label_grad_run<T, 1, false>, k_label_grad_run<T, V, false>,
+                                                  k_label_grad_run<T, 1, true>, k_label_grad_run<T, V, true>};
+        return launch(kernels[(F ? 2 : 0) + (p.wide ? 1 : 0)],
+                      dim3(grid.x, uint32_t(ceil_div(s.n[1], a.share))), dim3(256), 0, stream, a);
     });
 }
 
@@ -230,6 +369,7 @@ extern "C" int tm_label_logp_grad(const void *logits, int dtype, int64_t outer, 
 // ---------------------------------------------------------------------------
 namespace {
 
+constexpr int64_t kMaxHeads = 1 << 16;
 struct BiasShape {
     BiasSource src;
     uint64_t batch, field_batch;
@@ -266,13 +406,18 @@ int check_grid(int ndim, const int64_t *query_shape, const int64_t *key_shape, c
             return TM_ERR_SAMPLING;
         s.src.offset[a] = int32_t(off);
         s.src.sampling[a] = float(sp);
-        s.src.div_q[a] = Div32::make(uint32_t(query_shape[a] ? query_shape[a] : 1));
-        s.src.div_k[a] = Div32::make(uint32_t(key_shape[a] ? key_shape[a] : 1));
         nq *= uint64_t(query_shape[a]);
         nk *= uint64_t(key_shape[a]);
         if (nq >= kLimit || nk >= kLimit) return TM_ERR_TOO_LARGE;
     }
     if (nq * nk >= kLimit || uint64_t(batch) >= kLimit) return TM_ERR_TOO_LARGE;
+    uint64_t behind_q = 1, behind_k = 1;
+    for (int a = ndim - 1; a >= 0 && nq * nk; --a) {
+        s.src.div_q[a] = Div32::make(uint32_t(behind_q));
+        s.src.div_k[a] = Div32::make(uint32_t(behind_k));
+        behind_q *= uint64_t(query_shape[a]);
+        behind_k *= uint64_t(key_shape[a]);
+    }
     if (metric == TM_METRIC_OFFSET && s.src.sampling[0] != 1.0f) return TM_ERR_SAMPLING;
     s.src.source = metric == TM_METRIC_OFFSET ? kOffset : metric == TM_METRIC_EUCLIDEAN ? kEuclid
                    : metric == TM_METRIC_TAXICAB ? kTaxicab : kChess;
@@ -287,13 +432,14 @@ int check_grid(int ndim, const int64_t *query_shape, const int64_t *key_shape, c
 int check_table(int buckets, int64_t heads, const float *edges, int table_dtype, int value_dtype, BiasShape &s) {
     if (buckets < 1 || buckets > int(kMaxBuckets) || heads < 1) return TM_ERR_SHAPE;
     if (!float_type(table_dtype) || !float_type(value_dtype)) return TM_ERR_DTYPE;
-    if (uint64_t(heads) >= kLimit / kMaxBuckets) return TM_ERR_TOO_LARGE;
+    if (heads > kMaxHeads) return TM_ERR_TOO_LARGE;
     if (!edges && buckets > 1) return TM_ERR_NULL;
     const uint64_t lim = uint64_t(1) << 58;
     const uint64_t bh = s.batch * uint64_t(heads);          // below 2^54
     if (s.src.positions && bh > lim / s.src.positions) return TM_ERR_TOO_LARGE;
     s.src.edges = edges;
     s.src.buckets = uint32_t(buckets);
+    s.src.span = pow2_from(s.src.buckets);
     s.elements = bh * s.src.positions;
     return TM_OK;
 }
@@ -317,16 +463,43 @@ int run_bias(const BiasShape &s, const void *table, int table_dtype, int64_t hea
     a.heads = uint32_t(heads);
     a.batch = uint32_t(s.batch);
     a.field_batch = uint32_t(s.field_batch);
+    // Shares: all heads to a workgroup where the positions alone fill the chip,
+    // else four heads at a time and then parts of the batch; a share's table
+    // fits 32 KB of LDS.
+    const uint64_t vec = 16 / float_bytes(out_dtype);
+    const uint64_t tiles = ceil_div(s.src.positions, kBiasThreads * vec);
+    const uint64_t blocks = tiles * s.field_batch;
+    const uint64_t quads = ceil_div(uint64_t(heads), 4);
+    const uint64_t most = std::max<uint64_t>(1, 2048 / s.src.buckets);
+    const uint64_t want = ceil_div(kFill, blocks);
+    const uint64_t share = std::min(most, ceil_div(quads, std::min(quads, want)));
+    const uint64_t shares = ceil_div(quads, share);
+    uint64_t bshares = 1;
+    if (s.field_batch == 1)
+        bshares = std::min(std::min(s.batch, 65535 / shares), ceil_div(kFill, blocks * shares));
+    const uint64_t bshare = s.field_batch == 1 ? ceil_div(s.batch, bshares) : 1;
+    if (s.field_batch == 1) bshares = ceil_div(s.batch, bshare);
+    if (blocks >= kLimit) return TM_ERR_TOO_LARGE;
+    a.head_share = uint32_t(4 * share);
+    a.row = uint32_t(4 * (share | 1));
+    a.batch_share = uint32_t(bshare);
+    a.batch_shares = uint32_t(bshares);
+    a.div_tiles = Div32::make(uint32_t(tiles));
+    const size_t lds = (size_t(s.src.buckets) * a.row + s.src.span) * 4;
     return by_type(out_dtype, [&](auto t) {
-        return launch(k_bias<decltype(t)>, dim3((s.src.positions + 255u) / 256u), dim3(256), stream, a);
+        return launch(k_bias<decltype(t)>, dim3(uint32_t(blocks), uint32_t(shares * bshares)), dim3(kBiasThreads), lds,
+                      stream, a);
     });
 }
+
+uint64_t grad_splits_most(uint64_t head_groups) { return std::max<uint64_t>(64, 512 / head_groups); }
+uint64_t grad_tile_rows(uint32_t buckets) { return std::max<uint64_t>(16, pow2_from(buckets)); }
 
 int run_bias_grad(const BiasShape &s, const void *grad, int grad_dtype, int64_t heads, void *out, int table_dtype,
                   void *workspace, size_t workspace_bytes, hipStream_t stream) {
     if (!out) return TM_ERR_NO_OUTPUT;
     if (!grad && s.elements) return TM_ERR_NULL;
-    const size_t need = tm_bias_grad_workspace_size(int64_t(s.field_batch), s.src.positions, int(s.src.buckets), heads);
+    const size_t need = tm_bias_grad_workspace_size(int(s.src.buckets), heads);
     if (need && (!workspace || workspace_bytes < need || uintptr_t(workspace) % 16)) return TM_ERR_WORKSPACE;
     const Range in[] = {{s.src.field, s.field_bytes}, {s.src.edges, 4 * uint64_t(s.src.buckets - 1)},
                         {grad, s.elements * float_bytes(grad_dtype)}};
@@ -342,8 +515,33 @@ int run_bias_grad(const BiasShape &s, const void *grad, int grad_dtype, int64_t 
     a.batch = uint32_t(s.batch);
     a.field_batch = uint32_t(s.field_batch);
     a.table_type = table_dtype;
+    // Units of 128 positions and, where samples share the buckets, as many of
+    // them as leave enough units; two workgroups of eight waves to a CU.
+    const uint64_t groups = ceil_div(uint64_t(heads), 16);
+    const uint64_t steps = ceil_div(s.src.positions, kGradStep);
+    uint64_t shares = s.batch;
+    a.batch_share = 1;
+    if (s.field_batch == 1 && s.batch) {
+        a.batch_share = uint32_t(std::min(s.batch, std::max<uint64_t>(1, s.batch * steps / 4096)));
+        shares = ceil_div(s.batch, a.batch_share);
+    }
+    const uint64_t units = steps * shares;
+    if (units >= kLimit) return TM_ERR_TOO_LARGE;
+    a.units = uint32_t(units);
+    a.div_steps = Div32::make(uint32_t(std::max<uint64_t>(1, steps)));
+    a.splits = uint32_t(std::max<uint64_t>(1, std::min(ceil_div(units, kGradWaves), grad_splits_most(groups))));
+    a.tile_rows = uint32_t(grad_tile_rows(s.src.buckets));
+    const int rc = by_type(grad_dtype, [&](auto t) {
+        using T = decltype(t);
+        void (*const kernels[])(BiasGradArgs) = {k_bias_grad<T, 1>, k_bias_grad<T, 2>, k_bias_grad<T, 4>,
+                                                 k_bias_grad<T, 8>, k_bias_grad<T, 16>};
+        int tiles = 0;
+        while ((16u << tiles) < a.tile_rows) ++tiles;
+        return launch(kernels[tiles], dim3(a.splits, uint32_t(groups)), dim3(kGradThreads), 0, stream, a);
+    });
+    if (rc != TM_OK) return rc;
     return by_type(grad_dtype, [&](auto t) {
-        return launch(k_bias_grad<decltype(t)>, dim3(s.src.buckets * a.heads), dim3(256), stream, a);
+        return launch(k_bias_join<decltype(t)>, dim3(s.src.buckets, uint32_t(groups)), dim3(256), 0, stream, a);
     });
 }
 
@@ -369,7 +567,11 @@ extern "C" int tm_relative_bias(int ndim, const int64_t *query_shape, const int6
     return rc == TM_OK ? run_bias(s, table, table_dtype, heads, add, out, out_dtype, stream) : rc;
 }
 
-extern "C" size_t tm_bias_grad_workspace_size(int64_t, int64_t, int, int64_t) { return 0; }
+extern "C" size_t tm_bias_grad_workspace_size(int buckets, int64_t heads) {
+    if (buckets < 1 || buckets > int(kMaxBuckets) || heads < 1 || heads > kMaxHeads) return 0;
+    const uint64_t groups = ceil_div(uint64_t(heads), 16);
+    return grad_splits_most(groups) * groups * grad_tile_rows(uint32_t(buckets)) * 64;
+}
 
 extern "C" int tm_distance_bias_grad(const void *distances, int distance_dtype, int64_t batch, int64_t positions,
                                      const void *grad, int grad_dtype, int buckets, int64_t heads, const float *edges,

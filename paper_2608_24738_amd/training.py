@@ -236,8 +236,8 @@ class _Bias(torch.autograd.Function):
     distances, or ("tm_relative_bias", args, None)."""
 
     @staticmethod
-    def forward(ctx, table, edges, add, source, shape, sizes):
-        ctx.source, ctx.sizes = source, sizes
+    def forward(ctx, table, edges, add, source, shape):
+        ctx.source = source
         ctx.table_dtype, ctx.table_shape = table.dtype, tuple(table.shape)
         ctx.has_add = add is not None
         ctx.save_for_backward(edges, source[2])
@@ -254,18 +254,18 @@ class _Bias(torch.autograd.Function):
             buckets, heads = ctx.table_shape
             dev = edges.device
             grad = torch.empty(ctx.table_shape, dtype=ctx.table_dtype, device=dev)
-            nbytes = _bias_workspace(*ctx.sizes, buckets, heads)
+            nbytes = _bias_workspace(buckets, heads)
             workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
             if distances is not None:
                 args = (distances.data_ptr(),) + args[1:]
             _call(name + "_grad", dev, None, *args, up.data_ptr(), FLOATS[up.dtype], buckets, heads, edges.data_ptr(),
                   grad.data_ptr(), FLOATS[ctx.table_dtype], _ptr(workspace), nbytes)
-        return grad, None, up if ctx.has_add and ctx.needs_input_grad[2] else None, None, None, None
+        return grad, None, up if ctx.has_add and ctx.needs_input_grad[2] else None, None, None
 
 
 @functools.lru_cache(maxsize=1024)
-def _bias_workspace(batch, positions, buckets, heads):
-    return int(load().tm_bias_grad_workspace_size(batch, positions, buckets, heads))
+def _bias_workspace(buckets, heads):
+    return int(load().tm_bias_grad_workspace_size(buckets, heads))
 
 
 def _bias_forward(table, edges, add, source, shape):
@@ -276,9 +276,9 @@ def _bias_forward(table, edges, add, source, shape):
     return out
 
 
-def _run_bias(table, edges, add, source, shape, sizes):
+def _run_bias(table, edges, add, source, shape):
     if torch.is_grad_enabled() and (table.requires_grad or (add is not None and add.requires_grad)):
-        return _Bias.apply(table, edges, add, source, shape, sizes)
+        return _Bias.apply(table, edges, add, source, shape)
     return _bias_forward(table, edges, add, source, shape)
 
 
@@ -333,7 +333,7 @@ def distance_bias(distances: torch.Tensor, table: torch.Tensor, edges: torch.Ten
         raise ValueError("add must have shape %s, got %s" % (shape, tuple(add.shape)))
     sizes = (distances.shape[0], math.prod(distances.shape[1:]))
     source = ("tm_distance_bias", (distances.data_ptr(), DISTANCES[distances.dtype]) + sizes, distances)
-    return _run_bias(table, edges, add, source, shape, sizes)
+    return _run_bias(table, edges, add, source, shape)
 
 
 def _extents(value, what):
@@ -388,4 +388,4 @@ def relative_bias(table: torch.Tensor, edges: torch.Tensor, query_shape, key_sha
         batch = math.prod(shape[:-3])
     args = (ndim, _shape_array(query), _shape_array(key), _shape_array(offset), BIAS_METRICS[metric],
             _sampling_array(sampling, ndim), batch)
-    return _run_bias(table, edges, add, ("tm_relative_bias", args, None), shape, (1, tail[1] * tail[2]))
+    return _run_bias(table, edges, add, ("tm_relative_bias", args, None), shape)

@@ -137,7 +137,7 @@ def test_bias_grad_checks(lib):
     assert call(grad=None) == NULL
     assert call(out=None) == NO_OUTPUT
     assert call(out=B) == ALIAS
-    if lib.tm_bias_grad_workspace_size(2, 10, 4, 3):
+    if lib.tm_bias_grad_workspace_size(4, 3):
         assert call(ws=None) == WORKSPACE
         assert call(ws=E + 8) == WORKSPACE
         assert call(ws_bytes=4) == WORKSPACE

@@ -151,13 +151,13 @@ __global__ void __launch_bounds__(kBiasThreads) k_bias(BiasArgs a) {
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 if (h + r >= hn) break;
-                Pack<T, V> out;
+                float out[V];
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
                     const float x = r == 0 ? v[j].x : r == 1 ? v[j].y : r == 2 ? v[j].z : v[j].w;
-                    out.v[j] = narrow<T>(a.add ? x + widen(extra[r].v[j]) : x);
+                    out[j] = a.add ? x + widen(extra[r].at(j)) : x;
                 }
-                store_pack<V>(static_cast<T *>(a.out) + row + uint64_t(r) * a.src.positions, out, n);
+                store_pack<V>(static_cast<T *>(a.out) + row + uint64_t(r) * a.src.positions, narrow_pack<T, V>(out), n);
             }
         }
     }
@@ -275,7 +275,7 @@ __global__ void __launch_bounds__(kGradThreads) k_bias_grad(BiasGradArgs a) {
                         uint32_t cut[2][3];
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            const float v = x[q].v[2 * j + e];
+                            const float v = widen(x[q].at(2 * j + e));
                             cut[e][0] = __float_as_uint(v) & 0xffff0000u;
                             const float r = v - __uint_as_float(cut[e][0]);
                             cut[e][1] = __float_as_uint(r) & 0xffff0000u;
@@ -285,7 +285,7 @@ __global__ void __launch_bounds__(kGradThreads) k_bias_grad(BiasGradArgs a) {
                         for (int c = 0; c < 3; ++c) part[c][j] = __builtin_amdgcn_perm(cut[1][c], cut[0][c], 0x07060302u);
                     }
                 } else {
-                    part[0] = __builtin_bit_cast(u32x4, x[q]);
+                    part[0] = u32x4{x[q].w[0], x[q].w[1], x[q].w[2], x[q].w[3]};
                 }
 #pragma unroll
                 for (int t = 0; t < Tiles; ++t) {

@@ -80,9 +80,9 @@ __device__ __forceinline__ uint64_t top_key(float x, uint32_t c) { return uint64
 template <int V>
 __device__ __forceinline__ Pack<float, V> load_field(const float *p, int64_t stride, uint32_t n) {
     if (V == 1 || stride == 1) return load_pack<V>(p, n, 0.0f);
-    Pack<float, V> r;
+    Pack<float, V> r{};
 #pragma unroll
-    for (int j = 0; j < V; ++j) r.v[j] = uint32_t(j) < n ? p[j * stride] : 0.0f;
+    for (int j = 0; j < V; ++j) r.put(j, uint32_t(j) < n ? p[j * stride] : 0.0f);
     return r;
 }
 

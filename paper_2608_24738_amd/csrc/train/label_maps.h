@@ -19,7 +19,7 @@ template <int V, typename L>
 __device__ __forceinline__ void load_labels_as(const L *p, uint32_t n, uint32_t classes, int32_t (&y)[V]) {
     const Pack<L, V> r = load_pack<V>(p, n, L(0));
 #pragma unroll
-    for (int j = 0; j < V; ++j) y[j] = int64_t(r.v[j]) >= 0 && int64_t(r.v[j]) < int64_t(classes) ? int32_t(r.v[j]) : -1;
+    for (int j = 0; j < V; ++j) y[j] = int64_t(r.at(j)) >= 0 && int64_t(r.at(j)) < int64_t(classes) ? int32_t(r.at(j)) : -1;
 }
 template <int V>
 __device__ __forceinline__ void load_labels(const void *p, int32_t bytes, uint64_t i, uint32_t n, uint32_t classes,
@@ -66,12 +66,12 @@ template <int V>
 __device__ __forceinline__ void put_top(const LabelArgs &a, const Place<V> &w, uint32_t rank, const Pick (&best)[V],
                                         const Found (&q)[V]) {
     const int64_t at = w.o * a.ts[0] + rank * a.ts[1] + w.i * a.ts[2];
-    Pack<float, V> top;
-    Pack<int32_t, V> index;
+    Pack<float, V> top{};
+    Pack<int32_t, V> index{};
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-        top.v[j] = log_prob(q[j], best[j].x);
-        index.v[j] = best[j].c;
+        top.put(j, log_prob(q[j], best[j].x));
+        index.put(j, best[j].c);
     }
     if (V == 1 || a.ts[2] == 1) {
         store_pack<V>(a.top + at, top, w.n);
@@ -80,8 +80,8 @@ __device__ __forceinline__ void put_top(const LabelArgs &a, const Place<V> &w, u
 #pragma unroll
         for (int j = 0; j < V; ++j)
             if (uint32_t(j) < w.n) {
-                a.top[at + j * a.ts[2]] = top.v[j];
-                a.index[at + j * a.ts[2]] = index.v[j];
+                a.top[at + j * a.ts[2]] = top.at(j);
+                a.index[at + j * a.ts[2]] = index.at(j);
             }
     }
 }
@@ -90,28 +90,28 @@ __device__ __forceinline__ void put_top(const LabelArgs &a, const Place<V> &w, u
 template <int V>
 __device__ __forceinline__ void put_found(const LabelArgs &a, const Place<V> &w, const int32_t (&y)[V],
                                           const float (&xl)[V], const Found (&q)[V]) {
-    Pack<float, V> r;
+    Pack<float, V> r{};
     if (a.logp) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) r.v[j] = y[j] < 0 ? 0.0f : log_prob(q[j], xl[j]);
+        for (int j = 0; j < V; ++j) r.put(j, y[j] < 0 ? 0.0f : log_prob(q[j], xl[j]));
         store_pack<V>(a.logp + w.at, r, w.n);
     }
     if (a.entropy) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) r.v[j] = q[j].entropy;
+        for (int j = 0; j < V; ++j) r.put(j, q[j].entropy);
         store_pack<V>(a.entropy + w.at, r, w.n);
     }
     if (a.mean) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) r.v[j] = q[j].mean;
+        for (int j = 0; j < V; ++j) r.put(j, q[j].mean);
         store_pack<V>(a.mean + w.at, r, w.n);
     }
     if (a.stats) {
-        Pack<float, 2 * V> st;
+        Pack<float, 2 * V> st{};
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            st.v[2 * j] = q[j].m;
-            st.v[2 * j + 1] = stats_logs(q[j]);
+            st.put(2 * j, q[j].m);
+            st.put(2 * j + 1, stats_logs(q[j]));
         }
         store_pack<2 * V>(a.stats + 2 * w.at, st, 2 * w.n);
     }
@@ -141,7 +141,7 @@ __global__ void __launch_bounds__(256) k_label_held(LabelArgs a) {
     for (int c = 0; c < C; ++c)
         if (uint32_t(c) < a.classes) {
 #pragma unroll
-            for (int j = 0; j < V; ++j) r[j].m = fmaxf(r[j].m, widen(held[c].v[j]));
+            for (int j = 0; j < V; ++j) r[j].m = fmaxf(r[j].m, widen(held[c].at(j)));
         }
     if (a.mean) {
         const float *field = a.field + w.o * a.fs[0] + w.i * a.fs[2];
@@ -150,14 +150,14 @@ __global__ void __launch_bounds__(256) k_label_held(LabelArgs a) {
             if (uint32_t(c) < a.classes) {
                 const Pack<float, V> phi = load_field<V>(field + c * a.fs[1], a.fs[2], w.n);
 #pragma unroll
-                for (int j = 0; j < V; ++j) take<T>(r[j], widen(held[c].v[j]), a.entropy, phi.v[j]);
+                for (int j = 0; j < V; ++j) take<T>(r[j], widen(held[c].at(j)), a.entropy, phi.at(j));
             }
     } else {
 #pragma unroll
         for (int c = 0; c < C; ++c)
             if (uint32_t(c) < a.classes) {
 #pragma unroll
-                for (int j = 0; j < V; ++j) take<T>(r[j], widen(held[c].v[j]), a.entropy);
+                for (int j = 0; j < V; ++j) take<T>(r[j], widen(held[c].at(j)), a.entropy);
             }
     }
     Found q[V];
@@ -168,7 +168,7 @@ __global__ void __launch_bounds__(256) k_label_held(LabelArgs a) {
         for (int c = 0; c < C; ++c)
 #pragma unroll
             for (int j = 0; j < V; ++j)
-                if (y[j] == c) xl[j] = widen(held[c].v[j]);
+                if (y[j] == c) xl[j] = widen(held[c].at(j));
     }
     put_found<V>(a, w, y, xl, q);
     Pick last[V];
@@ -182,7 +182,7 @@ __global__ void __launch_bounds__(256) k_label_held(LabelArgs a) {
         for (int c = 0; c < C; ++c)
             if (uint32_t(c) < a.classes) {
 #pragma unroll
-                for (int j = 0; j < V; ++j) consider(best[j], last[j], widen(held[c].v[j]), c);
+                for (int j = 0; j < V; ++j) consider(best[j], last[j], widen(held[c].at(j)), c);
             }
         put_top<V>(a, w, rank, best, q);
 #pragma unroll
@@ -224,7 +224,7 @@ __global__ void __launch_bounds__(64 * kRunWaves) k_label_run(LabelArgs a) {
             float m = r[j].m;
 #pragma unroll
             for (int u = 0; u < kRunBlock; ++u)
-                if (c + u < c1) m = fmaxf(m, widen(held[u].v[j]));
+                if (c + u < c1) m = fmaxf(m, widen(held[u].at(j)));
             lift(r[j], m);
             part[j] = {m, 0.0f, 0.0f, 0.0f};
         }
@@ -234,10 +234,10 @@ __global__ void __launch_bounds__(64 * kRunWaves) k_label_run(LabelArgs a) {
                 if (field) {
                     const Pack<float, V> phi = load_field<V>(field + (c + u) * a.fs[1], a.fs[2], w.n);
 #pragma unroll
-                    for (int j = 0; j < V; ++j) take<T>(part[j], widen(held[u].v[j]), a.entropy, phi.v[j]);
+                    for (int j = 0; j < V; ++j) take<T>(part[j], widen(held[u].at(j)), a.entropy, phi.at(j));
                 } else {
 #pragma unroll
-                    for (int j = 0; j < V; ++j) take<T>(part[j], widen(held[u].v[j]), a.entropy);
+                    for (int j = 0; j < V; ++j) take<T>(part[j], widen(held[u].at(j)), a.entropy);
                 }
             }
 #pragma unroll
@@ -252,8 +252,8 @@ __global__ void __launch_bounds__(64 * kRunWaves) k_label_run(LabelArgs a) {
                 if (c + u < c1) {
 #pragma unroll
                     for (int j = 0; j < V; ++j)
-                        if (best[j].c < 0 || larger(widen(held[u].v[j]), best[j].x))
-                            best[j] = {widen(held[u].v[j]), int32_t(c + u)};
+                        if (best[j].c < 0 || larger(widen(held[u].at(j)), best[j].x))
+                            best[j] = {widen(held[u].at(j)), int32_t(c + u)};
                 }
         }
     }
@@ -304,7 +304,7 @@ __global__ void __launch_bounds__(64 * kRunWaves) k_label_run(LabelArgs a) {
             for (uint32_t c = c0; c < c1; ++c) {
                 const Pack<T, V> one = load_pack<V>(x + c * a.xs[1], w.n, T{});
 #pragma unroll
-                for (int j = 0; j < V; ++j) consider(best[j], last[j], widen(one.v[j]), int32_t(c));
+                for (int j = 0; j < V; ++j) consider(best[j], last[j], widen(one.at(j)), int32_t(c));
             }
         }
         if (waves > 1) {
@@ -347,9 +347,9 @@ __device__ __forceinline__ void load_upstream(const LabelGradArgs &a, const Plac
 #pragma unroll
     for (int j = 0; j < V; ++j) {
         if (!a.up_logp) y[j] = -1;
-        g[j].a = y[j] < 0 || g[j].logs == INFINITY ? 0.0f : ua.v[j];
-        g[j].h = uh.v[j];
-        g[j].f = uf.v[j];
+        g[j].a = y[j] < 0 || g[j].logs == INFINITY ? 0.0f : ua.at(j);
+        g[j].h = uh.at(j);
+        g[j].f = uf.at(j);
     }
 }
 
@@ -358,18 +358,19 @@ template <typename T, int V, bool F>
 __device__ __forceinline__ void put_slope(const LabelGradArgs &a, const Place<V> &w, uint32_t c, const Pack<T, V> &x,
                                           const Pack<float, V> &phi, const int32_t (&y)[V], const Slope (&g)[V]) {
     T *out = static_cast<T *>(a.grad) + w.o * a.gs[0] + c * a.gs[1] + w.i * a.gs[2];
-    Pack<T, V> r;
+    float v[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-        const float v = slope_of<T, F>(g[j], a.up_entropy, widen(x.v[j]), F ? phi.v[j] : 0.0f);
-        r.v[j] = narrow<T>(y[j] == int32_t(c) ? v + g[j].a : v);
+        v[j] = slope_of<T, F>(g[j], a.up_entropy, widen(x.at(j)), F ? phi.at(j) : 0.0f);
+        v[j] = y[j] == int32_t(c) ? v[j] + g[j].a : v[j];
     }
+    const Pack<T, V> r = narrow_pack<T, V>(v);
     if (V == 1 || a.gs[2] == 1) {
         store_pack<V>(out, r, w.n);
     } else {
 #pragma unroll
         for (int j = 0; j < V; ++j)
-            if (uint32_t(j) < w.n) out[j * a.gs[2]] = r.v[j];
+            if (uint32_t(j) < w.n) out[j * a.gs[2]] = r.at(j);
     }
 }
 
@@ -399,7 +400,7 @@ __global__ void __launch_bounds__(256) k_label_grad_held(LabelGradArgs a) {
     for (int c = 0; c < C; ++c)
         if (uint32_t(c) < a.classes) {
 #pragma unroll
-            for (int j = 0; j < V; ++j) r[j].m = fmaxf(r[j].m, widen(held[c].v[j]));
+            for (int j = 0; j < V; ++j) r[j].m = fmaxf(r[j].m, widen(held[c].at(j)));
         }
 #pragma unroll
     for (int c = 0; c < C; ++c)
@@ -407,8 +408,8 @@ __global__ void __launch_bounds__(256) k_label_grad_held(LabelGradArgs a) {
             if constexpr (F && !Keep) phi[0] = load_field<V>(field + c * a.fs[1], a.fs[2], w.n);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                if constexpr (F) take<T>(r[j], widen(held[c].v[j]), a.up_entropy, phi[Keep ? c : 0].v[j]);
-                else take<T>(r[j], widen(held[c].v[j]), a.up_entropy);
+                if constexpr (F) take<T>(r[j], widen(held[c].at(j)), a.up_entropy, phi[Keep ? c : 0].at(j));
+                else take<T>(r[j], widen(held[c].at(j)), a.up_entropy);
             }
         }
 #pragma unroll
@@ -445,10 +446,10 @@ __global__ void __launch_bounds__(256) k_label_grad_run(LabelGradArgs a) {
     if constexpr (F) mean = load_pack<V>(a.mean + w.at, w.n, 0.0f);
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-        g[j].m = st.v[2 * j];
-        g[j].logs = st.v[2 * j + 1];
-        g[j].entropy = entropy.v[j];
-        g[j].mean = mean.v[j];
+        g[j].m = st.at(2 * j);
+        g[j].logs = st.at(2 * j + 1);
+        g[j].entropy = entropy.at(j);
+        g[j].mean = mean.at(j);
     }
     int32_t y[V];
     load_upstream<V>(a, w, y, g);

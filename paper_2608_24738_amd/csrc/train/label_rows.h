@@ -73,7 +73,7 @@ __device__ __forceinline__ uint64_t next_of(const T *x, uint32_t first, uint32_t
 #pragma unroll
         for (int j = 0; j < V; ++j)
             if (uint32_t(j) < n) {
-                const uint64_t key = top_key(widen(r.v[j]), uint32_t(c) + j);
+                const uint64_t key = top_key(widen(r.at(j)), uint32_t(c) + j);
                 if (key < floor && key > best) best = key;
             }
     }
@@ -114,15 +114,15 @@ __global__ void __launch_bounds__(W == 1 ? 256 : 64 * W) k_label_rows(LabelArgs 
                 held[u] = load_pack<V>(x + at, end - uint32_t(at), none);
             } else {
 #pragma unroll
-                for (int j = 0; j < V; ++j) held[u].v[j] = none;
+                for (int j = 0; j < V; ++j) held[u].put(j, none);
             }
         }
         float m = r.m;
 #pragma unroll
         for (int u = 0; u < kRowLoads; ++u) {
-            most[u] = widen(held[u].v[0]);
+            most[u] = widen(held[u].at(0));
 #pragma unroll
-            for (int j = 1; j < V; ++j) most[u] = fmaxf(most[u], widen(held[u].v[j]));
+            for (int j = 1; j < V; ++j) most[u] = fmaxf(most[u], widen(held[u].at(j)));
             if (a.k && most[u] > best) {
                 best = most[u];
                 from = uint32_t(c + uint64_t(u) * kStride);
@@ -138,10 +138,10 @@ __global__ void __launch_bounds__(W == 1 ? 256 : 64 * W) k_label_rows(LabelArgs 
                 Pack<float, V> phi{};
                 if (at < end) phi = load_field<V>(field + at * a.fs[1], a.fs[1], end - uint32_t(at));
 #pragma unroll
-                for (int j = 0; j < V; ++j) take<T>(some, widen(held[u].v[j]), a.entropy, phi.v[j]);
+                for (int j = 0; j < V; ++j) take<T>(some, widen(held[u].at(j)), a.entropy, phi.at(j));
             } else {
 #pragma unroll
-                for (int j = 0; j < V; ++j) take<T>(some, widen(held[u].v[j]), a.entropy);
+                for (int j = 0; j < V; ++j) take<T>(some, widen(held[u].at(j)), a.entropy);
             }
         }
         r.s += some.s;
@@ -266,16 +266,13 @@ __global__ void __launch_bounds__(256) k_label_grad_rows(LabelGradArgs a) {
             if constexpr (F) phi = load_field<V>(field + at * a.fs[1], a.fs[1], end - uint32_t(at));
             float v[V];
 #pragma unroll
-            for (int j = 0; j < V; ++j) v[j] = slope_of<T, F>(g, a.up_entropy, widen(held[u].v[j]), phi.v[j]);
+            for (int j = 0; j < V; ++j) v[j] = slope_of<T, F>(g, a.up_entropy, widen(held[u].at(j)), phi.at(j));
             if (uint32_t(y) - uint32_t(at) < V) {          // false for y < 0
 #pragma unroll
                 for (int j = 0; j < V; ++j)
                     if (uint32_t(y) == uint32_t(at) + j) v[j] += g.a;
             }
-            Pack<T, V> r;
-#pragma unroll
-            for (int j = 0; j < V; ++j) r.v[j] = narrow<T>(v[j]);
-            store_pack<V>(out + at, r, end - uint32_t(at));
+            store_pack<V>(out + at, narrow_pack<T, V>(v), end - uint32_t(at));
         }
     }
 }

@@ -37,36 +37,132 @@ __device__ __forceinline__ f16 narrow<f16>(float x) { return {__builtin_bit_cast
 template <>
 __device__ __forceinline__ bf16 narrow<bf16>(float x) { return {__builtin_bit_cast(uint16_t, __bf16(x))}; }
 
-// V consecutive elements, loaded and stored in one piece of up to 16 bytes per
-// instruction; the address is aligned to one element.
+// V consecutive elements as the 32-bit words they are loaded and stored in, in
+// pieces of up to 16 bytes; the address is aligned to one element.  (Kept as
+// words, because loads of separate elements are not merged again.)
 template <typename T, int V>
-struct Pack { T v[V]; };
+struct Pack {
+    static constexpr int kWords = (V * int(sizeof(T)) + 3) / 4;
+    uint32_t w[kWords];
+
+    __device__ __forceinline__ T at(int j) const {
+        if constexpr (sizeof(T) == 8)
+            return __builtin_bit_cast(T, uint64_t(w[2 * j + 1]) << 32 | w[2 * j]);
+        else if constexpr (sizeof(T) == 4)
+            return __builtin_bit_cast(T, w[j]);
+        else if constexpr (sizeof(T) == 2)
+            return __builtin_bit_cast(T, uint16_t(w[j / 2] >> (16 * (j & 1))));
+        else
+            return __builtin_bit_cast(T, uint8_t(w[j / 4] >> (8 * (j & 3))));
+    }
+    __device__ __forceinline__ void put(int j, T v) {
+        if constexpr (sizeof(T) == 4)
+            w[j] = __builtin_bit_cast(uint32_t, v);
+        else if constexpr (sizeof(T) == 2)
+            w[j / 2] = j & 1 ? (w[j / 2] & 0xffffu) | uint32_t(__builtin_bit_cast(uint16_t, v)) << 16
+                             : (w[j / 2] & 0xffff0000u) | __builtin_bit_cast(uint16_t, v);
+        else if constexpr (sizeof(T) == 1)
+            w[j / 4] = (w[j / 4] & ~(0xffu << (8 * (j & 3)))) | uint32_t(__builtin_bit_cast(uint8_t, v)) << (8 * (j & 3));
+        else {
+            w[2 * j] = uint32_t(__builtin_bit_cast(uint64_t, v));
+            w[2 * j + 1] = uint32_t(__builtin_bit_cast(uint64_t, v) >> 32);
+        }
+    }
+};
+
+template <int N> struct Words;
+template <> struct Words<1> { typedef uint32_t type; };
+template <> struct Words<2> { typedef uint32_t type __attribute__((ext_vector_type(2))); };
+template <> struct Words<4> { typedef uint32_t type __attribute__((ext_vector_type(4))); };
+
+// N words at an address aligned to A bytes.
+template <int N, int A>
+struct Piece {
+    typedef typename Words<N>::type type __attribute__((aligned(A)));
+};
 
 template <int V, typename T>
 __device__ __forceinline__ Pack<T, V> load_pack(const T *p) {
-    Pack<T, V> r;
-    __builtin_memcpy(&r, p, sizeof r);
+    Pack<T, V> r{};
+    if constexpr (V * sizeof(T) < 4) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) r.put(j, p[j]);
+    } else {
+        constexpr int N = Pack<T, V>::kWords < 4 ? Pack<T, V>::kWords : 4;
+        static_assert(V * sizeof(T) % (4 * N) == 0);
+#pragma unroll
+        for (int i = 0; i < Pack<T, V>::kWords; i += N) {
+            const typename Words<N>::type v = *reinterpret_cast<const typename Piece<N, alignof(T)>::type *>(
+                reinterpret_cast<const char *>(p) + 4 * i);
+            if constexpr (N == 1) {
+                r.w[i] = v;
+            } else {
+#pragma unroll
+                for (int j = 0; j < N; ++j) r.w[i + j] = v[j];
+            }
+        }
+    }
     return r;
 }
 // The first n elements; the rest are `fill`.
 template <int V, typename T>
 __device__ __forceinline__ Pack<T, V> load_pack(const T *p, uint32_t n, T fill) {
-    if (n >= V) return load_pack<V>(p);
-    Pack<T, V> r;
+    if (V == 1 || n >= V) return load_pack<V>(p);
+    Pack<T, V> r{};
 #pragma unroll
-    for (int j = 0; j < V; ++j) r.v[j] = uint32_t(j) < n ? p[j] : fill;
+    for (int j = 0; j < V; ++j) r.put(j, uint32_t(j) < n ? p[j] : fill);
     return r;
 }
 template <int V, typename T>
 __device__ __forceinline__ void store_pack(T *p, const Pack<T, V> &r) {
-    __builtin_memcpy(p, &r, sizeof r);
+    if constexpr (V * sizeof(T) < 4) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) p[j] = r.at(j);
+    } else {
+        constexpr int N = Pack<T, V>::kWords < 4 ? Pack<T, V>::kWords : 4;
+#pragma unroll
+        for (int i = 0; i < Pack<T, V>::kWords; i += N) {
+            typename Words<N>::type v;
+            if constexpr (N == 1) {
+                v = r.w[i];
+            } else {
+#pragma unroll
+                for (int j = 0; j < N; ++j) v[j] = r.w[i + j];
+            }
+            *reinterpret_cast<typename Piece<N, alignof(T)>::type *>(reinterpret_cast<char *>(p) + 4 * i) = v;
+        }
+    }
 }
 template <int V, typename T>
 __device__ __forceinline__ void store_pack(T *p, const Pack<T, V> &r, uint32_t n) {
-    if (n >= V) return store_pack<V>(p, r);
+    if (V == 1 || n >= V) return store_pack<V>(p, r);
 #pragma unroll
     for (int j = 0; j < V; ++j)
-        if (uint32_t(j) < n) p[j] = r.v[j];
+        if (uint32_t(j) < n) p[j] = r.at(j);
+}
+
+// V floats rounded to T.
+template <typename T, int V>
+__device__ __forceinline__ Pack<T, V> narrow_pack(const float (&v)[V]) {
+    Pack<T, V> r{};
+    if constexpr (sizeof(T) == 2 && V % 2 == 0) {
+        typedef float f2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+        for (int j = 0; j < V; j += 2) {
+            const f2 x = {v[j], v[j + 1]};
+            if constexpr (__is_same(T, bf16)) {
+                typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+                r.w[j / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, b2));
+            } else {
+                typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+                r.w[j / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, h2));
+            }
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) r.put(j, narrow<T>(v[j]));
+    }
+    return r;
 }
 
 // 2^x by the hardware's v_exp_f32 (results below 2^-126 flush to 0).

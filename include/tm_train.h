@@ -33,7 +33,7 @@ extern "C" {
 enum {
     TM_METRIC_OFFSET = 3,         /* relative biases of rank 1: the signed offset key - query */
     TM_LABEL_MAX_TOP = 32,        /* most alternatives tm_label_logp reports */
-    TM_LABEL_MAX_RECOMPUTE = 16,  /* most classes whose gradient needs no out_stats */
+    TM_LABEL_MAX_RECOMPUTE = 32,  /* most classes whose gradient needs no out_stats */
     TM_BIAS_MAX_BUCKETS = 256
 };
 

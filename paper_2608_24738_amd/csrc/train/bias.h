@@ -329,7 +329,14 @@ __global__ void __launch_bounds__(256) k_bias_join(BiasGradArgs a) {
     const uint32_t k = blockIdx.x, h0 = blockIdx.y * 16;
     const float *p = a.partial + (uint64_t(blockIdx.y) * a.tile_rows + k) * 16 + col;
     float sum = 0.0f;
-    for (uint32_t w = slice; w < a.splits; w += 16) sum += p[uint64_t(w) * gridDim.y * a.tile_rows * 16];
+    const uint64_t step = uint64_t(gridDim.y) * a.tile_rows * 16;
+    for (uint32_t w = slice; w < a.splits; w += 16 * 8) {  // eight loads in flight
+        float v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = w + 16 * u < a.splits ? p[(w + 16 * u) * step] : 0.0f;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) sum += v[u];
+    }
     part[threadIdx.x] = sum;
     __syncthreads();
     for (uint32_t w = 8; w; w >>= 1) {

@@ -98,21 +98,18 @@ __device__ __forceinline__ float below(float x, float m) {
     return d < -200.0f ? -200.0f : d;
 }
 
-// exp d for the sums of type T.  The rounding of d log2(e) is an error of up to
-// 2^-24 |d|; float32 logits take it back to first order, 16-bit ones are
-// rounded to 2^-9 themselves.
-template <typename T>
+// exp d.  The rounding of d log2(e), an error of up to 2^-24 |d|, is taken
+// back to first order.
 __device__ __forceinline__ float exp_of(float d) {
     const float z = d * kLog2e;
     const float e = exp2_hw(z);
-    if constexpr (sizeof(T) == 4) return fmaf(e, fmaf(d, kLog2e, -z) * kLn2, e);
-    return e;
+    return fmaf(e, fmaf(d, kLog2e, -z) * kLn2, e);
 }
 
 // The sums seen from a larger maximum.
 __device__ __forceinline__ void lift(Sums &r, float m) {
     const float d = below(r.m, m);
-    const float e = exp_of<float>(d);
+    const float e = exp_of(d);
     r.t = e * fmaf(d, r.s, r.t);
     r.s *= e;
     r.f *= e;
@@ -125,21 +122,70 @@ __device__ __forceinline__ Sums join(Sums a, Sums b) {
     return {m, a.s + b.s, a.t + b.t, a.f + b.f};
 }
 
-// One class more; field is read only if it is there.
-template <typename T>
-__device__ __forceinline__ void take(Sums &r, float x, bool entropy) {
-    const float d = below(x, r.m);
-    const float e = exp_of<T>(d);
-    r.s += e;
-    if (entropy) r.t = fmaf(e, d, r.t);
-}
-template <typename T>
-__device__ __forceinline__ void take(Sums &r, float x, bool entropy, float field) {
-    const float d = below(x, r.m);
-    const float e = exp_of<T>(d);
-    r.s += e;
-    if (entropy) r.t = fmaf(e, d, r.t);
-    r.f = fmaf(e, e == 0.0f ? 0.0f : field, r.f);
+// Classes against a reference m.
+//
+// Near (16-bit logits, |m| <= kNear): z = x log2(e) - m log2(e) is one fused
+// operation, off by 2^-24 |z|, which the logits' own rounding of 2^-9 hides.
+// The rounding of m log2(e) is a common factor of every e and is taken out
+// again at the end.  Otherwise (float32 logits, or products in which that
+// factor would not be small, masks of the type's lowest value among them): d = x - m,
+// with the rounding of d log2(e) taken back to first order.
+constexpr float kNear = 1000.0f;                           // factor - 1 < 6e-5, its square below a rounding
+
+template <bool Near, bool Entropy, bool Mean>
+struct Ref {
+    static constexpr bool kMean = Mean;
+    float m, mz;
+
+    __device__ __forceinline__ explicit Ref(float m) : m(m), mz(m * kLog2e) {}
+
+    __device__ __forceinline__ void take(Sums &r, float x, float field) const {
+        float e;
+        if constexpr (Near) {
+            const float z = fmaf(x, kLog2e, -mz);
+            e = exp2_hw(z);
+            if constexpr (Entropy) r.t = fmaf(e, fmaxf(z, -300.0f), r.t);    // 0 times a finite number; NaN comes from e
+        } else {
+            const float d = below(x, m);
+            e = exp_of(d);
+            if constexpr (Entropy) r.t = fmaf(e, d, r.t);
+        }
+        r.s += e;
+        if constexpr (Mean) r.f = fmaf(e, e == 0.0f ? 0.0f : field, r.f);
+    }
+    // r += the sums of the classes taken into `some`
+    __device__ __forceinline__ void close(Sums &r, const Sums &some) const {
+        if constexpr (Near) {
+            const float off = fmaf(m, kLog2e, -mz) * kLn2;
+            const float scale = 1.0f - off;
+            r.s = fmaf(some.s, scale, r.s);
+            if constexpr (Entropy) r.t = fmaf(fmaf(some.t, kLn2, -off * some.s), scale, r.t);   // z to d
+            if constexpr (Mean) r.f = fmaf(some.f, scale, r.f);
+        } else {
+            r.s += some.s;
+            if constexpr (Entropy) r.t += some.t;
+            if constexpr (Mean) r.f += some.f;
+        }
+    }
+};
+
+// f(Ref(m) of the kind that serves): m the reference, size the largest |m| of
+// the thread.  The kinds are told apart here and not class by class, where
+// the compiler makes a selection of every branch.
+template <bool Near, bool Entropy, bool Mean>
+struct Kind {
+    typedef Ref<Near, Entropy, Mean> type;
+};
+template <typename T, bool Mean, typename F>
+__device__ __forceinline__ void by_kind(float size, bool entropy, F f) {
+    constexpr bool Near = sizeof(T) == 2;
+    if (!Near || size > kNear) {
+        if (Mean || entropy) f(Kind<false, true, Mean>{});
+        else f(Kind<false, false, Mean>{});
+    } else {
+        if (Mean || entropy) f(Kind<Near, true, Mean>{});
+        else f(Kind<Near, false, Mean>{});
+    }
 }
 
 // What a position's sums say.
@@ -151,9 +197,10 @@ __device__ __forceinline__ Found found(const Sums &r) {
     Found q;
     q.dead = r.s == 0.0f;
     q.m = r.m;
-    q.logs = logf(r.s);
-    q.entropy = q.dead ? 0.0f : q.logs - r.t / r.s;
-    q.mean = q.dead ? 0.0f : r.f / r.s;
+    q.logs = __builtin_amdgcn_logf(r.s) * kLn2;            // s is 0 or between 1/2 and 2^31: no subnormals
+    const float one = __builtin_amdgcn_rcpf(r.s);          // within 1 ulp
+    q.entropy = q.dead ? 0.0f : fmaf(-r.t, one, q.logs);
+    q.mean = q.dead ? 0.0f : r.f * one;
     return q;
 }
 __device__ __forceinline__ float log_prob(const Found &q, float x) {
@@ -170,7 +217,8 @@ template <typename T, bool F>
 __device__ __forceinline__ float slope_of(const Slope &g, bool entropy, float x, float field) {
     // x - m - log s; a dead position has log s = inf and so p = 0
     const float l = below(x - g.m, g.logs);
-    const float p = exp_of<T>(l);
+    // a 16-bit gradient hides the rounding of l log2(e)
+    const float p = sizeof(T) == 2 ? exp2_hw(l * kLog2e) : exp_of(l);
     float v = -g.a;
     if (entropy) v -= g.h * (l + g.entropy);
     if constexpr (F) v += g.f * (field - g.mean);

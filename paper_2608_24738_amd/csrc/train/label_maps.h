@@ -1,9 +1,9 @@
 // label_maps.h -- label log-probabilities where the classes of a position lie
 // apart and neighbouring positions side by side, as in (B, C, *spatial).
 //
-// A thread owns V neighbouring positions (16 bytes of logits of one class), so
-// a wave reads whole lines of every class plane.  Few classes are held in
-// registers between the passes for the maximum, the sums and the likeliest
+// A thread owns V neighbouring positions (16 or 8 bytes of logits of one
+// class), so a wave reads whole lines of every class plane.  Up to 32 classes
+// are held in registers between the passes for the maximum, the sums and the likeliest
 // classes (k_label_held): every logit is read once.  More run through in
 // blocks of 8 with a running maximum (k_label_run); where there are few
 // positions, the waves of a workgroup share the classes and join their sums.
@@ -14,6 +14,12 @@
 #include "label.h"
 
 namespace tmtrain {
+
+// Positions to a thread: 16 bytes, or 8 where the classes held would take more
+// than 32 registers or running ones with their sums more than 128.
+template <typename T, int C>
+constexpr int kHeldV = (C <= 8 ? 16 : 8) / int(sizeof(T));
+constexpr int kRunV = 4;
 
 template <int V, typename L>
 __device__ __forceinline__ void load_labels_as(const L *p, uint32_t n, uint32_t classes, int32_t (&y)[V]) {
@@ -48,18 +54,15 @@ __device__ __forceinline__ Place<V> place(const Args &a, uint32_t thread) {
     return r;
 }
 
-// The class below `last` (in the order of the alternatives) that is largest:
-// one step of a selection over the classes, in rising number.
+// One step of a selection over the classes, in rising number: the largest one
+// behind `last` in the order of the alternatives.  NaN is never picked.
 struct Pick {
     float x;
-    int32_t c;
+    int32_t c;                  // -1: none yet
 };
-constexpr Pick kNoPick = {0.0f, -1};
-// NaN counts as below -inf here: larger(a, b) for the order of the alternatives
-__device__ __forceinline__ bool larger(float a, float b) { return a > b || (b != b && a == a); }
 __device__ __forceinline__ void consider(Pick &best, const Pick &last, float x, int32_t c) {
-    const bool open = last.c < 0 || larger(last.x, x) || (!larger(x, last.x) && c > last.c);
-    if (open && (best.c < 0 || larger(x, best.x))) best = {x, c};
+    const bool open = x < last.x || (x == last.x && c > last.c);
+    if (open && (best.c < 0 || x > best.x)) best = {x, c};
 }
 
 template <int V>
@@ -71,7 +74,7 @@ __device__ __forceinline__ void put_top(const LabelArgs &a, const Place<V> &w, u
 #pragma unroll
     for (int j = 0; j < V; ++j) {
         top.put(j, log_prob(q[j], best[j].x));
-        index.put(j, best[j].c);
+        index.put(j, max(best[j].c, 0));                   // NaN everywhere: no class is larger
     }
     if (V == 1 || a.ts[2] == 1) {
         store_pack<V>(a.top + at, top, w.n);
@@ -117,8 +120,46 @@ __device__ __forceinline__ void put_found(const LabelArgs &a, const Place<V> &w,
     }
 }
 
+// Classes whose field is held too; others' is read again for the gradient.
+template <int C, int V, bool F>
+constexpr int kFieldHeld = F && C * V <= 32 ? C : 1;
+
+// The sums of held classes; r holds the maxima.
+// The field is left in `phi` as far as that has room.
+template <typename T, int V, int C, bool F, int P>
+__device__ __forceinline__ void held_sums(Sums (&r)[V], Pack<T, V> (&held)[C], uint32_t classes, bool entropy,
+                                          const float *field, const int64_t (&fs)[3], uint32_t n, Pack<float, V> (&phi)[P]) {
+    if constexpr (F && P == C) {
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+            if (uint32_t(c) < classes) phi[c] = load_field<V>(field + c * fs[1], fs[2], n);
+    }
+    float size = 0.0f;
+#pragma unroll
+    for (int j = 0; j < V; ++j) size = fmaxf(size, fabsf(r[j].m));
+#pragma unroll
+    for (int c = 0; c < C; ++c) forget_widened(held[c]);
+    by_kind<T, F>(size, entropy, [&](auto kind) __attribute__((always_inline)) {
+        typedef typename decltype(kind)::type R;
+        Sums some[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) some[j] = kNothing;
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+            if (uint32_t(c) < classes) {
+                if (F && P != C) phi[0] = load_field<V>(field + c * fs[1], fs[2], n);
+#pragma unroll
+                for (int j = 0; j < V; ++j) R(r[j].m).take(some[j], widen(held[c].at(j)), F ? phi[P == C ? c : 0].at(j) : 0.0f);
+            }
+#pragma unroll
+        for (int j = 0; j < V; ++j) R(r[j].m).close(r[j], some[j]);
+    });
+#pragma unroll
+    for (int c = 0; c < C; ++c) forget_widened(held[c]);
+}
+
 // At most C classes, held in registers.
-template <typename T, int V, int C>
+template <typename T, int V, int C, bool F>
 __global__ void __launch_bounds__(256) k_label_held(LabelArgs a) {
     const uint32_t thread = blockIdx.x * 256 + threadIdx.x;
     if (thread >= a.outer * a.groups) return;
@@ -143,23 +184,9 @@ __global__ void __launch_bounds__(256) k_label_held(LabelArgs a) {
 #pragma unroll
             for (int j = 0; j < V; ++j) r[j].m = fmaxf(r[j].m, widen(held[c].at(j)));
         }
-    if (a.mean) {
-        const float *field = a.field + w.o * a.fs[0] + w.i * a.fs[2];
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-            if (uint32_t(c) < a.classes) {
-                const Pack<float, V> phi = load_field<V>(field + c * a.fs[1], a.fs[2], w.n);
-#pragma unroll
-                for (int j = 0; j < V; ++j) take<T>(r[j], widen(held[c].at(j)), a.entropy, phi.at(j));
-            }
-    } else {
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-            if (uint32_t(c) < a.classes) {
-#pragma unroll
-                for (int j = 0; j < V; ++j) take<T>(r[j], widen(held[c].at(j)), a.entropy);
-            }
-    }
+    const float *const field = F ? a.field + w.o * a.fs[0] + w.i * a.fs[2] : nullptr;
+    Pack<float, V> phi[kFieldHeld<C, V, F>];
+    held_sums<T, V, C, F>(r, held, a.classes, a.entropy, field, a.fs, w.n, phi);
     Found q[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) q[j] = found(r[j]);
@@ -171,13 +198,32 @@ __global__ void __launch_bounds__(256) k_label_held(LabelArgs a) {
                 if (y[j] == c) xl[j] = widen(held[c].at(j));
     }
     put_found<V>(a, w, y, xl, q);
-    Pick last[V];
+    if (!a.k) return;
 #pragma unroll
-    for (int j = 0; j < V; ++j) last[j] = kNoPick;
-    for (uint32_t rank = 0; rank < a.k; ++rank) {
-        Pick best[V];
+    for (int c = 0; c < C; ++c) forget_widened(held[c]);
+    // the likeliest class is the first whose logit is the maximum; each other one takes a pass
+    Pick best[V], last[V];
 #pragma unroll
-        for (int j = 0; j < V; ++j) best[j] = kNoPick;
+    for (int j = 0; j < V; ++j) best[j] = {r[j].m, 0};
+#pragma unroll
+    for (int c = C - 1; c >= 0; --c)
+        if (uint32_t(c) < a.classes) {
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                if (widen(held[c].at(j)) == r[j].m) best[j].c = c;
+        }
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+        if (q[j].dead) best[j].x = -INFINITY;
+    put_top<V>(a, w, 0, best, q);
+    for (uint32_t rank = 1; rank < a.k; ++rank) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) forget_widened(held[c]);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            last[j] = best[j];
+            best[j] = {-INFINITY, -1};
+        }
 #pragma unroll
         for (int c = 0; c < C; ++c)
             if (uint32_t(c) < a.classes) {
@@ -185,8 +231,6 @@ __global__ void __launch_bounds__(256) k_label_held(LabelArgs a) {
                 for (int j = 0; j < V; ++j) consider(best[j], last[j], widen(held[c].at(j)), c);
             }
         put_top<V>(a, w, rank, best, q);
-#pragma unroll
-        for (int j = 0; j < V; ++j) last[j] = best[j];
     }
 }
 
@@ -194,7 +238,7 @@ __global__ void __launch_bounds__(256) k_label_held(LabelArgs a) {
 constexpr int kRunBlock = 8;                               // classes loaded at once
 constexpr int kRunWaves = 8;                               // at most
 
-template <typename T, int V>
+template <typename T, int V, bool F>
 __global__ void __launch_bounds__(64 * kRunWaves) k_label_run(LabelArgs a) {
     extern __shared__ float shared[];                      // [waves][V][4][64] sums, or [waves][V][2][64] picks
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
@@ -203,7 +247,7 @@ __global__ void __launch_bounds__(64 * kRunWaves) k_label_run(LabelArgs a) {
     const bool mine = blockIdx.x * 64 + lane < threads && wave == 0;   // writes the results
     const Place<V> w = place<V>(a, thread);
     const T *x = static_cast<const T *>(a.x) + w.o * a.xs[0] + w.i * a.xs[2];
-    const float *field = a.mean ? a.field + w.o * a.fs[0] + w.i * a.fs[2] : nullptr;
+    const float *field = F ? a.field + w.o * a.fs[0] + w.i * a.fs[2] : nullptr;
     const uint32_t share = (a.classes + waves - 1) / waves;
     const uint32_t c0 = min(a.classes, wave * share), c1 = min(a.classes, c0 + share);
     Sums r[V];
@@ -211,14 +255,14 @@ __global__ void __launch_bounds__(64 * kRunWaves) k_label_run(LabelArgs a) {
 #pragma unroll
     for (int j = 0; j < V; ++j) {
         r[j] = kNothing;
-        best[j] = kNoPick;
+        best[j] = {-INFINITY, c0 < c1 ? int32_t(c0) : -1};
     }
     for (uint32_t c = c0; c < c1; c += kRunBlock) {
         Pack<T, V> held[kRunBlock];
 #pragma unroll
         for (int u = 0; u < kRunBlock; ++u)
             if (c + u < c1) held[u] = load_pack<V>(x + (c + u) * a.xs[1], w.n, T{});
-        Sums part[V];
+        float size = 0.0f;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             float m = r[j].m;
@@ -226,34 +270,33 @@ __global__ void __launch_bounds__(64 * kRunWaves) k_label_run(LabelArgs a) {
             for (int u = 0; u < kRunBlock; ++u)
                 if (c + u < c1) m = fmaxf(m, widen(held[u].at(j)));
             lift(r[j], m);
-            part[j] = {m, 0.0f, 0.0f, 0.0f};
+            size = fmaxf(size, fabsf(m));
         }
 #pragma unroll
-        for (int u = 0; u < kRunBlock; ++u)
-            if (c + u < c1) {
-                if (field) {
-                    const Pack<float, V> phi = load_field<V>(field + (c + u) * a.fs[1], a.fs[2], w.n);
+        for (int u = 0; u < kRunBlock; ++u) forget_widened(held[u]);
+        by_kind<T, F>(size, a.entropy, [&](auto kind) __attribute__((always_inline)) {
+            typedef typename decltype(kind)::type R;
+            Sums some[V];
 #pragma unroll
-                    for (int j = 0; j < V; ++j) take<T>(part[j], widen(held[u].at(j)), a.entropy, phi.at(j));
-                } else {
+            for (int j = 0; j < V; ++j) some[j] = kNothing;
 #pragma unroll
-                    for (int j = 0; j < V; ++j) take<T>(part[j], widen(held[u].at(j)), a.entropy);
+            for (int u = 0; u < kRunBlock; ++u)
+                if (c + u < c1) {
+                    Pack<float, V> phi{};
+                    if (R::kMean) phi = load_field<V>(field + (c + u) * a.fs[1], a.fs[2], w.n);
+#pragma unroll
+                    for (int j = 0; j < V; ++j) R(r[j].m).take(some[j], widen(held[u].at(j)), phi.at(j));
                 }
-            }
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            r[j].s += part[j].s;
-            r[j].t += part[j].t;
-            r[j].f += part[j].f;
-        }
+            for (int j = 0; j < V; ++j) R(r[j].m).close(r[j], some[j]);
+        });
         if (a.k) {
 #pragma unroll
             for (int u = 0; u < kRunBlock; ++u)
                 if (c + u < c1) {
 #pragma unroll
                     for (int j = 0; j < V; ++j)
-                        if (best[j].c < 0 || larger(widen(held[u].at(j)), best[j].x))
-                            best[j] = {widen(held[u].at(j)), int32_t(c + u)};
+                        if (widen(held[u].at(j)) > best[j].x) best[j] = {widen(held[u].at(j)), int32_t(c + u)};
                 }
         }
     }
@@ -294,13 +337,11 @@ __global__ void __launch_bounds__(64 * kRunWaves) k_label_run(LabelArgs a) {
         put_found<V>(a, w, y, xl, q);
     }
     Pick last[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) last[j] = kNoPick;
     for (uint32_t rank = 0; rank < a.k; ++rank) {
         if (rank) {
             // the first was found on the way; each other one is a pass over the classes
 #pragma unroll
-            for (int j = 0; j < V; ++j) best[j] = kNoPick;
+            for (int j = 0; j < V; ++j) best[j] = {-INFINITY, -1};
             for (uint32_t c = c0; c < c1; ++c) {
                 const Pack<T, V> one = load_pack<V>(x + c * a.xs[1], w.n, T{});
 #pragma unroll
@@ -317,12 +358,12 @@ __global__ void __launch_bounds__(64 * kRunWaves) k_label_run(LabelArgs a) {
             __syncthreads();
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                best[j] = kNoPick;
+                best[j] = {-INFINITY, -1};
                 // shares of classes in rising number: of equal ones the first stays
                 for (uint32_t v = 0; v < waves; ++v) {
                     const float *p = shared + ((v * V + j) * 2) * 64 + lane;
                     const int32_t c = __float_as_int(p[64]);
-                    if (c >= 0 && (best[j].c < 0 || larger(p[0], best[j].x))) best[j] = {p[0], c};
+                    if (c >= 0 && (best[j].c < 0 || p[0] > best[j].x)) best[j] = {p[0], c};
                 }
             }
             __syncthreads();
@@ -383,14 +424,11 @@ __global__ void __launch_bounds__(256) k_label_grad_held(LabelGradArgs a) {
     const Place<V> w = place<V>(a, thread);
     const T *x = static_cast<const T *>(a.x) + w.o * a.xs[0] + w.i * a.xs[2];
     Pack<T, V> held[C];
-    constexpr bool Keep = F && C * V <= 64;                // the field too, or read it twice
-    Pack<float, V> phi[Keep ? C : 1];
     const float *const field = F ? a.field + w.o * a.fs[0] + w.i * a.fs[2] : nullptr;
 #pragma unroll
     for (int c = 0; c < C; ++c)
         if (uint32_t(c) < a.classes) {
             held[c] = load_pack<V>(x + c * a.xs[1], w.n, T{});
-            if constexpr (Keep) phi[c] = load_field<V>(field + c * a.fs[1], a.fs[2], w.n);
         }
     Sums r[V];
     Slope g[V];
@@ -402,16 +440,8 @@ __global__ void __launch_bounds__(256) k_label_grad_held(LabelGradArgs a) {
 #pragma unroll
             for (int j = 0; j < V; ++j) r[j].m = fmaxf(r[j].m, widen(held[c].at(j)));
         }
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-        if (uint32_t(c) < a.classes) {
-            if constexpr (F && !Keep) phi[0] = load_field<V>(field + c * a.fs[1], a.fs[2], w.n);
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                if constexpr (F) take<T>(r[j], widen(held[c].at(j)), a.up_entropy, phi[Keep ? c : 0].at(j));
-                else take<T>(r[j], widen(held[c].at(j)), a.up_entropy);
-            }
-        }
+    Pack<float, V> phi[kFieldHeld<C, V, F>];
+    held_sums<T, V, C, F>(r, held, a.classes, a.up_entropy, field, a.fs, w.n, phi);
 #pragma unroll
     for (int j = 0; j < V; ++j) {
         const Found q = found(r[j]);
@@ -425,8 +455,9 @@ __global__ void __launch_bounds__(256) k_label_grad_held(LabelGradArgs a) {
 #pragma unroll
     for (int c = 0; c < C; ++c)
         if (uint32_t(c) < a.classes) {
-            if constexpr (F && !Keep) phi[0] = load_field<V>(field + c * a.fs[1], a.fs[2], w.n);
-            put_slope<T, V, F>(a, w, c, held[c], phi[Keep ? c : 0], y, g);
+            constexpr bool kept = kFieldHeld<C, V, F> == C;
+            if constexpr (F && !kept) phi[0] = load_field<V>(field + c * a.fs[1], a.fs[2], w.n);
+            put_slope<T, V, F>(a, w, c, held[c], phi[kept ? c : 0], y, g);
         }
 }
 

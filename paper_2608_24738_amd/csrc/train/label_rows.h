@@ -7,7 +7,7 @@
 // Bound by the bytes of the logits; a row is read once.
 //
 // The k likeliest classes need no second reading either: a lane notes its
-// largest logit and the load it came with.  The wave's largest class then is
+// largest logit and the load it came with.  The wave's likeliest class then is
 // that of the lane that leads; only that lane's own classes, a 64 W-th of the
 // row, are looked through again for its next one, by the whole wave.  After k
 // rounds the waves' lists are merged by counting, for every candidate, the
@@ -24,20 +24,10 @@ struct RowPart {                                           // of one part of a r
     Sums sums;
 };
 
-__device__ __forceinline__ uint64_t shfl64(uint64_t v, int lane) {
-    return uint64_t(uint32_t(__shfl(int(v >> 32), lane))) << 32 | uint32_t(__shfl(int(v), lane));
-}
-__device__ __forceinline__ uint64_t wave_max(uint64_t v) {
-    for (int i = 32; i; i >>= 1) {
-        const uint64_t o = uint64_t(uint32_t(__shfl_xor(int(v >> 32), i))) << 32 | uint32_t(__shfl_xor(int(v), i));
-        v = v > o ? v : o;
-    }
-    return v;
-}
+// The sums of a wave's lanes together, the same in every lane.
 __device__ __forceinline__ Sums wave_join(Sums r) {
-    for (int i = 32; i; i >>= 1)
-        r = join(r, Sums{__shfl_xor(r.m, i), __shfl_xor(r.s, i), __shfl_xor(r.t, i), __shfl_xor(r.f, i)});
-    return r;
+    lift(r, wave_max(r.m));
+    return {r.m, wave_sum(r.s), wave_sum(r.t), wave_sum(r.f)};
 }
 
 // Results of row n (outer o, inner i) by one thread.
@@ -61,8 +51,8 @@ __device__ __forceinline__ void put_row_top(const LabelArgs &a, uint32_t o, uint
     a.top[at] = log_prob(q, unordered(uint32_t(key >> 32)));
 }
 
-// The first class of lane `owner` below `floor`, found by the whole wave.
-// `stride` classes lie between two loads of a lane.
+// The likeliest class of a lane below `floor`, found by the whole wave: the
+// lane's loads begin at `first`, `stride` classes apart.
 template <typename T, int V>
 __device__ __forceinline__ uint64_t next_of(const T *x, uint32_t first, uint32_t end, uint32_t stride, uint64_t floor) {
     const uint32_t lane = threadIdx.x & 63;
@@ -71,29 +61,29 @@ __device__ __forceinline__ uint64_t next_of(const T *x, uint32_t first, uint32_t
         const uint32_t n = min(uint32_t(V), end - uint32_t(c));
         const Pack<T, V> r = load_pack<V>(x + c, n, T{});
 #pragma unroll
-        for (int j = 0; j < V; ++j)
-            if (uint32_t(j) < n) {
-                const uint64_t key = top_key(widen(r.at(j)), uint32_t(c) + j);
-                if (key < floor && key > best) best = key;
-            }
+        for (int j = 0; j < V; ++j) {
+            const uint64_t key = top_key(widen(r.at(j)), uint32_t(c) + j);
+            if (uint32_t(j) < n && key < floor && key > best) best = key;
+        }
     }
     return wave_max(best);
 }
 
-template <typename T, int W>
-__global__ void __launch_bounds__(W == 1 ? 256 : 64 * W) k_label_rows(LabelArgs a) {
+template <typename T, int W, bool F>
+__global__ void __launch_bounds__(W == 1 ? 256 : 64 * W, F ? 4 : 8) k_label_rows(LabelArgs a) {
     constexpr int V = 16 / sizeof(T);
     constexpr uint32_t kStride = 64 * W * V;               // classes between two loads of a lane
     __shared__ Sums sums[W];
     __shared__ uint64_t keys[W][32];
     const uint32_t lane = threadIdx.x & 63, wave = W == 1 ? 0 : threadIdx.x >> 6;
     const uint32_t t = wave * 64 + lane;
-    const uint32_t n = W == 1 ? blockIdx.x * 4 + (threadIdx.x >> 6) : a.div_groups.div(blockIdx.x);
+    const uint32_t n = W == 1 ? blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)
+                              : a.div_groups.div(blockIdx.x);
     if (W == 1 && n >= a.n) return;                        // whole waves; nothing is shared between them
     const uint32_t part = W == 1 ? 0 : blockIdx.x - n * a.groups;
     const uint32_t o = a.div_inner.div(n), i = n - o * a.inner;
     const T *x = static_cast<const T *>(a.x) + o * a.xs[0] + i * a.xs[2];
-    const float *field = a.mean ? a.field + o * a.fs[0] + i * a.fs[2] : nullptr;
+    const float *field = F ? a.field + o * a.fs[0] + i * a.fs[2] : nullptr;
     // parts of whole strides
     const uint32_t strides = (a.classes + kStride - 1) / kStride, each = (strides + a.groups - 1) / a.groups;
     const uint32_t c0 = min(a.classes, part * each * kStride), end = min(a.classes, c0 + each * kStride);
@@ -102,74 +92,84 @@ __global__ void __launch_bounds__(W == 1 ? 256 : 64 * W) k_label_rows(LabelArgs 
     Sums r = kNothing;
     float best = -INFINITY;                                // the lane's largest logit, and the first class of its load
     uint32_t from = first;
-    // element by element where a load passes the end: those beyond are -inf
-    const T none = narrow<T>(-INFINITY);
-    for (uint64_t c = first; c < end; c += uint64_t(kRowLoads) * kStride) {
-        Pack<T, V> held[kRowLoads];
-        float most[kRowLoads];
+    const T none = narrow<T>(-INFINITY);                   // past the end
+    const auto run = [&](Pack<T, V> (&held)[kRowLoads], uint32_t c) __attribute__((always_inline)) {
+        float m = r.m;
 #pragma unroll
         for (int u = 0; u < kRowLoads; ++u) {
-            const uint64_t at = c + uint64_t(u) * kStride;
+            float most = widen(held[u].at(0));
+#pragma unroll
+            for (int j = 1; j < V; ++j) most = fmaxf(most, widen(held[u].at(j)));
+            const bool leads = most > best;
+            best = leads ? most : best;
+            from = leads ? c + u * kStride : from;
+            m = fmaxf(m, most);
+        }
+        lift(r, m);
+#pragma unroll
+        for (int u = 0; u < kRowLoads; ++u) forget_widened(held[u]);
+        by_kind<T, F>(fabsf(m), a.entropy, [&](auto kind) __attribute__((always_inline)) {
+            const typename decltype(kind)::type ref(m);
+            Sums some = kNothing;
+#pragma unroll
+            for (int u = 0; u < kRowLoads; ++u) {
+                const uint32_t at = c + u * kStride;
+                Pack<float, V> phi{};
+                if (ref.kMean && at < end) phi = load_field<V>(field + at * a.fs[1], a.fs[1], end - at);
+#pragma unroll
+                for (int j = 0; j < V; ++j) ref.take(some, widen(held[u].at(j)), phi.at(j));
+            }
+            ref.close(r, some);
+        });
+    };
+    // whole rounds of loads, then one that asks at every load whether it is there
+    uint32_t c = first;
+    uint32_t left = end - min(end, c0 + wave * 64 * V);    // from the wave's first class on
+    constexpr uint32_t kRound = kRowLoads * kStride;
+    for (; left >= kRound - kStride + 64 * V; left -= min(left, kRound), c += kRound) {
+        Pack<T, V> held[kRowLoads];
+#pragma unroll
+        for (int u = 0; u < kRowLoads; ++u) held[u] = load_pack<V>(x + c + u * kStride);
+        run(held, c);
+    }
+    if (c < end) {
+        Pack<T, V> held[kRowLoads];
+#pragma unroll
+        for (int u = 0; u < kRowLoads; ++u) {
+            const uint32_t at = c + u * kStride;
             if (at < end) {
-                held[u] = load_pack<V>(x + at, end - uint32_t(at), none);
+                held[u] = load_pack<V>(x + at, end - at, none);
             } else {
 #pragma unroll
                 for (int j = 0; j < V; ++j) held[u].put(j, none);
             }
         }
-        float m = r.m;
-#pragma unroll
-        for (int u = 0; u < kRowLoads; ++u) {
-            most[u] = widen(held[u].at(0));
-#pragma unroll
-            for (int j = 1; j < V; ++j) most[u] = fmaxf(most[u], widen(held[u].at(j)));
-            if (a.k && most[u] > best) {
-                best = most[u];
-                from = uint32_t(c + uint64_t(u) * kStride);
-            }
-            m = fmaxf(m, most[u]);
-        }
-        lift(r, m);
-        Sums some = {m, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int u = 0; u < kRowLoads; ++u) {
-            if (field) {
-                const uint64_t at = c + uint64_t(u) * kStride;
-                Pack<float, V> phi{};
-                if (at < end) phi = load_field<V>(field + at * a.fs[1], a.fs[1], end - uint32_t(at));
-#pragma unroll
-                for (int j = 0; j < V; ++j) take<T>(some, widen(held[u].at(j)), a.entropy, phi.at(j));
-            } else {
-#pragma unroll
-                for (int j = 0; j < V; ++j) take<T>(some, widen(held[u].at(j)), a.entropy);
-            }
-        }
-        r.s += some.s;
-        r.t += some.t;
-        r.f += some.f;
+        run(held, c);
     }
     r = wave_join(r);
 
     // the wave's k likeliest classes; lane j of the wave keeps the j-th
     uint64_t mine = 0;
     if (a.k) {
-        // an exact key once its lane has led, before that its load's: the
-        // largest logit with the first class of the load it came with, which
-        // orders lanes as the exact keys do
-        uint64_t key = first < end ? top_key(best, from) : 0;
-        bool exact = false;
-        for (uint32_t rank = 0; rank < a.k; ++rank) {
-            uint64_t lead = wave_max(key);
-            if (lead == 0) break;                          // no classes are left
-            const int owner = __ffsll(static_cast<long long>(__ballot(key == lead))) - 1;
-            const uint32_t start = uint32_t(__shfl(int(first), owner));
-            if (!__shfl(int(exact), owner)) lead = next_of<T, V>(x, start, end, kStride, ~uint64_t(0));
-            if (lane == rank) mine = lead;
-            const uint64_t next = next_of<T, V>(x, start, end, kStride, lead);
-            if (int(lane) == owner) {
-                key = next;
-                exact = true;
+        // the lane's likeliest class, exactly: within the load that it came with
+        uint64_t key = 0;
+        if (first < end) {
+            const uint32_t count = min(uint32_t(V), end - from);
+            const Pack<T, V> again = load_pack<V>(x + from, count, none);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const uint64_t one = top_key(widen(again.at(j)), from + j);
+                if (uint32_t(j) < count && one > key) key = one;
             }
+        }
+        for (uint32_t rank = 0; rank < a.k; ++rank) {
+            const uint64_t lead = wave_max(key);
+            if (lead == 0) break;                          // no classes are left
+            if (lane == rank) mine = lead;
+            if (rank + 1 == a.k) break;
+            const int owner = __ffsll(static_cast<long long>(__ballot(key == lead))) - 1;
+            const uint64_t next = next_of<T, V>(x, c0 + (wave * 64 + owner) * V, end, kStride, lead);
+            if (int(lane) == owner) key = next;
         }
     }
     if constexpr (W == 1) {
@@ -180,8 +180,7 @@ __global__ void __launch_bounds__(W == 1 ? 256 : 64 * W) k_label_rows(LabelArgs 
         if (lane == 0) sums[wave] = r;
         if (lane < a.k) keys[wave][lane] = mine;
         __syncthreads();
-        Sums all = kNothing;
-        for (int w = 0; w < W; ++w) all = join(all, sums[w]);
+        const Sums all = wave_join(lane < W ? sums[lane] : kNothing);
         const Found q = found(all);
         char *out = static_cast<char *>(a.partial) + uint64_t(blockIdx.x) * (sizeof(RowPart) + a.k * 8);
         if (t == 0) {
@@ -193,7 +192,8 @@ __global__ void __launch_bounds__(W == 1 ? 256 : 64 * W) k_label_rows(LabelArgs 
             const uint64_t key = keys[j / a.k][j % a.k];
             uint32_t rank = 0;
             for (uint32_t w = 0; w < W; ++w)
-                for (uint32_t v = 0; v < a.k; ++v) rank += keys[w][v] > key || (key == 0 && w * a.k + v < j && keys[w][v] == 0);
+                for (uint32_t v = 0; v < a.k; ++v)
+                    rank += keys[w][v] > key || (key == 0 && w * a.k + v < j && keys[w][v] == 0);
             if (rank < a.k) {
                 if (a.groups == 1) put_row_top(a, o, i, rank, key, q);
                 else reinterpret_cast<uint64_t *>(out + sizeof(RowPart))[rank] = key;
@@ -203,7 +203,7 @@ __global__ void __launch_bounds__(W == 1 ? 256 : 64 * W) k_label_rows(LabelArgs 
 }
 
 // Puts the parts of a row together, in their order.
-constexpr uint32_t kRowMostParts = 32;
+constexpr uint32_t kRowMostParts = 64;
 
 template <typename T>
 __global__ void __launch_bounds__(256) k_label_rows_join(LabelArgs a) {

@@ -141,6 +141,16 @@ __device__ __forceinline__ void store_pack(T *p, const Pack<T, V> &r, uint32_t n
         if (uint32_t(j) < n) p[j] = r.at(j);
 }
 
+// Makes the compiler take the elements out of their words again from here on:
+// kept widened from pass to pass they would need twice the registers.
+template <typename T, int V>
+__device__ __forceinline__ void forget_widened(Pack<T, V> &r) {
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int i = 0; i < Pack<T, V>::kWords; ++i) asm volatile("" : "+v"(r.w[i]));
+    }
+}
+
 // V floats rounded to T.
 template <typename T, int V>
 __device__ __forceinline__ Pack<T, V> narrow_pack(const float (&v)[V]) {
@@ -167,5 +177,42 @@ __device__ __forceinline__ Pack<T, V> narrow_pack(const float (&v)[V]) {
 
 // 2^x by the hardware's v_exp_f32 (results below 2^-126 flush to 0).
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// Reductions over a wave by data-parallel primitives: rows of 16 lanes by
+// shifts, then across rows by two broadcasts; lane 63 ends with the result,
+// which becomes uniform.  The order of the additions is fixed.
+template <int Ctrl, int Rows>
+__device__ __forceinline__ uint32_t dpp(uint32_t old, uint32_t x) {
+    return uint32_t(__builtin_amdgcn_update_dpp(int(old), int(x), Ctrl, Rows, 0xf, false));
+}
+template <typename F>
+__device__ __forceinline__ uint32_t wave_reduce(uint32_t x, uint32_t none, F op) {
+    x = op(x, dpp<0x111, 0xf>(none, x));                   // row_shr 1, 2, 4, 8
+    x = op(x, dpp<0x112, 0xf>(none, x));
+    x = op(x, dpp<0x114, 0xf>(none, x));
+    x = op(x, dpp<0x118, 0xf>(none, x));
+    x = op(x, dpp<0x142, 0xa>(none, x));                   // row_bcast 15 into rows 1 and 3, 31 into 2 and 3
+    x = op(x, dpp<0x143, 0xc>(none, x));
+    return uint32_t(__builtin_amdgcn_readlane(int(x), 63));
+}
+__device__ __forceinline__ float wave_max(float x) {       // not of NaN
+    return __uint_as_float(wave_reduce(__float_as_uint(x), 0xff800000u, [](uint32_t a, uint32_t b) {
+        return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+    }));
+}
+__device__ __forceinline__ float wave_sum(float x) {
+    return __uint_as_float(wave_reduce(__float_as_uint(x), 0u, [](uint32_t a, uint32_t b) {
+        return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+    }));
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+    return wave_reduce(x, 0u, [](uint32_t a, uint32_t b) { return max(a, b); });
+}
+// By halves: the largest upper word, then the largest lower word that has it.
+__device__ __forceinline__ uint64_t wave_max(uint64_t x) {
+    const uint32_t hi = wave_max(uint32_t(x >> 32));
+    const uint32_t lo = wave_max(uint32_t(x >> 32) == hi ? uint32_t(x) : 0u);
+    return uint64_t(hi) << 32 | lo;
+}
 
 }  // namespace tmtrain

@@ -64,6 +64,24 @@ int by_type(int dtype, F fn) {
     return fn(f16{});
 }
 
+template <int N>
+struct Int { static constexpr int value = N; };
+template <typename F>
+int by_waves(uint32_t waves, F fn) {
+    if (waves == 1) return fn(Int<1>{});
+    if (waves == 2) return fn(Int<2>{});
+    if (waves == 4) return fn(Int<4>{});
+    if (waves == 8) return fn(Int<8>{});
+    return fn(Int<16>{});
+}
+template <typename F>
+int by_held(int held, F fn) {
+    if (held == 4) return fn(Int<4>{});
+    if (held == 8) return fn(Int<8>{});
+    if (held == 16) return fn(Int<16>{});
+    return fn(Int<32>{});
+}
+
 // ---------------------------------------------------------------------------
 // Labels.
 // ---------------------------------------------------------------------------
@@ -130,14 +148,15 @@ int check_labels(const void *logits, int dtype, int64_t outer, int64_t classes, 
     return TM_OK;
 }
 
-constexpr uint64_t kBusyThreads = 65536;    // four waves to a SIMD
+constexpr uint64_t kBusyThreads = 65536;    // four waves to a CU
+constexpr uint64_t kRowBusyWaves = 8192;     // eight waves to a SIMD
 
 // How a request runs: on contiguous rows or on maps, with how many classes
 // held, positions to a thread and waves to a row or position.
 struct LabelPlan {
     bool rows;
     bool swap;                  // maps: the outer positions lie side by side, not the inner ones
-    bool wide;                  // maps: 16 bytes of positions to a thread
+    int wide;                   // maps: positions to a thread
     int held;                   // maps: classes held in registers, 0: they run through
     uint32_t waves;             // of a row, or sharing the classes of a map's positions
     uint32_t parts;             // of a row
@@ -151,18 +170,25 @@ LabelPlan label_plan(int dtype, uint64_t outer, uint64_t classes, uint64_t inner
     p.parts = 1;
     if ((strides[1] == 1 || classes == 1) && classes > 32) {
         p.rows = true;
-        // one wave while its lanes' first loads hold the row, then 4, then 16
-        p.waves = classes <= 64 * vec * kRowLoads ? 1 : classes <= 64 * 4 * vec * 2 * kRowLoads ? 4 : 16;
-        if (p.waves == 16 && n < 512)
-            p.parts = uint32_t(std::min<uint64_t>({kRowMostParts, ceil_div(classes, 64 * 16 * vec), ceil_div(512, n)}));
+        // as many waves as fill the chip, each lane with at least one round of loads
+        const uint64_t most = ceil_div(classes, 64 * vec * kRowLoads), want = ceil_div(kRowBusyWaves, n);
+        const uint64_t waves = std::min(most, want);
+        p.waves = waves <= 1 ? 1 : waves <= 2 ? 2 : waves <= 4 ? 4 : waves <= 8 ? 8 : 16;
+        if (want > 16) {
+            // few rows: parts of one load to a lane of four waves
+            p.waves = 4;
+            p.parts = uint32_t(std::min<uint64_t>({kRowMostParts, ceil_div(classes, 64 * 4 * vec), ceil_div(want, 4)}));
+            if (p.parts == 1 && classes <= 64 * vec) p.waves = 1;
+        }
         return p;
     }
     p.swap = inner == 1 && outer > 1 && strides[0] == 1;
     const uint64_t in = p.swap ? outer : inner, out = p.swap ? 1 : outer;
     const int64_t step = p.swap ? strides[0] : strides[2];
-    p.wide = step == 1 && out * ceil_div(in, vec) >= kBusyThreads / 2;
-    p.held = classes <= 4 ? 4 : classes <= 8 ? 8 : classes <= 16 ? 16 : 0;
-    const uint64_t threads = p.wide ? out * ceil_div(in, vec) : n;
+    p.held = classes <= 4 ? 4 : classes <= 8 ? 8 : classes <= 16 ? 16 : classes <= 32 ? 32 : 0;
+    p.wide = p.held == 0 ? kRunV : int((p.held <= 8 ? 16 : 8) / float_bytes(dtype));
+    if (step != 1 || out * ceil_div(in, p.wide) < kBusyThreads / 2) p.wide = 1;
+    const uint64_t threads = out * ceil_div(in, p.wide);
     p.waves = uint32_t(std::max<uint64_t>(1, std::min<uint64_t>({kRunWaves, kBusyThreads / threads, classes / 16})));
     return p;
 }
@@ -239,32 +265,36 @@ extern "C" int tm_label_logp(const void *logits, int dtype, int64_t outer, int64
     }
     a.div_inner = Div32::make(a.inner);
     a.partial = workspace;
+    const bool F = a.field;
     return by_type(dtype, [&](auto t) {
         using T = decltype(t);
-        constexpr int V = 16 / sizeof(T);
         if (p.rows) {
             a.groups = p.parts;
             a.div_groups = Div32::make(p.parts);
             if (s.positions * p.parts >= kLimit) return int(TM_ERR_TOO_LARGE);
-            if (p.waves == 1) return launch(k_label_rows<T, 1>, dim3((a.n + 3) / 4), dim3(256), 0, stream, a);
-            const int rc = p.waves == 4
-                ? launch(k_label_rows<T, 4>, dim3(a.n * p.parts), dim3(256), 0, stream, a)
-                : launch(k_label_rows<T, 16>, dim3(a.n * p.parts), dim3(1024), 0, stream, a);
+            const int rc = by_waves(p.waves, [&](auto waves) {
+                constexpr int W = decltype(waves)::value;
+                return launch(F ? k_label_rows<T, W, true> : k_label_rows<T, W, false>,
+                              dim3(W == 1 ? (a.n + 3) / 4 : a.n * p.parts), dim3(W == 1 ? 256 : 64 * W), 0, stream, a);
+            });
             if (rc != TM_OK || p.parts == 1) return rc;
             return launch(k_label_rows_join<T>, dim3(a.n), dim3(256), 0, stream, a);
         }
-        a.groups = p.wide ? (a.inner + V - 1) / V : a.inner;
+        a.groups = uint32_t(ceil_div(a.inner, p.wide));
         a.div_groups = Div32::make(a.groups);
         const uint32_t threads = a.outer * a.groups;
         if (p.held) {
-            void (*const kernels[])(LabelArgs) = {k_label_held<T, 1, 4>, k_label_held<T, 1, 8>, k_label_held<T, 1, 16>,
-                                                  k_label_held<T, V, 4>, k_label_held<T, V, 8>, k_label_held<T, V, 16>};
-            const int i = (p.wide ? 3 : 0) + (p.held == 4 ? 0 : p.held == 8 ? 1 : 2);
-            return launch(kernels[i], dim3((threads + 255) / 256), dim3(256), 0, stream, a);
+            return by_held(p.held, [&](auto held) {
+                constexpr int C = decltype(held)::value;
+                return launch(p.wide > 1 ? F ? k_label_held<T, kHeldV<T, C>, C, true> : k_label_held<T, kHeldV<T, C>, C, false>
+                                         : F ? k_label_held<T, 1, C, true> : k_label_held<T, 1, C, false>,
+                              dim3((threads + 255) / 256), dim3(256), 0, stream, a);
+            });
         }
-        const size_t lds = p.waves > 1 ? size_t(p.waves) * (p.wide ? V : 1) * 1024 : 0;
-        return launch(p.wide ? k_label_run<T, V> : k_label_run<T, 1>, dim3((threads + 63) / 64), dim3(64 * p.waves),
-                      lds, stream, a);
+        const size_t lds = p.waves > 1 ? size_t(p.waves) * p.wide * 1024 : 0;
+        return launch(p.wide > 1 ? F ? k_label_run<T, kRunV, true> : k_label_run<T, kRunV, false>
+                                 : F ? k_label_run<T, 1, true> : k_label_run<T, 1, false>,
+                      dim3((threads + 63) / 64), dim3(64 * p.waves), lds, stream, a);
     });
 }
 
@@ -318,11 +348,12 @@ extern "C" int tm_label_logp_grad(const void *logits, int dtype, int64_t outer, 
     a.n = uint32_t(s.positions);
     LabelPlan p = label_plan(dtype, s.n[0], s.n[1], s.n[2], strides);
     // rows and 16-byte stores need the gradient to lie as the logits do
-    if (classes > TM_LABEL_MAX_RECOMPUTE && p.rows && grad_strides[1] != 1) {
-        p.rows = p.swap = p.wide = false;
+    if (p.rows && grad_strides[1] != 1) {
+        p.rows = p.swap = false;
+        p.wide = 1;
         p.held = 0;
     }
-    if (p.wide && grad_strides[p.swap ? 0 : 2] != 1) p.wide = false;
+    if (grad_strides[p.swap ? 0 : 2] != 1) p.wide = 1;
     if (p.swap) {
         swap_positions(a);
         std::swap(a.gs[0], a.gs[2]);
@@ -330,11 +361,10 @@ extern "C" int tm_label_logp_grad(const void *logits, int dtype, int64_t outer, 
     a.div_inner = Div32::make(a.inner);
     return by_type(dtype, [&](auto t) {
         using T = decltype(t);
-        constexpr int V = 16 / sizeof(T);
         const bool F = a.field;
         if (p.rows) {
             // 8 loads to a thread, or one where that leaves CUs idle
-            const uint64_t load = 256 * V;
+            const uint64_t load = 256 * 16 / sizeof(T);
             a.share = uint32_t(load * (s.positions * ceil_div(s.n[1], 8 * load) < kFill ? 1 : 8));
             a.groups = uint32_t(ceil_div(s.n[1], a.share));
             a.div_groups = Div32::make(a.groups);
@@ -342,24 +372,23 @@ extern "C" int tm_label_logp_grad(const void *logits, int dtype, int64_t outer, 
             return launch(F ? k_label_grad_rows<T, true> : k_label_grad_rows<T, false>, dim3(a.n * a.groups), dim3(256),
                           0, stream, a);
         }
-        a.groups = p.wide ? (a.inner + V - 1) / V : a.inner;
+        a.groups = uint32_t(ceil_div(a.inner, p.wide));
         a.div_groups = Div32::make(a.groups);
         const uint32_t threads = a.outer * a.groups;
         const dim3 grid((threads + 255) / 256);
         if (p.held) {
-            void (*const kernels[])(LabelGradArgs) = {
-                k_label_grad_held<T, 1, 4, false>, k_label_grad_held<T, 1, 8, false>, k_label_grad_held<T, 1, 16, false>,
-                k_label_grad_held<T, V, 4, false>, k_label_grad_held<T, V, 8, false>, k_label_grad_held<T, V, 16, false>,
-                k_label_grad_held<T, 1, 4, true>, k_label_grad_held<T, 1, 8, true>, k_label_grad_held<T, 1, 16, true>,
-                k_label_grad_held<T, V, 4, true>, k_label_grad_held<T, V, 8, true>, k_label_grad_held<T, V, 16, true>};
-            const int i = (F ? 6 : 0) + (p.wide ? 3 : 0) + (p.held == 4 ? 0 : p.held == 8 ? 1 : 2);
-            return launch(kernels[i], grid, dim3(256), 0, stream, a);
+            return by_held(p.held, [&](auto held) {
+                constexpr int C = decltype(held)::value;
+                constexpr int HV = kHeldV<T, C>;
+                return launch(p.wide > 1 ? F ? k_label_grad_held<T, HV, C, true> : k_label_grad_held<T, HV, C, false>
+                                         : F ? k_label_grad_held<T, 1, C, true> : k_label_grad_held<T, 1, C, false>,
+                              grid, dim3(256), 0, stream, a);
+            });
         }
         const uint64_t shares = std::min<uint64_t>({ceil_div(kBusyThreads, threads), ceil_div(s.n[1], 8), 65535});
         a.share = uint32_t(ceil_div(s.n[1], shares));
-        void (*const kernels[])(LabelGradArgs) = {k_label_grad_run<T, 1, false>, k_label_grad_run<T, V, false>,
-                                                  k_label_grad_run<T, 1, true>, k_label_grad_run<T, V, true>};
-        return launch(kernels[(F ? 2 : 0) + (p.wide ? 1 : 0)],
+        return launch(p.wide > 1 ? F ? k_label_grad_run<T, kRunV, true> : k_label_grad_run<T, kRunV, false>
+                                 : F ? k_label_grad_run<T, 1, true> : k_label_grad_run<T, 1, false>,
                       dim3(grid.x, uint32_t(ceil_div(s.n[1], a.share))), dim3(256), 0, stream, a);
     });
 }

@@ -28,7 +28,7 @@ LABELS = {torch.uint8: 0, torch.int32: 2, torch.int64: 3}
 DISTANCES = {torch.int32: 2, torch.float32: 6}
 BIAS_METRICS = dict(METRICS, offset=3)
 MAX_TOP = 32
-MAX_RECOMPUTE = 16           # classes whose gradient needs no saved statistics
+MAX_RECOMPUTE = 32           # classes whose gradient needs no saved statistics
 MAX_BUCKETS = 256
 
 

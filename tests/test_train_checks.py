@@ -72,7 +72,7 @@ def test_label_grad_checks(lib):
     assert grad(lib, ua=None) == NULL
     assert grad(lib, labels=None) == NULL
     assert grad(lib, uf=F) == NULL                                 # no field
-    assert grad(lib, shape=(2, 17, 7), strides=(119, 7, 1), out_strides=(119, 7, 1)) == NULL   # no statistics
+    assert grad(lib, shape=(2, 33, 7), strides=(231, 7, 1), out_strides=(231, 7, 1)) == NULL   # no statistics
     assert grad(lib, stats=C, uh=F) == NULL                        # statistics without the entropy
     assert grad(lib, out=None) == NO_OUTPUT
     assert grad(lib, out=A) == ALIAS

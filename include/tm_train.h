@@ -50,8 +50,8 @@ enum {
  *                for the signed distance field of each class)
  *   out_top, out_index  l and number of the top_k classes with the largest
  *                logits, in falling order; equal logits by rising number
- *   out_stats    the largest logit and the log of the sum of exp(x - it), for
- *                tm_label_logp_grad
+ *   out_stats    a reference near the largest logit and the log of the sum of
+ *                exp(x - it), for tm_label_logp_grad
  *
  * A class with p_c = 0 adds nothing to the entropy and to the mean, whatever
  * its logit and field hold there.  Where every logit is -inf, log-probabilities

@@ -134,7 +134,6 @@ constexpr float kNear = 1000.0f;                           // factor - 1 < 6e-5,
 
 template <bool Near, bool Entropy, bool Mean>
 struct Ref {
-    static constexpr bool kMean = Mean;
     float m, mz;
 
     __device__ __forceinline__ explicit Ref(float m) : m(m), mz(m * kLog2e) {}
@@ -169,22 +168,17 @@ struct Ref {
     }
 };
 
-// f(Ref(m) of the kind that serves): m the reference, size the largest |m| of
-// the thread.  The kinds are told apart here and not class by class, where
-// the compiler makes a selection of every branch.
-template <bool Near, bool Entropy, bool Mean>
-struct Kind {
-    typedef Ref<Near, Entropy, Mean> type;
-};
-template <typename T, bool Mean, typename F>
-__device__ __forceinline__ void by_kind(float size, bool entropy, F f) {
-    constexpr bool Near = sizeof(T) == 2;
-    if (!Near || size > kNear) {
-        if (Mean || entropy) f(Kind<false, true, Mean>{});
-        else f(Kind<false, false, Mean>{});
+template <bool B>
+struct Bool { static constexpr bool value = B; };
+// f(Bool<near>): whether references up to `size` from 0 are near for logits of
+// type T.  Told apart here and not class by class.
+template <typename T, typename F>
+__device__ __forceinline__ void by_near(float size, F f) {
+    if constexpr (sizeof(T) == 2) {
+        if (size <= kNear) f(Bool<true>{});
+        else f(Bool<false>{});
     } else {
-        if (Mean || entropy) f(Kind<Near, true, Mean>{});
-        else f(Kind<Near, false, Mean>{});
+        f(Bool<false>{});
     }
 }
 
@@ -197,7 +191,7 @@ __device__ __forceinline__ Found found(const Sums &r) {
     Found q;
     q.dead = r.s == 0.0f;
     q.m = r.m;
-    q.logs = __builtin_amdgcn_logf(r.s) * kLn2;            // s is 0 or between 1/2 and 2^31: no subnormals
+    q.logs = __builtin_amdgcn_logf(r.s) * kLn2;            // s is 0 or between 1/2 and 2^45: no subnormals
     const float one = __builtin_amdgcn_rcpf(r.s);          // within 1 ulp
     q.entropy = q.dead ? 0.0f : fmaf(-r.t, one, q.logs);
     q.mean = q.dead ? 0.0f : r.f * one;
@@ -209,20 +203,51 @@ __device__ __forceinline__ float log_prob(const Found &q, float x) {
 // As tm_label_logp_grad reads it: probabilities of a dead position become 0.
 __device__ __forceinline__ float stats_logs(const Found &q) { return q.dead ? INFINITY : q.logs; }
 
-// The gradient of one class: p (f (field - mean) - a - h (l + entropy)) and a more for the label's.
+// The gradient of one class: p (f (field - mean) - a - h (l + entropy)) and a
+// more for the label's, a being 0 where there is no label.
 struct Slope {
     float m, logs, a, h, f, entropy, mean;
 };
-template <typename T, bool F>
-__device__ __forceinline__ float slope_of(const Slope &g, bool entropy, float x, float field) {
-    // x - m - log s; a dead position has log s = inf and so p = 0
-    const float l = below(x - g.m, g.logs);
-    // a 16-bit gradient hides the rounding of l log2(e)
-    const float p = sizeof(T) == 2 ? exp2_hw(l * kLog2e) : exp_of(l);
-    float v = -g.a;
-    if (entropy) v -= g.h * (l + g.entropy);
-    if constexpr (F) v += g.f * (field - g.mean);
-    return p == 0.0f ? 0.0f : p * v;
+
+// A position's slope, prepared: p = 2^z with z = x log2(e) - c, and the factor
+// of p is base + per z (+ f field).  Near as in Ref; a 16-bit gradient hides
+// that p is off by a factor as close to 1.
+template <bool Near, bool Entropy, bool Mean>
+struct Grad {
+    float base, per, f;         // per: of l
+    float m, logs, c;
+
+    __device__ __forceinline__ explicit Grad(const Slope &g)
+        : base(-g.a), per(-g.h), f(g.f), m(g.m), logs(g.logs), c((g.m + g.logs) * kLog2e) {
+        if constexpr (Entropy) base = fmaf(-g.h, g.entropy, base);
+        if constexpr (Mean) base = fmaf(-g.f, g.mean, base);
+        if constexpr (Near) per *= kLn2;
+    }
+    // extra: a for the label's class, else 0
+    __device__ __forceinline__ float at(float x, float field, float extra) const {
+        float p, l;
+        if constexpr (Near) {
+            l = fmaf(x, kLog2e, -c);                       // in units of log2
+            p = exp2_hw(l);
+            l = fmaxf(l, -300.0f);                         // 0 times a finite number; NaN comes from p
+        } else {
+            l = below(x - m, logs);                        // a dead position has log s = inf and so p = 0
+            p = exp_of(l);
+        }
+        float v = base;
+        if constexpr (Entropy) v = fmaf(per, l, v);
+        if constexpr (Mean) v = fmaf(f, p == 0.0f ? 0.0f : field, v);
+        return fmaf(p, v, extra);
+    }
+};
+
+// The largest distance from 0 among the positions' references; a dead one is far.
+template <int V>
+__device__ __forceinline__ float farthest(const Slope (&g)[V]) {
+    float size = 0.0f;
+#pragma unroll
+    for (int j = 0; j < V; ++j) size = fmaxf(size, fmaxf(fabsf(g[j].m), fabsf(g[j].logs)));
+    return size;
 }
 
 }  // namespace tmtrain

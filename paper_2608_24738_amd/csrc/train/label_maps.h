@@ -120,15 +120,24 @@ __device__ __forceinline__ void put_found(const LabelArgs &a, const Place<V> &w,
     }
 }
 
+// Up to 32 logits may as well stay widened.
+template <typename T, int V, int C>
+__device__ __forceinline__ void forget_held(Pack<T, V> (&held)[C]) {
+    if constexpr (V * C > 32) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) forget_widened(held[c]);
+    }
+}
+
 // Classes whose field is held too; others' is read again for the gradient.
 template <int C, int V, bool F>
 constexpr int kFieldHeld = F && C * V <= 32 ? C : 1;
 
 // The sums of held classes; r holds the maxima.
 // The field is left in `phi` as far as that has room.
-template <typename T, int V, int C, bool F, int P>
-__device__ __forceinline__ void held_sums(Sums (&r)[V], Pack<T, V> (&held)[C], uint32_t classes, bool entropy,
-                                          const float *field, const int64_t (&fs)[3], uint32_t n, Pack<float, V> (&phi)[P]) {
+template <typename T, int V, int C, bool E, bool F, int P>
+__device__ __forceinline__ void held_sums(Sums (&r)[V], Pack<T, V> (&held)[C], uint32_t classes, const float *field,
+                                          const int64_t (&fs)[3], uint32_t n, Pack<float, V> (&phi)[P]) {
     if constexpr (F && P == C) {
 #pragma unroll
         for (int c = 0; c < C; ++c)
@@ -137,10 +146,9 @@ __device__ __forceinline__ void held_sums(Sums (&r)[V], Pack<T, V> (&held)[C], u
     float size = 0.0f;
 #pragma unroll
     for (int j = 0; j < V; ++j) size = fmaxf(size, fabsf(r[j].m));
-#pragma unroll
-    for (int c = 0; c < C; ++c) forget_widened(held[c]);
-    by_kind<T, F>(size, entropy, [&](auto kind) __attribute__((always_inline)) {
-        typedef typename decltype(kind)::type R;
+    forget_held(held);
+    by_near<T>(size, [&](auto near) __attribute__((always_inline)) {
+        typedef Ref<decltype(near)::value, E, F> R;
         Sums some[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) some[j] = kNothing;
@@ -154,12 +162,12 @@ __device__ __forceinline__ void held_sums(Sums (&r)[V], Pack<T, V> (&held)[C], u
 #pragma unroll
         for (int j = 0; j < V; ++j) R(r[j].m).close(r[j], some[j]);
     });
-#pragma unroll
-    for (int c = 0; c < C; ++c) forget_widened(held[c]);
+    forget_held(held);
 }
 
-// At most C classes, held in registers.
-template <typename T, int V, int C, bool F>
+// At most C classes, held in registers.  E: with the entropy, F: with a field
+// (and the entropy, which then costs nothing).
+template <typename T, int V, int C, bool E, bool F>
 __global__ void __launch_bounds__(256) k_label_held(LabelArgs a) {
     const uint32_t thread = blockIdx.x * 256 + threadIdx.x;
     if (thread >= a.outer * a.groups) return;
@@ -185,8 +193,8 @@ __global__ void __launch_bounds__(256) k_label_held(LabelArgs a) {
             for (int j = 0; j < V; ++j) r[j].m = fmaxf(r[j].m, widen(held[c].at(j)));
         }
     const float *const field = F ? a.field + w.o * a.fs[0] + w.i * a.fs[2] : nullptr;
-    Pack<float, V> phi[kFieldHeld<C, V, F>];
-    held_sums<T, V, C, F>(r, held, a.classes, a.entropy, field, a.fs, w.n, phi);
+    Pack<float, V> phi[kFieldHeld<C, V, F>] = {};
+    held_sums<T, V, C, E, F>(r, held, a.classes, field, a.fs, w.n, phi);
     Found q[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) q[j] = found(r[j]);
@@ -199,8 +207,7 @@ __global__ void __launch_bounds__(256) k_label_held(LabelArgs a) {
     }
     put_found<V>(a, w, y, xl, q);
     if (!a.k) return;
-#pragma unroll
-    for (int c = 0; c < C; ++c) forget_widened(held[c]);
+    forget_held(held);
     // the likeliest class is the first whose logit is the maximum; each other one takes a pass
     Pick best[V], last[V];
 #pragma unroll
@@ -217,8 +224,7 @@ __global__ void __launch_bounds__(256) k_label_held(LabelArgs a) {
         if (q[j].dead) best[j].x = -INFINITY;
     put_top<V>(a, w, 0, best, q);
     for (uint32_t rank = 1; rank < a.k; ++rank) {
-#pragma unroll
-        for (int c = 0; c < C; ++c) forget_widened(held[c]);
+        forget_held(held);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             last[j] = best[j];
@@ -238,7 +244,7 @@ __global__ void __launch_bounds__(256) k_label_held(LabelArgs a) {
 constexpr int kRunBlock = 8;                               // classes loaded at once
 constexpr int kRunWaves = 8;                               // at most
 
-template <typename T, int V, bool F>
+template <typename T, int V, bool E, bool F>
 __global__ void __launch_bounds__(64 * kRunWaves) k_label_run(LabelArgs a) {
     extern __shared__ float shared[];                      // [waves][V][4][64] sums, or [waves][V][2][64] picks
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
@@ -274,8 +280,8 @@ __global__ void __launch_bounds__(64 * kRunWaves) k_label_run(LabelArgs a) {
         }
 #pragma unroll
         for (int u = 0; u < kRunBlock; ++u) forget_widened(held[u]);
-        by_kind<T, F>(size, a.entropy, [&](auto kind) __attribute__((always_inline)) {
-            typedef typename decltype(kind)::type R;
+        by_near<T>(size, [&](auto near) __attribute__((always_inline)) {
+            typedef Ref<decltype(near)::value, E, F> R;
             Sums some[V];
 #pragma unroll
             for (int j = 0; j < V; ++j) some[j] = kNothing;
@@ -283,7 +289,7 @@ __global__ void __launch_bounds__(64 * kRunWaves) k_label_run(LabelArgs a) {
             for (int u = 0; u < kRunBlock; ++u)
                 if (c + u < c1) {
                     Pack<float, V> phi{};
-                    if (R::kMean) phi = load_field<V>(field + (c + u) * a.fs[1], a.fs[2], w.n);
+                    if (F) phi = load_field<V>(field + (c + u) * a.fs[1], a.fs[2], w.n);
 #pragma unroll
                     for (int j = 0; j < V; ++j) R(r[j].m).take(some[j], widen(held[u].at(j)), phi.at(j));
                 }
@@ -395,16 +401,14 @@ __device__ __forceinline__ void load_upstream(const LabelGradArgs &a, const Plac
 }
 
 // One class of V positions.
-template <typename T, int V, bool F>
+template <typename T, int V, typename G>
 __device__ __forceinline__ void put_slope(const LabelGradArgs &a, const Place<V> &w, uint32_t c, const Pack<T, V> &x,
                                           const Pack<float, V> &phi, const int32_t (&y)[V], const Slope (&g)[V]) {
     T *out = static_cast<T *>(a.grad) + w.o * a.gs[0] + c * a.gs[1] + w.i * a.gs[2];
     float v[V];
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-        v[j] = slope_of<T, F>(g[j], a.up_entropy, widen(x.at(j)), F ? phi.at(j) : 0.0f);
-        v[j] = y[j] == int32_t(c) ? v[j] + g[j].a : v[j];
-    }
+    for (int j = 0; j < V; ++j)
+        v[j] = G(g[j]).at(widen(x.at(j)), phi.at(j), y[j] == int32_t(c) ? g[j].a : 0.0f);
     const Pack<T, V> r = narrow_pack<T, V>(v);
     if (V == 1 || a.gs[2] == 1) {
         store_pack<V>(out, r, w.n);
@@ -417,7 +421,7 @@ __device__ __forceinline__ void put_slope(const LabelGradArgs &a, const Place<V>
 
 // At most C classes: the sums are made anew, which reads nothing but the
 // logits that the gradient needs anyway.
-template <typename T, int V, int C, bool F>
+template <typename T, int V, int C, bool E, bool F>
 __global__ void __launch_bounds__(256) k_label_grad_held(LabelGradArgs a) {
     const uint32_t thread = blockIdx.x * 256 + threadIdx.x;
     if (thread >= a.outer * a.groups) return;
@@ -440,8 +444,8 @@ __global__ void __launch_bounds__(256) k_label_grad_held(LabelGradArgs a) {
 #pragma unroll
             for (int j = 0; j < V; ++j) r[j].m = fmaxf(r[j].m, widen(held[c].at(j)));
         }
-    Pack<float, V> phi[kFieldHeld<C, V, F>];
-    held_sums<T, V, C, F>(r, held, a.classes, a.up_entropy, field, a.fs, w.n, phi);
+    Pack<float, V> phi[kFieldHeld<C, V, F>] = {};
+    held_sums<T, V, C, E, F>(r, held, a.classes, field, a.fs, w.n, phi);
 #pragma unroll
     for (int j = 0; j < V; ++j) {
         const Found q = found(r[j]);
@@ -452,18 +456,20 @@ __global__ void __launch_bounds__(256) k_label_grad_held(LabelGradArgs a) {
     }
     int32_t y[V];
     load_upstream<V>(a, w, y, g);
+    by_near<T>(farthest(g), [&](auto near) __attribute__((always_inline)) {
 #pragma unroll
-    for (int c = 0; c < C; ++c)
-        if (uint32_t(c) < a.classes) {
-            constexpr bool kept = kFieldHeld<C, V, F> == C;
-            if constexpr (F && !kept) phi[0] = load_field<V>(field + c * a.fs[1], a.fs[2], w.n);
-            put_slope<T, V, F>(a, w, c, held[c], phi[kept ? c : 0], y, g);
-        }
+        for (int c = 0; c < C; ++c)
+            if (uint32_t(c) < a.classes) {
+                constexpr bool kept = kFieldHeld<C, V, F> == C;
+                if constexpr (F && !kept) phi[0] = load_field<V>(field + c * a.fs[1], a.fs[2], w.n);
+                put_slope<T, V, Grad<decltype(near)::value, E, F>>(a, w, c, held[c], phi[F && kept ? c : 0], y, g);
+            }
+    });
 }
 
 // Any number of classes, with the forward call's statistics; blockIdx.y takes
 // a share of the classes.
-template <typename T, int V, bool F>
+template <typename T, int V, bool E, bool F>
 __global__ void __launch_bounds__(256) k_label_grad_run(LabelGradArgs a) {
     const uint32_t thread = blockIdx.x * 256 + threadIdx.x;
     if (thread >= a.outer * a.groups) return;
@@ -473,7 +479,7 @@ __global__ void __launch_bounds__(256) k_label_grad_run(LabelGradArgs a) {
     Slope g[V];
     const Pack<float, 2 * V> st = load_pack<2 * V>(a.stats + 2 * w.at, 2 * w.n, 0.0f);
     Pack<float, V> entropy{}, mean{};
-    if (a.up_entropy) entropy = load_pack<V>(a.entropy + w.at, w.n, 0.0f);
+    if (E && a.up_entropy) entropy = load_pack<V>(a.entropy + w.at, w.n, 0.0f);
     if constexpr (F) mean = load_pack<V>(a.mean + w.at, w.n, 0.0f);
 #pragma unroll
     for (int j = 0; j < V; ++j) {
@@ -484,21 +490,24 @@ __global__ void __launch_bounds__(256) k_label_grad_run(LabelGradArgs a) {
     }
     int32_t y[V];
     load_upstream<V>(a, w, y, g);
-    for (uint32_t c = c0; c < c1; c += 4) {
-        Pack<T, V> held[4];
-        Pack<float, V> phi[F ? 4 : 1];
+    by_near<T>(farthest(g), [&](auto near) __attribute__((always_inline)) {
+        for (uint32_t c = c0; c < c1; c += 4) {
+            Pack<T, V> held[4];
+            Pack<float, V> phi[F ? 4 : 1] = {};
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
-            if (c + u < c1) {
-                held[u] = load_pack<V>(x + (c + u) * a.xs[1], w.n, T{});
-                if constexpr (F)
-                    phi[u] = load_field<V>(a.field + w.o * a.fs[0] + (c + u) * a.fs[1] + w.i * a.fs[2], a.fs[2],
-                                              w.n);
-            }
+            for (int u = 0; u < 4; ++u)
+                if (c + u < c1) {
+                    held[u] = load_pack<V>(x + (c + u) * a.xs[1], w.n, T{});
+                    if constexpr (F)
+                        phi[u] = load_field<V>(a.field + w.o * a.fs[0] + (c + u) * a.fs[1] + w.i * a.fs[2], a.fs[2],
+                                               w.n);
+                }
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
-            if (c + u < c1) put_slope<T, V, F>(a, w, c + u, held[u], phi[F ? u : 0], y, g);
-    }
+            for (int u = 0; u < 4; ++u)
+                if (c + u < c1)
+                    put_slope<T, V, Grad<decltype(near)::value, E, F>>(a, w, c + u, held[u], phi[F ? u : 0], y, g);
+        }
+    });
 }
 
 }  // namespace tmtrain

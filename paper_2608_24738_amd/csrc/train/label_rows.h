@@ -47,34 +47,58 @@ __device__ __forceinline__ void put_row(const LabelArgs &a, uint32_t n, const T 
 __device__ __forceinline__ void put_row_top(const LabelArgs &a, uint32_t o, uint32_t i, uint32_t rank, uint64_t key,
                                             const Found &q) {
     const int64_t at = o * a.ts[0] + rank * a.ts[1] + i * a.ts[2];
-    a.index[at] = int32_t(~uint32_t(key));
+    // a row with NaN may have fewer classes in order than were asked for
+    a.index[at] = key ? int32_t(~uint32_t(key)) : 0;
     a.top[at] = log_prob(q, unordered(uint32_t(key >> 32)));
 }
 
-// The likeliest class of a lane below `floor`, found by the whole wave: the
-// lane's loads begin at `first`, `stride` classes apart.
+// The likeliest class of a lane behind `last` in the order of the
+// alternatives, found by the whole wave: the lane's loads begin at `first`,
+// `stride` classes apart.
 template <typename T, int V>
-__device__ __forceinline__ uint64_t next_of(const T *x, uint32_t first, uint32_t end, uint32_t stride, uint64_t floor) {
-    const uint32_t lane = threadIdx.x & 63;
-    uint64_t best = 0;
+__device__ __forceinline__ uint64_t next_of(const T *x, uint32_t first, uint32_t end, uint32_t stride, uint64_t last) {
+    const float lx = unordered(uint32_t(last >> 32));
+    const uint32_t lc = ~uint32_t(last), lane = threadIdx.x & 63;
+    float best = -INFINITY;
+    uint32_t at = ~0u;                                     // none
     for (uint64_t c = first + uint64_t(lane) * stride; c < end; c += uint64_t(64) * stride) {
         const uint32_t n = min(uint32_t(V), end - uint32_t(c));
         const Pack<T, V> r = load_pack<V>(x + c, n, T{});
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            const uint64_t key = top_key(widen(r.at(j)), uint32_t(c) + j);
-            if (uint32_t(j) < n && key < floor && key > best) best = key;
+            const float v = widen(r.at(j));
+            const bool open = uint32_t(j) < n && (v < lx || (v == lx && uint32_t(c) + j > lc));
+            if (open && (v > best || at == ~0u)) {
+                best = v;
+                at = uint32_t(c) + j;
+            }
         }
     }
-    return wave_max(best);
+    return wave_max(at == ~0u ? 0 : top_key(best, at));
 }
 
-template <typename T, int W, bool F>
-__global__ void __launch_bounds__(W == 1 ? 256 : 64 * W, F ? 4 : 8) k_label_rows(LabelArgs a) {
+// The k largest of `count` <= 64 falling lists of k keys in LDS, by one wave:
+// lane j gets the j-th.  0 where there are no more.
+__device__ __forceinline__ uint64_t merge_lists(const uint64_t *lists, uint32_t count, uint32_t k) {
+    const uint32_t lane = threadIdx.x & 63;
+    uint32_t at = 0;
+    uint64_t mine = 0, key = lane < count ? lists[lane * k] : 0;
+    for (uint32_t rank = 0; rank < k; ++rank) {
+        const uint64_t lead = wave_max(key);
+        if (lead == 0) break;
+        if (lane == rank) mine = lead;
+        if (key == lead) key = ++at < k ? lists[lane * k + at] : 0;
+    }
+    return mine;
+}
+
+// E: with the entropy, F: with a field (and the entropy), K: with the likeliest classes.
+template <typename T, int W, bool E, bool F, bool K>
+__global__ void __launch_bounds__(W == 1 ? 256 : 64 * W, K && !F ? 7 : 4) k_label_rows(LabelArgs a) {
     constexpr int V = 16 / sizeof(T);
     constexpr uint32_t kStride = 64 * W * V;               // classes between two loads of a lane
     __shared__ Sums sums[W];
-    __shared__ uint64_t keys[W][32];
+    __shared__ uint64_t keys[W * 32], leads[W];
     const uint32_t lane = threadIdx.x & 63, wave = W == 1 ? 0 : threadIdx.x >> 6;
     const uint32_t t = wave * 64 + lane;
     const uint32_t n = W == 1 ? blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)
@@ -93,147 +117,172 @@ __global__ void __launch_bounds__(W == 1 ? 256 : 64 * W, F ? 4 : 8) k_label_rows
     float best = -INFINITY;                                // the lane's largest logit, and the first class of its load
     uint32_t from = first;
     const T none = narrow<T>(-INFINITY);                   // past the end
-    const auto run = [&](Pack<T, V> (&held)[kRowLoads], uint32_t c) __attribute__((always_inline)) {
-        float m = r.m;
+    // 16-bit logits, none of the likeliest asked for: a round against the
+    // reference so far, which is as good as the maximum until a sum outgrows it
+    const auto stride_over = [&](const Pack<T, V> (&held)[kRowLoads], uint32_t c) __attribute__((always_inline)) {
+        const Ref<true, E, F> ref(r.m);
+        Sums some = kNothing;
 #pragma unroll
         for (int u = 0; u < kRowLoads; ++u) {
+            Pack<float, V> phi{};
+            if constexpr (F) phi = load_field<V>(field + (c + u * kStride) * a.fs[1], a.fs[1], V);
+#pragma unroll
+            for (int j = 0; j < V; ++j) ref.take(some, widen(held[u].at(j)), phi.at(j));
+            __builtin_amdgcn_sched_barrier(0);             // one load's terms at a time: registers
+        }
+        if (!__all(some.s < 1e4f)) return false;           // nor NaN
+        ref.close(r, some);
+        return true;
+    };
+    const auto run = [&](auto &held, uint32_t c) __attribute__((always_inline)) {
+        constexpr int N = sizeof(held) / sizeof(held[0]);
+        float m = r.m;
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
             float most = widen(held[u].at(0));
 #pragma unroll
             for (int j = 1; j < V; ++j) most = fmaxf(most, widen(held[u].at(j)));
-            const bool leads = most > best;
-            best = leads ? most : best;
-            from = leads ? c + u * kStride : from;
+            if constexpr (K) {
+                const bool leads = most > best;
+                best = leads ? most : best;
+                from = leads ? c + u * kStride : from;
+            }
             m = fmaxf(m, most);
         }
         lift(r, m);
 #pragma unroll
-        for (int u = 0; u < kRowLoads; ++u) forget_widened(held[u]);
-        by_kind<T, F>(fabsf(m), a.entropy, [&](auto kind) __attribute__((always_inline)) {
-            const typename decltype(kind)::type ref(m);
+        for (int u = 0; u < N; ++u) forget_widened(held[u]);
+        by_near<T>(fabsf(m), [&](auto near) __attribute__((always_inline)) {
+            const Ref<decltype(near)::value, E, F> ref(m);
             Sums some = kNothing;
 #pragma unroll
-            for (int u = 0; u < kRowLoads; ++u) {
+            for (int u = 0; u < N; ++u) {
                 const uint32_t at = c + u * kStride;
                 Pack<float, V> phi{};
-                if (ref.kMean && at < end) phi = load_field<V>(field + at * a.fs[1], a.fs[1], end - at);
+                if constexpr (F) phi = load_field<V>(field + at * a.fs[1], a.fs[1], end - at);
 #pragma unroll
                 for (int j = 0; j < V; ++j) ref.take(some, widen(held[u].at(j)), phi.at(j));
+                __builtin_amdgcn_sched_barrier(0);         // one load's terms at a time: registers
             }
             ref.close(r, some);
         });
     };
-    // whole rounds of loads, then one that asks at every load whether it is there
+    // whole rounds of loads, then one load after the other
     uint32_t c = first;
-    uint32_t left = end - min(end, c0 + wave * 64 * V);    // from the wave's first class on
     constexpr uint32_t kRound = kRowLoads * kStride;
-    for (; left >= kRound - kStride + 64 * V; left -= min(left, kRound), c += kRound) {
+    uint32_t rounds = 0;                                   // of the wave, all of its lanes' loads whole
+    const uint32_t own = end - min(end, c0 + wave * 64 * V);
+    if (own >= kRound - kStride + 64 * V) rounds = (own - (kRound - kStride + 64 * V)) / kRound + 1;
+    if (sizeof(T) == 2 && !K && rounds > 1) {
+        Pack<T, V> first_load[1] = {load_pack<V>(x + c)};
+        run(first_load, c);
+        c += kStride;
+        for (--rounds; rounds && __all(fabsf(r.m) <= kNear); --rounds, c += kRound) {
+            Pack<T, V> held[kRowLoads];
+#pragma unroll
+            for (int u = 0; u < kRowLoads; ++u) held[u] = load_pack<V>(x + c + u * kStride);
+            if (!stride_over(held, c)) break;
+        }
+    }
+    for (; rounds; --rounds, c += kRound) {
         Pack<T, V> held[kRowLoads];
 #pragma unroll
         for (int u = 0; u < kRowLoads; ++u) held[u] = load_pack<V>(x + c + u * kStride);
         run(held, c);
     }
-    if (c < end) {
-        Pack<T, V> held[kRowLoads];
-#pragma unroll
-        for (int u = 0; u < kRowLoads; ++u) {
-            const uint32_t at = c + u * kStride;
-            if (at < end) {
-                held[u] = load_pack<V>(x + at, end - at, none);
-            } else {
-#pragma unroll
-                for (int j = 0; j < V; ++j) held[u].put(j, none);
-            }
-        }
+    for (; c < end; c += kStride) {
+        Pack<T, V> held[1] = {load_pack<V>(x + c, end - c, none)};
         run(held, c);
     }
     r = wave_join(r);
 
-    // the wave's k likeliest classes; lane j of the wave keeps the j-th
-    uint64_t mine = 0;
-    if (a.k) {
-        // the lane's likeliest class, exactly: within the load that it came with
-        uint64_t key = 0;
+    // the lane's likeliest class, exactly: within the load that it came with
+    uint64_t key = 0, mine = 0, lead = 0, least = 0;
+    if constexpr (K) {
         if (first < end) {
             const uint32_t count = min(uint32_t(V), end - from);
             const Pack<T, V> again = load_pack<V>(x + from, count, none);
+            uint32_t at = ~0u;
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const uint64_t one = top_key(widen(again.at(j)), from + j);
-                if (uint32_t(j) < count && one > key) key = one;
-            }
+            for (int j = V - 1; j >= 0; --j)
+                if (uint32_t(j) < count && widen(again.at(j)) == best) at = from + j;
+            if (at != ~0u) key = top_key(best, at);
         }
-        for (uint32_t rank = 0; rank < a.k; ++rank) {
-            const uint64_t lead = wave_max(key);
-            if (lead == 0) break;                          // no classes are left
-            if (lane == rank) mine = lead;
-            if (rank + 1 == a.k) break;
-            const int owner = __ffsll(static_cast<long long>(__ballot(key == lead))) - 1;
-            const uint64_t next = next_of<T, V>(x, c0 + (wave * 64 + owner) * V, end, kStride, lead);
-            if (int(lane) == owner) key = next;
+        lead = wave_max(key);
+    }
+    if constexpr (W > 1) {
+        if (lane == 0) {
+            sums[wave] = r;
+            leads[wave] = lead;
         }
+        __syncthreads();
+        // classes behind the k-th best wave's likeliest are not among the k
+        if (K && a.k <= W) {
+            const uint64_t one = lane < W ? leads[lane] : 0;
+            uint32_t above = 0;
+            for (int w = 0; w < W; ++w) above += leads[w] > one;
+            const uint64_t kth = __ballot(lane < W && above == a.k - 1);
+            if (kth) least = leads[__ffsll(static_cast<long long>(kth)) - 1];
+        }
+    }
+    // the wave's k likeliest classes; lane j keeps the j-th
+    for (uint32_t rank = 0; K && rank < a.k; ++rank) {
+        if (lead == 0 || lead < least) break;
+        if (lane == rank) mine = lead;
+        if (rank + 1 == a.k) break;
+        const int owner = __ffsll(static_cast<long long>(__ballot(key == lead))) - 1;
+        const uint64_t next = next_of<T, V>(x, c0 + (wave * 64 + owner) * V, end, kStride, lead);
+        if (int(lane) == owner) key = next;
+        lead = wave_max(key);
     }
     if constexpr (W == 1) {
         const Found q = found(r);
         if (lane == 0) put_row(a, n, x, q);
-        if (lane < a.k) put_row_top(a, o, i, lane, mine, q);
+        if (K && lane < a.k) put_row_top(a, o, i, lane, mine, q);
     } else {
-        if (lane == 0) sums[wave] = r;
-        if (lane < a.k) keys[wave][lane] = mine;
+        if (K && lane < a.k) keys[wave * a.k + lane] = mine;
         __syncthreads();
+        if (wave > 0) return;
         const Sums all = wave_join(lane < W ? sums[lane] : kNothing);
-        const Found q = found(all);
-        char *out = static_cast<char *>(a.partial) + uint64_t(blockIdx.x) * (sizeof(RowPart) + a.k * 8);
-        if (t == 0) {
-            if (a.groups == 1) put_row(a, n, x, q);
-            else reinterpret_cast<RowPart *>(out)->sums = all;
-        }
-        // a candidate's place is the number of larger ones; empty places (0) come last, in any order
-        for (uint32_t j = t; j < W * a.k; j += 64 * W) {
-            const uint64_t key = keys[j / a.k][j % a.k];
-            uint32_t rank = 0;
-            for (uint32_t w = 0; w < W; ++w)
-                for (uint32_t v = 0; v < a.k; ++v)
-                    rank += keys[w][v] > key || (key == 0 && w * a.k + v < j && keys[w][v] == 0);
-            if (rank < a.k) {
-                if (a.groups == 1) put_row_top(a, o, i, rank, key, q);
-                else reinterpret_cast<uint64_t *>(out + sizeof(RowPart))[rank] = key;
-            }
+        if constexpr (K) mine = merge_lists(keys, W, a.k);
+        if (a.groups == 1) {
+            const Found q = found(all);
+            if (lane == 0) put_row(a, n, x, q);
+            if (K && lane < a.k) put_row_top(a, o, i, lane, mine, q);
+        } else {
+            char *out = static_cast<char *>(a.partial) + uint64_t(blockIdx.x) * (sizeof(RowPart) + a.k * 8);
+            if (lane == 0) reinterpret_cast<RowPart *>(out)->sums = all;
+            if (K && lane < a.k) reinterpret_cast<uint64_t *>(out + sizeof(RowPart))[lane] = mine;
         }
     }
 }
 
-// Puts the parts of a row together, in their order.
+// Puts the parts of a row together: a lane for each.
 constexpr uint32_t kRowMostParts = 64;
 
 template <typename T>
-__global__ void __launch_bounds__(256) k_label_rows_join(LabelArgs a) {
+__global__ void __launch_bounds__(64) k_label_rows_join(LabelArgs a) {
     __shared__ uint64_t keys[kRowMostParts * 32];
-    const uint32_t n = blockIdx.x;
+    const uint32_t n = blockIdx.x, lane = threadIdx.x;
     const uint32_t o = a.div_inner.div(n), i = n - o * a.inner;
     const T *x = static_cast<const T *>(a.x) + o * a.xs[0] + i * a.xs[2];
     const uint64_t size = sizeof(RowPart) + a.k * 8;
-    const char *in = static_cast<const char *>(a.partial) + uint64_t(n) * a.groups * size;
+    const char *in = static_cast<const char *>(a.partial) + uint64_t(n) * a.groups * size + lane * size;
     Sums r = kNothing;
-    for (uint32_t p = threadIdx.x & 63; p < a.groups; p += 64)
-        r = join(r, reinterpret_cast<const RowPart *>(in + p * size)->sums);
-    const Found q = found(wave_join(r));
-    if (threadIdx.x == 0) put_row(a, n, x, q);
-    const uint32_t count = a.groups * a.k;
-    for (uint32_t j = threadIdx.x; j < count; j += 256)
-        keys[j] = reinterpret_cast<const uint64_t *>(in + j / a.k * size + sizeof(RowPart))[j % a.k];
-    __syncthreads();
-    for (uint32_t j = threadIdx.x; j < count; j += 256) {
-        const uint64_t key = keys[j];
-        if (key == 0) continue;
-        uint32_t rank = 0;
-        for (uint32_t v = 0; v < count; ++v) rank += keys[v] > key;
-        if (rank < a.k) put_row_top(a, o, i, rank, key, q);
+    if (lane < a.groups) {
+        r = reinterpret_cast<const RowPart *>(in)->sums;
+        for (uint32_t j = 0; j < a.k; ++j) keys[lane * a.k + j] = reinterpret_cast<const uint64_t *>(in + sizeof(RowPart))[j];
     }
+    const Found q = found(wave_join(r));
+    if (lane == 0) put_row(a, n, x, q);
+    __syncthreads();
+    const uint64_t mine = merge_lists(keys, a.groups, a.k);
+    if (lane < a.k) put_row_top(a, o, i, lane, mine, q);
 }
 
 // Gradient of rows, with the forward call's statistics: part blockIdx.x of the
 // rows' classes, 256 threads.
-template <typename T, bool F>
+template <typename T, bool E, bool F>
 __global__ void __launch_bounds__(256) k_label_grad_rows(LabelGradArgs a) {
     constexpr int V = 16 / sizeof(T);
     const uint32_t n = a.div_groups.div(blockIdx.x), part = blockIdx.x - n * a.groups;
@@ -251,30 +300,34 @@ __global__ void __launch_bounds__(256) k_label_grad_rows(LabelGradArgs a) {
     g.a = y < 0 || g.logs == INFINITY ? 0.0f : a.up_logp[n];
     g.h = a.up_entropy ? a.up_entropy[n] : 0.0f;
     g.f = F ? a.up_mean[n] : 0.0f;
-    for (uint64_t c = c0 + threadIdx.x * V; c < end; c += 256 * V * 2) {
-        Pack<T, V> held[2];
+    const Slope all[1] = {g};
+    by_near<T>(farthest(all), [&](auto near) __attribute__((always_inline)) {
+        const Grad<decltype(near)::value, E, F> grad(g);
+        for (uint32_t c = c0 + threadIdx.x * V; c < end; c += 256 * V * 2) {
+            Pack<T, V> held[2];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const uint64_t at = c + u * 256 * V;
-            if (at < end) held[u] = load_pack<V>(x + at, end - uint32_t(at), T{});
-        }
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const uint64_t at = c + u * 256 * V;
-            if (at >= end) break;
-            Pack<float, V> phi{};
-            if constexpr (F) phi = load_field<V>(field + at * a.fs[1], a.fs[1], end - uint32_t(at));
-            float v[V];
-#pragma unroll
-            for (int j = 0; j < V; ++j) v[j] = slope_of<T, F>(g, a.up_entropy, widen(held[u].at(j)), phi.at(j));
-            if (uint32_t(y) - uint32_t(at) < V) {          // false for y < 0
-#pragma unroll
-                for (int j = 0; j < V; ++j)
-                    if (uint32_t(y) == uint32_t(at) + j) v[j] += g.a;
+            for (int u = 0; u < 2; ++u) {
+                const uint32_t at = c + u * 256 * V;
+                if (at < end) held[u] = load_pack<V>(x + at, end - at, T{});
             }
-            store_pack<V>(out + at, narrow_pack<T, V>(v), end - uint32_t(at));
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const uint32_t at = c + u * 256 * V;
+                if (at >= end) break;
+                Pack<float, V> phi{};
+                if constexpr (F) phi = load_field<V>(field + at * a.fs[1], a.fs[1], end - at);
+                float v[V];
+#pragma unroll
+                for (int j = 0; j < V; ++j) v[j] = grad.at(widen(held[u].at(j)), phi.at(j), 0.0f);
+                if (uint32_t(y) - at < V) {                // false for y < 0
+#pragma unroll
+                    for (int j = 0; j < V; ++j)
+                        if (uint32_t(y) == at + j) v[j] += g.a;
+                }
+                store_pack<V>(out + at, narrow_pack<T, V>(v), end - at);
+            }
         }
-    }
+    });
 }
 
 }  // namespace tmtrain

@@ -64,6 +64,13 @@ int by_type(int dtype, F fn) {
     return fn(f16{});
 }
 
+// fn(entropy, field) of the parts asked for; a field brings the entropy along.
+template <typename F>
+int by_parts(const void *entropy, const void *field, F fn) {
+    if (field) return fn(Bool<true>{}, Bool<true>{});
+    if (entropy) return fn(Bool<true>{}, Bool<false>{});
+    return fn(Bool<false>{}, Bool<false>{});
+}
 template <int N>
 struct Int { static constexpr int value = N; };
 template <typename F>
@@ -149,7 +156,7 @@ int check_labels(const void *logits, int dtype, int64_t outer, int64_t classes, 
 }
 
 constexpr uint64_t kBusyThreads = 65536;    // four waves to a CU
-constexpr uint64_t kRowBusyWaves = 8192;     // eight waves to a SIMD
+constexpr uint64_t kRowBusyWaves = 4096;     // four waves to a SIMD
 
 // How a request runs: on contiguous rows or on maps, with how many classes
 // held, positions to a thread and waves to a row or position.
@@ -265,7 +272,6 @@ extern "C" int tm_label_logp(const void *logits, int dtype, int64_t outer, int64
     }
     a.div_inner = Div32::make(a.inner);
     a.partial = workspace;
-    const bool F = a.field;
     return by_type(dtype, [&](auto t) {
         using T = decltype(t);
         if (p.rows) {
@@ -273,28 +279,35 @@ extern "C" int tm_label_logp(const void *logits, int dtype, int64_t outer, int64
             a.div_groups = Div32::make(p.parts);
             if (s.positions * p.parts >= kLimit) return int(TM_ERR_TOO_LARGE);
             const int rc = by_waves(p.waves, [&](auto waves) {
-                constexpr int W = decltype(waves)::value;
-                return launch(F ? k_label_rows<T, W, true> : k_label_rows<T, W, false>,
-                              dim3(W == 1 ? (a.n + 3) / 4 : a.n * p.parts), dim3(W == 1 ? 256 : 64 * W), 0, stream, a);
+                return by_parts(a.entropy, a.field, [&](auto e, auto f) {
+                    constexpr int W = decltype(waves)::value;
+                    constexpr bool E = decltype(e)::value, F = decltype(f)::value;
+                    return launch(a.k ? k_label_rows<T, W, E, F, true> : k_label_rows<T, W, E, F, false>,
+                                  dim3(W == 1 ? (a.n + 3) / 4 : a.n * p.parts), dim3(W == 1 ? 256 : 64 * W), 0, stream, a);
+                });
             });
             if (rc != TM_OK || p.parts == 1) return rc;
-            return launch(k_label_rows_join<T>, dim3(a.n), dim3(256), 0, stream, a);
+            return launch(k_label_rows_join<T>, dim3(a.n), dim3(64), 0, stream, a);
         }
         a.groups = uint32_t(ceil_div(a.inner, p.wide));
         a.div_groups = Div32::make(a.groups);
         const uint32_t threads = a.outer * a.groups;
         if (p.held) {
             return by_held(p.held, [&](auto held) {
-                constexpr int C = decltype(held)::value;
-                return launch(p.wide > 1 ? F ? k_label_held<T, kHeldV<T, C>, C, true> : k_label_held<T, kHeldV<T, C>, C, false>
-                                         : F ? k_label_held<T, 1, C, true> : k_label_held<T, 1, C, false>,
-                              dim3((threads + 255) / 256), dim3(256), 0, stream, a);
+                return by_parts(a.entropy, a.field, [&](auto e, auto f) {
+                    constexpr int C = decltype(held)::value;
+                    constexpr bool E = decltype(e)::value, F = decltype(f)::value;
+                    return launch(p.wide > 1 ? k_label_held<T, kHeldV<T, C>, C, E, F> : k_label_held<T, 1, C, E, F>,
+                                  dim3((threads + 255) / 256), dim3(256), 0, stream, a);
+                });
             });
         }
         const size_t lds = p.waves > 1 ? size_t(p.waves) * p.wide * 1024 : 0;
-        return launch(p.wide > 1 ? F ? k_label_run<T, kRunV, true> : k_label_run<T, kRunV, false>
-                                 : F ? k_label_run<T, 1, true> : k_label_run<T, 1, false>,
-                      dim3((threads + 63) / 64), dim3(64 * p.waves), lds, stream, a);
+        return by_parts(a.entropy, a.field, [&](auto e, auto f) {
+            constexpr bool E = decltype(e)::value, F = decltype(f)::value;
+            return launch(p.wide > 1 ? k_label_run<T, kRunV, E, F> : k_label_run<T, 1, E, F>, dim3((threads + 63) / 64),
+                          dim3(64 * p.waves), lds, stream, a);
+        });
     });
 }
 
@@ -361,7 +374,6 @@ extern "C" int tm_label_logp_grad(const void *logits, int dtype, int64_t outer, 
     a.div_inner = Div32::make(a.inner);
     return by_type(dtype, [&](auto t) {
         using T = decltype(t);
-        const bool F = a.field;
         if (p.rows) {
             // 8 loads to a thread, or one where that leaves CUs idle
             const uint64_t load = 256 * 16 / sizeof(T);
@@ -369,8 +381,10 @@ extern "C" int tm_label_logp_grad(const void *logits, int dtype, int64_t outer, 
             a.groups = uint32_t(ceil_div(s.n[1], a.share));
             a.div_groups = Div32::make(a.groups);
             if (s.positions * a.groups >= kLimit) return int(TM_ERR_TOO_LARGE);
-            return launch(F ? k_label_grad_rows<T, true> : k_label_grad_rows<T, false>, dim3(a.n * a.groups), dim3(256),
-                          0, stream, a);
+            return by_parts(a.up_entropy, a.field, [&](auto e, auto f) {
+                constexpr bool E = decltype(e)::value, F = decltype(f)::value;
+                return launch(k_label_grad_rows<T, E, F>, dim3(a.n * a.groups), dim3(256), 0, stream, a);
+            });
         }
         a.groups = uint32_t(ceil_div(a.inner, p.wide));
         a.div_groups = Div32::make(a.groups);
@@ -378,18 +392,21 @@ extern "C" int tm_label_logp_grad(const void *logits, int dtype, int64_t outer, 
         const dim3 grid((threads + 255) / 256);
         if (p.held) {
             return by_held(p.held, [&](auto held) {
-                constexpr int C = decltype(held)::value;
-                constexpr int HV = kHeldV<T, C>;
-                return launch(p.wide > 1 ? F ? k_label_grad_held<T, HV, C, true> : k_label_grad_held<T, HV, C, false>
-                                         : F ? k_label_grad_held<T, 1, C, true> : k_label_grad_held<T, 1, C, false>,
-                              grid, dim3(256), 0, stream, a);
+                return by_parts(a.up_entropy, a.field, [&](auto e, auto f) {
+                    constexpr int C = decltype(held)::value;
+                    constexpr bool E = decltype(e)::value, F = decltype(f)::value;
+                    return launch(p.wide > 1 ? k_label_grad_held<T, kHeldV<T, C>, C, E, F>
+                                             : k_label_grad_held<T, 1, C, E, F>, grid, dim3(256), 0, stream, a);
+                });
             });
         }
         const uint64_t shares = std::min<uint64_t>({ceil_div(kBusyThreads, threads), ceil_div(s.n[1], 8), 65535});
         a.share = uint32_t(ceil_div(s.n[1], shares));
-        return launch(p.wide > 1 ? F ? k_label_grad_run<T, kRunV, true> : k_label_grad_run<T, kRunV, false>
-                                 : F ? k_label_grad_run<T, 1, true> : k_label_grad_run<T, 1, false>,
-                      dim3(grid.x, uint32_t(ceil_div(s.n[1], a.share))), dim3(256), 0, stream, a);
+        return by_parts(a.up_entropy, a.field, [&](auto e, auto f) {
+            constexpr bool E = decltype(e)::value, F = decltype(f)::value;
+            return launch(p.wide > 1 ? k_label_grad_run<T, kRunV, E, F> : k_label_grad_run<T, 1, E, F>,
+                          dim3(grid.x, uint32_t(ceil_div(s.n[1], a.share))), dim3(256), 0, stream, a);
+        });
     });
 }
 

@@ -110,9 +110,8 @@ __device__ __forceinline__ void table_put(void *table, int32_t type, uint64_t i,
 // ---------------------------------------------------------------------------
 constexpr int kBiasThreads = 256;
 
-template <typename T>
+template <typename T, int V>
 __global__ void __launch_bounds__(kBiasThreads) k_bias(BiasArgs a) {
-    constexpr int V = 16 / sizeof(T);
     extern __shared__ float lds[];
     float *const table = lds;                              // [buckets][row], row = heads of the share, padded
     float *const edges = lds + a.src.buckets * a.row;
@@ -126,13 +125,14 @@ __global__ void __launch_bounds__(kBiasThreads) k_bias(BiasArgs a) {
     __syncthreads();
     // field: samples are blocks' own; relative: this share of the batch, all with the same buckets
     const uint32_t fb = a.field_batch > 1 ? a.div_tiles.div(blockIdx.x) : 0;
-    const uint32_t p0 = ((blockIdx.x - fb * a.div_tiles.d) * kBiasThreads + threadIdx.x) * V;
-    if (p0 >= a.src.positions) return;
-    const uint32_t n = min(uint32_t(V), a.src.positions - p0);
+    const uint32_t own = ((blockIdx.x - fb * a.div_tiles.d) * kBiasThreads + threadIdx.x) * V;
+    if (own >= a.src.positions) return;
+    // the last thread reads whole loads, further back, and writes what is its own
+    const uint32_t p0 = min(own, a.src.positions - V), skip = own - p0;
     uint32_t at[V];
 #pragma unroll
     for (int j = 0; j < V; ++j)
-        at[j] = bucket_of(edges, a.src.span, distance_at(a.src, fb, min(p0 + j, a.src.positions - 1))) * a.row;
+        at[j] = bucket_of(edges, a.src.span, distance_at(a.src, fb, p0 + j)) * a.row;
     const uint32_t b0 = fb + bshare * a.batch_share;
     const uint32_t b1 = a.field_batch > 1 ? fb + 1 : min(a.batch, b0 + a.batch_share);
     for (uint32_t h = 0; h < hn; h += 4) {
@@ -145,8 +145,7 @@ __global__ void __launch_bounds__(kBiasThreads) k_bias(BiasArgs a) {
             if (a.add) {
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    if (h + r < hn)
-                        extra[r] = load_pack<V>(static_cast<const T *>(a.add) + row + uint64_t(r) * a.src.positions, n, T{});
+                    if (h + r < hn) extra[r] = load_pack<V>(static_cast<const T *>(a.add) + row + uint64_t(r) * a.src.positions);
             }
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
@@ -157,7 +156,7 @@ __global__ void __launch_bounds__(kBiasThreads) k_bias(BiasArgs a) {
                     const float x = r == 0 ? v[j].x : r == 1 ? v[j].y : r == 2 ? v[j].z : v[j].w;
                     out[j] = a.add ? x + widen(extra[r].at(j)) : x;
                 }
-                store_pack<V>(static_cast<T *>(a.out) + row + uint64_t(r) * a.src.positions, narrow_pack<T, V>(out), n);
+                store_own<V>(static_cast<T *>(a.out) + row + uint64_t(r) * a.src.positions, narrow_pack<T, V>(out), skip);
             }
         }
     }
@@ -166,22 +165,34 @@ __global__ void __launch_bounds__(kBiasThreads) k_bias(BiasArgs a) {
 // ---------------------------------------------------------------------------
 // Gradient of the table: out[k][h] = sum over positions of [bucket = k] g[h],
 // a matrix product with a matrix of ones and zeros.  A wave takes 16 heads and
-// 128 positions a step: every lane finds the buckets of two positions and
-// leaves them in LDS; the ones and zeros are made in registers as the first
-// operand of 16x16x32 products (16 buckets x 32 positions; a "one" is 2.0, a
-// single bit of either 16-bit format, and the sum is halved at the end) and
-// the gradients are the second, loaded as they lie: 8 consecutive positions of
-// a head are a lane's operand.  Sums are float32 in the accumulators, in an
+// a step of positions: its lanes find the buckets and leave them in LDS; the
+// ones and zeros are made in registers as the first operand of 16x16x32
+// products (16 buckets x 32 positions; a "one" is 2.0, a single bit of either
+// 16-bit format, and the sum is halved at the end) and the gradients are the
+// second.  They are loaded 256 bytes of a head to 16 lanes, the next step's
+// while one is added up, and change hands through LDS, since the operand wants
+// 8 positions of one head in a lane.  (Loaded as the operand lies, with
+// neighbouring lanes in different heads, every lane is an access of its own:
+// 86 us instead of XX for 2 x 16 x 2048 x 2048.)  Fewer than 9 heads leave
+// loads over for more positions.  Sums are float32 in the accumulators, in an
 // order fixed by the sizes.  float32 gradients are cut into three bf16 pieces
 // of 8 bits, which lose nothing.
 //
 // Each workgroup leaves its sums in the workspace; k_bias_join adds them up.
 // Zero times an infinity or NaN spreads it over the buckets of its tile, so a
-// sum that is not finite is made once more there, from its own bucket alone.
+// sum that is not finite is made once more there, from its own bucket alone;
+// so are all sums over fewer positions than a load holds (splits = 0).
+// Columns of heads that are not there hold anything and are not used.
 // ---------------------------------------------------------------------------
 constexpr int kGradThreads = 512;
 constexpr int kGradWaves = kGradThreads / kWave;
-constexpr uint32_t kGradStep = 128;                        // positions a wave takes at a time
+constexpr int kGradRow = 256 + 16;                         // bytes of a head in LDS: rows begin in different banks
+
+// Positions of a load of 256 bytes, and of a step with `Blocks` blocks of four heads.
+template <typename T>
+constexpr uint32_t kGradLoad = 256 / sizeof(T);
+template <typename T, int Blocks>
+constexpr uint32_t kGradStep = kGradLoad<T> * (4 / Blocks);
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
@@ -212,98 +223,131 @@ __device__ __forceinline__ f32x4 product(f16, u32x4 a, u32x4 b, f32x4 c) {
                                                   0);
 }
 
-// One step of 128 positions, for the samples of one share of the batch.
+// One step of positions, for the samples of one share of the batch.
 struct Unit {
-    uint32_t field, first, left;           // sample of the distances, first position, positions from there on
+    uint32_t field, first;                 // sample of the distances, first position
     uint32_t b0, b1;
 };
-__device__ __forceinline__ Unit unit_at(const BiasGradArgs &a, uint32_t unit) {
+__device__ __forceinline__ Unit unit_at(const BiasGradArgs &a, uint32_t unit, uint32_t step) {
     Unit u;
     const uint32_t share = a.div_steps.div(unit);
     u.field = a.field_batch > 1 ? share : 0;
-    u.first = (unit - share * a.div_steps.d) * kGradStep;
-    u.left = a.src.positions - u.first;
+    u.first = (unit - share * a.div_steps.d) * step;
     u.b0 = share * a.batch_share;
     u.b1 = min(a.batch, u.b0 + a.batch_share);
     return u;
 }
 
-// Tiles: buckets / 16, rounded up to a power of two.
-template <typename T, int Tiles>
+// Tiles: buckets / 16, rounded up to a power of two.  Blocks of four heads: 1, 2 or 4.
+template <typename T, int Tiles, int Blocks>
 __global__ void __launch_bounds__(kGradThreads) k_bias_grad(BiasGradArgs a) {
+    constexpr uint32_t L = kGradLoad<T>, Step = kGradStep<T, Blocks>;
+    constexpr int V = 16 / sizeof(T);
     __shared__ float edges[kMaxBuckets];
-    __shared__ __align__(16) uint16_t ids[kGradWaves][kGradStep];
+    __shared__ __align__(16) uint16_t ids[kGradWaves][Step];
+    __shared__ __align__(16) char rows[kGradWaves][4 * Blocks * kGradRow];
     __shared__ float sums[Tiles * 16][16];
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const uint32_t col = lane & 15, group = lane >> 4;     // operand: row or column, block of 8 positions
-    const uint32_t h0 = blockIdx.y * 16, h = h0 + col;
+    const uint32_t h0 = blockIdx.y * 16;
     stage_edges(edges, a.src, kGradThreads);
     for (uint32_t i = threadIdx.x; i < Tiles * 256; i += kGradThreads) sums[i >> 4][i & 15] = 0.0f;
     __syncthreads();
     f32x4 acc[Tiles] = {};
     const uint32_t splat = col * 0x10001u;
-    for (uint64_t at = uint64_t(blockIdx.x) * kGradWaves + wave; at < a.units; at += uint64_t(gridDim.x) * kGradWaves) {
-        const Unit u = unit_at(a, uint32_t(at));
-        const uint32_t left = u.left;
-        uint32_t here[2];
+    char *const mine = rows[wave];
+    // Load i: head 4 (i % Blocks) + group, 16 bytes at piece col of 256-byte run
+    // i / Blocks.  No load is behind a branch, where it would be waited for:
+    // heads that are not there read the last one, and pieces past the end the
+    // last V positions, whose doubles no bucket takes.
+    const uint32_t last = a.src.positions - V;
+    const auto fetch = [&](Pack<T, V> (&x)[4], const Unit &u, uint32_t b) __attribute__((always_inline)) {
+        const T *g = static_cast<const T *>(a.grad) + uint64_t(b) * a.heads * a.src.positions;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const uint32_t i = j * 64 + lane;
-            here[j] = i < left ? bucket_of(edges, a.src.span, distance_at(a.src, u.field, u.first + i)) : 0xffffu;
-            ids[wave][i] = uint16_t(here[j]);
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t head = min(h0 + 4 * (i % Blocks) + group, a.heads - 1);
+            x[i] = load_pack<V>(g + uint64_t(head) * a.src.positions + min(u.first + (i / Blocks) * L + col * V, last));
         }
-        wave_sync();
+    };
+    uint64_t at = uint64_t(blockIdx.x) * kGradWaves + wave;
+    Unit u{};
+    Pack<T, V> x[4];
+    if (at < a.units) {
+        u = unit_at(a, uint32_t(at), Step);
+        fetch(x, u, u.b0);
+    }
+    while (at < a.units) {
+#pragma unroll
+        for (uint32_t i = lane; i < Step; i += 64) {
+            const uint32_t piece = u.first + i / V * V, p = min(piece, last) + i % V;
+            const uint32_t k = bucket_of(edges, a.src.span, distance_at(a.src, u.field, p));
+            ids[wave][i] = uint16_t(p < piece ? 0xffffu : k);
+        }
+        at += uint64_t(gridDim.x) * kGradWaves;
+        const Unit v = at < a.units ? unit_at(a, uint32_t(at), Step) : Unit{};
         for (uint32_t b = u.b0; b < u.b1; ++b) {
-            const T *g = static_cast<const T *>(a.grad) + (uint64_t(b) * a.heads + h) * a.src.positions + u.first;
-            Pack<T, 8> x[4];
+            // runs of 256 bytes change hands one after the other
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const uint32_t i = q * 32 + group * 8;
-                x[q] = {};
-                if (h < a.heads && i < left) x[q] = load_pack<8>(g + i, left - i, T{});
-            }
+            for (int run = 0; run < 4 / Blocks; ++run) {
+                wave_sync();
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                u32x4 w = *reinterpret_cast<const u32x4 *>(&ids[wave][q * 32 + group * 8]);
-                w ^= splat;
-                // few tiles: their ones are kept for the other samples; many would not fit the registers
-                if (Tiles > 2) asm volatile("" : "+v"(w));
-                u32x4 part[sizeof(T) == 4 ? 3 : 1];
-                if constexpr (sizeof(T) == 4) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        uint32_t cut[2][3];
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const float v = widen(x[q].at(2 * j + e));
-                            cut[e][0] = __float_as_uint(v) & 0xffff0000u;
-                            const float r = v - __uint_as_float(cut[e][0]);
-                            cut[e][1] = __float_as_uint(r) & 0xffff0000u;
-                            cut[e][2] = __float_as_uint(r - __uint_as_float(cut[e][1]));
-                        }
-#pragma unroll
-                        for (int c = 0; c < 3; ++c) part[c][j] = __builtin_amdgcn_perm(cut[1][c], cut[0][c], 0x07060302u);
-                    }
-                } else {
-                    part[0] = u32x4{x[q].w[0], x[q].w[1], x[q].w[2], x[q].w[3]};
+                for (int i = 0; i < Blocks; ++i) {
+                    const Pack<T, V> &y = x[run * Blocks + i];
+                    *reinterpret_cast<u32x4 *>(mine + (4 * i + group) * kGradRow + col * 16) = u32x4{y.w[0], y.w[1], y.w[2], y.w[3]};
                 }
+                wave_sync();
+                if (run == 4 / Blocks - 1) {
+                    // the gradients of the step after this one are on their way meanwhile
+                    if (b + 1 < u.b1) fetch(x, u, b + 1);
+                    else if (at < a.units) fetch(x, v, v.b0);
+                }
+                const char *const operand = mine + (col & (4 * Blocks - 1)) * kGradRow + group * 8 * sizeof(T);
 #pragma unroll
-                for (int t = 0; t < Tiles; ++t) {
-                    // tiles that hold none of these 64 positions' buckets are passed over
-                    if (Tiles > 2 && !__any((here[q >> 1] >> 4) == uint32_t(t))) continue;
-                    u32x4 one;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) one[j] = match2(w[j], t * 0x00100010u);
+                for (uint32_t q = 0; q < L / 32; ++q) {
+                    u32x4 w = *reinterpret_cast<const u32x4 *>(&ids[wave][run * L + q * 32 + group * 8]);
+                    w ^= splat;
+                    u32x4 part[sizeof(T) == 4 ? 3 : 1];
                     if constexpr (sizeof(T) == 4) {
 #pragma unroll
-                        for (int c = 0; c < 3; ++c) acc[t] = product(bf16{}, one, part[c], acc[t]);
+                        for (int half = 0; half < 2; ++half) {
+                            const u32x4 v4 = *reinterpret_cast<const u32x4 *>(operand + q * 128 + half * 16);
+                            uint32_t cut[4][3];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const float g = __uint_as_float(v4[e]);
+                                cut[e][0] = v4[e] & 0xffff0000u;
+                                const float r = g - __uint_as_float(cut[e][0]);
+                                cut[e][1] = __float_as_uint(r) & 0xffff0000u;
+                                cut[e][2] = __float_as_uint(r - __uint_as_float(cut[e][1]));
+                            }
+#pragma unroll
+                            for (int c = 0; c < 3; ++c)
+#pragma unroll
+                                for (int j = 0; j < 2; ++j)
+                                    part[c][half * 2 + j] = __builtin_amdgcn_perm(cut[2 * j + 1][c], cut[2 * j][c], 0x07060302u);
+                        }
                     } else {
-                        acc[t] = product(T{}, one, part[0], acc[t]);
+                        part[0] = *reinterpret_cast<const u32x4 *>(operand + q * 64);
+                    }
+#pragma unroll
+                    for (int t = 0; t < Tiles; ++t) {
+                        u32x4 one;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) one[j] = match2(w[j], t * 0x00100010u);
+                        // tiles that hold none of these 32 positions' buckets are passed over
+                        if (Tiles > 1 && !__any((one[0] | one[1] | one[2] | one[3]) != 0)) continue;
+                        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+                            for (int c = 0; c < 3; ++c) acc[t] = product(bf16{}, one, part[c], acc[t]);
+                        } else {
+                            acc[t] = product(T{}, one, part[0], acc[t]);
+                        }
                     }
                 }
             }
         }
         wave_sync();
+        u = v;
     }
     // lane holds rows group * 4 .. + 3 of column col of each tile; waves add in turn
     for (uint32_t w = 0; w < kGradWaves; ++w) {
@@ -345,7 +389,7 @@ __global__ void __launch_bounds__(256) k_bias_join(BiasGradArgs a) {
     }
     sum = part[col];
     if (slice == 0 && h0 + col < a.heads) table_put(a.out, a.table_type, uint64_t(k) * a.heads + h0 + col, sum);
-    const uint64_t odd = __ballot(h0 + col < a.heads && !__builtin_isfinite(sum)) & 0xffff;
+    const uint64_t odd = __ballot(h0 + col < a.heads && (!__builtin_isfinite(sum) || a.splits == 0)) & 0xffff;
     if (!odd) return;                                      // the same in every wave
     stage_edges(edges, a.src, 256);
     for (uint32_t i = 0; i < 16; ++i) {

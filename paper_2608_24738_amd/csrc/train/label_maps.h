@@ -22,34 +22,38 @@ constexpr int kHeldV = (C <= 8 ? 16 : 8) / int(sizeof(T));
 constexpr int kRunV = 4;
 
 template <int V, typename L>
-__device__ __forceinline__ void load_labels_as(const L *p, uint32_t n, uint32_t classes, int32_t (&y)[V]) {
-    const Pack<L, V> r = load_pack<V>(p, n, L(0));
+__device__ __forceinline__ void load_labels_as(const L *p, uint32_t classes, int32_t (&y)[V]) {
+    const Pack<L, V> r = load_pack<V>(p);
 #pragma unroll
     for (int j = 0; j < V; ++j) y[j] = int64_t(r.at(j)) >= 0 && int64_t(r.at(j)) < int64_t(classes) ? int32_t(r.at(j)) : -1;
 }
 template <int V>
-__device__ __forceinline__ void load_labels(const void *p, int32_t bytes, uint64_t i, uint32_t n, uint32_t classes,
+__device__ __forceinline__ void load_labels(const void *p, int32_t bytes, uint64_t i, uint32_t classes,
                                             int32_t (&y)[V]) {
     if (bytes == 1)
-        load_labels_as<V>(static_cast<const uint8_t *>(p) + i, n, classes, y);
+        load_labels_as<V>(static_cast<const uint8_t *>(p) + i, classes, y);
     else if (bytes == 4)
-        load_labels_as<V>(static_cast<const int32_t *>(p) + i, n, classes, y);
+        load_labels_as<V>(static_cast<const int32_t *>(p) + i, classes, y);
     else
-        load_labels_as<V>(static_cast<const int64_t *>(p) + i, n, classes, y);
+        load_labels_as<V>(static_cast<const int64_t *>(p) + i, classes, y);
 }
 
 // Where a thread's positions lie.
 template <int V>
 struct Place {
-    uint32_t o, i, n;           // outer, first inner position, positions
+    uint32_t o, i;              // outer, first inner position
+    uint32_t skip;              // positions in front that are another thread's
     uint64_t at;                // in [outer][inner]
 };
 template <int V, typename Args>
 __device__ __forceinline__ Place<V> place(const Args &a, uint32_t thread) {
     Place<V> r;
     r.o = a.div_groups.div(thread);
-    r.i = (thread - r.o * a.groups) * V;
-    r.n = min(uint32_t(V), a.inner - r.i);
+    // the last thread of an outer position takes whole loads, further back, and
+    // writes what is its own: loads behind a branch would be waited for
+    const uint32_t own = (thread - r.o * a.groups) * V;
+    r.i = min(own, a.inner - V);
+    r.skip = own - r.i;
     r.at = uint64_t(r.o) * a.inner + r.i;
     return r;
 }
@@ -77,12 +81,12 @@ __device__ __forceinline__ void put_top(const LabelArgs &a, const Place<V> &w, u
         index.put(j, max(best[j].c, 0));                   // NaN everywhere: no class is larger
     }
     if (V == 1 || a.ts[2] == 1) {
-        store_pack<V>(a.top + at, top, w.n);
-        store_pack<V>(a.index + at, index, w.n);
+        store_own<V>(a.top + at, top, w.skip);
+        store_own<V>(a.index + at, index, w.skip);
     } else {
 #pragma unroll
         for (int j = 0; j < V; ++j)
-            if (uint32_t(j) < w.n) {
+            if (uint32_t(j) >= w.skip) {
                 a.top[at + j * a.ts[2]] = top.at(j);
                 a.index[at + j * a.ts[2]] = index.at(j);
             }
@@ -97,17 +101,17 @@ __device__ __forceinline__ void put_found(const LabelArgs &a, const Place<V> &w,
     if (a.logp) {
 #pragma unroll
         for (int j = 0; j < V; ++j) r.put(j, y[j] < 0 ? 0.0f : log_prob(q[j], xl[j]));
-        store_pack<V>(a.logp + w.at, r, w.n);
+        store_own<V>(a.logp + w.at, r, w.skip);
     }
     if (a.entropy) {
 #pragma unroll
         for (int j = 0; j < V; ++j) r.put(j, q[j].entropy);
-        store_pack<V>(a.entropy + w.at, r, w.n);
+        store_own<V>(a.entropy + w.at, r, w.skip);
     }
     if (a.mean) {
 #pragma unroll
         for (int j = 0; j < V; ++j) r.put(j, q[j].mean);
-        store_pack<V>(a.mean + w.at, r, w.n);
+        store_own<V>(a.mean + w.at, r, w.skip);
     }
     if (a.stats) {
         Pack<float, 2 * V> st{};
@@ -116,7 +120,7 @@ __device__ __forceinline__ void put_found(const LabelArgs &a, const Place<V> &w,
             st.put(2 * j, q[j].m);
             st.put(2 * j + 1, stats_logs(q[j]));
         }
-        store_pack<2 * V>(a.stats + 2 * w.at, st, 2 * w.n);
+        store_own<2 * V>(a.stats + 2 * w.at, st, 2 * w.skip);
     }
 }
 
@@ -137,11 +141,11 @@ constexpr int kFieldHeld = F && C * V <= 32 ? C : 1;
 // The field is left in `phi` as far as that has room.
 template <typename T, int V, int C, bool E, bool F, int P>
 __device__ __forceinline__ void held_sums(Sums (&r)[V], Pack<T, V> (&held)[C], uint32_t classes, const float *field,
-                                          const int64_t (&fs)[3], uint32_t n, Pack<float, V> (&phi)[P]) {
+                                          const int64_t (&fs)[3], Pack<float, V> (&phi)[P]) {
     if constexpr (F && P == C) {
 #pragma unroll
         for (int c = 0; c < C; ++c)
-            if (uint32_t(c) < classes) phi[c] = load_field<V>(field + c * fs[1], fs[2], n);
+            if (uint32_t(c) < classes) phi[c] = load_field<V>(field + c * fs[1], fs[2], V);
     }
     float size = 0.0f;
 #pragma unroll
@@ -155,7 +159,7 @@ __device__ __forceinline__ void held_sums(Sums (&r)[V], Pack<T, V> (&held)[C], u
 #pragma unroll
         for (int c = 0; c < C; ++c)
             if (uint32_t(c) < classes) {
-                if (F && P != C) phi[0] = load_field<V>(field + c * fs[1], fs[2], n);
+                if (F && P != C) phi[0] = load_field<V>(field + c * fs[1], fs[2], V);
 #pragma unroll
                 for (int j = 0; j < V; ++j) R(r[j].m).take(some[j], widen(held[c].at(j)), F ? phi[P == C ? c : 0].at(j) : 0.0f);
             }
@@ -176,9 +180,9 @@ __global__ void __launch_bounds__(256) k_label_held(LabelArgs a) {
     Pack<T, V> held[C];
 #pragma unroll
     for (int c = 0; c < C; ++c)
-        if (uint32_t(c) < a.classes) held[c] = load_pack<V>(x + c * a.xs[1], w.n, T{});
+        if (uint32_t(c) < a.classes) held[c] = load_pack<V>(x + c * a.xs[1]);
     int32_t y[V];
-    if (a.logp) load_labels<V>(a.label, a.label_bytes, w.at, w.n, a.classes, y);
+    if (a.logp) load_labels<V>(a.label, a.label_bytes, w.at, a.classes, y);
     Sums r[V];
     float xl[V];
 #pragma unroll
@@ -194,7 +198,7 @@ __global__ void __launch_bounds__(256) k_label_held(LabelArgs a) {
         }
     const float *const field = F ? a.field + w.o * a.fs[0] + w.i * a.fs[2] : nullptr;
     Pack<float, V> phi[kFieldHeld<C, V, F>] = {};
-    held_sums<T, V, C, E, F>(r, held, a.classes, field, a.fs, w.n, phi);
+    held_sums<T, V, C, E, F>(r, held, a.classes, field, a.fs, phi);
     Found q[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) q[j] = found(r[j]);
@@ -267,7 +271,7 @@ __global__ void __launch_bounds__(64 * kRunWaves) k_label_run(LabelArgs a) {
         Pack<T, V> held[kRunBlock];
 #pragma unroll
         for (int u = 0; u < kRunBlock; ++u)
-            if (c + u < c1) held[u] = load_pack<V>(x + (c + u) * a.xs[1], w.n, T{});
+            if (c + u < c1) held[u] = load_pack<V>(x + (c + u) * a.xs[1]);
         float size = 0.0f;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
@@ -289,7 +293,7 @@ __global__ void __launch_bounds__(64 * kRunWaves) k_label_run(LabelArgs a) {
             for (int u = 0; u < kRunBlock; ++u)
                 if (c + u < c1) {
                     Pack<float, V> phi{};
-                    if (F) phi = load_field<V>(field + (c + u) * a.fs[1], a.fs[2], w.n);
+                    if (F) phi = load_field<V>(field + (c + u) * a.fs[1], a.fs[2], V);
 #pragma unroll
                     for (int j = 0; j < V; ++j) R(r[j].m).take(some[j], widen(held[u].at(j)), phi.at(j));
                 }
@@ -335,10 +339,10 @@ __global__ void __launch_bounds__(64 * kRunWaves) k_label_run(LabelArgs a) {
         int32_t y[V];
         float xl[V];
         if (a.logp) {
-            load_labels<V>(a.label, a.label_bytes, w.at, w.n, a.classes, y);
+            load_labels<V>(a.label, a.label_bytes, w.at, a.classes, y);
 #pragma unroll
             for (int j = 0; j < V; ++j)
-                xl[j] = uint32_t(j) < w.n && y[j] >= 0 ? widen(x[y[j] * a.xs[1] + j * a.xs[2]]) : 0.0f;
+                xl[j] = y[j] >= 0 ? widen(x[y[j] * a.xs[1] + j * a.xs[2]]) : 0.0f;
         }
         put_found<V>(a, w, y, xl, q);
     }
@@ -349,7 +353,7 @@ __global__ void __launch_bounds__(64 * kRunWaves) k_label_run(LabelArgs a) {
 #pragma unroll
             for (int j = 0; j < V; ++j) best[j] = {-INFINITY, -1};
             for (uint32_t c = c0; c < c1; ++c) {
-                const Pack<T, V> one = load_pack<V>(x + c * a.xs[1], w.n, T{});
+                const Pack<T, V> one = load_pack<V>(x + c * a.xs[1]);
 #pragma unroll
                 for (int j = 0; j < V; ++j) consider(best[j], last[j], widen(one.at(j)), int32_t(c));
             }
@@ -386,11 +390,11 @@ __global__ void __launch_bounds__(64 * kRunWaves) k_label_run(LabelArgs a) {
 template <int V>
 __device__ __forceinline__ void load_upstream(const LabelGradArgs &a, const Place<V> &w, int32_t (&y)[V],
                                               Slope (&g)[V]) {
-    if (a.up_logp) load_labels<V>(a.label, a.label_bytes, w.at, w.n, a.classes, y);
+    if (a.up_logp) load_labels<V>(a.label, a.label_bytes, w.at, a.classes, y);
     Pack<float, V> ua{}, uh{}, uf{};
-    if (a.up_logp) ua = load_pack<V>(a.up_logp + w.at, w.n, 0.0f);
-    if (a.up_entropy) uh = load_pack<V>(a.up_entropy + w.at, w.n, 0.0f);
-    if (a.up_mean) uf = load_pack<V>(a.up_mean + w.at, w.n, 0.0f);
+    if (a.up_logp) ua = load_pack<V>(a.up_logp + w.at);
+    if (a.up_entropy) uh = load_pack<V>(a.up_entropy + w.at);
+    if (a.up_mean) uf = load_pack<V>(a.up_mean + w.at);
 #pragma unroll
     for (int j = 0; j < V; ++j) {
         if (!a.up_logp) y[j] = -1;
@@ -411,11 +415,11 @@ __device__ __forceinline__ void put_slope(const LabelGradArgs &a, const Place<V>
         v[j] = G(g[j]).at(widen(x.at(j)), phi.at(j), y[j] == int32_t(c) ? g[j].a : 0.0f);
     const Pack<T, V> r = narrow_pack<T, V>(v);
     if (V == 1 || a.gs[2] == 1) {
-        store_pack<V>(out, r, w.n);
+        store_own<V>(out, r, w.skip);
     } else {
 #pragma unroll
         for (int j = 0; j < V; ++j)
-            if (uint32_t(j) < w.n) out[j * a.gs[2]] = r.at(j);
+            if (uint32_t(j) >= w.skip) out[j * a.gs[2]] = r.at(j);
     }
 }
 
@@ -432,7 +436,7 @@ __global__ void __launch_bounds__(256) k_label_grad_held(LabelGradArgs a) {
 #pragma unroll
     for (int c = 0; c < C; ++c)
         if (uint32_t(c) < a.classes) {
-            held[c] = load_pack<V>(x + c * a.xs[1], w.n, T{});
+            held[c] = load_pack<V>(x + c * a.xs[1]);
         }
     Sums r[V];
     Slope g[V];
@@ -445,7 +449,7 @@ __global__ void __launch_bounds__(256) k_label_grad_held(LabelGradArgs a) {
             for (int j = 0; j < V; ++j) r[j].m = fmaxf(r[j].m, widen(held[c].at(j)));
         }
     Pack<float, V> phi[kFieldHeld<C, V, F>] = {};
-    held_sums<T, V, C, E, F>(r, held, a.classes, field, a.fs, w.n, phi);
+    held_sums<T, V, C, E, F>(r, held, a.classes, field, a.fs, phi);
 #pragma unroll
     for (int j = 0; j < V; ++j) {
         const Found q = found(r[j]);
@@ -461,7 +465,7 @@ __global__ void __launch_bounds__(256) k_label_grad_held(LabelGradArgs a) {
         for (int c = 0; c < C; ++c)
             if (uint32_t(c) < a.classes) {
                 constexpr bool kept = kFieldHeld<C, V, F> == C;
-                if constexpr (F && !kept) phi[0] = load_field<V>(field + c * a.fs[1], a.fs[2], w.n);
+                if constexpr (F && !kept) phi[0] = load_field<V>(field + c * a.fs[1], a.fs[2], V);
                 put_slope<T, V, Grad<decltype(near)::value, E, F>>(a, w, c, held[c], phi[F && kept ? c : 0], y, g);
             }
     });
@@ -477,10 +481,10 @@ __global__ void __launch_bounds__(256) k_label_grad_run(LabelGradArgs a) {
     const T *x = static_cast<const T *>(a.x) + w.o * a.xs[0] + w.i * a.xs[2];
     const uint32_t c0 = blockIdx.y * a.share, c1 = min(a.classes, c0 + a.share);
     Slope g[V];
-    const Pack<float, 2 * V> st = load_pack<2 * V>(a.stats + 2 * w.at, 2 * w.n, 0.0f);
+    const Pack<float, 2 * V> st = load_pack<2 * V>(a.stats + 2 * w.at);
     Pack<float, V> entropy{}, mean{};
-    if (E && a.up_entropy) entropy = load_pack<V>(a.entropy + w.at, w.n, 0.0f);
-    if constexpr (F) mean = load_pack<V>(a.mean + w.at, w.n, 0.0f);
+    if (E && a.up_entropy) entropy = load_pack<V>(a.entropy + w.at);
+    if constexpr (F) mean = load_pack<V>(a.mean + w.at);
 #pragma unroll
     for (int j = 0; j < V; ++j) {
         g[j].m = st.at(2 * j);
@@ -497,10 +501,10 @@ __global__ void __launch_bounds__(256) k_label_grad_run(LabelGradArgs a) {
 #pragma unroll
             for (int u = 0; u < 4; ++u)
                 if (c + u < c1) {
-                    held[u] = load_pack<V>(x + (c + u) * a.xs[1], w.n, T{});
+                    held[u] = load_pack<V>(x + (c + u) * a.xs[1]);
                     if constexpr (F)
                         phi[u] = load_field<V>(a.field + w.o * a.fs[0] + (c + u) * a.fs[1] + w.i * a.fs[2], a.fs[2],
-                                               w.n);
+                                               V);
                 }
 #pragma unroll
             for (int u = 0; u < 4; ++u)

@@ -140,6 +140,14 @@ __device__ __forceinline__ void store_pack(T *p, const Pack<T, V> &r, uint32_t n
     for (int j = 0; j < V; ++j)
         if (uint32_t(j) < n) p[j] = r.at(j);
 }
+// All but the first `skip` elements.
+template <int V, typename T>
+__device__ __forceinline__ void store_own(T *p, const Pack<T, V> &r, uint32_t skip) {
+    if (V == 1 || skip == 0) return store_pack<V>(p, r);
+#pragma unroll
+    for (int j = 1; j < V; ++j)
+        if (uint32_t(j) >= skip) p[j] = r.at(j);
+}
 
 // Makes the compiler take the elements out of their words again from here on:
 // kept widened from pass to pass they would need twice the registers.

@@ -194,7 +194,7 @@ LabelPlan label_plan(int dtype, uint64_t outer, uint64_t classes, uint64_t inner
     const int64_t step = p.swap ? strides[0] : strides[2];
     p.held = classes <= 4 ? 4 : classes <= 8 ? 8 : classes <= 16 ? 16 : classes <= 32 ? 32 : 0;
     p.wide = p.held == 0 ? kRunV : int((p.held <= 8 ? 16 : 8) / float_bytes(dtype));
-    if (step != 1 || out * ceil_div(in, p.wide) < kBusyThreads / 2) p.wide = 1;
+    if (step != 1 || in < uint64_t(p.wide) || out * ceil_div(in, p.wide) < kBusyThreads / 2) p.wide = 1;
     const uint64_t threads = out * ceil_div(in, p.wide);
     p.waves = uint32_t(std::max<uint64_t>(1, std::min<uint64_t>({kRunWaves, kBusyThreads / threads, classes / 16})));
     return p;
@@ -512,7 +512,8 @@ int run_bias(const BiasShape &s, const void *table, int table_dtype, int64_t hea
     // Shares: all heads to a workgroup where the positions alone fill the chip,
     // else four heads at a time and then parts of the batch; a share's table
     // fits 32 KB of LDS.
-    const uint64_t vec = 16 / float_bytes(out_dtype);
+    uint64_t vec = 16 / float_bytes(out_dtype);
+    if (s.src.positions < vec) vec = 1;
     const uint64_t tiles = ceil_div(s.src.positions, kBiasThreads * vec);
     const uint64_t blocks = tiles * s.field_batch;
     const uint64_t quads = ceil_div(uint64_t(heads), 4);
@@ -533,9 +534,17 @@ int run_bias(const BiasShape &s, const void *table, int table_dtype, int64_t hea
     a.div_tiles = Div32::make(uint32_t(tiles));
     const size_t lds = (size_t(s.src.buckets) * a.row + s.src.span) * 4;
     return by_type(out_dtype, [&](auto t) {
-        return launch(k_bias<decltype(t)>, dim3(uint32_t(blocks), uint32_t(shares * bshares)), dim3(kBiasThreads), lds,
+        using T = decltype(t);
+        return launch(vec > 1 ? k_bias<T, 16 / sizeof(T)> : k_bias<T, 1>, dim3(uint32_t(blocks), uint32_t(shares * bshares)), dim3(kBiasThreads), lds,
                       stream, a);
     });
+}
+
+template <typename F>
+int by_blocks(int blocks, F fn) {
+    if (blocks == 1) return fn(Int<1>{});
+    if (blocks == 2) return fn(Int<2>{});
+    return fn(Int<4>{});
 }
 
 uint64_t grad_splits_most(uint64_t head_groups) { return std::max<uint64_t>(64, 512 / head_groups); }
@@ -561,10 +570,12 @@ int run_bias_grad(const BiasShape &s, const void *grad, int grad_dtype, int64_t 
     a.batch = uint32_t(s.batch);
     a.field_batch = uint32_t(s.field_batch);
     a.table_type = table_dtype;
-    // Units of 128 positions and, where samples share the buckets, as many of
+    // Units of one step of positions and, where samples share the buckets, as many of
     // them as leave enough units; two workgroups of eight waves to a CU.
     const uint64_t groups = ceil_div(uint64_t(heads), 16);
-    const uint64_t steps = ceil_div(s.src.positions, kGradStep);
+    const int blocks = heads <= 4 ? 1 : heads <= 8 ? 2 : 4;
+    const uint64_t step = 256 / float_bytes(grad_dtype) * (4 / blocks);
+    const uint64_t steps = ceil_div(s.src.positions, step);
     uint64_t shares = s.batch;
     a.batch_share = 1;
     if (s.field_batch == 1 && s.batch) {
@@ -575,15 +586,19 @@ int run_bias_grad(const BiasShape &s, const void *grad, int grad_dtype, int64_t 
     if (units >= kLimit) return TM_ERR_TOO_LARGE;
     a.units = uint32_t(units);
     a.div_steps = Div32::make(uint32_t(std::max<uint64_t>(1, steps)));
-    a.splits = uint32_t(std::max<uint64_t>(1, std::min(ceil_div(units, kGradWaves), grad_splits_most(groups))));
+    const bool few = s.src.positions < 16 / float_bytes(grad_dtype);
+    a.splits = few ? 0 : uint32_t(std::max<uint64_t>(1, std::min(ceil_div(units, kGradWaves), grad_splits_most(groups))));
     a.tile_rows = uint32_t(grad_tile_rows(s.src.buckets));
-    const int rc = by_type(grad_dtype, [&](auto t) {
+    const int rc = few ? int(TM_OK) : by_type(grad_dtype, [&](auto t) {
         using T = decltype(t);
-        void (*const kernels[])(BiasGradArgs) = {k_bias_grad<T, 1>, k_bias_grad<T, 2>, k_bias_grad<T, 4>,
-                                                 k_bias_grad<T, 8>, k_bias_grad<T, 16>};
-        int tiles = 0;
-        while ((16u << tiles) < a.tile_rows) ++tiles;
-        return launch(kernels[tiles], dim3(a.splits, uint32_t(groups)), dim3(kGradThreads), 0, stream, a);
+        return by_blocks(blocks, [&](auto n) {
+            constexpr int B = decltype(n)::value;
+            void (*const kernels[])(BiasGradArgs) = {k_bias_grad<T, 1, B>, k_bias_grad<T, 2, B>, k_bias_grad<T, 4, B>,
+                                                     k_bias_grad<T, 8, B>, k_bias_grad<T, 16, B>};
+            int tiles = 0;
+            while ((16u << tiles) < a.tile_rows) ++tiles;
+            return launch(kernels[tiles], dim3(a.splits, uint32_t(groups)), dim3(kGradThreads), 0, stream, a);
+        });
     });
     if (rc != TM_OK) return rc;
     return by_type(grad_dtype, [&](auto t) {

@@ -186,7 +186,9 @@ __global__ void __launch_bounds__(kBiasThreads) k_bias(BiasArgs a) {
 // ---------------------------------------------------------------------------
 constexpr int kGradThreads = 512;
 constexpr int kGradWaves = kGradThreads / kWave;
-constexpr int kGradRow = 256 + 16;                         // bytes of a head in LDS: rows begin in different banks
+// Bytes of a head in LDS, a 16-bit value a position or three pieces; rows begin in different banks.
+template <typename T>
+constexpr int kGradRow = (sizeof(T) == 4 ? 3 * 128 : 256) + 16;
 
 // Positions of a load of 256 bytes, and of a step with `Blocks` blocks of four heads.
 template <typename T>
@@ -198,7 +200,13 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+template <bool B, typename X, typename Y>
+struct Select { typedef X type; };
+template <typename X, typename Y>
+struct Select<false, X, Y> { typedef Y type; };
 
 // Orders a wave's LDS writes and reads around it.
 __device__ __forceinline__ void wave_sync() {
@@ -245,17 +253,17 @@ __global__ void __launch_bounds__(kGradThreads) k_bias_grad(BiasGradArgs a) {
     constexpr int V = 16 / sizeof(T);
     __shared__ float edges[kMaxBuckets];
     __shared__ __align__(16) uint16_t ids[kGradWaves][Step];
-    __shared__ __align__(16) char rows[kGradWaves][4 * Blocks * kGradRow];
-    __shared__ float sums[Tiles * 16][16];
+    constexpr int Row = kGradRow<T>, Rows = 4 * Blocks * Row;
+    // the rows of every wave, and after them the sums
+    __shared__ __align__(16) char shared[kGradWaves * Rows > Tiles * 1024 ? kGradWaves * Rows : Tiles * 1024];
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const uint32_t col = lane & 15, group = lane >> 4;     // operand: row or column, block of 8 positions
     const uint32_t h0 = blockIdx.y * 16;
     stage_edges(edges, a.src, kGradThreads);
-    for (uint32_t i = threadIdx.x; i < Tiles * 256; i += kGradThreads) sums[i >> 4][i & 15] = 0.0f;
     __syncthreads();
     f32x4 acc[Tiles] = {};
     const uint32_t splat = col * 0x10001u;
-    char *const mine = rows[wave];
+    char *const mine = shared + wave * Rows;
     // Load i: head 4 (i % Blocks) + group, 16 bytes at piece col of 256-byte run
     // i / Blocks.  No load is behind a branch, where it would be waited for:
     // heads that are not there read the last one, and pieces past the end the
@@ -277,11 +285,16 @@ __global__ void __launch_bounds__(kGradThreads) k_bias_grad(BiasGradArgs a) {
         fetch(x, u, u.b0);
     }
     while (at < a.units) {
+        uint32_t present[Step / 64] = {};                  // tiles with a bucket of these 64 positions, a bit each
 #pragma unroll
-        for (uint32_t i = lane; i < Step; i += 64) {
+        for (uint32_t s = 0; s < Step / 64; ++s) {
+            const uint32_t i = s * 64 + lane;
             const uint32_t piece = u.first + i / V * V, p = min(piece, last) + i % V;
-            const uint32_t k = bucket_of(edges, a.src.span, distance_at(a.src, u.field, p));
-            ids[wave][i] = uint16_t(p < piece ? 0xffffu : k);
+            uint32_t k = bucket_of(edges, a.src.span, distance_at(a.src, u.field, p));
+            if (p < piece) k = 0xffffu;
+            ids[wave][i] = uint16_t(k);
+#pragma unroll
+            for (int t = 0; t < Tiles; ++t) present[s] |= uint32_t(__any(k >> 4 == uint32_t(t))) << t;
         }
         at += uint64_t(gridDim.x) * kGradWaves;
         const Unit v = at < a.units ? unit_at(a, uint32_t(at), Step) : Unit{};
@@ -293,7 +306,25 @@ __global__ void __launch_bounds__(kGradThreads) k_bias_grad(BiasGradArgs a) {
 #pragma unroll
                 for (int i = 0; i < Blocks; ++i) {
                     const Pack<T, V> &y = x[run * Blocks + i];
-                    *reinterpret_cast<u32x4 *>(mine + (4 * i + group) * kGradRow + col * 16) = u32x4{y.w[0], y.w[1], y.w[2], y.w[3]};
+                    char *const to = mine + (4 * i + group) * Row;
+                    if constexpr (sizeof(T) == 4) {
+                        uint32_t cut[4][3];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float g = __uint_as_float(y.w[e]);
+                            cut[e][0] = y.w[e] & 0xffff0000u;
+                            const float rest = g - __uint_as_float(cut[e][0]);
+                            cut[e][1] = __float_as_uint(rest) & 0xffff0000u;
+                            cut[e][2] = __float_as_uint(rest - __uint_as_float(cut[e][1]));
+                        }
+#pragma unroll
+                        for (int c = 0; c < 3; ++c)
+                            *reinterpret_cast<u32x2 *>(to + c * 128 + col * 8) =
+                                u32x2{__builtin_amdgcn_perm(cut[1][c], cut[0][c], 0x07060302u),
+                                      __builtin_amdgcn_perm(cut[3][c], cut[2][c], 0x07060302u)};
+                    } else {
+                        *reinterpret_cast<u32x4 *>(to + col * 16) = u32x4{y.w[0], y.w[1], y.w[2], y.w[3]};
+                    }
                 }
                 wave_sync();
                 if (run == 4 / Blocks - 1) {
@@ -301,47 +332,24 @@ __global__ void __launch_bounds__(kGradThreads) k_bias_grad(BiasGradArgs a) {
                     if (b + 1 < u.b1) fetch(x, u, b + 1);
                     else if (at < a.units) fetch(x, v, v.b0);
                 }
-                const char *const operand = mine + (col & (4 * Blocks - 1)) * kGradRow + group * 8 * sizeof(T);
+                const char *const operand = mine + (col & (4 * Blocks - 1)) * Row + group * 16;
 #pragma unroll
                 for (uint32_t q = 0; q < L / 32; ++q) {
                     u32x4 w = *reinterpret_cast<const u32x4 *>(&ids[wave][run * L + q * 32 + group * 8]);
                     w ^= splat;
-                    u32x4 part[sizeof(T) == 4 ? 3 : 1];
-                    if constexpr (sizeof(T) == 4) {
+                    constexpr int Parts = sizeof(T) == 4 ? 3 : 1;
+                    u32x4 part[Parts];
 #pragma unroll
-                        for (int half = 0; half < 2; ++half) {
-                            const u32x4 v4 = *reinterpret_cast<const u32x4 *>(operand + q * 128 + half * 16);
-                            uint32_t cut[4][3];
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const float g = __uint_as_float(v4[e]);
-                                cut[e][0] = v4[e] & 0xffff0000u;
-                                const float r = g - __uint_as_float(cut[e][0]);
-                                cut[e][1] = __float_as_uint(r) & 0xffff0000u;
-                                cut[e][2] = __float_as_uint(r - __uint_as_float(cut[e][1]));
-                            }
-#pragma unroll
-                            for (int c = 0; c < 3; ++c)
-#pragma unroll
-                                for (int j = 0; j < 2; ++j)
-                                    part[c][half * 2 + j] = __builtin_amdgcn_perm(cut[2 * j + 1][c], cut[2 * j][c], 0x07060302u);
-                        }
-                    } else {
-                        part[0] = *reinterpret_cast<const u32x4 *>(operand + q * 64);
-                    }
+                    for (int c = 0; c < Parts; ++c) part[c] = *reinterpret_cast<const u32x4 *>(operand + c * 128 + q * 64);
 #pragma unroll
                     for (int t = 0; t < Tiles; ++t) {
+                        if (Tiles > 1 && !(present[(run * L + q * 32) / 64] >> t & 1)) continue;
                         u32x4 one;
 #pragma unroll
                         for (int j = 0; j < 4; ++j) one[j] = match2(w[j], t * 0x00100010u);
-                        // tiles that hold none of these 32 positions' buckets are passed over
-                        if (Tiles > 1 && !__any((one[0] | one[1] | one[2] | one[3]) != 0)) continue;
-                        if constexpr (sizeof(T) == 4) {
+                        typedef typename Select<sizeof(T) == 4, bf16, T>::type P;
 #pragma unroll
-                            for (int c = 0; c < 3; ++c) acc[t] = product(bf16{}, one, part[c], acc[t]);
-                        } else {
-                            acc[t] = product(T{}, one, part[0], acc[t]);
-                        }
+                        for (int c = 0; c < Parts; ++c) acc[t] = product(P{}, one, part[c], acc[t]);
                     }
                 }
             }
@@ -350,6 +358,10 @@ __global__ void __launch_bounds__(kGradThreads) k_bias_grad(BiasGradArgs a) {
         u = v;
     }
     // lane holds rows group * 4 .. + 3 of column col of each tile; waves add in turn
+    float(*const sums)[16] = reinterpret_cast<float(*)[16]>(shared);
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < Tiles * 256; i += kGradThreads) sums[i >> 4][i & 15] = 0.0f;
+    __syncthreads();
     for (uint32_t w = 0; w < kGradWaves; ++w) {
         if (w == wave) {
 #pragma unroll

@@ -34,7 +34,8 @@ struct BiasArgs {
     int32_t table_type;                    // tm_dtype
     uint32_t head_share, row;              // heads of a workgroup, and their floats per bucket in LDS
     uint32_t batch_share, batch_shares;    // samples of a workgroup (relative)
-    Div32 div_tiles;                       // workgroups along the positions of one sample
+    uint32_t tiles;                        // of 256 threads' positions, over all samples with buckets of their own
+    Div32 div_tiles;                       // those of one sample
 };
 
 struct BiasGradArgs {
@@ -104,7 +105,8 @@ __device__ __forceinline__ void table_put(void *table, int32_t type, uint64_t i,
 // ---------------------------------------------------------------------------
 // Forward.  One thread owns V consecutive positions: it finds their buckets
 // once and writes every head and sample of its workgroup's share with them,
-// 16 bytes a store.  The table lies in LDS by bucket, four heads to a 16-byte
+// 16 bytes a store.  Workgroups go on to further positions rather than lay out
+// the table again.  It lies in LDS by bucket, four heads to a 16-byte
 // read, so a position's address serves all heads.  Bound by the bytes of add
 // and out.
 // ---------------------------------------------------------------------------
@@ -123,40 +125,51 @@ __global__ void __launch_bounds__(kBiasThreads) k_bias(BiasArgs a) {
         table[i] = h < hn ? table_at(a.table, a.table_type, uint64_t(k) * a.heads + h0 + h) : 0.0f;
     }
     __syncthreads();
-    // field: samples are blocks' own; relative: this share of the batch, all with the same buckets
-    const uint32_t fb = a.field_batch > 1 ? a.div_tiles.div(blockIdx.x) : 0;
-    const uint32_t own = ((blockIdx.x - fb * a.div_tiles.d) * kBiasThreads + threadIdx.x) * V;
-    if (own >= a.src.positions) return;
-    // the last thread reads whole loads, further back, and writes what is its own
-    const uint32_t p0 = min(own, a.src.positions - V), skip = own - p0;
-    uint32_t at[V];
+    for (uint32_t tile = blockIdx.x; tile < a.tiles; tile += gridDim.x) {
+        // field: samples are tiles' own; relative: this share of the batch, all with the same buckets
+        const uint32_t fb = a.field_batch > 1 ? a.div_tiles.div(tile) : 0;
+        const uint32_t own = ((tile - fb * a.div_tiles.d) * kBiasThreads + threadIdx.x) * V;
+        if (own >= a.src.positions) continue;
+        // the last thread reads whole loads, further back, and writes what is its own
+        const uint32_t p0 = min(own, a.src.positions - V), skip = own - p0;
+        float d[V];
+        if (a.src.source == kFieldF32 || a.src.source == kFieldI32) {
+            const Pack<int32_t, V> raw = load_pack<V>(static_cast<const int32_t *>(a.src.field) + uint64_t(fb) * a.src.positions + p0);
 #pragma unroll
-    for (int j = 0; j < V; ++j)
-        at[j] = bucket_of(edges, a.src.span, distance_at(a.src, fb, p0 + j)) * a.row;
-    const uint32_t b0 = fb + bshare * a.batch_share;
-    const uint32_t b1 = a.field_batch > 1 ? fb + 1 : min(a.batch, b0 + a.batch_share);
-    for (uint32_t h = 0; h < hn; h += 4) {
-        float4 v[V];
+            for (int j = 0; j < V; ++j)
+                d[j] = a.src.source == kFieldF32 ? __int_as_float(raw.at(j)) : float(raw.at(j));
+        } else {
 #pragma unroll
-        for (int j = 0; j < V; ++j) v[j] = *reinterpret_cast<const float4 *>(table + at[j] + h);
-        for (uint32_t b = b0; b < b1; ++b) {
-            const uint64_t row = (uint64_t(b) * a.heads + h0 + h) * a.src.positions + p0;
-            Pack<T, V> extra[4];
-            if (a.add) {
+            for (int j = 0; j < V; ++j) d[j] = distance_at(a.src, fb, p0 + j);
+        }
+        uint32_t at[V];
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (h + r < hn) extra[r] = load_pack<V>(static_cast<const T *>(a.add) + row + uint64_t(r) * a.src.positions);
-            }
+        for (int j = 0; j < V; ++j) at[j] = bucket_of(edges, a.src.span, d[j]) * a.row;
+        const uint32_t b0 = fb + bshare * a.batch_share;
+        const uint32_t b1 = a.field_batch > 1 ? fb + 1 : min(a.batch, b0 + a.batch_share);
+        for (uint32_t h = 0; h < hn; h += 4) {
+            float4 v[V];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                if (h + r >= hn) break;
-                float out[V];
+            for (int j = 0; j < V; ++j) v[j] = *reinterpret_cast<const float4 *>(table + at[j] + h);
+            for (uint32_t b = b0; b < b1; ++b) {
+                const uint64_t row = (uint64_t(b) * a.heads + h0 + h) * a.src.positions + p0;
+                Pack<T, V> extra[4];
+                if (a.add) {
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    const float x = r == 0 ? v[j].x : r == 1 ? v[j].y : r == 2 ? v[j].z : v[j].w;
-                    out[j] = a.add ? x + widen(extra[r].at(j)) : x;
+                    for (int r = 0; r < 4; ++r)
+                        if (h + r < hn) extra[r] = load_pack<V>(static_cast<const T *>(a.add) + row + uint64_t(r) * a.src.positions);
                 }
-                store_own<V>(static_cast<T *>(a.out) + row + uint64_t(r) * a.src.positions, narrow_pack<T, V>(out), skip);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    if (h + r >= hn) break;
+                    float out[V];
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        const float x = r == 0 ? v[j].x : r == 1 ? v[j].y : r == 2 ? v[j].z : v[j].w;
+                        out[j] = a.add ? x + widen(extra[r].at(j)) : x;
+                    }
+                    store_own<V>(static_cast<T *>(a.out) + row + uint64_t(r) * a.src.positions, narrow_pack<T, V>(out), skip);
+                }
             }
         }
     }

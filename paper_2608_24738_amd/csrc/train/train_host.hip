@@ -531,11 +531,14 @@ int run_bias(const BiasShape &s, const void *table, int table_dtype, int64_t hea
     a.row = uint32_t(4 * (share | 1));
     a.batch_share = uint32_t(bshare);
     a.batch_shares = uint32_t(bshares);
+    a.tiles = uint32_t(blocks);
     a.div_tiles = Div32::make(uint32_t(tiles));
+    // all workgroups at once, eight to a CU
+    const uint64_t grid = std::min(blocks, std::max<uint64_t>(1, 2 * kFill / (shares * bshares)));
     const size_t lds = (size_t(s.src.buckets) * a.row + s.src.span) * 4;
     return by_type(out_dtype, [&](auto t) {
         using T = decltype(t);
-        return launch(vec > 1 ? k_bias<T, 16 / sizeof(T)> : k_bias<T, 1>, dim3(uint32_t(blocks), uint32_t(shares * bshares)), dim3(kBiasThreads), lds,
+        return launch(vec > 1 ? k_bias<T, 16 / sizeof(T)> : k_bias<T, 1>, dim3(uint32_t(grid), uint32_t(shares * bshares)), dim3(kBiasThreads), lds,
                       stream, a);
     });
 }

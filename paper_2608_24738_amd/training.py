@@ -89,7 +89,8 @@ def _label_workspace(dtype, extents, strides, top_k):
 
 
 def _label_forward(logits, labels, field, dim, entropy, top_k, stats):
-    """Runs tm_label_logp; returns (logits, field) as they were read and the outputs."""
+    """Runs tm_label_logp; returns (logits, field) as they were read, what describes
+    them to the library, the outputs and the statistics for the gradient."""
     dev = logits.device
     logits, extents, strides = _viewed(logits, dim)
     shape = logits.shape[:dim] + logits.shape[dim + 1:]
@@ -106,44 +107,54 @@ def _label_forward(logits, labels, field, dim, entropy, top_k, stats):
         index = torch.empty(shape_k, dtype=torch.int32, device=dev)
     if stats:
         kept = torch.empty(tuple(shape) + (2,), dtype=torch.float32, device=dev)
-    nbytes = _label_workspace(FLOATS[logits.dtype], extents, tuple(strides), top_k)
-    if nbytes:
-        workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
-    _call("tm_label_logp", dev, None, logits.data_ptr(), FLOATS[logits.dtype], *extents, strides, _ptr(labels),
-          LABELS[labels.dtype] if labels is not None else 0, _ptr(field), field_strides, top_k, _ptr(logp), _ptr(ent),
-          _ptr(mean), _ptr(top), _ptr(index), _ptr(kept), _ptr(workspace), nbytes)
-    return logits, field, (logp, ent, mean, top, index), kept
+    dtype = FLOATS[logits.dtype]
+    nbytes = 0
+    if extents[1] > MAX_RECOMPUTE:               # rows may be cut into parts
+        nbytes = _label_workspace(dtype, extents, tuple(strides), top_k)
+        if nbytes:
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    label_dtype = LABELS[labels.dtype] if labels is not None else 0
+    _call("tm_label_logp", dev, None, logits.data_ptr(), dtype, *extents, strides, _ptr(labels), label_dtype,
+          _ptr(field), field_strides, top_k, _ptr(logp), _ptr(ent), _ptr(mean), _ptr(top), _ptr(index), _ptr(kept),
+          _ptr(workspace), nbytes)
+    return logits, field, (dtype, *extents, strides), (label_dtype, field_strides), (logp, ent, mean, top, index), kept
 
 
 def _upstream(grad):
-    return None if grad is None else grad.to(torch.float32).contiguous()
+    if grad is None or (grad.dtype == torch.float32 and grad.is_contiguous()):
+        return grad
+    return grad.to(torch.float32).contiguous()
+
+
+def _once():
+    if torch.is_grad_enabled():
+        raise RuntimeError("the training operators can be differentiated once only")
 
 
 class _LabelLogProbs(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, labels, field, dim, entropy, top_k):
         stats = logits.shape[dim] > MAX_RECOMPUTE
-        logits, field, out, kept = _label_forward(logits, labels, field, dim, entropy, top_k, stats)
+        logits, field, ctx.view, ctx.others, out, kept = _label_forward(logits, labels, field, dim, entropy, top_k, stats)
         ctx.dim = dim
         ctx.set_materialize_grads(False)
-        ctx.mark_non_differentiable(*[t for t in out[3:] if t is not None])
+        if top_k:
+            ctx.mark_non_differentiable(out[3], out[4])
         ctx.save_for_backward(logits, labels, field, kept, out[1] if stats else None, out[2] if stats else None)
         return out
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
     def backward(ctx, up_logp, up_entropy, up_mean, _top, _index):
+        _once()
         logits, labels, field, kept, entropy, mean = ctx.saved_tensors
         if up_logp is None and up_entropy is None and up_mean is None:
             return None, None, None, None, None, None
         up_logp, up_entropy, up_mean = _upstream(up_logp), _upstream(up_entropy), _upstream(up_mean)
-        grad = torch.empty_like(logits)
-        _, extents, strides = _viewed(logits, ctx.dim)
-        grad, _, grad_strides = _viewed(grad, ctx.dim)
-        field_strides = _viewed(field, ctx.dim)[2] if field is not None else None
-        _call("tm_label_logp_grad", logits.device, None, logits.data_ptr(), FLOATS[logits.dtype], *extents, strides,
-              _ptr(labels), LABELS[labels.dtype] if labels is not None else 0, _ptr(field), field_strides, _ptr(kept),
-              _ptr(entropy), _ptr(mean), _ptr(up_logp), _ptr(up_entropy), _ptr(up_mean), grad.data_ptr(), grad_strides)
+        grad, _, grad_strides = _viewed(torch.empty_like(logits), ctx.dim)
+        label_dtype, field_strides = ctx.others
+        _call("tm_label_logp_grad", logits.device, None, logits.data_ptr(), *ctx.view, _ptr(labels), label_dtype,
+              _ptr(field), field_strides, _ptr(kept), _ptr(entropy), _ptr(mean), _ptr(up_logp), _ptr(up_entropy),
+              _ptr(up_mean), grad.data_ptr(), grad_strides)
         return grad, None, None, None, None, None
 
 
@@ -203,7 +214,7 @@ def label_log_probs(logits: torch.Tensor, labels: Optional[torch.Tensor] = None,
     entropy, top_k = bool(entropy), int(top_k)
     if logits.requires_grad and torch.is_grad_enabled():
         return LabelLogProbs(*_LabelLogProbs.apply(logits, labels, field, dim, entropy, top_k))
-    return LabelLogProbs(*_label_forward(logits, labels, field, dim, entropy, top_k, False)[2])
+    return LabelLogProbs(*_label_forward(logits, labels, field, dim, entropy, top_k, False)[4])
 
 
 def distance_edges(buckets: int, reach: float, *, signed: bool = False, device=None) -> torch.Tensor:
@@ -244,8 +255,8 @@ class _Bias(torch.autograd.Function):
         return _bias_forward(table, edges, add, source, shape)
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
     def backward(ctx, up):
+        _once()
         edges, distances = ctx.saved_tensors
         name, args, _ = ctx.source
         grad = None

@@ -296,3 +296,22 @@ def test_empty():
     add = torch.zeros((0, 2, 3, 4), device=dev)
     assert training.relative_bias(table, edges, 3, 4, add=add).shape == (0, 2, 3, 4)
     assert training.relative_bias(table, edges, 0, 4).shape == (2, 0, 4)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+def test_small_gradients(dtype):
+    """Gradients among the subnormals of float16 count in full."""
+    import torch
+    from paper_2608_24738_amd import training
+    dev = "cuda:0"
+    gen = torch.Generator().manual_seed(4)
+    d = torch.rand((2, 3000), generator=gen) * 30
+    edges = training.distance_edges(16, 30)
+    for heads in (2, 16):
+        up = (torch.randn((2, heads, 3000), generator=gen) * 2.0 ** -18).to(getattr(torch, TYPES[dtype]))
+        table = torch.zeros((16, heads), device=dev, requires_grad=True)
+        announce("small gradients heads=%d %s" % (heads, dtype))
+        bias = training.distance_bias(d.to(dev), table, edges.to(dev), add=up.to(dev))
+        grad, = torch.autograd.grad([bias], [table], [up.to(dev)])
+        total, size, _ = ref.gradient(up.double().numpy(), ref.buckets(d.numpy(), edges.numpy()), 16)
+        ref.check(grad.cpu().double().numpy(), total, 16 * U * size, "f32", "small gradients")

@@ -275,3 +275,33 @@ def test_graph_replays():
             want = training.label_log_probs(fresh, y, entropy=True, top_k=3, field=phi)
             for a, b in zip(got, want):
                 assert torch.equal(a, b)
+
+
+def test_differentiated_once():
+    import torch
+    from paper_2608_24738_amd import training
+    x, y, _, _ = case((2, 5, 3), "f32")
+    x.requires_grad_(True)
+    with pytest.raises(RuntimeError):
+        torch.autograd.grad(training.label_log_probs(x, y).log_probs.sum(), [x], create_graph=True)
+
+
+def test_accumulated_gradients():
+    """backward() of a weighted loss of several parts adds to .grad, as for any operator."""
+    import torch
+    from paper_2608_24738_amd import training
+    x, y, phi, _ = case((2, 5, 30), "f32", seed=12, field=True)
+    x.requires_grad_(True)
+    got = training.label_log_probs(x, y, entropy=True, field=phi)
+    (-got.log_probs.mean() + 0.1 * got.entropy.mean() - 0.01 * got.field_mean.mean()).backward()
+    first = x.grad.clone()
+    n = y.numel()
+    flat = x.detach().movedim(1, -1).reshape(-1, 5).double().cpu().numpy()
+    ups = [np.full(n, -1.0 / n), np.full(n, 0.1 / n), np.full(n, -0.01 / n)]
+    want = ref.exact(flat, y.reshape(-1).cpu().numpy(), phi.movedim(1, -1).reshape(-1, 5).cpu().numpy(), 0, ups)
+    # the upstream values themselves are rounded to float32
+    ref.check(first.movedim(1, -1).reshape(-1, 5).double().cpu().numpy(), want["grad"],
+              want["tol_grad"] + 4 * ref.U * np.abs(want["grad"]) + 4 * ref.U * np.abs(ups[2][0]) * 100, "mean loss")
+    got = training.label_log_probs(x, y, entropy=True, field=phi)
+    (-got.log_probs.mean() + 0.1 * got.entropy.mean() - 0.01 * got.field_mean.mean()).backward()
+    assert torch.equal(x.grad, first + first)

@@ -221,12 +221,6 @@ struct Select { typedef X type; };
 template <typename X, typename Y>
 struct Select<false, X, Y> { typedef Y type; };
 
-// Orders a wave's LDS writes and reads around it.
-__device__ __forceinline__ void wave_sync() {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-}
-
 // Two ones (0x4000) or zeros: is either half of w the bucket?
 __device__ __forceinline__ uint32_t match2(uint32_t w, uint32_t bucket2) {
     const u16x2 x = __builtin_bit_cast(u16x2, w ^ bucket2);

@@ -203,11 +203,17 @@ __global__ void __launch_bounds__(256) k_label_held(LabelArgs a) {
 #pragma unroll
     for (int j = 0; j < V; ++j) q[j] = found(r[j]);
     if (a.logp) {
+        // few classes: a comparison for each; of more, the label's logit is read once more
+        if constexpr (C <= 8) {
 #pragma unroll
-        for (int c = 0; c < C; ++c)
+            for (int c = 0; c < C; ++c)
 #pragma unroll
-            for (int j = 0; j < V; ++j)
-                if (y[j] == c) xl[j] = widen(held[c].at(j));
+                for (int j = 0; j < V; ++j)
+                    if (y[j] == c) xl[j] = widen(held[c].at(j));
+        } else {
+#pragma unroll
+            for (int j = 0; j < V; ++j) xl[j] = widen(x[max(y[j], 0) * a.xs[1] + j * a.xs[2]]);
+        }
     }
     put_found<V>(a, w, y, xl, q);
     if (!a.k) return;

@@ -7,17 +7,17 @@
 // Bound by the bytes of the logits; a row is read once.
 //
 // The k likeliest classes need no second reading either: a lane notes its
-// largest logit and the load it came with.  The wave's likeliest class then is
-// that of the lane that leads; only that lane's own classes, a 64 W-th of the
-// row, are looked through again for its next one, by the whole wave.  After k
-// rounds the waves' lists are merged by counting, for every candidate, the
-// larger ones.
+// largest logit and the load it came with.  The k-th largest of the lanes'
+// bests bounds the k likeliest classes from below, so only the k lanes at or
+// above it, each with a 64 W-th of the row, are looked through again; what
+// they hold at or above the bound is ranked by counting.
 #pragma once
 
 #include "label.h"
 
 namespace tmtrain {
 
+constexpr uint32_t kRowFound = 256;                        // classes at or above the bound that a row has room for
 constexpr int kRowLoads = 4;                               // loads in flight per lane
 
 struct RowPart {                                           // of one part of a row, followed by its k keys
@@ -52,31 +52,6 @@ __device__ __forceinline__ void put_row_top(const LabelArgs &a, uint32_t o, uint
     a.top[at] = log_prob(q, unordered(uint32_t(key >> 32)));
 }
 
-// The likeliest class of a lane behind `last` in the order of the
-// alternatives, found by the whole wave: the lane's loads begin at `first`,
-// `stride` classes apart.
-template <typename T, int V>
-__device__ __forceinline__ uint64_t next_of(const T *x, uint32_t first, uint32_t end, uint32_t stride, uint64_t last) {
-    const float lx = unordered(uint32_t(last >> 32));
-    const uint32_t lc = ~uint32_t(last), lane = threadIdx.x & 63;
-    float best = -INFINITY;
-    uint32_t at = ~0u;                                     // none
-    for (uint64_t c = first + uint64_t(lane) * stride; c < end; c += uint64_t(64) * stride) {
-        const uint32_t n = min(uint32_t(V), end - uint32_t(c));
-        const Pack<T, V> r = load_pack<V>(x + c, n, T{});
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const float v = widen(r.at(j));
-            const bool open = uint32_t(j) < n && (v < lx || (v == lx && uint32_t(c) + j > lc));
-            if (open && (v > best || at == ~0u)) {
-                best = v;
-                at = uint32_t(c) + j;
-            }
-        }
-    }
-    return wave_max(at == ~0u ? 0 : top_key(best, at));
-}
-
 // The k largest of `count` <= 64 falling lists of k keys in LDS, by one wave:
 // lane j gets the j-th.  0 where there are no more.
 __device__ __forceinline__ uint64_t merge_lists(const uint64_t *lists, uint32_t count, uint32_t k) {
@@ -97,8 +72,11 @@ template <typename T, int W, bool E, bool F, bool K>
 __global__ void __launch_bounds__(W == 1 ? 256 : 64 * W, K && !F ? 7 : 4) k_label_rows(LabelArgs a) {
     constexpr int V = 16 / sizeof(T);
     constexpr uint32_t kStride = 64 * W * V;               // classes between two loads of a lane
+    constexpr int R = W == 1 ? 4 : 1;                      // rows of a workgroup
     __shared__ Sums sums[W];
-    __shared__ uint64_t keys[W * 32], leads[W];
+    __shared__ uint64_t bests_of[K ? R : 1][W * 64], leads_of[K ? R : 1][W * 32], found_of[K ? R : 1][kRowFound];
+    __shared__ uint64_t top_of[K ? R : 1][32];
+    __shared__ uint32_t count_of[R];
     const uint32_t lane = threadIdx.x & 63, wave = W == 1 ? 0 : threadIdx.x >> 6;
     const uint32_t t = wave * 64 + lane;
     const uint32_t n = W == 1 ? blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)
@@ -196,64 +174,121 @@ __global__ void __launch_bounds__(W == 1 ? 256 : 64 * W, K && !F ? 7 : 4) k_labe
     }
     r = wave_join(r);
 
-    // the lane's likeliest class, exactly: within the load that it came with
-    uint64_t key = 0, mine = 0, lead = 0, least = 0;
+    if constexpr (W > 1) {
+        if (lane == 0) sums[wave] = r;
+    }
+    const auto sync = [] {
+        if constexpr (W == 1) wave_sync();
+        else __syncthreads();
+    };
+    uint64_t mine = 0;                                     // lane j of the row's first wave: the j-th likeliest class
     if constexpr (K) {
+        const uint32_t row = W == 1 ? threadIdx.x >> 6 : 0;
+        uint64_t *const bests = bests_of[row] + wave * 64, *const leads = leads_of[row];
+        uint64_t *const among = found_of[row], *const top = top_of[row];
+        uint32_t *const count = &count_of[row];
+        // the lane's likeliest class, exactly: within the load that it came with
+        uint64_t key = 0;
         if (first < end) {
-            const uint32_t count = min(uint32_t(V), end - from);
-            const Pack<T, V> again = load_pack<V>(x + from, count, none);
+            const uint32_t have = min(uint32_t(V), end - from);
+            const Pack<T, V> again = load_pack<V>(x + from, have, none);
             uint32_t at = ~0u;
 #pragma unroll
             for (int j = V - 1; j >= 0; --j)
-                if (uint32_t(j) < count && widen(again.at(j)) == best) at = from + j;
+                if (uint32_t(j) < have && widen(again.at(j)) == best) at = from + j;
             if (at != ~0u) key = top_key(best, at);
         }
-        lead = wave_max(key);
-    }
-    if constexpr (W > 1) {
-        if (lane == 0) {
-            sums[wave] = r;
-            leads[wave] = lead;
-        }
-        __syncthreads();
-        // classes behind the k-th best wave's likeliest are not among the k
-        if (K && a.k <= W) {
-            const uint64_t one = lane < W ? leads[lane] : 0;
-            uint32_t above = 0;
-            for (int w = 0; w < W; ++w) above += leads[w] > one;
-            const uint64_t kth = __ballot(lane < W && above == a.k - 1);
+        // the k best lanes of the wave, in order
+        bests[lane] = key;
+        if (lane < a.k) leads[wave * a.k + lane] = 0;
+        if (t < a.k) top[t] = 0;
+        if (t == 0) *count = 0;
+        wave_sync();
+        uint32_t above = 0;
+        for (int v = 0; v < 64; ++v) above += bests[v] > key;
+        if (above < a.k && key) leads[wave * a.k + above] = key;
+        sync();
+        // the k-th best lane of the row (0: there are fewer)
+        uint64_t least = 0;
+        if (W == 1) {
+            least = leads[a.k - 1];
+        } else if (W * a.k <= 64) {
+            const uint64_t one = lane < W * a.k ? leads[lane] : 0;
+            above = 0;
+            for (uint32_t v = 0; v < W * a.k; ++v) above += leads[v] > one;
+            const uint64_t kth = __ballot(one != 0 && above == a.k - 1);
             if (kth) least = leads[__ffsll(static_cast<long long>(kth)) - 1];
+        } else {
+            bests[lane] = merge_lists(leads, W, a.k);
+            wave_sync();
+            least = bests[a.k - 1];
         }
+        // what the lanes at or above it hold at or above it
+        const float bound = least ? unordered(uint32_t(least >> 32)) : -INFINITY;
+        for (uint64_t lanes = __ballot(key != 0 && key >= least); lanes; lanes &= lanes - 1) {
+            const uint32_t owner = __ffsll(static_cast<long long>(lanes)) - 1;
+            for (uint64_t at = c0 + (wave * 64 + owner) * V + uint64_t(lane) * kStride; at < end; at += 64 * kStride) {
+                const uint32_t have = min(uint32_t(V), end - uint32_t(at));
+                const Pack<T, V> again = load_pack<V>(x + at, have, none);
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    if (uint32_t(j) < have && widen(again.at(j)) >= bound) {
+                        const uint64_t one = top_key(widen(again.at(j)), uint32_t(at) + j);
+                        if (one >= least) {
+                            const uint32_t place = atomicAdd(count, 1u);   // any order: they are ranked next
+                            if (place < kRowFound) among[place] = one;
+                        }
+                    }
+            }
+        }
+        sync();
+        const uint32_t n_found = *count;
+        if (n_found <= kRowFound) {
+            if (wave == 0)
+                for (uint32_t v = lane; v < n_found; v += 64) {
+                    const uint64_t one = among[v];
+                    above = 0;
+                    for (uint32_t u = 0; u < n_found; ++u) above += among[u] > one;
+                    if (above < a.k) top[above] = one;
+                }
+        } else {
+            // one lane's classes hold most of the largest logits: one pass over the row for each
+            uint64_t last = ~uint64_t(0);
+            for (uint32_t rank = 0; rank < a.k; ++rank) {
+                uint64_t next = 0;
+                for (uint64_t at = first; at < end; at += kStride) {
+                    const uint32_t have = min(uint32_t(V), end - uint32_t(at));
+                    const Pack<T, V> again = load_pack<V>(x + at, have, none);
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        const uint64_t one = top_key(widen(again.at(j)), uint32_t(at) + j);
+                        if (uint32_t(j) < have && one < last && one > next) next = one;
+                    }
+                }
+                next = wave_max(next);
+                if (lane == 0) leads[wave] = next;
+                sync();
+                last = leads[0];
+                for (int w = 1; w < W; ++w) last = last > leads[w] ? last : leads[w];
+                sync();
+                if (t == 0) top[rank] = last;
+            }
+        }
+        wave_sync();
+        if (wave == 0 && lane < a.k) mine = top[lane];
+    } else if constexpr (W > 1) {
+        __syncthreads();
     }
-    // the wave's k likeliest classes; lane j keeps the j-th
-    for (uint32_t rank = 0; K && rank < a.k; ++rank) {
-        if (lead == 0 || lead < least) break;
-        if (lane == rank) mine = lead;
-        if (rank + 1 == a.k) break;
-        const int owner = __ffsll(static_cast<long long>(__ballot(key == lead))) - 1;
-        const uint64_t next = next_of<T, V>(x, c0 + (wave * 64 + owner) * V, end, kStride, lead);
-        if (int(lane) == owner) key = next;
-        lead = wave_max(key);
-    }
-    if constexpr (W == 1) {
+    if (wave > 0) return;
+    if constexpr (W > 1) r = wave_join(lane < W ? sums[lane] : kNothing);
+    if (W == 1 || a.groups == 1) {
         const Found q = found(r);
         if (lane == 0) put_row(a, n, x, q);
         if (K && lane < a.k) put_row_top(a, o, i, lane, mine, q);
     } else {
-        if (K && lane < a.k) keys[wave * a.k + lane] = mine;
-        __syncthreads();
-        if (wave > 0) return;
-        const Sums all = wave_join(lane < W ? sums[lane] : kNothing);
-        if constexpr (K) mine = merge_lists(keys, W, a.k);
-        if (a.groups == 1) {
-            const Found q = found(all);
-            if (lane == 0) put_row(a, n, x, q);
-            if (K && lane < a.k) put_row_top(a, o, i, lane, mine, q);
-        } else {
-            char *out = static_cast<char *>(a.partial) + uint64_t(blockIdx.x) * (sizeof(RowPart) + a.k * 8);
-            if (lane == 0) reinterpret_cast<RowPart *>(out)->sums = all;
-            if (K && lane < a.k) reinterpret_cast<uint64_t *>(out + sizeof(RowPart))[lane] = mine;
-        }
+        char *out = static_cast<char *>(a.partial) + uint64_t(blockIdx.x) * (sizeof(RowPart) + a.k * 8);
+        if (lane == 0) reinterpret_cast<RowPart *>(out)->sums = r;
+        if (K && lane < a.k) reinterpret_cast<uint64_t *>(out + sizeof(RowPart))[lane] = mine;
     }
 }
 

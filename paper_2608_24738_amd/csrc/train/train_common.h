@@ -186,6 +186,12 @@ __device__ __forceinline__ Pack<T, V> narrow_pack(const float (&v)[V]) {
 // 2^x by the hardware's v_exp_f32 (results below 2^-126 flush to 0).
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// Orders a wave's LDS writes and reads around it.
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // Reductions over a wave by data-parallel primitives: rows of 16 lanes by
 // shifts, then across rows by two broadcasts; lane 63 ends with the result,
 // which becomes uniform.  The order of the additions is fixed.

@@ -305,3 +305,19 @@ def test_accumulated_gradients():
     got = training.label_log_probs(x, y, entropy=True, field=phi)
     (-got.log_probs.mean() + 0.1 * got.entropy.mean() - 0.01 * got.field_mean.mean()).backward()
     assert torch.equal(x.grad, first + first)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("period", [64, 128, 256, 512, 1024])
+def test_top_of_one_lane(period, dtype):
+    """The largest logits at one distance from each other, so that a few lanes of a wave hold all of them."""
+    import torch
+    gen = torch.Generator().manual_seed(period)
+    for rows, classes in [(2, 50000), (100, 20000)]:
+        x = torch.randn((rows, classes), generator=gen)
+        vec = 8 if dtype == "bf16" else 4
+        big = (torch.arange(classes) // vec) % period == 3
+        x = torch.where(big, x.abs() + 6, x).to(getattr(torch, TYPES[dtype])).to("cuda:0")
+        y = torch.zeros(rows, dtype=torch.int64, device="cuda:0")
+        for k in (1, 5, 32):
+            run(x, y, top_k=k, entropy=False, what="one lane's", dtype=dtype)

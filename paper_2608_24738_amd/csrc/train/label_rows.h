@@ -315,12 +315,15 @@ __global__ void __launch_bounds__(64) k_label_rows_join(LabelArgs a) {
     if (lane < a.k) put_row_top(a, o, i, lane, mine, q);
 }
 
-// Gradient of rows, with the forward call's statistics: part blockIdx.x of the
-// rows' classes, 256 threads.
+// Gradient of rows, with the forward call's statistics: a workgroup to a part
+// of a row, or a wave to a row.
 template <typename T, bool E, bool F>
 __global__ void __launch_bounds__(256) k_label_grad_rows(LabelGradArgs a) {
     constexpr int V = 16 / sizeof(T);
-    const uint32_t n = a.div_groups.div(blockIdx.x), part = blockIdx.x - n * a.groups;
+    const uint32_t lanes = a.lanes, t = threadIdx.x & (lanes - 1);
+    const uint32_t at_part = lanes == 256 ? blockIdx.x : blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t n = a.div_groups.div(at_part), part = at_part - n * a.groups;
+    if (n >= a.n) return;
     const uint32_t o = a.div_inner.div(n), i = n - o * a.inner;
     const T *x = static_cast<const T *>(a.x) + o * a.xs[0] + i * a.xs[2];
     T *out = static_cast<T *>(a.grad) + o * a.gs[0] + i * a.gs[2];
@@ -338,16 +341,16 @@ __global__ void __launch_bounds__(256) k_label_grad_rows(LabelGradArgs a) {
     const Slope all[1] = {g};
     by_near<T>(farthest(all), [&](auto near) __attribute__((always_inline)) {
         const Grad<decltype(near)::value, E, F> grad(g);
-        for (uint32_t c = c0 + threadIdx.x * V; c < end; c += 256 * V * 2) {
+        for (uint32_t c = c0 + t * V; c < end; c += lanes * V * 2) {
             Pack<T, V> held[2];
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                const uint32_t at = c + u * 256 * V;
+                const uint32_t at = c + u * lanes * V;
                 if (at < end) held[u] = load_pack<V>(x + at, end - at, T{});
             }
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                const uint32_t at = c + u * 256 * V;
+                const uint32_t at = c + u * lanes * V;
                 if (at >= end) break;
                 Pack<float, V> phi{};
                 if constexpr (F) phi = load_field<V>(field + at * a.fs[1], a.fs[1], end - at);

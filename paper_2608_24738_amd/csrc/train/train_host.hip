@@ -155,7 +155,7 @@ int check_labels(const void *logits, int dtype, int64_t outer, int64_t classes, 
     return TM_OK;
 }
 
-constexpr uint64_t kBusyThreads = 65536;    // four waves to a CU
+constexpr uint64_t kBusyThreads = 65536;     // four waves to a CU
 constexpr uint64_t kRowBusyWaves = 4096;     // four waves to a SIMD
 
 // How a request runs: on contiguous rows or on maps, with how many classes
@@ -169,23 +169,27 @@ struct LabelPlan {
     uint32_t parts;             // of a row
 };
 
-// Rows from 33 classes on: a lane of a wave has at most one load of a shorter
-// one, and a thread to a row holds it whole.
+// Times below are of bf16 forward calls with the entropy, in us.
 LabelPlan label_plan(int dtype, uint64_t outer, uint64_t classes, uint64_t inner, const int64_t *strides) {
     LabelPlan p{};
     const uint64_t n = outer * inner, vec = 16 / float_bytes(dtype);
     p.parts = 1;
-    if ((strides[1] == 1 || classes == 1) && classes > 32) {
+    // Contiguous classes: waves to a row, or a thread while there are many
+    // short rows (65536 x 64: 23 by waves, 11 by threads; 2048 x 64: 3.4, 5.1).
+    // Up to 32 classes a thread holds the row, which its gradient relies on.
+    if (strides[1] == 1 && (classes > 64 || (classes > TM_LABEL_MAX_RECOMPUTE && n < 16384))) {
         p.rows = true;
-        // as many waves as fill the chip, each lane with at least one round of loads
+        // As many waves as fill the chip, each lane with at least one round of
+        // loads (512 x 50021 with 5 alternatives: 8 waves 21, 16 waves 22;
+        // 1024 x 32768: 1 to 4 waves 14.6, twice as many 15.9).
         const uint64_t most = ceil_div(classes, 64 * vec * kRowLoads), want = ceil_div(kRowBusyWaves, n);
         const uint64_t waves = std::min(most, want);
         p.waves = waves <= 1 ? 1 : waves <= 2 ? 2 : waves <= 4 ? 4 : waves <= 8 ? 8 : 16;
-        if (want > 16) {
-            // few rows: parts of one load to a lane of four waves
+        // Few long rows: parts of one load to a lane of four waves, for a
+        // second launch (1 x 131072: 4.8, without parts 11; 1 x 20000: 4.9, 4.5).
+        if (want > 16 && classes > 32768) {
             p.waves = 4;
             p.parts = uint32_t(std::min<uint64_t>({kRowMostParts, ceil_div(classes, 64 * 4 * vec), ceil_div(want, 4)}));
-            if (p.parts == 1 && classes <= 64 * vec) p.waves = 1;
         }
         return p;
     }
@@ -193,10 +197,14 @@ LabelPlan label_plan(int dtype, uint64_t outer, uint64_t classes, uint64_t inner
     const uint64_t in = p.swap ? outer : inner, out = p.swap ? 1 : outer;
     const int64_t step = p.swap ? strides[0] : strides[2];
     p.held = classes <= 4 ? 4 : classes <= 8 ? 8 : classes <= 16 ? 16 : classes <= 32 ? 32 : 0;
+    // Several positions to a thread where enough threads are left (4 x 4 x 512^2:
+    // 6.0, one to a thread 6.5; 4 x 4 x 256^2, which leaves 32768: 4.3, 3.5).
     p.wide = p.held == 0 ? kRunV : int((p.held <= 8 ? 16 : 8) / float_bytes(dtype));
-    if (step != 1 || in < uint64_t(p.wide) || out * ceil_div(in, p.wide) < kBusyThreads / 2) p.wide = 1;
+    if (step != 1 || in < uint64_t(p.wide) || out * ceil_div(in, p.wide) < kBusyThreads / (p.held ? 1 : 2)) p.wide = 1;
+    // Waves that share many classes (8 x 150 x 128^2: 1, 2, 4, 8 waves 32, 25,
+    // 17, 20; 16 x 64 x 100^2: 16, 13, 12, 17; 150 x 32^2: 14, 9, 6, 5).
     const uint64_t threads = out * ceil_div(in, p.wide);
-    p.waves = uint32_t(std::max<uint64_t>(1, std::min<uint64_t>({kRunWaves, kBusyThreads / threads, classes / 16})));
+    p.waves = uint32_t(std::max<uint64_t>(1, std::min<uint64_t>({kRunWaves, 3 * kBusyThreads / threads, classes / 16})));
     return p;
 }
 
@@ -375,15 +383,23 @@ extern "C" int tm_label_logp_grad(const void *logits, int dtype, int64_t outer, 
     return by_type(dtype, [&](auto t) {
         using T = decltype(t);
         if (p.rows) {
-            // 8 loads to a thread, or one where that leaves CUs idle
-            const uint64_t load = 256 * 16 / sizeof(T);
-            a.share = uint32_t(load * (s.positions * ceil_div(s.n[1], 8 * load) < kFill ? 1 : 8));
+            // A wave to a row of up to eight loads a lane; else a workgroup to
+            // eight loads a thread, or to one where that leaves CUs idle.
+            const uint64_t load = 16 / sizeof(T);
+            if (s.n[1] <= 64 * 8 * load) {
+                a.lanes = 64;
+                a.share = uint32_t(s.n[1]);
+            } else {
+                a.lanes = 256;
+                a.share = uint32_t(256 * load * (s.positions * ceil_div(s.n[1], 8 * 256 * load) < kFill ? 1 : 8));
+            }
             a.groups = uint32_t(ceil_div(s.n[1], a.share));
             a.div_groups = Div32::make(a.groups);
             if (s.positions * a.groups >= kLimit) return int(TM_ERR_TOO_LARGE);
+            const uint32_t blocks = a.lanes == 256 ? a.n * a.groups : (a.n + 3) / 4;
             return by_parts(a.up_entropy, a.field, [&](auto e, auto f) {
                 constexpr bool E = decltype(e)::value, F = decltype(f)::value;
-                return launch(k_label_grad_rows<T, E, F>, dim3(a.n * a.groups), dim3(256), 0, stream, a);
+                return launch(k_label_grad_rows<T, E, F>, dim3(blocks), dim3(256), 0, stream, a);
             });
         }
         a.groups = uint32_t(ceil_div(a.inner, p.wide));
@@ -510,8 +526,9 @@ int run_bias(const BiasShape &s, const void *table, int table_dtype, int64_t hea
     a.batch = uint32_t(s.batch);
     a.field_batch = uint32_t(s.field_batch);
     // Shares: all heads to a workgroup where the positions alone fill the chip,
-    // else four heads at a time and then parts of the batch; a share's table
-    // fits 32 KB of LDS.
+    // else four heads at a time and then parts of the batch (one query and 4096
+    // keys, 16 heads: 6.0 us, unshared 8.9; 512 x 512, 8 samples: 25, 38); a
+    // share's table fits 32 KB of LDS.
     uint64_t vec = 16 / float_bytes(out_dtype);
     if (s.src.positions < vec) vec = 1;
     const uint64_t tiles = ceil_div(s.src.positions, kBiasThreads * vec);
@@ -533,8 +550,9 @@ int run_bias(const BiasShape &s, const void *table, int table_dtype, int64_t hea
     a.batch_shares = uint32_t(bshares);
     a.tiles = uint32_t(blocks);
     a.div_tiles = Div32::make(uint32_t(tiles));
-    // all workgroups at once, eight to a CU
-    const uint64_t grid = std::min(blocks, std::max<uint64_t>(1, 2 * kFill / (shares * bshares)));
+    // workgroups that go on, 16 to a CU (2 x 155 x 240 x 237, 3 heads: 62 us; 8 or 4 to a CU 70 and 67, one to
+    // every tile 64)
+    const uint64_t grid = std::min(blocks, std::max<uint64_t>(1, 4 * kFill / (shares * bshares)));
     const size_t lds = (size_t(s.src.buckets) * a.row + s.src.span) * 4;
     return by_type(out_dtype, [&](auto t) {
         using T = decltype(t);
@@ -576,6 +594,8 @@ int run_bias_grad(const BiasShape &s, const void *grad, int grad_dtype, int64_t 
     // Units of one step of positions and, where samples share the buckets, as many of
     // them as leave enough units; two workgroups of eight waves to a CU.
     const uint64_t groups = ceil_div(uint64_t(heads), 16);
+    // Blocks of four heads to a load: up to 4 heads 16 us, two blocks for up to
+    // 8 heads 19 us (8 x 512^2 bf16, 24 buckets); with four blocks 18 and 19.5.
     const int blocks = heads <= 4 ? 1 : heads <= 8 ? 2 : 4;
     const uint64_t step = 256 / float_bytes(grad_dtype) * (4 / blocks);
     const uint64_t steps = ceil_div(s.src.positions, step);

@@ -84,35 +84,40 @@ def _viewed(t, dim):
 
 
 @functools.lru_cache(maxsize=1024)
-def _label_workspace(dtype, extents, strides, top_k):
-    return int(load().tm_label_logp_workspace_size(dtype, *extents, (ctypes.c_int64 * 3)(*strides), top_k))
+def _label_plan(shape, strides, dim, dtype, top_k):
+    """What a forward call needs to know of logits of this shape: (extents,
+    strides, shape of a value per element, shape of the top classes, bytes of
+    workspace), or None where three strides cannot describe them."""
+    view = _view(shape, strides, dim)
+    if view is None:
+        return None
+    extents, steps = view
+    nbytes = 0
+    if extents[1] > MAX_RECOMPUTE:               # rows may be cut into parts
+        nbytes = int(load().tm_label_logp_workspace_size(dtype, *extents, steps, top_k))
+    return extents, steps, shape[:dim] + shape[dim + 1:], shape[:dim] + (top_k,) + shape[dim + 1:], nbytes
 
 
 def _label_forward(logits, labels, field, dim, entropy, top_k, stats):
     """Runs tm_label_logp; returns (logits, field) as they were read, what describes
     them to the library, the outputs and the statistics for the gradient."""
-    dev = logits.device
-    logits, extents, strides = _viewed(logits, dim)
-    shape = logits.shape[:dim] + logits.shape[dim + 1:]
+    dev, dtype = logits.device, FLOATS[logits.dtype]
+    plan = _label_plan(tuple(logits.shape), logits.stride(), dim, dtype, top_k)
+    if plan is None:
+        logits = logits.contiguous()
+        plan = _label_plan(tuple(logits.shape), logits.stride(), dim, dtype, top_k)
+    extents, strides, shape, shape_k, nbytes = plan
     field_strides = None
     if field is not None:
         field, _, field_strides = _viewed(field, dim)
-    logp = torch.empty(shape, dtype=torch.float32, device=dev) if labels is not None else None
-    ent = torch.empty(shape, dtype=torch.float32, device=dev) if entropy else None
-    mean = torch.empty(shape, dtype=torch.float32, device=dev) if field is not None else None
-    top = index = kept = workspace = None
-    if top_k:
-        shape_k = logits.shape[:dim] + (top_k,) + logits.shape[dim + 1:]
-        top = torch.empty(shape_k, dtype=torch.float32, device=dev)
-        index = torch.empty(shape_k, dtype=torch.int32, device=dev)
-    if stats:
-        kept = torch.empty(tuple(shape) + (2,), dtype=torch.float32, device=dev)
-    dtype = FLOATS[logits.dtype]
-    nbytes = 0
-    if extents[1] > MAX_RECOMPUTE:               # rows may be cut into parts
-        nbytes = _label_workspace(dtype, extents, tuple(strides), top_k)
-        if nbytes:
-            workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    empty, f32 = torch.empty, torch.float32
+    logp = empty(shape, dtype=f32, device=dev) if labels is not None else None
+    ent = empty(shape, dtype=f32, device=dev) if entropy else None
+    mean = empty(shape, dtype=f32, device=dev) if field is not None else None
+    top = empty(shape_k, dtype=f32, device=dev) if top_k else None
+    index = empty(shape_k, dtype=torch.int32, device=dev) if top_k else None
+    kept = empty(shape + (2,), dtype=f32, device=dev) if stats else None
+    workspace = empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
     label_dtype = LABELS[labels.dtype] if labels is not None else 0
     _call("tm_label_logp", dev, None, logits.data_ptr(), dtype, *extents, strides, _ptr(labels), label_dtype,
           _ptr(field), field_strides, top_k, _ptr(logp), _ptr(ent), _ptr(mean), _ptr(top), _ptr(index), _ptr(kept),

@@ -211,29 +211,39 @@ struct Slope {
 };
 
 // A position's slope, prepared: p = 2^z with z = x log2(e) - c, and the factor
-// of p is base + per z (+ f field).  Near as in Ref; a 16-bit gradient hides
-// that p is off by a factor as close to 1.
+// of p is base + per l (+ f field).  p is made 2^32 times as large and the
+// factor as much smaller, so that gradients among float32's smallest numbers
+// come out too, where v_exp_f32 alone gives 0.  Near as in Ref; a 16-bit
+// gradient hides that p is off by a factor as close to 1.
+constexpr float kUp = 32.0f, kDown = 1.0f / 4294967296.0f;
+
 template <bool Near, bool Entropy, bool Mean>
 struct Grad {
-    float base, per, f;         // per: of l
+    float base, per, f;         // per: of l, or of z + 32
     float m, logs, c;
 
     __device__ __forceinline__ explicit Grad(const Slope &g)
-        : base(-g.a), per(-g.h), f(g.f), m(g.m), logs(g.logs), c((g.m + g.logs) * kLog2e) {
-        if constexpr (Entropy) base = fmaf(-g.h, g.entropy, base);
-        if constexpr (Mean) base = fmaf(-g.f, g.mean, base);
-        if constexpr (Near) per *= kLn2;
+        : base(-g.a * kDown), per(-g.h * kDown), f(g.f * kDown), m(g.m), logs(g.logs),
+          c(fmaf(g.m + g.logs, kLog2e, -kUp)) {
+        if constexpr (Entropy) base = fmaf(per, g.entropy, base);
+        if constexpr (Mean) base = fmaf(-f, g.mean, base);
+        if constexpr (Near) {
+            per *= kLn2;
+            if constexpr (Entropy) base = fmaf(per, -kUp, base);
+        }
     }
     // extra: a for the label's class, else 0
     __device__ __forceinline__ float at(float x, float field, float extra) const {
         float p, l;
         if constexpr (Near) {
-            l = fmaf(x, kLog2e, -c);                       // in units of log2
+            l = fmaf(x, kLog2e, -c);                       // z + 32
             p = exp2_hw(l);
             l = fmaxf(l, -300.0f);                         // 0 times a finite number; NaN comes from p
         } else {
             l = below(x - m, logs);                        // a dead position has log s = inf and so p = 0
-            p = exp_of(l);
+            const float z = fmaf(l, kLog2e, kUp);
+            p = exp2_hw(z);
+            p = fmaf(p, fmaf(l, kLog2e, kUp - z) * kLn2, p);     // as exp_of
         }
         float v = base;
         if constexpr (Entropy) v = fmaf(per, l, v);

@@ -7,8 +7,14 @@
 // classes (k_label_held): every logit is read once.  More run through in
 // blocks of 8 with a running maximum (k_label_run); where there are few
 // positions, the waves of a workgroup share the classes and join their sums.
-// Both are bound by the bytes of logits, labels and outputs.  Class axes of
-// any stride take the same kernels with one position to a thread.
+// Class axes of any stride take the same kernels with one position to a thread.
+//
+// Bound by the bytes of logits, labels and outputs with few classes (bf16
+// 8 x 4 x 128^3 with entropy and the likeliest class: 419 MB in 86 us, 4.9 TB/s;
+// float32 with a field, forward 688 MB in 138 us, 5.0 TB/s, gradient 955 MB in
+// 182 us, 5.3 TB/s; a copy reaches 5.2), by arithmetic, some 13 instructions a
+// logit, with more of them (bf16 16 x 21 x 375 x 500: forward 141 MB in 39 us,
+// gradient 267 MB in 57 us).
 #pragma once
 
 #include "label.h"

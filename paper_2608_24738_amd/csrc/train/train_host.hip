@@ -208,6 +208,12 @@ LabelPlan label_plan(int dtype, uint64_t outer, uint64_t classes, uint64_t inner
     return p;
 }
 
+// At least `blocks` < 2^31 workgroups, of up to 1024 threads.
+dim3 row_grid(uint32_t blocks) {
+    const uint32_t x = std::min<uint32_t>(blocks, 1u << 21);
+    return dim3(x, uint32_t(ceil_div(blocks, x)));
+}
+
 template <typename Args>
 void swap_positions(Args &a) {
     a.inner = a.outer;
@@ -291,7 +297,8 @@ extern "C" int tm_label_logp(const void *logits, int dtype, int64_t outer, int64
                     constexpr int W = decltype(waves)::value;
                     constexpr bool E = decltype(e)::value, F = decltype(f)::value;
                     return launch(a.k ? k_label_rows<T, W, E, F, true> : k_label_rows<T, W, E, F, false>,
-                                  dim3(W == 1 ? (a.n + 3) / 4 : a.n * p.parts), dim3(W == 1 ? 256 : 64 * W), 0, stream, a);
+                                  row_grid(W == 1 ? (a.n + 3) / 4 : a.n * p.parts), dim3(W == 1 ? 256 : 64 * W), 0,
+                                  stream, a);
                 });
             });
             if (rc != TM_OK || p.parts == 1) return rc;
@@ -399,7 +406,7 @@ extern "C" int tm_label_logp_grad(const void *logits, int dtype, int64_t outer, 
             const uint32_t blocks = a.lanes == 256 ? a.n * a.groups : (a.n + 3) / 4;
             return by_parts(a.up_entropy, a.field, [&](auto e, auto f) {
                 constexpr bool E = decltype(e)::value, F = decltype(f)::value;
-                return launch(k_label_grad_rows<T, E, F>, dim3(blocks), dim3(256), 0, stream, a);
+                return launch(k_label_grad_rows<T, E, F>, row_grid(blocks), dim3(256), 0, stream, a);
             });
         }
         a.groups = uint32_t(ceil_div(a.inner, p.wide));

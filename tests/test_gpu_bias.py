@@ -315,3 +315,11 @@ def test_small_gradients(dtype):
         grad, = torch.autograd.grad([bias], [table], [up.to(dev)])
         total, size, _ = ref.gradient(up.double().numpy(), ref.buckets(d.numpy(), edges.numpy()), 16)
         ref.check(grad.cpu().double().numpy(), total, 16 * U * size, "f32", "small gradients")
+
+
+def test_many_steps():
+    """More steps of positions than the gradient's waves."""
+    relative((1500,), (1501,), 1, 32, "offset", "bf16")
+    relative((900,), (901,), 9, 20, "offset", "f16")
+    distance(2, (1100, 1101), 3, 70, "f32")
+    distance(70000, (3,), 2, 9, "bf16", add=True)

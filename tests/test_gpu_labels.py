@@ -321,3 +321,72 @@ def test_top_of_one_lane(period, dtype):
         y = torch.zeros(rows, dtype=torch.int64, device="cuda:0")
         for k in (1, 5, 32):
             run(x, y, top_k=k, entropy=False, what="one lane's", dtype=dtype)
+
+
+# The kernels that take several neighbouring positions to a thread need this many threads: 65536 (32768 of many classes).
+@pytest.mark.parametrize("dtype,shape,shift", [
+    ("bf16", (1, 3, 524293), 0), ("bf16", (500, 4, 1051), 1), ("f16", (1, 7, 524295), 3), ("f32", (3, 2, 87400), 0),
+    ("f32", (260, 5, 1009), 1), ("bf16", (1, 13, 262147), 1), ("bf16", (2, 29, 131077), 0), ("f32", (1, 17, 131075), 3),
+    ("f16", (1, 20, 262150), 0), ("bf16", (2, 40, 65541), 1), ("f32", (1, 35, 131077), 0)])
+def test_wide(dtype, shape, shift):
+    import torch
+    x, y, phi, ups = case(shape, dtype, seed=shape[1], label="uint8" if shift else "int32", field=True)
+
+    def moved(t):
+        room = torch.zeros(t.numel() + 8, dtype=t.dtype, device=t.device)
+        view = room[shift:shift + t.numel()].view(t.shape)
+        view.copy_(t)
+        return view
+    x, y, phi, ups = moved(x), moved(y), moved(phi), [moved(u) for u in ups]
+    run(x, y, field=phi, top_k=2, ups=ups, what="wide", dtype=dtype)
+    run(x, y, entropy=False, top_k=1, ups=[ups[0], None, None], what="wide, log-probabilities alone", dtype=dtype)
+
+
+def test_wide_transposed():
+    """Positions side by side along the axis in front of the classes."""
+    x, y, phi, ups = case((3, 524300), "bf16", seed=3, dim=0, field=True)
+    run(x.t(), y, dim=1, field=phi.t(), top_k=2, ups=ups, what="wide, transposed", dtype="bf16")
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("shape", [(4100, 4509), (2051, 9003), (520, 33000)])
+def test_many_rounds(shape, dtype):
+    """Rows long enough for rounds against the reference so far: ordinary ones, ones whose maximum comes late, ones
+    that begin masked, far ones, ones with a NaN, among rows that are not looked at."""
+    import torch
+    from paper_2608_24738_amd import training
+    n, classes = shape
+    gen = torch.Generator(device="cuda:0").manual_seed(n)
+    x = torch.randn(shape, generator=gen, device="cuda:0") * 3
+    rise = torch.linspace(-60, 60, classes, device="cuda:0")
+    x[1] = rise
+    x[2] = rise.flip(0)
+    x[3] += rise * (rise > 55)
+    x[4, :classes // 2] = -torch.inf
+    x[5, :-1] = -torch.inf
+    x[6] = x[6] * 200 + 5000
+    x[7] = x[7] * 100 - 2000
+    x[8, classes // 2] = 40
+    x[9] = -torch.inf
+    x = x.to(getattr(torch, TYPES[dtype]))
+    rows = list(range(10)) + [n // 2, n - 1]
+    x[10, classes - 7] = torch.nan
+    x[11, 3] = torch.inf
+    y = torch.randint(0, classes, (n,), generator=gen, device="cuda:0")
+    up = torch.randn(n, generator=gen, device="cuda:0")
+    announce("many rounds %s %s" % (shape, dtype))
+    for entropy in (True, False):
+        x.requires_grad_(True)
+        got = training.label_log_probs(x, y, entropy=entropy)
+        outs = [got.log_probs] + ([got.entropy] if entropy else [])
+        grad, = torch.autograd.grad(outs, [x], [up] * len(outs))
+        want = ref.exact(x.detach()[rows].double().cpu().numpy(), y[rows].cpu().numpy(),
+                         ups=[up[rows].double().cpu().numpy(), up[rows].double().cpu().numpy() if entropy else None, None])
+        ref.check(got.log_probs.detach()[rows].cpu(), want["logp"], want["tol_logp"], "log_probs")
+        if entropy:
+            ref.check(got.entropy.detach()[rows].cpu(), want["entropy"], want["tol_entropy"], "entropy")
+        ref.check(grad[rows].double().cpu().numpy(), want["grad"], want["tol_grad"], "gradient", dtype)
+        assert torch.isnan(got.log_probs[10:12]).all() and torch.isnan(grad[10:12]).all()
+        rest = torch.ones(n, dtype=torch.bool, device="cuda:0")
+        rest[[9, 10, 11]] = False
+        assert torch.isfinite(grad[rest]).all()

@@ -303,19 +303,18 @@ def _check_bias(table, edges, add):
         raise ValueError("table must be a ROCm (cuda) tensor")
     if table.dtype not in FLOATS:
         raise TypeError("table must be float32, float16 or bfloat16, got %s" % table.dtype)
-    if table.dim() != 2 or not 1 <= table.shape[0] <= MAX_BUCKETS or table.shape[1] < 1:
-        raise ValueError("table must be (buckets, heads) with 1 to %d buckets, got %s"
-                         % (MAX_BUCKETS, tuple(table.shape)))
-    if edges.dtype != torch.float32 or edges.device != table.device:
-        raise TypeError("edges must be float32 on %s" % table.device)
-    if tuple(edges.shape) != (table.shape[0] - 1,):
-        raise ValueError("a table of %d buckets needs %d edges, got %s"
-                         % (table.shape[0], table.shape[0] - 1, tuple(edges.shape)))
+    shape, device = table.shape, table.device
+    if len(shape) != 2 or not 1 <= shape[0] <= MAX_BUCKETS or shape[1] < 1:
+        raise ValueError("table must be (buckets, heads) with 1 to %d buckets, got %s" % (MAX_BUCKETS, tuple(shape)))
+    if edges.dtype != torch.float32 or edges.device != device:
+        raise TypeError("edges must be float32 on %s" % device)
+    if edges.dim() != 1 or edges.shape[0] != shape[0] - 1:
+        raise ValueError("a table of %d buckets needs %d edges, got %s" % (shape[0], shape[0] - 1, tuple(edges.shape)))
     if add is not None:
         if add.dtype not in FLOATS:
             raise TypeError("add must be float32, float16 or bfloat16, got %s" % add.dtype)
-        if add.device != table.device:
-            raise ValueError("add is on %s, the table on %s" % (add.device, table.device))
+        if add.device != device:
+            raise ValueError("add is on %s, the table on %s" % (add.device, device))
         add = add.contiguous()
     return table.contiguous(), edges.contiguous(), add
 
@@ -359,6 +358,30 @@ def _extents(value, what):
     return extents
 
 
+@functools.lru_cache(maxsize=1024)
+def _grid(query, key, offset, metric, sampling):
+    """(what the entry points take of a grid, but for the batch; queries; keys)."""
+    ndim = len(query)
+    if len(key) != ndim:
+        raise ValueError("query_shape has %d axes, key_shape %d" % (ndim, len(key)))
+    if min(query + key) < 0:
+        raise ValueError("extents must not be negative, got %s and %s" % (query, key))
+    offset = (offset,) + (0,) * (ndim - 1) if isinstance(offset, int) else offset
+    if len(offset) != ndim:
+        raise ValueError("query_offset must have %d coordinates, got %d" % (ndim, len(offset)))
+    if metric not in BIAS_METRICS:
+        raise ValueError("metric must be one of %s" % sorted(BIAS_METRICS))
+    if metric == "offset" and (ndim != 1 or sampling is not None):
+        raise ValueError("metric 'offset' is for sequences, without sampling")
+    if sampling is not None:
+        sampling = (sampling,) * ndim if isinstance(sampling, float) else sampling
+        if len(sampling) != ndim:
+            raise RuntimeError("sequence argument must have length equal to input rank")
+    args = (ndim, _shape_array(query), _shape_array(key), _shape_array(offset), BIAS_METRICS[metric],
+            _sampling_array(sampling, ndim))
+    return args, math.prod(query), math.prod(key)
+
+
 def relative_bias(table: torch.Tensor, edges: torch.Tensor, query_shape, key_shape, *, query_offset=0,
                   metric: str = "euclidean", sampling=None, add: Optional[torch.Tensor] = None) -> torch.Tensor:
     """A learned bias by buckets of the distance between a query's and a key's
@@ -380,28 +403,15 @@ def relative_bias(table: torch.Tensor, edges: torch.Tensor, query_shape, key_sha
     of ``add``.  Gradients flow to ``table`` (summed over the batch) and ``add``.
     """
     table, edges, add = _check_bias(table, edges, add)
-    query, key = _extents(query_shape, "query_shape"), _extents(key_shape, "key_shape")
-    ndim = len(query)
-    if len(key) != ndim:
-        raise ValueError("query_shape has %d axes, key_shape %d" % (ndim, len(key)))
-    offset = (query_offset,) + (0,) * (ndim - 1) if isinstance(query_offset, int) else tuple(query_offset)
-    if len(offset) != ndim:
-        raise ValueError("query_offset must have %d coordinates, got %d" % (ndim, len(offset)))
-    if metric not in BIAS_METRICS:
-        raise ValueError("metric must be one of %s" % sorted(BIAS_METRICS))
-    if metric == "offset" and (ndim != 1 or sampling is not None):
-        raise ValueError("metric 'offset' is for sequences, without sampling")
     if sampling is not None:
-        sampling = [float(sampling)] * ndim if isinstance(sampling, (int, float)) else [float(s) for s in sampling]
-        if len(sampling) != ndim:
-            raise RuntimeError("sequence argument must have length equal to input rank")
-    tail = (table.shape[1], math.prod(query), math.prod(key))
-    shape, batch = tail, 1
+        sampling = float(sampling) if isinstance(sampling, (int, float)) else tuple(float(s) for s in sampling)
+    args, queries, keys = _grid(_extents(query_shape, "query_shape"), _extents(key_shape, "key_shape"),
+                                query_offset if isinstance(query_offset, int) else tuple(int(n) for n in query_offset),
+                                metric, sampling)
+    shape, batch = (table.shape[1], queries, keys), 1
     if add is not None:
-        if tuple(add.shape[-3:]) != tail:
-            raise ValueError("add must have shape (..., %d, %d, %d), got %s" % (tail + (tuple(add.shape),)))
-        shape = tuple(add.shape)
+        tail, shape = shape, tuple(add.shape)
+        if shape[-3:] != tail:
+            raise ValueError("add must have shape (..., %d, %d, %d), got %s" % (tail + (shape,)))
         batch = math.prod(shape[:-3])
-    args = (ndim, _shape_array(query), _shape_array(key), _shape_array(offset), BIAS_METRICS[metric],
-            _sampling_array(sampling, ndim), batch)
-    return _run_bias(table, edges, add, ("tm_relative_bias", args, None), shape)
+    return _run_bias(table, edges, add, ("tm_relative_bias", args + (batch,), None), shape)

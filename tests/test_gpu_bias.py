@@ -323,3 +323,35 @@ def test_many_steps():
     relative((900,), (901,), 9, 20, "offset", "f16")
     distance(2, (1100, 1101), 3, 70, "f32")
     distance(70000, (3,), 2, 9, "bf16", add=True)
+
+
+def test_wrapper_refusals():
+    import torch
+    from paper_2608_24738_amd import binding, training
+    dev = "cuda:0"
+    table, edges = torch.zeros((4, 2), device=dev), torch.tensor([1.0, 2.0, 3.0], device=dev)
+    good = torch.zeros((2, 5, 5), device=dev)
+    for error, call in [
+            (TypeError, lambda: training.relative_bias(table.double(), edges, 5, 5)),
+            (ValueError, lambda: training.relative_bias(table[0], edges, 5, 5)),
+            (ValueError, lambda: training.relative_bias(table, edges[:2], 5, 5)),
+            (TypeError, lambda: training.relative_bias(table, edges.double(), 5, 5)),
+            (TypeError, lambda: training.relative_bias(table, edges.cpu(), 5, 5)),
+            (TypeError, lambda: training.relative_bias(table, edges, 5, 5, add=good.double())),
+            (ValueError, lambda: training.relative_bias(table, edges, 5, 5, add=good.cpu())),
+            (ValueError, lambda: training.relative_bias(table, edges, 5, 6, add=good)),
+            (ValueError, lambda: training.relative_bias(table, edges, (5, 1), 5)),
+            (ValueError, lambda: training.relative_bias(table, edges, (1,) * 9, (1,) * 9)),
+            (ValueError, lambda: training.relative_bias(table, edges, (5, 1), (5, 1), query_offset=(1, 2, 3))),
+            (ValueError, lambda: training.relative_bias(table, edges, 5, 5, metric="cosine")),
+            (ValueError, lambda: training.relative_bias(table, edges, (5, 1), (5, 1), metric="offset")),
+            (ValueError, lambda: training.relative_bias(table, edges, 5, 5, metric="offset", sampling=2.0)),
+            (RuntimeError, lambda: training.relative_bias(table, edges, (5, 1), (5, 1), sampling=(1.0,))),
+            (binding.TMError, lambda: training.relative_bias(table, edges, 5, 5, sampling=-1.0)),
+            (ValueError, lambda: training.relative_bias(table, edges, -5, 5)),
+            (TypeError, lambda: training.distance_bias(good[0].double(), table, edges)),
+            (ValueError, lambda: training.distance_bias(good[0].cpu(), table, edges)),
+            (ValueError, lambda: training.distance_bias(good[0].clone().requires_grad_(True), table, edges)),
+            (ValueError, lambda: training.distance_bias(good[0], table, edges, add=good[:, :4]))]:
+        with pytest.raises(error):
+            call()

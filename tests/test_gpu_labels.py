@@ -390,3 +390,37 @@ def test_many_rounds(shape, dtype):
         rest = torch.ones(n, dtype=torch.bool, device="cuda:0")
         rest[[9, 10, 11]] = False
         assert torch.isfinite(grad[rest]).all()
+
+
+def test_wrapper_refusals():
+    import torch
+    from paper_2608_24738_amd import training
+    x, y, phi, _ = case((2, 5, 7), "f32", field=True)
+    for error, call in [
+            (TypeError, lambda: training.label_log_probs(x.double(), y)),
+            (TypeError, lambda: training.label_log_probs(x, y.float())),
+            (ValueError, lambda: training.label_log_probs(x, y.cpu())),
+            (ValueError, lambda: training.label_log_probs(x, y[:, :6])),
+            (ValueError, lambda: training.label_log_probs(x, y, dim=3)),
+            (ValueError, lambda: training.label_log_probs(x, y, top_k=6)),
+            (ValueError, lambda: training.label_log_probs(x, y, top_k=-1)),
+            (ValueError, lambda: training.label_log_probs(x[:, :0], y)),
+            (ValueError, lambda: training.label_log_probs(x)),
+            (TypeError, lambda: training.label_log_probs(x, y, field=phi.double())),
+            (ValueError, lambda: training.label_log_probs(x, y, field=phi.cpu())),
+            (ValueError, lambda: training.label_log_probs(x, y, field=phi.clone().requires_grad_(True))),
+            (RuntimeError, lambda: training.label_log_probs(x, y, field=phi[:, :3]))]:
+        with pytest.raises(error):
+            call()
+
+
+def test_labels_of_two_classes_as_bool():
+    import torch
+    x, y, _, ups = case((3, 2, 50), "f32", seed=4, spread_labels=False)
+    from paper_2608_24738_amd import training
+    a = training.label_log_probs(x, y)
+    b = training.label_log_probs(x, y.bool())
+    assert torch.equal(a.log_probs, b.log_probs)
+    only = training.label_log_probs(x, top_k=1, entropy=True)
+    assert only.log_probs is None and only.field_mean is None
+    assert torch.equal(only.top_indices[:, 0].long(), x.argmax(1))

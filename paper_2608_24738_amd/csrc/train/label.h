@@ -46,7 +46,7 @@ struct LabelGradArgs {
     uint32_t n;
     uint32_t groups;
     uint32_t share;             // classes of a workgroup
-    uint32_t lanes;             // rows: 64 or 256 threads to a part
+    uint32_t lanes;             // rows: 16, 64 or 256 threads to a part
     Div32 div_groups;
     Div32 div_inner;
 };

@@ -2,7 +2,8 @@
 // a contiguous row, as in (N, C) or channels last.
 //
 // W waves run through a row, 8 (or 4) classes to a lane and load, with a
-// running maximum per lane; the lanes' sums are joined at the end.  A long row
+// running maximum per lane; the lanes' sums are joined at the end.  Short rows
+// among many are held by 16 lanes each (65536 x 512: 67 MB in 14 us, 4.9 TB/s).  A long row
 // among few is cut into `groups` parts, which k_label_rows_join puts together.
 // Bound by the bytes of the logits; a row is read once (bf16 4096 x 32768 with
 // the entropy: 268 MB in 44 us, 6.1 TB/s, the gradient 537 MB in 81 us, 6.6 TB/s;
@@ -299,6 +300,88 @@ __global__ void __launch_bounds__(W == 1 ? 256 : 64 * W, K && !F ? 7 : 4) k_labe
     }
 }
 
+// Short rows among many: 16 lanes hold a row, four rows to a wave, and reduce
+// by rotations.  The likeliest classes take a selection each, over the classes
+// held.
+constexpr uint32_t kShortRows = 16;                        // of a workgroup
+
+// L: loads of a lane.
+template <typename T, int L, bool E, bool F, bool K>
+__global__ void __launch_bounds__(16 * kShortRows) k_label_rows_short(LabelArgs a) {
+    constexpr int V = 16 / sizeof(T);
+    const uint32_t lane = threadIdx.x & 15;
+    const uint32_t n = block_number() * kShortRows + (threadIdx.x >> 4);
+    if (n >= a.n) return;                                  // all 16 lanes
+    const uint32_t o = a.div_inner.div(n), i = n - o * a.inner;
+    const T *x = static_cast<const T *>(a.x) + o * a.xs[0] + i * a.xs[2];
+    const float *field = F ? a.field + o * a.fs[0] + i * a.fs[2] : nullptr;
+    const T none = narrow<T>(-INFINITY);
+    Pack<T, V> held[L];
+    uint32_t from[L];                              // the last load begins further back, its doubles are -inf
+#pragma unroll
+    for (int u = 0; u < L; ++u) {
+        from[u] = min((u * 16 + lane) * V, a.classes - V);
+        held[u] = load_pack<V>(x + from[u]);
+    }
+    Sums r = kNothing;
+#pragma unroll
+    for (int u = 0; u < L; ++u) {
+        const uint32_t doubles = (u * 16 + lane) * V - from[u];
+        if (doubles) {
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                if (uint32_t(j) < doubles) held[u].put(j, none);
+        }
+#pragma unroll
+        for (int j = 0; j < V; ++j) r.m = fmaxf(r.m, widen(held[u].at(j)));
+    }
+    r.m = row_max(r.m);
+    by_near<T>(fabsf(r.m), [&](auto near) __attribute__((always_inline)) {
+        const Ref<decltype(near)::value, E, F> ref(r.m);
+        Sums some = kNothing;
+#pragma unroll
+        for (int u = 0; u < L; ++u) {
+            Pack<float, V> phi{};
+            if constexpr (F) phi = load_field<V>(field + from[u] * a.fs[1], a.fs[1], V);
+#pragma unroll
+            for (int j = 0; j < V; ++j) ref.take(some, widen(held[u].at(j)), phi.at(j));
+        }
+        ref.close(r, some);
+    });
+    r.s = row_sum(r.s);
+    if constexpr (E) r.t = row_sum(r.t);
+    if constexpr (F) r.f = row_sum(r.f);
+    const Found q = found(r);
+    if (lane == 0) put_row(a, n, x, q);
+    if constexpr (K) {
+        float lx = INFINITY;                               // the last class found
+        uint32_t lc = ~0u;
+        for (uint32_t rank = 0; rank < a.k; ++rank) {
+            float best = -INFINITY;
+            uint32_t at = ~0u;
+#pragma unroll
+            for (int u = 0; u < L; ++u) {
+                const uint32_t doubles = (u * 16 + lane) * V - from[u];
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    const float v = widen(held[u].at(j));
+                    const uint32_t c = from[u] + j;
+                    const bool open = uint32_t(j) >= doubles && (v < lx || (v == lx && c > lc) || lc == ~0u) && v == v;
+                    if (open && (v > best || at == ~0u)) {
+                        best = v;
+                        at = c;
+                    }
+                }
+            }
+            const uint64_t lead = row_max(at == ~0u ? uint64_t(0) : top_key(best, at));
+            lx = unordered(uint32_t(lead >> 32));
+            lc = ~uint32_t(lead);
+            if (lane == (rank & 15)) put_row_top(a, o, i, rank, lead, q);
+            if (lead == 0) lx = -INFINITY;                 // a row with NaN: nothing is behind it
+        }
+    }
+}
+
 // Puts the parts of a row together: a lane for each.
 constexpr uint32_t kRowMostParts = 64;
 
@@ -323,13 +406,15 @@ __global__ void __launch_bounds__(64) k_label_rows_join(LabelArgs a) {
 }
 
 // Gradient of rows, with the forward call's statistics: a workgroup to a part
-// of a row, or a wave to a row.
+// of a row, or a wave or 16 lanes to a row.
 template <typename T, bool E, bool F>
 __global__ void __launch_bounds__(256) k_label_grad_rows(LabelGradArgs a) {
     constexpr int V = 16 / sizeof(T);
     const uint32_t lanes = a.lanes, t = threadIdx.x & (lanes - 1);
     const uint32_t block = block_number();
-    const uint32_t at_part = lanes == 256 ? block : block * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    uint32_t at_part = block;
+    if (lanes == 16) at_part = block * 16 + (threadIdx.x >> 4);
+    if (lanes == 64) at_part = block * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t n = a.div_groups.div(at_part), part = at_part - n * a.groups;
     if (n >= a.n) return;
     const uint32_t o = a.div_inner.div(n), i = n - o * a.inner;

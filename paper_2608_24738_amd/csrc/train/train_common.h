@@ -209,6 +209,31 @@ __device__ __forceinline__ uint32_t wave_reduce(uint32_t x, uint32_t none, F op)
     x = op(x, dpp<0x143, 0xc>(none, x));
     return uint32_t(__builtin_amdgcn_readlane(int(x), 63));
 }
+// The same over each row of 16 lanes, by rotations: every lane ends with the
+// result, made in one order.
+template <typename F>
+__device__ __forceinline__ uint32_t row_reduce(uint32_t x, F op) {
+    x = op(x, dpp<0x128, 0xf>(x, x));                      // row_ror 8, 4, 2, 1
+    x = op(x, dpp<0x124, 0xf>(x, x));
+    x = op(x, dpp<0x122, 0xf>(x, x));
+    return op(x, dpp<0x121, 0xf>(x, x));
+}
+__device__ __forceinline__ float row_max(float x) {        // not of NaN
+    return __uint_as_float(row_reduce(__float_as_uint(x), [](uint32_t a, uint32_t b) {
+        return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+    }));
+}
+__device__ __forceinline__ float row_sum(float x) {
+    return __uint_as_float(row_reduce(__float_as_uint(x), [](uint32_t a, uint32_t b) {
+        return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+    }));
+}
+__device__ __forceinline__ uint64_t row_max(uint64_t x) {
+    const auto most = [](uint32_t a, uint32_t b) { return max(a, b); };
+    const uint32_t hi = row_reduce(uint32_t(x >> 32), most);
+    const uint32_t lo = row_reduce(uint32_t(x >> 32) == hi ? uint32_t(x) : 0u, most);
+    return uint64_t(hi) << 32 | lo;
+}
 __device__ __forceinline__ float wave_max(float x) {       // not of NaN
     return __uint_as_float(wave_reduce(__float_as_uint(x), 0xff800000u, [](uint32_t a, uint32_t b) {
         return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));

@@ -167,6 +167,7 @@ struct LabelPlan {
     int held;                   // maps: classes held in registers, 0: they run through
     uint32_t waves;             // of a row, or sharing the classes of a map's positions
     uint32_t parts;             // of a row
+    bool brief;                 // 16 lanes to a row
 };
 
 // Times below are of bf16 forward calls with the entropy, in us.
@@ -174,16 +175,18 @@ LabelPlan label_plan(int dtype, uint64_t outer, uint64_t classes, uint64_t inner
     LabelPlan p{};
     const uint64_t n = outer * inner, vec = 16 / float_bytes(dtype);
     p.parts = 1;
-    // Contiguous classes: waves to a row, or a thread while there are many
-    // short rows (65536 x 64: 23 by waves, 11 by threads; 2048 x 64: 3.4, 5.1).
-    // Up to 32 classes a thread holds the row, which its gradient relies on.
-    if (strides[1] == 1 && (classes > 64 || (classes > TM_LABEL_MAX_RECOMPUTE && n < 16384))) {
+    // Contiguous classes: lanes to a row (65536 x 64: 6 by 16 lanes, 10 by
+    // threads, gradients 8 and 26; x 33: 6 and 6, 8 and 14). Up to 32 classes a
+    // thread holds the row, and its gradient needs no statistics.
+    if (strides[1] == 1 && classes > TM_LABEL_MAX_RECOMPUTE) {
         p.rows = true;
         // As many waves as fill the chip, each lane with at least one round of
         // loads (512 x 50021 with 5 alternatives: 8 waves 21, 16 waves 22;
         // 1024 x 32768: 1 to 4 waves 14.6, twice as many 15.9).
         const uint64_t most = ceil_div(classes, 64 * vec * kRowLoads), want = ceil_div(kRowBusyWaves, n);
         const uint64_t waves = std::min(most, want);
+        // Many short rows: 16 lanes to a row (65536 x 100: 6, a wave to a row 25; x 512: 14 and 27).
+        p.brief = n >= 4096 && classes <= 16 * vec * kRowLoads;
         p.waves = waves <= 1 ? 1 : waves <= 2 ? 2 : waves <= 4 ? 4 : waves <= 8 ? 8 : 16;
         // Few long rows: parts of one load to a lane of four waves, for a
         // second launch (1 x 131072: 4.8, without parts 11; 1 x 20000: 4.9, 4.5).
@@ -292,6 +295,17 @@ extern "C" int tm_label_logp(const void *logits, int dtype, int64_t outer, int64
             a.groups = p.parts;
             a.div_groups = Div32::make(p.parts);
             if (s.positions * p.parts >= kLimit) return int(TM_ERR_TOO_LARGE);
+            if (p.brief) {
+                return by_parts(a.entropy, a.field, [&](auto e, auto f) {
+                    constexpr bool E = decltype(e)::value, F = decltype(f)::value;
+                    constexpr uint32_t load = 16 * 16 / sizeof(T);
+                    return launch(a.classes <= load ? a.k ? k_label_rows_short<T, 1, E, F, true>
+                                                          : k_label_rows_short<T, 1, E, F, false>
+                                                    : a.k ? k_label_rows_short<T, kRowLoads, E, F, true>
+                                                          : k_label_rows_short<T, kRowLoads, E, F, false>,
+                                  row_grid(uint32_t(ceil_div(a.n, kShortRows))), dim3(16 * kShortRows), 0, stream, a);
+                });
+            }
             const int rc = by_waves(p.waves, [&](auto waves) {
                 return by_parts(a.entropy, a.field, [&](auto e, auto f) {
                     constexpr int W = decltype(waves)::value;
@@ -390,11 +404,12 @@ extern "C" int tm_label_logp_grad(const void *logits, int dtype, int64_t outer, 
     return by_type(dtype, [&](auto t) {
         using T = decltype(t);
         if (p.rows) {
-            // A wave to a row of up to eight loads a lane; else a workgroup to
-            // eight loads a thread, or to one where that leaves CUs idle.
+            // 16 lanes (65536 x 100: 10, a wave 25) or a wave to a row of up to
+            // eight loads a lane; else a workgroup to eight loads a thread, or
+            // to one where that leaves CUs idle.
             const uint64_t load = 16 / sizeof(T);
             if (s.n[1] <= 64 * 8 * load) {
-                a.lanes = 64;
+                a.lanes = p.brief ? 16 : 64;
                 a.share = uint32_t(s.n[1]);
             } else {
                 a.lanes = 256;
@@ -403,7 +418,7 @@ extern "C" int tm_label_logp_grad(const void *logits, int dtype, int64_t outer, 
             a.groups = uint32_t(ceil_div(s.n[1], a.share));
             a.div_groups = Div32::make(a.groups);
             if (s.positions * a.groups >= kLimit) return int(TM_ERR_TOO_LARGE);
-            const uint32_t blocks = a.lanes == 256 ? a.n * a.groups : (a.n + 3) / 4;
+            const uint32_t blocks = a.lanes == 256 ? a.n * a.groups : uint32_t(ceil_div(a.n, 256 / a.lanes));
             return by_parts(a.up_entropy, a.field, [&](auto e, auto f) {
                 constexpr bool E = decltype(e)::value, F = decltype(f)::value;
                 return launch(k_label_grad_rows<T, E, F>, row_grid(blocks), dim3(256), 0, stream, a);

@@ -424,3 +424,26 @@ def test_labels_of_two_classes_as_bool():
     only = training.label_log_probs(x, top_k=1, entropy=True)
     assert only.log_probs is None and only.field_mean is None
     assert torch.equal(only.top_indices[:, 0].long(), x.argmax(1))
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("classes", [65, 71, 100, 128, 130, 255, 256, 257, 500, 512, 513])
+def test_many_short_rows(classes, dtype):
+    import torch
+    x, y, phi, ups = case((4099, classes), dtype, seed=classes, field=True)
+    x[7] = -torch.inf
+    x[8, 1:] = -torch.inf
+    x[9] = torch.finfo(x.dtype).min
+    x[10] = 1.25
+    run(x, y, field=phi, top_k=20, ups=ups, what="short rows", dtype=dtype)
+    run(x, y, entropy=False, top_k=1, ups=[ups[0], None, None], what="short rows", dtype=dtype)
+    from paper_2608_24738_amd import training
+    clean = training.label_log_probs(x, y, top_k=3)
+    x[5, 3], x[6, classes - 1] = torch.nan, torch.inf
+    got = training.label_log_probs(x, y, top_k=3)
+    assert torch.isnan(got.log_probs[5:7]).all() or bool(((y[5:7] < 0)).any())
+    assert ((got.top_indices >= 0) & (got.top_indices < classes)).all()
+    keep = torch.ones(4099, dtype=torch.bool, device=x.device)
+    keep[5:7] = False
+    assert torch.equal(got.log_probs[keep], clean.log_probs[keep])
+    assert torch.equal(got.top_indices[keep], clean.top_indices[keep])

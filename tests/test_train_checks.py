@@ -177,3 +177,16 @@ def test_collapse():
     assert training._collapse((5, 1), (7, 3)) == (5, 7)
     assert training._collapse((3, 4), (0, 0)) == (12, 0)
     assert training._collapse((3, 4), (0, 1)) is None
+
+
+def test_constants_match_the_header():
+    import os
+    import re
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    with open(os.path.join(root, "include", "tm_train.h"), encoding="utf-8") as f:
+        text = f.read()
+    value = {name: int(number) for name, number in re.findall(r"(TM_[A-Z_]+) = (\d+)", text)}
+    assert training.MAX_TOP == value["TM_LABEL_MAX_TOP"]
+    assert training.MAX_RECOMPUTE == value["TM_LABEL_MAX_RECOMPUTE"]
+    assert training.MAX_BUCKETS == value["TM_BIAS_MAX_BUCKETS"]
+    assert training.BIAS_METRICS["offset"] == value["TM_METRIC_OFFSET"]

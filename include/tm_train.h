@@ -90,9 +90,10 @@ size_t tm_label_logp_workspace_size(int dtype, int64_t outer, int64_t classes, i
  *   a (1[c = y] - p_c) - h p_c (l_c + entropy) + f p_c (field_c - mean)
  *
  * with a = 0 where there is no label.  out_grad has the logits' type and its
- * own strides, in which no two elements may coincide.  stats, entropy and mean are what tm_label_logp gave (entropy
- * with up_entropy, mean with up_mean); with at most TM_LABEL_MAX_RECOMPUTE
- * classes they are computed anew from the logits and may be NULL.
+ * own strides, in which no two elements may coincide.  stats, entropy and mean
+ * are what tm_label_logp gave (entropy with up_entropy, mean with up_mean);
+ * with at most TM_LABEL_MAX_RECOMPUTE classes they are computed anew from the
+ * logits and may be NULL.
  * Errors: as tm_label_logp.
  */
 int tm_label_logp_grad(const void *logits, int dtype, int64_t outer, int64_t classes, int64_t inner,
@@ -114,7 +115,8 @@ int tm_label_logp_grad(const void *logits, int dtype, int64_t outer, int64_t cla
  * table_dtype and out_dtype: TM_DTYPE_F32, _F16 or _BF16.
  * Errors: TM_ERR_SHAPE (buckets outside [1, TM_BIAS_MAX_BUCKETS], heads < 1,
  * negative extents), TM_ERR_NULL, TM_ERR_NO_OUTPUT, TM_ERR_DTYPE,
- * TM_ERR_TOO_LARGE (2^31 positions or samples, more than 2^16 heads), TM_ERR_ALIAS, TM_ERR_HIP.
+ * TM_ERR_TOO_LARGE (2^31 positions or samples, more than 2^16 heads),
+ * TM_ERR_ALIAS, TM_ERR_HIP.
  */
 int tm_distance_bias(const void *distances, int distance_dtype, int64_t batch, int64_t positions, const void *table,
                      int table_dtype, int buckets, int64_t heads, const float *edges, const void *add, void *out,

@@ -187,11 +187,11 @@ __global__ void __launch_bounds__(kBiasThreads) k_bias(BiasArgs a) {
 // second.  They are loaded 256 bytes of a head to 16 lanes, the next step's
 // while one is added up, and change hands through LDS, since the operand wants
 // 8 positions of one head in a lane.  (Loaded as the operand lies, with
-// neighbouring lanes in different heads, every lane is an access of its own: 86 us
-// instead of 81 for 2 x 16 x 2048 x 2048, 53 instead of 40 for 32 x 4 x 512^2.)
-// Fewer than 9 heads leave loads over for more positions.  Sums are float32 in the accumulators, in an
-// order fixed by the sizes.  float32 gradients are cut into three bf16 pieces
-// of 8 bits, which lose nothing.
+// neighbouring lanes in different heads, every lane is an access of its own:
+// 86 us instead of 81 for 2 x 16 x 2048 x 2048, 53 instead of 40 for 32 x 4 x
+// 512^2.)  Fewer than 9 heads leave loads over for more positions.  Sums are
+// float32 in the accumulators, in an order fixed by the sizes.  float32
+// gradients are cut into three bf16 pieces of 8 bits, which lose nothing.
 //
 // With 16 heads bound by the gradients' bytes (bf16 2 x 16 x 2048 x 2048: 268 MB
 // in 81 us, 3.3 TB/s right after the forward pass has written as much; without

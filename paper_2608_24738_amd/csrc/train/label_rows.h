@@ -3,8 +3,9 @@
 //
 // W waves run through a row, 8 (or 4) classes to a lane and load, with a
 // running maximum per lane; the lanes' sums are joined at the end.  Short rows
-// among many are held by 16 lanes each (65536 x 512: 67 MB in 14 us, 4.9 TB/s).  A long row
-// among few is cut into `groups` parts, which k_label_rows_join puts together.
+// among many are held by 16 lanes each (65536 x 512: 67 MB in 14 us, 4.9 TB/s).
+// A long row among few is cut into `groups` parts, which k_label_rows_join puts
+// together.
 // Bound by the bytes of the logits; a row is read once (bf16 4096 x 32768 with
 // the entropy: 268 MB in 44 us, 6.1 TB/s, the gradient 537 MB in 81 us, 6.6 TB/s;
 // 512 x 50021 with 5 alternatives: 51 MB in 18.5 us, of them 6 the alternatives';
@@ -34,11 +35,11 @@ __device__ __forceinline__ Sums wave_join(Sums r) {
     return {r.m, wave_sum(r.s), wave_sum(r.t), wave_sum(r.f)};
 }
 
-// Results of row n (outer o, inner i) by one thread.
 // The workgroup's number in a grid of two dimensions: one of them holds fewer
 // than 2^32 threads.
 __device__ __forceinline__ uint32_t block_number() { return blockIdx.y * gridDim.x + blockIdx.x; }
 
+// Results of row n by one thread.
 template <typename T>
 __device__ __forceinline__ void put_row(const LabelArgs &a, uint32_t n, const T *x, const Found &q) {
     if (a.logp) {

@@ -447,3 +447,17 @@ def test_many_short_rows(classes, dtype):
     keep[5:7] = False
     assert torch.equal(got.log_probs[keep], clean.log_probs[keep])
     assert torch.equal(got.top_indices[keep], clean.top_indices[keep])
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("classes", [33, 36, 40, 47, 63, 64])
+def test_many_rows_of_one_load(classes, dtype):
+    """Fewer classes than 16 lanes load at once: the lanes past the end read the last classes again."""
+    import torch
+    x, y, phi, ups = case((4097, classes), dtype, seed=classes, field=True)
+    x[7] = -torch.inf
+    x[8, :-1] = -torch.inf
+    x[9] = torch.finfo(x.dtype).min
+    x[10] = -2.5
+    run(x, y, field=phi, top_k=32, ups=ups, what="rows of one load", dtype=dtype)
+    run(x, y, entropy=False, top_k=1, ups=[ups[0], None, None], what="rows of one load", dtype=dtype)

@@ -98,7 +98,9 @@ def main(argv=None):
         images, labels, marks = make_images(gen, args.batch, args.size)
         label_loss, boundary_loss, entropy = losses(network(images, marks), labels)
         optimizer.zero_grad(set_to_none=True)
-        (label_loss + 0.02 * boundary_loss).backward()
+        # with one GPU, handing a pass over to autograd's own thread and back takes longer than its launches
+        with torch.autograd.set_multithreading_enabled(False):
+            (label_loss + 0.02 * boundary_loss).backward()
         optimizer.step()
         history.append(float(label_loss.detach()))
         if not args.quiet and step % 10 == 0:

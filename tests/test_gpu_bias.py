@@ -355,3 +355,32 @@ def test_wrapper_refusals():
             (ValueError, lambda: training.distance_bias(good[0], table, edges, add=good[:, :4]))]:
         with pytest.raises(error):
             call()
+
+
+def test_on_the_callers_thread():
+    """Gradients are the same where autograd starts no thread of its own, on another stream too."""
+    import torch
+    from paper_2608_24738_amd import training
+    dev = "cuda:0"
+    gen = torch.Generator().manual_seed(9)
+    edges = training.distance_edges(20, 40.0, device=dev)
+    table = torch.randn((20, 5), generator=gen).to(dev).requires_grad_(True)
+    d = (torch.rand((2, 33, 41), generator=gen) * 50).to(dev)
+    logits = torch.randn((2, 5, 33, 41), generator=gen).to(dev).requires_grad_(True)
+    labels = torch.randint(0, 5, (2, 33, 41), generator=gen).to(dev)
+    announce("a backward pass on the caller's thread")
+
+    def step():
+        got = training.label_log_probs(training.distance_bias(d, table, edges, add=logits), labels, entropy=True)
+        return torch.autograd.grad(got.log_probs.sum() + 0.1 * got.entropy.sum(), [table, logits])
+
+    want = step()
+    torch.cuda.synchronize()
+    other = torch.cuda.Stream()
+    with torch.autograd.set_multithreading_enabled(False):
+        here = step()
+        with torch.cuda.stream(other):
+            there = step()
+    torch.cuda.synchronize()
+    for w, a, b in zip(want, here, there):
+        assert torch.equal(w, a) and torch.equal(w, b)

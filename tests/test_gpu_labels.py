@@ -461,3 +461,13 @@ def test_many_rows_of_one_load(classes, dtype):
     x[10] = -2.5
     run(x, y, field=phi, top_k=32, ups=ups, what="rows of one load", dtype=dtype)
     run(x, y, entropy=False, top_k=1, ups=[ups[0], None, None], what="rows of one load", dtype=dtype)
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("classes", [15, 16, 17, 23, 24, 25, 31, 32, 33])
+def test_maps_around_the_held_counts(classes, dtype):
+    """One class fewer and more than the kernels hold in registers; many positions to a thread, and one."""
+    for shape in ((2, classes, 1, 7), (2, classes, 371, 401)):
+        x, y, phi, ups = case(shape, dtype, seed=classes, label="uint8", field=True)
+        run(x, y, field=phi, top_k=4, ups=ups, what="maps", dtype=dtype)
+        run(x, y, entropy=False, ups=[ups[0], None, None], what="maps, log-probabilities alone", dtype=dtype)

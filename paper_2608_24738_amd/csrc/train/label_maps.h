@@ -139,6 +139,22 @@ __device__ __forceinline__ void forget_held(Pack<T, V> (&held)[C]) {
     }
 }
 
+// The maxima of held classes, two at a time.
+template <typename T, int V, int C>
+__device__ __forceinline__ void held_maxima(Sums (&r)[V], const Pack<T, V> (&held)[C], uint32_t classes) {
+#pragma unroll
+    for (int c = 0; c < C; c += 2) {
+        if (c + 1 < C && uint32_t(c + 1) < classes) {
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                r[j].m = max_of(r[j].m, widen(held[c].at(j)), widen(held[c + 1 < C ? c + 1 : c].at(j)));
+        } else if (uint32_t(c) < classes) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) r[j].m = max_of(r[j].m, r[j].m, widen(held[c].at(j)));
+        }
+    }
+}
+
 // Classes whose field is held too; others' is read again for the gradient.
 template <int C, int V, bool F>
 constexpr int kFieldHeld = F && C * V <= 32 ? C : 1;
@@ -196,12 +212,7 @@ __global__ void __launch_bounds__(256) k_label_held(LabelArgs a) {
         r[j] = kNothing;
         xl[j] = 0.0f;
     }
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-        if (uint32_t(c) < a.classes) {
-#pragma unroll
-            for (int j = 0; j < V; ++j) r[j].m = fmaxf(r[j].m, widen(held[c].at(j)));
-        }
+    held_maxima(r, held, a.classes);
     const float *const field = F ? a.field + w.o * a.fs[0] + w.i * a.fs[2] : nullptr;
     Pack<float, V> phi[kFieldHeld<C, V, F>] = {};
     held_sums<T, V, C, E, F>(r, held, a.classes, field, a.fs, phi);
@@ -416,11 +427,17 @@ __device__ __forceinline__ void load_upstream(const LabelGradArgs &a, const Plac
     }
 }
 
+// Where a thread's gradients begin.
+template <typename T, int V>
+__device__ __forceinline__ T *slopes(const LabelGradArgs &a, const Place<V> &w) {
+    return static_cast<T *>(a.grad) + w.o * a.gs[0] + w.i * a.gs[2];
+}
 // One class of V positions.
-template <typename T, int V, typename G>
-__device__ __forceinline__ void put_slope(const LabelGradArgs &a, const Place<V> &w, uint32_t c, const Pack<T, V> &x,
-                                          const Pack<float, V> &phi, const int32_t (&y)[V], const Slope (&g)[V]) {
-    T *out = static_cast<T *>(a.grad) + w.o * a.gs[0] + c * a.gs[1] + w.i * a.gs[2];
+template <typename G, typename T, int V>
+__device__ __forceinline__ void put_slope(const LabelGradArgs &a, T *out, const Place<V> &w, uint32_t c,
+                                          const Pack<T, V> &x, const Pack<float, V> &phi, const int32_t (&y)[V],
+                                          const Slope (&g)[V]) {
+    out += c * a.gs[1];
     float v[V];
 #pragma unroll
     for (int j = 0; j < V; ++j)
@@ -454,12 +471,7 @@ __global__ void __launch_bounds__(256) k_label_grad_held(LabelGradArgs a) {
     Slope g[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) r[j] = kNothing;
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-        if (uint32_t(c) < a.classes) {
-#pragma unroll
-            for (int j = 0; j < V; ++j) r[j].m = fmaxf(r[j].m, widen(held[c].at(j)));
-        }
+    held_maxima(r, held, a.classes);
     Pack<float, V> phi[kFieldHeld<C, V, F>] = {};
     held_sums<T, V, C, E, F>(r, held, a.classes, field, a.fs, phi);
 #pragma unroll
@@ -472,13 +484,14 @@ __global__ void __launch_bounds__(256) k_label_grad_held(LabelGradArgs a) {
     }
     int32_t y[V];
     load_upstream<V>(a, w, y, g);
+    T *const out = slopes<T>(a, w);
     by_near<T>(farthest(g), [&](auto near) __attribute__((always_inline)) {
 #pragma unroll
         for (int c = 0; c < C; ++c)
             if (uint32_t(c) < a.classes) {
                 constexpr bool kept = kFieldHeld<C, V, F> == C;
                 if constexpr (F && !kept) phi[0] = load_field<V>(field + c * a.fs[1], a.fs[2], V);
-                put_slope<T, V, Grad<decltype(near)::value, E, F>>(a, w, c, held[c], phi[F && kept ? c : 0], y, g);
+                put_slope<Grad<decltype(near)::value, E, F>>(a, out, w, c, held[c], phi[F && kept ? c : 0], y, g);
             }
     });
 }
@@ -506,6 +519,7 @@ __global__ void __launch_bounds__(256) k_label_grad_run(LabelGradArgs a) {
     }
     int32_t y[V];
     load_upstream<V>(a, w, y, g);
+    T *const out = slopes<T>(a, w);
     by_near<T>(farthest(g), [&](auto near) __attribute__((always_inline)) {
         for (uint32_t c = c0; c < c1; c += 4) {
             Pack<T, V> held[4];
@@ -521,7 +535,7 @@ __global__ void __launch_bounds__(256) k_label_grad_run(LabelGradArgs a) {
 #pragma unroll
             for (int u = 0; u < 4; ++u)
                 if (c + u < c1)
-                    put_slope<T, V, Grad<decltype(near)::value, E, F>>(a, w, c + u, held[u], phi[F ? u : 0], y, g);
+                    put_slope<Grad<decltype(near)::value, E, F>>(a, out, w, c + u, held[u], phi[F ? u : 0], y, g);
         }
     });
 }

@@ -183,6 +183,14 @@ __device__ __forceinline__ Pack<T, V> narrow_pack(const float (&v)[V]) {
     return r;
 }
 
+// The largest of three by one instruction; fmaxf makes each operand quiet by
+// another first.  A signalling NaN comes out as NaN, quiet ones are passed over.
+__device__ __forceinline__ float max_of(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+
 // 2^x by the hardware's v_exp_f32 (results below 2^-126 flush to 0).
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 

@@ -282,7 +282,10 @@ extern "C" int tm_label_logp(const void *logits, int dtype, int64_t outer, int64
     a.k = uint32_t(top_k);
     a.label_bytes = int32_t(s.label_bytes);
     a.n = uint32_t(s.positions);
-    const LabelPlan p = label_plan(dtype, s.n[0], s.n[1], s.n[2], strides);
+    LabelPlan p = label_plan(dtype, s.n[0], s.n[1], s.n[2], strides);
+    // Many alternatives of rows of two loads a lane and more: a wave to a row, whose lanes' bests cost less than a pass
+    // each (65536 x 500, 5, 8, 32: 86, 104, 272 us, by 16 lanes 92, 149, 676; x 100: 81, 103, 265 and 30, 48, 197).
+    if (top_k >= 8 && s.n[1] >= 32 * (16 / float_bytes(dtype))) p.brief = false;
     a.ts[0] = top_k * inner;
     a.ts[1] = inner;
     a.ts[2] = 1;

@@ -471,3 +471,12 @@ def test_maps_around_the_held_counts(classes, dtype):
         x, y, phi, ups = case(shape, dtype, seed=classes, label="uint8", field=True)
         run(x, y, field=phi, top_k=4, ups=ups, what="maps", dtype=dtype)
         run(x, y, entropy=False, ups=[ups[0], None, None], what="maps, log-probabilities alone", dtype=dtype)
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("k", [7, 8, 32])
+@pytest.mark.parametrize("classes", [127, 128, 255, 256, 511])
+def test_alternatives_of_short_rows(classes, k, dtype):
+    x, y, phi, ups = case((4096, classes), dtype, seed=classes + k, field=True)
+    x[3] = 0.5
+    run(x, y, field=phi, top_k=k, ups=ups, what="alternatives of short rows", dtype=dtype)

@@ -103,8 +103,8 @@ def _label_plan(shape, strides, dim, dtype, top_k):
 
 
 def _label_forward(logits, labels, field, dim, entropy, top_k, stats):
-    """Runs tm_label_logp; returns (logits, field) as they were read, what describes
-    them to the library, the outputs and the statistics for the gradient."""
+    """Runs tm_label_logp; returns (logits, field) as they were read, the outputs
+    and the statistics for the gradient."""
     dev, dtype = logits.device, FLOATS[logits.dtype]
     plan = _label_plan(tuple(logits.shape), logits.stride(), dim, dtype, top_k)
     if plan is None:
@@ -126,13 +126,30 @@ def _label_forward(logits, labels, field, dim, entropy, top_k, stats):
     _call("tm_label_logp", dev, None, logits.data_ptr(), dtype, *extents, strides, _ptr(labels), label_dtype,
           _ptr(field), field_strides, top_k, _ptr(logp), _ptr(ent), _ptr(mean), _ptr(top), _ptr(index), _ptr(kept),
           _ptr(workspace), nbytes)
-    return logits, field, (dtype, *extents, strides), (label_dtype, field_strides), (logp, ent, mean, top, index), kept
+    return logits, field, (logp, ent, mean, top, index), kept
 
 
 def _upstream(grad):
     if grad is None or (grad.dtype == torch.float32 and grad.is_contiguous()):
         return grad
     return grad.to(torch.float32).contiguous()
+
+
+def _kind(t):
+    return None if t is None else (t.dtype, t.device, t.shape)
+
+
+def _restored(tensors, kinds):
+    """Checks tensors that autograd kept.  Hooks on saved tensors (such as
+    torch.autograd.graph.save_on_cpu) may give them another layout, nothing else."""
+    for t, kind in zip(tensors, kinds):
+        if _kind(t) != kind:
+            raise RuntimeError("a hook on saved tensors gave back %s for %s" % (_kind(t), kind))
+    return tensors
+
+
+def _dense(t):
+    return None if t is None else t.contiguous()
 
 
 def _once():
@@ -144,26 +161,34 @@ class _LabelLogProbs(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, labels, field, dim, entropy, top_k):
         stats = logits.shape[dim] > MAX_RECOMPUTE
-        logits, field, ctx.view, ctx.others, out, kept = _label_forward(logits, labels, field, dim, entropy, top_k, stats)
+        logits, field, out, kept = _label_forward(logits, labels, field, dim, entropy, top_k, stats)
         ctx.dim = dim
         ctx.set_materialize_grads(False)
         if top_k:
             ctx.mark_non_differentiable(out[3], out[4])
-        ctx.save_for_backward(logits, labels, field, kept, out[1] if stats else None, out[2] if stats else None)
+        saved = (logits, labels, field, kept, out[1] if stats else None, out[2] if stats else None)
+        ctx.kinds = [_kind(t) for t in saved]
+        ctx.save_for_backward(*saved)
         return out
 
     @staticmethod
     def backward(ctx, up_logp, up_entropy, up_mean, _top, _index):
         _once()
-        logits, labels, field, kept, entropy, mean = ctx.saved_tensors
         if up_logp is None and up_entropy is None and up_mean is None:
             return None, None, None, None, None, None
+        logits, labels, field, kept, entropy, mean = _restored(ctx.saved_tensors, ctx.kinds)
+        # strides are those of the tensors at hand, not the forward call's
+        logits, extents, strides = _viewed(logits, ctx.dim)
+        field_strides = None
+        if field is not None:
+            field, _, field_strides = _viewed(field, ctx.dim)
+        labels, kept, entropy, mean = _dense(labels), _dense(kept), _dense(entropy), _dense(mean)
         up_logp, up_entropy, up_mean = _upstream(up_logp), _upstream(up_entropy), _upstream(up_mean)
         grad, _, grad_strides = _viewed(torch.empty_like(logits), ctx.dim)
-        label_dtype, field_strides = ctx.others
-        _call("tm_label_logp_grad", logits.device, None, logits.data_ptr(), *ctx.view, _ptr(labels), label_dtype,
-              _ptr(field), field_strides, _ptr(kept), _ptr(entropy), _ptr(mean), _ptr(up_logp), _ptr(up_entropy),
-              _ptr(up_mean), grad.data_ptr(), grad_strides)
+        label_dtype = LABELS[labels.dtype] if labels is not None else 0
+        _call("tm_label_logp_grad", logits.device, None, logits.data_ptr(), FLOATS[logits.dtype], *extents, strides,
+              _ptr(labels), label_dtype, _ptr(field), field_strides, _ptr(kept), _ptr(entropy), _ptr(mean),
+              _ptr(up_logp), _ptr(up_entropy), _ptr(up_mean), grad.data_ptr(), grad_strides)
         return grad, None, None, None, None, None
 
 
@@ -223,7 +248,7 @@ def label_log_probs(logits: torch.Tensor, labels: Optional[torch.Tensor] = None,
     entropy, top_k = bool(entropy), int(top_k)
     if logits.requires_grad and torch.is_grad_enabled():
         return LabelLogProbs(*_LabelLogProbs.apply(logits, labels, field, dim, entropy, top_k))
-    return LabelLogProbs(*_label_forward(logits, labels, field, dim, entropy, top_k, False)[4])
+    return LabelLogProbs(*_label_forward(logits, labels, field, dim, entropy, top_k, False)[2])
 
 
 def distance_edges(buckets: int, reach: float, *, signed: bool = False, device=None) -> torch.Tensor:
@@ -257,19 +282,20 @@ class _Bias(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, table, edges, add, source, shape):
-        ctx.source = source
+        ctx.name, ctx.args, distances = source
         ctx.table_dtype, ctx.table_shape = table.dtype, tuple(table.shape)
         ctx.has_add = add is not None
-        ctx.save_for_backward(edges, source[2])
+        ctx.kinds = (_kind(edges), _kind(distances))
+        ctx.save_for_backward(edges, distances)
         return _bias_forward(table, edges, add, source, shape)
 
     @staticmethod
     def backward(ctx, up):
         _once()
-        edges, distances = ctx.saved_tensors
-        name, args, _ = ctx.source
         grad = None
         if ctx.needs_input_grad[0]:
+            edges, distances = _restored(ctx.saved_tensors, ctx.kinds)
+            edges, distances, args = edges.contiguous(), _dense(distances), ctx.args
             up = up.contiguous()
             buckets, heads = ctx.table_shape
             dev = edges.device
@@ -278,7 +304,7 @@ class _Bias(torch.autograd.Function):
             workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
             if distances is not None:
                 args = (distances.data_ptr(),) + args[1:]
-            _call(name + "_grad", dev, None, *args, up.data_ptr(), FLOATS[up.dtype], buckets, heads, edges.data_ptr(),
+            _call(ctx.name + "_grad", dev, None, *args, up.data_ptr(), FLOATS[up.dtype], buckets, heads, edges.data_ptr(),
                   grad.data_ptr(), FLOATS[ctx.table_dtype], _ptr(workspace), nbytes)
         return grad, None, up if ctx.has_add and ctx.needs_input_grad[2] else None, None, None
 

@@ -210,45 +210,44 @@ struct Slope {
     float m, logs, a, h, f, entropy, mean;
 };
 
-// A position's slope, prepared: p = 2^z with z = x log2(e) - c, and the factor
-// of p is base + per l (+ f field).  p is made 2^32 times as large and the
-// factor as much smaller, so that gradients among float32's smallest numbers
-// come out too, where v_exp_f32 alone gives 0.  Near as in Ref; a 16-bit
-// gradient hides that p is off by a factor as close to 1.
-constexpr float kUp = 32.0f, kDown = 1.0f / 4294967296.0f;
+// A position's slope, prepared: the factor of p is base + per l (+ f field).
+// p is the square of q = 2^z with z = (x - m - log s) log2(e) / 2, and its
+// factor stands between the two: v_exp_f32 gives 0 below 2^-126, which for q
+// is p = 2^-252, so that gradients among float32's smallest numbers come out
+// whether p or the upstream gradient is small.  (A z made larger by a constant
+// instead would be rounded as coarsely as the constant is large.)  Near as in
+// Ref; a 16-bit gradient hides that p is off by a factor as close to 1.
+constexpr float kHalfLog2e = 0.5f * kLog2e;
+constexpr float kGone = 1.0f / 604462909807314587353088.0f;   // q of p = 2^-158: the field is not looked at
 
 template <bool Near, bool Entropy, bool Mean>
 struct Grad {
-    float base, per, f;         // per: of l, or of z + 32
+    float base, per, f;         // per: of l, or of z
     float m, logs, c;
 
     __device__ __forceinline__ explicit Grad(const Slope &g)
-        : base(-g.a * kDown), per(-g.h * kDown), f(g.f * kDown), m(g.m), logs(g.logs),
-          c(fmaf(g.m + g.logs, kLog2e, -kUp)) {
+        : base(-g.a), per(-g.h), f(g.f), m(g.m), logs(g.logs), c((g.m + g.logs) * kHalfLog2e) {
         if constexpr (Entropy) base = fmaf(per, g.entropy, base);
         if constexpr (Mean) base = fmaf(-f, g.mean, base);
-        if constexpr (Near) {
-            per *= kLn2;
-            if constexpr (Entropy) base = fmaf(per, -kUp, base);
-        }
+        if constexpr (Near) per *= 2.0f * kLn2;
     }
     // extra: a for the label's class, else 0
     __device__ __forceinline__ float at(float x, float field, float extra) const {
-        float p, l;
+        float q, l;
         if constexpr (Near) {
-            l = fmaf(x, kLog2e, -c);                       // z + 32
-            p = exp2_hw(l);
-            l = fmaxf(l, -300.0f);                         // 0 times a finite number; NaN comes from p
+            l = fmaf(x, kHalfLog2e, -c);                   // z
+            q = exp2_hw(l);
+            l = fmaxf(l, -150.0f);                         // 0 times a finite number; NaN comes from q
         } else {
-            l = below(x - m, logs);                        // a dead position has log s = inf and so p = 0
-            const float z = fmaf(l, kLog2e, kUp);
-            p = exp2_hw(z);
-            p = fmaf(p, fmaf(l, kLog2e, kUp - z) * kLn2, p);     // as exp_of
+            l = below(x - m, logs);                        // a dead position has log s = inf and so q = 0
+            const float z = l * kHalfLog2e;
+            q = exp2_hw(z);
+            q = fmaf(q, fmaf(l, kHalfLog2e, -z) * kLn2, q);      // as exp_of
         }
         float v = base;
         if constexpr (Entropy) v = fmaf(per, l, v);
-        if constexpr (Mean) v = fmaf(f, p == 0.0f ? 0.0f : field, v);
-        return fmaf(p, v, extra);
+        if constexpr (Mean) v = fmaf(f, q < kGone ? 0.0f : field, v);
+        return fmaf(q * v, q, extra);
     }
 };
 

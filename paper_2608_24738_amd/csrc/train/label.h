@@ -216,7 +216,11 @@ struct Slope {
 // is p = 2^-252, so that gradients among float32's smallest numbers come out
 // whether p or the upstream gradient is small.  (A z made larger by a constant
 // instead would be rounded as coarsely as the constant is large.)  Near as in
-// Ref; a 16-bit gradient hides that p is off by a factor as close to 1.
+// Ref: c = (m + log s) log2(e) / 2 is rounded twice, which is a factor common to
+// every p and a term common to every l.  Where p is close to 1 or l to minus
+// the entropy, the gradient is what is left of a difference and shows them, so
+// both are taken out, once for all classes; what stays is of second order,
+// below 4e-9.
 constexpr float kHalfLog2e = 0.5f * kLog2e;
 constexpr float kGone = 1.0f / 604462909807314587353088.0f;   // q of p = 2^-158: the field is not looked at
 
@@ -229,7 +233,18 @@ struct Grad {
         : base(-g.a), per(-g.h), f(g.f), m(g.m), logs(g.logs), c((g.m + g.logs) * kHalfLog2e) {
         if constexpr (Entropy) base = fmaf(per, g.entropy, base);
         if constexpr (Mean) base = fmaf(-f, g.mean, base);
-        if constexpr (Near) per *= 2.0f * kLn2;
+        if constexpr (Near) {
+            // m + log s - sum, exactly, and (m + log s) log2(e) / 2 - c
+            const float sum = m + logs, part = sum - m;
+            const float rest = (m - (sum - part)) + (logs - part);
+            const float off = fmaf(rest, kHalfLog2e, fmaf(sum, kHalfLog2e, -c));
+            const float scale = 1.0f - 2.0f * kLn2 * off;
+            per *= 2.0f * kLn2;
+            if constexpr (Entropy) base = fmaf(per, -off, base);
+            base *= scale;
+            if constexpr (Entropy) per *= scale;
+            if constexpr (Mean) f *= scale;
+        }
     }
     // extra: a for the label's class, else 0
     __device__ __forceinline__ float at(float x, float field, float extra) const {

@@ -17,6 +17,8 @@
 // gradient 267 MB in 51 us).
 #pragma once
 
+#include <utility>
+
 #include "label.h"
 
 namespace tmtrain {
@@ -432,16 +434,26 @@ template <typename T, int V>
 __device__ __forceinline__ T *slopes(const LabelGradArgs &a, const Place<V> &w) {
     return static_cast<T *>(a.grad) + w.o * a.gs[0] + w.i * a.gs[2];
 }
+// The positions' slopes, prepared before the classes: each of these is behind a
+// branch on their number, where nothing is shared with the one before.
+template <typename G, int V>
+struct Grads {
+    G at[V];
+    template <size_t... J>
+    __device__ __forceinline__ Grads(const Slope (&g)[V], std::index_sequence<J...>) : at{G(g[J])...} {}
+    __device__ __forceinline__ explicit Grads(const Slope (&g)[V]) : Grads(g, std::make_index_sequence<V>()) {}
+};
+
 // One class of V positions.
 template <typename G, typename T, int V>
 __device__ __forceinline__ void put_slope(const LabelGradArgs &a, T *out, const Place<V> &w, uint32_t c,
                                           const Pack<T, V> &x, const Pack<float, V> &phi, const int32_t (&y)[V],
-                                          const Slope (&g)[V]) {
+                                          const Slope (&g)[V], const Grads<G, V> &grads) {
     out += c * a.gs[1];
     float v[V];
 #pragma unroll
     for (int j = 0; j < V; ++j)
-        v[j] = G(g[j]).at(widen(x.at(j)), phi.at(j), y[j] == int32_t(c) ? g[j].a : 0.0f);
+        v[j] = grads.at[j].at(widen(x.at(j)), phi.at(j), y[j] == int32_t(c) ? g[j].a : 0.0f);
     const Pack<T, V> r = narrow_pack<T, V>(v);
     if (V == 1 || a.gs[2] == 1) {
         store_own<V>(out, r, w.skip);
@@ -486,12 +498,13 @@ __global__ void __launch_bounds__(256) k_label_grad_held(LabelGradArgs a) {
     load_upstream<V>(a, w, y, g);
     T *const out = slopes<T>(a, w);
     by_near<T>(farthest(g), [&](auto near) __attribute__((always_inline)) {
+        const Grads<Grad<decltype(near)::value, E, F>, V> grads(g);
 #pragma unroll
         for (int c = 0; c < C; ++c)
             if (uint32_t(c) < a.classes) {
                 constexpr bool kept = kFieldHeld<C, V, F> == C;
                 if constexpr (F && !kept) phi[0] = load_field<V>(field + c * a.fs[1], a.fs[2], V);
-                put_slope<Grad<decltype(near)::value, E, F>>(a, out, w, c, held[c], phi[F && kept ? c : 0], y, g);
+                put_slope(a, out, w, c, held[c], phi[F && kept ? c : 0], y, g, grads);
             }
     });
 }
@@ -521,6 +534,7 @@ __global__ void __launch_bounds__(256) k_label_grad_run(LabelGradArgs a) {
     load_upstream<V>(a, w, y, g);
     T *const out = slopes<T>(a, w);
     by_near<T>(farthest(g), [&](auto near) __attribute__((always_inline)) {
+        const Grads<Grad<decltype(near)::value, E, F>, V> grads(g);
         for (uint32_t c = c0; c < c1; c += 4) {
             Pack<T, V> held[4];
             Pack<float, V> phi[F ? 4 : 1] = {};
@@ -535,7 +549,7 @@ __global__ void __launch_bounds__(256) k_label_grad_run(LabelGradArgs a) {
 #pragma unroll
             for (int u = 0; u < 4; ++u)
                 if (c + u < c1)
-                    put_slope<Grad<decltype(near)::value, E, F>>(a, out, w, c + u, held[u], phi[F ? u : 0], y, g);
+                    put_slope(a, out, w, c + u, held[u], phi[F ? u : 0], y, g, grads);
         }
     });
 }

@@ -46,9 +46,9 @@ struct BiasGradArgs {
     uint32_t heads, batch, field_batch;
     int32_t table_type;
     uint32_t splits, tile_rows;
-    uint32_t units;                        // shares of the batch x steps of positions
-    uint32_t batch_share;                  // samples of a share: those of a unit have the same buckets
-    Div32 div_steps;
+    uint32_t units;                        // shares of the batch x steps of positions, or groups of samples
+    uint32_t batch_share;                  // samples of a share: those of a unit have the same buckets; or of a group
+    Div32 div_steps;                       // steps of a sample; or positions of one
 };
 
 // The float32 distance of position p of sample b.  Every operation rounds by
@@ -201,9 +201,11 @@ __global__ void __launch_bounds__(kBiasThreads) k_bias(BiasArgs a) {
 //
 // Each workgroup leaves its sums in the workspace; k_bias_join adds them up.
 // Zero times an infinity or NaN spreads it over the buckets of its tile, so a
-// sum that is not finite is made once more there, from its own bucket alone;
-// so are all sums over fewer positions than a load holds (splits = 0).
+// sum that is not finite is made once more there, from its own bucket alone.
 // Columns of heads that are not there hold anything and are not used.
+//
+// Samples of fewer positions than a load holds (Few) go into a step one behind
+// the other, as many as fit, and are loaded element by element.
 // ---------------------------------------------------------------------------
 constexpr int kGradThreads = 512;
 constexpr int kGradWaves = kGradThreads / kWave;
@@ -246,12 +248,15 @@ __device__ __forceinline__ f32x4 product(f16, u32x4 a, u32x4 b, f32x4 c) {
                                                   0);
 }
 
-// One step of positions, for the samples of one share of the batch.
+// One step of positions, for the samples of one share of the batch; Few: a
+// group of samples from b0 on, as one.
 struct Unit {
     uint32_t field, first;                 // sample of the distances, first position
     uint32_t b0, b1;
 };
+template <bool Few>
 __device__ __forceinline__ Unit unit_at(const BiasGradArgs &a, uint32_t unit, uint32_t step) {
+    if constexpr (Few) return {0, 0, unit * a.batch_share, unit * a.batch_share + 1};
     Unit u;
     const uint32_t share = a.div_steps.div(unit);
     u.field = a.field_batch > 1 ? share : 0;
@@ -261,8 +266,8 @@ __device__ __forceinline__ Unit unit_at(const BiasGradArgs &a, uint32_t unit, ui
     return u;
 }
 
-// Tiles: buckets / 16, rounded up to a power of two.  Blocks of four heads: 1, 2 or 4.
-template <typename T, int Tiles, int Blocks>
+// Tiles: buckets / 16, rounded up to a power of two.  Blocks of four heads: 1, 2 or 4 (Few: 4).
+template <typename T, int Tiles, int Blocks, bool Few>
 __global__ void __launch_bounds__(kGradThreads) k_bias_grad(BiasGradArgs a) {
     constexpr uint32_t L = kGradLoad<T>, Step = kGradStep<T, Blocks>;
     constexpr int V = 16 / sizeof(T);
@@ -285,6 +290,27 @@ __global__ void __launch_bounds__(kGradThreads) k_bias_grad(BiasGradArgs a) {
     // last V positions, whose doubles no bucket takes.
     const uint32_t last = a.src.positions - V;
     const auto fetch = [&](Pack<T, V> (&x)[4], const Unit &u, uint32_t b) __attribute__((always_inline)) {
+        if constexpr (Few) {
+            static_assert(Blocks == 4);
+            // below 2^26 elements from the group's first
+            const uint32_t b0 = __builtin_amdgcn_readfirstlane(u.b0), have = min(a.batch_share, a.batch - b0);
+            const T *const g = static_cast<const T *>(a.grad) + uint64_t(b0) * a.heads * a.src.positions;
+            uint32_t at_j[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const uint32_t s = a.div_steps.div(col * V + j), p = col * V + j - s * a.src.positions;
+                at_j[j] = min(s, have - 1) * a.heads * a.src.positions + p;
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t at_i = min(h0 + 4 * i + group, a.heads - 1) * a.src.positions;
+                Pack<T, V> r{};
+#pragma unroll
+                for (int j = 0; j < V; ++j) r.put(j, g[at_j[j] + at_i]);
+                x[i] = r;
+            }
+            return;
+        }
         const T *g = static_cast<const T *>(a.grad) + uint64_t(b) * a.heads * a.src.positions;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -296,7 +322,7 @@ __global__ void __launch_bounds__(kGradThreads) k_bias_grad(BiasGradArgs a) {
     Unit u{};
     Pack<T, V> x[4];
     if (at < a.units) {
-        u = unit_at(a, uint32_t(at), Step);
+        u = unit_at<Few>(a, uint32_t(at), Step);
         fetch(x, u, u.b0);
     }
     while (at < a.units) {
@@ -304,15 +330,23 @@ __global__ void __launch_bounds__(kGradThreads) k_bias_grad(BiasGradArgs a) {
 #pragma unroll
         for (uint32_t s = 0; s < Step / 64; ++s) {
             const uint32_t i = s * 64 + lane;
-            const uint32_t piece = u.first + i / V * V, p = min(piece, last) + i % V;
-            uint32_t k = bucket_of(edges, a.src.span, distance_at(a.src, u.field, p));
-            if (p < piece) k = 0xffffu;
+            uint32_t k;
+            if constexpr (Few) {
+                const uint32_t sample = a.div_steps.div(i), b = min(u.b0 + sample, a.batch - 1);
+                k = bucket_of(edges, a.src.span,
+                              distance_at(a.src, a.field_batch > 1 ? b : 0, i - sample * a.src.positions));
+                if (sample >= a.batch_share || u.b0 + sample >= a.batch) k = 0xffffu;
+            } else {
+                const uint32_t piece = u.first + i / V * V, p = min(piece, last) + i % V;
+                k = bucket_of(edges, a.src.span, distance_at(a.src, u.field, p));
+                if (p < piece) k = 0xffffu;
+            }
             ids[wave][i] = uint16_t(k);
 #pragma unroll
             for (int t = 0; t < Tiles; ++t) present[s] |= uint32_t(__any(k >> 4 == uint32_t(t))) << t;
         }
         at += uint64_t(gridDim.x) * kGradWaves;
-        const Unit v = at < a.units ? unit_at(a, uint32_t(at), Step) : Unit{};
+        const Unit v = at < a.units ? unit_at<Few>(a, uint32_t(at), Step) : Unit{};
         for (uint32_t b = u.b0; b < u.b1; ++b) {
             // runs of 256 bytes change hands one after the other
 #pragma unroll
@@ -416,7 +450,7 @@ __global__ void __launch_bounds__(256) k_bias_join(BiasGradArgs a) {
     }
     sum = part[col];
     if (slice == 0 && h0 + col < a.heads) table_put(a.out, a.table_type, uint64_t(k) * a.heads + h0 + col, sum);
-    const uint64_t odd = __ballot(h0 + col < a.heads && (!__builtin_isfinite(sum) || a.splits == 0)) & 0xffff;
+    const uint64_t odd = __ballot(h0 + col < a.heads && !__builtin_isfinite(sum)) & 0xffff;
     if (!odd) return;                                      // the same in every wave
     stage_edges(edges, a.src, 256);
     for (uint32_t i = 0; i < 16; ++i) {

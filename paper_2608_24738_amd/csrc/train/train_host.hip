@@ -622,9 +622,11 @@ int run_bias_grad(const BiasShape &s, const void *grad, int grad_dtype, int64_t 
     // Units of one step of positions and, where samples share the buckets, as many of
     // them as leave enough units; two workgroups of eight waves to a CU.
     const uint64_t groups = ceil_div(uint64_t(heads), 16);
+    // Samples smaller than a load share steps, as many whole ones as fit.
+    const bool few = s.src.positions && s.src.positions < 16 / float_bytes(grad_dtype);
     // Blocks of four heads to a load: up to 4 heads 16 us, two blocks for up to
     // 8 heads 19 us (8 x 512^2 bf16, 24 buckets); with four blocks 18 and 19.5.
-    const int blocks = heads <= 4 ? 1 : heads <= 8 ? 2 : 4;
+    const int blocks = few ? 4 : heads <= 4 ? 1 : heads <= 8 ? 2 : 4;
     const uint64_t step = 256 / float_bytes(grad_dtype) * (4 / blocks);
     const uint64_t steps = ceil_div(s.src.positions, step);
     uint64_t shares = s.batch;
@@ -633,23 +635,30 @@ int run_bias_grad(const BiasShape &s, const void *grad, int grad_dtype, int64_t 
         a.batch_share = uint32_t(std::min(s.batch, std::max<uint64_t>(1, s.batch * steps / 4096)));
         shares = ceil_div(s.batch, a.batch_share);
     }
-    const uint64_t units = steps * shares;
+    if (few) {
+        a.batch_share = uint32_t(step / s.src.positions);
+        shares = ceil_div(s.batch, a.batch_share);
+    }
+    const uint64_t units = steps * shares;                  // few: one step to a group
     if (units >= kLimit) return TM_ERR_TOO_LARGE;
     a.units = uint32_t(units);
-    a.div_steps = Div32::make(uint32_t(std::max<uint64_t>(1, steps)));
-    const bool few = s.src.positions < 16 / float_bytes(grad_dtype);
-    a.splits = few ? 0 : uint32_t(std::max<uint64_t>(1, std::min(ceil_div(units, kGradWaves), grad_splits_most(groups))));
+    a.div_steps = Div32::make(few ? s.src.positions : uint32_t(std::max<uint64_t>(1, steps)));
+    a.splits = uint32_t(std::max<uint64_t>(1, std::min(ceil_div(units, kGradWaves), grad_splits_most(groups))));
     a.tile_rows = uint32_t(grad_tile_rows(s.src.buckets));
-    const int rc = few ? int(TM_OK) : by_type(grad_dtype, [&](auto t) {
+    const int rc = by_type(grad_dtype, [&](auto t) {
         using T = decltype(t);
-        return by_blocks(blocks, [&](auto n) {
+        const auto run = [&](auto n, auto f) {
             constexpr int B = decltype(n)::value;
-            void (*const kernels[])(BiasGradArgs) = {k_bias_grad<T, 1, B>, k_bias_grad<T, 2, B>, k_bias_grad<T, 4, B>,
-                                                     k_bias_grad<T, 8, B>, k_bias_grad<T, 16, B>};
+            constexpr bool Few = decltype(f)::value;
+            void (*const kernels[])(BiasGradArgs) = {k_bias_grad<T, 1, B, Few>, k_bias_grad<T, 2, B, Few>,
+                                                     k_bias_grad<T, 4, B, Few>, k_bias_grad<T, 8, B, Few>,
+                                                     k_bias_grad<T, 16, B, Few>};
             int tiles = 0;
             while ((16u << tiles) < a.tile_rows) ++tiles;
             return launch(kernels[tiles], dim3(a.splits, uint32_t(groups)), dim3(kGradThreads), 0, stream, a);
-        });
+        };
+        if (few) return run(Int<4>{}, Bool<true>{});
+        return by_blocks(blocks, [&](auto n) { return run(n, Bool<false>{}); });
     });
     if (rc != TM_OK) return rc;
     return by_type(grad_dtype, [&](auto t) {

@@ -200,9 +200,13 @@ __global__ void __launch_bounds__(kBiasThreads) k_bias(BiasArgs a) {
 // 101 MB in 40 us; float32 4 x 3 x 990 x 990: 47 MB in 26 us).
 //
 // Each workgroup leaves its sums in the workspace; k_bias_join adds them up.
-// Zero times an infinity or NaN spreads it over the buckets of its tile, so a
-// sum that is not finite is made once more there, from its own bucket alone.
 // Columns of heads that are not there hold anything and are not used.
+//
+// Zero times an infinity or NaN spreads it over the buckets of its tile.  A
+// workgroup that finds a sum which is not finite goes over its positions once
+// more (`clean`): what is not finite is noted by bucket and head and counts as
+// zero.  bf16 and float32 gradients are taken a quarter as large, so that twice
+// the largest one is in range.  Sums that were finite stay as they were.
 //
 // Samples of fewer positions than a load holds (Few) go into a step one behind
 // the other, as many as fit, and are loaded element by element.
@@ -218,6 +222,21 @@ template <typename T>
 constexpr uint32_t kGradLoad = 256 / sizeof(T);
 template <typename T, int Blocks>
 constexpr uint32_t kGradStep = kGradLoad<T> * (4 / Blocks);
+
+// A gradient of the second pass: 0 where it is not finite, with what it is left in `what`.
+enum { kPlusInf = 1, kMinusInf = 2, kNaN = 4 };
+template <typename T>
+__device__ __forceinline__ T cleaned(T g, uint32_t &what) {
+    const float x = widen(g);
+    what = x != x ? kNaN : x == INFINITY ? kPlusInf : x == -INFINITY ? kMinusInf : 0;
+    if (what) return T{};
+    if constexpr (__is_same(T, f16)) return g;
+    else return narrow<T>(0.25f * x);
+}
+__device__ __forceinline__ float noted(uint32_t what, float sum) {
+    if (what & kNaN || (what & (kPlusInf | kMinusInf)) == (kPlusInf | kMinusInf)) return __uint_as_float(0x7fc00000u);
+    return what == kPlusInf ? INFINITY : what == kMinusInf ? -INFINITY : sum;
+}
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
@@ -267,8 +286,11 @@ __device__ __forceinline__ Unit unit_at(const BiasGradArgs &a, uint32_t unit, ui
 }
 
 // Tiles: buckets / 16, rounded up to a power of two.  Blocks of four heads: 1, 2 or 4 (Few: 4).
+// Two workgroups to a CU, four waves to a SIMD, as far as the sums leave registers for it.
 template <typename T, int Tiles, int Blocks, bool Few>
-__global__ void __launch_bounds__(kGradThreads) k_bias_grad(BiasGradArgs a) {
+__global__ void __launch_bounds__(kGradThreads,
+                                  !Few && (Tiles <= 4 || (Tiles == 8 && Blocks == 2 && sizeof(T) == 2)) ? 4 : 1)
+    k_bias_grad(BiasGradArgs a) {
     constexpr uint32_t L = kGradLoad<T>, Step = kGradStep<T, Blocks>;
     constexpr int V = 16 / sizeof(T);
     __shared__ float edges[kMaxBuckets];
@@ -276,12 +298,13 @@ __global__ void __launch_bounds__(kGradThreads) k_bias_grad(BiasGradArgs a) {
     constexpr int Row = kGradRow<T>, Rows = 4 * Blocks * Row;
     // the rows of every wave, and after them the sums
     __shared__ __align__(16) char shared[kGradWaves * Rows > Tiles * 1024 ? kGradWaves * Rows : Tiles * 1024];
+    __shared__ uint32_t odd[Tiles * 64];                   // [bucket][head], a byte each: what is not finite
+    __shared__ uint32_t finite[kGradWaves];                // are a wave's sums?
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const uint32_t col = lane & 15, group = lane >> 4;     // operand: row or column, block of 8 positions
     const uint32_t h0 = blockIdx.y * 16;
     stage_edges(edges, a.src, kGradThreads);
     __syncthreads();
-    f32x4 acc[Tiles] = {};
     const uint32_t splat = col * 0x10001u;
     char *const mine = shared + wave * Rows;
     // Load i: head 4 (i % Blocks) + group, 16 bytes at piece col of 256-byte run
@@ -318,15 +341,9 @@ __global__ void __launch_bounds__(kGradThreads) k_bias_grad(BiasGradArgs a) {
             x[i] = load_pack<V>(g + uint64_t(head) * a.src.positions + min(u.first + (i / Blocks) * L + col * V, last));
         }
     };
-    uint64_t at = uint64_t(blockIdx.x) * kGradWaves + wave;
-    Unit u{};
-    Pack<T, V> x[4];
-    if (at < a.units) {
-        u = unit_at<Few>(a, uint32_t(at), Step);
-        fetch(x, u, u.b0);
-    }
-    while (at < a.units) {
-        uint32_t present[Step / 64] = {};                  // tiles with a bucket of these 64 positions, a bit each
+    f32x4 acc[Tiles] = {};
+    uint32_t present[Step / 64];                           // tiles with a bucket of 64 positions, a bit each
+    const auto find = [&](const Unit &u) __attribute__((always_inline)) {
 #pragma unroll
         for (uint32_t s = 0; s < Step / 64; ++s) {
             const uint32_t i = s * 64 + lane;
@@ -342,94 +359,159 @@ __global__ void __launch_bounds__(kGradThreads) k_bias_grad(BiasGradArgs a) {
                 if (p < piece) k = 0xffffu;
             }
             ids[wave][i] = uint16_t(k);
+            present[s] = 0;
 #pragma unroll
             for (int t = 0; t < Tiles; ++t) present[s] |= uint32_t(__any(k >> 4 == uint32_t(t))) << t;
         }
-        at += uint64_t(gridDim.x) * kGradWaves;
-        const Unit v = at < a.units ? unit_at<Few>(a, uint32_t(at), Step) : Unit{};
+    };
+    const auto hand_over = [&](const Pack<T, V> &y, uint32_t row) __attribute__((always_inline)) {
+        char *const to = mine + row * Row;
+        if constexpr (sizeof(T) == 4) {
+            uint32_t cut[4][3];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float g = __uint_as_float(y.w[e]);
+                cut[e][0] = y.w[e] & 0xffff0000u;
+                const float rest = g - __uint_as_float(cut[e][0]);
+                cut[e][1] = __float_as_uint(rest) & 0xffff0000u;
+                cut[e][2] = __float_as_uint(rest - __uint_as_float(cut[e][1]));
+            }
+#pragma unroll
+            for (int c = 0; c < 3; ++c)
+                *reinterpret_cast<u32x2 *>(to + c * 128 + col * 8) =
+                    u32x2{__builtin_amdgcn_perm(cut[1][c], cut[0][c], 0x07060302u),
+                          __builtin_amdgcn_perm(cut[3][c], cut[2][c], 0x07060302u)};
+        } else {
+            *reinterpret_cast<u32x4 *>(to + col * 16) = u32x4{y.w[0], y.w[1], y.w[2], y.w[3]};
+        }
+    };
+    const auto add_up = [&](int run) __attribute__((always_inline)) {
+        const char *const operand = mine + (col & (4 * Blocks - 1)) * Row + group * 16;
+#pragma unroll
+        for (uint32_t q = 0; q < L / 32; ++q) {
+            u32x4 w = *reinterpret_cast<const u32x4 *>(&ids[wave][run * L + q * 32 + group * 8]);
+            w ^= splat;
+            constexpr int Parts = sizeof(T) == 4 ? 3 : 1;
+            u32x4 part[Parts];
+#pragma unroll
+            for (int c = 0; c < Parts; ++c) part[c] = *reinterpret_cast<const u32x4 *>(operand + c * 128 + q * 64);
+#pragma unroll
+            for (int t = 0; t < Tiles; ++t) {
+                if (Tiles > 1 && !(present[(run * L + q * 32) / 64] >> t & 1)) continue;
+                u32x4 one;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) one[j] = match2(w[j], t * 0x00100010u);
+                typedef typename Select<sizeof(T) == 4, bf16, T>::type P;
+#pragma unroll
+                for (int c = 0; c < Parts; ++c) acc[t] = product(P{}, one, part[c], acc[t]);
+            }
+        }
+    };
+    // lane holds rows group * 4 .. + 3 of column col of each tile; waves add in turn
+    float(*const sums)[16] = reinterpret_cast<float(*)[16]>(shared);
+    const auto join_waves = [&]() __attribute__((always_inline)) {
+        __syncthreads();
+        for (uint32_t i = threadIdx.x; i < Tiles * 256; i += kGradThreads) sums[i >> 4][i & 15] = 0.0f;
+        __syncthreads();
+        for (uint32_t w = 0; w < kGradWaves; ++w) {
+            if (w == wave) {
+#pragma unroll
+                for (int t = 0; t < Tiles; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) sums[t * 16 + group * 4 + r][col] += 0.5f * acc[t][r];
+            }
+            __syncthreads();
+        }
+    };
+    uint32_t at = blockIdx.x * kGradWaves + wave;          // below 2^31 + 4096
+    Unit u{};
+    Pack<T, V> x[4];
+    if (at < a.units) {
+        u = unit_at<Few>(a, at, Step);
+        fetch(x, u, u.b0);
+    }
+    while (at < a.units) {
+        find(u);
+        at += gridDim.x * kGradWaves;
+        const Unit v = at < a.units ? unit_at<Few>(a, at, Step) : Unit{};
         for (uint32_t b = u.b0; b < u.b1; ++b) {
             // runs of 256 bytes change hands one after the other
 #pragma unroll
             for (int run = 0; run < 4 / Blocks; ++run) {
                 wave_sync();
 #pragma unroll
-                for (int i = 0; i < Blocks; ++i) {
-                    const Pack<T, V> &y = x[run * Blocks + i];
-                    char *const to = mine + (4 * i + group) * Row;
-                    if constexpr (sizeof(T) == 4) {
-                        uint32_t cut[4][3];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float g = __uint_as_float(y.w[e]);
-                            cut[e][0] = y.w[e] & 0xffff0000u;
-                            const float rest = g - __uint_as_float(cut[e][0]);
-                            cut[e][1] = __float_as_uint(rest) & 0xffff0000u;
-                            cut[e][2] = __float_as_uint(rest - __uint_as_float(cut[e][1]));
-                        }
-#pragma unroll
-                        for (int c = 0; c < 3; ++c)
-                            *reinterpret_cast<u32x2 *>(to + c * 128 + col * 8) =
-                                u32x2{__builtin_amdgcn_perm(cut[1][c], cut[0][c], 0x07060302u),
-                                      __builtin_amdgcn_perm(cut[3][c], cut[2][c], 0x07060302u)};
-                    } else {
-                        *reinterpret_cast<u32x4 *>(to + col * 16) = u32x4{y.w[0], y.w[1], y.w[2], y.w[3]};
-                    }
-                }
+                for (int i = 0; i < Blocks; ++i) hand_over(x[run * Blocks + i], 4 * i + group);
                 wave_sync();
                 if (run == 4 / Blocks - 1) {
                     // the gradients of the step after this one are on their way meanwhile
                     if (b + 1 < u.b1) fetch(x, u, b + 1);
                     else if (at < a.units) fetch(x, v, v.b0);
                 }
-                const char *const operand = mine + (col & (4 * Blocks - 1)) * Row + group * 16;
-#pragma unroll
-                for (uint32_t q = 0; q < L / 32; ++q) {
-                    u32x4 w = *reinterpret_cast<const u32x4 *>(&ids[wave][run * L + q * 32 + group * 8]);
-                    w ^= splat;
-                    constexpr int Parts = sizeof(T) == 4 ? 3 : 1;
-                    u32x4 part[Parts];
-#pragma unroll
-                    for (int c = 0; c < Parts; ++c) part[c] = *reinterpret_cast<const u32x4 *>(operand + c * 128 + q * 64);
-#pragma unroll
-                    for (int t = 0; t < Tiles; ++t) {
-                        if (Tiles > 1 && !(present[(run * L + q * 32) / 64] >> t & 1)) continue;
-                        u32x4 one;
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) one[j] = match2(w[j], t * 0x00100010u);
-                        typedef typename Select<sizeof(T) == 4, bf16, T>::type P;
-#pragma unroll
-                        for (int c = 0; c < Parts; ++c) acc[t] = product(P{}, one, part[c], acc[t]);
-                    }
-                }
+                add_up(run);
             }
         }
         wave_sync();
         u = v;
     }
-    // lane holds rows group * 4 .. + 3 of column col of each tile; waves add in turn
-    float(*const sums)[16] = reinterpret_cast<float(*)[16]>(shared);
-    __syncthreads();
-    for (uint32_t i = threadIdx.x; i < Tiles * 256; i += kGradThreads) sums[i >> 4][i & 15] = 0.0f;
-    __syncthreads();
-    for (uint32_t w = 0; w < kGradWaves; ++w) {
-        if (w == wave) {
+    bool whole = true;
 #pragma unroll
-            for (int t = 0; t < Tiles; ++t)
+    for (int t = 0; t < Tiles; ++t)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) sums[t * 16 + group * 4 + r][col] += 0.5f * acc[t][r];
-        }
-        __syncthreads();
-    }
+        for (int r = 0; r < 4; ++r) whole &= __builtin_isfinite(acc[t][r]);
+    whole = __all(whole);
+    if (lane == 0) finite[wave] = whole;
+    join_waves();
     float *const out = a.partial + (uint64_t(blockIdx.x) * gridDim.y + blockIdx.y) * (Tiles * 256);
     for (uint32_t i = threadIdx.x; i < Tiles * 256; i += kGradThreads) out[i] = sums[i >> 4][i & 15];
+    uint32_t all = 1;
+#pragma unroll
+    for (int w = 0; w < kGradWaves; ++w) all &= finite[w];
+    if (all) return;
+
+    // once more, without what is not finite
+    for (uint32_t i = threadIdx.x; i < Tiles * 64; i += kGradThreads) odd[i] = 0;
+#pragma unroll
+    for (int t = 0; t < Tiles; ++t) acc[t] = f32x4{};
+    __syncthreads();
+    for (at = blockIdx.x * kGradWaves + wave; at < a.units; at += gridDim.x * kGradWaves) {
+        u = unit_at<Few>(a, at, Step);
+        find(u);
+        for (uint32_t b = u.b0; b < u.b1; ++b) {
+            fetch(x, u, b);
+#pragma unroll
+            for (int run = 0; run < 4 / Blocks; ++run) {
+                wave_sync();
+#pragma unroll
+                for (int i = 0; i < Blocks; ++i) {
+                    Pack<T, V> y = x[run * Blocks + i];
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        const uint32_t k = ids[wave][run * L + col * V + j], row = 4 * i + group;
+                        uint32_t what;
+                        y.put(j, cleaned(y.at(j), what));
+                        if (what && k != 0xffffu) atomicOr(&odd[k * 4 + row / 4], what << (8 * (row & 3)));
+                    }
+                    hand_over(y, 4 * i + group);
+                }
+                wave_sync();
+                add_up(run);
+            }
+        }
+        wave_sync();
+    }
+    join_waves();
+    for (uint32_t i = threadIdx.x; i < Tiles * 256; i += kGradThreads) {
+        const float sum = sums[i >> 4][i & 15];
+        const uint32_t row = i & (4 * Blocks - 1);
+        if (!__builtin_isfinite(out[i]))
+            out[i] = noted(odd[(i >> 4) * 4 + row / 4] >> (8 * (row & 3)) & 0xffu, __is_same(T, f16) ? sum : 4.0f * sum);
+    }
 }
 
 // One workgroup per bucket and 16 heads: thread (slice, head) adds every 16th
 // workgroup's sum, then the slices are added.
-template <typename T>
 __global__ void __launch_bounds__(256) k_bias_join(BiasGradArgs a) {
     __shared__ float part[256];
-    __shared__ float edges[kMaxBuckets];
     const uint32_t col = threadIdx.x & 15, slice = threadIdx.x >> 4;
     const uint32_t k = blockIdx.x, h0 = blockIdx.y * 16;
     const float *p = a.partial + (uint64_t(blockIdx.y) * a.tile_rows + k) * 16 + col;
@@ -450,25 +532,6 @@ __global__ void __launch_bounds__(256) k_bias_join(BiasGradArgs a) {
     }
     sum = part[col];
     if (slice == 0 && h0 + col < a.heads) table_put(a.out, a.table_type, uint64_t(k) * a.heads + h0 + col, sum);
-    const uint64_t odd = __ballot(h0 + col < a.heads && !__builtin_isfinite(sum)) & 0xffff;
-    if (!odd) return;                                      // the same in every wave
-    stage_edges(edges, a.src, 256);
-    for (uint32_t i = 0; i < 16; ++i) {
-        if (!(odd >> i & 1)) continue;
-        __syncthreads();
-        sum = 0.0f;
-        for (uint32_t b = 0; b < a.batch; ++b)
-            for (uint64_t q = threadIdx.x; q < a.src.positions; q += 256)
-                if (bucket_of(edges, a.src.span, distance_at(a.src, b, uint32_t(q))) == k)
-                    sum += widen(static_cast<const T *>(a.grad)[(uint64_t(b) * a.heads + h0 + i) * a.src.positions + q]);
-        part[threadIdx.x] = sum;
-        __syncthreads();
-        for (uint32_t w = 128; w; w >>= 1) {
-            if (threadIdx.x < w) part[threadIdx.x] += part[threadIdx.x + w];
-            __syncthreads();
-        }
-        if (threadIdx.x == 0) table_put(a.out, a.table_type, uint64_t(k) * a.heads + h0 + i, part[0]);
-    }
 }
 
 }  // namespace tmtrain

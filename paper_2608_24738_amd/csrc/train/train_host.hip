@@ -661,9 +661,7 @@ int run_bias_grad(const BiasShape &s, const void *grad, int grad_dtype, int64_t 
         return by_blocks(blocks, [&](auto n) { return run(n, Bool<false>{}); });
     });
     if (rc != TM_OK) return rc;
-    return by_type(grad_dtype, [&](auto t) {
-        return launch(k_bias_join<decltype(t)>, dim3(s.src.buckets, uint32_t(groups)), dim3(256), 0, stream, a);
-    });
+    return launch(k_bias_join, dim3(s.src.buckets, uint32_t(groups)), dim3(256), 0, stream, a);
 }
 
 }  // namespace

@@ -1,10 +1,12 @@
-"""The gradient of a bias's table where its sums are long, against sums in float64.
+"""The gradient of a bias's table where its sums are long or not finite, against sums in float64.
 
 Bounds.  With u = 2^-24, a sum of positive terms is off by at most u of itself for every addition that a term goes
 through.  The positions of 16 heads are spread over the waves of up to 512 workgroups, 4096 in all, but for a last
 step of up to 512 positions to a wave; a wave's sum takes every position of it, float32 ones in three pieces; behind it
 come 8 waves, 32 workgroups and 4 halvings: u (3 (positions / 4096 + 512) + 44) of the sum for any order of additions.
 """
+import time
+
 import numpy as np
 import pytest
 
@@ -74,3 +76,83 @@ def test_small_samples(batch, heads, buckets, positions, dtype):
     bucket = ref.buckets(ref.grid_distances((1,), (positions,), (3,), "taxicab", None), edges.numpy()).reshape(1, -1)
     total, size, _ = ref.gradient(up.double().numpy(), bucket, buckets)
     ref.check(got.double().cpu().numpy(), total, 16 * U * size, "f32", "a grid")
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("heads,buckets", [(1, 5), (3, 24), (6, 17), (16, 32), (20, 70), (5, 256)])
+@pytest.mark.parametrize("positions", [1, 3, 7, 9, 2100, 70001])
+def test_not_finite(heads, buckets, positions, dtype):
+    """Infinities of one sign, of both, and NaN reach their own bucket and head; all other sums are as without them."""
+    import torch
+    from paper_2608_24738_amd import training
+    dev = "cuda:0"
+    batch = max(2, 3000 // positions)
+    gen = torch.Generator().manual_seed(positions + heads)
+    edges = training.distance_edges(buckets, 40)
+    announce("not finite %d x %d, %d heads, %d buckets, %s" % (batch, positions, heads, buckets, dtype))
+    d = torch.rand((batch, positions), generator=gen) * 60
+    up = torch.randn((batch, heads, positions), generator=gen)
+    bucket = ref.buckets(d.numpy(), edges.numpy())
+    inf, nan = float("inf"), float("nan")
+    for h in range(heads):
+        odd = [[inf], [inf, -inf], [nan], [-inf, -inf], [inf, nan]][h % 5]
+        for value in odd:
+            b, p = (int(torch.randint(0, n, (1,), generator=gen)) for n in (batch, positions))
+            up[b, h, p] = value
+    # opposite infinities in one bucket
+    up[0, 0, 0], up[1, 0, positions - 1] = inf, -inf
+    d[1, positions - 1] = d[0, 0]
+    bucket = ref.buckets(d.numpy(), edges.numpy())
+    up = up.to(getattr(torch, TYPES[dtype]))
+    got = field_gradient(d.to(dev), edges.to(dev), up.to(dev), heads)
+    total, _, _ = ref.gradient(up.double().numpy(), bucket, buckets)
+    finite = torch.where(torch.isfinite(up), up, torch.zeros_like(up))
+    size = ref.gradient(finite.double().numpy(), bucket, buckets)[1]
+    ref.check(got, total, 16 * U * size, "f32", "not finite")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_largest(dtype):
+    """Gradients next to the type's largest whose sums stay in range."""
+    import torch
+    from paper_2608_24738_amd import training
+    dev = "cuda:0"
+    edges = training.distance_edges(20, 40)
+    gen = torch.Generator().manual_seed(2)
+    d = torch.rand((3, 4000), generator=gen) * 40
+    up = torch.randn((3, 5, 4000), generator=gen)
+    kind = getattr(torch, TYPES[dtype])
+    up[0, 1, 17], up[2, 1, 40], up[1, 3, 3999] = 0.75 * torch.finfo(kind).max, 1e-3, -torch.finfo(kind).max
+    d[2, 40] = d[0, 17] + 20 if d[0, 17] < 20 else d[0, 17] - 20
+    up = up.to(kind)
+    announce("the largest gradients %s" % dtype)
+    got = field_gradient(d.to(dev), edges.to(dev), up.to(dev), 5)
+    total, size, _ = ref.gradient(up.double().numpy(), ref.buckets(d.numpy(), edges.numpy()), 20)
+    assert np.isfinite(got).all()
+    ref.check(got, total, 16 * U * size, "f32", "largest")
+
+
+def test_infinities_cost_little():
+    """An infinity in every head, as a scaled loss that overflowed leaves them: the sums are made twice, and
+    32 times the time of a clean call is far out."""
+    import torch
+    from paper_2608_24738_amd import training
+    dev = "cuda:0"
+    edges = training.distance_edges(32, 1024, signed=True).to(dev)
+    up = torch.randn((2, 16, 1024, 1024), device=dev).to(torch.bfloat16)
+    table = torch.zeros((32, 16), device=dev, requires_grad=True)
+    announce("an infinity in every head")
+
+    def once(up):
+        bias = training.relative_bias(table, edges, 1024, 1024, metric="offset", add=up)
+        torch.cuda.synchronize()
+        begin = time.perf_counter()
+        grad, = torch.autograd.grad([bias], [table], [up])
+        torch.cuda.synchronize()
+        return time.perf_counter() - begin, grad
+    clean = sorted(once(up)[0] for _ in range(7))[3]
+    up[1, :, 700, 3] = float("inf")
+    times, grad = zip(*[once(up) for _ in range(7)])
+    print("clean %.0f us, with infinities %.0f us" % (1e6 * clean, 1e6 * sorted(times)[3]), flush=True)
+    assert int(torch.isinf(grad[0]).sum()) == 16 and not torch.isnan(grad[0]).any()
+    assert sorted(times)[3] < 32 * clean

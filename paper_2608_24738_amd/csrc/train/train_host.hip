@@ -556,7 +556,7 @@ int run_bias(const BiasShape &s, const void *table, int table_dtype, int64_t hea
     // Shares: all heads to a workgroup where the positions alone fill the chip,
     // else four heads at a time and then parts of the batch (one query and 4096
     // keys, 16 heads: 6.0 us, unshared 8.9; 512 x 512, 8 samples: 25, 38); a
-    // share's table fits 32 KB of LDS.
+    // share's table takes at most 36 KB of LDS.
     uint64_t vec = 16 / float_bytes(out_dtype);
     if (s.src.positions < vec) vec = 1;
     const uint64_t tiles = ceil_div(s.src.positions, kBiasThreads * vec);

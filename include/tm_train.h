@@ -56,7 +56,8 @@ enum {
  * A class with p_c = 0 adds nothing to the entropy and to the mean, whatever
  * its logit and field hold there.  Where every logit is -inf, log-probabilities
  * are -inf and the entropy, the mean and the gradient 0.  Where one is NaN or
- * +inf, the position's float results are NaN and its out_index unspecified.
+ * +inf, the position's float results are NaN (out_logp stays 0 without a label)
+ * and its out_index is any class.
  * All arithmetic is float32.
  *
  *   logits   dtype TM_DTYPE_F32, _F16 or _BF16; element (o, c, i) lies at
@@ -149,8 +150,9 @@ int tm_relative_bias(int ndim, const int64_t *query_shape, const int64_t *key_sh
  *   out_grad[k][h] = sum of grad[b][h][p] over the b, p in bucket k
  *
  * grad: [batch][heads][positions] of grad_dtype; out_grad: [buckets][heads]
- * of table_dtype, summed in float32 and rounded once.  An infinity or NaN
- * reaches its own bucket and head only.  workspace: at least
+ * of table_dtype, summed in float32 and rounded once: some 4096 sums (512 for
+ * 128 heads and more) over shares of b and p in series, added together.  An
+ * infinity or NaN reaches its own bucket and head only.  workspace: at least
  * tm_bias_grad_workspace_size() bytes, 16-byte aligned, no initialisation.
  * Errors: as the forward calls, and TM_ERR_WORKSPACE.
  */

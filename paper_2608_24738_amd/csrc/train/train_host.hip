@@ -284,7 +284,8 @@ extern "C" int tm_label_logp(const void *logits, int dtype, int64_t outer, int64
     a.n = uint32_t(s.positions);
     LabelPlan p = label_plan(dtype, s.n[0], s.n[1], s.n[2], strides);
     // Many alternatives of rows of two loads a lane and more: a wave to a row, whose lanes' bests cost less than a pass
-    // each (65536 x 500, 5, 8, 32: 86, 104, 272 us, by 16 lanes 92, 149, 676; x 100: 81, 103, 265 and 30, 48, 197).
+    // each (65536 x 500, 8 and 32 of them: 104 and 272 us, by 16 lanes 149 and 676; 5, about where the two meet: 86 and
+    // 92; x 100 with 5, 8, 32: 81, 103, 265 and 30, 48, 197).
     if (top_k >= 8 && s.n[1] >= 32 * (16 / float_bytes(dtype))) p.brief = false;
     a.ts[0] = top_k * inner;
     a.ts[1] = inner;

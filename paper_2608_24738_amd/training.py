@@ -14,7 +14,7 @@ where the library refuses a request; there is no fallback.
 
 Small calls are bound by the host.  On one GPU a backward pass inside ``with
 torch.autograd.set_multithreading_enabled(False):`` stays on the caller's
-thread, which takes a forward and backward pass from 92 to 40 us.
+thread, which takes a forward and backward pass from some 95 to 40 us.
 """
 from __future__ import annotations
 

@@ -1,9 +1,10 @@
 """The gradient of a bias's table where its sums are long or not finite, against sums in float64.
 
 Bounds.  With u = 2^-24, a sum of positive terms is off by at most u of itself for every addition that a term goes
-through.  The positions of 16 heads are spread over the waves of up to 512 workgroups, 4096 in all, but for a last
-step of up to 512 positions to a wave; a wave's sum takes every position of it, float32 ones in three pieces; behind it
-come 8 waves, 32 workgroups and 4 halvings: u (3 (positions / 4096 + 512) + 44) of the sum for any order of additions.
+through.  The positions of 16 heads are spread over the waves of up to 512 workgroups, 4096 in all (half as many for
+20 heads, whose shares stay below the second term here), but for a last step of up to 512 positions to a wave; a wave's
+sum takes every position of it, float32 ones in three pieces; behind it come 8 waves, 32 workgroups and 4 halvings:
+u (3 (positions / 4096 + 512) + 44) of the sum for any order of additions.
 """
 import time
 

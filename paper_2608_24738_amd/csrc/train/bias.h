@@ -191,7 +191,11 @@ __global__ void __launch_bounds__(kBiasThreads) k_bias(BiasArgs a) {
 // 86 us instead of 81 for 2 x 16 x 2048 x 2048, 53 instead of 40 for 32 x 4 x
 // 512^2.)  Fewer than 9 heads leave loads over for more positions.  Sums are
 // float32 in the accumulators, in an order fixed by the sizes.  float32
-// gradients are cut into three bf16 pieces of 8 bits, which lose nothing.
+// gradients are cut into three bf16 pieces of 8 bits, which lose nothing.  The
+// first pieces have sums of their own: those of gradients of about one size are
+// exact for 2^16 of them, and the others' are so much smaller that their
+// roundings do not add up (32 x 2^20 positions of 0.1: off by 5 of 2^-24, in one
+// sum by 166).
 //
 // With 16 heads bound by the gradients' bytes (bf16 2 x 16 x 2048 x 2048: 268 MB
 // in 83 us, 3.2 TB/s right after the forward pass has written as much; without
@@ -343,7 +347,8 @@ __global__ void __launch_bounds__(kGradThreads,
             x[i] = load_pack<V>(g + uint64_t(head) * a.src.positions + min(u.first + (i / Blocks) * L + col * V, last));
         }
     };
-    f32x4 acc[Tiles] = {};
+    constexpr int Lows = sizeof(T) == 4 ? Tiles : 1;
+    f32x4 acc[Tiles] = {}, low[Lows] = {};                 // of the first pieces, of the others
     uint32_t present[Step / 64];                           // tiles with a bucket of 64 positions, a bit each
     const auto find = [&](const Unit &u) __attribute__((always_inline)) {
 #pragma unroll
@@ -405,7 +410,10 @@ __global__ void __launch_bounds__(kGradThreads,
                 for (int j = 0; j < 4; ++j) one[j] = match2(w[j], t * 0x00100010u);
                 typedef typename Select<sizeof(T) == 4, bf16, T>::type P;
 #pragma unroll
-                for (int c = 0; c < Parts; ++c) acc[t] = product(P{}, one, part[c], acc[t]);
+                for (int c = 0; c < Parts; ++c) {
+                    f32x4 &sum = c ? low[t % Lows] : acc[t];
+                    sum = product(P{}, one, part[c], sum);
+                }
             }
         }
     };
@@ -455,6 +463,16 @@ __global__ void __launch_bounds__(kGradThreads,
         wave_sync();
         u = v;
     }
+    const auto add_low = [&]() __attribute__((always_inline)) {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int t = 0; t < Tiles; ++t) {
+                acc[t] += low[t];
+                low[t] = f32x4{};
+            }
+        }
+    };
+    add_low();
     bool whole = true;
 #pragma unroll
     for (int t = 0; t < Tiles; ++t)
@@ -501,6 +519,7 @@ __global__ void __launch_bounds__(kGradThreads,
         }
         wave_sync();
     }
+    add_low();
     join_waves();
     for (uint32_t i = threadIdx.x; i < Tiles * 256; i += kGradThreads) {
         const float sum = sums[i >> 4][i & 15];

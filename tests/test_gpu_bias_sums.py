@@ -53,6 +53,24 @@ def test_equal_gradients(batch, shape, heads, dtype):
 
 
 @pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("batch,positions,heads", [(32, 1 << 20, 1), (8, 1 << 20, 3), (5, 1 << 19, 16)])
+def test_long_sums(batch, positions, heads, dtype):
+    """Many equal gradients.  Their first 8 bits (16-bit ones have 11 at most) add up exactly while a wave has no more
+    than 2^13 of them, 2^25 to 4096 waves.  What is left of float32 ones is below 2^-7 of them in two pieces: 512
+    products of 32 positions, of 8 additions each, that round by half of 2^-23 of a sum which grows evenly, 2^-24 of its
+    last value on average, are 4096 u 2^-7 = 32 u; 20 more for the waves and workgroups, each by half a unit."""
+    import torch
+    dev = "cuda:0"
+    announce("long sums %d x %d, %d heads, %s" % (batch, positions, heads, dtype))
+    d = torch.full((batch, positions), 7.0, device=dev)
+    up = torch.full((batch, heads, positions), 0.1, dtype=getattr(torch, TYPES[dtype]), device=dev)
+    got = field_gradient(d, torch.tensor([1.0, 15.0], device=dev), up, heads)
+    want = np.zeros((3, heads))
+    want[1] = float(up[0, 0, 0]) * batch * positions
+    ref.check(got, want, 52 * U * want, "f32", "long sums")
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
 @pytest.mark.parametrize("positions", [1, 2, 3, 4, 5, 7, 8, 9])
 @pytest.mark.parametrize("batch,heads,buckets", [(1, 1, 1), (2, 5, 9), (63, 16, 40), (64, 4, 256), (65, 33, 17),
                                                  (1001, 2, 130)])

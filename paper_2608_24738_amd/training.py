@@ -31,6 +31,7 @@ from .binding import METRICS, _call, _sampling_array, _shape_array, load
 FLOATS = {torch.float16: 4, torch.bfloat16: 5, torch.float32: 6}
 LABELS = {torch.uint8: 0, torch.int32: 2, torch.int64: 3}
 DISTANCES = {torch.int32: 2, torch.float32: 6}
+DISTANCE_TYPES = {code: kind for kind, code in DISTANCES.items()}
 BIAS_METRICS = dict(METRICS, offset=3)
 MAX_TOP = 32
 MAX_RECOMPUTE = 32           # classes whose gradient needs no saved statistics
@@ -104,13 +105,15 @@ def _label_plan(shape, strides, dim, dtype, top_k):
 
 
 def _label_forward(logits, labels, field, dim, entropy, top_k, stats):
-    """Runs tm_label_logp; returns (logits, field) as they were read, the outputs
-    and the statistics for the gradient."""
-    dev, dtype = logits.device, FLOATS[logits.dtype]
-    plan = _label_plan(tuple(logits.shape), logits.stride(), dim, dtype, top_k)
+    """Runs tm_label_logp; returns (logits, field) as they were read, the outputs,
+    the statistics for the gradient and what the tensors are: (axis, type, device
+    and shape of the logits, type of the labels, both types' codes)."""
+    dev, kind, whole = logits.device, logits.dtype, tuple(logits.shape)
+    dtype = FLOATS[kind]
+    plan = _label_plan(whole, logits.stride(), dim, dtype, top_k)
     if plan is None:
         logits = logits.contiguous()
-        plan = _label_plan(tuple(logits.shape), logits.stride(), dim, dtype, top_k)
+        plan = _label_plan(whole, logits.stride(), dim, dtype, top_k)
     extents, strides, shape, shape_k, nbytes = plan
     field_strides = None
     if field is not None:
@@ -123,11 +126,12 @@ def _label_forward(logits, labels, field, dim, entropy, top_k, stats):
     index = empty(shape_k, dtype=torch.int32, device=dev) if top_k else None
     kept = empty(shape + (2,), dtype=f32, device=dev) if stats else None
     workspace = empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
-    label_dtype = LABELS[labels.dtype] if labels is not None else 0
+    label_kind, label_dtype = (labels.dtype, LABELS[labels.dtype]) if labels is not None else (None, 0)
     _call("tm_label_logp", dev, None, logits.data_ptr(), dtype, *extents, strides, _ptr(labels), label_dtype,
           _ptr(field), field_strides, top_k, _ptr(logp), _ptr(ent), _ptr(mean), _ptr(top), _ptr(index), _ptr(kept),
           _ptr(workspace), nbytes)
-    return logits, field, (logp, ent, mean, top, index), kept
+    what = (dim, kind, dev, whole, label_kind, dtype, label_dtype)
+    return logits, field, (logp, ent, mean, top, index), kept, what
 
 
 def _upstream(grad):
@@ -136,21 +140,18 @@ def _upstream(grad):
     return grad.to(torch.float32).contiguous()
 
 
-def _kind(t):
-    return None if t is None else (t.dtype, t.device, t.shape)
+def _restored(t, dtype, device, shape):
+    """A dense tensor that autograd kept.  Hooks on saved tensors (such as
+    torch.autograd.graph.save_on_cpu) may give it another layout, nothing else."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.device != device or t.shape != shape:
+        _changed()
+    return t.contiguous()
 
 
-def _restored(tensors, kinds):
-    """Checks tensors that autograd kept.  Hooks on saved tensors (such as
-    torch.autograd.graph.save_on_cpu) may give them another layout, nothing else."""
-    for t, kind in zip(tensors, kinds):
-        if _kind(t) != kind:
-            raise RuntimeError("a hook on saved tensors gave back %s for %s" % (_kind(t), kind))
-    return tensors
-
-
-def _dense(t):
-    return None if t is None else t.contiguous()
+def _changed():
+    raise RuntimeError("a hook on saved tensors gave back another type, shape or device")
 
 
 def _once():
@@ -170,14 +171,11 @@ class _LabelLogProbs(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, labels, field, dim, entropy, top_k):
         stats = logits.shape[dim] > MAX_RECOMPUTE
-        logits, field, out, kept = _label_forward(logits, labels, field, dim, entropy, top_k, stats)
-        ctx.dim = dim
+        logits, field, out, kept, ctx.what = _label_forward(logits, labels, field, dim, entropy, top_k, stats)
         ctx.set_materialize_grads(False)
         if top_k:
             ctx.mark_non_differentiable(out[3], out[4])
-        saved = (logits, labels, field, kept, out[1] if stats else None, out[2] if stats else None)
-        ctx.kinds = [_kind(t) for t in saved]
-        ctx.save_for_backward(*saved)
+        ctx.save_for_backward(logits, labels, field, kept, out[1] if stats else None, out[2] if stats else None)
         return out
 
     @staticmethod
@@ -185,17 +183,35 @@ class _LabelLogProbs(torch.autograd.Function):
         _once()
         if up_logp is None and up_entropy is None and up_mean is None:
             return None, None, None, None, None, None
-        logits, labels, field, kept, entropy, mean = _restored(ctx.saved_tensors, ctx.kinds)
+        logits, labels, field, kept, entropy, mean = ctx.saved_tensors
+        dim, kind, dev, shape, label_kind, dtype, label_dtype = ctx.what
+        if logits.dtype is not kind or logits.device != dev or logits.shape != shape:
+            _changed()
         # strides are those of the tensors at hand, not the forward call's
-        logits, extents, strides = _viewed(logits, ctx.dim)
-        field_strides = None
+        plan = _label_plan(shape, logits.stride(), dim, dtype, 0)
+        if plan is None:
+            logits = logits.contiguous()
+            plan = _label_plan(shape, logits.stride(), dim, dtype, 0)
+        extents, strides, rest = plan[:3]
+        f32, field_strides = torch.float32, None
+        labels = _restored(labels, label_kind, dev, rest)
         if field is not None:
-            field, _, field_strides = _viewed(field, ctx.dim)
-        labels, kept, entropy, mean = _dense(labels), _dense(kept), _dense(entropy), _dense(mean)
+            if field.dtype is not f32 or field.device != dev or field.shape != shape:
+                _changed()
+            view = _view(shape, field.stride(), dim)
+            if view is None:
+                field = field.contiguous()
+                view = _view(shape, field.stride(), dim)
+            field_strides = view[1]
+        if kept is not None:
+            kept = _restored(kept, f32, dev, rest + (2,))
+            entropy, mean = _restored(entropy, f32, dev, rest), _restored(mean, f32, dev, rest)
         up_logp, up_entropy, up_mean = _upstream(up_logp), _upstream(up_entropy), _upstream(up_mean)
-        grad, _, grad_strides = _viewed(torch.empty_like(logits), ctx.dim)
-        label_dtype = LABELS[labels.dtype] if labels is not None else 0
-        _call("tm_label_logp_grad", logits.device, None, logits.data_ptr(), FLOATS[logits.dtype], *extents, strides,
+        grad = torch.empty_like(logits)
+        grad_strides = strides
+        if grad.stride() != logits.stride():
+            grad, _, grad_strides = _viewed(grad, dim)
+        _call("tm_label_logp_grad", dev, None, logits.data_ptr(), dtype, *extents, strides,
               _ptr(labels), label_dtype, _ptr(field), field_strides, _ptr(kept), _ptr(entropy), _ptr(mean),
               _ptr(up_logp), _ptr(up_entropy), _ptr(up_mean), grad.data_ptr(), grad_strides)
         return grad, None, None, None, None, None
@@ -292,31 +308,33 @@ class _Bias(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, table, edges, add, source, shape):
-        ctx.name, ctx.args, distances = source
-        ctx.table_dtype, ctx.table_shape = table.dtype, tuple(table.shape)
-        ctx.has_add = add is not None
-        ctx.kinds = (_kind(edges), _kind(distances))
+        name, args, distances = source
         ctx.save_for_backward(edges, distances)
+        ctx.kind = (name + "_grad", args, table.dtype, tuple(table.shape), add is not None,
+                    None if distances is None else distances.shape)
         return _bias_forward(table, edges, add, source, shape)
 
     @staticmethod
     def backward(ctx, up):
         _once()
         grad = None
-        if ctx.needs_input_grad[0]:
-            edges, distances = _restored(ctx.saved_tensors, ctx.kinds)
-            edges, distances, args = edges.contiguous(), _dense(distances), ctx.args
+        name, args, dtype, shape, has_add, field_shape = ctx.kind
+        wanted = ctx.needs_input_grad
+        if wanted[0]:
+            edges, distances = ctx.saved_tensors
             up = up.contiguous()
-            buckets, heads = ctx.table_shape
-            dev = edges.device
-            grad = torch.empty(ctx.table_shape, dtype=ctx.table_dtype, device=dev)
+            buckets, heads = shape
+            dev = up.device
+            edges = _restored(edges, torch.float32, dev, (buckets - 1,))
+            grad = torch.empty(shape, dtype=dtype, device=dev)
             nbytes = _bias_workspace(buckets, heads)
             workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
             if distances is not None:
+                distances = _restored(distances, DISTANCE_TYPES[args[1]], dev, field_shape)
                 args = (distances.data_ptr(),) + args[1:]
-            _call(ctx.name + "_grad", dev, None, *args, up.data_ptr(), FLOATS[up.dtype], buckets, heads, edges.data_ptr(),
-                  grad.data_ptr(), FLOATS[ctx.table_dtype], _ptr(workspace), nbytes)
-        return grad, None, up if ctx.has_add and ctx.needs_input_grad[2] else None, None, None
+            _call(name, dev, None, *args, up.data_ptr(), FLOATS[up.dtype], buckets, heads, edges.data_ptr(),
+                  grad.data_ptr(), FLOATS[dtype], _ptr(workspace), nbytes)
+        return grad, None, up if has_add and wanted[2] else None, None, None
 
 
 @functools.lru_cache(maxsize=1024)

@@ -167,6 +167,68 @@ int tm_relative_bias_grad(int ndim, const int64_t *query_shape, const int64_t *k
                           hipStream_t stream);
 size_t tm_bias_grad_workspace_size(int buckets, int64_t heads);
 
+/*
+ * tm_head_logp -- log-probabilities of given labels from hidden states and a
+ * vocabulary's weight, whose logits are never stored:
+ *
+ *   x_nv = scale * sum_d hidden[n][d] weight[v][d]
+ *   out_logp[n]     x_ny - log sum_v exp x_nv for the row's label y; 0 where y
+ *                   lies outside [0, classes) (a row without a label)
+ *   out_log_sum[n]  log sum_v exp x_nv, of every row
+ *   out_stats[n][2] for tm_head_logp_grad: M, near the largest x_nv log2(e), and
+ *                   sum_v 2^(x_nv log2(e) - M)
+ *
+ * Rows without a label take no part, unless out_log_sum is asked for: what
+ * they hold, NaN included, changes nothing, and no work is done for them.
+ * Where every logit is -inf, out_logp and out_log_sum are -inf; where one is NaN
+ * or +inf, the row's results are NaN (out_logp stays 0 without a label).
+ * Products are summed in float32.
+ *
+ *   hidden   [rows][width] of dtype (TM_DTYPE_F32, _F16 or _BF16), rows
+ *            hidden_stride elements apart.
+ *   weight   [classes][width] of dtype, rows weight_stride elements apart.
+ *   labels   [rows] contiguous, label_dtype TM_DTYPE_U8 (read unsigned), _I32
+ *            or _I64; NULL if out_log_sum alone is asked for.
+ *   scale    positive and finite, rounded to float32.
+ *   out_logp, out_log_sum  [rows] float32, one may be NULL; out_stats may be NULL.
+ *   workspace  at least tm_head_logp_workspace_size() bytes, 16-byte aligned;
+ *            needs no initialisation.
+ *
+ * Errors: TM_ERR_SHAPE (classes or width < 1, negative rows or strides),
+ * TM_ERR_NULL, TM_ERR_NO_OUTPUT, TM_ERR_DTYPE, TM_ERR_SAMPLING (scale),
+ * TM_ERR_TOO_LARGE (some 2^31 rows or classes, 2^31 tiles of 128 x 128 logits,
+ * more than 2^24 columns), TM_ERR_WORKSPACE, TM_ERR_ALIAS, TM_ERR_HIP.
+ */
+int tm_head_logp(const void *hidden, int dtype, int64_t rows, int64_t classes, int64_t width, int64_t hidden_stride,
+                 const void *weight, int64_t weight_stride, const void *labels, int label_dtype, double scale,
+                 float *out_logp, float *out_log_sum, float *out_stats, void *workspace, size_t workspace_bytes,
+                 hipStream_t stream);
+size_t tm_head_logp_workspace_size(int dtype, int64_t rows, int64_t classes, int64_t width);
+
+/*
+ * tm_head_logp_grad -- the gradients, given the upstream gradients a of
+ * out_logp and z of out_log_sum (each may be NULL, not both): with
+ *
+ *   g_nv = scale * (a_n 1[v = y_n] - (a_n - z_n) p_nv),   a_n = 0 without a label,
+ *   out_hidden[n][d] = sum_v g_nv weight[v][d]     [rows][width] contiguous, of dtype
+ *   out_weight[v][d] = sum_n g_nv hidden[n][d]     [classes][width] contiguous, of dtype
+ *
+ * Either may be NULL.  Rows without a label take part only if z is given; those
+ * that do not get zeros and reach no gradient.  stats are what tm_head_logp
+ * gave.  g is computed in float32, a piece of the vocabulary at a time, and for
+ * more than 16 rows rounded once to dtype for the two products, which are
+ * summed in float32 (float16: g is rounded as a multiple of powers of two, one
+ * to a row for out_hidden and a common one, of the largest |a| and |z|, for
+ * out_weight).  Where every logit of a row is -inf, its g is 0.
+ * Errors: as tm_head_logp.
+ */
+int tm_head_logp_grad(const void *hidden, int dtype, int64_t rows, int64_t classes, int64_t width,
+                      int64_t hidden_stride, const void *weight, int64_t weight_stride, const void *labels,
+                      int label_dtype, double scale, const float *stats, const float *up_logp, const float *up_log_sum,
+                      void *out_hidden, void *out_weight, void *workspace, size_t workspace_bytes, hipStream_t stream);
+size_t tm_head_logp_grad_workspace_size(int dtype, int64_t rows, int64_t classes, int64_t width, int hidden,
+                                        int weight);
+
 #ifdef __cplusplus
 }
 #endif

@@ -97,7 +97,14 @@ def load() -> ctypes.CDLL:
             lib.tm_distance_bias_grad.argtypes = [vp, i32, i64, i64, vp, i32, i32, i64, vp, vp, i32, vp, size, vp]
             lib.tm_relative_bias_grad.argtypes = grid + [vp, i32, i32, i64, vp, vp, i32, vp, size, vp]
             lib.tm_bias_grad_workspace_size.argtypes = [i32, i64]
-            for name in ("tm_label_logp", "tm_label_logp_grad", "tm_distance_bias", "tm_relative_bias",
+            head = [vp, i32, i64, i64, i64, i64, vp, i64, vp, i32, ctypes.c_double]
+            lib.tm_head_logp.argtypes = head + [vp, vp, vp, vp, size, vp]
+            lib.tm_head_logp_grad.argtypes = head + [vp, vp, vp, vp, vp, vp, size, vp]
+            lib.tm_head_logp_workspace_size.argtypes = [i32, i64, i64, i64]
+            lib.tm_head_logp_grad_workspace_size.argtypes = [i32, i64, i64, i64, i32, i32]
+            lib.tm_head_logp_workspace_size.restype = size
+            lib.tm_head_logp_grad_workspace_size.restype = size
+            for name in ("tm_head_logp", "tm_head_logp_grad", "tm_label_logp", "tm_label_logp_grad", "tm_distance_bias", "tm_relative_bias",
                          "tm_distance_bias_grad", "tm_relative_bias_grad"):
                 getattr(lib, name).restype = i32
             lib.tm_label_logp_workspace_size.restype = size

@@ -1,0 +1,517 @@
+// head.h -- kernels of the log-probabilities from hidden states and a
+// vocabulary's weight (tm_head_logp in include/tm_train.h).
+//
+// With x = scale h w^T, c = scale log2(e) and a whole number M near the largest
+// c h w of a row:
+//     s = sum_v 2^(c h w_v - M),   log sum exp x = ln 2 (M + log2 s),
+//     log p_y = ln 2 ((c h w_y - M) - log2 s),   p_v = 2^(c h w_v - M) / s.
+// M being whole, one fma gives the exponent with one rounding, and sums with
+// different M are put together by exact powers of two.  M starts at -FLT_MAX
+// instead of -inf, so that the exponent is never inf - inf: logits at -inf get
+// 0, and s = 0 marks a row with no class left.
+//
+// The logits are never stored: a tile's pass over k ends in sums of its rows.
+// The gradient computes them anew, a piece of the vocabulary at a time, as
+//     g_nv = alpha_n 1[v = y_n] - beta_n p_nv,   alpha = scale up_logp,
+//     beta = scale (up_logp - up_log_sum),
+// and leaves g and its transpose in the operands' type for the two products
+//     dh = g w,   dw = g^T h.
+// Rows without a label take part only where the log sums are asked for: the
+// rows that do are packed first, and the products run over those alone.
+#pragma once
+
+#include "label.h"
+#include "product.h"
+
+namespace tmtrain {
+
+constexpr uint32_t kFewRows = 16;               // rows of hidden states that one matrix instruction holds
+constexpr uint32_t kListChunk = 4096;           // rows that a workgroup packs
+
+struct HeadSum {
+    float m, s;                 // M, sum of 2^(c h w - M)
+};
+constexpr float kLowest = -FLT_MAX;
+
+// 2^(a - b) for whole a <= b; 0 where a is kLowest and b is not.
+__device__ __forceinline__ float shrink(float a, float b) { return a == b ? 1.0f : exp2_hw(fmaxf(a - b, -200.0f)); }
+
+// inf - inf of the references of rows with +inf stays NaN in s.
+__device__ __forceinline__ HeadSum join(HeadSum a, HeadSum b) {
+    const float m = fmaxf(a.m, b.m);
+    return {m, a.s * shrink(a.m, m) + b.s * shrink(b.m, m)};
+}
+__device__ __forceinline__ float whole(float most, float c) { return fmaxf(rintf(most * c), kLowest); }
+
+// A packed row, for the gradient.
+struct HeadRow {
+    float m;
+    float a, b;                 // alpha, beta / s, for float16 times a power of two
+    int32_t y;
+};
+
+struct HeadArgs {
+    const void *hidden, *weight;
+    uint64_t hidden_stride, weight_stride;      // elements
+    const void *label;
+    int32_t label_bytes;
+    uint32_t n, classes, width;
+    bool all;                   // rows without a label take part
+    float scale, c;             // c = scale log2(e)
+    float *logp, *log_sum;
+    HeadSum *stats;             // of the rows in the caller's order
+    const float *up_logp, *up_log_sum;
+    void *grad_hidden, *grad_weight;
+    // in the workspace
+    uint32_t *count;            // packed rows
+    uint32_t *chunk_count;      // of each chunk of the list, then their exponents
+    uint32_t *list;             // the packed rows' numbers
+    int32_t *place;             // and where each row went, or -1
+    HeadRow *row;
+    float *inverse;             // float16: what takes a packed row's power of two back; then the common one's
+    void *packed, *turned;      // packed hidden states [n][width], and [width][n]
+    HeadSum *part;              // [parts][n_pad]
+    float *found;               // c h w of the packed rows' labels
+    void *slope, *slope_turned; // [n_pad][piece], [piece][n_pad]
+    void *weight_turned;        // [width][piece]
+    void *weight_laid;          // a piece's weights in whole steps, where they do not lie so
+    float *sum;                 // [splits][n_pad][sum_stride]
+    uint32_t n_pad, width_pad, sum_stride;
+    uint32_t parts;
+    uint32_t first, piece;      // classes of the piece at hand, and its width
+    uint32_t splits, steps;     // of the product for dh
+    bool add;                   // to the sums so far
+};
+
+// ---------------------------------------------------------------------------
+// The packed rows.
+// ---------------------------------------------------------------------------
+
+// For float16, g is held times a power of two that brings |alpha| + |beta| to
+// [2^14, 2^15): p is then exact to 11 bits down to 2^-29 of it, where as it
+// stands everything below 2^-14 would lose bits.
+constexpr int kSlopeExponent = 15;
+__device__ __forceinline__ int exponent_of(float x) {       // 2^e > x, 0 for zeros and what is not finite
+    if (!(x > 0.0f) || !(x <= FLT_MAX)) return 0;
+    return max(-100, int(__builtin_amdgcn_frexp_expf(x)));
+}
+__device__ __forceinline__ float power(int e) { return __builtin_amdgcn_ldexpf(1.0f, e); }
+
+struct HeadUp {
+    float a, b;
+};
+__device__ __forceinline__ HeadUp head_up(const HeadArgs &p, uint32_t n, int32_t y) {
+    const float a = y >= 0 && p.up_logp ? p.up_logp[n] : 0.0f;
+    return {p.scale * a, p.scale * (a - (p.up_log_sum ? p.up_log_sum[n] : 0.0f))};
+}
+
+// Sum over a workgroup of 1024 threads of what each holds: the sum of the lower threads' and the total.
+__device__ __forceinline__ uint32_t rank_in_block(uint32_t x, uint32_t *lds, uint32_t &total) {
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t up = x;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t o = __shfl_up(up, d);
+        if (lane >= uint32_t(d)) up += o;
+    }
+    __syncthreads();
+    if (lane == 63) lds[wave] = up;
+    __syncthreads();
+    uint32_t before = 0;
+    total = 0;
+    for (uint32_t w = 0; w < blockDim.x / 64; ++w) {
+        before += w < wave ? lds[w] : 0;
+        total += lds[w];
+    }
+    return before + up - x;
+}
+
+// Four rows a thread: which take part, and the largest exponent of theirs.
+struct HeadFour {
+    int32_t y[4];
+    uint32_t in;
+    int exponent;
+};
+__device__ __forceinline__ HeadFour head_four(const HeadArgs &p, uint32_t n0, bool exponents) {
+    HeadFour f{};
+    f.exponent = -1000;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t n = n0 + i;
+        f.y[i] = -1;
+        if (n >= p.n) continue;
+        f.y[i] = p.label ? load_label(p.label, p.label_bytes, n, p.classes) : -1;
+        if (f.y[i] < 0 && !p.all) continue;
+        f.in |= 1u << i;
+        if (exponents) {
+            const HeadUp u = head_up(p, n, f.y[i]);
+            const float size = fabsf(u.a) + fabsf(u.b);
+            if (size > 0.0f) f.exponent = max(f.exponent, exponent_of(size));
+        }
+    }
+    return f;
+}
+
+// Rows of each chunk that take part (and their largest exponent), where there are several chunks.
+__global__ __launch_bounds__(1024) void k_head_count(HeadArgs p) {
+    __shared__ uint32_t lds[16];
+    __shared__ int top;
+    if (threadIdx.x == 0) top = -1000;
+    __syncthreads();
+    const HeadFour f = head_four(p, blockIdx.x * kListChunk + threadIdx.x * 4, p.inverse != nullptr);
+    if (p.inverse) atomicMax(&top, f.exponent);             // the order does not matter
+    uint32_t total;
+    rank_in_block(__popc(f.in), lds, total);
+    if (threadIdx.x == 0) {
+        p.chunk_count[blockIdx.x] = total;
+        p.chunk_count[gridDim.x + blockIdx.x] = uint32_t(top);
+    }
+}
+
+// The list of packed rows, where each row went, and for the gradient what its
+// tiles need of them.  One workgroup to a chunk.
+__global__ __launch_bounds__(1024) void k_head_list(HeadArgs p) {
+    __shared__ uint32_t lds[16];
+    __shared__ int top;
+    const uint32_t chunks = gridDim.x, chunk = blockIdx.x;
+    if (threadIdx.x == 0) top = -1000;
+    __syncthreads();
+    const bool exponents = p.inverse != nullptr;
+    const uint32_t n0 = chunk * kListChunk + threadIdx.x * 4;
+    const HeadFour f = head_four(p, n0, exponents);
+    uint32_t before = 0, all = 0;
+    if (chunks > 1) {
+        uint32_t mine = 0, sum = 0;
+        for (uint32_t i = threadIdx.x; i < chunks; i += blockDim.x) {
+            const uint32_t x = p.chunk_count[i];
+            sum += x;
+            mine += i < chunk ? x : 0;
+            if (exponents) atomicMax(&top, int(p.chunk_count[chunks + i]));
+        }
+        uint32_t total;
+        rank_in_block(mine, lds, before);
+        rank_in_block(sum, lds, total);
+        all = total;
+    } else if (exponents) {
+        atomicMax(&top, f.exponent);
+    }
+    uint32_t total;
+    uint32_t at = before + rank_in_block(__popc(f.in), lds, total);
+    if (chunks == 1) all = total;
+    __syncthreads();
+    const int common = top < -900 ? 0 : top;
+    if (threadIdx.x == 0 && chunk == 0) {
+        *p.count = all;
+        if (exponents) p.inverse[p.n_pad] = power(common - kSlopeExponent);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t n = n0 + i;
+        if (n >= p.n) break;
+        const bool in = f.in >> i & 1;
+        if (p.place) p.place[n] = in ? int32_t(at) : -1;
+        if (!in) {
+            if (!p.row && p.logp) p.logp[n] = 0.0f;
+            if (!p.row && p.stats) p.stats[n] = {0.0f, 1.0f};
+            continue;
+        }
+        p.list[at] = n;
+        if (p.row) {
+            HeadUp u = head_up(p, n, f.y[i]);
+            const HeadSum s = p.stats[n];
+            if (s.s == 0.0f) u = {0.0f, 0.0f};              // no class left
+            HeadRow r = {s.m, u.a, s.s == 0.0f ? 0.0f : u.b / s.s, f.y[i]};
+            if (exponents) {
+                const float size = fabsf(u.a) + fabsf(u.b);
+                const int e = size > 0.0f ? exponent_of(size) : common;
+                r.a = __builtin_amdgcn_ldexpf(r.a, kSlopeExponent - e);
+                r.b = __builtin_amdgcn_ldexpf(r.b, kSlopeExponent - e);
+                p.inverse[at] = power(e - kSlopeExponent);
+            }
+            p.row[at] = r;
+        }
+        ++at;
+    }
+}
+
+// Rows of `width` elements, `stride` apart, laid out in whole steps with zeros
+// behind them.
+struct LayArgs {
+    const void *from;
+    uint64_t stride;
+    const uint32_t *list, *count;   // which rows; NULL: `rows` of them in order
+    uint32_t rows, width;
+    uint32_t fill;                  // turned: columns to fill with zeros at least
+    void *to;
+    uint32_t to_stride;             // elements
+};
+template <typename T>
+__global__ __launch_bounds__(256) void k_lay_rows(LayArgs p) {
+    constexpr int V = 16 / sizeof(T);
+    const uint32_t rows = p.count ? *p.count : p.rows;
+    const uint32_t pieces = p.to_stride / V;
+    for (uint32_t r = blockIdx.x; r < rows; r += gridDim.x) {
+        const T *from = static_cast<const T *>(p.from) + (p.list ? p.list[r] : r) * p.stride;
+        T *to = static_cast<T *>(p.to) + uint64_t(r) * p.to_stride;
+        for (uint32_t i = threadIdx.x; i < pieces; i += blockDim.x) {
+            const uint32_t c = i * V;
+            store_pack<V>(to + c, c < p.width ? load_pack<V>(from + c, p.width - c, T{}) : Pack<T, V>{});
+        }
+    }
+}
+
+// The same rows turned: `to` is [width][to_stride], its columns from the number
+// of rows to the next whole step zero.  Tiles of 64 x 64 through LDS.
+template <typename T>
+__global__ __launch_bounds__(256) void k_turn_rows(LayArgs p) {
+    constexpr int V = 16 / sizeof(T), kSide = 64, kPieces = kSide / V;
+    __shared__ T tile[kSide][kSide + 4 / sizeof(T)];
+    const uint32_t rows = p.count ? *p.count : p.rows;
+    const uint32_t r0 = blockIdx.x * kSide, c0 = blockIdx.y * kSide;
+    if (r0 >= max(rows, p.fill)) return;
+    for (uint32_t i = threadIdx.x; i < kSide * kPieces; i += 256) {
+        const uint32_t r = r0 + i / kPieces, c = c0 + i % kPieces * V;
+        Pack<T, V> v{};
+        if (r < rows && c < p.width)
+            v = load_pack<V>(static_cast<const T *>(p.from) + (p.list ? p.list[r] : r) * p.stride + c, p.width - c, T{});
+#pragma unroll
+        for (int j = 0; j < V; ++j) tile[i / kPieces][i % kPieces * V + j] = v.at(j);
+    }
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < kSide * kPieces; i += 256) {
+        const uint32_t c = i / kPieces, r = i % kPieces * V;
+        if (c0 + c >= p.width) continue;
+        Pack<T, V> v{};
+#pragma unroll
+        for (int j = 0; j < V; ++j) v.put(j, tile[r + j][c]);
+        store_pack<V>(static_cast<T *>(p.to) + uint64_t(c0 + c) * p.to_stride + r0 + r, v);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Products over tiles.
+// ---------------------------------------------------------------------------
+
+// The weights of the piece at hand, as the left operand.
+template <typename T>
+__device__ __forceinline__ Operand weight_rows(const HeadArgs &p) {
+    const uint32_t rows = min(p.piece, p.classes - p.first);
+    if (p.weight_laid)
+        return {static_cast<const char *>(p.weight_laid), uint64_t(p.width_pad) * sizeof(T), rows, 0};
+    return {static_cast<const char *>(p.weight) + uint64_t(p.first) * p.weight_stride * sizeof(T),
+            p.weight_stride * sizeof(T), rows, uint32_t(p.width * sizeof(T) / 16)};
+}
+template <typename T>
+__device__ __forceinline__ Operand hidden_rows(const HeadArgs &p) {
+    return {static_cast<const char *>(p.packed), uint64_t(p.width_pad) * sizeof(T), p.n_pad, 0};
+}
+
+// Sums of 2^(c x - M) of the packed rows over a tile's classes, one for each
+// wave's classes, and c x of the labels.
+template <typename T, typename Tile>
+__global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_sums(HeadArgs p) {
+    __shared__ __attribute__((aligned(1024))) typename Tile::Buffer even, odd;
+    const uint32_t count = *p.count, tiles_n = (count + Tile::BN - 1) / Tile::BN;
+    const uint32_t rows = min(p.piece, p.classes - p.first), tiles_m = (rows + Tile::BM - 1) / Tile::BM;
+    if (blockIdx.x >= uint64_t(tiles_m) * tiles_n) return;
+    const TilePlace at = tile_place(blockIdx.x, tiles_m, tiles_n);
+    Tile tile;
+    tile.run(weight_rows<T>(p), at.m * Tile::BM, hidden_rows<T>(p), at.n * Tile::BN, 0, p.width_pad / kStep<T>, even,
+             odd);
+    const bool edge = (at.m + 1) * Tile::BM > rows;
+    const uint32_t part = (p.first / Tile::BM + at.m) * Tile::WM + tile.wave / Tile::WN;
+#pragma unroll
+    for (int j = 0; j < Tile::TN; ++j) {
+        const uint32_t n = at.n * Tile::BN + tile.column(j);
+        const bool real = n < count;
+        const int32_t y = real && p.label ? load_label(p.label, p.label_bytes, p.list[n], p.classes) : -1;
+        // the label's row in the tile
+        const uint32_t want = y < 0 ? ~0u : uint32_t(y) - p.first - at.m * Tile::BM;
+        float most = -INFINITY, label = 0.0f;
+#pragma unroll
+        for (int i = 0; i < Tile::TM; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                if (edge && at.m * Tile::BM + tile.row(i) + q >= rows) tile.acc[i][j][q] = -INFINITY;
+                const float x = tile.acc[i][j][q];
+                if (want == tile.row(i) + q) label = x;
+                most = fmaxf(most, x);
+            }
+        most = fmaxf(most, __shfl_xor(most, 16));
+        most = fmaxf(most, __shfl_xor(most, 32));
+        const float m = whole(most, p.c);
+        float s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < Tile::TM; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) s += exp2_hw(fmaf(tile.acc[i][j][q], p.c, -m));
+        s += __shfl_xor(s, 16);
+        s += __shfl_xor(s, 32);
+        if (real && tile.lane < 16) p.part[uint64_t(part) * p.n_pad + n] = {m, s};
+        const uint32_t inside = want - (tile.row(0) & ~15u);
+        if (inside < 16u * Tile::TM && (inside & 15) - uint32_t(tile.lane >> 4) * 4 < 4) p.found[n] = label;
+    }
+}
+
+// The sums of a row over all parts: 64 rows to a workgroup, parts over its 16 waves.
+__global__ __launch_bounds__(1024) void k_head_join(HeadArgs p) {
+    __shared__ HeadSum lds[16][64];
+    const uint32_t count = p.count ? *p.count : p.n;
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint32_t j = blockIdx.x * 64 + lane;
+    if (blockIdx.x * 64 >= count) return;
+    HeadSum sum = {kLowest, 0.0f};
+    if (j < count) {
+        // several loads on their way at once
+        constexpr int kAhead = 8;
+        for (uint32_t i = wave; i < p.parts; i += 16 * kAhead) {
+            HeadSum got[kAhead];
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k)
+                got[k] = i + 16 * k < p.parts ? p.part[uint64_t(i + 16 * k) * p.n_pad + j] : HeadSum{kLowest, 0.0f};
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) sum = join(sum, got[k]);
+        }
+    }
+    lds[wave][lane] = sum;
+    __syncthreads();
+    if (wave || j >= count) return;
+    for (int w = 1; w < 16; ++w) sum = join(sum, lds[w][lane]);
+    const uint32_t n = p.count ? p.list[j] : j;
+    const int32_t y = p.label ? load_label(p.label, p.label_bytes, n, p.classes) : -1;
+    const float log_s = log2f(sum.s);
+    if (p.logp) {
+        float l = 0.0f;
+        if (y >= 0) {
+            l = (fmaf(p.found[j], p.c, -sum.m) - log_s) * kLn2;
+            if (sum.s == 0.0f) l = -INFINITY;
+        }
+        p.logp[n] = l;
+    }
+    if (p.log_sum) p.log_sum[n] = sum.s == 0.0f ? -INFINITY : fmaf(log_s, kLn2, sum.m * kLn2);
+    if (p.stats) p.stats[n] = sum;
+}
+
+// g of a piece of the vocabulary, and turned.
+template <typename T, typename Tile>
+__global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_slopes(HeadArgs p) {
+    __shared__ __attribute__((aligned(1024))) typename Tile::Buffer even, odd;
+    const uint32_t count = *p.count, tiles_n = (count + Tile::BN - 1) / Tile::BN, tiles_m = p.piece / Tile::BM;
+    if (blockIdx.x >= uint64_t(tiles_m) * tiles_n) return;
+    const TilePlace at = tile_place(blockIdx.x, tiles_m, tiles_n);
+    const uint32_t rows = min(p.piece, p.classes - p.first);
+    Tile tile;
+    tile.run(weight_rows<T>(p), at.m * Tile::BM, hidden_rows<T>(p), at.n * Tile::BN, 0, p.width_pad / kStep<T>, even,
+             odd);
+    const float common = p.inverse ? 1.0f / p.inverse[p.n_pad] : 1.0f;
+#pragma unroll
+    for (int j = 0; j < Tile::TN; ++j) {
+        const uint32_t n = at.n * Tile::BN + tile.column(j);
+        const bool real = n < count;
+        HeadRow r = {0.0f, 0.0f, 0.0f, -1};
+        if (real) r = p.row[n];
+        const float ratio = p.inverse && real ? common * p.inverse[n] : 1.0f;
+#pragma unroll
+        for (int i = 0; i < Tile::TM; ++i) {
+            const uint32_t v = at.m * Tile::BM + tile.row(i);
+            float g[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                g[q] = -r.b * exp2_hw(fmaf(tile.acc[i][j][q], p.c, -r.m));
+                if (int32_t(p.first + v + q) == r.y) g[q] += r.a;
+                if (!real || v + q >= rows) g[q] = 0.0f;
+            }
+            if (p.slope)
+                store_pack<4>(static_cast<T *>(p.slope) + uint64_t(n) * p.piece + v, narrow_pack<T>(g));
+            if (p.slope_turned)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    static_cast<T *>(p.slope_turned)[uint64_t(v + q) * p.n_pad + n] = narrow<T>(g[q] * ratio);
+        }
+    }
+}
+
+// The piece's share of dh = g w, over a split of its classes.
+template <typename T, typename Tile>
+__global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_hidden(HeadArgs p) {
+    __shared__ __attribute__((aligned(1024))) typename Tile::Buffer even, odd;
+    const uint32_t count = *p.count, tiles_n = (count + Tile::BN - 1) / Tile::BN;
+    const uint32_t tiles_m = (p.width + Tile::BM - 1) / Tile::BM;
+    if (blockIdx.x >= uint64_t(tiles_m) * tiles_n) return;
+    const TilePlace at = tile_place(blockIdx.x, tiles_m, tiles_n);
+    const uint64_t stride = uint64_t(p.piece) * sizeof(T);
+    const uint32_t all = p.piece / kStep<T>;
+    Tile tile;
+    tile.run({static_cast<const char *>(p.weight_turned), stride, p.width, 0}, at.m * Tile::BM,
+             {static_cast<const char *>(p.slope), stride, p.n_pad, 0}, at.n * Tile::BN,
+             min(all, blockIdx.y * p.steps), min(all, (blockIdx.y + 1) * p.steps), even, odd);
+#pragma unroll
+    for (int j = 0; j < Tile::TN; ++j) {
+        const uint32_t n = at.n * Tile::BN + tile.column(j);
+        float *to = p.sum + (uint64_t(blockIdx.y) * p.n_pad + n) * p.sum_stride;
+        if (n >= count) continue;
+#pragma unroll
+        for (int i = 0; i < Tile::TM; ++i) {
+            const uint32_t d = at.m * Tile::BM + tile.row(i);
+            if (d >= p.sum_stride) continue;
+            f32x4 *q = reinterpret_cast<f32x4 *>(to + d);
+            *q = p.add ? *q + tile.acc[i][j] : tile.acc[i][j];
+        }
+    }
+}
+
+// dh of every row from the splits' sums; rows that took no part get zeros.
+template <typename T>
+__global__ __launch_bounds__(256) void k_head_hidden_join(HeadArgs p) {
+    const uint32_t quads = (p.width + 3) / 4;
+    const uint64_t total = uint64_t(p.n) * quads;
+    for (uint64_t i = uint64_t(blockIdx.x) * 256 + threadIdx.x; i < total; i += uint64_t(gridDim.x) * 256) {
+        const uint32_t n = uint32_t(i / quads), d = uint32_t(i % quads) * 4;
+        const int32_t at = p.place[n];
+        float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (at >= 0) {
+            for (uint32_t s = 0; s < p.splits; ++s) {
+                const f32x4 x = *reinterpret_cast<const f32x4 *>(p.sum + (uint64_t(s) * p.n_pad + at) * p.sum_stride + d);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) v[q] += x[q];
+            }
+            if (p.inverse) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) v[q] *= p.inverse[at];
+            }
+        }
+        store_pack<4>(static_cast<T *>(p.grad_hidden) + uint64_t(n) * p.width + d, narrow_pack<T>(v), p.width - d);
+    }
+}
+
+// The piece's rows of dw = g^T h.
+template <typename T, typename Tile>
+__global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_weight(HeadArgs p) {
+    __shared__ __attribute__((aligned(1024))) typename Tile::Buffer even, odd;
+    const uint32_t count = *p.count, rows = min(p.piece, p.classes - p.first);
+    const uint32_t tiles_m = (p.width + Tile::BM - 1) / Tile::BM, tiles_n = (rows + Tile::BN - 1) / Tile::BN;
+    const TilePlace at = tile_place(blockIdx.x, tiles_m, tiles_n);
+    const uint64_t stride = uint64_t(p.n_pad) * sizeof(T);
+    Tile tile;
+    tile.run({static_cast<const char *>(p.turned), stride, p.width, 0}, at.m * Tile::BM,
+             {static_cast<const char *>(p.slope_turned), stride, p.piece, 0}, at.n * Tile::BN, 0,
+             (count + kStep<T> - 1) / kStep<T>, even, odd);
+    const float back = p.inverse ? p.inverse[p.n_pad] : 1.0f;
+#pragma unroll
+    for (int j = 0; j < Tile::TN; ++j) {
+        const uint32_t v = at.n * Tile::BN + tile.column(j);
+        if (v >= rows) continue;
+        T *to = static_cast<T *>(p.grad_weight) + uint64_t(p.first + v) * p.width;
+#pragma unroll
+        for (int i = 0; i < Tile::TM; ++i) {
+            const uint32_t d = at.m * Tile::BM + tile.row(i);
+            if (d >= p.width) continue;
+            float x[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) x[q] = tile.acc[i][j][q] * back;
+            store_pack<4>(to + d, narrow_pack<T>(x), p.width - d);
+        }
+    }
+}
+
+}  // namespace tmtrain

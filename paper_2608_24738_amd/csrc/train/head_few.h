@@ -1,0 +1,182 @@
+// head_few.h -- the kernels of head.h for up to kFewRows rows, such as one new
+// token: bound by one read of the weight, which goes from memory to registers.
+#pragma once
+
+#include "head.h"
+
+namespace tmtrain {
+
+constexpr int kFewWaves = 4;
+constexpr int kFewClasses = 16 * kFewWaves;     // of a workgroup
+constexpr int kFewAhead = 8;                    // pieces of a row on their way to a lane
+
+// c h w of 16 classes from v0 on and all rows: the lane holds classes v0 + 4 g + q of row n = lane % 16.
+template <typename T>
+__device__ __forceinline__ f32x4 few_logits(const HeadArgs &p, uint32_t v0) {
+    constexpr uint32_t V = 16 / sizeof(T), kRound = 4 * V;
+    const uint32_t lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const T *w = static_cast<const T *>(p.weight) + uint64_t(min(v0 + r, p.classes - 1)) * p.weight_stride;
+    const T *h = static_cast<const T *>(p.hidden) + uint64_t(min(r, p.n - 1)) * p.hidden_stride;
+    f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    uint32_t k = g * V;
+    const auto words = [](const Pack<T, int(V)> &x) { return u32x4{x.w[0], x.w[1], x.w[2], x.w[3]}; };
+    for (; k - g * V + kFewAhead * kRound <= p.width; k += kFewAhead * kRound) {
+        Pack<T, int(V)> a[kFewAhead], b[kFewAhead];
+#pragma unroll
+        for (int i = 0; i < kFewAhead; ++i) a[i] = load_pack<int(V)>(w + k + i * kRound);
+#pragma unroll
+        for (int i = 0; i < kFewAhead; ++i) b[i] = load_pack<int(V)>(h + k + i * kRound);
+#pragma unroll
+        for (int i = 0; i < kFewAhead; ++i) acc = multiply<T>(words(a[i]), words(b[i]), acc);
+    }
+    for (; k - g * V < p.width; k += kRound) {
+        Pack<T, int(V)> a{}, b{};
+        if (k < p.width) {
+            a = load_pack<int(V)>(w + k, p.width - k, T{});
+            b = load_pack<int(V)>(h + k, p.width - k, T{});
+        }
+        acc = multiply<T>(words(a), words(b), acc);
+    }
+    return acc;
+}
+
+// Sums of 2^(c x - M) over a workgroup's classes, and c x of the labels.
+template <typename T>
+__global__ __launch_bounds__(64 * kFewWaves) void k_few_sums(HeadArgs p) {
+    __shared__ HeadSum lds[kFewWaves][kFewRows];
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15;
+    const uint32_t v0 = (blockIdx.x * kFewWaves + wave) * 16, v = v0 + (lane >> 4) * 4;
+    HeadSum sum = {kLowest, 0.0f};
+    if (v0 < p.classes) {
+        f32x4 x = few_logits<T>(p, v0);
+        const int32_t y = n < p.n && p.label ? load_label(p.label, p.label_bytes, n, p.classes) : -1;
+        if (y >= 0 && uint32_t(y) - v < 4) {
+            const uint32_t q = uint32_t(y) - v;
+            p.found[n] = q == 0 ? x[0] : q == 1 ? x[1] : q == 2 ? x[2] : x[3];
+        }
+        float most = -INFINITY;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            if (v + q >= p.classes) x[q] = -INFINITY;
+            most = fmaxf(most, x[q]);
+        }
+        most = fmaxf(most, __shfl_xor(most, 16));
+        most = fmaxf(most, __shfl_xor(most, 32));
+        sum.m = whole(most, p.c);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) sum.s += exp2_hw(fmaf(x[q], p.c, -sum.m));
+        sum.s += __shfl_xor(sum.s, 16);
+        sum.s += __shfl_xor(sum.s, 32);
+    }
+    if (lane < 16) lds[wave][n] = sum;
+    __syncthreads();
+    if (threadIdx.x >= 16) return;
+    sum = lds[0][n];
+#pragma unroll
+    for (int w = 1; w < kFewWaves; ++w) sum = join(sum, lds[w][n]);
+    p.part[uint64_t(blockIdx.x) * kFewRows + n] = sum;
+}
+
+// g in float32, [classes][kFewRows]; 0 for rows that take no part.
+template <typename T>
+__global__ __launch_bounds__(64 * kFewWaves) void k_few_slopes(HeadArgs p) {
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15;
+    const uint32_t v0 = (blockIdx.x * kFewWaves + wave) * 16, v = v0 + (lane >> 4) * 4;
+    if (v0 >= p.classes) return;
+    const f32x4 x = few_logits<T>(p, v0);
+    int32_t y = -1;
+    HeadUp u = {0.0f, 0.0f};
+    HeadSum s = {0.0f, 1.0f};
+    bool in = n < p.n;
+    if (in) {
+        y = p.label ? load_label(p.label, p.label_bytes, n, p.classes) : -1;
+        in = y >= 0 || p.all;
+        u = head_up(p, n, y);
+        s = p.stats[n];
+        in = in && s.s != 0.0f;
+    }
+    const float b = u.b / s.s;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        if (v + q >= p.classes) break;
+        float g = -b * exp2_hw(fmaf(x[q], p.c, -s.m));
+        if (int32_t(v + q) == y) g += u.a;
+        static_cast<float *>(p.slope)[uint64_t(v + q) * kFewRows + n] = in ? g : 0.0f;
+    }
+}
+
+// dw = g^T h and the workgroup's share of dh = g w: a thread has C columns, its
+// workgroup p.steps classes, which the rows of threads take in turn.  N rows of hidden states.
+template <typename T, int N, int C>
+__global__ __launch_bounds__(256) void k_few_outer(HeadArgs p) {
+    const uint32_t d = (blockIdx.y * blockDim.x + threadIdx.x) * C;
+    if (d >= p.width) return;
+    const uint32_t left = p.width - d;
+    float h[N][C], sum[N][C];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        Pack<T, C> x{};
+        // what a row that takes no part holds reaches no gradient
+        const bool in = uint32_t(n) < p.n &&
+                        (p.all || (p.label && load_label(p.label, p.label_bytes, n, p.classes) >= 0));
+        if (in && p.grad_weight)
+            x = load_pack<C>(static_cast<const T *>(p.hidden) + n * p.hidden_stride + d, left, T{});
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            h[n][i] = widen(x.at(i));
+            sum[n][i] = 0.0f;
+        }
+    }
+    const uint32_t end = min(p.classes, (blockIdx.x + 1) * p.steps);
+    for (uint32_t v = blockIdx.x * p.steps + threadIdx.y; v < end; v += blockDim.y) {
+        const float *g = static_cast<const float *>(p.slope) + uint64_t(v) * kFewRows;
+        float gv[N];
+#pragma unroll
+        for (int n = 0; n < N; ++n) gv[n] = g[n];
+        if (p.grad_hidden) {
+            const Pack<T, C> w = load_pack<C>(static_cast<const T *>(p.weight) + v * p.weight_stride + d, left, T{});
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int i = 0; i < C; ++i) sum[n][i] = fmaf(gv[n], widen(w.at(i)), sum[n][i]);
+        }
+        if (p.grad_weight) {
+            float x[C] = {};
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int i = 0; i < C; ++i) x[i] = fmaf(gv[n], h[n][i], x[i]);
+            store_pack<C>(static_cast<T *>(p.grad_weight) + uint64_t(v) * p.width + d, narrow_pack<T>(x), left);
+        }
+    }
+    if (!p.grad_hidden) return;
+    const uint32_t split = blockIdx.x * blockDim.y + threadIdx.y;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        Pack<float, C> x;
+#pragma unroll
+        for (int i = 0; i < C; ++i) x.put(i, sum[n][i]);
+        if (uint32_t(n) < p.n) store_pack<C>(p.sum + (uint64_t(split) * p.n + n) * p.sum_stride + d, x);
+    }
+}
+
+// dh from the splits: 64 columns of a row to a workgroup, splits over its 16 waves.
+template <typename T>
+__global__ __launch_bounds__(1024) void k_few_join(HeadArgs p) {
+    __shared__ float lds[16][64];
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, d = blockIdx.x * 64 + lane, n = blockIdx.y;
+    float sum = 0.0f;
+    if (d < p.width)
+#pragma unroll 8
+        for (uint32_t s = wave; s < p.splits; s += 16) sum += p.sum[(uint64_t(s) * p.n + n) * p.sum_stride + d];
+    lds[wave][lane] = sum;
+    __syncthreads();
+    if (wave || d >= p.width) return;
+#pragma unroll
+    for (int w = 1; w < 16; ++w) sum += lds[w][lane];
+    // rows that take no part: 0 x w is not 0 for every w
+    const bool in = p.all || (p.label && load_label(p.label, p.label_bytes, n, p.classes) >= 0);
+    static_cast<T *>(p.grad_hidden)[uint64_t(n) * p.width + d] = narrow<T>(in ? sum : 0.0f);
+}
+
+}  // namespace tmtrain

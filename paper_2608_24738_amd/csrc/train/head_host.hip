@@ -1,0 +1,394 @@
+// head_host.hip -- C-ABI of the log-probabilities from hidden states: argument
+// checks, layout of the workspace, choice of kernel and launches (declared in
+// include/tm_train.h).
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "head_few.h"
+#include "host_common.h"
+
+using namespace tmtrain;
+
+namespace {
+
+constexpr uint64_t kMaxWidth = uint64_t(1) << 24;
+constexpr uint64_t kPieceBytes = uint64_t(1) << 27;     // of one layout of g
+constexpr uint64_t kLaidBytes = uint64_t(1) << 28;      // of weights laid out in whole steps
+constexpr uint64_t kCus = 256;
+
+struct HeadShape {
+    uint64_t n, classes, width, size;
+    uint64_t hidden_bytes, weight_bytes, label_bytes;
+};
+
+// Bytes from a matrix's first to the end of its last element, or 0 if it is too long to address.
+uint64_t matrix_bytes(uint64_t rows, uint64_t width, uint64_t stride, uint64_t size) {
+    if (rows > 1 && stride > (uint64_t(1) << 56) / rows) return 0;
+    return ((rows - 1) * stride + width) * size;
+}
+
+int check_head(const void *hidden, int dtype, int64_t rows, int64_t classes, int64_t width, int64_t hidden_stride,
+               const void *weight, int64_t weight_stride, int label_dtype, const void *labels, double scale,
+               HeadShape &s) {
+    if (rows < 0 || classes < 1 || width < 1 || hidden_stride < 0 || weight_stride < 0) return TM_ERR_SHAPE;
+    if (!float_type(dtype)) return TM_ERR_DTYPE;
+    if (labels && label_dtype != TM_DTYPE_U8 && label_dtype != TM_DTYPE_I32 && label_dtype != TM_DTYPE_I64)
+        return TM_ERR_DTYPE;
+    if (!std::isfinite(scale) || !std::isfinite(float(scale) * kLog2e) || !(float(scale) > FLT_MIN))
+        return TM_ERR_SAMPLING;
+    if (uint64_t(rows) >= kLimit - kTilePad || uint64_t(classes) >= kLimit - kTilePad || uint64_t(width) > kMaxWidth)
+        return TM_ERR_TOO_LARGE;
+    s.n = uint64_t(rows);
+    s.classes = uint64_t(classes);
+    s.width = uint64_t(width);
+    s.size = float_bytes(dtype);
+    // workgroups of the smaller tiles
+    if (ceil_div(s.n, 128) * ceil_div(s.classes, 128) >= kLimit) return TM_ERR_TOO_LARGE;
+    s.label_bytes = label_dtype == TM_DTYPE_U8 ? 1 : label_dtype == TM_DTYPE_I32 ? 4 : 8;
+    if (s.n == 0) return TM_OK;
+    if (!hidden || !weight) return TM_ERR_NULL;
+    s.hidden_bytes = matrix_bytes(s.n, s.width, uint64_t(hidden_stride), s.size);
+    s.weight_bytes = matrix_bytes(s.classes, s.width, uint64_t(weight_stride), s.size);
+    return s.hidden_bytes && s.weight_bytes ? TM_OK : TM_ERR_TOO_LARGE;
+}
+
+// A workspace, handed out front to back.
+struct Room {
+    char *at;
+    uint64_t used;
+    template <typename T>
+    T *take(uint64_t count) {
+        T *p = at ? reinterpret_cast<T *>(at + used) : nullptr;
+        used += ceil_div(count * sizeof(T), 256) * 256;
+        return p;
+    }
+};
+
+uint64_t whole_tiles(uint64_t n) { return ceil_div(n, kTilePad) * kTilePad; }
+
+bool few(const HeadShape &s) { return s.n <= kFewRows; }
+
+// Largest tiles, unless they leave CUs without one.
+bool large_tiles(uint64_t m, uint64_t n) { return ceil_div(m, 256) * ceil_div(n, 256) >= kCus; }
+
+// Tiles read whole 16-byte pieces of the weight, from addresses of 16 bytes.
+bool lies_well(const void *p, uint64_t stride, const HeadShape &s) {
+    return uintptr_t(p) % 16 == 0 && stride * s.size % 16 == 0 && s.width * s.size % 16 == 0;
+}
+
+// Classes of a piece, in whole tiles, so that `bytes` hold a row of `each` for every class.
+uint64_t piece_of(uint64_t classes, uint64_t each, uint64_t bytes) {
+    const uint64_t most = std::max<uint64_t>(kTilePad, bytes / each / kTilePad * kTilePad);
+    return whole_tiles(ceil_div(classes, ceil_div(classes, most)));
+}
+
+void head_sizes(const HeadShape &s, HeadArgs &a) {
+    a.n = uint32_t(s.n);
+    a.classes = uint32_t(s.classes);
+    a.width = uint32_t(s.width);
+    const uint64_t step = kStepBytes / s.size;
+    a.width_pad = uint32_t(ceil_div(s.width, step) * step);
+    a.n_pad = uint32_t(few(s) ? kFewRows : whole_tiles(s.n));
+}
+
+// Layout of the forward call's workspace; returns its size.
+uint64_t head_room(const HeadShape &s, bool laid, void *at, HeadArgs &a) {
+    Room room{static_cast<char *>(at), 0};
+    head_sizes(s, a);
+    a.found = room.take<float>(a.n_pad);
+    if (few(s)) {
+        a.parts = uint32_t(ceil_div(s.classes, kFewClasses));
+        a.part = room.take<HeadSum>(uint64_t(a.parts) * kFewRows);
+        return room.used;
+    }
+    const bool large = large_tiles(s.classes, s.n);
+    a.parts = uint32_t(ceil_div(s.classes, large ? 256 : 128) * 2);
+    a.piece = uint32_t(laid ? piece_of(s.classes, a.width_pad * s.size, kLaidBytes) : whole_tiles(s.classes));
+    a.count = room.take<uint32_t>(1);
+    a.chunk_count = room.take<uint32_t>(2 * ceil_div(s.n, kListChunk));
+    a.list = room.take<uint32_t>(a.n_pad);
+    a.packed = room.take<char>(uint64_t(a.n_pad) * a.width_pad * s.size);
+    a.part = room.take<HeadSum>(uint64_t(a.parts) * a.n_pad);
+    if (laid) a.weight_laid = room.take<char>(uint64_t(a.piece) * a.width_pad * s.size);
+    return room.used;
+}
+
+// Classes of a workgroup of k_few_outer.
+uint64_t few_share(const HeadShape &s) { return std::max<uint64_t>(16, ceil_div(s.classes, 256)); }
+// Columns of a thread of k_few_outer: what its registers hold of n rows, twice in float32.
+uint32_t few_columns(const HeadShape &s) { return s.n > 4 || s.size == 4 ? 4 : 8; }
+// and its block: as many threads as a row needs, up to 256, the rest for other classes.
+dim3 few_block(const HeadShape &s) {
+    const uint32_t x = std::min<uint32_t>(256, std::max<uint32_t>(16, pow2_from(uint32_t(ceil_div(s.width, few_columns(s))))));
+    return dim3(x, 256 / x);
+}
+
+// Layout of the gradient's workspace.
+uint64_t head_grad_room(const HeadShape &s, int dtype, bool laid, bool hidden, bool weight, void *at, HeadArgs &a) {
+    Room room{static_cast<char *>(at), 0};
+    head_sizes(s, a);
+    if (few(s)) {
+        a.sum_stride = uint32_t(ceil_div(s.width, 8) * 8);
+        a.steps = uint32_t(few_share(s));
+        a.splits = uint32_t(ceil_div(s.classes, a.steps) * few_block(s).y);
+        a.slope = room.take<float>(s.classes * kFewRows);
+        if (hidden) a.sum = room.take<float>(uint64_t(a.splits) * s.n * a.sum_stride);
+        return room.used;
+    }
+    a.piece = uint32_t(piece_of(s.classes, a.n_pad * s.size, kPieceBytes));
+    a.sum_stride = uint32_t(ceil_div(s.width, 4) * 4);
+    const bool large = large_tiles(s.width, s.n);
+    const uint64_t tiles = ceil_div(s.width, large ? 256 : 128) * ceil_div(s.n, large ? 256 : 128);
+    // splits that give every CU a tile (two of the small ones), each of 8 steps at least
+    const uint64_t steps = a.piece * s.size / kStepBytes, slots = large ? kCus : 2 * kCus;
+    const uint64_t splits = std::max<uint64_t>(1, std::min<uint64_t>({slots / tiles, steps / 8, 32}));
+    a.steps = uint32_t(ceil_div(steps, splits));
+    a.splits = uint32_t(ceil_div(steps, a.steps));
+    a.count = room.take<uint32_t>(1);
+    a.chunk_count = room.take<uint32_t>(2 * ceil_div(s.n, kListChunk));
+    a.list = room.take<uint32_t>(a.n_pad);
+    a.place = room.take<int32_t>(a.n_pad);
+    a.row = room.take<HeadRow>(a.n_pad);
+    if (dtype == TM_DTYPE_F16) a.inverse = room.take<float>(a.n_pad + 1);
+    a.packed = room.take<char>(uint64_t(a.n_pad) * a.width_pad * s.size);
+    if (weight) {
+        a.turned = room.take<char>(uint64_t(a.n_pad) * s.width * s.size);
+        a.slope_turned = room.take<char>(uint64_t(a.n_pad) * a.piece * s.size);
+    }
+    if (hidden) {
+        a.slope = room.take<char>(uint64_t(a.n_pad) * a.piece * s.size);
+        a.weight_turned = room.take<char>(s.width * a.piece * s.size);
+        a.sum = room.take<float>(uint64_t(a.splits) * a.n_pad * a.sum_stride);
+    }
+    if (laid) a.weight_laid = room.take<char>(uint64_t(a.piece) * a.width_pad * s.size);
+    return room.used;
+}
+
+// fn(tile) of the tile that m x n elements take.
+template <typename T, typename F>
+int by_tile(uint64_t m, uint64_t n, F fn) {
+    return large_tiles(m, n) ? fn(static_cast<LargeTile<T> *>(nullptr)) : fn(static_cast<SmallTile<T> *>(nullptr));
+}
+
+template <typename Tile>
+dim3 tile_grid(uint64_t m, uint64_t n) {
+    return dim3(uint32_t(ceil_div(m, Tile::BM) * ceil_div(n, Tile::BN)));
+}
+
+// The list of packed rows and the rows themselves, packed and turned.
+template <typename T>
+int pack_rows(const HeadArgs &a, hipStream_t stream) {
+    const uint32_t chunks = uint32_t(ceil_div(a.n, kListChunk));
+    int rc = TM_OK;
+    if (chunks > 1) rc = launch(k_head_count, dim3(chunks), dim3(1024), 0, stream, a);
+    if (rc == TM_OK) rc = launch(k_head_list, dim3(chunks), dim3(1024), 0, stream, a);
+    if (rc != TM_OK) return rc;
+    LayArgs lay{};
+    lay.from = a.hidden;
+    lay.stride = a.hidden_stride;
+    lay.list = a.list;
+    lay.count = a.count;
+    lay.rows = a.n;
+    lay.width = a.width;
+    lay.to = a.packed;
+    lay.to_stride = a.width_pad;
+    rc = launch(k_lay_rows<T>, dim3(std::min(a.n, 4096u)), dim3(256), 0, stream, lay);
+    if (rc != TM_OK || !a.turned) return rc;
+    lay.to = a.turned;
+    lay.to_stride = a.n_pad;
+    return launch(k_turn_rows<T>, dim3(a.n_pad / 64, uint32_t(ceil_div(a.width, 64))), dim3(256), 0, stream, lay);
+}
+
+// The weights of the piece at hand in whole steps.
+template <typename T>
+int lay_piece(const HeadArgs &a, hipStream_t stream) {
+    LayArgs lay{};
+    lay.from = static_cast<const T *>(a.weight) + uint64_t(a.first) * a.weight_stride;
+    lay.stride = a.weight_stride;
+    lay.rows = std::min(a.piece, a.classes - a.first);
+    lay.width = a.width;
+    lay.to = a.weight_laid;
+    lay.to_stride = a.width_pad;
+    return launch(k_lay_rows<T>, dim3(std::min(lay.rows, 4096u)), dim3(256), 0, stream, lay);
+}
+
+// and turned.
+template <typename T>
+int turn_piece(const HeadArgs &a, hipStream_t stream) {
+    LayArgs lay{};
+    lay.from = static_cast<const T *>(a.weight) + uint64_t(a.first) * a.weight_stride;
+    lay.stride = a.weight_stride;
+    lay.rows = std::min(a.piece, a.classes - a.first);
+    lay.width = a.width;
+    lay.fill = a.piece;
+    lay.to = a.weight_turned;
+    lay.to_stride = a.piece;
+    return launch(k_turn_rows<T>, dim3(a.piece / 64, uint32_t(ceil_div(a.width, 64))), dim3(256), 0, stream, lay);
+}
+
+template <typename T>
+int run_head(HeadArgs a, const HeadShape &s, hipStream_t stream) {
+    if (few(s)) {
+        const int rc = launch(k_few_sums<T>, dim3(a.parts), dim3(64 * kFewWaves), 0, stream, a);
+        return rc == TM_OK ? launch(k_head_join, dim3(1), dim3(1024), 0, stream, a) : rc;
+    }
+    int rc = pack_rows<T>(a, stream);
+    for (uint64_t first = 0; rc == TM_OK && first < s.classes; first += a.piece) {
+        a.first = uint32_t(first);
+        if (a.weight_laid) rc = lay_piece<T>(a, stream);
+        if (rc != TM_OK) break;
+        // the tile is that of all classes: it says how many parts there are
+        rc = by_tile<T>(s.classes, s.n, [&](auto *t) {
+            using Tile = std::remove_pointer_t<decltype(t)>;
+            return launch(k_head_sums<T, Tile>, tile_grid<Tile>(std::min<uint64_t>(a.piece, s.classes - first), s.n),
+                          dim3(Tile::kThreads), 0, stream, a);
+        });
+    }
+    return rc == TM_OK ? launch(k_head_join, dim3(uint32_t(ceil_div(s.n, 64))), dim3(1024), 0, stream, a) : rc;
+}
+
+template <typename T>
+int run_few_grad(const HeadArgs &a, const HeadShape &s, hipStream_t stream) {
+    int rc = launch(k_few_slopes<T>, dim3(uint32_t(ceil_div(s.classes, kFewClasses))), dim3(64 * kFewWaves), 0, stream, a);
+    if (rc != TM_OK) return rc;
+    const dim3 block = few_block(s);
+    const dim3 grid(uint32_t(ceil_div(s.classes, a.steps)), uint32_t(ceil_div(s.width, block.x * few_columns(s))));
+    constexpr int C = sizeof(T) == 4 ? 4 : 8;
+    rc = launch(s.n == 1 ? k_few_outer<T, 1, C> : s.n <= 4 ? k_few_outer<T, 4, C> : k_few_outer<T, 16, 4>, grid, block,
+                0, stream, a);
+    if (rc != TM_OK || !a.grad_hidden) return rc;
+    return launch(k_few_join<T>, dim3(uint32_t(ceil_div(s.width, 64)), a.n), dim3(1024), 0, stream, a);
+}
+
+template <typename T>
+int run_head_grad(HeadArgs a, const HeadShape &s, hipStream_t stream) {
+    if (few(s)) return run_few_grad<T>(a, s, stream);
+    int rc = pack_rows<T>(a, stream);
+    for (uint64_t first = 0; rc == TM_OK && first < s.classes; first += a.piece) {
+        a.first = uint32_t(first);
+        a.add = first > 0;
+        if (a.weight_laid) rc = lay_piece<T>(a, stream);
+        if (rc != TM_OK) break;
+        rc = by_tile<T>(a.piece, s.n, [&](auto *t) {
+            using Tile = std::remove_pointer_t<decltype(t)>;
+            return launch(k_head_slopes<T, Tile>, tile_grid<Tile>(a.piece, s.n), dim3(Tile::kThreads), 0, stream, a);
+        });
+        if (rc == TM_OK && a.grad_hidden) {
+            rc = turn_piece<T>(a, stream);
+            if (rc != TM_OK) break;
+            rc = by_tile<T>(s.width, s.n, [&](auto *t) {
+                using Tile = std::remove_pointer_t<decltype(t)>;
+                return launch(k_head_hidden<T, Tile>, dim3(tile_grid<Tile>(s.width, s.n).x, a.splits),
+                              dim3(Tile::kThreads), 0, stream, a);
+            });
+        }
+        if (rc == TM_OK && a.grad_weight) {
+            const uint64_t rows = std::min<uint64_t>(a.piece, s.classes - first);
+            rc = by_tile<T>(s.width, rows, [&](auto *t) {
+                using Tile = std::remove_pointer_t<decltype(t)>;
+                return launch(k_head_weight<T, Tile>, tile_grid<Tile>(s.width, rows), dim3(Tile::kThreads), 0, stream, a);
+            });
+        }
+    }
+    if (rc != TM_OK || !a.grad_hidden) return rc;
+    const uint64_t blocks = ceil_div(s.n * ceil_div(s.width, 4), 256);
+    return launch(k_head_hidden_join<T>, dim3(uint32_t(std::min<uint64_t>(blocks, 4096))), dim3(256), 0, stream, a);
+}
+
+void head_args(const HeadShape &s, const void *hidden, int64_t hidden_stride, const void *weight, int64_t weight_stride,
+               const void *labels, double scale, HeadArgs &a) {
+    a.hidden = hidden;
+    a.hidden_stride = uint64_t(hidden_stride);
+    a.weight = weight;
+    a.weight_stride = uint64_t(weight_stride);
+    a.label = labels;
+    a.label_bytes = int32_t(s.label_bytes);
+    a.scale = float(scale);
+    a.c = float(double(float(scale)) * 1.4426950408889634);
+}
+
+}  // namespace
+
+extern "C" size_t tm_head_logp_workspace_size(int dtype, int64_t rows, int64_t classes, int64_t width) {
+    HeadShape s{};
+    HeadArgs a{};
+    const void *some = reinterpret_cast<const void *>(uintptr_t(4096));
+    if (check_head(some, dtype, rows, classes, width, 0, some, 0, 0, nullptr, 1.0, s) != TM_OK || s.n == 0) return 0;
+    return std::max(head_room(s, true, nullptr, a), head_room(s, false, nullptr, a));
+}
+
+extern "C" int tm_head_logp(const void *hidden, int dtype, int64_t rows, int64_t classes, int64_t width,
+                            int64_t hidden_stride, const void *weight, int64_t weight_stride, const void *labels,
+                            int label_dtype, double scale, float *out_logp, float *out_log_sum, float *out_stats,
+                            void *workspace, size_t workspace_bytes, hipStream_t stream) {
+    HeadShape s{};
+    const int rc = check_head(hidden, dtype, rows, classes, width, hidden_stride, weight, weight_stride, label_dtype,
+                              labels, scale, s);
+    if (rc != TM_OK) return rc;
+    if (s.n == 0) return TM_OK;
+    if (!labels && (out_logp || !out_log_sum)) return TM_ERR_NULL;
+    if (!out_logp && !out_log_sum) return TM_ERR_NO_OUTPUT;
+    const size_t need = tm_head_logp_workspace_size(dtype, rows, classes, width);
+    if (!workspace || workspace_bytes < need || uintptr_t(workspace) % 16) return TM_ERR_WORKSPACE;
+    const Range in[] = {{hidden, s.hidden_bytes}, {weight, s.weight_bytes}, {labels, s.n * s.label_bytes}};
+    const Range out[] = {{out_logp, s.n * 4}, {out_log_sum, s.n * 4}, {out_stats, s.n * 8}, {workspace, need}};
+    if (aliased(in, out)) return TM_ERR_ALIAS;
+    HeadArgs a{};
+    head_args(s, hidden, hidden_stride, weight, weight_stride, labels, scale, a);
+    head_room(s, !few(s) && !lies_well(weight, a.weight_stride, s), workspace, a);
+    a.all = out_log_sum != nullptr;
+    a.logp = out_logp;
+    a.log_sum = out_log_sum;
+    a.stats = reinterpret_cast<HeadSum *>(out_stats);
+    return by_type(dtype, [&](auto t) { return run_head<decltype(t)>(a, s, stream); });
+}
+
+extern "C" size_t tm_head_logp_grad_workspace_size(int dtype, int64_t rows, int64_t classes, int64_t width, int hidden,
+                                                   int weight) {
+    HeadShape s{};
+    HeadArgs a{};
+    const void *some = reinterpret_cast<const void *>(uintptr_t(4096));
+    if (check_head(some, dtype, rows, classes, width, 0, some, 0, 0, nullptr, 1.0, s) != TM_OK || s.n == 0) return 0;
+    return head_grad_room(s, dtype, true, hidden != 0, weight != 0, nullptr, a);
+}
+
+extern "C" int tm_head_logp_grad(const void *hidden, int dtype, int64_t rows, int64_t classes, int64_t width,
+                                 int64_t hidden_stride, const void *weight, int64_t weight_stride, const void *labels,
+                                 int label_dtype, double scale, const float *stats, const float *up_logp,
+                                 const float *up_log_sum, void *out_hidden, void *out_weight, void *workspace,
+                                 size_t workspace_bytes, hipStream_t stream) {
+    HeadShape s{};
+    const int rc = check_head(hidden, dtype, rows, classes, width, hidden_stride, weight, weight_stride, label_dtype,
+                              labels, scale, s);
+    if (rc != TM_OK) return rc;
+    if (s.n == 0 && !out_weight) return TM_OK;
+    if (!out_hidden && !out_weight) return TM_ERR_NO_OUTPUT;
+    if (s.n && ((!up_logp && !up_log_sum) || (up_logp && !labels) || !stats)) return TM_ERR_NULL;
+    const uint64_t grad_bytes = s.classes * s.width * s.size;
+    const size_t need = tm_head_logp_grad_workspace_size(dtype, rows, classes, width, out_hidden != nullptr,
+                                                         out_weight != nullptr);
+    if (need && (!workspace || workspace_bytes < need || uintptr_t(workspace) % 16)) return TM_ERR_WORKSPACE;
+    const Range in[] = {{hidden, s.hidden_bytes}, {weight, s.weight_bytes}, {labels, s.n * s.label_bytes},
+                        {stats, s.n * 8}, {up_logp, s.n * 4}, {up_log_sum, s.n * 4}};
+    const Range out[] = {{out_hidden, s.n * s.width * s.size}, {out_weight, grad_bytes}, {need ? workspace : nullptr, need}};
+    if (aliased(in, out)) return TM_ERR_ALIAS;
+    if (s.n == 0) {
+        FillArgs f{out_weight, grad_bytes};
+        return launch(k_fill_zeros<256>, dim3(uint32_t(std::min<uint64_t>(4 * kFill, ceil_div(grad_bytes, 4096)))), dim3(256), 0,
+                      stream, f);
+    }
+    HeadArgs a{};
+    head_args(s, hidden, hidden_stride, weight, weight_stride, labels, scale, a);
+    head_grad_room(s, dtype, !few(s) && !lies_well(weight, a.weight_stride, s), out_hidden != nullptr,
+                   out_weight != nullptr, workspace, a);
+    a.all = up_log_sum != nullptr;
+    a.stats = reinterpret_cast<HeadSum *>(const_cast<float *>(stats));
+    a.up_logp = up_logp;
+    a.up_log_sum = up_log_sum;
+    a.grad_hidden = out_hidden;
+    a.grad_weight = out_weight;
+    return by_type(dtype, [&](auto t) { return run_head_grad<decltype(t)>(a, s, stream); });
+}

@@ -262,4 +262,17 @@ __device__ __forceinline__ uint64_t wave_max(uint64_t x) {
     return uint64_t(hi) << 32 | lo;
 }
 
+// Zeros, to any address.
+struct FillArgs {
+    void *to;
+    uint64_t bytes;
+};
+template <int Threads>
+__global__ __launch_bounds__(Threads) void k_fill_zeros(FillArgs p) {
+    char *to = static_cast<char *>(p.to);
+    const uint64_t step = uint64_t(gridDim.x) * Threads * 16;
+    for (uint64_t i = (uint64_t(blockIdx.x) * Threads + threadIdx.x) * 16; i < p.bytes; i += step)
+        store_pack<16>(reinterpret_cast<uint8_t *>(to + i), Pack<uint8_t, 16>{}, uint32_t(p.bytes - i < 16 ? p.bytes - i : 16));
+}
+
 }  // namespace tmtrain

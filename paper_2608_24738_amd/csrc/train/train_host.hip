@@ -6,63 +6,14 @@
 #include <algorithm>
 #include <cmath>
 
-#include "../../../include/tm_train.h"
 #include "bias.h"
+#include "host_common.h"
 #include "label_maps.h"
 #include "label_rows.h"
 
 using namespace tmtrain;
 
 namespace {
-
-constexpr uint64_t kLimit = uint64_t(1) << 31;
-
-bool float_type(int dtype) { return dtype == TM_DTYPE_F32 || dtype == TM_DTYPE_F16 || dtype == TM_DTYPE_BF16; }
-uint64_t float_bytes(int dtype) { return dtype == TM_DTYPE_F32 ? 4 : 2; }
-
-constexpr uint64_t kFill = 1024;            // workgroups that keep the chip busy
-
-uint32_t pow2_from(uint32_t n) {
-    uint32_t p = 1;
-    while (p < n) p <<= 1;
-    return p;
-}
-uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
-
-struct Range {
-    const void *at;
-    uint64_t bytes;
-};
-bool meet(const Range &a, const Range &b) {
-    if (!a.at || !b.at || !a.bytes || !b.bytes) return false;
-    const uintptr_t x = uintptr_t(a.at), y = uintptr_t(b.at);
-    return x < y + b.bytes && y < x + a.bytes;
-}
-// No output may overlap an input or another output.
-template <int NI, int NO>
-bool aliased(const Range (&in)[NI], const Range (&out)[NO]) {
-    for (int o = 0; o < NO; ++o) {
-        for (int i = 0; i < NI; ++i)
-            if (meet(out[o], in[i])) return true;
-        for (int p = 0; p < o; ++p)
-            if (meet(out[o], out[p])) return true;
-    }
-    return false;
-}
-
-template <typename Args>
-int launch(void (*kernel)(Args), dim3 grid, dim3 block, size_t lds, hipStream_t s, const Args &args) {
-    hipLaunchKernelGGL(kernel, grid, block, lds, s, args);
-    return hipGetLastError() == hipSuccess ? TM_OK : TM_ERR_HIP;
-}
-
-// fn(T{}) with T the storage type of dtype.
-template <typename F>
-int by_type(int dtype, F fn) {
-    if (dtype == TM_DTYPE_F32) return fn(float{});
-    if (dtype == TM_DTYPE_BF16) return fn(bf16{});
-    return fn(f16{});
-}
 
 // fn(entropy, field) of the parts asked for; a field brings the entropy along.
 template <typename F>
@@ -212,12 +163,6 @@ LabelPlan label_plan(int dtype, uint64_t outer, uint64_t classes, uint64_t inner
     const uint64_t threads = out * ceil_div(in, p.wide);
     p.waves = uint32_t(std::max<uint64_t>(1, std::min<uint64_t>({kRunWaves, 3 * kBusyThreads / threads, classes / 16})));
     return p;
-}
-
-// At least `blocks` < 2^31 workgroups, of up to 1024 threads.
-dim3 row_grid(uint32_t blocks) {
-    const uint32_t x = std::min<uint32_t>(blocks, 1u << 21);
-    return dim3(x, uint32_t(ceil_div(blocks, x)));
 }
 
 template <typename Args>

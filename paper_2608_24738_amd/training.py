@@ -475,3 +475,149 @@ def relative_bias(table: torch.Tensor, edges: torch.Tensor, query_shape, key_sha
             raise ValueError("add must have shape (..., %d, %d, %d), got %s" % (tail + (shape,)))
         batch = math.prod(shape[:-3])
     return _run_bias(table, edges, add, ("tm_relative_bias", args + (batch,), None), shape)
+
+
+class HeadLogProbs(NamedTuple):
+    """What ``head_log_probs`` gives; None for what was not asked for."""
+    log_probs: Optional[torch.Tensor]
+    log_sums: Optional[torch.Tensor]
+
+
+def _rows(t):
+    """(tensor, rows, stride between them): ``t`` (..., width) as rows whose
+    elements lie side by side, or a contiguous copy of it where it is none."""
+    shape, strides = t.shape, t.stride()
+    width = shape[-1]
+    if 0 in shape:
+        return t, math.prod(shape[:-1]), width
+    outer = _collapse(shape[:-1], strides[:-1]) if strides[-1] == 1 or width == 1 else None
+    if outer is None:
+        return t.contiguous(), math.prod(shape[:-1]), width
+    return t, outer[0], outer[1] if outer[0] > 1 else width
+
+
+@functools.lru_cache(maxsize=1024)
+def _head_workspace(dtype, rows, classes, width):
+    return int(load().tm_head_logp_workspace_size(dtype, rows, classes, width))
+
+
+@functools.lru_cache(maxsize=1024)
+def _head_grad_workspace(dtype, rows, classes, width, hidden, weight):
+    return int(load().tm_head_logp_grad_workspace_size(dtype, rows, classes, width, hidden, weight))
+
+
+def _head_args(hidden, weight, labels, scale):
+    """(hidden, weight, what the entry points take of the inputs)."""
+    hidden, rows, hidden_stride = _rows(hidden)
+    weight, classes, weight_stride = _rows(weight)
+    return hidden, weight, (hidden.data_ptr(), FLOATS[hidden.dtype], rows, classes, weight.shape[1], hidden_stride,
+                            weight.data_ptr(), weight_stride, _ptr(labels),
+                            0 if labels is None else LABELS[labels.dtype], scale)
+
+
+def _head_forward(hidden, weight, labels, scale, log_sums, stats):
+    dev = hidden.device
+    hidden, weight, args = _head_args(hidden, weight, labels, scale)
+    shape = hidden.shape[:-1]
+    logp = torch.empty(shape, dtype=torch.float32, device=dev) if labels is not None else None
+    sums = torch.empty(shape, dtype=torch.float32, device=dev) if log_sums else None
+    kept = torch.empty(shape + (2,), dtype=torch.float32, device=dev) if stats else None
+    nbytes = _head_workspace(*args[1:5])
+    workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
+    _call("tm_head_logp", dev, None, *args, _ptr(logp), _ptr(sums), _ptr(kept), _ptr(workspace), nbytes)
+    return hidden, weight, logp, sums, kept
+
+
+class _HeadLogProbs(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, hidden, weight, labels, scale, log_sums):
+        hidden, weight, logp, sums, kept = _head_forward(hidden, weight, labels, scale, log_sums, True)
+        ctx.set_materialize_grads(False)
+        ctx.save_for_backward(hidden, weight, labels, kept)
+        ctx.what = (hidden.dtype, hidden.device, hidden.shape, weight.shape, scale,
+                    None if labels is None else labels.dtype)
+        return logp, sums
+
+    @staticmethod
+    def backward(ctx, up_logp, up_sums):
+        _once()
+        wanted = ctx.needs_input_grad[:2]
+        if (up_logp is None and up_sums is None) or not any(wanted):
+            return None, None, None, None, None
+        hidden, weight, labels, kept = ctx.saved_tensors
+        dtype, dev, shape, table, scale, label_dtype = ctx.what
+        for t, size in ((hidden, shape), (weight, table)):
+            if t.dtype is not dtype or t.device != dev or t.shape != size:
+                _changed()
+        labels = _restored(labels, label_dtype, dev, shape[:-1])
+        kept = _restored(kept, torch.float32, dev, shape[:-1] + (2,))
+        # strides are those of the tensors at hand, not the forward call's
+        hidden, weight, args = _head_args(hidden, weight, labels, scale)
+        up_logp, up_sums = _upstream(up_logp), _upstream(up_sums)
+        grad_hidden = torch.empty(shape, dtype=dtype, device=dev) if wanted[0] else None
+        grad_weight = torch.empty(table, dtype=dtype, device=dev) if wanted[1] else None
+        nbytes = _head_grad_workspace(*args[1:5], *(int(w) for w in wanted))
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
+        _call("tm_head_logp_grad", dev, None, *args, kept.data_ptr(), _ptr(up_logp), _ptr(up_sums),
+              _ptr(grad_hidden), _ptr(grad_weight), _ptr(workspace), nbytes)
+        return grad_hidden, grad_weight, None, None, None
+
+
+def head_log_probs(hidden: torch.Tensor, weight: torch.Tensor, labels: Optional[torch.Tensor] = None, *,
+                   scale: float = 1.0, log_sums: bool = False) -> HeadLogProbs:
+    """Log-probabilities of given labels under the softmax of the logits
+    ``scale * hidden @ weight.T``, which are never kept: ``label_log_probs`` for
+    a large vocabulary, with the product in front of it.
+
+    ``hidden``  (..., width) float32, float16 or bfloat16.
+    ``weight``  (classes, width) of the same type.
+    ``labels``  (...); uint8, bool, int32 or int64.  A label outside [0, classes)
+                marks a row without one: log-probability 0, and whatever the row
+                holds reaches no gradient; unless ``log_sums`` are asked for, no
+                work is done for it.  None: no ``log_probs``.
+    ``scale``   positive factor of the logits, such as one over a temperature.
+    ``log_sums``  also the log of the sum of each row's exponentials.
+
+    Results are float32.  Gradients flow to ``hidden`` and ``weight`` from both
+    results.  For more than 16 rows the logits' gradient is rounded to the
+    operands' type before its two products, which are summed in float32.
+    """
+    if not hidden.is_cuda:
+        raise ValueError("hidden must be a ROCm (cuda) tensor")
+    if hidden.dtype not in FLOATS:
+        raise TypeError("hidden must be float32, float16 or bfloat16, got %s" % hidden.dtype)
+    if hidden.dim() < 1 or weight.dim() != 2 or weight.shape[0] < 1 or weight.shape[1] < 1:
+        raise ValueError("hidden must be (..., width) and weight (classes, width), got %s and %s"
+                         % (tuple(hidden.shape), tuple(weight.shape)))
+    if weight.dtype != hidden.dtype:
+        raise TypeError("weight must be %s as the hidden states are, got %s" % (hidden.dtype, weight.dtype))
+    if weight.device != hidden.device:
+        raise ValueError("weight is on %s, the hidden states on %s" % (weight.device, hidden.device))
+    if weight.shape[1] != hidden.shape[-1]:
+        raise ValueError("hidden states of width %d do not fit a weight of width %d"
+                         % (hidden.shape[-1], weight.shape[1]))
+    labels = _check_tokens(labels, "labels", hidden.device, hidden.shape[:-1])
+    scale, log_sums = float(scale), bool(log_sums)
+    if not 2.0 ** -126 < scale < math.inf:
+        raise ValueError("scale must be positive and finite, got %r" % scale)
+    if labels is None and not log_sums:
+        raise ValueError("nothing to compute: give labels or ask for log_sums")
+    _reverse_only(hidden, weight)
+    if torch.is_grad_enabled() and (hidden.requires_grad or weight.requires_grad):
+        return HeadLogProbs(*_HeadLogProbs.apply(hidden, weight, labels, scale, log_sums))
+    return HeadLogProbs(*_head_forward(hidden, weight, labels, scale, log_sums, False)[2:4])
+
+
+def _check_tokens(tokens, what, device, shape=None):
+    """Whole numbers that name rows of a table, contiguous."""
+    if tokens is None:
+        return None
+    if tokens.device != device:
+        raise ValueError("%s are on %s, not on %s" % (what, tokens.device, device))
+    if tokens.dtype == torch.bool:
+        tokens = tokens.contiguous().view(torch.uint8)
+    if tokens.dtype not in LABELS:
+        raise TypeError("%s must be uint8, bool, int32 or int64, got %s" % (what, tokens.dtype))
+    if shape is not None and tokens.shape != shape:
+        raise ValueError("%s of shape %s do not fit rows of shape %s" % (what, tuple(tokens.shape), tuple(shape)))
+    return tokens.contiguous()

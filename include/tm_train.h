@@ -1,9 +1,11 @@
 /*
  * tm_train.h -- the operators of a training step on distances, on AMD MI355X
  * (gfx950): log-probabilities of given labels with the expected distance
- * field under the softmax, and learned biases by buckets of distance, each
- * with its gradient.  Part of libtm_edt.so; status codes, metrics and element
- * types are those of tm_edt.h.
+ * field under the softmax, and learned biases by buckets of distance; and
+ * those around a vocabulary: log-probabilities from hidden states without
+ * their logits, layer norm, and rows of a table by token; each with its
+ * gradient.  Part of libtm_edt.so; status codes, metrics and element types are
+ * those of tm_edt.h.
  *
  * Conventions shared by every entry point:
  *   - Memory: pointers are DEVICE pointers owned by the caller, except shape,
@@ -228,6 +230,82 @@ int tm_head_logp_grad(const void *hidden, int dtype, int64_t rows, int64_t class
                       void *out_hidden, void *out_weight, void *workspace, size_t workspace_bytes, hipStream_t stream);
 size_t tm_head_logp_grad_workspace_size(int dtype, int64_t rows, int64_t classes, int64_t width, int hidden,
                                         int weight);
+
+/*
+ * tm_layer_norm -- the norm of each row, with mean m and r = 1 / sqrt(mean
+ * (x - m)^2 + eps) of its elements:
+ *
+ *   out[n][d] = (x[n][d] - m) r weight[d] + bias[d]
+ *
+ *   x        [rows][width] of dtype (TM_DTYPE_F32, _F16 or _BF16), rows stride
+ *            elements apart.
+ *   weight, bias  [width] of param_dtype, likewise; NULL: ones, zeros.
+ *   eps      positive and finite, rounded to float32.
+ *   out      [rows][width] contiguous of dtype, rounded once.
+ *   out_stats  [rows][2] float32, m and r for tm_layer_norm_grad, or NULL.
+ *
+ * All arithmetic is float32, the mean taken first.  A row that holds an infinity
+ * or NaN becomes NaN, and no other does.
+ * Errors: TM_ERR_SHAPE (width < 1, negative rows or stride), TM_ERR_DTYPE,
+ * TM_ERR_SAMPLING (eps), TM_ERR_TOO_LARGE (2^31 rows, more than 2^24 columns),
+ * TM_ERR_NULL, TM_ERR_NO_OUTPUT, TM_ERR_ALIAS, TM_ERR_HIP.
+ */
+int tm_layer_norm(const void *x, int dtype, int64_t rows, int64_t width, int64_t stride, const void *weight,
+                  const void *bias, int param_dtype, double eps, void *out, float *out_stats, hipStream_t stream);
+
+/*
+ * tm_layer_norm_grad -- the gradients, given that of out ([rows][width]
+ * contiguous of dtype): with t = (x - m) r and g = up weight,
+ *
+ *   out_x[n][d]   r (g - mean_d g - t mean_d (g t))   contiguous, of dtype
+ *   out_weight[d] sum_n up t,   out_bias[d] sum_n up  of param_dtype
+ *
+ * Each may be NULL, not all.  stats are what tm_layer_norm gave.  Sums are made
+ * in float32, over shares of the rows in series that are then added.
+ * workspace: at least tm_layer_norm_grad_workspace_size() bytes, 16-byte
+ * aligned, no initialisation; not used without out_weight and out_bias.
+ * Errors: as tm_layer_norm, and TM_ERR_WORKSPACE.
+ */
+int tm_layer_norm_grad(const void *x, int dtype, int64_t rows, int64_t width, int64_t stride, const void *weight,
+                       int param_dtype, const float *stats, const void *up, void *out_x, void *out_weight,
+                       void *out_bias, void *workspace, size_t workspace_bytes, hipStream_t stream);
+size_t tm_layer_norm_grad_workspace_size(int dtype, int64_t rows, int64_t width);
+
+/*
+ * tm_embedding -- scaled rows of a table by given tokens:
+ *
+ *   out[n][d] = scale * table[tokens[n]][d], zeros for a token outside [0, rows)
+ *
+ *   table    [rows][width] of dtype (TM_DTYPE_F32, _F16 or _BF16), rows stride
+ *            elements apart.
+ *   tokens   [count] contiguous, token_dtype TM_DTYPE_U8 (read unsigned), _I32
+ *            or _I64.
+ *   scale    finite, rounded to float32; the product is rounded once.
+ *   out      [count][width] contiguous of dtype.
+ * Errors: TM_ERR_SHAPE (rows or width < 1, negative count or stride),
+ * TM_ERR_DTYPE, TM_ERR_SAMPLING (scale), TM_ERR_TOO_LARGE (2^31 - 1 rows, 2^31
+ * tokens, more than 2^24 columns), TM_ERR_NULL, TM_ERR_NO_OUTPUT, TM_ERR_ALIAS,
+ * TM_ERR_HIP.
+ */
+int tm_embedding(const void *table, int dtype, int64_t rows, int64_t width, int64_t stride, const void *tokens,
+                 int token_dtype, int64_t count, double scale, void *out, hipStream_t stream);
+
+/*
+ * tm_embedding_grad -- the table's gradient, given that of out ([count][width]
+ * contiguous of dtype):
+ *
+ *   out_grad[v][d] = scale * sum of up[n][d] over the n with tokens[n] = v
+ *
+ * [rows][width] contiguous of dtype, written completely.  The numbers n are
+ * sorted by token; each row is summed in float32 in rising order of n, in
+ * shares that are then added, and rounded once.  workspace: at least
+ * tm_embedding_grad_workspace_size() bytes, 16-byte aligned, no initialisation.
+ * Errors: as tm_embedding, and TM_ERR_WORKSPACE.
+ */
+int tm_embedding_grad(const void *tokens, int token_dtype, int64_t count, const void *up, int dtype, int64_t rows,
+                      int64_t width, double scale, void *out_grad, void *workspace, size_t workspace_bytes,
+                      hipStream_t stream);
+size_t tm_embedding_grad_workspace_size(int64_t rows, int64_t width, int64_t count);
 
 #ifdef __cplusplus
 }

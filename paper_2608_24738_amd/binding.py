@@ -104,7 +104,16 @@ def load() -> ctypes.CDLL:
             lib.tm_head_logp_grad_workspace_size.argtypes = [i32, i64, i64, i64, i32, i32]
             lib.tm_head_logp_workspace_size.restype = size
             lib.tm_head_logp_grad_workspace_size.restype = size
-            for name in ("tm_head_logp", "tm_head_logp_grad", "tm_label_logp", "tm_label_logp_grad", "tm_distance_bias", "tm_relative_bias",
+            lib.tm_layer_norm.argtypes = [vp, i32, i64, i64, i64, vp, vp, i32, ctypes.c_double, vp, vp, vp]
+            lib.tm_layer_norm_grad.argtypes = [vp, i32, i64, i64, i64, vp, i32, vp, vp, vp, vp, vp, vp, size, vp]
+            lib.tm_layer_norm_grad_workspace_size.argtypes = [i32, i64, i64]
+            lib.tm_layer_norm_grad_workspace_size.restype = size
+            lib.tm_embedding.argtypes = [vp, i32, i64, i64, i64, vp, i32, i64, ctypes.c_double, vp, vp]
+            lib.tm_embedding_grad.argtypes = [vp, i32, i64, vp, i32, i64, i64, ctypes.c_double, vp, vp, size, vp]
+            lib.tm_embedding_grad_workspace_size.argtypes = [i64, i64, i64]
+            lib.tm_embedding_grad_workspace_size.restype = size
+            for name in ("tm_layer_norm", "tm_layer_norm_grad", "tm_embedding", "tm_embedding_grad",
+                         "tm_head_logp", "tm_head_logp_grad", "tm_label_logp", "tm_label_logp_grad", "tm_distance_bias", "tm_relative_bias",
                          "tm_distance_bias_grad", "tm_relative_bias_grad"):
                 getattr(lib, name).restype = i32
             lib.tm_label_logp_workspace_size.restype = size

@@ -11,7 +11,8 @@ ROOT = os.path.dirname(PKG)
 LIB = os.path.join(PKG, "libtm_edt.so")
 SOURCES = [os.path.join(PKG, "csrc", "edt_host.hip"),
            os.path.join(PKG, "csrc", "train", "train_host.hip"),
-           os.path.join(PKG, "csrc", "train", "head_host.hip")]
+           os.path.join(PKG, "csrc", "train", "head_host.hip"),
+           os.path.join(PKG, "csrc", "train", "rows_host.hip")]
 DEPS = SOURCES + sorted(glob.glob(os.path.join(PKG, "csrc", "*.h"))) + sorted(
     glob.glob(os.path.join(PKG, "csrc", "train", "*.h"))) + [
     os.path.join(ROOT, "include", "tm_edt.h"), os.path.join(ROOT, "include", "tm_train.h")]

@@ -1,4 +1,4 @@
-"""The operators of a training step on distances, over torch tensors.
+"""The operators of a training step on distances, and those around a vocabulary, over torch tensors.
 
 ``label_log_probs``  log-probabilities of given labels, with the entropy, the
                      likeliest classes and the expected value of a field under
@@ -7,8 +7,12 @@
 ``relative_bias``    a learned bias by buckets of the distance between a
                      query's and a key's position
 ``distance_bias``    the same bias from a distance field
+``embedding``        scaled rows of a learned table by given tokens
+``layer_norm``       the norm of rows, with or without weight and bias
+``head_log_probs``   log-probabilities of given labels from hidden states and a
+                     vocabulary's weight, without keeping the logits
 
-All three run in the HIP kernels of ``libtm_edt.so`` (``include/tm_train.h``)
+All run in the HIP kernels of ``libtm_edt.so`` (``include/tm_train.h``)
 on the current stream, take part in autograd (in reverse mode, once), and raise
 where the library refuses a request; there is no fallback.
 
@@ -621,3 +625,158 @@ def _check_tokens(tokens, what, device, shape=None):
     if shape is not None and tokens.shape != shape:
         raise ValueError("%s of shape %s do not fit rows of shape %s" % (what, tuple(tokens.shape), tuple(shape)))
     return tokens.contiguous()
+
+
+@functools.lru_cache(maxsize=1024)
+def _norm_workspace(dtype, rows, width):
+    return int(load().tm_layer_norm_grad_workspace_size(dtype, rows, width))
+
+
+def _norm_forward(x, weight, bias, eps, stats):
+    dev = x.device
+    out = torch.empty(x.shape, dtype=x.dtype, device=dev)
+    kept = torch.empty(x.shape[:-1] + (2,), dtype=torch.float32, device=dev) if stats else None
+    x, rows, stride = _rows(x)
+    param = weight if weight is not None else bias
+    _call("tm_layer_norm", dev, None, x.data_ptr(), FLOATS[x.dtype], rows, x.shape[-1], stride, _ptr(weight),
+          _ptr(bias), 0 if param is None else FLOATS[param.dtype], eps, out.data_ptr(), _ptr(kept))
+    return x, out, kept
+
+
+class _LayerNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, eps):
+        x, out, kept = _norm_forward(x, weight, bias, eps, True)
+        ctx.save_for_backward(x, weight, kept)
+        param = weight if weight is not None else bias
+        ctx.what = (x.dtype, x.device, x.shape, None if param is None else param.dtype)
+        return out
+
+    @staticmethod
+    def backward(ctx, up):
+        _once()
+        x, weight, kept = ctx.saved_tensors
+        dtype, dev, shape, param = ctx.what
+        wants_x, wants_weight, wants_bias = ctx.needs_input_grad[:3]
+        if x.dtype is not dtype or x.device != dev or x.shape != shape:
+            _changed()
+        weight = _restored(weight, param, dev, shape[-1:])
+        kept = _restored(kept, torch.float32, dev, shape[:-1] + (2,))
+        up = up.contiguous()
+        x, rows, stride = _rows(x)
+        grad_x = torch.empty(shape, dtype=dtype, device=dev) if wants_x else None
+        grad_weight = torch.empty(shape[-1:], dtype=param, device=dev) if wants_weight else None
+        grad_bias = torch.empty(shape[-1:], dtype=param, device=dev) if wants_bias else None
+        nbytes = _norm_workspace(FLOATS[dtype], rows, shape[-1]) if wants_weight or wants_bias else 0
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
+        _call("tm_layer_norm_grad", dev, None, x.data_ptr(), FLOATS[dtype], rows, shape[-1], stride, _ptr(weight),
+              0 if param is None else FLOATS[param], kept.data_ptr(), up.data_ptr(), _ptr(grad_x), _ptr(grad_weight),
+              _ptr(grad_bias), _ptr(workspace), nbytes)
+        return grad_x, grad_weight, grad_bias, None
+
+
+def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, *,
+               eps: float = 1e-5) -> torch.Tensor:
+    """The norm of each row of ``x`` (..., width) over its last axis,
+
+        (x - mean x) / sqrt(mean (x - mean x)^2 + eps) * weight + bias
+
+    ``x``       float32, float16 or bfloat16.
+    ``weight``, ``bias``  (width,) of one type, any of these; None: ones, zeros.
+
+    Arithmetic and sums are float32; the result has the type of ``x``, rounded
+    once.  Gradients flow to ``x``, ``weight`` and ``bias``.
+    """
+    if not x.is_cuda:
+        raise ValueError("x must be a ROCm (cuda) tensor")
+    if x.dtype not in FLOATS:
+        raise TypeError("x must be float32, float16 or bfloat16, got %s" % x.dtype)
+    if x.dim() < 1 or x.shape[-1] < 1:
+        raise ValueError("x must be (..., width), got %s" % (tuple(x.shape),))
+    for what, param in (("weight", weight), ("bias", bias)):
+        if param is None:
+            continue
+        if param.dtype not in FLOATS:
+            raise TypeError("%s must be float32, float16 or bfloat16, got %s" % (what, param.dtype))
+        if param.device != x.device:
+            raise ValueError("%s is on %s, x on %s" % (what, param.device, x.device))
+        if param.shape != x.shape[-1:]:
+            raise ValueError("%s must be (%d,), got %s" % (what, x.shape[-1], tuple(param.shape)))
+    if weight is not None and bias is not None and weight.dtype != bias.dtype:
+        raise TypeError("weight and bias must have one type, got %s and %s" % (weight.dtype, bias.dtype))
+    eps = float(eps)
+    if not 2.0 ** -126 < eps < math.inf:
+        raise ValueError("eps must be positive and finite, got %r" % eps)
+    _reverse_only(x, weight, bias)
+    weight = None if weight is None else weight.contiguous()
+    bias = None if bias is None else bias.contiguous()
+    if torch.is_grad_enabled() and (x.requires_grad or (weight is not None and weight.requires_grad)
+                                    or (bias is not None and bias.requires_grad)):
+        return _LayerNorm.apply(x, weight, bias, eps)
+    return _norm_forward(x, weight, bias, eps, False)[1]
+
+
+@functools.lru_cache(maxsize=1024)
+def _embedding_workspace(rows, width, count):
+    return int(load().tm_embedding_grad_workspace_size(rows, width, count))
+
+
+def _embedding_forward(tokens, table, scale):
+    dev, dtype, shape = table.device, table.dtype, table.shape
+    table, rows, stride = _rows(table)
+    out = torch.empty(tokens.shape + shape[1:], dtype=dtype, device=dev)
+    _call("tm_embedding", dev, None, table.data_ptr(), FLOATS[dtype], rows, shape[1], stride, tokens.data_ptr(),
+          LABELS[tokens.dtype], tokens.numel(), scale, out.data_ptr())
+    return out
+
+
+class _Embedding(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, tokens, table, scale):
+        ctx.save_for_backward(tokens)
+        ctx.what = (tokens.dtype, tokens.shape, table.dtype, table.device, table.shape, scale)
+        return _embedding_forward(tokens, table, scale)
+
+    @staticmethod
+    def backward(ctx, up):
+        _once()
+        tokens, = ctx.saved_tensors
+        token_dtype, shape, dtype, dev, table, scale = ctx.what
+        tokens = _restored(tokens, token_dtype, dev, shape)
+        up = up.contiguous()
+        grad = torch.empty(table, dtype=dtype, device=dev)
+        nbytes = _embedding_workspace(table[0], table[1], tokens.numel())
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
+        _call("tm_embedding_grad", dev, None, tokens.data_ptr(), LABELS[token_dtype], tokens.numel(), up.data_ptr(),
+              FLOATS[dtype], table[0], table[1], scale, grad.data_ptr(), _ptr(workspace), nbytes)
+        return None, grad, None
+
+
+def embedding(tokens: torch.Tensor, table: torch.Tensor, *, scale: float = 1.0) -> torch.Tensor:
+    """Rows of a learned table by given tokens: from ``tokens`` (...) to (..., width) with
+
+        out[..., :] = scale * table[tokens[...], :]
+
+    ``tokens``  uint8, bool, int32 or int64.  A token outside the table, such as
+                padding, gives a row of zeros and no gradient.
+    ``table``   (rows, width) float32, float16 or bfloat16.
+    ``scale``   any finite factor; the product is rounded once.
+
+    The gradient flows to ``table``.  It is dense; equal tokens are brought
+    together by sorting and summed in float32, in one order whatever their
+    number, so that two calls give the same bits.
+    """
+    if not table.is_cuda:
+        raise ValueError("table must be a ROCm (cuda) tensor")
+    if table.dtype not in FLOATS:
+        raise TypeError("table must be float32, float16 or bfloat16, got %s" % table.dtype)
+    if table.dim() != 2 or table.shape[0] < 1 or table.shape[1] < 1:
+        raise ValueError("table must be (rows, width), got %s" % (tuple(table.shape),))
+    tokens = _check_tokens(tokens, "tokens", table.device)
+    scale = float(scale)
+    if not -math.inf < scale < math.inf:
+        raise ValueError("scale must be finite, got %r" % scale)
+    _reverse_only(table)
+    if torch.is_grad_enabled() and table.requires_grad:
+        return _Embedding.apply(tokens, table, scale)
+    return _embedding_forward(tokens, table, scale)

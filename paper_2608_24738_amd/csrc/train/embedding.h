@@ -15,7 +15,7 @@
 
 namespace tmtrain {
 
-constexpr uint32_t kSortTile = 2048;            // tokens that a workgroup sorts at once
+constexpr uint32_t kSortTile = 1024;            // tokens that a workgroup sorts at once
 constexpr uint32_t kSortMost = 512;             // values of a digit
 constexpr uint32_t kSortFew = 64;               // tiles whose counts each workgroup adds up by itself
 constexpr uint32_t kClearRows = 64;             // rows of the table that a workgroup looks for
@@ -112,6 +112,14 @@ __global__ __launch_bounds__(256) void k_sort_move(EmbeddingArgs p) {
     __shared__ uint16_t wave_has[kWaves][kSortMost];    // how many a wave has, then how many before it
     __shared__ uint32_t scan[kWaves];
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    // a wave has a stretch of the tile and takes 64 of it a round
+    const uint32_t first = blockIdx.x * kSortTile + wave * (kSortTile / kWaves);
+    uint32_t key[kRounds], rank[kRounds];
+#pragma unroll
+    for (uint32_t r = 0; r < kRounds; ++r) {
+        const uint32_t i = first + r * 64 + lane;
+        key[r] = i < p.count ? sort_key(p, i) : 0;
+    }
     for (uint32_t i = threadIdx.x; i < kWaves * kSortMost; i += 256) (&wave_has[0][0])[i] = 0;
     // sums over the lower values: two values to a thread, side by side
     uint32_t total[2] = {0, 0}, before[2] = {0, 0};
@@ -123,6 +131,7 @@ __global__ __launch_bounds__(256) void k_sort_move(EmbeddingArgs p) {
             total[j] = p.total[v];
             before[j] = p.digits[uint64_t(blockIdx.x) * p.values + v];
         } else {
+#pragma unroll 8
             for (uint32_t t = 0; t < p.tiles; ++t) {
                 const uint32_t x = p.digits[t * p.values + v];
                 total[j] += x;
@@ -142,14 +151,10 @@ __global__ __launch_bounds__(256) void k_sort_move(EmbeddingArgs p) {
     for (uint32_t w = 0; w < wave; ++w) up += scan[w];
     place[threadIdx.x * 2] = up + before[0];
     place[threadIdx.x * 2 + 1] = up + total[0] + before[1];
-    // a wave has a stretch of the tile and takes 64 of it a round
-    uint32_t key[kRounds], rank[kRounds];
-    const uint32_t first = blockIdx.x * kSortTile + wave * (kSortTile / kWaves);
 #pragma unroll
     for (uint32_t r = 0; r < kRounds; ++r) {
         const uint32_t i = first + r * 64 + lane;
         const bool real = i < p.count;
-        key[r] = real ? sort_key(p, i) : 0;
         const uint32_t digit = key[r] >> p.shift & (p.values - 1);
         uint64_t same = __ballot(real);                 // lanes with this lane's digit
         for (uint32_t bit = 1; bit < p.values; bit <<= 1) {

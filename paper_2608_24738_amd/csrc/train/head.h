@@ -1,12 +1,12 @@
 // head.h -- kernels of the log-probabilities from hidden states and a
 // vocabulary's weight (tm_head_logp in include/tm_train.h).
 //
-// With x = scale h w^T, c = scale log2(e) and a whole number M near the largest
-// c h w of a row:
+// With x = scale h w^T, c = scale log2(e) and M the largest c h w of a row:
 //     s = sum_v 2^(c h w_v - M),   log sum exp x = ln 2 (M + log2 s),
 //     log p_y = ln 2 ((c h w_y - M) - log2 s),   p_v = 2^(c h w_v - M) / s.
-// M being whole, one fma gives the exponent with one rounding, and sums with
-// different M are put together by exact powers of two.  M starts at -FLT_MAX
+// One fma gives an exponent with one rounding.  M is the largest itself, not a
+// whole number near it: a class with nearly all of the mass then has a power
+// and a sum next to 1, whose logarithms lose least.  M starts at -FLT_MAX
 // instead of -inf, so that the exponent is never inf - inf: logits at -inf get
 // 0, and s = 0 marks a row with no class left.
 //
@@ -14,7 +14,7 @@
 // The gradient computes them anew, a piece of the vocabulary at a time, as
 //     g_nv = alpha_n 1[v = y_n] - beta_n p_nv,   alpha = scale up_logp,
 //     beta = scale (up_logp - up_log_sum),
-// and leaves g and its transpose in the operands' type for the two products
+// and leaves g in the operands' type for the two products
 //     dh = g w,   dw = g^T h.
 // Rows without a label take part only where the log sums are asked for: the
 // rows that do are packed first, and the products run over those alone.
@@ -33,7 +33,7 @@ struct HeadSum {
 };
 constexpr float kLowest = -FLT_MAX;
 
-// 2^(a - b) for whole a <= b; 0 where a is kLowest and b is not.
+// 2^(a - b) for a <= b; 0 where a is kLowest and b is not.
 __device__ __forceinline__ float shrink(float a, float b) { return a == b ? 1.0f : exp2_hw(fmaxf(a - b, -200.0f)); }
 
 // inf - inf of the references of rows with +inf stays NaN in s.
@@ -41,7 +41,7 @@ __device__ __forceinline__ HeadSum join(HeadSum a, HeadSum b) {
     const float m = fmaxf(a.m, b.m);
     return {m, a.s * shrink(a.m, m) + b.s * shrink(b.m, m)};
 }
-__device__ __forceinline__ float whole(float most, float c) { return fmaxf(rintf(most * c), kLowest); }
+__device__ __forceinline__ float reference(float most, float c) { return fmaxf(most * c, kLowest); }
 
 // A packed row, for the gradient.
 struct HeadRow {
@@ -69,17 +69,17 @@ struct HeadArgs {
     int32_t *place;             // and where each row went, or -1
     HeadRow *row;
     float *inverse;             // float16: what takes a packed row's power of two back; then the common one's
-    void *packed, *turned;      // packed hidden states [n][width], and [width][n]
+    void *packed;               // packed hidden states [n_pad][width_pad]
     HeadSum *part;              // [parts][n_pad]
     float *found;               // c h w of the packed rows' labels
-    void *slope, *slope_turned; // [n_pad][piece], [piece][n_pad]
-    void *weight_turned;        // [width][piece]
+    void *slope, *slope_common; // g [n_pad][piece]; float16: times its row's power of two, and the common one
     void *weight_laid;          // a piece's weights in whole steps, where they do not lie so
     float *sum;                 // [splits][n_pad][sum_stride]
     uint32_t n_pad, width_pad, sum_stride;
     uint32_t parts;
     uint32_t first, piece;      // classes of the piece at hand, and its width
     uint32_t splits, steps;     // of the product for dh
+    bool large;                 // its tiles
     bool add;                   // to the sums so far
 };
 
@@ -241,7 +241,6 @@ struct LayArgs {
     uint64_t stride;
     const uint32_t *list, *count;   // which rows; NULL: `rows` of them in order
     uint32_t rows, width;
-    uint32_t fill;                  // turned: columns to fill with zeros at least
     void *to;
     uint32_t to_stride;             // elements
 };
@@ -260,50 +259,28 @@ __global__ __launch_bounds__(256) void k_lay_rows(LayArgs p) {
     }
 }
 
-// The same rows turned: `to` is [width][to_stride], its columns from the number
-// of rows to the next whole step zero.  Tiles of 64 x 64 through LDS.
-template <typename T>
-__global__ __launch_bounds__(256) void k_turn_rows(LayArgs p) {
-    constexpr int V = 16 / sizeof(T), kSide = 64, kPieces = kSide / V;
-    __shared__ T tile[kSide][kSide + 4 / sizeof(T)];
-    const uint32_t rows = p.count ? *p.count : p.rows;
-    const uint32_t r0 = blockIdx.x * kSide, c0 = blockIdx.y * kSide;
-    if (r0 >= max(rows, p.fill)) return;
-    for (uint32_t i = threadIdx.x; i < kSide * kPieces; i += 256) {
-        const uint32_t r = r0 + i / kPieces, c = c0 + i % kPieces * V;
-        Pack<T, V> v{};
-        if (r < rows && c < p.width)
-            v = load_pack<V>(static_cast<const T *>(p.from) + (p.list ? p.list[r] : r) * p.stride + c, p.width - c, T{});
-#pragma unroll
-        for (int j = 0; j < V; ++j) tile[i / kPieces][i % kPieces * V + j] = v.at(j);
-    }
-    __syncthreads();
-    for (uint32_t i = threadIdx.x; i < kSide * kPieces; i += 256) {
-        const uint32_t c = i / kPieces, r = i % kPieces * V;
-        if (c0 + c >= p.width) continue;
-        Pack<T, V> v{};
-#pragma unroll
-        for (int j = 0; j < V; ++j) v.put(j, tile[r + j][c]);
-        store_pack<V>(static_cast<T *>(p.to) + uint64_t(c0 + c) * p.to_stride + r0 + r, v);
-    }
-}
-
 // ---------------------------------------------------------------------------
 // Products over tiles.
 // ---------------------------------------------------------------------------
 
-// The weights of the piece at hand, as the left operand.
+// The weights of the piece at hand.
 template <typename T>
 __device__ __forceinline__ Operand weight_rows(const HeadArgs &p) {
     const uint32_t rows = min(p.piece, p.classes - p.first);
     if (p.weight_laid)
-        return {static_cast<const char *>(p.weight_laid), uint64_t(p.width_pad) * sizeof(T), rows, 0};
+        return {static_cast<const char *>(p.weight_laid), uint64_t(p.width_pad) * sizeof(T), rows,
+                uint32_t(p.width_pad * sizeof(T) / 16)};
     return {static_cast<const char *>(p.weight) + uint64_t(p.first) * p.weight_stride * sizeof(T),
             p.weight_stride * sizeof(T), rows, uint32_t(p.width * sizeof(T) / 16)};
 }
 template <typename T>
-__device__ __forceinline__ Operand hidden_rows(const HeadArgs &p) {
-    return {static_cast<const char *>(p.packed), uint64_t(p.width_pad) * sizeof(T), p.n_pad, 0};
+__device__ __forceinline__ Operand hidden_rows(const HeadArgs &p, uint32_t rows) {
+    return {static_cast<const char *>(p.packed), uint64_t(p.width_pad) * sizeof(T), rows,
+            uint32_t(p.width_pad * sizeof(T) / 16)};
+}
+template <typename T>
+__device__ __forceinline__ Operand slope_rows(const HeadArgs &p, const void *at, uint32_t rows) {
+    return {static_cast<const char *>(at), uint64_t(p.piece) * sizeof(T), rows, uint32_t(p.piece * sizeof(T) / 16)};
 }
 
 // Sums of 2^(c x - M) of the packed rows over a tile's classes, one for each
@@ -316,8 +293,8 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_sums(
     if (blockIdx.x >= uint64_t(tiles_m) * tiles_n) return;
     const TilePlace at = tile_place(blockIdx.x, tiles_m, tiles_n);
     Tile tile;
-    tile.run(weight_rows<T>(p), at.m * Tile::BM, hidden_rows<T>(p), at.n * Tile::BN, 0, p.width_pad / kStep<T>, even,
-             odd);
+    tile.template run<false, false>(weight_rows<T>(p), at.m * Tile::BM, hidden_rows<T>(p, p.n_pad), at.n * Tile::BN, 0,
+                                    p.width_pad / kStep<T>, even, odd);
     const bool edge = (at.m + 1) * Tile::BM > rows;
     const uint32_t part = (p.first / Tile::BM + at.m) * Tile::WM + tile.wave / Tile::WN;
 #pragma unroll
@@ -339,7 +316,7 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_sums(
             }
         most = fmaxf(most, __shfl_xor(most, 16));
         most = fmaxf(most, __shfl_xor(most, 32));
-        const float m = whole(most, p.c);
+        const float m = reference(most, p.c);
         float s = 0.0f;
 #pragma unroll
         for (int i = 0; i < Tile::TM; ++i)
@@ -353,10 +330,26 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_sums(
     }
 }
 
+// A row's results.
+__device__ __forceinline__ void head_store(const HeadArgs &p, uint32_t n, const float *found, HeadSum sum) {
+    const int32_t y = p.label ? load_label(p.label, p.label_bytes, n, p.classes) : -1;
+    const float log_s = log2f(sum.s);
+    if (p.logp) {
+        float l = 0.0f;
+        if (y >= 0) {
+            l = (fmaf(*found, p.c, -sum.m) - log_s) * kLn2;
+            if (sum.s == 0.0f) l = -INFINITY;
+        }
+        p.logp[n] = l;
+    }
+    if (p.log_sum) p.log_sum[n] = sum.s == 0.0f ? -INFINITY : fmaf(log_s, kLn2, sum.m * kLn2);
+    if (p.stats) p.stats[n] = sum;
+}
+
 // The sums of a row over all parts: 64 rows to a workgroup, parts over its 16 waves.
 __global__ __launch_bounds__(1024) void k_head_join(HeadArgs p) {
     __shared__ HeadSum lds[16][64];
-    const uint32_t count = p.count ? *p.count : p.n;
+    const uint32_t count = *p.count;
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const uint32_t j = blockIdx.x * 64 + lane;
     if (blockIdx.x * 64 >= count) return;
@@ -377,22 +370,10 @@ __global__ __launch_bounds__(1024) void k_head_join(HeadArgs p) {
     __syncthreads();
     if (wave || j >= count) return;
     for (int w = 1; w < 16; ++w) sum = join(sum, lds[w][lane]);
-    const uint32_t n = p.count ? p.list[j] : j;
-    const int32_t y = p.label ? load_label(p.label, p.label_bytes, n, p.classes) : -1;
-    const float log_s = log2f(sum.s);
-    if (p.logp) {
-        float l = 0.0f;
-        if (y >= 0) {
-            l = (fmaf(p.found[j], p.c, -sum.m) - log_s) * kLn2;
-            if (sum.s == 0.0f) l = -INFINITY;
-        }
-        p.logp[n] = l;
-    }
-    if (p.log_sum) p.log_sum[n] = sum.s == 0.0f ? -INFINITY : fmaf(log_s, kLn2, sum.m * kLn2);
-    if (p.stats) p.stats[n] = sum;
+    head_store(p, p.list[j], p.found + j, sum);
 }
 
-// g of a piece of the vocabulary, and turned.
+// g of a piece of the vocabulary.
 template <typename T, typename Tile>
 __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_slopes(HeadArgs p) {
     __shared__ __attribute__((aligned(1024))) typename Tile::Buffer even, odd;
@@ -401,8 +382,8 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_slope
     const TilePlace at = tile_place(blockIdx.x, tiles_m, tiles_n);
     const uint32_t rows = min(p.piece, p.classes - p.first);
     Tile tile;
-    tile.run(weight_rows<T>(p), at.m * Tile::BM, hidden_rows<T>(p), at.n * Tile::BN, 0, p.width_pad / kStep<T>, even,
-             odd);
+    tile.template run<false, false>(weight_rows<T>(p), at.m * Tile::BM, hidden_rows<T>(p, p.n_pad), at.n * Tile::BN, 0,
+                                    p.width_pad / kStep<T>, even, odd);
     const float common = p.inverse ? 1.0f / p.inverse[p.n_pad] : 1.0f;
 #pragma unroll
     for (int j = 0; j < Tile::TN; ++j) {
@@ -423,10 +404,11 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_slope
             }
             if (p.slope)
                 store_pack<4>(static_cast<T *>(p.slope) + uint64_t(n) * p.piece + v, narrow_pack<T>(g));
-            if (p.slope_turned)
+            if (__is_same(T, f16) && p.slope_common) {
 #pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    static_cast<T *>(p.slope_turned)[uint64_t(v + q) * p.n_pad + n] = narrow<T>(g[q] * ratio);
+                for (int q = 0; q < 4; ++q) g[q] *= ratio;
+                store_pack<4>(static_cast<T *>(p.slope_common) + uint64_t(n) * p.piece + v, narrow_pack<T>(g));
+            }
         }
     }
 }
@@ -437,18 +419,17 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_hidde
     __shared__ __attribute__((aligned(1024))) typename Tile::Buffer even, odd;
     const uint32_t count = *p.count, tiles_n = (count + Tile::BN - 1) / Tile::BN;
     const uint32_t tiles_m = (p.width + Tile::BM - 1) / Tile::BM;
-    if (blockIdx.x >= uint64_t(tiles_m) * tiles_n) return;
-    const TilePlace at = tile_place(blockIdx.x, tiles_m, tiles_n);
-    const uint64_t stride = uint64_t(p.piece) * sizeof(T);
+    if (blockIdx.x >= uint64_t(tiles_m) * tiles_n * p.splits) return;
+    const TilePlace at = tile_place(blockIdx.x, tiles_m, tiles_n, p.splits);
     const uint32_t all = p.piece / kStep<T>;
     Tile tile;
-    tile.run({static_cast<const char *>(p.weight_turned), stride, p.width, 0}, at.m * Tile::BM,
-             {static_cast<const char *>(p.slope), stride, p.n_pad, 0}, at.n * Tile::BN,
-             min(all, blockIdx.y * p.steps), min(all, (blockIdx.y + 1) * p.steps), even, odd);
+    tile.template run<true, false>(weight_rows<T>(p), at.m * Tile::BM, slope_rows<T>(p, p.slope, p.n_pad),
+                                   at.n * Tile::BN, min(all, at.split * p.steps), min(all, (at.split + 1) * p.steps),
+                                   even, odd);
 #pragma unroll
     for (int j = 0; j < Tile::TN; ++j) {
         const uint32_t n = at.n * Tile::BN + tile.column(j);
-        float *to = p.sum + (uint64_t(blockIdx.y) * p.n_pad + n) * p.sum_stride;
+        float *to = p.sum + (uint64_t(at.split) * p.n_pad + n) * p.sum_stride;
         if (n >= count) continue;
 #pragma unroll
         for (int i = 0; i < Tile::TM; ++i) {
@@ -491,11 +472,10 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_weigh
     const uint32_t count = *p.count, rows = min(p.piece, p.classes - p.first);
     const uint32_t tiles_m = (p.width + Tile::BM - 1) / Tile::BM, tiles_n = (rows + Tile::BN - 1) / Tile::BN;
     const TilePlace at = tile_place(blockIdx.x, tiles_m, tiles_n);
-    const uint64_t stride = uint64_t(p.n_pad) * sizeof(T);
+    const void *slope = __is_same(T, f16) ? p.slope_common : p.slope;
     Tile tile;
-    tile.run({static_cast<const char *>(p.turned), stride, p.width, 0}, at.m * Tile::BM,
-             {static_cast<const char *>(p.slope_turned), stride, p.piece, 0}, at.n * Tile::BN, 0,
-             (count + kStep<T> - 1) / kStep<T>, even, odd);
+    tile.template run<true, true>(hidden_rows<T>(p, count), at.m * Tile::BM, slope_rows<T>(p, slope, count),
+                                  at.n * Tile::BN, 0, (count + kStep<T> - 1) / kStep<T>, even, odd);
     const float back = p.inverse ? p.inverse[p.n_pad] : 1.0f;
 #pragma unroll
     for (int j = 0; j < Tile::TN; ++j) {

@@ -8,6 +8,7 @@ namespace tmtrain {
 
 constexpr int kFewWaves = 4;
 constexpr int kFewClasses = 16 * kFewWaves;     // of a workgroup
+constexpr int kFewSums = 8;
 constexpr int kFewAhead = 8;                    // pieces of a row on their way to a lane
 
 // c h w of 16 classes from v0 on and all rows: the lane holds classes v0 + 4 g + q of row n = lane % 16.
@@ -17,7 +18,10 @@ __device__ __forceinline__ f32x4 few_logits(const HeadArgs &p, uint32_t v0) {
     const uint32_t lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const T *w = static_cast<const T *>(p.weight) + uint64_t(min(v0 + r, p.classes - 1)) * p.weight_stride;
     const T *h = static_cast<const T *>(p.hidden) + uint64_t(min(r, p.n - 1)) * p.hidden_stride;
-    f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    // several sums, so that none grows to the whole logit step by step
+    f32x4 acc[kFewSums];
+#pragma unroll
+    for (int i = 0; i < kFewSums; ++i) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     uint32_t k = g * V;
     const auto words = [](const Pack<T, int(V)> &x) { return u32x4{x.w[0], x.w[1], x.w[2], x.w[3]}; };
     for (; k - g * V + kFewAhead * kRound <= p.width; k += kFewAhead * kRound) {
@@ -27,7 +31,7 @@ __device__ __forceinline__ f32x4 few_logits(const HeadArgs &p, uint32_t v0) {
 #pragma unroll
         for (int i = 0; i < kFewAhead; ++i) b[i] = load_pack<int(V)>(h + k + i * kRound);
 #pragma unroll
-        for (int i = 0; i < kFewAhead; ++i) acc = multiply<T>(words(a[i]), words(b[i]), acc);
+        for (int i = 0; i < kFewAhead; ++i) acc[i % kFewSums] = multiply<T>(words(a[i]), words(b[i]), acc[i % kFewSums]);
     }
     for (; k - g * V < p.width; k += kRound) {
         Pack<T, int(V)> a{}, b{};
@@ -35,9 +39,13 @@ __device__ __forceinline__ f32x4 few_logits(const HeadArgs &p, uint32_t v0) {
             a = load_pack<int(V)>(w + k, p.width - k, T{});
             b = load_pack<int(V)>(h + k, p.width - k, T{});
         }
-        acc = multiply<T>(words(a), words(b), acc);
+        acc[0] = multiply<T>(words(a), words(b), acc[0]);
     }
-    return acc;
+#pragma unroll
+    for (int d = kFewSums / 2; d; d /= 2)
+#pragma unroll
+        for (int i = 0; i < d; ++i) acc[i] += acc[i + d];
+    return acc[0];
 }
 
 // Sums of 2^(c x - M) over a workgroup's classes, and c x of the labels.
@@ -62,7 +70,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_few_sums(HeadArgs p) {
         }
         most = fmaxf(most, __shfl_xor(most, 16));
         most = fmaxf(most, __shfl_xor(most, 32));
-        sum.m = whole(most, p.c);
+        sum.m = reference(most, p.c);
 #pragma unroll
         for (int q = 0; q < 4; ++q) sum.s += exp2_hw(fmaf(x[q], p.c, -sum.m));
         sum.s += __shfl_xor(sum.s, 16);
@@ -74,7 +82,30 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_few_sums(HeadArgs p) {
     sum = lds[0][n];
 #pragma unroll
     for (int w = 1; w < kFewWaves; ++w) sum = join(sum, lds[w][n]);
-    p.part[uint64_t(blockIdx.x) * kFewRows + n] = sum;
+    if (n < p.n) p.part[uint64_t(n) * p.parts + blockIdx.x] = sum;
+}
+
+// The sums of a row over all parts, a workgroup to a row.
+__global__ __launch_bounds__(256) void k_few_rows(HeadArgs p) {
+    __shared__ HeadSum lds[4];
+    constexpr int kAhead = 4;
+    const HeadSum *part = p.part + uint64_t(blockIdx.x) * p.parts;
+    HeadSum sum = {kLowest, 0.0f};
+    for (uint32_t i = threadIdx.x; i < p.parts; i += 256 * kAhead) {
+        HeadSum got[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) got[k] = i + 256 * k < p.parts ? part[i + 256 * k] : HeadSum{kLowest, 0.0f};
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) sum = join(sum, got[k]);
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) sum = join(sum, HeadSum{__shfl_xor(sum.m, d), __shfl_xor(sum.s, d)});
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    if (threadIdx.x) return;
+#pragma unroll
+    for (int w = 1; w < 4; ++w) sum = join(sum, lds[w]);
+    head_store(p, blockIdx.x, p.found + blockIdx.x, sum);
 }
 
 // g in float32, [classes][kFewRows]; 0 for rows that take no part.

@@ -71,8 +71,10 @@ uint64_t whole_tiles(uint64_t n) { return ceil_div(n, kTilePad) * kTilePad; }
 
 bool few(const HeadShape &s) { return s.n <= kFewRows; }
 
-// Largest tiles, unless they leave CUs without one.
-bool large_tiles(uint64_t m, uint64_t n) { return ceil_div(m, 256) * ceil_div(n, 256) >= kCus; }
+// Largest tiles, unless they leave CUs without one; `most` is how often k can be split.
+bool large_tiles(uint64_t m, uint64_t n, uint64_t most = 1) {
+    return ceil_div(m, 256) * ceil_div(n, 256) * most >= kCus;
+}
 
 // Tiles read whole 16-byte pieces of the weight, from addresses of 16 bytes.
 bool lies_well(const void *p, uint64_t stride, const HeadShape &s) {
@@ -101,7 +103,7 @@ uint64_t head_room(const HeadShape &s, bool laid, void *at, HeadArgs &a) {
     a.found = room.take<float>(a.n_pad);
     if (few(s)) {
         a.parts = uint32_t(ceil_div(s.classes, kFewClasses));
-        a.part = room.take<HeadSum>(uint64_t(a.parts) * kFewRows);
+        a.part = room.take<HeadSum>(uint64_t(a.parts) * a.n);
         return room.used;
     }
     const bool large = large_tiles(s.classes, s.n);
@@ -140,11 +142,11 @@ uint64_t head_grad_room(const HeadShape &s, int dtype, bool laid, bool hidden, b
     }
     a.piece = uint32_t(piece_of(s.classes, a.n_pad * s.size, kPieceBytes));
     a.sum_stride = uint32_t(ceil_div(s.width, 4) * 4);
-    const bool large = large_tiles(s.width, s.n);
-    const uint64_t tiles = ceil_div(s.width, large ? 256 : 128) * ceil_div(s.n, large ? 256 : 128);
     // splits that give every CU a tile (two of the small ones), each of 8 steps at least
-    const uint64_t steps = a.piece * s.size / kStepBytes, slots = large ? kCus : 2 * kCus;
-    const uint64_t splits = std::max<uint64_t>(1, std::min<uint64_t>({slots / tiles, steps / 8, 32}));
+    const uint64_t steps = a.piece * s.size / kStepBytes, most = std::max<uint64_t>(1, std::min<uint64_t>(steps / 8, 32));
+    a.large = large_tiles(s.width, s.n, most);
+    const uint64_t side = a.large ? 256 : 128, tiles = ceil_div(s.width, side) * ceil_div(s.n, side);
+    const uint64_t splits = std::max<uint64_t>(1, std::min(most, (a.large ? kCus : 2 * kCus) / tiles));
     a.steps = uint32_t(ceil_div(steps, splits));
     a.splits = uint32_t(ceil_div(steps, a.steps));
     a.count = room.take<uint32_t>(1);
@@ -154,23 +156,18 @@ uint64_t head_grad_room(const HeadShape &s, int dtype, bool laid, bool hidden, b
     a.row = room.take<HeadRow>(a.n_pad);
     if (dtype == TM_DTYPE_F16) a.inverse = room.take<float>(a.n_pad + 1);
     a.packed = room.take<char>(uint64_t(a.n_pad) * a.width_pad * s.size);
-    if (weight) {
-        a.turned = room.take<char>(uint64_t(a.n_pad) * s.width * s.size);
-        a.slope_turned = room.take<char>(uint64_t(a.n_pad) * a.piece * s.size);
-    }
-    if (hidden) {
-        a.slope = room.take<char>(uint64_t(a.n_pad) * a.piece * s.size);
-        a.weight_turned = room.take<char>(s.width * a.piece * s.size);
-        a.sum = room.take<float>(uint64_t(a.splits) * a.n_pad * a.sum_stride);
-    }
+    const uint64_t slopes = uint64_t(a.n_pad) * a.piece * s.size;
+    if (hidden || dtype != TM_DTYPE_F16) a.slope = room.take<char>(slopes);
+    if (weight && dtype == TM_DTYPE_F16) a.slope_common = room.take<char>(slopes);
+    if (hidden) a.sum = room.take<float>(uint64_t(a.splits) * a.n_pad * a.sum_stride);
     if (laid) a.weight_laid = room.take<char>(uint64_t(a.piece) * a.width_pad * s.size);
     return room.used;
 }
 
-// fn(tile) of the tile that m x n elements take.
+// fn(tile)
 template <typename T, typename F>
-int by_tile(uint64_t m, uint64_t n, F fn) {
-    return large_tiles(m, n) ? fn(static_cast<LargeTile<T> *>(nullptr)) : fn(static_cast<SmallTile<T> *>(nullptr));
+int by_tile(bool large, F fn) {
+    return large ? fn(static_cast<LargeTile<T> *>(nullptr)) : fn(static_cast<SmallTile<T> *>(nullptr));
 }
 
 template <typename Tile>
@@ -178,7 +175,7 @@ dim3 tile_grid(uint64_t m, uint64_t n) {
     return dim3(uint32_t(ceil_div(m, Tile::BM) * ceil_div(n, Tile::BN)));
 }
 
-// The list of packed rows and the rows themselves, packed and turned.
+// The list of packed rows, and the rows.
 template <typename T>
 int pack_rows(const HeadArgs &a, hipStream_t stream) {
     const uint32_t chunks = uint32_t(ceil_div(a.n, kListChunk));
@@ -195,11 +192,7 @@ int pack_rows(const HeadArgs &a, hipStream_t stream) {
     lay.width = a.width;
     lay.to = a.packed;
     lay.to_stride = a.width_pad;
-    rc = launch(k_lay_rows<T>, dim3(std::min(a.n, 4096u)), dim3(256), 0, stream, lay);
-    if (rc != TM_OK || !a.turned) return rc;
-    lay.to = a.turned;
-    lay.to_stride = a.n_pad;
-    return launch(k_turn_rows<T>, dim3(a.n_pad / 64, uint32_t(ceil_div(a.width, 64))), dim3(256), 0, stream, lay);
+    return launch(k_lay_rows<T>, dim3(std::min(a.n, 4096u)), dim3(256), 0, stream, lay);
 }
 
 // The weights of the piece at hand in whole steps.
@@ -215,25 +208,11 @@ int lay_piece(const HeadArgs &a, hipStream_t stream) {
     return launch(k_lay_rows<T>, dim3(std::min(lay.rows, 4096u)), dim3(256), 0, stream, lay);
 }
 
-// and turned.
-template <typename T>
-int turn_piece(const HeadArgs &a, hipStream_t stream) {
-    LayArgs lay{};
-    lay.from = static_cast<const T *>(a.weight) + uint64_t(a.first) * a.weight_stride;
-    lay.stride = a.weight_stride;
-    lay.rows = std::min(a.piece, a.classes - a.first);
-    lay.width = a.width;
-    lay.fill = a.piece;
-    lay.to = a.weight_turned;
-    lay.to_stride = a.piece;
-    return launch(k_turn_rows<T>, dim3(a.piece / 64, uint32_t(ceil_div(a.width, 64))), dim3(256), 0, stream, lay);
-}
-
 template <typename T>
 int run_head(HeadArgs a, const HeadShape &s, hipStream_t stream) {
     if (few(s)) {
         const int rc = launch(k_few_sums<T>, dim3(a.parts), dim3(64 * kFewWaves), 0, stream, a);
-        return rc == TM_OK ? launch(k_head_join, dim3(1), dim3(1024), 0, stream, a) : rc;
+        return rc == TM_OK ? launch(k_few_rows, dim3(a.n), dim3(256), 0, stream, a) : rc;
     }
     int rc = pack_rows<T>(a, stream);
     for (uint64_t first = 0; rc == TM_OK && first < s.classes; first += a.piece) {
@@ -241,7 +220,7 @@ int run_head(HeadArgs a, const HeadShape &s, hipStream_t stream) {
         if (a.weight_laid) rc = lay_piece<T>(a, stream);
         if (rc != TM_OK) break;
         // the tile is that of all classes: it says how many parts there are
-        rc = by_tile<T>(s.classes, s.n, [&](auto *t) {
+        rc = by_tile<T>(large_tiles(s.classes, s.n), [&](auto *t) {
             using Tile = std::remove_pointer_t<decltype(t)>;
             return launch(k_head_sums<T, Tile>, tile_grid<Tile>(std::min<uint64_t>(a.piece, s.classes - first), s.n),
                           dim3(Tile::kThreads), 0, stream, a);
@@ -272,22 +251,20 @@ int run_head_grad(HeadArgs a, const HeadShape &s, hipStream_t stream) {
         a.add = first > 0;
         if (a.weight_laid) rc = lay_piece<T>(a, stream);
         if (rc != TM_OK) break;
-        rc = by_tile<T>(a.piece, s.n, [&](auto *t) {
+        rc = by_tile<T>(large_tiles(a.piece, s.n), [&](auto *t) {
             using Tile = std::remove_pointer_t<decltype(t)>;
             return launch(k_head_slopes<T, Tile>, tile_grid<Tile>(a.piece, s.n), dim3(Tile::kThreads), 0, stream, a);
         });
         if (rc == TM_OK && a.grad_hidden) {
-            rc = turn_piece<T>(a, stream);
-            if (rc != TM_OK) break;
-            rc = by_tile<T>(s.width, s.n, [&](auto *t) {
+            rc = by_tile<T>(a.large, [&](auto *t) {
                 using Tile = std::remove_pointer_t<decltype(t)>;
-                return launch(k_head_hidden<T, Tile>, dim3(tile_grid<Tile>(s.width, s.n).x, a.splits),
+                return launch(k_head_hidden<T, Tile>, dim3(tile_grid<Tile>(s.width, s.n).x * a.splits),
                               dim3(Tile::kThreads), 0, stream, a);
             });
         }
         if (rc == TM_OK && a.grad_weight) {
             const uint64_t rows = std::min<uint64_t>(a.piece, s.classes - first);
-            rc = by_tile<T>(s.width, rows, [&](auto *t) {
+            rc = by_tile<T>(large_tiles(s.width, rows), [&](auto *t) {
                 using Tile = std::remove_pointer_t<decltype(t)>;
                 return launch(k_head_weight<T, Tile>, tile_grid<Tile>(s.width, rows), dim3(Tile::kThreads), 0, stream, a);
             });

@@ -1,24 +1,30 @@
 // product.h -- tiles of a matrix product  C[m][n] = sum_k A[m][k] B[n][k]  on
-// the matrix cores, both operands with k side by side, for the kernels of
-// head.h.
+// the matrix cores, for the kernels of head.h.  An operand lies along k (k side
+// by side in a row, the rows are m or n) or across it (m or n side by side, the
+// rows are k), so that none is ever turned in memory.
 //
-// A workgroup's tile goes through k in steps of 128 bytes a row (64 elements of
-// 16 bits, 32 floats).  A step's rows of both operands are copied from memory
-// straight to LDS, one step ahead of the one that is multiplied, into two
-// buffers that are separate objects: the compiler then knows that a copy under
-// way is not what is read, and waits for it at the barrier alone.
+// A workgroup's tile goes through k in steps of 64 elements of 16 bits or 32
+// floats.  A step of both operands is copied from memory straight to LDS, one
+// step ahead of the one that is multiplied, into two buffers that are separate
+// objects: the compiler then knows that a copy under way is not what is read,
+// and waits for it at the barrier alone.
 //
-// In LDS the eight 16-byte pieces of row r lie in the order piece ^ (r & 7).
-// A copy writes 64 pieces side by side, so the order is made by which piece a
-// lane fetches; a read of one piece from each of 16 rows then meets all banks
-// alike.
+// A copy writes 64 pieces of 16 bytes side by side, one a lane, so the order of
+// the pieces within a row of LDS is made by which piece a lane fetches.  Along
+// k, the eight pieces of row r lie in the order piece ^ (r & 7); across it, the
+// 32 bytes (floats: 64) that a read takes of a row lie in the order unit ^ u,
+// with u another number for each of the rows that one instruction reads.  All
+// reads then meet the banks alike.
 //
-// A lane of a matrix instruction holds one piece of one row, whatever the type:
-// 16-bit elements go in by one 16x16x32 instruction (k = 8 g + e for lane group
-// g = lane / 16), floats by four 16x16x4 instructions, of which number e takes
-// k = 4 g + e.  A and B agree on the order of k, which is all that matters.
-// Of the result, a lane holds rows m = 4 g .. 4 g + 3 in column n = lane % 16.
+// A lane of a matrix instruction holds 16 bytes of one m or n: 16-bit elements
+// go in by one 16x16x32 instruction (k = 8 g + e for lane group g = lane / 16),
+// floats by four 16x16x4 instructions, of which number e takes k = 4 g + e.
+// Across k, 16-bit elements come from LDS by reads that turn blocks of 4 x 16,
+// floats one by one.  Of the result, a lane holds rows m = 4 g .. 4 g + 3 in
+// column n = lane % 16.
 #pragma once
+
+#include <type_traits>
 
 #include "train_common.h"
 
@@ -63,25 +69,138 @@ __device__ __attribute__((aligned(16))) const uint32_t kZeroPiece[4] = {0, 0, 0,
 // Which tile of tiles_m x tiles_n a workgroup takes.  Workgroups go round robin
 // over the eight XCDs: each gets one stretch of the tiles, so that its L2 holds
 // what neighbouring tiles share, and a stretch goes down m over a few columns.
+// Splits of k come one after the other: tiles that run together read the same k.
 struct TilePlace {
-    uint32_t m, n;
+    uint32_t m, n, split;
 };
-__device__ __forceinline__ TilePlace tile_place(uint32_t block, uint32_t tiles_m, uint32_t tiles_n) {
+__device__ __forceinline__ TilePlace tile_place(uint32_t block, uint32_t tiles_m, uint32_t tiles_n, uint32_t splits = 1) {
     constexpr uint32_t kXcds = 8, kColumns = 4;
-    const uint32_t total = tiles_m * tiles_n;
+    const uint32_t total = tiles_m * tiles_n * splits;
     const uint32_t xcd = block % kXcds, share = total / kXcds, more = total % kXcds;
-    const uint32_t t = xcd * share + min(xcd, more) + block / kXcds;
+    uint32_t t = xcd * share + min(xcd, more) + block / kXcds;
+    const uint32_t split = t / (tiles_m * tiles_n);
+    t -= split * tiles_m * tiles_n;
     const uint32_t group = t / (kColumns * tiles_m), in = t - group * kColumns * tiles_m;
     const uint32_t columns = min(kColumns, tiles_n - group * kColumns);
-    return {in / columns, group * kColumns + in % columns};
+    return {in / columns, group * kColumns + in % columns, split};
 }
 
-// One operand: rows of k, `stride` bytes apart, 16-byte aligned.
+// One operand: rows `stride` bytes apart, 16-byte aligned.
 struct Operand {
     const char *at;
     uint64_t stride;
-    uint32_t rows;              // rows beyond are read as the last one
-    uint32_t pieces;            // whole pieces in a row, beyond them zeros; 0: rows hold whole steps
+    uint32_t rows;              // along k: rows beyond are read as the last one; across: as zeros
+    uint32_t pieces;            // whole pieces in a row; along k: beyond them zeros, across: anything
+};
+
+// Copies of an operand's steps to LDS, S elements of m or n by Waves waves.
+template <typename T, int S, int Waves>
+struct Along {
+    static constexpr int kCopies = S / 8 / Waves;
+    const char *from[kCopies];
+    uint32_t piece, pieces;
+
+    __device__ __forceinline__ Along(const Operand &o, uint32_t m0, uint32_t first, int lane, int wave) {
+        const uint32_t r = lane >> 3;
+        piece = (lane & 7) ^ r;
+        pieces = o.pieces;
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i)
+            from[i] = o.at + min(m0 + (i * Waves + wave) * 8 + r, o.rows - 1) * o.stride + first * kStepBytes + piece * 16;
+    }
+    __device__ __forceinline__ void fetch(char *lds, uint32_t step, int wave) {
+        if (step == pieces / 8) {               // the step that rows end in
+#pragma unroll
+            for (int i = 0; i < kCopies; ++i)
+                from[i] = step * 8 + piece < pieces ? from[i] : reinterpret_cast<const char *>(kZeroPiece);
+        }
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i) {
+            copy_to_lds(from[i], lds + (i * Waves + wave) * 1024);
+            from[i] += kStepBytes;
+        }
+    }
+    // Where the lane's reads of block 0 begin, and the 16 bytes of block i in half of a step.
+    uint32_t place;
+    __device__ __forceinline__ void reads(int lane, uint32_t block) {
+        place = (block * 16 + (lane & 15)) * kStepBytes + (((lane >> 4) ^ (lane & 7)) * 16);
+    }
+    __device__ __forceinline__ u32x4 read(const char *lds, int i, int half) const {
+        return *reinterpret_cast<const u32x4 *>(lds + (half ? place ^ 64 : place) + i * 16 * kStepBytes);
+    }
+};
+
+template <typename T, int S, int Waves, int Blocks>
+struct Across {
+    static constexpr int kCopies = S / 8 / Waves;
+    static constexpr uint32_t kRow = S * sizeof(T), kPieces = kRow / 16;    // of a row in LDS
+    static constexpr uint32_t kUnits = S / 16;                              // of 16 elements
+    const char *from[kCopies];
+    uint64_t stride;
+    uint32_t rows;
+
+    // Pieces of a unit, and the number that orders the units of row r.
+    static constexpr uint32_t kUnitPieces = sizeof(T);
+    static __device__ __forceinline__ uint32_t order(uint32_t r) {
+        const uint32_t u = sizeof(T) == 4 ? r >> 2 & 3 : (r & 3) | (r >> 3 & 3) << 2;
+        return u & (kUnits - 1);
+    }
+    static __device__ __forceinline__ uint32_t row_of(int i, int lane, int wave) {
+        return (i * Waves + wave) * (64 / kPieces) + lane / kPieces;
+    }
+    __device__ __forceinline__ Across(const Operand &o, uint32_t m0, uint32_t first, int lane, int wave) {
+        stride = o.stride;
+        rows = o.rows;
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i) {
+            const uint32_t r = row_of(i, lane, wave);
+            const uint32_t piece = m0 * sizeof(T) / 16 + (lane % kPieces ^ order(r) * kUnitPieces);
+            from[i] = o.at + (uint64_t(first) * kStep<T> + r) * stride + min(piece, o.pieces - 1) * 16;
+        }
+    }
+    __device__ __forceinline__ void fetch(char *lds, uint32_t step, int lane, int wave) {
+        if ((step + 1) * kStep<T> > rows) {
+#pragma unroll
+            for (int i = 0; i < kCopies; ++i)
+                if (step * kStep<T> + row_of(i, lane, wave) >= rows) from[i] = reinterpret_cast<const char *>(kZeroPiece);
+        }
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i) {
+            copy_to_lds(from[i], lds + (i * Waves + wave) * 1024);
+            from[i] += kStep<T> * stride;
+        }
+    }
+    uint32_t place[Blocks];
+    __device__ __forceinline__ void reads(int lane, uint32_t block) {
+        const uint32_t c = lane & 15, g = lane >> 4;
+#pragma unroll
+        for (int i = 0; i < Blocks; ++i) {
+            if constexpr (sizeof(T) == 4)
+                place[i] = 4 * g * kRow + ((block + i) ^ order(4 * g)) * 64 + c * 4;
+            else
+                place[i] = (8 * g + (c >> 2)) * kRow + ((block + i) ^ order(8 * g + (c >> 2))) * 32 + (c & 3) * 8;
+        }
+    }
+    __device__ __forceinline__ u32x4 read(const char *lds, int i, int half) const {
+        u32x4 v;
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                v[e] = *reinterpret_cast<const uint32_t *>(lds + place[i] + (16 * half + e) * kRow);
+        } else {
+            typedef short s4 __attribute__((ext_vector_type(4)));
+            typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+            typedef __attribute__((address_space(3))) s4 *Local;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const u2 q = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (Local)(lds + place[i] + (32 * half + 4 * e) * kRow)));
+                v[2 * e] = q[0];
+                v[2 * e + 1] = q[1];
+            }
+        }
+        return v;
+    }
 };
 
 // BM x BN elements by WM x WN waves.
@@ -90,7 +209,6 @@ struct Tile {
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
     static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves;
     static constexpr int TM = BM / WM / 16, TN = BN / WN / 16;  // 16 x 16 blocks of a wave
-    static constexpr int LM = BM / 8 / kWaves, LN = BN / 8 / kWaves;  // copies of a wave, eight rows each
 
     struct Buffer {
         char row[(BM + BN) * int(kStepBytes)];
@@ -111,49 +229,28 @@ struct Tile {
     __device__ __forceinline__ uint32_t row(int i) const { return ((wave / WN) * TM + i) * 16 + (lane >> 4) * 4; }
     __device__ __forceinline__ uint32_t column(int j) const { return ((wave % WN) * TN + j) * 16 + (lane & 15); }
 
-    // Adds the products of rows m0.. of A and n0.. of B over steps [first, last).
+    // Adds the products of m0.. of A and n0.. of B over steps [first, last).
+    template <bool AAcross, bool BAcross>
     __device__ __forceinline__ void run(const Operand &a, uint32_t m0, const Operand &b, uint32_t n0, uint32_t first,
                                         uint32_t last, Buffer &even, Buffer &odd) {
         if (first >= last) return;
-        const uint32_t r = lane >> 3, piece = (lane & 7) ^ r;
-        const char *pa[LM], *pb[LN];
-#pragma unroll
-        for (int i = 0; i < LM; ++i)
-            pa[i] = a.at + min(m0 + (i * kWaves + wave) * 8 + r, a.rows - 1) * a.stride + first * kStepBytes + piece * 16;
-#pragma unroll
-        for (int i = 0; i < LN; ++i)
-            pb[i] = b.at + min(n0 + (i * kWaves + wave) * 8 + r, b.rows - 1) * b.stride + first * kStepBytes + piece * 16;
-        const uint32_t ragged = a.pieces ? a.pieces / 8 : ~0u;        // the step that A's rows end in
+        constexpr uint32_t kBehind = BM * kStepBytes;           // where B's part of a buffer begins
+        std::conditional_t<AAcross, Across<T, BM, kWaves, TM>, Along<T, BM, kWaves>> from_a(a, m0, first, lane, wave);
+        std::conditional_t<BAcross, Across<T, BN, kWaves, TN>, Along<T, BN, kWaves>> from_b(b, n0, first, lane, wave);
+        from_a.reads(lane, (wave / WN) * TM);
+        from_b.reads(lane, (wave % WN) * TN);
         const auto fetch = [&](Buffer &s, uint32_t step) {
-            if (step == ragged) {
-                const bool out = step * 8 + piece >= a.pieces;
-#pragma unroll
-                for (int i = 0; i < LM; ++i)
-                    pa[i] = out ? reinterpret_cast<const char *>(kZeroPiece) : pa[i];
-            }
-#pragma unroll
-            for (int i = 0; i < LM; ++i) {
-                copy_to_lds(pa[i], s.row + (i * kWaves + wave) * 1024);
-                pa[i] += kStepBytes;
-            }
-#pragma unroll
-            for (int i = 0; i < LN; ++i) {
-                copy_to_lds(pb[i], s.row + BM * kStepBytes + (i * kWaves + wave) * 1024);
-                pb[i] += kStepBytes;
-            }
+            if constexpr (AAcross) from_a.fetch(s.row, step, lane, wave); else from_a.fetch(s.row, step, wave);
+            if constexpr (BAcross) from_b.fetch(s.row + kBehind, step, lane, wave); else from_b.fetch(s.row + kBehind, step, wave);
         };
-        const uint32_t c = lane & 15, g = lane >> 4;
         const auto work = [&](const Buffer &s) {
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                const char *at = s.row + c * kStepBytes + ((g + 4 * half) ^ (c & 7)) * 16;
                 u32x4 fa[TM], fb[TN];
 #pragma unroll
-                for (int i = 0; i < TM; ++i)
-                    fa[i] = *reinterpret_cast<const u32x4 *>(at + ((wave / WN) * TM + i) * 16 * kStepBytes);
+                for (int i = 0; i < TM; ++i) fa[i] = from_a.read(s.row, i, half);
 #pragma unroll
-                for (int j = 0; j < TN; ++j)
-                    fb[j] = *reinterpret_cast<const u32x4 *>(at + (BM + ((wave % WN) * TN + j) * 16) * kStepBytes);
+                for (int j = 0; j < TN; ++j) fb[j] = from_b.read(s.row + kBehind, j, half);
 #pragma unroll
                 for (int i = 0; i < TM; ++i)
 #pragma unroll

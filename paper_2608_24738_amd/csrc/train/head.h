@@ -79,7 +79,7 @@ struct HeadArgs {
     uint32_t parts;
     uint32_t first, piece;      // classes of the piece at hand, and its width
     uint32_t splits, steps;     // of the product for dh
-    bool large;                 // its tiles
+    uint32_t most;              // splits that its k allows
     bool add;                   // to the sums so far
 };
 
@@ -243,13 +243,14 @@ struct LayArgs {
     uint32_t rows, width;
     void *to;
     uint32_t to_stride;             // elements
+    uint64_t plane;                 // elements of a plane, for the three of k_split_rows
 };
 template <typename T>
 __global__ __launch_bounds__(256) void k_lay_rows(LayArgs p) {
     constexpr int V = 16 / sizeof(T);
     const uint32_t rows = p.count ? *p.count : p.rows;
     const uint32_t pieces = p.to_stride / V;
-    for (uint32_t r = blockIdx.x; r < rows; r += gridDim.x) {
+    for (uint32_t r = blockIdx.x * blockDim.y + threadIdx.y; r < rows; r += gridDim.x * blockDim.y) {
         const T *from = static_cast<const T *>(p.from) + (p.list ? p.list[r] : r) * p.stride;
         T *to = static_cast<T *>(p.to) + uint64_t(r) * p.to_stride;
         for (uint32_t i = threadIdx.x; i < pieces; i += blockDim.x) {
@@ -259,42 +260,83 @@ __global__ __launch_bounds__(256) void k_lay_rows(LayArgs p) {
     }
 }
 
+// x as three numbers of 8 bits each, whose sum it is; not finite: NaN.
+template <int V>
+__device__ __forceinline__ void split(const float (&x)[V], Pack<bf16, V> (&out)[3]) {
+    float rest[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) rest[j] = x[j];
+#pragma unroll
+    for (int p = 0; p < 3; ++p) {
+        out[p] = narrow_pack<bf16>(rest);
+#pragma unroll
+        for (int j = 0; j < V; ++j) rest[j] -= widen(out[p].at(j));
+    }
+}
+
+// Floats laid out likewise, in three planes.
+__global__ __launch_bounds__(256) void k_split_rows(LayArgs p) {
+    constexpr int V = 8;
+    const uint32_t rows = p.count ? *p.count : p.rows;
+    const uint32_t pieces = p.to_stride / V;
+    for (uint32_t r = blockIdx.x * blockDim.y + threadIdx.y; r < rows; r += gridDim.x * blockDim.y) {
+        const float *from = static_cast<const float *>(p.from) + (p.list ? p.list[r] : r) * p.stride;
+        bf16 *to = static_cast<bf16 *>(p.to) + uint64_t(r) * p.to_stride;
+        for (uint32_t i = threadIdx.x; i < pieces; i += blockDim.x) {
+            const uint32_t c = i * V;
+            const Pack<float, V> q = c < p.width ? load_pack<V>(from + c, p.width - c, 0.0f) : Pack<float, V>{};
+            float x[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j) x[j] = q.at(j);
+            Pack<bf16, V> planes[3];
+            split(x, planes);
+#pragma unroll
+            for (int k = 0; k < 3; ++k) store_pack<V>(to + k * p.plane + c, planes[k]);
+        }
+    }
+}
+
 // ---------------------------------------------------------------------------
 // Products over tiles.
 // ---------------------------------------------------------------------------
 
-// The weights of the piece at hand.
-template <typename T>
+// The weights of the piece at hand, packed hidden states and g; S is the type they are held in, P the planes.
+template <typename S, int P>
 __device__ __forceinline__ Operand weight_rows(const HeadArgs &p) {
     const uint32_t rows = min(p.piece, p.classes - p.first);
-    if (p.weight_laid)
-        return {static_cast<const char *>(p.weight_laid), uint64_t(p.width_pad) * sizeof(T), rows,
-                uint32_t(p.width_pad * sizeof(T) / 16)};
-    return {static_cast<const char *>(p.weight) + uint64_t(p.first) * p.weight_stride * sizeof(T),
-            p.weight_stride * sizeof(T), rows, uint32_t(p.width * sizeof(T) / 16)};
+    if (P > 1 || p.weight_laid)
+        return {static_cast<const char *>(p.weight_laid), uint64_t(p.width_pad) * sizeof(S),
+                uint64_t(p.piece) * p.width_pad * sizeof(S), rows, uint32_t(p.width_pad * sizeof(S) / 16)};
+    return {static_cast<const char *>(p.weight) + uint64_t(p.first) * p.weight_stride * sizeof(S),
+            p.weight_stride * sizeof(S), 0, rows, uint32_t(p.width * sizeof(S) / 16)};
 }
-template <typename T>
+template <typename S>
 __device__ __forceinline__ Operand hidden_rows(const HeadArgs &p, uint32_t rows) {
-    return {static_cast<const char *>(p.packed), uint64_t(p.width_pad) * sizeof(T), rows,
-            uint32_t(p.width_pad * sizeof(T) / 16)};
+    return {static_cast<const char *>(p.packed), uint64_t(p.width_pad) * sizeof(S),
+            uint64_t(p.n_pad) * p.width_pad * sizeof(S), rows, uint32_t(p.width_pad * sizeof(S) / 16)};
 }
-template <typename T>
+template <typename S>
 __device__ __forceinline__ Operand slope_rows(const HeadArgs &p, const void *at, uint32_t rows) {
-    return {static_cast<const char *>(at), uint64_t(p.piece) * sizeof(T), rows, uint32_t(p.piece * sizeof(T) / 16)};
+    return {static_cast<const char *>(at), uint64_t(p.piece) * sizeof(S), uint64_t(p.n_pad) * p.piece * sizeof(S), rows,
+            uint32_t(p.piece * sizeof(S) / 16)};
 }
+// The type that T is held in for a tile.
+template <typename T, typename Tile>
+using Held = std::conditional_t<Tile::kPlanes == 3, bf16, T>;
 
 // Sums of 2^(c x - M) of the packed rows over a tile's classes, one for each
 // wave's classes, and c x of the labels.
 template <typename T, typename Tile>
 __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_sums(HeadArgs p) {
+    typedef Held<T, Tile> S;
     __shared__ __attribute__((aligned(1024))) typename Tile::Buffer even, odd;
     const uint32_t count = *p.count, tiles_n = (count + Tile::BN - 1) / Tile::BN;
     const uint32_t rows = min(p.piece, p.classes - p.first), tiles_m = (rows + Tile::BM - 1) / Tile::BM;
     if (blockIdx.x >= uint64_t(tiles_m) * tiles_n) return;
     const TilePlace at = tile_place(blockIdx.x, tiles_m, tiles_n);
     Tile tile;
-    tile.template run<false, false>(weight_rows<T>(p), at.m * Tile::BM, hidden_rows<T>(p, p.n_pad), at.n * Tile::BN, 0,
-                                    p.width_pad / kStep<T>, even, odd);
+    tile.template run<false, false>(weight_rows<S, Tile::kPlanes>(p), at.m * Tile::BM, hidden_rows<S>(p, p.n_pad),
+                                    at.n * Tile::BN, 0, p.width_pad / Tile::kStep, even, odd);
     const bool edge = (at.m + 1) * Tile::BM > rows;
     const uint32_t part = (p.first / Tile::BM + at.m) * Tile::WM + tile.wave / Tile::WN;
 #pragma unroll
@@ -376,14 +418,15 @@ __global__ __launch_bounds__(1024) void k_head_join(HeadArgs p) {
 // g of a piece of the vocabulary.
 template <typename T, typename Tile>
 __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_slopes(HeadArgs p) {
+    typedef Held<T, Tile> S;
     __shared__ __attribute__((aligned(1024))) typename Tile::Buffer even, odd;
     const uint32_t count = *p.count, tiles_n = (count + Tile::BN - 1) / Tile::BN, tiles_m = p.piece / Tile::BM;
     if (blockIdx.x >= uint64_t(tiles_m) * tiles_n) return;
     const TilePlace at = tile_place(blockIdx.x, tiles_m, tiles_n);
     const uint32_t rows = min(p.piece, p.classes - p.first);
     Tile tile;
-    tile.template run<false, false>(weight_rows<T>(p), at.m * Tile::BM, hidden_rows<T>(p, p.n_pad), at.n * Tile::BN, 0,
-                                    p.width_pad / kStep<T>, even, odd);
+    tile.template run<false, false>(weight_rows<S, Tile::kPlanes>(p), at.m * Tile::BM, hidden_rows<S>(p, p.n_pad),
+                                    at.n * Tile::BN, 0, p.width_pad / Tile::kStep, even, odd);
     const float common = p.inverse ? 1.0f / p.inverse[p.n_pad] : 1.0f;
 #pragma unroll
     for (int j = 0; j < Tile::TN; ++j) {
@@ -402,8 +445,15 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_slope
                 if (int32_t(p.first + v + q) == r.y) g[q] += r.a;
                 if (!real || v + q >= rows) g[q] = 0.0f;
             }
-            if (p.slope)
-                store_pack<4>(static_cast<T *>(p.slope) + uint64_t(n) * p.piece + v, narrow_pack<T>(g));
+            S *to = static_cast<S *>(p.slope) + uint64_t(n) * p.piece + v;
+            if constexpr (Tile::kPlanes == 3) {
+                Pack<bf16, 4> planes[3];
+                split(g, planes);
+#pragma unroll
+                for (int k = 0; k < 3; ++k) store_pack<4>(to + k * uint64_t(p.n_pad) * p.piece, planes[k]);
+            } else if (p.slope) {
+                store_pack<4>(to, narrow_pack<T>(g));
+            }
             if (__is_same(T, f16) && p.slope_common) {
 #pragma unroll
                 for (int q = 0; q < 4; ++q) g[q] *= ratio;
@@ -416,14 +466,15 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_slope
 // The piece's share of dh = g w, over a split of its classes.
 template <typename T, typename Tile>
 __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_hidden(HeadArgs p) {
+    typedef Held<T, Tile> S;
     __shared__ __attribute__((aligned(1024))) typename Tile::Buffer even, odd;
     const uint32_t count = *p.count, tiles_n = (count + Tile::BN - 1) / Tile::BN;
     const uint32_t tiles_m = (p.width + Tile::BM - 1) / Tile::BM;
     if (blockIdx.x >= uint64_t(tiles_m) * tiles_n * p.splits) return;
     const TilePlace at = tile_place(blockIdx.x, tiles_m, tiles_n, p.splits);
-    const uint32_t all = p.piece / kStep<T>;
+    const uint32_t all = p.piece / Tile::kStep;
     Tile tile;
-    tile.template run<true, false>(weight_rows<T>(p), at.m * Tile::BM, slope_rows<T>(p, p.slope, p.n_pad),
+    tile.template run<true, false>(weight_rows<S, Tile::kPlanes>(p), at.m * Tile::BM, slope_rows<S>(p, p.slope, p.n_pad),
                                    at.n * Tile::BN, min(all, at.split * p.steps), min(all, (at.split + 1) * p.steps),
                                    even, odd);
 #pragma unroll
@@ -468,14 +519,15 @@ __global__ __launch_bounds__(256) void k_head_hidden_join(HeadArgs p) {
 // The piece's rows of dw = g^T h.
 template <typename T, typename Tile>
 __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_weight(HeadArgs p) {
+    typedef Held<T, Tile> S;
     __shared__ __attribute__((aligned(1024))) typename Tile::Buffer even, odd;
     const uint32_t count = *p.count, rows = min(p.piece, p.classes - p.first);
     const uint32_t tiles_m = (p.width + Tile::BM - 1) / Tile::BM, tiles_n = (rows + Tile::BN - 1) / Tile::BN;
     const TilePlace at = tile_place(blockIdx.x, tiles_m, tiles_n);
     const void *slope = __is_same(T, f16) ? p.slope_common : p.slope;
     Tile tile;
-    tile.template run<true, true>(hidden_rows<T>(p, count), at.m * Tile::BM, slope_rows<T>(p, slope, count),
-                                  at.n * Tile::BN, 0, (count + kStep<T> - 1) / kStep<T>, even, odd);
+    tile.template run<true, true>(hidden_rows<S>(p, count), at.m * Tile::BM, slope_rows<S>(p, slope, count),
+                                  at.n * Tile::BN, 0, (count + Tile::kStep - 1) / Tile::kStep, even, odd);
     const float back = p.inverse ? p.inverse[p.n_pad] : 1.0f;
 #pragma unroll
     for (int j = 0; j < Tile::TN; ++j) {

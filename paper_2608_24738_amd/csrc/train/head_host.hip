@@ -18,6 +18,7 @@ constexpr uint64_t kMaxWidth = uint64_t(1) << 24;
 constexpr uint64_t kPieceBytes = uint64_t(1) << 27;     // of one layout of g
 constexpr uint64_t kLaidBytes = uint64_t(1) << 28;      // of weights laid out in whole steps
 constexpr uint64_t kCus = 256;
+constexpr uint64_t kPlaneRows = 128;
 
 struct HeadShape {
     uint64_t n, classes, width, size;
@@ -71,14 +72,27 @@ uint64_t whole_tiles(uint64_t n) { return ceil_div(n, kTilePad) * kTilePad; }
 
 bool few(const HeadShape &s) { return s.n <= kFewRows; }
 
-// Largest tiles, unless they leave CUs without one; `most` is how often k can be split.
-bool large_tiles(uint64_t m, uint64_t n, uint64_t most = 1) {
-    return ceil_div(m, 256) * ceil_div(n, 256) * most >= kCus;
+// Floats go to the matrix cores as three 16-bit planes, unless the rows are few.
+bool planes(const HeadShape &s) { return s.size == 4 && s.n > kPlaneRows; }
+
+// fn(tile): the larger of two, unless it leaves CUs without one; `most` is how
+// often k can be split.
+template <typename T, typename F>
+auto by_tile(const HeadShape &s, uint64_t m, uint64_t n, uint64_t most, F fn) {
+    const bool large = ceil_div(m, 256) * ceil_div(n, planes(s) ? 128 : 256) * most >= kCus;
+    if (std::is_same<T, float>::value && planes(s))
+        return large ? fn(static_cast<LargeSplit *>(nullptr)) : fn(static_cast<SmallSplit *>(nullptr));
+    return large ? fn(static_cast<LargeTile<T> *>(nullptr)) : fn(static_cast<SmallTile<T> *>(nullptr));
+}
+// The same where the type does not matter: all have tiles of one size but for the planes.
+template <typename F>
+auto by_tile_size(const HeadShape &s, uint64_t m, uint64_t n, uint64_t most, F fn) {
+    return by_tile<float>(s, m, n, most, fn);
 }
 
-// Tiles read whole 16-byte pieces of the weight, from addresses of 16 bytes.
-bool lies_well(const void *p, uint64_t stride, const HeadShape &s) {
-    return uintptr_t(p) % 16 == 0 && stride * s.size % 16 == 0 && s.width * s.size % 16 == 0;
+// Tiles read whole 16-byte pieces of the weight, from addresses of 16 bytes: whether it is to be laid out for them.
+bool to_lay(const void *p, uint64_t stride, const HeadShape &s) {
+    return !few(s) && (planes(s) || uintptr_t(p) % 16 || stride * s.size % 16 || s.width * s.size % 16);
 }
 
 // Classes of a piece, in whole tiles, so that `bytes` hold a row of `each` for every class.
@@ -91,10 +105,13 @@ void head_sizes(const HeadShape &s, HeadArgs &a) {
     a.n = uint32_t(s.n);
     a.classes = uint32_t(s.classes);
     a.width = uint32_t(s.width);
-    const uint64_t step = kStepBytes / s.size;
+    const uint64_t step = s.size == 4 ? 32 : 64;
     a.width_pad = uint32_t(ceil_div(s.width, step) * step);
     a.n_pad = uint32_t(few(s) ? kFewRows : whole_tiles(s.n));
 }
+
+// Bytes of a laid out element.
+uint64_t held(const HeadShape &s) { return planes(s) ? 6 : s.size; }
 
 // Layout of the forward call's workspace; returns its size.
 uint64_t head_room(const HeadShape &s, bool laid, void *at, HeadArgs &a) {
@@ -106,15 +123,17 @@ uint64_t head_room(const HeadShape &s, bool laid, void *at, HeadArgs &a) {
         a.part = room.take<HeadSum>(uint64_t(a.parts) * a.n);
         return room.used;
     }
-    const bool large = large_tiles(s.classes, s.n);
-    a.parts = uint32_t(ceil_div(s.classes, large ? 256 : 128) * 2);
-    a.piece = uint32_t(laid ? piece_of(s.classes, a.width_pad * s.size, kLaidBytes) : whole_tiles(s.classes));
+    a.parts = by_tile_size(s, s.classes, s.n, 1, [&](auto *t) {
+        using Tile = std::remove_pointer_t<decltype(t)>;
+        return uint32_t(ceil_div(s.classes, Tile::BM) * Tile::WM);
+    });
+    a.piece = uint32_t(laid ? piece_of(s.classes, a.width_pad * held(s), kLaidBytes) : whole_tiles(s.classes));
     a.count = room.take<uint32_t>(1);
     a.chunk_count = room.take<uint32_t>(2 * ceil_div(s.n, kListChunk));
     a.list = room.take<uint32_t>(a.n_pad);
-    a.packed = room.take<char>(uint64_t(a.n_pad) * a.width_pad * s.size);
+    a.packed = room.take<char>(uint64_t(a.n_pad) * a.width_pad * held(s));
     a.part = room.take<HeadSum>(uint64_t(a.parts) * a.n_pad);
-    if (laid) a.weight_laid = room.take<char>(uint64_t(a.piece) * a.width_pad * s.size);
+    if (laid) a.weight_laid = room.take<char>(uint64_t(a.piece) * a.width_pad * held(s));
     return room.used;
 }
 
@@ -140,13 +159,17 @@ uint64_t head_grad_room(const HeadShape &s, int dtype, bool laid, bool hidden, b
         if (hidden) a.sum = room.take<float>(uint64_t(a.splits) * s.n * a.sum_stride);
         return room.used;
     }
-    a.piece = uint32_t(piece_of(s.classes, a.n_pad * s.size, kPieceBytes));
+    a.piece = uint32_t(piece_of(s.classes, a.n_pad * held(s), kPieceBytes));
     a.sum_stride = uint32_t(ceil_div(s.width, 4) * 4);
-    // splits that give every CU a tile (two of the small ones), each of 8 steps at least
-    const uint64_t steps = a.piece * s.size / kStepBytes, most = std::max<uint64_t>(1, std::min<uint64_t>(steps / 8, 32));
-    a.large = large_tiles(s.width, s.n, most);
-    const uint64_t side = a.large ? 256 : 128, tiles = ceil_div(s.width, side) * ceil_div(s.n, side);
-    const uint64_t splits = std::max<uint64_t>(1, std::min(most, (a.large ? kCus : 2 * kCus) / tiles));
+    // splits that give every CU a tile (two of the small ones, unless they fill its LDS), each of 8 steps at least
+    const uint64_t steps = a.piece / (s.size == 4 ? 32 : 64);
+    const uint64_t most = std::max<uint64_t>(1, std::min<uint64_t>(steps / 8, 32));
+    a.most = uint32_t(most);
+    const uint64_t splits = by_tile_size(s, s.width, s.n, most, [&](auto *t) {
+        using Tile = std::remove_pointer_t<decltype(t)>;
+        const uint64_t tiles = ceil_div(s.width, Tile::BM) * ceil_div(s.n, Tile::BN);
+        return std::max<uint64_t>(1, std::min(most, (Tile::kWaves == 4 ? 2 : 1) * kCus / tiles));
+    });
     a.steps = uint32_t(ceil_div(steps, splits));
     a.splits = uint32_t(ceil_div(steps, a.steps));
     a.count = room.take<uint32_t>(1);
@@ -155,19 +178,13 @@ uint64_t head_grad_room(const HeadShape &s, int dtype, bool laid, bool hidden, b
     a.place = room.take<int32_t>(a.n_pad);
     a.row = room.take<HeadRow>(a.n_pad);
     if (dtype == TM_DTYPE_F16) a.inverse = room.take<float>(a.n_pad + 1);
-    a.packed = room.take<char>(uint64_t(a.n_pad) * a.width_pad * s.size);
-    const uint64_t slopes = uint64_t(a.n_pad) * a.piece * s.size;
+    a.packed = room.take<char>(uint64_t(a.n_pad) * a.width_pad * held(s));
+    const uint64_t slopes = uint64_t(a.n_pad) * a.piece * held(s);
     if (hidden || dtype != TM_DTYPE_F16) a.slope = room.take<char>(slopes);
     if (weight && dtype == TM_DTYPE_F16) a.slope_common = room.take<char>(slopes);
     if (hidden) a.sum = room.take<float>(uint64_t(a.splits) * a.n_pad * a.sum_stride);
-    if (laid) a.weight_laid = room.take<char>(uint64_t(a.piece) * a.width_pad * s.size);
+    if (laid) a.weight_laid = room.take<char>(uint64_t(a.piece) * a.width_pad * held(s));
     return room.used;
-}
-
-// fn(tile)
-template <typename T, typename F>
-int by_tile(bool large, F fn) {
-    return large ? fn(static_cast<LargeTile<T> *>(nullptr)) : fn(static_cast<SmallTile<T> *>(nullptr));
 }
 
 template <typename Tile>
@@ -175,37 +192,48 @@ dim3 tile_grid(uint64_t m, uint64_t n) {
     return dim3(uint32_t(ceil_div(m, Tile::BM) * ceil_div(n, Tile::BN)));
 }
 
+// Rows laid out in whole steps, or in planes.
+template <typename T>
+int lay(const HeadShape &s, LayArgs l, hipStream_t stream) {
+    const bool split = std::is_same<T, float>::value && planes(s);
+    const uint32_t x = std::min<uint32_t>(256, pow2_from(uint32_t(ceil_div(uint64_t(l.to_stride) * (split ? 2 : sizeof(T)), 16))));
+    const dim3 block(x, 256 / x), grid(uint32_t(std::min<uint64_t>(ceil_div(l.rows, block.y), 4096)));
+    return launch(split ? k_split_rows : k_lay_rows<T>, grid, block, 0, stream, l);
+}
+
 // The list of packed rows, and the rows.
 template <typename T>
-int pack_rows(const HeadArgs &a, hipStream_t stream) {
+int pack_rows(const HeadShape &s, const HeadArgs &a, hipStream_t stream) {
     const uint32_t chunks = uint32_t(ceil_div(a.n, kListChunk));
     int rc = TM_OK;
     if (chunks > 1) rc = launch(k_head_count, dim3(chunks), dim3(1024), 0, stream, a);
     if (rc == TM_OK) rc = launch(k_head_list, dim3(chunks), dim3(1024), 0, stream, a);
     if (rc != TM_OK) return rc;
-    LayArgs lay{};
-    lay.from = a.hidden;
-    lay.stride = a.hidden_stride;
-    lay.list = a.list;
-    lay.count = a.count;
-    lay.rows = a.n;
-    lay.width = a.width;
-    lay.to = a.packed;
-    lay.to_stride = a.width_pad;
-    return launch(k_lay_rows<T>, dim3(std::min(a.n, 4096u)), dim3(256), 0, stream, lay);
+    LayArgs l{};
+    l.from = a.hidden;
+    l.stride = a.hidden_stride;
+    l.list = a.list;
+    l.count = a.count;
+    l.rows = a.n;
+    l.width = a.width;
+    l.to = a.packed;
+    l.to_stride = a.width_pad;
+    l.plane = uint64_t(a.n_pad) * a.width_pad;
+    return lay<T>(s, l, stream);
 }
 
-// The weights of the piece at hand in whole steps.
+// The weights of the piece at hand.
 template <typename T>
-int lay_piece(const HeadArgs &a, hipStream_t stream) {
-    LayArgs lay{};
-    lay.from = static_cast<const T *>(a.weight) + uint64_t(a.first) * a.weight_stride;
-    lay.stride = a.weight_stride;
-    lay.rows = std::min(a.piece, a.classes - a.first);
-    lay.width = a.width;
-    lay.to = a.weight_laid;
-    lay.to_stride = a.width_pad;
-    return launch(k_lay_rows<T>, dim3(std::min(lay.rows, 4096u)), dim3(256), 0, stream, lay);
+int lay_piece(const HeadShape &s, const HeadArgs &a, hipStream_t stream) {
+    LayArgs l{};
+    l.from = static_cast<const T *>(a.weight) + uint64_t(a.first) * a.weight_stride;
+    l.stride = a.weight_stride;
+    l.rows = std::min(a.piece, a.classes - a.first);
+    l.width = a.width;
+    l.to = a.weight_laid;
+    l.to_stride = a.width_pad;
+    l.plane = uint64_t(a.piece) * a.width_pad;
+    return lay<T>(s, l, stream);
 }
 
 template <typename T>
@@ -214,13 +242,13 @@ int run_head(HeadArgs a, const HeadShape &s, hipStream_t stream) {
         const int rc = launch(k_few_sums<T>, dim3(a.parts), dim3(64 * kFewWaves), 0, stream, a);
         return rc == TM_OK ? launch(k_few_rows, dim3(a.n), dim3(256), 0, stream, a) : rc;
     }
-    int rc = pack_rows<T>(a, stream);
+    int rc = pack_rows<T>(s, a, stream);
     for (uint64_t first = 0; rc == TM_OK && first < s.classes; first += a.piece) {
         a.first = uint32_t(first);
-        if (a.weight_laid) rc = lay_piece<T>(a, stream);
+        if (a.weight_laid) rc = lay_piece<T>(s, a, stream);
         if (rc != TM_OK) break;
         // the tile is that of all classes: it says how many parts there are
-        rc = by_tile<T>(large_tiles(s.classes, s.n), [&](auto *t) {
+        rc = by_tile<T>(s, s.classes, s.n, 1, [&](auto *t) {
             using Tile = std::remove_pointer_t<decltype(t)>;
             return launch(k_head_sums<T, Tile>, tile_grid<Tile>(std::min<uint64_t>(a.piece, s.classes - first), s.n),
                           dim3(Tile::kThreads), 0, stream, a);
@@ -245,18 +273,18 @@ int run_few_grad(const HeadArgs &a, const HeadShape &s, hipStream_t stream) {
 template <typename T>
 int run_head_grad(HeadArgs a, const HeadShape &s, hipStream_t stream) {
     if (few(s)) return run_few_grad<T>(a, s, stream);
-    int rc = pack_rows<T>(a, stream);
+    int rc = pack_rows<T>(s, a, stream);
     for (uint64_t first = 0; rc == TM_OK && first < s.classes; first += a.piece) {
         a.first = uint32_t(first);
         a.add = first > 0;
-        if (a.weight_laid) rc = lay_piece<T>(a, stream);
+        if (a.weight_laid) rc = lay_piece<T>(s, a, stream);
         if (rc != TM_OK) break;
-        rc = by_tile<T>(large_tiles(a.piece, s.n), [&](auto *t) {
+        rc = by_tile<T>(s, a.piece, s.n, 1, [&](auto *t) {
             using Tile = std::remove_pointer_t<decltype(t)>;
             return launch(k_head_slopes<T, Tile>, tile_grid<Tile>(a.piece, s.n), dim3(Tile::kThreads), 0, stream, a);
         });
         if (rc == TM_OK && a.grad_hidden) {
-            rc = by_tile<T>(a.large, [&](auto *t) {
+            rc = by_tile<T>(s, s.width, s.n, a.most, [&](auto *t) {
                 using Tile = std::remove_pointer_t<decltype(t)>;
                 return launch(k_head_hidden<T, Tile>, dim3(tile_grid<Tile>(s.width, s.n).x * a.splits),
                               dim3(Tile::kThreads), 0, stream, a);
@@ -264,7 +292,7 @@ int run_head_grad(HeadArgs a, const HeadShape &s, hipStream_t stream) {
         }
         if (rc == TM_OK && a.grad_weight) {
             const uint64_t rows = std::min<uint64_t>(a.piece, s.classes - first);
-            rc = by_tile<T>(large_tiles(s.width, rows), [&](auto *t) {
+            rc = by_tile<T>(s, s.width, rows, 1, [&](auto *t) {
                 using Tile = std::remove_pointer_t<decltype(t)>;
                 return launch(k_head_weight<T, Tile>, tile_grid<Tile>(s.width, rows), dim3(Tile::kThreads), 0, stream, a);
             });
@@ -315,7 +343,7 @@ extern "C" int tm_head_logp(const void *hidden, int dtype, int64_t rows, int64_t
     if (aliased(in, out)) return TM_ERR_ALIAS;
     HeadArgs a{};
     head_args(s, hidden, hidden_stride, weight, weight_stride, labels, scale, a);
-    head_room(s, !few(s) && !lies_well(weight, a.weight_stride, s), workspace, a);
+    head_room(s, to_lay(weight, a.weight_stride, s), workspace, a);
     a.all = out_log_sum != nullptr;
     a.logp = out_logp;
     a.log_sum = out_log_sum;
@@ -359,7 +387,7 @@ extern "C" int tm_head_logp_grad(const void *hidden, int dtype, int64_t rows, in
     }
     HeadArgs a{};
     head_args(s, hidden, hidden_stride, weight, weight_stride, labels, scale, a);
-    head_grad_room(s, dtype, !few(s) && !lies_well(weight, a.weight_stride, s), out_hidden != nullptr,
+    head_grad_room(s, dtype, to_lay(weight, a.weight_stride, s), out_hidden != nullptr,
                    out_weight != nullptr, workspace, a);
     a.all = up_log_sum != nullptr;
     a.stats = reinterpret_cast<HeadSum *>(const_cast<float *>(stats));

@@ -25,6 +25,7 @@
 #pragma once
 
 #include <type_traits>
+#include <utility>
 
 #include "train_common.h"
 
@@ -33,11 +34,7 @@ namespace tmtrain {
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr uint32_t kStepBytes = 128;            // of a row, in one step
 constexpr uint32_t kTilePad = 256;              // rows of laid out operands come in whole largest tiles
-
-template <typename T>
-constexpr uint32_t kStep = kStepBytes / sizeof(T);
 
 // acc += the products over one piece of k.
 template <typename T>
@@ -88,51 +85,54 @@ __device__ __forceinline__ TilePlace tile_place(uint32_t block, uint32_t tiles_m
 // One operand: rows `stride` bytes apart, 16-byte aligned.
 struct Operand {
     const char *at;
-    uint64_t stride;
+    uint64_t stride, plane;     // plane: bytes from one plane to the next
     uint32_t rows;              // along k: rows beyond are read as the last one; across: as zeros
     uint32_t pieces;            // whole pieces in a row; along k: beyond them zeros, across: anything
 };
 
-// Copies of an operand's steps to LDS, S elements of m or n by Waves waves.
-template <typename T, int S, int Waves>
+// Copies of an operand's steps to LDS, S elements of m or n by Waves waves, K
+// elements of k a step (one or two instructions' worth).
+template <typename T, int S, int Waves, int K>
 struct Along {
-    static constexpr int kCopies = S / 8 / Waves;
+    static constexpr uint32_t kRow = K * sizeof(T), kPieces = kRow / 16;    // 8 or 4 pieces in a row
+    static constexpr uint32_t kAtOnce = 64 / kPieces;                       // rows of one copy
+    static constexpr int kCopies = S / kAtOnce / Waves;
     const char *from[kCopies];
-    uint32_t piece, pieces;
+    uint32_t piece, pieces, place;
 
+    static __device__ __forceinline__ uint32_t order(uint32_t r) { return kPieces == 8 ? r & 7 : r >> 2 & 3; }
     __device__ __forceinline__ Along(const Operand &o, uint32_t m0, uint32_t first, int lane, int wave) {
-        const uint32_t r = lane >> 3;
-        piece = (lane & 7) ^ r;
+        const uint32_t r = lane / kPieces;
+        piece = lane % kPieces ^ order(r);
         pieces = o.pieces;
 #pragma unroll
         for (int i = 0; i < kCopies; ++i)
-            from[i] = o.at + min(m0 + (i * Waves + wave) * 8 + r, o.rows - 1) * o.stride + first * kStepBytes + piece * 16;
+            from[i] = o.at + min(m0 + (i * Waves + wave) * kAtOnce + r, o.rows - 1) * o.stride + first * kRow + piece * 16;
     }
-    __device__ __forceinline__ void fetch(char *lds, uint32_t step, int wave) {
-        if (step == pieces / 8) {               // the step that rows end in
+    __device__ __forceinline__ void fetch(char *lds, uint32_t step, int, int wave) {
+        if (step == pieces / kPieces) {         // the step that rows end in
 #pragma unroll
             for (int i = 0; i < kCopies; ++i)
-                from[i] = step * 8 + piece < pieces ? from[i] : reinterpret_cast<const char *>(kZeroPiece);
+                from[i] = step * kPieces + piece < pieces ? from[i] : reinterpret_cast<const char *>(kZeroPiece);
         }
 #pragma unroll
         for (int i = 0; i < kCopies; ++i) {
             copy_to_lds(from[i], lds + (i * Waves + wave) * 1024);
-            from[i] += kStepBytes;
+            from[i] += kRow;
         }
     }
     // Where the lane's reads of block 0 begin, and the 16 bytes of block i in half of a step.
-    uint32_t place;
     __device__ __forceinline__ void reads(int lane, uint32_t block) {
-        place = (block * 16 + (lane & 15)) * kStepBytes + (((lane >> 4) ^ (lane & 7)) * 16);
+        place = (block * 16 + (lane & 15)) * kRow + (((lane >> 4) ^ order(lane & 15)) * 16);
     }
     __device__ __forceinline__ u32x4 read(const char *lds, int i, int half) const {
-        return *reinterpret_cast<const u32x4 *>(lds + (half ? place ^ 64 : place) + i * 16 * kStepBytes);
+        return *reinterpret_cast<const u32x4 *>(lds + (half ? place ^ 64 : place) + i * 16 * kRow);
     }
 };
 
-template <typename T, int S, int Waves, int Blocks>
+template <typename T, int S, int Waves, int K, int Blocks>
 struct Across {
-    static constexpr int kCopies = S / 8 / Waves;
+    static constexpr int kCopies = S * K * int(sizeof(T)) / 1024 / Waves;
     static constexpr uint32_t kRow = S * sizeof(T), kPieces = kRow / 16;    // of a row in LDS
     static constexpr uint32_t kUnits = S / 16;                              // of 16 elements
     const char *from[kCopies];
@@ -155,19 +155,19 @@ struct Across {
         for (int i = 0; i < kCopies; ++i) {
             const uint32_t r = row_of(i, lane, wave);
             const uint32_t piece = m0 * sizeof(T) / 16 + (lane % kPieces ^ order(r) * kUnitPieces);
-            from[i] = o.at + (uint64_t(first) * kStep<T> + r) * stride + min(piece, o.pieces - 1) * 16;
+            from[i] = o.at + (uint64_t(first) * K + r) * stride + min(piece, o.pieces - 1) * 16;
         }
     }
     __device__ __forceinline__ void fetch(char *lds, uint32_t step, int lane, int wave) {
-        if ((step + 1) * kStep<T> > rows) {
+        if ((step + 1) * K > rows) {
 #pragma unroll
             for (int i = 0; i < kCopies; ++i)
-                if (step * kStep<T> + row_of(i, lane, wave) >= rows) from[i] = reinterpret_cast<const char *>(kZeroPiece);
+                if (step * K + row_of(i, lane, wave) >= rows) from[i] = reinterpret_cast<const char *>(kZeroPiece);
         }
 #pragma unroll
         for (int i = 0; i < kCopies; ++i) {
             copy_to_lds(from[i], lds + (i * Waves + wave) * 1024);
-            from[i] += kStep<T> * stride;
+            from[i] += K * stride;
         }
     }
     uint32_t place[Blocks];
@@ -203,15 +203,22 @@ struct Across {
     }
 };
 
-// BM x BN elements by WM x WN waves.
-template <typename T, int BM_, int BN_, int WM_, int WN_>
+// BM x BN elements by WM x WN waves.  With three planes, an operand's floats
+// are held as sums of three of T = bf16, x = h + m + l, exact since each takes
+// eight more bits, and a product is hh + hm + mh + mm + hl + lh: what is left
+// out is below 2^-23 of it, and six instructions of 16 bits take less time than
+// those of floats (head.h has the figures).
+template <typename T, int BM_, int BN_, int WM_, int WN_, int Planes = 1>
 struct Tile {
-    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, kPlanes = Planes;
     static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves;
-    static constexpr int TM = BM / WM / 16, TN = BN / WN / 16;  // 16 x 16 blocks of a wave
+    static constexpr int TM = BM / WM / 16, TN = BN / WN / 16;              // 16 x 16 blocks of a wave
+    static constexpr int kHalves = Planes == 1 ? 2 : 1;                     // instructions' worth of k in a step
+    static constexpr int kStep = kHalves * 64 / int(sizeof(T));             // elements
+    static constexpr int kPlaneA = BM * kHalves * 64, kPlaneB = BN * kHalves * 64;     // bytes of a plane's step
 
     struct Buffer {
-        char row[(BM + BN) * int(kStepBytes)];
+        char a[Planes * kPlaneA], b[Planes * kPlaneB];
     };
 
     f32x4 acc[TM][TN];
@@ -229,32 +236,58 @@ struct Tile {
     __device__ __forceinline__ uint32_t row(int i) const { return ((wave / WN) * TM + i) * 16 + (lane >> 4) * 4; }
     __device__ __forceinline__ uint32_t column(int j) const { return ((wave % WN) * TN + j) * 16 + (lane & 15); }
 
+    template <typename From>
+    struct Sources {
+        From plane[Planes];
+        template <size_t... I>
+        __device__ __forceinline__ Sources(const Operand &o, uint32_t m0, uint32_t first, int lane, int wave,
+                                           std::index_sequence<I...>)
+            : plane{From({o.at + I * o.plane, o.stride, 0, o.rows, o.pieces}, m0, first, lane, wave)...} {}
+    };
+
     // Adds the products of m0.. of A and n0.. of B over steps [first, last).
     template <bool AAcross, bool BAcross>
     __device__ __forceinline__ void run(const Operand &a, uint32_t m0, const Operand &b, uint32_t n0, uint32_t first,
                                         uint32_t last, Buffer &even, Buffer &odd) {
         if (first >= last) return;
-        constexpr uint32_t kBehind = BM * kStepBytes;           // where B's part of a buffer begins
-        std::conditional_t<AAcross, Across<T, BM, kWaves, TM>, Along<T, BM, kWaves>> from_a(a, m0, first, lane, wave);
-        std::conditional_t<BAcross, Across<T, BN, kWaves, TN>, Along<T, BN, kWaves>> from_b(b, n0, first, lane, wave);
-        from_a.reads(lane, (wave / WN) * TM);
-        from_b.reads(lane, (wave % WN) * TN);
+        typedef std::conditional_t<AAcross, Across<T, BM, kWaves, kStep, TM>, Along<T, BM, kWaves, kStep>> FromA;
+        typedef std::conditional_t<BAcross, Across<T, BN, kWaves, kStep, TN>, Along<T, BN, kWaves, kStep>> FromB;
+        Sources<FromA> from_a(a, m0, first, lane, wave, std::make_index_sequence<Planes>{});
+        Sources<FromB> from_b(b, n0, first, lane, wave, std::make_index_sequence<Planes>{});
+        from_a.plane[0].reads(lane, (wave / WN) * TM);
+        from_b.plane[0].reads(lane, (wave % WN) * TN);
         const auto fetch = [&](Buffer &s, uint32_t step) {
-            if constexpr (AAcross) from_a.fetch(s.row, step, lane, wave); else from_a.fetch(s.row, step, wave);
-            if constexpr (BAcross) from_b.fetch(s.row + kBehind, step, lane, wave); else from_b.fetch(s.row + kBehind, step, wave);
+#pragma unroll
+            for (int p = 0; p < Planes; ++p) {
+                from_a.plane[p].fetch(s.a + p * kPlaneA, step, lane, wave);
+                from_b.plane[p].fetch(s.b + p * kPlaneB, step, lane, wave);
+            }
         };
         const auto work = [&](const Buffer &s) {
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                u32x4 fa[TM], fb[TN];
+            for (int half = 0; half < kHalves; ++half) {
+                u32x4 fa[Planes][TM], fb[Planes][TN];
 #pragma unroll
-                for (int i = 0; i < TM; ++i) fa[i] = from_a.read(s.row, i, half);
+                for (int p = 0; p < Planes; ++p) {
 #pragma unroll
-                for (int j = 0; j < TN; ++j) fb[j] = from_b.read(s.row + kBehind, j, half);
+                    for (int i = 0; i < TM; ++i) fa[p][i] = from_a.plane[0].read(s.a + p * kPlaneA, i, half);
 #pragma unroll
-                for (int i = 0; i < TM; ++i)
+                    for (int j = 0; j < TN; ++j) fb[p][j] = from_b.plane[0].read(s.b + p * kPlaneB, j, half);
+                }
+                const auto add = [&](int pa, int pb) {
 #pragma unroll
-                    for (int j = 0; j < TN; ++j) acc[i][j] = multiply<T>(fa[i], fb[j], acc[i][j]);
+                    for (int i = 0; i < TM; ++i)
+#pragma unroll
+                        for (int j = 0; j < TN; ++j) acc[i][j] = multiply<T>(fa[pa][i], fb[pb][j], acc[i][j]);
+                };
+                add(0, 0);
+                if constexpr (Planes == 3) {
+                    add(0, 1);
+                    add(1, 0);
+                    add(1, 1);
+                    add(0, 2);
+                    add(2, 0);
+                }
             }
         };
         fetch(even, first);
@@ -271,5 +304,7 @@ struct Tile {
 
 template <typename T> using LargeTile = Tile<T, 256, 256, 2, 4>;
 template <typename T> using SmallTile = Tile<T, 128, 128, 2, 2>;
+typedef Tile<bf16, 256, 128, 4, 2, 3> LargeSplit;
+typedef Tile<bf16, 128, 128, 4, 2, 3> SmallSplit;
 
 }  // namespace tmtrain

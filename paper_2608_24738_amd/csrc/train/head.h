@@ -74,12 +74,13 @@ struct HeadArgs {
     float *found;               // c h w of the packed rows' labels
     void *slope, *slope_common; // g [n_pad][piece]; float16: times its row's power of two, and the common one
     void *weight_laid;          // a piece's weights in whole steps, where they do not lie so
-    float *sum;                 // [splits][n_pad][sum_stride]
+    float *sum;                 // dh by splits: [splits][rows of tiles][sum_stride]; few rows: [splits][n][sum_stride]
     uint32_t n_pad, width_pad, sum_stride;
     uint32_t parts;
     uint32_t first, piece;      // classes of the piece at hand, and its width
-    uint32_t splits, steps;     // of the product for dh
-    uint32_t most;              // splits that its k allows
+    uint32_t splits, steps;     // few rows: shares of the classes, and classes of one
+    uint32_t blocks, most;      // of the product for dh: workgroups, splits that its k allows
+    uint32_t tiles_m, tile_n;   // its tiles across the width, and the rows of one
     bool add;                   // to the sums so far
 };
 
@@ -339,13 +340,17 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_sums(
                                     at.n * Tile::BN, 0, p.width_pad / Tile::kStep, even, odd);
     const bool edge = (at.m + 1) * Tile::BM > rows;
     const uint32_t part = (p.first / Tile::BM + at.m) * Tile::WM + tile.wave / Tile::WN;
+    uint32_t wants[Tile::TN];                       // the labels' rows in the tile
 #pragma unroll
     for (int j = 0; j < Tile::TN; ++j) {
         const uint32_t n = at.n * Tile::BN + tile.column(j);
+        const int32_t y = n < count && p.label ? load_label(p.label, p.label_bytes, p.list[n], p.classes) : -1;
+        wants[j] = y < 0 ? ~0u : uint32_t(y) - p.first - at.m * Tile::BM;
+    }
+#pragma unroll
+    for (int j = 0; j < Tile::TN; ++j) {
+        const uint32_t n = at.n * Tile::BN + tile.column(j), want = wants[j];
         const bool real = n < count;
-        const int32_t y = real && p.label ? load_label(p.label, p.label_bytes, p.list[n], p.classes) : -1;
-        // the label's row in the tile
-        const uint32_t want = y < 0 ? ~0u : uint32_t(y) - p.first - at.m * Tile::BM;
         float most = -INFINITY, label = 0.0f;
 #pragma unroll
         for (int i = 0; i < Tile::TM; ++i)
@@ -427,14 +432,21 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_slope
     Tile tile;
     tile.template run<false, false>(weight_rows<S, Tile::kPlanes>(p), at.m * Tile::BM, hidden_rows<S>(p, p.n_pad),
                                     at.n * Tile::BN, 0, p.width_pad / Tile::kStep, even, odd);
-    const float common = p.inverse ? 1.0f / p.inverse[p.n_pad] : 1.0f;
+    // What the columns need comes first: a wait for a load is one for all stores before it.
+    HeadRow row[Tile::TN];
+    float ratios[Tile::TN];
+#pragma unroll
+    for (int j = 0; j < Tile::TN; ++j) {
+        const uint32_t n = at.n * Tile::BN + tile.column(j);
+        row[j] = {0.0f, 0.0f, 0.0f, -1};
+        if (n < count) row[j] = p.row[n];
+        if constexpr (__is_same(T, f16)) ratios[j] = n < count ? p.inverse[n] / p.inverse[p.n_pad] : 1.0f;
+    }
 #pragma unroll
     for (int j = 0; j < Tile::TN; ++j) {
         const uint32_t n = at.n * Tile::BN + tile.column(j);
         const bool real = n < count;
-        HeadRow r = {0.0f, 0.0f, 0.0f, -1};
-        if (real) r = p.row[n];
-        const float ratio = p.inverse && real ? common * p.inverse[n] : 1.0f;
+        const HeadRow r = row[j];
 #pragma unroll
         for (int i = 0; i < Tile::TM; ++i) {
             const uint32_t v = at.m * Tile::BM + tile.row(i);
@@ -454,13 +466,20 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_slope
             } else if (p.slope) {
                 store_pack<4>(to, narrow_pack<T>(g));
             }
-            if (__is_same(T, f16) && p.slope_common) {
+            if constexpr (__is_same(T, f16)) {
+                if (p.slope_common) {
 #pragma unroll
-                for (int q = 0; q < 4; ++q) g[q] *= ratio;
-                store_pack<4>(static_cast<T *>(p.slope_common) + uint64_t(n) * p.piece + v, narrow_pack<T>(g));
+                    for (int q = 0; q < 4; ++q) g[q] *= ratios[j];
+                    store_pack<4>(static_cast<T *>(p.slope_common) + uint64_t(n) * p.piece + v, narrow_pack<T>(g));
+                }
             }
         }
     }
+}
+
+// Splits of the product for dh: as many as its workgroups make of the tiles that the packed rows take.
+__device__ __forceinline__ uint32_t hidden_splits(const HeadArgs &p, uint32_t tiles_n) {
+    return max(1u, min(p.most, p.blocks / max(1u, p.tiles_m * tiles_n)));
 }
 
 // The piece's share of dh = g w, over a split of its classes.
@@ -468,26 +487,32 @@ template <typename T, typename Tile>
 __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_hidden(HeadArgs p) {
     typedef Held<T, Tile> S;
     __shared__ __attribute__((aligned(1024))) typename Tile::Buffer even, odd;
-    const uint32_t count = *p.count, tiles_n = (count + Tile::BN - 1) / Tile::BN;
-    const uint32_t tiles_m = (p.width + Tile::BM - 1) / Tile::BM;
-    if (blockIdx.x >= uint64_t(tiles_m) * tiles_n * p.splits) return;
-    const TilePlace at = tile_place(blockIdx.x, tiles_m, tiles_n, p.splits);
-    const uint32_t all = p.piece / Tile::kStep;
+    const uint32_t count = *p.count, tiles_n = (count + Tile::BN - 1) / Tile::BN, splits = hidden_splits(p, tiles_n);
+    if (blockIdx.x >= p.tiles_m * tiles_n * splits) return;
+    const TilePlace at = tile_place(blockIdx.x, p.tiles_m, tiles_n, splits);
+    const uint32_t all = p.piece / Tile::kStep, steps = (all + splits - 1) / splits;
     Tile tile;
     tile.template run<true, false>(weight_rows<S, Tile::kPlanes>(p), at.m * Tile::BM, slope_rows<S>(p, p.slope, p.n_pad),
-                                   at.n * Tile::BN, min(all, at.split * p.steps), min(all, (at.split + 1) * p.steps),
+                                   at.n * Tile::BN, min(all, at.split * steps), min(all, (at.split + 1) * steps),
                                    even, odd);
 #pragma unroll
     for (int j = 0; j < Tile::TN; ++j) {
         const uint32_t n = at.n * Tile::BN + tile.column(j);
-        float *to = p.sum + (uint64_t(at.split) * p.n_pad + n) * p.sum_stride;
+        float *to = p.sum + (uint64_t(at.split) * tiles_n * Tile::BN + n) * p.sum_stride;
         if (n >= count) continue;
+        // all loads of a column before its stores
+        if (p.add) {
+            f32x4 before[Tile::TM];
+#pragma unroll
+            for (int i = 0; i < Tile::TM; ++i)
+                before[i] = *reinterpret_cast<const f32x4 *>(to + min(at.m * Tile::BM + tile.row(i), p.sum_stride - 4));
+#pragma unroll
+            for (int i = 0; i < Tile::TM; ++i) tile.acc[i][j] += before[i];
+        }
 #pragma unroll
         for (int i = 0; i < Tile::TM; ++i) {
             const uint32_t d = at.m * Tile::BM + tile.row(i);
-            if (d >= p.sum_stride) continue;
-            f32x4 *q = reinterpret_cast<f32x4 *>(to + d);
-            *q = p.add ? *q + tile.acc[i][j] : tile.acc[i][j];
+            if (d < p.sum_stride) *reinterpret_cast<f32x4 *>(to + d) = tile.acc[i][j];
         }
     }
 }
@@ -495,15 +520,19 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_hidde
 // dh of every row from the splits' sums; rows that took no part get zeros.
 template <typename T>
 __global__ __launch_bounds__(256) void k_head_hidden_join(HeadArgs p) {
-    const uint32_t quads = (p.width + 3) / 4;
+    const uint32_t quads = (p.width + 3) / 4, tiles_n = (*p.count + p.tile_n - 1) / p.tile_n;
+    const uint32_t splits = hidden_splits(p, tiles_n);
+    const uint64_t step = uint64_t(tiles_n) * p.tile_n * p.sum_stride;
     const uint64_t total = uint64_t(p.n) * quads;
     for (uint64_t i = uint64_t(blockIdx.x) * 256 + threadIdx.x; i < total; i += uint64_t(gridDim.x) * 256) {
         const uint32_t n = uint32_t(i / quads), d = uint32_t(i % quads) * 4;
         const int32_t at = p.place[n];
         float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         if (at >= 0) {
-            for (uint32_t s = 0; s < p.splits; ++s) {
-                const f32x4 x = *reinterpret_cast<const f32x4 *>(p.sum + (uint64_t(s) * p.n_pad + at) * p.sum_stride + d);
+            const float *from = p.sum + uint64_t(at) * p.sum_stride + d;
+#pragma unroll 4
+            for (uint32_t s = 0; s < splits; ++s) {
+                const f32x4 x = *reinterpret_cast<const f32x4 *>(from + s * step);
 #pragma unroll
                 for (int q = 0; q < 4; ++q) v[q] += x[q];
             }
@@ -528,7 +557,11 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_weigh
     Tile tile;
     tile.template run<true, true>(hidden_rows<S>(p, count), at.m * Tile::BM, slope_rows<S>(p, slope, count),
                                   at.n * Tile::BN, 0, (count + Tile::kStep - 1) / Tile::kStep, even, odd);
-    const float back = p.inverse ? p.inverse[p.n_pad] : 1.0f;
+    float back = 1.0f;
+    if constexpr (__is_same(T, f16)) {
+        back = p.inverse[p.n_pad];
+        __builtin_amdgcn_s_waitcnt(0x0f70);         // here, not behind each store
+    }
 #pragma unroll
     for (int j = 0; j < Tile::TN; ++j) {
         const uint32_t v = at.n * Tile::BN + tile.column(j);
@@ -540,7 +573,7 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_weigh
             if (d >= p.width) continue;
             float x[4];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) x[q] = tile.acc[i][j][q] * back;
+            for (int q = 0; q < 4; ++q) x[q] = __is_same(T, f16) ? tile.acc[i][j][q] * back : tile.acc[i][j][q];
             store_pack<4>(to + d, narrow_pack<T>(x), p.width - d);
         }
     }

@@ -77,17 +77,17 @@ bool planes(const HeadShape &s) { return s.size == 4 && s.n > kPlaneRows; }
 
 // fn(tile): the larger of two, unless it leaves CUs without one; `most` is how
 // often k can be split.
-template <typename T, typename F>
+template <typename T, bool Across, typename F>
 auto by_tile(const HeadShape &s, uint64_t m, uint64_t n, uint64_t most, F fn) {
     const bool large = ceil_div(m, 256) * ceil_div(n, planes(s) ? 128 : 256) * most >= kCus;
     if (std::is_same<T, float>::value && planes(s))
         return large ? fn(static_cast<LargeSplit *>(nullptr)) : fn(static_cast<SmallSplit *>(nullptr));
-    return large ? fn(static_cast<LargeTile<T> *>(nullptr)) : fn(static_cast<SmallTile<T> *>(nullptr));
+    return large ? fn(static_cast<LargeTile<T, Across> *>(nullptr)) : fn(static_cast<SmallTile<T> *>(nullptr));
 }
 // The same where the type does not matter: all have tiles of one size but for the planes.
 template <typename F>
 auto by_tile_size(const HeadShape &s, uint64_t m, uint64_t n, uint64_t most, F fn) {
-    return by_tile<float>(s, m, n, most, fn);
+    return by_tile<float, false>(s, m, n, most, fn);
 }
 
 // Tiles read whole 16-byte pieces of the weight, from addresses of 16 bytes: whether it is to be laid out for them.
@@ -161,17 +161,18 @@ uint64_t head_grad_room(const HeadShape &s, int dtype, bool laid, bool hidden, b
     }
     a.piece = uint32_t(piece_of(s.classes, a.n_pad * held(s), kPieceBytes));
     a.sum_stride = uint32_t(ceil_div(s.width, 4) * 4);
-    // splits that give every CU a tile (two of the small ones, unless they fill its LDS), each of 8 steps at least
+    // dh: a workgroup to every CU (two of the small tiles, where LDS has room), which the kernel spreads over the tiles
+    // that the packed rows take and splits of k, each of 8 steps at least
     const uint64_t steps = a.piece / (s.size == 4 ? 32 : 64);
-    const uint64_t most = std::max<uint64_t>(1, std::min<uint64_t>(steps / 8, 32));
-    a.most = uint32_t(most);
-    const uint64_t splits = by_tile_size(s, s.width, s.n, most, [&](auto *t) {
+    a.most = uint32_t(std::max<uint64_t>(1, std::min<uint64_t>(steps / 8, 32)));
+    by_tile_size(s, s.width, s.n, a.most, [&](auto *t) {
         using Tile = std::remove_pointer_t<decltype(t)>;
-        const uint64_t tiles = ceil_div(s.width, Tile::BM) * ceil_div(s.n, Tile::BN);
-        return std::max<uint64_t>(1, std::min(most, (Tile::kWaves == 4 ? 2 : 1) * kCus / tiles));
+        a.tiles_m = uint32_t(ceil_div(s.width, Tile::BM));
+        a.tile_n = Tile::BN;
+        const uint64_t slots = (2 * sizeof(typename Tile::Buffer) <= 80 * 1024 ? 2 : 1) * kCus;
+        a.blocks = uint32_t(std::max(slots, a.tiles_m * ceil_div(s.n, Tile::BN)));
+        return 0;
     });
-    a.steps = uint32_t(ceil_div(steps, splits));
-    a.splits = uint32_t(ceil_div(steps, a.steps));
     a.count = room.take<uint32_t>(1);
     a.chunk_count = room.take<uint32_t>(2 * ceil_div(s.n, kListChunk));
     a.list = room.take<uint32_t>(a.n_pad);
@@ -182,7 +183,10 @@ uint64_t head_grad_room(const HeadShape &s, int dtype, bool laid, bool hidden, b
     const uint64_t slopes = uint64_t(a.n_pad) * a.piece * held(s);
     if (hidden || dtype != TM_DTYPE_F16) a.slope = room.take<char>(slopes);
     if (weight && dtype == TM_DTYPE_F16) a.slope_common = room.take<char>(slopes);
-    if (hidden) a.sum = room.take<float>(uint64_t(a.splits) * a.n_pad * a.sum_stride);
+    if (hidden) {
+        const uint64_t rows = std::min<uint64_t>(uint64_t(a.most) * a.n_pad, uint64_t(a.blocks / a.tiles_m) * a.tile_n);
+        a.sum = room.take<float>(rows * a.sum_stride);
+    }
     if (laid) a.weight_laid = room.take<char>(uint64_t(a.piece) * a.width_pad * held(s));
     return room.used;
 }
@@ -248,7 +252,7 @@ int run_head(HeadArgs a, const HeadShape &s, hipStream_t stream) {
         if (a.weight_laid) rc = lay_piece<T>(s, a, stream);
         if (rc != TM_OK) break;
         // the tile is that of all classes: it says how many parts there are
-        rc = by_tile<T>(s, s.classes, s.n, 1, [&](auto *t) {
+        rc = by_tile<T, false>(s, s.classes, s.n, 1, [&](auto *t) {
             using Tile = std::remove_pointer_t<decltype(t)>;
             return launch(k_head_sums<T, Tile>, tile_grid<Tile>(std::min<uint64_t>(a.piece, s.classes - first), s.n),
                           dim3(Tile::kThreads), 0, stream, a);
@@ -279,20 +283,19 @@ int run_head_grad(HeadArgs a, const HeadShape &s, hipStream_t stream) {
         a.add = first > 0;
         if (a.weight_laid) rc = lay_piece<T>(s, a, stream);
         if (rc != TM_OK) break;
-        rc = by_tile<T>(s, a.piece, s.n, 1, [&](auto *t) {
+        rc = by_tile<T, false>(s, a.piece, s.n, 1, [&](auto *t) {
             using Tile = std::remove_pointer_t<decltype(t)>;
             return launch(k_head_slopes<T, Tile>, tile_grid<Tile>(a.piece, s.n), dim3(Tile::kThreads), 0, stream, a);
         });
         if (rc == TM_OK && a.grad_hidden) {
-            rc = by_tile<T>(s, s.width, s.n, a.most, [&](auto *t) {
+            rc = by_tile<T, true>(s, s.width, s.n, a.most, [&](auto *t) {
                 using Tile = std::remove_pointer_t<decltype(t)>;
-                return launch(k_head_hidden<T, Tile>, dim3(tile_grid<Tile>(s.width, s.n).x * a.splits),
-                              dim3(Tile::kThreads), 0, stream, a);
+                return launch(k_head_hidden<T, Tile>, dim3(a.blocks), dim3(Tile::kThreads), 0, stream, a);
             });
         }
         if (rc == TM_OK && a.grad_weight) {
             const uint64_t rows = std::min<uint64_t>(a.piece, s.classes - first);
-            rc = by_tile<T>(s, s.width, rows, 1, [&](auto *t) {
+            rc = by_tile<T, true>(s, s.width, rows, 1, [&](auto *t) {
                 using Tile = std::remove_pointer_t<decltype(t)>;
                 return launch(k_head_weight<T, Tile>, tile_grid<Tile>(s.width, rows), dim3(Tile::kThreads), 0, stream, a);
             });

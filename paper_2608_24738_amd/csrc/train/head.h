@@ -240,7 +240,7 @@ __global__ __launch_bounds__(1024) void k_head_list(HeadArgs p) {
 struct LayArgs {
     const void *from;
     uint64_t stride;
-    const uint32_t *list, *count;   // which rows; NULL: `rows` of them in order
+    const uint32_t *list, *count;   // which rows, and zeros up to a multiple of 64; NULL: `rows` of them in order
     uint32_t rows, width;
     void *to;
     uint32_t to_stride;             // elements
@@ -249,14 +249,15 @@ struct LayArgs {
 template <typename T>
 __global__ __launch_bounds__(256) void k_lay_rows(LayArgs p) {
     constexpr int V = 16 / sizeof(T);
-    const uint32_t rows = p.count ? *p.count : p.rows;
+    const uint32_t rows = p.count ? *p.count : p.rows, end = p.count ? (rows + 63) & ~63u : rows;
     const uint32_t pieces = p.to_stride / V;
-    for (uint32_t r = blockIdx.x * blockDim.y + threadIdx.y; r < rows; r += gridDim.x * blockDim.y) {
-        const T *from = static_cast<const T *>(p.from) + (p.list ? p.list[r] : r) * p.stride;
+    for (uint32_t r = blockIdx.x * blockDim.y + threadIdx.y; r < end; r += gridDim.x * blockDim.y) {
+        const uint32_t width = r < rows ? p.width : 0;
+        const T *from = static_cast<const T *>(p.from) + (width && p.list ? p.list[r] : r) * p.stride;
         T *to = static_cast<T *>(p.to) + uint64_t(r) * p.to_stride;
         for (uint32_t i = threadIdx.x; i < pieces; i += blockDim.x) {
             const uint32_t c = i * V;
-            store_pack<V>(to + c, c < p.width ? load_pack<V>(from + c, p.width - c, T{}) : Pack<T, V>{});
+            store_pack<V>(to + c, c < width ? load_pack<V>(from + c, width - c, T{}) : Pack<T, V>{});
         }
     }
 }
@@ -278,14 +279,15 @@ __device__ __forceinline__ void split(const float (&x)[V], Pack<bf16, V> (&out)[
 // Floats laid out likewise, in three planes.
 __global__ __launch_bounds__(256) void k_split_rows(LayArgs p) {
     constexpr int V = 8;
-    const uint32_t rows = p.count ? *p.count : p.rows;
+    const uint32_t rows = p.count ? *p.count : p.rows, end = p.count ? (rows + 63) & ~63u : rows;
     const uint32_t pieces = p.to_stride / V;
-    for (uint32_t r = blockIdx.x * blockDim.y + threadIdx.y; r < rows; r += gridDim.x * blockDim.y) {
-        const float *from = static_cast<const float *>(p.from) + (p.list ? p.list[r] : r) * p.stride;
+    for (uint32_t r = blockIdx.x * blockDim.y + threadIdx.y; r < end; r += gridDim.x * blockDim.y) {
+        const uint32_t width = r < rows ? p.width : 0;
+        const float *from = static_cast<const float *>(p.from) + (width && p.list ? p.list[r] : r) * p.stride;
         bf16 *to = static_cast<bf16 *>(p.to) + uint64_t(r) * p.to_stride;
         for (uint32_t i = threadIdx.x; i < pieces; i += blockDim.x) {
             const uint32_t c = i * V;
-            const Pack<float, V> q = c < p.width ? load_pack<V>(from + c, p.width - c, 0.0f) : Pack<float, V>{};
+            const Pack<float, V> q = c < width ? load_pack<V>(from + c, width - c, 0.0f) : Pack<float, V>{};
             float x[V];
 #pragma unroll
             for (int j = 0; j < V; ++j) x[j] = q.at(j);
@@ -325,56 +327,98 @@ __device__ __forceinline__ Operand slope_rows(const HeadArgs &p, const void *at,
 template <typename T, typename Tile>
 using Held = std::conditional_t<Tile::kPlanes == 3, bf16, T>;
 
+// Goes through the tiles of logits of `rows` classes and the packed rows, a
+// workgroup taking several: the next tile's first step is on its way while
+// before(place) has brought what finish(tile, place) needs, and finish runs.
+template <typename T, typename Tile, typename Before, typename Finish>
+__device__ __forceinline__ void each_tile(const HeadArgs &p, uint32_t rows, uint32_t count,
+                                          typename Tile::Buffer &even, typename Tile::Buffer &odd, Before before,
+                                          Finish finish) {
+    typedef Held<T, Tile> S;
+    const uint32_t tiles_n = (count + Tile::BN - 1) / Tile::BN;
+    const uint32_t tiles_m = (rows + Tile::BM - 1) / Tile::BM;
+    const uint32_t total = tiles_m * tiles_n, steps = p.width_pad / Tile::kStep;
+    if (blockIdx.x >= total) return;
+    Tile tile;
+    const auto begin = [&](TilePlace at) {
+        return tile.template begin<false, false>(weight_rows<S, Tile::kPlanes>(p), at.m * Tile::BM,
+                                                 hidden_rows<S>(p, p.n_pad), at.n * Tile::BN, 0, even);
+    };
+    TilePlace at = tile_place(blockIdx.x, tiles_m, tiles_n);
+    auto from = begin(at);
+    for (uint32_t block = blockIdx.x;;) {
+        tile.run(from, 0, steps, even, odd);
+        const TilePlace now = at;
+        before(tile, now);
+        block += gridDim.x;
+        const bool more = block < total;
+        if (more) {
+            if (steps & 1) __syncthreads();     // the last step was even's
+            at = tile_place(block, tiles_m, tiles_n);
+            from = begin(at);
+        }
+        finish(tile, now);
+        if (!more) return;
+    }
+}
+
 // Sums of 2^(c x - M) of the packed rows over a tile's classes, one for each
 // wave's classes, and c x of the labels.
 template <typename T, typename Tile>
 __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_sums(HeadArgs p) {
-    typedef Held<T, Tile> S;
     __shared__ __attribute__((aligned(1024))) typename Tile::Buffer even, odd;
-    const uint32_t count = *p.count, tiles_n = (count + Tile::BN - 1) / Tile::BN;
-    const uint32_t rows = min(p.piece, p.classes - p.first), tiles_m = (rows + Tile::BM - 1) / Tile::BM;
-    if (blockIdx.x >= uint64_t(tiles_m) * tiles_n) return;
-    const TilePlace at = tile_place(blockIdx.x, tiles_m, tiles_n);
-    Tile tile;
-    tile.template run<false, false>(weight_rows<S, Tile::kPlanes>(p), at.m * Tile::BM, hidden_rows<S>(p, p.n_pad),
-                                    at.n * Tile::BN, 0, p.width_pad / Tile::kStep, even, odd);
-    const bool edge = (at.m + 1) * Tile::BM > rows;
-    const uint32_t part = (p.first / Tile::BM + at.m) * Tile::WM + tile.wave / Tile::WN;
-    uint32_t wants[Tile::TN];                       // the labels' rows in the tile
+    const uint32_t count = *p.count, rows = min(p.piece, p.classes - p.first);
+    uint32_t wants[Tile::TN];                       // the labels' rows among the wave's
+    each_tile<T, Tile>(p, rows, count, even, odd, [&](const Tile &tile, TilePlace at) {
 #pragma unroll
-    for (int j = 0; j < Tile::TN; ++j) {
-        const uint32_t n = at.n * Tile::BN + tile.column(j);
-        const int32_t y = n < count && p.label ? load_label(p.label, p.label_bytes, p.list[n], p.classes) : -1;
-        wants[j] = y < 0 ? ~0u : uint32_t(y) - p.first - at.m * Tile::BM;
-    }
+        for (int j = 0; j < Tile::TN; ++j) {
+            const uint32_t n = at.n * Tile::BN + tile.column(j);
+            const int32_t y = n < count && p.label ? load_label(p.label, p.label_bytes, p.list[n], p.classes) : -1;
+            wants[j] = y < 0 ? ~0u : uint32_t(y) - p.first - at.m * Tile::BM - (tile.row(0) & ~15u);
+        }
+    }, [&](Tile &tile, TilePlace at) {
+        const uint32_t part = (p.first / Tile::BM + at.m) * Tile::WM + tile.wave / Tile::WN;
+        if ((at.m + 1) * Tile::BM > rows) {         // classes beyond the last
 #pragma unroll
-    for (int j = 0; j < Tile::TN; ++j) {
-        const uint32_t n = at.n * Tile::BN + tile.column(j), want = wants[j];
-        const bool real = n < count;
-        float most = -INFINITY, label = 0.0f;
+            for (int i = 0; i < Tile::TM; ++i)
 #pragma unroll
-        for (int i = 0; i < Tile::TM; ++i)
+                for (int j = 0; j < Tile::TN; ++j)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                if (edge && at.m * Tile::BM + tile.row(i) + q >= rows) tile.acc[i][j][q] = -INFINITY;
-                const float x = tile.acc[i][j][q];
-                if (want == tile.row(i) + q) label = x;
-                most = fmaxf(most, x);
+                    for (int q = 0; q < 4; ++q)
+                        if (at.m * Tile::BM + tile.row(i) + q >= rows) tile.acc[i][j][q] = -INFINITY;
+        }
+#pragma unroll
+        for (int j = 0; j < Tile::TN; ++j) {
+            const uint32_t n = at.n * Tile::BN + tile.column(j);
+            const bool mine = wants[j] < 16u * Tile::TM && (wants[j] & 15) - uint32_t(tile.lane >> 4) * 4 < 4;
+            if (__any(mine)) {                      // few tiles hold a column's label
+                float label = 0.0f;
+#pragma unroll
+                for (int i = 0; i < Tile::TM; ++i)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        if ((wants[j] >> 4) == uint32_t(i) && (wants[j] & 3) == uint32_t(q)) label = tile.acc[i][j][q];
+                if (mine) p.found[n] = label;
             }
-        most = fmaxf(most, __shfl_xor(most, 16));
-        most = fmaxf(most, __shfl_xor(most, 32));
-        const float m = reference(most, p.c);
-        float s = 0.0f;
+            float most = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < Tile::TM; ++i)
+            for (int i = 0; i < Tile::TM; ++i) {
+                most = max_of(most, tile.acc[i][j][0], tile.acc[i][j][1]);
+                most = max_of(most, tile.acc[i][j][2], tile.acc[i][j][3]);
+            }
+            most = fmaxf(most, __shfl_xor(most, 16));
+            most = fmaxf(most, __shfl_xor(most, 32));
+            const float m = reference(most, p.c);
+            float s = 0.0f;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) s += exp2_hw(fmaf(tile.acc[i][j][q], p.c, -m));
-        s += __shfl_xor(s, 16);
-        s += __shfl_xor(s, 32);
-        if (real && tile.lane < 16) p.part[uint64_t(part) * p.n_pad + n] = {m, s};
-        const uint32_t inside = want - (tile.row(0) & ~15u);
-        if (inside < 16u * Tile::TM && (inside & 15) - uint32_t(tile.lane >> 4) * 4 < 4) p.found[n] = label;
-    }
+            for (int i = 0; i < Tile::TM; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) s += exp2_hw(fmaf(tile.acc[i][j][q], p.c, -m));
+            s += __shfl_xor(s, 16);
+            s += __shfl_xor(s, 32);
+            if (n < count && tile.lane < 16) p.part[uint64_t(part) * p.n_pad + n] = {m, s};
+        }
+    });
 }
 
 // A row's results.
@@ -425,56 +469,62 @@ template <typename T, typename Tile>
 __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_slopes(HeadArgs p) {
     typedef Held<T, Tile> S;
     __shared__ __attribute__((aligned(1024))) typename Tile::Buffer even, odd;
-    const uint32_t count = *p.count, tiles_n = (count + Tile::BN - 1) / Tile::BN, tiles_m = p.piece / Tile::BM;
-    if (blockIdx.x >= uint64_t(tiles_m) * tiles_n) return;
-    const TilePlace at = tile_place(blockIdx.x, tiles_m, tiles_n);
-    const uint32_t rows = min(p.piece, p.classes - p.first);
-    Tile tile;
-    tile.template run<false, false>(weight_rows<S, Tile::kPlanes>(p), at.m * Tile::BM, hidden_rows<S>(p, p.n_pad),
-                                    at.n * Tile::BN, 0, p.width_pad / Tile::kStep, even, odd);
-    // What the columns need comes first: a wait for a load is one for all stores before it.
+    const uint32_t count = *p.count, rows = min(p.piece, p.classes - p.first);
+    // what the columns need comes first: a wait for a load is one for all stores before it
     HeadRow row[Tile::TN];
     float ratios[Tile::TN];
+    each_tile<T, Tile>(p, p.piece, count, even, odd, [&](const Tile &tile, TilePlace at) {
 #pragma unroll
-    for (int j = 0; j < Tile::TN; ++j) {
-        const uint32_t n = at.n * Tile::BN + tile.column(j);
-        row[j] = {0.0f, 0.0f, 0.0f, -1};
-        if (n < count) row[j] = p.row[n];
-        if constexpr (__is_same(T, f16)) ratios[j] = n < count ? p.inverse[n] / p.inverse[p.n_pad] : 1.0f;
-    }
+        for (int j = 0; j < Tile::TN; ++j) {
+            const uint32_t n = at.n * Tile::BN + tile.column(j);
+            row[j] = {0.0f, 0.0f, 0.0f, -1};
+            if (n < count) row[j] = p.row[n];
+            if constexpr (__is_same(T, f16)) ratios[j] = n < count ? p.inverse[n] / p.inverse[p.n_pad] : 1.0f;
+        }
+    }, [&](Tile &tile, TilePlace at) {
+        const bool edge = (at.m + 1) * Tile::BM > rows || (at.n + 1) * Tile::BN > count;
 #pragma unroll
-    for (int j = 0; j < Tile::TN; ++j) {
-        const uint32_t n = at.n * Tile::BN + tile.column(j);
-        const bool real = n < count;
-        const HeadRow r = row[j];
+        for (int j = 0; j < Tile::TN; ++j) {
+            const uint32_t n = at.n * Tile::BN + tile.column(j);
+            const HeadRow r = row[j];
+            // the label's row among the lane's
+            const uint32_t want = uint32_t(r.y) - p.first - at.m * Tile::BM - tile.row(0);
+            const bool labels = __any(r.y >= 0 && want < 16u * Tile::TM);
 #pragma unroll
-        for (int i = 0; i < Tile::TM; ++i) {
-            const uint32_t v = at.m * Tile::BM + tile.row(i);
-            float g[4];
+            for (int i = 0; i < Tile::TM; ++i) {
+                const uint32_t v = at.m * Tile::BM + tile.row(i);
+                float g[4];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                g[q] = -r.b * exp2_hw(fmaf(tile.acc[i][j][q], p.c, -r.m));
-                if (int32_t(p.first + v + q) == r.y) g[q] += r.a;
-                if (!real || v + q >= rows) g[q] = 0.0f;
-            }
-            S *to = static_cast<S *>(p.slope) + uint64_t(n) * p.piece + v;
-            if constexpr (Tile::kPlanes == 3) {
-                Pack<bf16, 4> planes[3];
-                split(g, planes);
+                for (int q = 0; q < 4; ++q) g[q] = -r.b * exp2_hw(fmaf(tile.acc[i][j][q], p.c, -r.m));
+                if (labels) {
 #pragma unroll
-                for (int k = 0; k < 3; ++k) store_pack<4>(to + k * uint64_t(p.n_pad) * p.piece, planes[k]);
-            } else if (p.slope) {
-                store_pack<4>(to, narrow_pack<T>(g));
-            }
-            if constexpr (__is_same(T, f16)) {
-                if (p.slope_common) {
+                    for (int q = 0; q < 4; ++q)
+                        if (r.y >= 0 && want == uint32_t(16 * i + q)) g[q] += r.a;
+                }
+                if (edge) {
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) g[q] *= ratios[j];
-                    store_pack<4>(static_cast<T *>(p.slope_common) + uint64_t(n) * p.piece + v, narrow_pack<T>(g));
+                    for (int q = 0; q < 4; ++q)
+                        if (n >= count || v + q >= rows) g[q] = 0.0f;
+                }
+                S *to = static_cast<S *>(p.slope) + uint64_t(n) * p.piece + v;
+                if constexpr (Tile::kPlanes == 3) {
+                    Pack<bf16, 4> planes[3];
+                    split(g, planes);
+#pragma unroll
+                    for (int k = 0; k < 3; ++k) store_pack<4>(to + k * uint64_t(p.n_pad) * p.piece, planes[k]);
+                } else if (p.slope) {
+                    store_pack<4>(to, narrow_pack<T>(g));
+                }
+                if constexpr (__is_same(T, f16)) {
+                    if (p.slope_common) {
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) g[q] *= ratios[j];
+                        store_pack<4>(static_cast<T *>(p.slope_common) + uint64_t(n) * p.piece + v, narrow_pack<T>(g));
+                    }
                 }
             }
         }
-    }
+    });
 }
 
 // Splits of the product for dh: as many as its workgroups make of the tiles that the packed rows take.
@@ -490,7 +540,8 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_hidde
     const uint32_t count = *p.count, tiles_n = (count + Tile::BN - 1) / Tile::BN, splits = hidden_splits(p, tiles_n);
     if (blockIdx.x >= p.tiles_m * tiles_n * splits) return;
     const TilePlace at = tile_place(blockIdx.x, p.tiles_m, tiles_n, splits);
-    const uint32_t all = p.piece / Tile::kStep, steps = (all + splits - 1) / splits;
+    const uint32_t rows = min(p.piece, p.classes - p.first);
+    const uint32_t all = (rows + Tile::kStep - 1) / Tile::kStep, steps = (all + splits - 1) / splits;
     Tile tile;
     tile.template run<true, false>(weight_rows<S, Tile::kPlanes>(p), at.m * Tile::BM, slope_rows<S>(p, p.slope, p.n_pad),
                                    at.n * Tile::BN, min(all, at.split * steps), min(all, (at.split + 1) * steps),
@@ -555,7 +606,7 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_weigh
     const TilePlace at = tile_place(blockIdx.x, tiles_m, tiles_n);
     const void *slope = __is_same(T, f16) ? p.slope_common : p.slope;
     Tile tile;
-    tile.template run<true, true>(hidden_rows<S>(p, count), at.m * Tile::BM, slope_rows<S>(p, slope, count),
+    tile.template run<true, true>(hidden_rows<S>(p, p.n_pad), at.m * Tile::BM, slope_rows<S>(p, slope, p.n_pad),
                                   at.n * Tile::BN, 0, (count + Tile::kStep - 1) / Tile::kStep, even, odd);
     float back = 1.0f;
     if constexpr (__is_same(T, f16)) {

@@ -14,8 +14,8 @@ using namespace tmtrain;
 
 namespace {
 
-constexpr uint64_t kMaxWidth = uint64_t(1) << 24;
-constexpr uint64_t kPieceBytes = uint64_t(1) << 27;     // of one layout of g
+constexpr uint64_t kMaxWidth = uint64_t(1) << 20;      // 256 rows fit an offset of 32 bits
+constexpr uint64_t kPieceBytes = uint64_t(1) << 27;     // of g
 constexpr uint64_t kLaidBytes = uint64_t(1) << 28;      // of weights laid out in whole steps
 constexpr uint64_t kCus = 256;
 constexpr uint64_t kPlaneRows = 128;
@@ -75,6 +75,10 @@ bool few(const HeadShape &s) { return s.n <= kFewRows; }
 // Floats go to the matrix cores as three 16-bit planes, unless the rows are few.
 bool planes(const HeadShape &s) { return s.size == 4 && s.n > kPlaneRows; }
 
+// Workgroups that the chip holds at once.
+template <typename Tile>
+constexpr uint64_t kSlots = (2 * sizeof(typename Tile::Buffer) <= 80 * 1024 ? 2 : 1) * kCus;
+
 // fn(tile): the larger of two, unless it leaves CUs without one; `most` is how
 // often k can be split.
 template <typename T, bool Across, typename F>
@@ -90,9 +94,11 @@ auto by_tile_size(const HeadShape &s, uint64_t m, uint64_t n, uint64_t most, F f
     return by_tile<float, false>(s, m, n, most, fn);
 }
 
-// Tiles read whole 16-byte pieces of the weight, from addresses of 16 bytes: whether it is to be laid out for them.
+// Tiles read whole steps of the weight's rows, 16 bytes at a time and with offsets of 32 bits: whether it is to be laid
+// out for them.
 bool to_lay(const void *p, uint64_t stride, const HeadShape &s) {
-    return !few(s) && (planes(s) || uintptr_t(p) % 16 || stride * s.size % 16 || s.width * s.size % 16);
+    return !few(s) && (planes(s) || uintptr_t(p) % 16 || stride * s.size % 16 || s.width * s.size % 128 ||
+                       stride * s.size > kMostStride);
 }
 
 // Classes of a piece, in whole tiles, so that `bytes` hold a row of `each` for every class.
@@ -169,8 +175,7 @@ uint64_t head_grad_room(const HeadShape &s, int dtype, bool laid, bool hidden, b
         using Tile = std::remove_pointer_t<decltype(t)>;
         a.tiles_m = uint32_t(ceil_div(s.width, Tile::BM));
         a.tile_n = Tile::BN;
-        const uint64_t slots = (2 * sizeof(typename Tile::Buffer) <= 80 * 1024 ? 2 : 1) * kCus;
-        a.blocks = uint32_t(std::max(slots, a.tiles_m * ceil_div(s.n, Tile::BN)));
+        a.blocks = uint32_t(std::max(kSlots<Tile>, a.tiles_m * ceil_div(s.n, Tile::BN)));
         return 0;
     });
     a.count = room.take<uint32_t>(1);
@@ -194,6 +199,10 @@ uint64_t head_grad_room(const HeadShape &s, int dtype, bool laid, bool hidden, b
 template <typename Tile>
 dim3 tile_grid(uint64_t m, uint64_t n) {
     return dim3(uint32_t(ceil_div(m, Tile::BM) * ceil_div(n, Tile::BN)));
+}
+template <typename Tile>
+dim3 lasting_grid(uint64_t m, uint64_t n) {
+    return dim3(uint32_t(std::min<uint64_t>(tile_grid<Tile>(m, n).x, kSlots<Tile>)));
 }
 
 // Rows laid out in whole steps, or in planes.
@@ -254,7 +263,7 @@ int run_head(HeadArgs a, const HeadShape &s, hipStream_t stream) {
         // the tile is that of all classes: it says how many parts there are
         rc = by_tile<T, false>(s, s.classes, s.n, 1, [&](auto *t) {
             using Tile = std::remove_pointer_t<decltype(t)>;
-            return launch(k_head_sums<T, Tile>, tile_grid<Tile>(std::min<uint64_t>(a.piece, s.classes - first), s.n),
+            return launch(k_head_sums<T, Tile>, lasting_grid<Tile>(std::min<uint64_t>(a.piece, s.classes - first), s.n),
                           dim3(Tile::kThreads), 0, stream, a);
         });
     }
@@ -285,7 +294,7 @@ int run_head_grad(HeadArgs a, const HeadShape &s, hipStream_t stream) {
         if (rc != TM_OK) break;
         rc = by_tile<T, false>(s, a.piece, s.n, 1, [&](auto *t) {
             using Tile = std::remove_pointer_t<decltype(t)>;
-            return launch(k_head_slopes<T, Tile>, tile_grid<Tile>(a.piece, s.n), dim3(Tile::kThreads), 0, stream, a);
+            return launch(k_head_slopes<T, Tile>, lasting_grid<Tile>(a.piece, s.n), dim3(Tile::kThreads), 0, stream, a);
         });
         if (rc == TM_OK && a.grad_hidden) {
             rc = by_tile<T, true>(s, s.width, s.n, a.most, [&](auto *t) {

@@ -53,15 +53,13 @@ __device__ __forceinline__ f32x4 multiply(u32x4 a, u32x4 b, f32x4 acc) {
     }
 }
 
-// 16 bytes a lane from memory to LDS: lane l's go to `to` + 16 l.
-__device__ __forceinline__ void copy_to_lds(const char *from, char *to) {
+// 16 bytes a lane from memory to LDS: lane l's go to `to` + 16 l.  One address
+// for the wave and an offset of 32 bits a lane, which stays from step to step.
+__device__ __forceinline__ void copy_to_lds(const char *from, uint32_t offset, char *to) {
     typedef const __attribute__((address_space(1))) uint32_t *Global;
     typedef __attribute__((address_space(3))) uint32_t *Local;
-    __builtin_amdgcn_global_load_lds((Global)from, (Local)to, 16, 0, 0);
+    __builtin_amdgcn_global_load_lds((Global)(from + offset), (Local)to, 16, 0, 0);
 }
-
-// What a row's pieces beyond its end are read from.
-__device__ __attribute__((aligned(16))) const uint32_t kZeroPiece[4] = {0, 0, 0, 0};
 
 // Which tile of tiles_m x tiles_n a workgroup takes.  Workgroups go round robin
 // over the eight XCDs: each gets one stretch of the tiles, so that its L2 holds
@@ -82,12 +80,14 @@ __device__ __forceinline__ TilePlace tile_place(uint32_t block, uint32_t tiles_m
     return {in / columns, group * kColumns + in % columns, split};
 }
 
-// One operand: rows `stride` bytes apart, 16-byte aligned.
+// One operand: rows `stride` <= kMostStride bytes apart, 16-byte aligned.  Along
+// k, rows hold whole steps.
+constexpr uint64_t kMostStride = uint64_t(1) << 23;     // 256 of them fit an offset of 32 bits
 struct Operand {
     const char *at;
     uint64_t stride, plane;     // plane: bytes from one plane to the next
-    uint32_t rows;              // along k: rows beyond are read as the last one; across: as zeros
-    uint32_t pieces;            // whole pieces in a row; along k: beyond them zeros, across: anything
+    uint32_t rows;              // rows beyond are read as the last one
+    uint32_t pieces;            // of 16 bytes in a row; across k: those beyond are read as the last one
 };
 
 // Copies of an operand's steps to LDS, S elements of m or n by Waves waves, K
@@ -97,29 +97,22 @@ struct Along {
     static constexpr uint32_t kRow = K * sizeof(T), kPieces = kRow / 16;    // 8 or 4 pieces in a row
     static constexpr uint32_t kAtOnce = 64 / kPieces;                       // rows of one copy
     static constexpr int kCopies = S / kAtOnce / Waves;
-    const char *from[kCopies];
-    uint32_t piece, pieces, place;
+    const char *from;
+    uint32_t offset[kCopies], place;
 
     static __device__ __forceinline__ uint32_t order(uint32_t r) { return kPieces == 8 ? r & 7 : r >> 2 & 3; }
     __device__ __forceinline__ Along(const Operand &o, uint32_t m0, uint32_t first, int lane, int wave) {
         const uint32_t r = lane / kPieces;
-        piece = lane % kPieces ^ order(r);
-        pieces = o.pieces;
+        from = o.at + m0 * o.stride + uint64_t(first) * kRow;
 #pragma unroll
         for (int i = 0; i < kCopies; ++i)
-            from[i] = o.at + min(m0 + (i * Waves + wave) * kAtOnce + r, o.rows - 1) * o.stride + first * kRow + piece * 16;
+            offset[i] = min((i * Waves + wave) * kAtOnce + r, o.rows - 1 - m0) * uint32_t(o.stride) +
+                        (lane % kPieces ^ order(r)) * 16;
     }
-    __device__ __forceinline__ void fetch(char *lds, uint32_t step, int, int wave) {
-        if (step == pieces / kPieces) {         // the step that rows end in
+    __device__ __forceinline__ void fetch(char *lds, uint32_t, int, int wave) {
 #pragma unroll
-            for (int i = 0; i < kCopies; ++i)
-                from[i] = step * kPieces + piece < pieces ? from[i] : reinterpret_cast<const char *>(kZeroPiece);
-        }
-#pragma unroll
-        for (int i = 0; i < kCopies; ++i) {
-            copy_to_lds(from[i], lds + (i * Waves + wave) * 1024);
-            from[i] += kRow;
-        }
+        for (int i = 0; i < kCopies; ++i) copy_to_lds(from, offset[i], lds + (i * Waves + wave) * 1024);
+        from += kRow;
     }
     // Where the lane's reads of block 0 begin, and the 16 bytes of block i in half of a step.
     __device__ __forceinline__ void reads(int lane, uint32_t block) {
@@ -135,9 +128,9 @@ struct Across {
     static constexpr int kCopies = S * K * int(sizeof(T)) / 1024 / Waves;
     static constexpr uint32_t kRow = S * sizeof(T), kPieces = kRow / 16;    // of a row in LDS
     static constexpr uint32_t kUnits = S / 16;                              // of 16 elements
-    const char *from[kCopies];
-    uint64_t stride;
-    uint32_t rows;
+    const char *from;
+    uint32_t stride, rows;
+    uint32_t offset[kCopies];
 
     // Pieces of a unit, and the number that orders the units of row r.
     static constexpr uint32_t kUnitPieces = sizeof(T);
@@ -149,26 +142,27 @@ struct Across {
         return (i * Waves + wave) * (64 / kPieces) + lane / kPieces;
     }
     __device__ __forceinline__ Across(const Operand &o, uint32_t m0, uint32_t first, int lane, int wave) {
-        stride = o.stride;
+        stride = uint32_t(o.stride);
         rows = o.rows;
+        from = o.at + uint64_t(first) * K * stride;
 #pragma unroll
         for (int i = 0; i < kCopies; ++i) {
             const uint32_t r = row_of(i, lane, wave);
             const uint32_t piece = m0 * sizeof(T) / 16 + (lane % kPieces ^ order(r) * kUnitPieces);
-            from[i] = o.at + (uint64_t(first) * K + r) * stride + min(piece, o.pieces - 1) * 16;
+            offset[i] = r * stride + min(piece, o.pieces - 1) * 16;
         }
     }
     __device__ __forceinline__ void fetch(char *lds, uint32_t step, int lane, int wave) {
-        if ((step + 1) * K > rows) {
+        if ((step + 1) * K > rows) {            // the last step
 #pragma unroll
-            for (int i = 0; i < kCopies; ++i)
-                if (step * K + row_of(i, lane, wave) >= rows) from[i] = reinterpret_cast<const char *>(kZeroPiece);
+            for (int i = 0; i < kCopies; ++i) {
+                const uint32_t r = row_of(i, lane, wave);
+                offset[i] -= (r - min(r, rows - 1 - step * K)) * stride;
+            }
         }
 #pragma unroll
-        for (int i = 0; i < kCopies; ++i) {
-            copy_to_lds(from[i], lds + (i * Waves + wave) * 1024);
-            from[i] += K * stride;
-        }
+        for (int i = 0; i < kCopies; ++i) copy_to_lds(from, offset[i], lds + (i * Waves + wave) * 1024);
+        from += uint64_t(K) * stride;
     }
     uint32_t place[Blocks];
     __device__ __forceinline__ void reads(int lane, uint32_t block) {
@@ -227,42 +221,56 @@ struct Tile {
     __device__ __forceinline__ Tile() {
         lane = threadIdx.x & 63;
         wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-#pragma unroll
-        for (int i = 0; i < TM; ++i)
-#pragma unroll
-            for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
     // First row and column, in the tile, of what the lane holds of block i, j.
     __device__ __forceinline__ uint32_t row(int i) const { return ((wave / WN) * TM + i) * 16 + (lane >> 4) * 4; }
     __device__ __forceinline__ uint32_t column(int j) const { return ((wave % WN) * TN + j) * 16 + (lane & 15); }
 
-    template <typename From>
-    struct Sources {
-        From plane[Planes];
-        template <size_t... I>
-        __device__ __forceinline__ Sources(const Operand &o, uint32_t m0, uint32_t first, int lane, int wave,
-                                           std::index_sequence<I...>)
-            : plane{From({o.at + I * o.plane, o.stride, 0, o.rows, o.pieces}, m0, first, lane, wave)...} {}
-    };
-
-    // Adds the products of m0.. of A and n0.. of B over steps [first, last).
+    // Where a tile's operands come from, and the next step of both.
     template <bool AAcross, bool BAcross>
-    __device__ __forceinline__ void run(const Operand &a, uint32_t m0, const Operand &b, uint32_t n0, uint32_t first,
-                                        uint32_t last, Buffer &even, Buffer &odd) {
-        if (first >= last) return;
+    struct Sources {
         typedef std::conditional_t<AAcross, Across<T, BM, kWaves, kStep, TM>, Along<T, BM, kWaves, kStep>> FromA;
         typedef std::conditional_t<BAcross, Across<T, BN, kWaves, kStep, TN>, Along<T, BN, kWaves, kStep>> FromB;
-        Sources<FromA> from_a(a, m0, first, lane, wave, std::make_index_sequence<Planes>{});
-        Sources<FromB> from_b(b, n0, first, lane, wave, std::make_index_sequence<Planes>{});
-        from_a.plane[0].reads(lane, (wave / WN) * TM);
-        from_b.plane[0].reads(lane, (wave % WN) * TN);
-        const auto fetch = [&](Buffer &s, uint32_t step) {
+        // Waves with their operands at hand go first (4096 x 32768 x 1024: sums 246 -> 238 us); those that
+        // read across k would hold up the others' reads (dw 121 -> 158), and planes leave time (309 -> 321).
+        static constexpr bool kFirst = !AAcross && !BAcross && Planes == 1;
+        FromA a[Planes];
+        FromB b[Planes];
+
+        template <size_t... I>
+        __device__ __forceinline__ Sources(const Tile &t, const Operand &x, uint32_t m0, const Operand &y, uint32_t n0,
+                                           uint32_t first, std::index_sequence<I...>)
+            : a{FromA({x.at + I * x.plane, x.stride, 0, x.rows, x.pieces}, m0, first, t.lane, t.wave)...},
+              b{FromB({y.at + I * y.plane, y.stride, 0, y.rows, y.pieces}, n0, first, t.lane, t.wave)...} {
+            a[0].reads(t.lane, (t.wave / WN) * TM);
+            b[0].reads(t.lane, (t.wave % WN) * TN);
+        }
+        __device__ __forceinline__ void fetch(const Tile &t, Buffer &s, uint32_t step) {
 #pragma unroll
             for (int p = 0; p < Planes; ++p) {
-                from_a.plane[p].fetch(s.a + p * kPlaneA, step, lane, wave);
-                from_b.plane[p].fetch(s.b + p * kPlaneB, step, lane, wave);
+                a[p].fetch(s.a + p * kPlaneA, step, t.lane, t.wave);
+                b[p].fetch(s.b + p * kPlaneB, step, t.lane, t.wave);
             }
-        };
+        }
+    };
+
+    // Sources for m0.. of A and n0.. of B from step `first` on, which is on its way.
+    template <bool AAcross, bool BAcross>
+    __device__ __forceinline__ Sources<AAcross, BAcross> begin(const Operand &a, uint32_t m0, const Operand &b, uint32_t n0,
+                                                               uint32_t first, Buffer &even) const {
+        Sources<AAcross, BAcross> from(*this, a, m0, b, n0, first, std::make_index_sequence<Planes>{});
+        from.fetch(*this, even, first);
+        return from;
+    }
+
+    // The products over steps [first, last), of which `even` has got the first.
+    // Afterwards `even` can be filled again where last - first is even.
+    template <typename From>
+    __device__ __forceinline__ void run(From &from, uint32_t first, uint32_t last, Buffer &even, Buffer &odd) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         const auto work = [&](const Buffer &s) {
 #pragma unroll
             for (int half = 0; half < kHalves; ++half) {
@@ -270,9 +278,9 @@ struct Tile {
 #pragma unroll
                 for (int p = 0; p < Planes; ++p) {
 #pragma unroll
-                    for (int i = 0; i < TM; ++i) fa[p][i] = from_a.plane[0].read(s.a + p * kPlaneA, i, half);
+                    for (int i = 0; i < TM; ++i) fa[p][i] = from.a[0].read(s.a + p * kPlaneA, i, half);
 #pragma unroll
-                    for (int j = 0; j < TN; ++j) fb[p][j] = from_b.plane[0].read(s.b + p * kPlaneB, j, half);
+                    for (int j = 0; j < TN; ++j) fb[p][j] = from.b[0].read(s.b + p * kPlaneB, j, half);
                 }
                 const auto add = [&](int pa, int pb) {
 #pragma unroll
@@ -280,10 +288,7 @@ struct Tile {
 #pragma unroll
                         for (int j = 0; j < TN; ++j) acc[i][j] = multiply<T>(fa[pa][i], fb[pb][j], acc[i][j]);
                 };
-                // Waves with their operands at hand go first (4096 x 32768 x 1024: sums 246 -> 238 us); those that
-                // read across k would hold up the others' reads (dw 121 -> 158), and planes leave time (309 -> 321).
-                constexpr bool kFirst = !AAcross && !BAcross && Planes == 1;
-                if constexpr (kFirst) __builtin_amdgcn_s_setprio(1);
+                if constexpr (From::kFirst) __builtin_amdgcn_s_setprio(1);
                 add(0, 0);
                 if constexpr (Planes == 3) {
                     add(0, 1);
@@ -292,18 +297,30 @@ struct Tile {
                     add(0, 2);
                     add(2, 0);
                 }
-                if constexpr (kFirst) __builtin_amdgcn_s_setprio(0);
+                if constexpr (From::kFirst) __builtin_amdgcn_s_setprio(0);
             }
         };
-        fetch(even, first);
         for (uint32_t k = first; k < last; k += 2) {
             __syncthreads();                    // even has arrived, odd is read
-            if (k + 1 < last) fetch(odd, k + 1);
+            if (k + 1 < last) from.fetch(*this, odd, k + 1);
             work(even);
             __syncthreads();
-            if (k + 2 < last) fetch(even, k + 2);
+            if (k + 2 < last) from.fetch(*this, even, k + 2);
             if (k + 1 < last) work(odd);
         }
+    }
+    template <bool AAcross, bool BAcross>
+    __device__ __forceinline__ void run(const Operand &a, uint32_t m0, const Operand &b, uint32_t n0, uint32_t first,
+                                        uint32_t last, Buffer &even, Buffer &odd) {
+        if (first >= last) {
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            return;
+        }
+        auto from = begin<AAcross, BAcross>(a, m0, b, n0, first, even);
+        run(from, first, last, even, odd);
     }
 };
 

@@ -17,6 +17,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import importlib
 import math
 import os
 import threading
@@ -27,6 +28,7 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libtm_edt.so")
 _lock = threading.Lock()
 _lib = None
+_torch_ops = None
 
 TM_OK = 0
 
@@ -120,6 +122,19 @@ def load() -> ctypes.CDLL:
             lib.tm_bias_grad_workspace_size.restype = size
             _lib = lib
     return _lib
+
+
+def torch_ops():
+    """The torch functions of ``_torch_ops.so``, which call the library. Raises if it has not been built."""
+    global _torch_ops
+    if _torch_ops is None:
+        load()
+        try:
+            _torch_ops = importlib.import_module("._torch_ops", __package__)
+        except ImportError as err:
+            raise RuntimeError("_torch_ops.so is not built or does not fit the installed torch; run "
+                               "`python -m paper_2608_24738_amd.build` or __graft_entry__.build()") from err
+    return _torch_ops
 
 
 def tm_strerror(status: int) -> str:

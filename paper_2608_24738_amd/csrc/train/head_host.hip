@@ -84,8 +84,9 @@ constexpr uint64_t kSlots = (2 * sizeof(typename Tile::Buffer) <= 80 * 1024 ? 2 
 template <typename T, bool Across, typename F>
 auto by_tile(const HeadShape &s, uint64_t m, uint64_t n, uint64_t most, F fn) {
     const bool large = ceil_div(m, 256) * ceil_div(n, planes(s) ? 128 : 256) * most >= kCus;
-    if (std::is_same<T, float>::value && planes(s))
-        return large ? fn(static_cast<LargeSplit *>(nullptr)) : fn(static_cast<SmallSplit *>(nullptr));
+    if constexpr (std::is_same<T, float>::value) {
+        if (planes(s)) return large ? fn(static_cast<LargeSplit *>(nullptr)) : fn(static_cast<SmallSplit *>(nullptr));
+    }
     return large ? fn(static_cast<LargeTile<T, Across> *>(nullptr)) : fn(static_cast<SmallTile<T> *>(nullptr));
 }
 // The same where the type does not matter: all have tiles of one size but for the planes.

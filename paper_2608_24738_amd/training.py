@@ -16,7 +16,8 @@ All run in the HIP kernels of ``libtm_edt.so`` (``include/tm_train.h``)
 on the current stream, take part in autograd (in reverse mode, once), and raise
 where the library refuses a request; there is no fallback.
 
-Small calls are bound by the host.  On one GPU a backward pass inside ``with
+The last three are torch functions in C++ (``_torch_ops.so``); the others go
+through ctypes.  Small calls are bound by the host.  On one GPU a backward pass inside ``with
 torch.autograd.set_multithreading_enabled(False):`` stays on the caller's
 thread, which takes a forward and backward pass from some 95 to 40 us.
 """
@@ -30,7 +31,7 @@ from typing import NamedTuple, Optional
 import torch
 from torch.autograd import forward_ad
 
-from .binding import METRICS, _call, _sampling_array, _shape_array, load
+from .binding import METRICS, _call, _sampling_array, _shape_array, load, torch_ops
 
 FLOATS = {torch.float16: 4, torch.bfloat16: 5, torch.float32: 6}
 LABELS = {torch.uint8: 0, torch.int32: 2, torch.int64: 3}
@@ -487,86 +488,6 @@ class HeadLogProbs(NamedTuple):
     log_sums: Optional[torch.Tensor]
 
 
-def _rows(t):
-    """(tensor, rows, stride between them): ``t`` (..., width) as rows whose
-    elements lie side by side, or a contiguous copy of it where it is none."""
-    shape, strides = t.shape, t.stride()
-    width = shape[-1]
-    if 0 in shape:
-        return t, math.prod(shape[:-1]), width
-    outer = _collapse(shape[:-1], strides[:-1]) if strides[-1] == 1 or width == 1 else None
-    if outer is None:
-        return t.contiguous(), math.prod(shape[:-1]), width
-    return t, outer[0], outer[1] if outer[0] > 1 else width
-
-
-@functools.lru_cache(maxsize=1024)
-def _head_workspace(dtype, rows, classes, width):
-    return int(load().tm_head_logp_workspace_size(dtype, rows, classes, width))
-
-
-@functools.lru_cache(maxsize=1024)
-def _head_grad_workspace(dtype, rows, classes, width, hidden, weight):
-    return int(load().tm_head_logp_grad_workspace_size(dtype, rows, classes, width, hidden, weight))
-
-
-def _head_args(hidden, weight, labels, scale):
-    """(hidden, weight, what the entry points take of the inputs)."""
-    hidden, rows, hidden_stride = _rows(hidden)
-    weight, classes, weight_stride = _rows(weight)
-    return hidden, weight, (hidden.data_ptr(), FLOATS[hidden.dtype], rows, classes, weight.shape[1], hidden_stride,
-                            weight.data_ptr(), weight_stride, _ptr(labels),
-                            0 if labels is None else LABELS[labels.dtype], scale)
-
-
-def _head_forward(hidden, weight, labels, scale, log_sums, stats):
-    dev = hidden.device
-    hidden, weight, args = _head_args(hidden, weight, labels, scale)
-    shape = hidden.shape[:-1]
-    logp = torch.empty(shape, dtype=torch.float32, device=dev) if labels is not None else None
-    sums = torch.empty(shape, dtype=torch.float32, device=dev) if log_sums else None
-    kept = torch.empty(shape + (2,), dtype=torch.float32, device=dev) if stats else None
-    nbytes = _head_workspace(*args[1:5])
-    workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
-    _call("tm_head_logp", dev, None, *args, _ptr(logp), _ptr(sums), _ptr(kept), _ptr(workspace), nbytes)
-    return hidden, weight, logp, sums, kept
-
-
-class _HeadLogProbs(torch.autograd.Function):
-    @staticmethod
-    def forward(ctx, hidden, weight, labels, scale, log_sums):
-        hidden, weight, logp, sums, kept = _head_forward(hidden, weight, labels, scale, log_sums, True)
-        ctx.set_materialize_grads(False)
-        ctx.save_for_backward(hidden, weight, labels, kept)
-        ctx.what = (hidden.dtype, hidden.device, hidden.shape, weight.shape, scale,
-                    None if labels is None else labels.dtype)
-        return logp, sums
-
-    @staticmethod
-    def backward(ctx, up_logp, up_sums):
-        _once()
-        wanted = ctx.needs_input_grad[:2]
-        if (up_logp is None and up_sums is None) or not any(wanted):
-            return None, None, None, None, None
-        hidden, weight, labels, kept = ctx.saved_tensors
-        dtype, dev, shape, table, scale, label_dtype = ctx.what
-        for t, size in ((hidden, shape), (weight, table)):
-            if t.dtype is not dtype or t.device != dev or t.shape != size:
-                _changed()
-        labels = _restored(labels, label_dtype, dev, shape[:-1])
-        kept = _restored(kept, torch.float32, dev, shape[:-1] + (2,))
-        # strides are those of the tensors at hand, not the forward call's
-        hidden, weight, args = _head_args(hidden, weight, labels, scale)
-        up_logp, up_sums = _upstream(up_logp), _upstream(up_sums)
-        grad_hidden = torch.empty(shape, dtype=dtype, device=dev) if wanted[0] else None
-        grad_weight = torch.empty(table, dtype=dtype, device=dev) if wanted[1] else None
-        nbytes = _head_grad_workspace(*args[1:5], *(int(w) for w in wanted))
-        workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
-        _call("tm_head_logp_grad", dev, None, *args, kept.data_ptr(), _ptr(up_logp), _ptr(up_sums),
-              _ptr(grad_hidden), _ptr(grad_weight), _ptr(workspace), nbytes)
-        return grad_hidden, grad_weight, None, None, None
-
-
 def head_log_probs(hidden: torch.Tensor, weight: torch.Tensor, labels: Optional[torch.Tensor] = None, *,
                    scale: float = 1.0, log_sums: bool = False) -> HeadLogProbs:
     """Log-probabilities of given labels under the softmax of the logits
@@ -586,93 +507,8 @@ def head_log_probs(hidden: torch.Tensor, weight: torch.Tensor, labels: Optional[
     results.  For more than 16 rows the logits' gradient is rounded to the
     operands' type before its two products, which are summed in float32.
     """
-    if not hidden.is_cuda:
-        raise ValueError("hidden must be a ROCm (cuda) tensor")
-    if hidden.dtype not in FLOATS:
-        raise TypeError("hidden must be float32, float16 or bfloat16, got %s" % hidden.dtype)
-    if hidden.dim() < 1 or weight.dim() != 2 or weight.shape[0] < 1 or weight.shape[1] < 1:
-        raise ValueError("hidden must be (..., width) and weight (classes, width), got %s and %s"
-                         % (tuple(hidden.shape), tuple(weight.shape)))
-    if weight.dtype != hidden.dtype:
-        raise TypeError("weight must be %s as the hidden states are, got %s" % (hidden.dtype, weight.dtype))
-    if weight.device != hidden.device:
-        raise ValueError("weight is on %s, the hidden states on %s" % (weight.device, hidden.device))
-    if weight.shape[1] != hidden.shape[-1]:
-        raise ValueError("hidden states of width %d do not fit a weight of width %d"
-                         % (hidden.shape[-1], weight.shape[1]))
-    labels = _check_tokens(labels, "labels", hidden.device, hidden.shape[:-1])
-    scale, log_sums = float(scale), bool(log_sums)
-    if not 2.0 ** -126 < scale < math.inf:
-        raise ValueError("scale must be positive and finite, got %r" % scale)
-    if labels is None and not log_sums:
-        raise ValueError("nothing to compute: give labels or ask for log_sums")
     _reverse_only(hidden, weight)
-    if torch.is_grad_enabled() and (hidden.requires_grad or weight.requires_grad):
-        return HeadLogProbs(*_HeadLogProbs.apply(hidden, weight, labels, scale, log_sums))
-    return HeadLogProbs(*_head_forward(hidden, weight, labels, scale, log_sums, False)[2:4])
-
-
-def _check_tokens(tokens, what, device, shape=None):
-    """Whole numbers that name rows of a table, contiguous."""
-    if tokens is None:
-        return None
-    if tokens.device != device:
-        raise ValueError("%s are on %s, not on %s" % (what, tokens.device, device))
-    if tokens.dtype == torch.bool:
-        tokens = tokens.contiguous().view(torch.uint8)
-    if tokens.dtype not in LABELS:
-        raise TypeError("%s must be uint8, bool, int32 or int64, got %s" % (what, tokens.dtype))
-    if shape is not None and tokens.shape != shape:
-        raise ValueError("%s of shape %s do not fit rows of shape %s" % (what, tuple(tokens.shape), tuple(shape)))
-    return tokens.contiguous()
-
-
-@functools.lru_cache(maxsize=1024)
-def _norm_workspace(dtype, rows, width):
-    return int(load().tm_layer_norm_grad_workspace_size(dtype, rows, width))
-
-
-def _norm_forward(x, weight, bias, eps, stats):
-    dev = x.device
-    out = torch.empty(x.shape, dtype=x.dtype, device=dev)
-    kept = torch.empty(x.shape[:-1] + (2,), dtype=torch.float32, device=dev) if stats else None
-    x, rows, stride = _rows(x)
-    param = weight if weight is not None else bias
-    _call("tm_layer_norm", dev, None, x.data_ptr(), FLOATS[x.dtype], rows, x.shape[-1], stride, _ptr(weight),
-          _ptr(bias), 0 if param is None else FLOATS[param.dtype], eps, out.data_ptr(), _ptr(kept))
-    return x, out, kept
-
-
-class _LayerNorm(torch.autograd.Function):
-    @staticmethod
-    def forward(ctx, x, weight, bias, eps):
-        x, out, kept = _norm_forward(x, weight, bias, eps, True)
-        ctx.save_for_backward(x, weight, kept)
-        param = weight if weight is not None else bias
-        ctx.what = (x.dtype, x.device, x.shape, None if param is None else param.dtype)
-        return out
-
-    @staticmethod
-    def backward(ctx, up):
-        _once()
-        x, weight, kept = ctx.saved_tensors
-        dtype, dev, shape, param = ctx.what
-        wants_x, wants_weight, wants_bias = ctx.needs_input_grad[:3]
-        if x.dtype is not dtype or x.device != dev or x.shape != shape:
-            _changed()
-        weight = _restored(weight, param, dev, shape[-1:])
-        kept = _restored(kept, torch.float32, dev, shape[:-1] + (2,))
-        up = up.contiguous()
-        x, rows, stride = _rows(x)
-        grad_x = torch.empty(shape, dtype=dtype, device=dev) if wants_x else None
-        grad_weight = torch.empty(shape[-1:], dtype=param, device=dev) if wants_weight else None
-        grad_bias = torch.empty(shape[-1:], dtype=param, device=dev) if wants_bias else None
-        nbytes = _norm_workspace(FLOATS[dtype], rows, shape[-1]) if wants_weight or wants_bias else 0
-        workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
-        _call("tm_layer_norm_grad", dev, None, x.data_ptr(), FLOATS[dtype], rows, shape[-1], stride, _ptr(weight),
-              0 if param is None else FLOATS[param], kept.data_ptr(), up.data_ptr(), _ptr(grad_x), _ptr(grad_weight),
-              _ptr(grad_bias), _ptr(workspace), nbytes)
-        return grad_x, grad_weight, grad_bias, None
+    return HeadLogProbs(*torch_ops().head_log_probs(hidden, weight, labels, scale, log_sums))
 
 
 def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, *,
@@ -687,69 +523,8 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
     Arithmetic and sums are float32; the result has the type of ``x``, rounded
     once.  Gradients flow to ``x``, ``weight`` and ``bias``.
     """
-    if not x.is_cuda:
-        raise ValueError("x must be a ROCm (cuda) tensor")
-    if x.dtype not in FLOATS:
-        raise TypeError("x must be float32, float16 or bfloat16, got %s" % x.dtype)
-    if x.dim() < 1 or x.shape[-1] < 1:
-        raise ValueError("x must be (..., width), got %s" % (tuple(x.shape),))
-    for what, param in (("weight", weight), ("bias", bias)):
-        if param is None:
-            continue
-        if param.dtype not in FLOATS:
-            raise TypeError("%s must be float32, float16 or bfloat16, got %s" % (what, param.dtype))
-        if param.device != x.device:
-            raise ValueError("%s is on %s, x on %s" % (what, param.device, x.device))
-        if param.shape != x.shape[-1:]:
-            raise ValueError("%s must be (%d,), got %s" % (what, x.shape[-1], tuple(param.shape)))
-    if weight is not None and bias is not None and weight.dtype != bias.dtype:
-        raise TypeError("weight and bias must have one type, got %s and %s" % (weight.dtype, bias.dtype))
-    eps = float(eps)
-    if not 2.0 ** -126 < eps < math.inf:
-        raise ValueError("eps must be positive and finite, got %r" % eps)
     _reverse_only(x, weight, bias)
-    weight = None if weight is None else weight.contiguous()
-    bias = None if bias is None else bias.contiguous()
-    if torch.is_grad_enabled() and (x.requires_grad or (weight is not None and weight.requires_grad)
-                                    or (bias is not None and bias.requires_grad)):
-        return _LayerNorm.apply(x, weight, bias, eps)
-    return _norm_forward(x, weight, bias, eps, False)[1]
-
-
-@functools.lru_cache(maxsize=1024)
-def _embedding_workspace(rows, width, count):
-    return int(load().tm_embedding_grad_workspace_size(rows, width, count))
-
-
-def _embedding_forward(tokens, table, scale):
-    dev, dtype, shape = table.device, table.dtype, table.shape
-    table, rows, stride = _rows(table)
-    out = torch.empty(tokens.shape + shape[1:], dtype=dtype, device=dev)
-    _call("tm_embedding", dev, None, table.data_ptr(), FLOATS[dtype], rows, shape[1], stride, tokens.data_ptr(),
-          LABELS[tokens.dtype], tokens.numel(), scale, out.data_ptr())
-    return out
-
-
-class _Embedding(torch.autograd.Function):
-    @staticmethod
-    def forward(ctx, tokens, table, scale):
-        ctx.save_for_backward(tokens)
-        ctx.what = (tokens.dtype, tokens.shape, table.dtype, table.device, table.shape, scale)
-        return _embedding_forward(tokens, table, scale)
-
-    @staticmethod
-    def backward(ctx, up):
-        _once()
-        tokens, = ctx.saved_tensors
-        token_dtype, shape, dtype, dev, table, scale = ctx.what
-        tokens = _restored(tokens, token_dtype, dev, shape)
-        up = up.contiguous()
-        grad = torch.empty(table, dtype=dtype, device=dev)
-        nbytes = _embedding_workspace(table[0], table[1], tokens.numel())
-        workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
-        _call("tm_embedding_grad", dev, None, tokens.data_ptr(), LABELS[token_dtype], tokens.numel(), up.data_ptr(),
-              FLOATS[dtype], table[0], table[1], scale, grad.data_ptr(), _ptr(workspace), nbytes)
-        return None, grad, None
+    return torch_ops().layer_norm(x, weight, bias, eps)
 
 
 def embedding(tokens: torch.Tensor, table: torch.Tensor, *, scale: float = 1.0) -> torch.Tensor:
@@ -766,17 +541,5 @@ def embedding(tokens: torch.Tensor, table: torch.Tensor, *, scale: float = 1.0) 
     together by sorting and summed in float32, in one order whatever their
     number, so that two calls give the same bits.
     """
-    if not table.is_cuda:
-        raise ValueError("table must be a ROCm (cuda) tensor")
-    if table.dtype not in FLOATS:
-        raise TypeError("table must be float32, float16 or bfloat16, got %s" % table.dtype)
-    if table.dim() != 2 or table.shape[0] < 1 or table.shape[1] < 1:
-        raise ValueError("table must be (rows, width), got %s" % (tuple(table.shape),))
-    tokens = _check_tokens(tokens, "tokens", table.device)
-    scale = float(scale)
-    if not -math.inf < scale < math.inf:
-        raise ValueError("scale must be finite, got %r" % scale)
     _reverse_only(table)
-    if torch.is_grad_enabled() and table.requires_grad:
-        return _Embedding.apply(tokens, table, scale)
-    return _embedding_forward(tokens, table, scale)
+    return torch_ops().embedding(tokens, table, scale)

@@ -16,6 +16,9 @@
 //     beta = scale (up_logp - up_log_sum),
 // and leaves g in the operands' type for the two products
 //     dh = g w,   dw = g^T h.
+// Its rounding to 16 bits is off by as much as that of the results.  With up to
+// kFineRows rows, of which few make up most of a result, g has two planes, 16
+// bits or more, which costs less there than it would among many.
 // Rows without a label take part only where the log sums are asked for: the
 // rows that do are packed first, and the products run over those alone.
 #pragma once
@@ -26,7 +29,8 @@
 namespace tmtrain {
 
 constexpr uint32_t kFewRows = 16;               // rows of hidden states that one matrix instruction holds
-constexpr uint32_t kListChunk = 4096;           // rows that a workgroup packs
+constexpr uint32_t kFineRows = 512;             // rows up to which g of 16-bit operands has two planes
+constexpr uint32_t kListChunk = 1024;           // rows that a workgroup counts
 
 struct HeadSum {
     float m, s;                 // M, sum of 2^(c h w - M)
@@ -64,7 +68,9 @@ struct HeadArgs {
     void *grad_hidden, *grad_weight;
     // in the workspace
     uint32_t *count;            // packed rows
-    uint32_t *chunk_count;      // of each chunk of the list, then their exponents
+    uint32_t *chunk_count;      // of each chunk, then their exponents
+    uint32_t chunks;            // 0: few rows, which are counted where they are needed
+    Div32 div_pieces;           // pieces of a packed row
     uint32_t *list;             // the packed rows' numbers
     int32_t *place;             // and where each row went, or -1
     HeadRow *row;
@@ -106,197 +112,181 @@ __device__ __forceinline__ HeadUp head_up(const HeadArgs &p, uint32_t n, int32_t
     return {p.scale * a, p.scale * (a - (p.up_log_sum ? p.up_log_sum[n] : 0.0f))};
 }
 
-// Sum over a workgroup of 1024 threads of what each holds: the sum of the lower threads' and the total.
-__device__ __forceinline__ uint32_t rank_in_block(uint32_t x, uint32_t *lds, uint32_t &total) {
-    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    uint32_t up = x;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const uint32_t o = __shfl_up(up, d);
-        if (lane >= uint32_t(d)) up += o;
-    }
-    __syncthreads();
-    if (lane == 63) lds[wave] = up;
-    __syncthreads();
-    uint32_t before = 0;
-    total = 0;
-    for (uint32_t w = 0; w < blockDim.x / 64; ++w) {
-        before += w < wave ? lds[w] : 0;
-        total += lds[w];
-    }
-    return before + up - x;
+// The label of row n, and whether the row takes part.
+__device__ __forceinline__ bool takes_part(const HeadArgs &p, uint32_t n, int32_t &y) {
+    y = p.label ? load_label(p.label, p.label_bytes, n, p.classes) : -1;
+    return y >= 0 || p.all;
+}
+// Exponent of a row's slopes, kNoExponent for zeros.
+constexpr int kNoExponent = -1000;
+__device__ __forceinline__ int slope_exponent(HeadUp u) {
+    const float size = fabsf(u.a) + fabsf(u.b);
+    return size > 0.0f ? exponent_of(size) : kNoExponent;
 }
 
-// Four rows a thread: which take part, and the largest exponent of theirs.
-struct HeadFour {
-    int32_t y[4];
-    uint32_t in;
-    int exponent;
-};
-__device__ __forceinline__ HeadFour head_four(const HeadArgs &p, uint32_t n0, bool exponents) {
-    HeadFour f{};
-    f.exponent = -1000;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t n = n0 + i;
-        f.y[i] = -1;
-        if (n >= p.n) continue;
-        f.y[i] = p.label ? load_label(p.label, p.label_bytes, n, p.classes) : -1;
-        if (f.y[i] < 0 && !p.all) continue;
-        f.in |= 1u << i;
-        if (exponents) {
-            const HeadUp u = head_up(p, n, f.y[i]);
-            const float size = fabsf(u.a) + fabsf(u.b);
-            if (size > 0.0f) f.exponent = max(f.exponent, exponent_of(size));
-        }
+// Adds up a workgroup's counts and takes the largest of its exponents: whole numbers, whose order does not matter.
+__device__ __forceinline__ void tally(uint32_t mine, int most, uint32_t *found, int *top) {
+    const uint32_t all = wave_reduce(mine, 0u, [](uint32_t a, uint32_t b) { return a + b; });
+    const int best = int(wave_max(uint32_t(most - kNoExponent))) + kNoExponent;
+    if ((threadIdx.x & 63) == 0) {
+        atomicAdd(found, all);
+        atomicMax(top, best);
     }
-    return f;
 }
 
-// Rows of each chunk that take part (and their largest exponent), where there are several chunks.
-__global__ __launch_bounds__(1024) void k_head_count(HeadArgs p) {
-    __shared__ uint32_t lds[16];
+// Rows of each chunk that take part (and their largest exponent), where there are many chunks.
+__global__ __launch_bounds__(256) void k_head_count(HeadArgs p) {
+    __shared__ uint32_t found;
     __shared__ int top;
-    if (threadIdx.x == 0) top = -1000;
-    __syncthreads();
-    const HeadFour f = head_four(p, blockIdx.x * kListChunk + threadIdx.x * 4, p.inverse != nullptr);
-    if (p.inverse) atomicMax(&top, f.exponent);             // the order does not matter
-    uint32_t total;
-    rank_in_block(__popc(f.in), lds, total);
     if (threadIdx.x == 0) {
-        p.chunk_count[blockIdx.x] = total;
+        found = 0;
+        top = kNoExponent;
+    }
+    __syncthreads();
+    const uint32_t last = min(p.n, (blockIdx.x + 1) * kListChunk);
+    uint32_t mine = 0;
+    int most = kNoExponent;
+#pragma unroll 4
+    for (uint32_t n = blockIdx.x * kListChunk + threadIdx.x; n < last; n += 256) {
+        int32_t y;
+        if (!takes_part(p, n, y)) continue;
+        ++mine;
+        if (p.inverse) most = max(most, slope_exponent(head_up(p, n, y)));
+    }
+    tally(mine, most, &found, &top);
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        p.chunk_count[blockIdx.x] = found;
         p.chunk_count[gridDim.x + blockIdx.x] = uint32_t(top);
     }
 }
 
-// The list of packed rows, where each row went, and for the gradient what its
-// tiles need of them.  One workgroup to a chunk.
-__global__ __launch_bounds__(1024) void k_head_list(HeadArgs p) {
-    __shared__ uint32_t lds[16];
-    __shared__ int top;
-    const uint32_t chunks = gridDim.x, chunk = blockIdx.x;
-    if (threadIdx.x == 0) top = -1000;
-    __syncthreads();
-    const bool exponents = p.inverse != nullptr;
-    const uint32_t n0 = chunk * kListChunk + threadIdx.x * 4;
-    const HeadFour f = head_four(p, n0, exponents);
-    uint32_t before = 0, all = 0;
-    if (chunks > 1) {
-        uint32_t mine = 0, sum = 0;
-        for (uint32_t i = threadIdx.x; i < chunks; i += blockDim.x) {
-            const uint32_t x = p.chunk_count[i];
-            sum += x;
-            mine += i < chunk ? x : 0;
-            if (exponents) atomicMax(&top, int(p.chunk_count[chunks + i]));
-        }
-        uint32_t total;
-        rank_in_block(mine, lds, before);
-        rank_in_block(sum, lds, total);
-        all = total;
-    } else if (exponents) {
-        atomicMax(&top, f.exponent);
-    }
-    uint32_t total;
-    uint32_t at = before + rank_in_block(__popc(f.in), lds, total);
-    if (chunks == 1) all = total;
-    __syncthreads();
-    const int common = top < -900 ? 0 : top;
-    if (threadIdx.x == 0 && chunk == 0) {
-        *p.count = all;
-        if (exponents) p.inverse[p.n_pad] = power(common - kSlopeExponent);
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t n = n0 + i;
-        if (n >= p.n) break;
-        const bool in = f.in >> i & 1;
-        if (p.place) p.place[n] = in ? int32_t(at) : -1;
-        if (!in) {
-            if (!p.row && p.logp) p.logp[n] = 0.0f;
-            if (!p.row && p.stats) p.stats[n] = {0.0f, 1.0f};
-            continue;
-        }
-        p.list[at] = n;
-        if (p.row) {
-            HeadUp u = head_up(p, n, f.y[i]);
-            const HeadSum s = p.stats[n];
-            if (s.s == 0.0f) u = {0.0f, 0.0f};              // no class left
-            HeadRow r = {s.m, u.a, s.s == 0.0f ? 0.0f : u.b / s.s, f.y[i]};
-            if (exponents) {
-                const float size = fabsf(u.a) + fabsf(u.b);
-                const int e = size > 0.0f ? exponent_of(size) : common;
-                r.a = __builtin_amdgcn_ldexpf(r.a, kSlopeExponent - e);
-                r.b = __builtin_amdgcn_ldexpf(r.b, kSlopeExponent - e);
-                p.inverse[at] = power(e - kSlopeExponent);
-            }
-            p.row[at] = r;
-        }
-        ++at;
-    }
-}
-
-// Rows of `width` elements, `stride` apart, laid out in whole steps with zeros
-// behind them.
-struct LayArgs {
-    const void *from;
-    uint64_t stride;
-    const uint32_t *list, *count;   // which rows, and zeros up to a multiple of 64; NULL: `rows` of them in order
-    uint32_t rows, width;
-    void *to;
-    uint32_t to_stride;             // elements
-    uint64_t plane;                 // elements of a plane, for the three of k_split_rows
-};
-template <typename T>
-__global__ __launch_bounds__(256) void k_lay_rows(LayArgs p) {
-    constexpr int V = 16 / sizeof(T);
-    const uint32_t rows = p.count ? *p.count : p.rows, end = p.count ? (rows + 63) & ~63u : rows;
-    const uint32_t pieces = p.to_stride / V;
-    for (uint32_t r = blockIdx.x * blockDim.y + threadIdx.y; r < end; r += gridDim.x * blockDim.y) {
-        const uint32_t width = r < rows ? p.width : 0;
-        const T *from = static_cast<const T *>(p.from) + (width && p.list ? p.list[r] : r) * p.stride;
-        T *to = static_cast<T *>(p.to) + uint64_t(r) * p.to_stride;
-        for (uint32_t i = threadIdx.x; i < pieces; i += blockDim.x) {
-            const uint32_t c = i * V;
-            store_pack<V>(to + c, c < width ? load_pack<V>(from + c, width - c, T{}) : Pack<T, V>{});
-        }
-    }
-}
-
-// x as three numbers of 8 bits each, whose sum it is; not finite: NaN.
-template <int V>
-__device__ __forceinline__ void split(const float (&x)[V], Pack<bf16, V> (&out)[3]) {
+// x in planes, each of what the ones before it leave; not finite: NaN.
+template <typename T, int V, int P>
+__device__ __forceinline__ void split(const float (&x)[V], Pack<T, V> (&out)[P]) {
     float rest[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) rest[j] = x[j];
 #pragma unroll
-    for (int p = 0; p < 3; ++p) {
-        out[p] = narrow_pack<bf16>(rest);
+    for (int p = 0; p < P; ++p) {
+        out[p] = narrow_pack<T>(rest);
 #pragma unroll
         for (int j = 0; j < V; ++j) rest[j] -= widen(out[p].at(j));
     }
 }
 
-// Floats laid out likewise, in three planes.
-__global__ __launch_bounds__(256) void k_split_rows(LayArgs p) {
-    constexpr int V = 8;
-    const uint32_t rows = p.count ? *p.count : p.rows, end = p.count ? (rows + 63) & ~63u : rows;
-    const uint32_t pieces = p.to_stride / V;
-    for (uint32_t r = blockIdx.x * blockDim.y + threadIdx.y; r < end; r += gridDim.x * blockDim.y) {
-        const uint32_t width = r < rows ? p.width : 0;
-        const float *from = static_cast<const float *>(p.from) + (width && p.list ? p.list[r] : r) * p.stride;
-        bf16 *to = static_cast<bf16 *>(p.to) + uint64_t(r) * p.to_stride;
-        for (uint32_t i = threadIdx.x; i < pieces; i += blockDim.x) {
-            const uint32_t c = i * V;
-            const Pack<float, V> q = c < width ? load_pack<V>(from + c, width - c, 0.0f) : Pack<float, V>{};
-            float x[V];
+// V elements as they are laid out: in P planes of S, `plane` elements apart.
+template <typename T, typename S, int P, int V>
+__device__ __forceinline__ void lay(const T *from, uint32_t n, S *to, uint64_t plane) {
+    Pack<T, V> q{};
+    if (n) q = load_pack<V>(from, n, T{});
+    if constexpr (P == 1) {
+        store_pack<V>(to, q);
+    } else {
+        float x[V];
 #pragma unroll
-            for (int j = 0; j < V; ++j) x[j] = q.at(j);
-            Pack<bf16, V> planes[3];
-            split(x, planes);
+        for (int j = 0; j < V; ++j) x[j] = widen(q.at(j));
+        Pack<S, V> planes[P];
+        split(x, planes);
 #pragma unroll
-            for (int k = 0; k < 3; ++k) store_pack<V>(to + k * p.plane + c, planes[k]);
+        for (int k = 0; k < P; ++k) store_pack<V>(to + k * plane, planes[k]);
+    }
+}
+
+// Packs the hidden states of kPackRows rows, in whole steps with zeros behind
+// them, and writes where they went and what the gradient needs of them.  Every
+// workgroup counts the rows before its own: all of them, or those of its chunk
+// and the chunks' counts.  The last one leaves zeros up to a multiple of 64.
+constexpr uint32_t kPackRows = 8;
+template <typename T, typename S, int P>
+__global__ __launch_bounds__(256) void k_head_pack(HeadArgs p) {
+    constexpr uint32_t V = 16 / sizeof(S);
+    __shared__ uint32_t before, own;
+    __shared__ int top;
+    __shared__ uint32_t from[kPackRows];
+    if (threadIdx.x == 0) {
+        before = 0;
+        top = kNoExponent;
+    }
+    __syncthreads();
+    const uint32_t r0 = blockIdx.x * kPackRows, chunk = r0 / kListChunk;
+    const bool exponents = p.inverse != nullptr;
+    uint32_t mine = 0;
+    int most = kNoExponent;
+    const uint32_t last = exponents && !p.chunks ? p.n : r0;
+#pragma unroll 4
+    for (uint32_t n = (p.chunks ? chunk * kListChunk : 0) + threadIdx.x; n < last; n += 256) {
+        int32_t y;
+        if (!takes_part(p, n, y)) continue;
+        mine += n < r0;
+        if (exponents && !p.chunks) most = max(most, slope_exponent(head_up(p, n, y)));
+    }
+    for (uint32_t i = threadIdx.x; i < p.chunks; i += 256) {
+        mine += i < chunk ? p.chunk_count[i] : 0;
+        if (exponents) most = max(most, int(p.chunk_count[p.chunks + i]));
+    }
+    tally(mine, most, &before, &top);
+    __syncthreads();
+    if (threadIdx.x < 64) {
+        const uint32_t n = r0 + threadIdx.x;
+        int32_t y = -1;
+        const bool real = threadIdx.x < kPackRows && n < p.n, in = real && takes_part(p, n, y);
+        const uint64_t set = __ballot(in);
+        const uint32_t rank = __popcll(set & ((uint64_t(1) << threadIdx.x) - 1)), at = before + rank;
+        if (threadIdx.x == 0) own = __popcll(set);
+        const int common = top == kNoExponent ? 0 : top;
+        if (threadIdx.x == 0 && blockIdx.x == 0 && exponents) p.inverse[p.n_pad] = power(common - kSlopeExponent);
+        if (real && p.place) p.place[n] = in ? int32_t(at) : -1;
+        if (real && !in && !p.row) {
+            if (p.logp) p.logp[n] = 0.0f;
+            if (p.stats) p.stats[n] = {0.0f, 1.0f};
+        }
+        if (in) {
+            from[rank] = n;
+            p.list[at] = n;
+            if (p.row) {
+                HeadUp u = head_up(p, n, y);
+                const HeadSum s = p.stats[n];
+                if (s.s == 0.0f) u = {0.0f, 0.0f};          // no class left
+                HeadRow r = {s.m, u.a, s.s == 0.0f ? 0.0f : u.b / s.s, y};
+                if (exponents) {
+                    int e = slope_exponent(u);
+                    if (e == kNoExponent) e = common;
+                    r.a = __builtin_amdgcn_ldexpf(r.a, kSlopeExponent - e);
+                    r.b = __builtin_amdgcn_ldexpf(r.b, kSlopeExponent - e);
+                    p.inverse[at] = power(e - kSlopeExponent);
+                }
+                p.row[at] = r;
+            }
         }
     }
+    __syncthreads();
+    const bool final = blockIdx.x + 1 == gridDim.x;
+    const uint32_t total = before + own;
+    if (final && threadIdx.x == 0) *p.count = total;
+    const uint32_t pieces = p.width_pad / V, rows = final ? ((total + 63) & ~63u) - before : own;
+    const uint64_t plane = uint64_t(p.n_pad) * p.width_pad;
+#pragma unroll 4
+    for (uint32_t i = threadIdx.x; i < rows * pieces; i += 256) {
+        const uint32_t r = p.div_pieces.div(i), c = (i - r * pieces) * V;
+        const bool real = r < own && c < p.width;
+        lay<T, S, P, V>(static_cast<const T *>(p.hidden) + (real ? from[r] * p.hidden_stride + c : 0),
+                        real ? p.width - c : 0, static_cast<S *>(p.packed) + uint64_t(before + r) * p.width_pad + c, plane);
+    }
+}
+
+// The weights of the piece at hand, laid out likewise.
+template <typename T, typename S, int P>
+__global__ __launch_bounds__(256) void k_head_lay(HeadArgs p) {
+    constexpr uint32_t V = 16 / sizeof(S);
+    const uint32_t rows = min(p.piece, p.classes - p.first), pieces = p.width_pad / V;
+    for (uint32_t r = blockIdx.x * blockDim.y + threadIdx.y; r < rows; r += gridDim.x * blockDim.y)
+        for (uint32_t i = threadIdx.x; i < pieces; i += blockDim.x) {
+            const uint32_t c = i * V;
+            lay<T, S, P, V>(static_cast<const T *>(p.weight) + (p.first + r) * p.weight_stride + c,
+                            c < p.width ? p.width - c : 0, static_cast<S *>(p.weight_laid) + uint64_t(r) * p.width_pad + c,
+                            uint64_t(p.piece) * p.width_pad);
+        }
 }
 
 // ---------------------------------------------------------------------------
@@ -437,35 +427,37 @@ __device__ __forceinline__ void head_store(const HeadArgs &p, uint32_t n, const 
     if (p.stats) p.stats[n] = sum;
 }
 
-// The sums of a row over all parts: 64 rows to a workgroup, parts over its 16 waves.
+// The sums of a row over all parts: 16 rows to a workgroup, parts over its 64 rows of threads.
 __global__ __launch_bounds__(1024) void k_head_join(HeadArgs p) {
-    __shared__ HeadSum lds[16][64];
+    constexpr uint32_t kRows = 16, kShares = 64;
+    __shared__ HeadSum lds[16][kRows];
     const uint32_t count = *p.count;
-    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint32_t j = blockIdx.x * 64 + lane;
-    if (blockIdx.x * 64 >= count) return;
+    if (blockIdx.x * kRows >= count) return;
+    const uint32_t row = threadIdx.x % kRows, share = threadIdx.x / kRows, j = blockIdx.x * kRows + row;
     HeadSum sum = {kLowest, 0.0f};
     if (j < count) {
         // several loads on their way at once
         constexpr int kAhead = 8;
-        for (uint32_t i = wave; i < p.parts; i += 16 * kAhead) {
+        for (uint32_t i = share; i < p.parts; i += kShares * kAhead) {
             HeadSum got[kAhead];
 #pragma unroll
             for (int k = 0; k < kAhead; ++k)
-                got[k] = i + 16 * k < p.parts ? p.part[uint64_t(i + 16 * k) * p.n_pad + j] : HeadSum{kLowest, 0.0f};
+                got[k] = i + kShares * k < p.parts ? p.part[uint64_t(i + kShares * k) * p.n_pad + j] : HeadSum{kLowest, 0.0f};
 #pragma unroll
             for (int k = 0; k < kAhead; ++k) sum = join(sum, got[k]);
         }
     }
-    lds[wave][lane] = sum;
+#pragma unroll
+    for (int d = 16; d < 64; d <<= 1) sum = join(sum, HeadSum{__shfl_xor(sum.m, d), __shfl_xor(sum.s, d)});
+    if ((threadIdx.x & 63) < kRows) lds[threadIdx.x >> 6][row] = sum;
     __syncthreads();
-    if (wave || j >= count) return;
-    for (int w = 1; w < 16; ++w) sum = join(sum, lds[w][lane]);
+    if (threadIdx.x >= kRows || j >= count) return;
+    for (int w = 1; w < 16; ++w) sum = join(sum, lds[w][row]);
     head_store(p, p.list[j], p.found + j, sum);
 }
 
-// g of a piece of the vocabulary.
-template <typename T, typename Tile>
+// g of a piece of the vocabulary, in G planes.
+template <typename T, typename Tile, int G>
 __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_slopes(HeadArgs p) {
     typedef Held<T, Tile> S;
     __shared__ __attribute__((aligned(1024))) typename Tile::Buffer even, odd;
@@ -506,21 +498,20 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_slope
                     for (int q = 0; q < 4; ++q)
                         if (n >= count || v + q >= rows) g[q] = 0.0f;
                 }
-                S *to = static_cast<S *>(p.slope) + uint64_t(n) * p.piece + v;
-                if constexpr (Tile::kPlanes == 3) {
-                    Pack<bf16, 4> planes[3];
-                    split(g, planes);
+                const uint64_t to = uint64_t(n) * p.piece + v, plane = uint64_t(p.n_pad) * p.piece;
+                Pack<S, 4> out[G];
+                if (!__is_same(T, f16) || p.slope) {
+                    split(g, out);
 #pragma unroll
-                    for (int k = 0; k < 3; ++k) store_pack<4>(to + k * uint64_t(p.n_pad) * p.piece, planes[k]);
-                } else if (p.slope) {
-                    store_pack<4>(to, narrow_pack<T>(g));
+                    for (int k = 0; k < G; ++k) store_pack<4>(static_cast<S *>(p.slope) + to + k * plane, out[k]);
                 }
                 if constexpr (__is_same(T, f16)) {
-                    if (p.slope_common) {
+                    if (!p.slope_common) continue;
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) g[q] *= ratios[j];
-                        store_pack<4>(static_cast<T *>(p.slope_common) + uint64_t(n) * p.piece + v, narrow_pack<T>(g));
-                    }
+                    for (int q = 0; q < 4; ++q) g[q] *= ratios[j];
+                    split(g, out);
+#pragma unroll
+                    for (int k = 0; k < G; ++k) store_pack<4>(static_cast<S *>(p.slope_common) + to + k * plane, out[k]);
                 }
             }
         }

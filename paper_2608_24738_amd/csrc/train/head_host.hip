@@ -79,6 +79,9 @@ bool planes(const HeadShape &s) { return s.size == 4 && s.n > kPlaneRows; }
 template <typename Tile>
 constexpr uint64_t kSlots = (2 * sizeof(typename Tile::Buffer) <= 80 * 1024 ? 2 : 1) * kCus;
 
+// 16-bit operands whose g has two planes.
+bool fine(const HeadShape &s) { return s.size == 2 && s.n <= kFineRows; }
+
 // fn(tile): the larger of two, unless it leaves CUs without one; `most` is how
 // often k can be split.
 template <typename T, bool Across, typename F>
@@ -87,12 +90,15 @@ auto by_tile(const HeadShape &s, uint64_t m, uint64_t n, uint64_t most, F fn) {
     if constexpr (std::is_same<T, float>::value) {
         if (planes(s)) return large ? fn(static_cast<LargeSplit *>(nullptr)) : fn(static_cast<SmallSplit *>(nullptr));
     }
+    if constexpr (Across && sizeof(T) == 2) {
+        if (fine(s)) return fn(static_cast<FineTile<T> *>(nullptr));
+    }
     return large ? fn(static_cast<LargeTile<T, Across> *>(nullptr)) : fn(static_cast<SmallTile<T> *>(nullptr));
 }
-// The same where the type does not matter: all have tiles of one size but for the planes.
-template <typename F>
+// The same where no kernel is meant.
+template <bool Across, typename F>
 auto by_tile_size(const HeadShape &s, uint64_t m, uint64_t n, uint64_t most, F fn) {
-    return by_tile<float, false>(s, m, n, most, fn);
+    return s.size == 4 ? by_tile<float, Across>(s, m, n, most, fn) : by_tile<bf16, Across>(s, m, n, most, fn);
 }
 
 // Tiles read whole steps of the weight's rows, 16 bytes at a time and with offsets of 32 bits: whether it is to be laid
@@ -117,8 +123,9 @@ void head_sizes(const HeadShape &s, HeadArgs &a) {
     a.n_pad = uint32_t(few(s) ? kFewRows : whole_tiles(s.n));
 }
 
-// Bytes of a laid out element.
+// Bytes of a laid out element, and of one of g.
 uint64_t held(const HeadShape &s) { return planes(s) ? 6 : s.size; }
+uint64_t slope_held(const HeadShape &s) { return fine(s) ? 4 : held(s); }
 
 // Layout of the forward call's workspace; returns its size.
 uint64_t head_room(const HeadShape &s, bool laid, void *at, HeadArgs &a) {
@@ -130,7 +137,7 @@ uint64_t head_room(const HeadShape &s, bool laid, void *at, HeadArgs &a) {
         a.part = room.take<HeadSum>(uint64_t(a.parts) * a.n);
         return room.used;
     }
-    a.parts = by_tile_size(s, s.classes, s.n, 1, [&](auto *t) {
+    a.parts = by_tile_size<false>(s, s.classes, s.n, 1, [&](auto *t) {
         using Tile = std::remove_pointer_t<decltype(t)>;
         return uint32_t(ceil_div(s.classes, Tile::BM) * Tile::WM);
     });
@@ -166,13 +173,13 @@ uint64_t head_grad_room(const HeadShape &s, int dtype, bool laid, bool hidden, b
         if (hidden) a.sum = room.take<float>(uint64_t(a.splits) * s.n * a.sum_stride);
         return room.used;
     }
-    a.piece = uint32_t(piece_of(s.classes, a.n_pad * held(s), kPieceBytes));
+    a.piece = uint32_t(piece_of(s.classes, a.n_pad * slope_held(s), kPieceBytes));
     a.sum_stride = uint32_t(ceil_div(s.width, 4) * 4);
     // dh: a workgroup to every CU (two of the small tiles, where LDS has room), which the kernel spreads over the tiles
     // that the packed rows take and splits of k, each of 8 steps at least
     const uint64_t steps = a.piece / (s.size == 4 ? 32 : 64);
     a.most = uint32_t(std::max<uint64_t>(1, std::min<uint64_t>(steps / 8, 32)));
-    by_tile_size(s, s.width, s.n, a.most, [&](auto *t) {
+    by_tile_size<true>(s, s.width, s.n, a.most, [&](auto *t) {
         using Tile = std::remove_pointer_t<decltype(t)>;
         a.tiles_m = uint32_t(ceil_div(s.width, Tile::BM));
         a.tile_n = Tile::BN;
@@ -186,7 +193,7 @@ uint64_t head_grad_room(const HeadShape &s, int dtype, bool laid, bool hidden, b
     a.row = room.take<HeadRow>(a.n_pad);
     if (dtype == TM_DTYPE_F16) a.inverse = room.take<float>(a.n_pad + 1);
     a.packed = room.take<char>(uint64_t(a.n_pad) * a.width_pad * held(s));
-    const uint64_t slopes = uint64_t(a.n_pad) * a.piece * held(s);
+    const uint64_t slopes = uint64_t(a.n_pad) * a.piece * slope_held(s);
     if (hidden || dtype != TM_DTYPE_F16) a.slope = room.take<char>(slopes);
     if (weight && dtype == TM_DTYPE_F16) a.slope_common = room.take<char>(slopes);
     if (hidden) {
@@ -206,48 +213,35 @@ dim3 lasting_grid(uint64_t m, uint64_t n) {
     return dim3(uint32_t(std::min<uint64_t>(tile_grid<Tile>(m, n).x, kSlots<Tile>)));
 }
 
-// Rows laid out in whole steps, or in planes.
+// The packed rows.
 template <typename T>
-int lay(const HeadShape &s, LayArgs l, hipStream_t stream) {
+int pack_rows(const HeadShape &s, HeadArgs &a, hipStream_t stream) {
+    a.chunks = a.n <= 2 * kListChunk ? 0 : uint32_t(ceil_div(a.n, kListChunk));
+    if (a.chunks) {
+        const int rc = launch(k_head_count, dim3(a.chunks), dim3(256), 0, stream, a);
+        if (rc != TM_OK) return rc;
+    }
     const bool split = std::is_same<T, float>::value && planes(s);
-    const uint32_t x = std::min<uint32_t>(256, pow2_from(uint32_t(ceil_div(uint64_t(l.to_stride) * (split ? 2 : sizeof(T)), 16))));
-    const dim3 block(x, 256 / x), grid(uint32_t(std::min<uint64_t>(ceil_div(l.rows, block.y), 4096)));
-    return launch(split ? k_split_rows : k_lay_rows<T>, grid, block, 0, stream, l);
-}
-
-// The list of packed rows, and the rows.
-template <typename T>
-int pack_rows(const HeadShape &s, const HeadArgs &a, hipStream_t stream) {
-    const uint32_t chunks = uint32_t(ceil_div(a.n, kListChunk));
-    int rc = TM_OK;
-    if (chunks > 1) rc = launch(k_head_count, dim3(chunks), dim3(1024), 0, stream, a);
-    if (rc == TM_OK) rc = launch(k_head_list, dim3(chunks), dim3(1024), 0, stream, a);
-    if (rc != TM_OK) return rc;
-    LayArgs l{};
-    l.from = a.hidden;
-    l.stride = a.hidden_stride;
-    l.list = a.list;
-    l.count = a.count;
-    l.rows = a.n;
-    l.width = a.width;
-    l.to = a.packed;
-    l.to_stride = a.width_pad;
-    l.plane = uint64_t(a.n_pad) * a.width_pad;
-    return lay<T>(s, l, stream);
+    a.div_pieces = Div32::make(uint32_t(a.width_pad * (split ? 2 : sizeof(T)) / 16));
+    const dim3 grid(uint32_t(ceil_div(a.n, kPackRows)));
+    if constexpr (std::is_same<T, float>::value) {
+        if (split) return launch(k_head_pack<float, bf16, 3>, grid, dim3(256), 0, stream, a);
+    }
+    return launch(k_head_pack<T, T, 1>, grid, dim3(256), 0, stream, a);
 }
 
 // The weights of the piece at hand.
 template <typename T>
 int lay_piece(const HeadShape &s, const HeadArgs &a, hipStream_t stream) {
-    LayArgs l{};
-    l.from = static_cast<const T *>(a.weight) + uint64_t(a.first) * a.weight_stride;
-    l.stride = a.weight_stride;
-    l.rows = std::min(a.piece, a.classes - a.first);
-    l.width = a.width;
-    l.to = a.weight_laid;
-    l.to_stride = a.width_pad;
-    l.plane = uint64_t(a.piece) * a.width_pad;
-    return lay<T>(s, l, stream);
+    const bool split = std::is_same<T, float>::value && planes(s);
+    const uint64_t pieces = a.width_pad * (split ? 2 : sizeof(T)) / 16;
+    const uint32_t x = uint32_t(std::min<uint64_t>(256, pow2_from(uint32_t(pieces))));
+    const uint64_t rows = std::min(a.piece, a.classes - a.first);
+    const dim3 block(x, 256 / x), grid(uint32_t(std::min<uint64_t>(ceil_div(rows, block.y), 4096)));
+    if constexpr (std::is_same<T, float>::value) {
+        if (split) return launch(k_head_lay<float, bf16, 3>, grid, block, 0, stream, a);
+    }
+    return launch(k_head_lay<T, T, 1>, grid, block, 0, stream, a);
 }
 
 template <typename T>
@@ -268,7 +262,7 @@ int run_head(HeadArgs a, const HeadShape &s, hipStream_t stream) {
                           dim3(Tile::kThreads), 0, stream, a);
         });
     }
-    return rc == TM_OK ? launch(k_head_join, dim3(uint32_t(ceil_div(s.n, 64))), dim3(1024), 0, stream, a) : rc;
+    return rc == TM_OK ? launch(k_head_join, dim3(uint32_t(ceil_div(s.n, 16))), dim3(1024), 0, stream, a) : rc;
 }
 
 template <typename T>
@@ -295,7 +289,12 @@ int run_head_grad(HeadArgs a, const HeadShape &s, hipStream_t stream) {
         if (rc != TM_OK) break;
         rc = by_tile<T, false>(s, a.piece, s.n, 1, [&](auto *t) {
             using Tile = std::remove_pointer_t<decltype(t)>;
-            return launch(k_head_slopes<T, Tile>, lasting_grid<Tile>(a.piece, s.n), dim3(Tile::kThreads), 0, stream, a);
+            constexpr int G = Tile::kPlanes;
+            auto kernel = k_head_slopes<T, Tile, G>;
+            if constexpr (sizeof(T) == 2) {
+                if (fine(s)) kernel = k_head_slopes<T, Tile, 2>;
+            }
+            return launch(kernel, lasting_grid<Tile>(a.piece, s.n), dim3(Tile::kThreads), 0, stream, a);
         });
         if (rc == TM_OK && a.grad_hidden) {
             rc = by_tile<T, true>(s, s.width, s.n, a.most, [&](auto *t) {

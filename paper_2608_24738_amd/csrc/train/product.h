@@ -197,22 +197,24 @@ struct Across {
     }
 };
 
-// BM x BN elements by WM x WN waves.  With three planes, an operand's floats
-// are held as sums of three of T = bf16, x = h + m + l, exact since each takes
-// eight more bits, and a product is hh + hm + mh + mm + hl + lh: what is left
-// out is below 2^-23 of it, and six instructions of 16 bits take less time than
-// those of floats (head.h has the figures).
-template <typename T, int BM_, int BN_, int WM_, int WN_, int Planes = 1>
+// BM x BN elements by WM x WN waves.  An operand may lie in planes of T, whose
+// sum it is.  Three of bf16 hold a float, x = h + m + l, exactly, since each
+// takes eight more bits; a product of two is hh + hm + mh + mm + hl + lh, what is
+// left out being below 2^-23 of it, and six instructions of 16 bits take less
+// time than those of floats (2048 x 16384 x 1024: sums 309 us and 495).  All but
+// hh have sums of their own: they are 2^-8 of the whole and add no rounding at
+// its size.  Two planes, of B alone, make 16 or 22 bits of a number.
+template <typename T, int BM_, int BN_, int WM_, int WN_, int PlanesA = 1, int PlanesB = PlanesA>
 struct Tile {
-    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, kPlanes = Planes;
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, kPlanes = PlanesA, kPlanesB = PlanesB;
     static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves;
     static constexpr int TM = BM / WM / 16, TN = BN / WN / 16;              // 16 x 16 blocks of a wave
-    static constexpr int kHalves = Planes == 1 ? 2 : 1;                     // instructions' worth of k in a step
+    static constexpr int kHalves = PlanesB == 1 ? 2 : 1;                    // instructions' worth of k in a step
     static constexpr int kStep = kHalves * 64 / int(sizeof(T));             // elements
     static constexpr int kPlaneA = BM * kHalves * 64, kPlaneB = BN * kHalves * 64;     // bytes of a plane's step
 
     struct Buffer {
-        char a[Planes * kPlaneA], b[Planes * kPlaneB];
+        char a[PlanesA * kPlaneA], b[PlanesB * kPlaneB];
     };
 
     f32x4 acc[TM][TN];
@@ -233,24 +235,23 @@ struct Tile {
         typedef std::conditional_t<BAcross, Across<T, BN, kWaves, kStep, TN>, Along<T, BN, kWaves, kStep>> FromB;
         // Waves with their operands at hand go first (4096 x 32768 x 1024: sums 246 -> 238 us); those that
         // read across k would hold up the others' reads (dw 121 -> 158), and planes leave time (309 -> 321).
-        static constexpr bool kFirst = !AAcross && !BAcross && Planes == 1;
-        FromA a[Planes];
-        FromB b[Planes];
+        static constexpr bool kFirst = !AAcross && !BAcross && PlanesB == 1;
+        FromA a[PlanesA];
+        FromB b[PlanesB];
 
-        template <size_t... I>
+        template <size_t... I, size_t... J>
         __device__ __forceinline__ Sources(const Tile &t, const Operand &x, uint32_t m0, const Operand &y, uint32_t n0,
-                                           uint32_t first, std::index_sequence<I...>)
+                                           uint32_t first, std::index_sequence<I...>, std::index_sequence<J...>)
             : a{FromA({x.at + I * x.plane, x.stride, 0, x.rows, x.pieces}, m0, first, t.lane, t.wave)...},
-              b{FromB({y.at + I * y.plane, y.stride, 0, y.rows, y.pieces}, n0, first, t.lane, t.wave)...} {
+              b{FromB({y.at + J * y.plane, y.stride, 0, y.rows, y.pieces}, n0, first, t.lane, t.wave)...} {
             a[0].reads(t.lane, (t.wave / WN) * TM);
             b[0].reads(t.lane, (t.wave % WN) * TN);
         }
         __device__ __forceinline__ void fetch(const Tile &t, Buffer &s, uint32_t step) {
 #pragma unroll
-            for (int p = 0; p < Planes; ++p) {
-                a[p].fetch(s.a + p * kPlaneA, step, t.lane, t.wave);
-                b[p].fetch(s.b + p * kPlaneB, step, t.lane, t.wave);
-            }
+            for (int p = 0; p < PlanesA; ++p) a[p].fetch(s.a + p * kPlaneA, step, t.lane, t.wave);
+#pragma unroll
+            for (int p = 0; p < PlanesB; ++p) b[p].fetch(s.b + p * kPlaneB, step, t.lane, t.wave);
         }
     };
 
@@ -258,7 +259,8 @@ struct Tile {
     template <bool AAcross, bool BAcross>
     __device__ __forceinline__ Sources<AAcross, BAcross> begin(const Operand &a, uint32_t m0, const Operand &b, uint32_t n0,
                                                                uint32_t first, Buffer &even) const {
-        Sources<AAcross, BAcross> from(*this, a, m0, b, n0, first, std::make_index_sequence<Planes>{});
+        Sources<AAcross, BAcross> from(*this, a, m0, b, n0, first, std::make_index_sequence<PlanesA>{},
+                                       std::make_index_sequence<PlanesB>{});
         from.fetch(*this, even, first);
         return from;
     }
@@ -271,31 +273,40 @@ struct Tile {
         for (int i = 0; i < TM; ++i)
 #pragma unroll
             for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        f32x4 low[PlanesA == 3 ? TM : 1][PlanesA == 3 ? TN : 1];
+        if constexpr (PlanesA == 3) {
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) low[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        }
         const auto work = [&](const Buffer &s) {
 #pragma unroll
             for (int half = 0; half < kHalves; ++half) {
-                u32x4 fa[Planes][TM], fb[Planes][TN];
+                u32x4 fa[PlanesA][TM], fb[PlanesB][TN];
 #pragma unroll
-                for (int p = 0; p < Planes; ++p) {
+                for (int p = 0; p < PlanesA; ++p)
 #pragma unroll
                     for (int i = 0; i < TM; ++i) fa[p][i] = from.a[0].read(s.a + p * kPlaneA, i, half);
 #pragma unroll
+                for (int p = 0; p < PlanesB; ++p)
+#pragma unroll
                     for (int j = 0; j < TN; ++j) fb[p][j] = from.b[0].read(s.b + p * kPlaneB, j, half);
-                }
-                const auto add = [&](int pa, int pb) {
+                const auto add = [&](auto &to, int pa, int pb) {
 #pragma unroll
                     for (int i = 0; i < TM; ++i)
 #pragma unroll
-                        for (int j = 0; j < TN; ++j) acc[i][j] = multiply<T>(fa[pa][i], fb[pb][j], acc[i][j]);
+                        for (int j = 0; j < TN; ++j) to[i][j] = multiply<T>(fa[pa][i], fb[pb][j], to[i][j]);
                 };
                 if constexpr (From::kFirst) __builtin_amdgcn_s_setprio(1);
-                add(0, 0);
-                if constexpr (Planes == 3) {
-                    add(0, 1);
-                    add(1, 0);
-                    add(1, 1);
-                    add(0, 2);
-                    add(2, 0);
+                add(acc, 0, 0);
+                if constexpr (PlanesB == 2) add(acc, 0, 1);
+                if constexpr (PlanesA == 3) {
+                    add(low, 0, 1);
+                    add(low, 1, 0);
+                    add(low, 1, 1);
+                    add(low, 0, 2);
+                    add(low, 2, 0);
                 }
                 if constexpr (From::kFirst) __builtin_amdgcn_s_setprio(0);
             }
@@ -307,6 +318,12 @@ struct Tile {
             __syncthreads();
             if (k + 2 < last) from.fetch(*this, even, k + 2);
             if (k + 1 < last) work(odd);
+        }
+        if constexpr (PlanesA == 3) {
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) acc[i][j] += low[i][j];
         }
     }
     template <bool AAcross, bool BAcross>
@@ -330,5 +347,6 @@ template <typename T, bool Across> using LargeTile = std::conditional_t<Across, 
 template <typename T> using SmallTile = Tile<T, 128, 128, 2, 4>;
 typedef Tile<bf16, 256, 128, 4, 2, 3> LargeSplit;
 typedef Tile<bf16, 128, 128, 4, 2, 3> SmallSplit;
+template <typename T> using FineTile = Tile<T, 256, 128, 4, 2, 1, 2>;
 
 }  // namespace tmtrain

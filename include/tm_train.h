@@ -194,7 +194,11 @@ size_t tm_bias_grad_workspace_size(int buckets, int64_t heads);
  *   scale    positive and finite, rounded to float32.
  *   out_logp, out_log_sum  [rows] float32, one may be NULL; out_stats may be NULL.
  *   workspace  at least tm_head_logp_workspace_size() bytes, 16-byte aligned;
- *            needs no initialisation.
+ *            needs no initialisation.  Rows of the weight that are no multiple of
+ *            128 bytes, or not aligned to 16, are laid out there first, and so is
+ *            float32 for more than 128 rows, which goes to the matrix cores as
+ *            three numbers of 16 bits whose sum it is; an infinity then makes the
+ *            logits that it takes part in NaN.
  *
  * Errors: TM_ERR_SHAPE (classes or width < 1, negative rows or strides),
  * TM_ERR_NULL, TM_ERR_NO_OUTPUT, TM_ERR_DTYPE, TM_ERR_SAMPLING (scale),
@@ -205,7 +209,8 @@ int tm_head_logp(const void *hidden, int dtype, int64_t rows, int64_t classes, i
                  const void *weight, int64_t weight_stride, const void *labels, int label_dtype, double scale,
                  float *out_logp, float *out_log_sum, float *out_stats, void *workspace, size_t workspace_bytes,
                  hipStream_t stream);
-size_t tm_head_logp_workspace_size(int dtype, int64_t rows, int64_t classes, int64_t width);
+size_t tm_head_logp_workspace_size(int dtype, int64_t rows, int64_t classes, int64_t width, const void *weight,
+                                   int64_t weight_stride);
 
 /*
  * tm_head_logp_grad -- the gradients, given the upstream gradients a of
@@ -217,19 +222,20 @@ size_t tm_head_logp_workspace_size(int dtype, int64_t rows, int64_t classes, int
  *
  * Either may be NULL.  Rows without a label take part only if z is given; those
  * that do not get zeros and reach no gradient.  stats are what tm_head_logp
- * gave.  g is computed in float32, a piece of the vocabulary at a time, and for
- * more than 16 rows rounded once to dtype for the two products, which are
- * summed in float32 (float16: g is rounded as a multiple of powers of two, one
- * to a row for out_hidden and a common one, of the largest |a| and |z|, for
- * out_weight).  Where every logit of a row is -inf, its g is 0.
+ * gave.  g is computed in float32, a piece of the vocabulary at a time; the two
+ * products are summed in float32.  Of 16-bit operands, g is rounded to dtype for
+ * more than 512 rows, and for 17 to 512 it is the sum of two numbers of dtype
+ * (float16: of a multiple by a power of two, one to a row for out_hidden and a
+ * common one, of the largest |a| and |z|, for out_weight).  Where every logit
+ * of a row is -inf, its g is 0.
  * Errors: as tm_head_logp.
  */
 int tm_head_logp_grad(const void *hidden, int dtype, int64_t rows, int64_t classes, int64_t width,
                       int64_t hidden_stride, const void *weight, int64_t weight_stride, const void *labels,
                       int label_dtype, double scale, const float *stats, const float *up_logp, const float *up_log_sum,
                       void *out_hidden, void *out_weight, void *workspace, size_t workspace_bytes, hipStream_t stream);
-size_t tm_head_logp_grad_workspace_size(int dtype, int64_t rows, int64_t classes, int64_t width, int hidden,
-                                        int weight);
+size_t tm_head_logp_grad_workspace_size(int dtype, int64_t rows, int64_t classes, int64_t width, const void *weight,
+                                        int64_t weight_stride, int for_hidden, int for_weight);
 
 /*
  * tm_layer_norm -- the norm of each row, with mean m and r = 1 / sqrt(mean

@@ -102,8 +102,8 @@ def load() -> ctypes.CDLL:
             head = [vp, i32, i64, i64, i64, i64, vp, i64, vp, i32, ctypes.c_double]
             lib.tm_head_logp.argtypes = head + [vp, vp, vp, vp, size, vp]
             lib.tm_head_logp_grad.argtypes = head + [vp, vp, vp, vp, vp, vp, size, vp]
-            lib.tm_head_logp_workspace_size.argtypes = [i32, i64, i64, i64]
-            lib.tm_head_logp_grad_workspace_size.argtypes = [i32, i64, i64, i64, i32, i32]
+            lib.tm_head_logp_workspace_size.argtypes = [i32, i64, i64, i64, vp, i64]
+            lib.tm_head_logp_grad_workspace_size.argtypes = [i32, i64, i64, i64, vp, i64, i32, i32]
             lib.tm_head_logp_workspace_size.restype = size
             lib.tm_head_logp_grad_workspace_size.restype = size
             lib.tm_layer_norm.argtypes = [vp, i32, i64, i64, i64, vp, vp, i32, ctypes.c_double, vp, vp, vp]

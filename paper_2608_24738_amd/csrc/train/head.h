@@ -343,7 +343,6 @@ __device__ __forceinline__ void each_tile(const HeadArgs &p, uint32_t rows, uint
         block += gridDim.x;
         const bool more = block < total;
         if (more) {
-            if (steps & 1) __syncthreads();     // the last step was even's
             at = tile_place(block, tiles_m, tiles_n);
             from = begin(at);
         }

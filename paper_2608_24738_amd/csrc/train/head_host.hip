@@ -329,12 +329,14 @@ void head_args(const HeadShape &s, const void *hidden, int64_t hidden_stride, co
 
 }  // namespace
 
-extern "C" size_t tm_head_logp_workspace_size(int dtype, int64_t rows, int64_t classes, int64_t width) {
+extern "C" size_t tm_head_logp_workspace_size(int dtype, int64_t rows, int64_t classes, int64_t width,
+                                              const void *weight, int64_t weight_stride) {
     HeadShape s{};
     HeadArgs a{};
     const void *some = reinterpret_cast<const void *>(uintptr_t(4096));
-    if (check_head(some, dtype, rows, classes, width, 0, some, 0, 0, nullptr, 1.0, s) != TM_OK || s.n == 0) return 0;
-    return std::max(head_room(s, true, nullptr, a), head_room(s, false, nullptr, a));
+    if (check_head(some, dtype, rows, classes, width, 0, some, weight_stride, 0, nullptr, 1.0, s) != TM_OK || s.n == 0)
+        return 0;
+    return head_room(s, to_lay(weight, uint64_t(weight_stride), s), nullptr, a);
 }
 
 extern "C" int tm_head_logp(const void *hidden, int dtype, int64_t rows, int64_t classes, int64_t width,
@@ -348,7 +350,7 @@ extern "C" int tm_head_logp(const void *hidden, int dtype, int64_t rows, int64_t
     if (s.n == 0) return TM_OK;
     if (!labels && (out_logp || !out_log_sum)) return TM_ERR_NULL;
     if (!out_logp && !out_log_sum) return TM_ERR_NO_OUTPUT;
-    const size_t need = tm_head_logp_workspace_size(dtype, rows, classes, width);
+    const size_t need = tm_head_logp_workspace_size(dtype, rows, classes, width, weight, weight_stride);
     if (!workspace || workspace_bytes < need || uintptr_t(workspace) % 16) return TM_ERR_WORKSPACE;
     const Range in[] = {{hidden, s.hidden_bytes}, {weight, s.weight_bytes}, {labels, s.n * s.label_bytes}};
     const Range out[] = {{out_logp, s.n * 4}, {out_log_sum, s.n * 4}, {out_stats, s.n * 8}, {workspace, need}};
@@ -363,13 +365,15 @@ extern "C" int tm_head_logp(const void *hidden, int dtype, int64_t rows, int64_t
     return by_type(dtype, [&](auto t) { return run_head<decltype(t)>(a, s, stream); });
 }
 
-extern "C" size_t tm_head_logp_grad_workspace_size(int dtype, int64_t rows, int64_t classes, int64_t width, int hidden,
-                                                   int weight) {
+extern "C" size_t tm_head_logp_grad_workspace_size(int dtype, int64_t rows, int64_t classes, int64_t width,
+                                                   const void *weight, int64_t weight_stride, int for_hidden,
+                                                   int for_weight) {
     HeadShape s{};
     HeadArgs a{};
     const void *some = reinterpret_cast<const void *>(uintptr_t(4096));
-    if (check_head(some, dtype, rows, classes, width, 0, some, 0, 0, nullptr, 1.0, s) != TM_OK || s.n == 0) return 0;
-    return head_grad_room(s, dtype, true, hidden != 0, weight != 0, nullptr, a);
+    if (check_head(some, dtype, rows, classes, width, 0, some, weight_stride, 0, nullptr, 1.0, s) != TM_OK || s.n == 0)
+        return 0;
+    return head_grad_room(s, dtype, to_lay(weight, uint64_t(weight_stride), s), for_hidden != 0, for_weight != 0, nullptr, a);
 }
 
 extern "C" int tm_head_logp_grad(const void *hidden, int dtype, int64_t rows, int64_t classes, int64_t width,
@@ -385,8 +389,8 @@ extern "C" int tm_head_logp_grad(const void *hidden, int dtype, int64_t rows, in
     if (!out_hidden && !out_weight) return TM_ERR_NO_OUTPUT;
     if (s.n && ((!up_logp && !up_log_sum) || (up_logp && !labels) || !stats)) return TM_ERR_NULL;
     const uint64_t grad_bytes = s.classes * s.width * s.size;
-    const size_t need = tm_head_logp_grad_workspace_size(dtype, rows, classes, width, out_hidden != nullptr,
-                                                         out_weight != nullptr);
+    const size_t need = tm_head_logp_grad_workspace_size(dtype, rows, classes, width, weight, weight_stride,
+                                                         out_hidden != nullptr, out_weight != nullptr);
     if (need && (!workspace || workspace_bytes < need || uintptr_t(workspace) % 16)) return TM_ERR_WORKSPACE;
     const Range in[] = {{hidden, s.hidden_bytes}, {weight, s.weight_bytes}, {labels, s.n * s.label_bytes},
                         {stats, s.n * 8}, {up_logp, s.n * 4}, {up_log_sum, s.n * 4}};

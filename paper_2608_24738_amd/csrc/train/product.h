@@ -102,11 +102,11 @@ struct Along {
 
     static __device__ __forceinline__ uint32_t order(uint32_t r) { return kPieces == 8 ? r & 7 : r >> 2 & 3; }
     __device__ __forceinline__ Along(const Operand &o, uint32_t m0, uint32_t first, int lane, int wave) {
-        const uint32_t r = lane / kPieces;
-        from = o.at + m0 * o.stride + uint64_t(first) * kRow;
+        const uint32_t r = lane / kPieces, row = min(m0, o.rows - 1);       // tiles may lie behind the last row
+        from = o.at + row * o.stride + uint64_t(first) * kRow;
 #pragma unroll
         for (int i = 0; i < kCopies; ++i)
-            offset[i] = min((i * Waves + wave) * kAtOnce + r, o.rows - 1 - m0) * uint32_t(o.stride) +
+            offset[i] = min((i * Waves + wave) * kAtOnce + r, o.rows - 1 - row) * uint32_t(o.stride) +
                         (lane % kPieces ^ order(r)) * 16;
     }
     __device__ __forceinline__ void fetch(char *lds, uint32_t, int, int wave) {
@@ -265,8 +265,14 @@ struct Tile {
         return from;
     }
 
+    // A barrier behind which all waves' copies have arrived and all their reads are done.
+    static __device__ __forceinline__ void sync() {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+    }
+
     // The products over steps [first, last), of which `even` has got the first.
-    // Afterwards `even` can be filled again where last - first is even.
+    // Afterwards `even` can be filled again: all waves have done with it.
     template <typename From>
     __device__ __forceinline__ void run(From &from, uint32_t first, uint32_t last, Buffer &even, Buffer &odd) {
 #pragma unroll
@@ -312,10 +318,10 @@ struct Tile {
             }
         };
         for (uint32_t k = first; k < last; k += 2) {
-            __syncthreads();                    // even has arrived, odd is read
+            sync();                             // even has arrived, odd is read
             if (k + 1 < last) from.fetch(*this, odd, k + 1);
             work(even);
-            __syncthreads();
+            sync();
             if (k + 2 < last) from.fetch(*this, even, k + 2);
             if (k + 1 < last) work(odd);
         }

@@ -273,7 +273,7 @@ HeadOut head_forward(const Tensor &hidden, const Tensor &weight, const Tensor &l
     if (keep) out.kept = floats(with(shape, 2), hidden);
     const Rows h = rows_of(hidden), w = rows_of(weight);
     const int dtype = float_type(hidden.scalar_type());
-    const size_t bytes = tm_head_logp_workspace_size(dtype, h.rows, w.rows, h.width);
+    const size_t bytes = tm_head_logp_workspace_size(dtype, h.rows, w.rows, h.width, w.t.data_ptr(), w.stride);
     const Tensor workspace = room(bytes, hidden);
     const Call call(hidden);
     done(tm_head_logp(h.t.data_ptr(), dtype, h.rows, w.rows, h.width, h.stride, w.t.data_ptr(), w.stride, at_of(labels),
@@ -327,7 +327,8 @@ struct HeadLogProbs : torch::autograd::Function<HeadLogProbs> {
         const Tensor dh = wants_h ? at::empty(shape, h.t.options()) : Tensor();
         const Tensor dw = wants_w ? at::empty({classes, width}, w.t.options()) : Tensor();
         const int dtype = float_type(type);
-        const size_t bytes = tm_head_logp_grad_workspace_size(dtype, h.rows, w.rows, width, wants_h, wants_w);
+        const size_t bytes = tm_head_logp_grad_workspace_size(dtype, h.rows, w.rows, width, w.t.data_ptr(), w.stride,
+                                                              wants_h, wants_w);
         const Tensor workspace = room(bytes, kept);
         const Call call(kept);
         done(tm_head_logp_grad(h.t.data_ptr(), dtype, h.rows, w.rows, width, h.stride, w.t.data_ptr(), w.stride,

@@ -504,8 +504,8 @@ def head_log_probs(hidden: torch.Tensor, weight: torch.Tensor, labels: Optional[
     ``log_sums``  also the log of the sum of each row's exponentials.
 
     Results are float32.  Gradients flow to ``hidden`` and ``weight`` from both
-    results.  For more than 16 rows the logits' gradient is rounded to the
-    operands' type before its two products, which are summed in float32.
+    results.  Products are summed in float32; for more than 512 rows of 16-bit
+    operands the logits' gradient is rounded to their type before its two.
     """
     _reverse_only(hidden, weight)
     return HeadLogProbs(*torch_ops().head_log_probs(hidden, weight, labels, scale, log_sums))

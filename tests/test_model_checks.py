@@ -17,7 +17,7 @@ def lib():
 
 def head(lib, hidden=A, dtype=5, rows=40, classes=300, width=64, hs=64, weight=B, ws=64, labels=C, kind=3, scale=1.0,
          logp=D, sums=None, stats=None, room=E, nbytes=None):
-    need = lib.tm_head_logp_workspace_size(dtype, rows, classes, width)
+    need = lib.tm_head_logp_workspace_size(dtype, rows, classes, width, weight, ws)
     return lib.tm_head_logp(hidden, dtype, rows, classes, width, hs, weight, ws, labels, kind, scale, logp, sums, stats,
                             room, need if nbytes is None else nbytes, None)
 
@@ -36,7 +36,7 @@ def test_head_checks(lib):
     assert head(lib, labels=None, logp=None) == NULL
     assert head(lib, logp=None) == NO_OUTPUT
     assert head(lib, room=None) == WORKSPACE and head(lib, room=E + 8) == WORKSPACE
-    assert head(lib, nbytes=lib.tm_head_logp_workspace_size(5, 40, 300, 64) - 1) == WORKSPACE
+    assert head(lib, nbytes=lib.tm_head_logp_workspace_size(5, 40, 300, 64, B, 64) - 1) == WORKSPACE
     for out in (dict(logp=A + 64), dict(logp=B + 64), dict(logp=C), dict(sums=D + 4), dict(stats=D - 4),
                 dict(room=D), dict(room=A), dict(sums=A)):
         assert head(lib, **out) == ALIAS
@@ -45,7 +45,7 @@ def test_head_checks(lib):
 
 def head_grad(lib, hidden=A, dtype=5, rows=40, classes=300, width=64, weight=B, labels=C, scale=1.0, stats=D, up=E,
               up_sum=None, dh=F, dw=G, room=H, nbytes=None):
-    need = lib.tm_head_logp_grad_workspace_size(dtype, rows, classes, width, dh is not None, dw is not None)
+    need = lib.tm_head_logp_grad_workspace_size(dtype, rows, classes, width, weight, width, dh is not None, dw is not None)
     return lib.tm_head_logp_grad(hidden, dtype, rows, classes, width, width, weight, width, labels, 3, scale, stats, up,
                                  up_sum, dh, dw, room, need if nbytes is None else nbytes, None)
 
@@ -57,24 +57,28 @@ def test_head_grad_checks(lib):
     assert head_grad(lib, scale=-2.0) == SAMPLING and head_grad(lib, dtype=0) == DTYPE
     assert head_grad(lib, width=0) == SHAPE
     assert head_grad(lib, room=None) == WORKSPACE and head_grad(lib, room=H + 4) == WORKSPACE
-    assert head_grad(lib, nbytes=lib.tm_head_logp_grad_workspace_size(5, 40, 300, 64, 1, 1) - 1) == WORKSPACE
+    assert head_grad(lib, nbytes=lib.tm_head_logp_grad_workspace_size(5, 40, 300, 64, B, 64, 1, 1) - 1) == WORKSPACE
     for out in (dict(dh=A), dict(dw=B + 2), dict(dh=E), dict(dw=F + 8), dict(room=F), dict(room=D), dict(dw=C), dict(dh=D)):
         assert head_grad(lib, **out) == ALIAS
     assert head_grad(lib, rows=0, dw=None) == OK
 
 
 def test_head_workspaces(lib):
-    """One class more, one row more, another type: never less room, and none for nothing."""
+    """None for nothing, more where the weight has to be laid out, less for one gradient than for both."""
     size, grad = lib.tm_head_logp_workspace_size, lib.tm_head_logp_grad_workspace_size
-    assert size(5, 0, 300, 64) == 0 and grad(5, 0, 300, 64, 1, 1) == 0
-    assert size(9, 3, 300, 64) == 0 and grad(9, 3, 300, 64, 1, 1) == 0
+    assert size(5, 0, 300, 64, A, 64) == 0 and grad(5, 0, 300, 64, A, 64, 1, 1) == 0
+    assert size(9, 3, 300, 64, A, 64) == 0 and grad(9, 3, 300, 64, A, 64, 1, 1) == 0
     for rows in (1, 16, 17, 300, 5000, 100000):
         for dtype in (4, 5, 6):
-            both = grad(dtype, rows, 50021, 777, 1, 1)
-            assert size(dtype, rows, 50021, 777) > 0
-            assert 0 < grad(dtype, rows, 50021, 777, 1, 0) <= both and 0 < grad(dtype, rows, 50021, 777, 0, 1) <= both
+            both = grad(dtype, rows, 50021, 777, A, 777, 1, 1)
+            assert size(dtype, rows, 50021, 777, A, 777) > 0
+            assert 0 < grad(dtype, rows, 50021, 777, A, 777, 1, 0) <= both
+            assert 0 < grad(dtype, rows, 50021, 777, A, 777, 0, 1) <= both
+    laid = 50176 * 1024 * 2
+    for call in (lambda *w: size(5, 300, 50021, 1024, *w), lambda *w: grad(5, 300, 50021, 1024, *w, 1, 1)):
+        assert call(A, 1024) + laid == call(A + 2, 1024) == call(A, 1025) == call(A, 1 << 23)
     # pieces of the vocabulary keep it far below a float32 for each logit
-    assert grad(5, 8192, 131072, 2048, 1, 1) < 8192 * 131072 * 4 // 4
+    assert grad(5, 8192, 131072, 2048, A, 2048, 1, 1) < 8192 * 131072 * 4 // 4
 
 
 def norm(lib, x=A, dtype=5, rows=40, width=100, stride=100, weight=B, bias=C, params=6, eps=1e-5, out=D, stats=None):

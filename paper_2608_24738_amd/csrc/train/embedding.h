@@ -34,7 +34,7 @@ struct EmbeddingArgs {
     uint32_t *digits;           // [tile][values]: how often a tile has each value of the digit
     uint32_t *total;            // [values]: how often all have, where there are many tiles
     uint32_t tiles, values;
-    uint32_t shift;             // of the digit at hand
+    uint32_t shift;             // of the digit at hand; of each one, for k_sort_whole
     int32_t from;               // which of the two is read; -1: the tokens themselves
     const uint32_t *sorted_key, *sorted_number;
     float *part;                // [chunks][2][part_stride]
@@ -188,6 +188,89 @@ __global__ __launch_bounds__(256) void k_sort_move(EmbeddingArgs p) {
         const uint32_t at = place[digit] + wave_has[wave][digit] + rank[r];
         p.key[to][at] = key[r];
         p.number[to][at] = p.from < 0 ? i : p.number[p.from][i];
+    }
+}
+
+// All digits in one workgroup, whose LDS holds the tokens: R rounds of a wave.
+template <int R>
+__global__ __launch_bounds__(1024) void k_sort_whole(EmbeddingArgs p) {
+    constexpr uint32_t kWaves = 16;
+    __shared__ uint32_t keys[R * 1024];
+    __shared__ uint16_t numbers[R * 1024];
+    __shared__ uint16_t wave_has[kWaves][kSortMost];    // how many a wave has of a value, then where they begin
+    __shared__ uint32_t scan[kWaves];
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = wave * (R * 64) + lane;
+    uint32_t key[R], number[R], rank[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        number[r] = first + r * 64;
+        key[r] = number[r] < p.count ? sort_key(p, number[r]) : 0;
+    }
+    for (uint32_t shift = 0;; shift += p.shift) {
+        for (uint32_t i = threadIdx.x; i < kWaves * kSortMost; i += 1024) (&wave_has[0][0])[i] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const bool real = first + r * 64 < p.count;
+            const uint32_t digit = key[r] >> shift & (p.values - 1);
+            uint64_t same = __ballot(real);             // lanes with this lane's digit
+            for (uint32_t bit = 1; bit < p.values; bit <<= 1) {
+                const uint64_t set = __ballot(digit & bit);
+                same &= digit & bit ? set : ~set;
+            }
+            const uint64_t below = same & ((uint64_t(1) << lane) - 1);
+            rank[r] = 0;
+            if (real) rank[r] = wave_has[wave][digit] + __popcll(below);
+            wave_sync();                                // every lane has read before the first of each digit writes
+            if (real && below == 0) wave_has[wave][digit] = uint16_t(rank[r] + __popcll(same));
+            wave_sync();
+        }
+        __syncthreads();
+        // sums over the waves of each value, and over the lower values
+        uint32_t sum = 0;
+        if (threadIdx.x < p.values)
+#pragma unroll
+            for (uint32_t w = 0; w < kWaves; ++w) sum += wave_has[w][threadIdx.x];
+        uint32_t up = sum;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const uint32_t o = __shfl_up(up, d);
+            if (lane >= uint32_t(d)) up += o;
+        }
+        if (lane == 63) scan[wave] = up;
+        __syncthreads();
+        if (threadIdx.x < p.values) {
+            up -= sum;
+            for (uint32_t w = 0; w < wave; ++w) up += scan[w];
+#pragma unroll
+            for (uint32_t w = 0; w < kWaves; ++w) {
+                const uint32_t x = wave_has[w][threadIdx.x];
+                wave_has[w][threadIdx.x] = uint16_t(up);
+                up += x;
+            }
+        }
+        __syncthreads();
+        const bool last = uint64_t(1) << (shift + p.shift) > p.rows;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            if (first + r * 64 >= p.count) continue;
+            const uint32_t at = wave_has[wave][key[r] >> shift & (p.values - 1)] + rank[r];
+            if (last) {
+                p.key[0][at] = key[r];
+                p.number[0][at] = number[r];
+            } else {
+                keys[at] = key[r];
+                numbers[at] = uint16_t(number[r]);
+            }
+        }
+        if (last) return;
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            key[r] = keys[first + r * 64];
+            number[r] = numbers[first + r * 64];
+        }
+        __syncthreads();
     }
 }
 

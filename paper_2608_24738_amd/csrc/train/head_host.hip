@@ -16,9 +16,10 @@ namespace {
 
 constexpr uint64_t kMaxWidth = uint64_t(1) << 20;      // 256 rows fit an offset of 32 bits
 constexpr uint64_t kPieceBytes = uint64_t(1) << 27;     // of g
-constexpr uint64_t kLaidBytes = uint64_t(1) << 28;      // of weights laid out in whole steps
+constexpr uint64_t kLaidBytes = uint64_t(1) << 30;      // of weights laid out in whole steps
 constexpr uint64_t kCus = 256;
 constexpr uint64_t kPlaneRows = 128;
+constexpr uint64_t kNarrowRows = 64;
 
 struct HeadShape {
     uint64_t n, classes, width, size;
@@ -71,6 +72,9 @@ struct Room {
 uint64_t whole_tiles(uint64_t n) { return ceil_div(n, kTilePad) * kTilePad; }
 
 bool few(const HeadShape &s) { return s.n <= kFewRows; }
+// The gradient of 16-bit operands reads and writes them at the tiles' pace from five rows on (5 x 32768 x 1024 bf16,
+// both passes: 109 us, by the kernels for few 140; float32 284 and 168).
+bool few_grad(const HeadShape &s) { return s.n <= (s.size == 4 ? kFewRows : 4); }
 
 // Floats go to the matrix cores as three 16-bit planes, unless the rows are few.
 bool planes(const HeadShape &s) { return s.size == 4 && s.n > kPlaneRows; }
@@ -82,13 +86,14 @@ constexpr uint64_t kSlots = (2 * sizeof(typename Tile::Buffer) <= 80 * 1024 ? 2 
 // 16-bit operands whose g has two planes.
 bool fine(const HeadShape &s) { return s.size == 2 && s.n <= kFineRows; }
 
-// fn(tile): the larger of two, unless it leaves CUs without one; `most` is how
-// often k can be split.
+// fn(tile): the larger of two, unless it leaves CUs without one or more than
+// half of itself empty; `most` is how often k can be split.
 template <typename T, bool Across, typename F>
 auto by_tile(const HeadShape &s, uint64_t m, uint64_t n, uint64_t most, F fn) {
-    const bool large = ceil_div(m, 256) * ceil_div(n, planes(s) ? 128 : 256) * most >= kCus;
+    const bool large = ceil_div(m, 256) * ceil_div(n, planes(s) ? 128 : 256) * most >= kCus && n > 128 && m > 128;
     if constexpr (std::is_same<T, float>::value) {
         if (planes(s)) return large ? fn(static_cast<LargeSplit *>(nullptr)) : fn(static_cast<SmallSplit *>(nullptr));
+        if (n <= kNarrowRows) return fn(static_cast<NarrowTile *>(nullptr));
     }
     if constexpr (Across && sizeof(T) == 2) {
         if (fine(s)) return fn(static_cast<FineTile<T> *>(nullptr));
@@ -104,8 +109,8 @@ auto by_tile_size(const HeadShape &s, uint64_t m, uint64_t n, uint64_t most, F f
 // Tiles read whole steps of the weight's rows, 16 bytes at a time and with offsets of 32 bits: whether it is to be laid
 // out for them.
 bool to_lay(const void *p, uint64_t stride, const HeadShape &s) {
-    return !few(s) && (planes(s) || uintptr_t(p) % 16 || stride * s.size % 16 || s.width * s.size % 128 ||
-                       stride * s.size > kMostStride);
+    return planes(s) || uintptr_t(p) % 16 || stride * s.size % 16 || s.width * s.size % 128 ||
+           stride * s.size > kMostStride;
 }
 
 // Classes of a piece, in whole tiles, so that `bytes` hold a row of `each` for every class.
@@ -114,13 +119,13 @@ uint64_t piece_of(uint64_t classes, uint64_t each, uint64_t bytes) {
     return whole_tiles(ceil_div(classes, ceil_div(classes, most)));
 }
 
-void head_sizes(const HeadShape &s, HeadArgs &a) {
+void head_sizes(const HeadShape &s, bool few, HeadArgs &a) {
     a.n = uint32_t(s.n);
     a.classes = uint32_t(s.classes);
     a.width = uint32_t(s.width);
     const uint64_t step = s.size == 4 ? 32 : 64;
     a.width_pad = uint32_t(ceil_div(s.width, step) * step);
-    a.n_pad = uint32_t(few(s) ? kFewRows : whole_tiles(s.n));
+    a.n_pad = uint32_t(few ? kFewRows : whole_tiles(s.n));
 }
 
 // Bytes of a laid out element, and of one of g.
@@ -130,7 +135,7 @@ uint64_t slope_held(const HeadShape &s) { return fine(s) ? 4 : held(s); }
 // Layout of the forward call's workspace; returns its size.
 uint64_t head_room(const HeadShape &s, bool laid, void *at, HeadArgs &a) {
     Room room{static_cast<char *>(at), 0};
-    head_sizes(s, a);
+    head_sizes(s, few(s), a);
     a.found = room.take<float>(a.n_pad);
     if (few(s)) {
         a.parts = uint32_t(ceil_div(s.classes, kFewClasses));
@@ -154,7 +159,7 @@ uint64_t head_room(const HeadShape &s, bool laid, void *at, HeadArgs &a) {
 // Classes of a workgroup of k_few_outer.
 uint64_t few_share(const HeadShape &s) { return std::max<uint64_t>(16, ceil_div(s.classes, 256)); }
 // Columns of a thread of k_few_outer: what its registers hold of n rows, twice in float32.
-uint32_t few_columns(const HeadShape &s) { return s.n > 4 || s.size == 4 ? 4 : 8; }
+uint32_t few_columns(const HeadShape &s) { return s.size == 4 ? 4 : 8; }
 // and its block: as many threads as a row needs, up to 256, the rest for other classes.
 dim3 few_block(const HeadShape &s) {
     const uint32_t x = std::min<uint32_t>(256, std::max<uint32_t>(16, pow2_from(uint32_t(ceil_div(s.width, few_columns(s))))));
@@ -164,8 +169,8 @@ dim3 few_block(const HeadShape &s) {
 // Layout of the gradient's workspace.
 uint64_t head_grad_room(const HeadShape &s, int dtype, bool laid, bool hidden, bool weight, void *at, HeadArgs &a) {
     Room room{static_cast<char *>(at), 0};
-    head_sizes(s, a);
-    if (few(s)) {
+    head_sizes(s, few_grad(s), a);
+    if (few_grad(s)) {
         a.sum_stride = uint32_t(ceil_div(s.width, 8) * 8);
         a.steps = uint32_t(few_share(s));
         a.splits = uint32_t(ceil_div(s.classes, a.steps) * few_block(s).y);
@@ -272,15 +277,18 @@ int run_few_grad(const HeadArgs &a, const HeadShape &s, hipStream_t stream) {
     const dim3 block = few_block(s);
     const dim3 grid(uint32_t(ceil_div(s.classes, a.steps)), uint32_t(ceil_div(s.width, block.x * few_columns(s))));
     constexpr int C = sizeof(T) == 4 ? 4 : 8;
-    rc = launch(s.n == 1 ? k_few_outer<T, 1, C> : s.n <= 4 ? k_few_outer<T, 4, C> : k_few_outer<T, 16, 4>, grid, block,
-                0, stream, a);
+    auto kernel = s.n == 1 ? k_few_outer<T, 1, C> : k_few_outer<T, 4, C>;
+    if constexpr (sizeof(T) == 4) {
+        if (s.n > 4) kernel = k_few_outer<T, 16, 4>;
+    }
+    rc = launch(kernel, grid, block, 0, stream, a);
     if (rc != TM_OK || !a.grad_hidden) return rc;
     return launch(k_few_join<T>, dim3(uint32_t(ceil_div(s.width, 64)), a.n), dim3(1024), 0, stream, a);
 }
 
 template <typename T>
 int run_head_grad(HeadArgs a, const HeadShape &s, hipStream_t stream) {
-    if (few(s)) return run_few_grad<T>(a, s, stream);
+    if (few_grad(s)) return run_few_grad<T>(a, s, stream);
     int rc = pack_rows<T>(s, a, stream);
     for (uint64_t first = 0; rc == TM_OK && first < s.classes; first += a.piece) {
         a.first = uint32_t(first);
@@ -336,7 +344,7 @@ extern "C" size_t tm_head_logp_workspace_size(int dtype, int64_t rows, int64_t c
     const void *some = reinterpret_cast<const void *>(uintptr_t(4096));
     if (check_head(some, dtype, rows, classes, width, 0, some, weight_stride, 0, nullptr, 1.0, s) != TM_OK || s.n == 0)
         return 0;
-    return head_room(s, to_lay(weight, uint64_t(weight_stride), s), nullptr, a);
+    return head_room(s, !few(s) && to_lay(weight, uint64_t(weight_stride), s), nullptr, a);
 }
 
 extern "C" int tm_head_logp(const void *hidden, int dtype, int64_t rows, int64_t classes, int64_t width,
@@ -357,7 +365,7 @@ extern "C" int tm_head_logp(const void *hidden, int dtype, int64_t rows, int64_t
     if (aliased(in, out)) return TM_ERR_ALIAS;
     HeadArgs a{};
     head_args(s, hidden, hidden_stride, weight, weight_stride, labels, scale, a);
-    head_room(s, to_lay(weight, a.weight_stride, s), workspace, a);
+    head_room(s, !few(s) && to_lay(weight, a.weight_stride, s), workspace, a);
     a.all = out_log_sum != nullptr;
     a.logp = out_logp;
     a.log_sum = out_log_sum;
@@ -373,7 +381,7 @@ extern "C" size_t tm_head_logp_grad_workspace_size(int dtype, int64_t rows, int6
     const void *some = reinterpret_cast<const void *>(uintptr_t(4096));
     if (check_head(some, dtype, rows, classes, width, 0, some, weight_stride, 0, nullptr, 1.0, s) != TM_OK || s.n == 0)
         return 0;
-    return head_grad_room(s, dtype, to_lay(weight, uint64_t(weight_stride), s), for_hidden != 0, for_weight != 0, nullptr, a);
+    return head_grad_room(s, dtype, !few_grad(s) && to_lay(weight, uint64_t(weight_stride), s), for_hidden != 0, for_weight != 0, nullptr, a);
 }
 
 extern "C" int tm_head_logp_grad(const void *hidden, int dtype, int64_t rows, int64_t classes, int64_t width,
@@ -403,7 +411,7 @@ extern "C" int tm_head_logp_grad(const void *hidden, int dtype, int64_t rows, in
     }
     HeadArgs a{};
     head_args(s, hidden, hidden_stride, weight, weight_stride, labels, scale, a);
-    head_grad_room(s, dtype, to_lay(weight, a.weight_stride, s), out_hidden != nullptr,
+    head_grad_room(s, dtype, !few_grad(s) && to_lay(weight, a.weight_stride, s), out_hidden != nullptr,
                    out_weight != nullptr, workspace, a);
     a.all = up_log_sum != nullptr;
     a.stats = reinterpret_cast<HeadSum *>(const_cast<float *>(stats));

@@ -351,6 +351,8 @@ struct Tile {
 // reads there are twice as many, eight waves of larger tiles (dh 137 and 135, dw 121 and 116).
 template <typename T, bool Across> using LargeTile = std::conditional_t<Across, Tile<T, 256, 256, 2, 4>, Tile<T, 256, 256, 2, 8>>;
 template <typename T> using SmallTile = Tile<T, 128, 128, 2, 4>;
+// Few rows of floats, whose instructions would bound the larger tiles (17 x 131072 x 2048: 330 us, by 128 x 128 some 580).
+typedef Tile<float, 128, 64, 4, 2> NarrowTile;
 typedef Tile<bf16, 256, 128, 4, 2, 3> LargeSplit;
 typedef Tile<bf16, 128, 128, 4, 2, 3> SmallSplit;
 template <typename T> using FineTile = Tile<T, 256, 128, 4, 2, 1, 2>;

@@ -303,13 +303,23 @@ extern "C" int tm_embedding_grad(const void *tokens, int token_dtype, int64_t co
     a.grad = out_grad;
     a.from = -1;
     const uint32_t each = uint32_t(__builtin_ctz(a.values));
-    for (uint32_t d = 0; d < digits; ++d, a.shift += each) {
-        int rc = launch(k_sort_count, dim3(a.tiles), dim3(256), 0, stream, a);
-        if (rc == TM_OK && a.tiles > kSortFew)
-            rc = launch(k_sort_tiles, dim3(uint32_t(ceil_div(a.values, 4))), dim3(256), 0, stream, a);
-        if (rc == TM_OK) rc = launch(k_sort_move, dim3(a.tiles), dim3(256), 0, stream, a);
+    // Few tokens are sorted by one workgroup (2048 of 50021: 8 us, 4096: 13; by tiles and digits 8192 take 22 in four
+    // launches, 16384 take 25, by one workgroup 37).
+    if (s.count <= 8192) {
+        a.shift = each;
+        const int rc = launch(s.count <= 2048 ? k_sort_whole<2> : s.count <= 4096 ? k_sort_whole<4> : k_sort_whole<8>,
+                              dim3(1), dim3(1024), 0, stream, a);
         if (rc != TM_OK) return rc;
-        a.from = a.from == 0 ? 1 : 0;
+        a.from = 0;
+    } else {
+        for (uint32_t d = 0; d < digits; ++d, a.shift += each) {
+            int rc = launch(k_sort_count, dim3(a.tiles), dim3(256), 0, stream, a);
+            if (rc == TM_OK && a.tiles > kSortFew)
+                rc = launch(k_sort_tiles, dim3(uint32_t(ceil_div(a.values, 4))), dim3(256), 0, stream, a);
+            if (rc == TM_OK) rc = launch(k_sort_move, dim3(a.tiles), dim3(256), 0, stream, a);
+            if (rc != TM_OK) return rc;
+            a.from = a.from == 0 ? 1 : 0;
+        }
     }
     a.sorted_key = a.key[a.from];
     a.sorted_number = a.number[a.from];

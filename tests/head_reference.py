@@ -6,7 +6,9 @@ the additions' roundings are independent and add up like a random walk, for whic
 largest such error of a row's logits and X its largest logit: probabilities are off by 2 x relatively, by the rounding
 of the factor log2(e), 2 u X, and by that of a sum of V terms, u (8 + 8 sqrt V).  A slope g is rounded to the operands'
 type (half a step; of float16 also half the spacing of its smallest numbers, after the powers of two), and the products
-with it are again float32 sums.
+with it are again float32 sums.  For 5 to 256 rows of 16 bits it is the sum of two such numbers: the second is the
+rounding of what the first leaves, which is half a step at most, so half a step of it is half a step squared (2^-16 of
+bfloat16, 2^-22 of float16).  For fewer it is kept in float32.
 
 Exponentials below 2^-126 flush to zero, and so do operands of a product below that: p and then g lose up to 2^-126
 each, which times |w| or |h| and summed is far above a float32's smallest numbers where those are in the hundreds.
@@ -53,12 +55,12 @@ def exact(hidden, weight, labels, scale, dtype, ups=None, all_rows=False):
     tol = scale * (np.abs(a - z)[:, None] * p * (rel[:, None] + 8 * U) + 4 * U * np.abs(a)[:, None] * one)
     tol += 2.0 ** -126 * (1 + scale * np.abs(a - z))[:, None]
     tol[~part] = 0.0
-    few = n <= 16
+    few = n <= 4 or (dtype == "f32" and n <= 16)
     size = scale * (np.abs(a) + np.abs(a - z))
     if few:
         tol_w = tol_h = tol
     else:
-        half = HALF[dtype]
+        half = HALF[dtype] ** 2 if n <= 256 else HALF[dtype]
         tol_h = tol + half * (np.abs(g) + tol)
         tol_w = tol_h
         if dtype == "f16":

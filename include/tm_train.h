@@ -177,8 +177,8 @@ size_t tm_bias_grad_workspace_size(int buckets, int64_t heads);
  *   out_logp[n]     x_ny - log sum_v exp x_nv for the row's label y; 0 where y
  *                   lies outside [0, classes) (a row without a label)
  *   out_log_sum[n]  log sum_v exp x_nv, of every row
- *   out_stats[n][2] for tm_head_logp_grad: M, the largest x_nv log2(e), and
- *                   sum_v 2^(x_nv log2(e) - M)
+ *   out_stats[n][2] for tm_head_logp_grad: M, the largest x_nv / scale, and the
+ *                   sum over v of exp(x_nv - scale M)
  *
  * Rows without a label take no part, unless out_log_sum is asked for: what
  * they hold, NaN included, changes nothing, and no work is done for them.

@@ -1,14 +1,13 @@
 // head.h -- kernels of the log-probabilities from hidden states and a
 // vocabulary's weight (tm_head_logp in include/tm_train.h).
 //
-// With x = scale h w^T, c = scale log2(e) and M the largest c h w of a row:
-//     s = sum_v 2^(c h w_v - M),   log sum exp x = ln 2 (M + log2 s),
-//     log p_y = ln 2 ((c h w_y - M) - log2 s),   p_v = 2^(c h w_v - M) / s.
-// One fma gives an exponent with one rounding.  M is the largest itself, not a
-// whole number near it: a class with nearly all of the mass then has a power
-// and a sum next to 1, whose logarithms lose least.  M starts at -FLT_MAX
-// instead of -inf, so that the exponent is never inf - inf: logits at -inf get
-// 0, and s = 0 marks a row with no class left.
+// With x = h w^T, c = scale log2(e) and M the largest x of a row:
+//     s = sum_v 2^(c (x_v - M)),   log sum exp (scale x) = scale M + ln 2 log2 s,
+//     log p_y = ln 2 (c (x_y - M) - log2 s),   p_v = 2^(c (x_v - M)) / s.
+// M is taken off first, which is exact for logits near it: the largest has the
+// power 1, and what is left out of a sum next to 1 is no more than its rounding.
+// M starts at -FLT_MAX instead of -inf, so that no difference is inf - inf:
+// logits at -inf get 0, and s = 0 marks a row with no class left.
 //
 // The logits are never stored: a tile's pass over k ends in sums of its rows.
 // The gradient computes them anew, a piece of the vocabulary at a time, as
@@ -33,19 +32,20 @@ constexpr uint32_t kFineRows = 256;             // rows up to which g of 16-bit 
 constexpr uint32_t kListChunk = 1024;           // rows that a workgroup counts
 
 struct HeadSum {
-    float m, s;                 // M, sum of 2^(c h w - M)
+    float m, s;                 // M, sum of 2^(c (h w - M))
 };
 constexpr float kLowest = -FLT_MAX;
 
-// 2^(a - b) for a <= b; 0 where a is kLowest and b is not.
-__device__ __forceinline__ float shrink(float a, float b) { return a == b ? 1.0f : exp2_hw(fmaxf(a - b, -200.0f)); }
+// 2^(c (a - b)) for a <= b; 0 where a is kLowest and b is not.
+__device__ __forceinline__ float shrink(float a, float b, float c) {
+    return a == b ? 1.0f : exp2_hw(fmaxf((a - b) * c, -200.0f));
+}
 
 // inf - inf of the references of rows with +inf stays NaN in s.
-__device__ __forceinline__ HeadSum join(HeadSum a, HeadSum b) {
+__device__ __forceinline__ HeadSum join(HeadSum a, HeadSum b, float c) {
     const float m = fmaxf(a.m, b.m);
-    return {m, a.s * shrink(a.m, m) + b.s * shrink(b.m, m)};
+    return {m, a.s * shrink(a.m, m, c) + b.s * shrink(b.m, m, c)};
 }
-__device__ __forceinline__ float reference(float most, float c) { return fmaxf(most * c, kLowest); }
 
 // A packed row, for the gradient.
 struct HeadRow {
@@ -77,7 +77,7 @@ struct HeadArgs {
     float *inverse;             // float16: what takes a packed row's power of two back; then the common one's
     void *packed;               // packed hidden states [n_pad][width_pad]
     HeadSum *part;              // [parts][n_pad]
-    float *found;               // c h w of the packed rows' labels
+    float *found;               // h w of the packed rows' labels
     void *slope, *slope_common; // g [n_pad][piece]; float16: times its row's power of two, and the common one
     void *weight_laid;          // a piece's weights in whole steps, where they do not lie so
     float *sum;                 // dh by splits: [splits][rows of tiles][sum_stride]; few rows: [splits][n][sum_stride]
@@ -87,6 +87,8 @@ struct HeadArgs {
     uint32_t splits, steps;     // few rows: shares of the classes, and classes of one
     uint32_t blocks, most;      // of the product for dh: workgroups, splits that its k allows
     uint32_t tiles_m, tile_n;   // its tiles across the width, and the rows of one
+    uint32_t weight_splits;     // of the product for dw, where the classes' tiles are few
+    float *weight_sum;          // dw by splits: [splits][classes][sum_stride]
     bool add;                   // to the sums so far
 };
 
@@ -351,8 +353,8 @@ __device__ __forceinline__ void each_tile(const HeadArgs &p, uint32_t rows, uint
     }
 }
 
-// Sums of 2^(c x - M) of the packed rows over a tile's classes, one for each
-// wave's classes, and c x of the labels.
+// Sums of the packed rows over a tile's classes, one for each wave's classes,
+// and the labels' x.
 template <typename T, typename Tile>
 __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_sums(HeadArgs p) {
     __shared__ __attribute__((aligned(1024))) typename Tile::Buffer even, odd;
@@ -397,12 +399,12 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_sums(
             }
             most = fmaxf(most, __shfl_xor(most, 16));
             most = fmaxf(most, __shfl_xor(most, 32));
-            const float m = reference(most, p.c);
+            const float m = fmaxf(most, kLowest);
             float s = 0.0f;
 #pragma unroll
             for (int i = 0; i < Tile::TM; ++i)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) s += exp2_hw(fmaf(tile.acc[i][j][q], p.c, -m));
+                for (int q = 0; q < 4; ++q) s += exp2_hw((tile.acc[i][j][q] - m) * p.c);
             s += __shfl_xor(s, 16);
             s += __shfl_xor(s, 32);
             if (n < count && tile.lane < 16) p.part[uint64_t(part) * p.n_pad + n] = {m, s};
@@ -417,12 +419,12 @@ __device__ __forceinline__ void head_store(const HeadArgs &p, uint32_t n, const 
     if (p.logp) {
         float l = 0.0f;
         if (y >= 0) {
-            l = (fmaf(*found, p.c, -sum.m) - log_s) * kLn2;
+            l = fmaf(*found - sum.m, p.c, -log_s) * kLn2;
             if (sum.s == 0.0f) l = -INFINITY;
         }
         p.logp[n] = l;
     }
-    if (p.log_sum) p.log_sum[n] = sum.s == 0.0f ? -INFINITY : fmaf(log_s, kLn2, sum.m * kLn2);
+    if (p.log_sum) p.log_sum[n] = sum.s == 0.0f ? -INFINITY : fmaf(sum.m, p.scale, log_s * kLn2);
     if (p.stats) p.stats[n] = sum;
 }
 
@@ -443,15 +445,15 @@ __global__ __launch_bounds__(1024) void k_head_join(HeadArgs p) {
             for (int k = 0; k < kAhead; ++k)
                 got[k] = i + kShares * k < p.parts ? p.part[uint64_t(i + kShares * k) * p.n_pad + j] : HeadSum{kLowest, 0.0f};
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k) sum = join(sum, got[k]);
+            for (int k = 0; k < kAhead; ++k) sum = join(sum, got[k], p.c);
         }
     }
 #pragma unroll
-    for (int d = 16; d < 64; d <<= 1) sum = join(sum, HeadSum{__shfl_xor(sum.m, d), __shfl_xor(sum.s, d)});
+    for (int d = 16; d < 64; d <<= 1) sum = join(sum, HeadSum{__shfl_xor(sum.m, d), __shfl_xor(sum.s, d)}, p.c);
     if ((threadIdx.x & 63) < kRows) lds[threadIdx.x >> 6][row] = sum;
     __syncthreads();
     if (threadIdx.x >= kRows || j >= count) return;
-    for (int w = 1; w < 16; ++w) sum = join(sum, lds[w][row]);
+    for (int w = 1; w < 16; ++w) sum = join(sum, lds[w][row], p.c);
     head_store(p, p.list[j], p.found + j, sum);
 }
 
@@ -486,7 +488,7 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_slope
                 const uint32_t v = at.m * Tile::BM + tile.row(i);
                 float g[4];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) g[q] = -r.b * exp2_hw(fmaf(tile.acc[i][j][q], p.c, -r.m));
+                for (int q = 0; q < 4; ++q) g[q] = -r.b * exp2_hw((tile.acc[i][j][q] - r.m) * p.c);
                 if (labels) {
 #pragma unroll
                     for (int q = 0; q < 4; ++q)
@@ -586,27 +588,37 @@ __global__ __launch_bounds__(256) void k_head_hidden_join(HeadArgs p) {
     }
 }
 
-// The piece's rows of dw = g^T h.
+// The piece's rows of dw = g^T h, or their sums over a split of the packed rows.
 template <typename T, typename Tile>
 __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_weight(HeadArgs p) {
     typedef Held<T, Tile> S;
     __shared__ __attribute__((aligned(1024))) typename Tile::Buffer even, odd;
     const uint32_t count = *p.count, rows = min(p.piece, p.classes - p.first);
     const uint32_t tiles_m = (p.width + Tile::BM - 1) / Tile::BM, tiles_n = (rows + Tile::BN - 1) / Tile::BN;
-    const TilePlace at = tile_place(blockIdx.x, tiles_m, tiles_n);
+    const TilePlace at = tile_place(blockIdx.x, tiles_m, tiles_n, p.weight_splits);
+    const uint32_t all = (count + Tile::kStep - 1) / Tile::kStep, steps = (all + p.weight_splits - 1) / p.weight_splits;
     const void *slope = __is_same(T, f16) ? p.slope_common : p.slope;
     Tile tile;
     tile.template run<true, true>(hidden_rows<S>(p, p.n_pad), at.m * Tile::BM, slope_rows<S>(p, slope, p.n_pad),
-                                  at.n * Tile::BN, 0, (count + Tile::kStep - 1) / Tile::kStep, even, odd);
+                                  at.n * Tile::BN, min(all, at.split * steps), min(all, (at.split + 1) * steps), even, odd);
     float back = 1.0f;
     if constexpr (__is_same(T, f16)) {
         back = p.inverse[p.n_pad];
-        __builtin_amdgcn_s_waitcnt(0x0f70);         // here, not behind each store
+        __builtin_amdgcn_s_waitcnt(0x0f70);         // vmcnt(0), here and not behind each store
     }
 #pragma unroll
     for (int j = 0; j < Tile::TN; ++j) {
         const uint32_t v = at.n * Tile::BN + tile.column(j);
         if (v >= rows) continue;
+        if (p.weight_splits > 1) {
+            float *to = p.weight_sum + (uint64_t(at.split) * rows + v) * p.sum_stride;
+#pragma unroll
+            for (int i = 0; i < Tile::TM; ++i) {
+                const uint32_t d = at.m * Tile::BM + tile.row(i);
+                if (d < p.sum_stride) *reinterpret_cast<f32x4 *>(to + d) = tile.acc[i][j];
+            }
+            continue;
+        }
         T *to = static_cast<T *>(p.grad_weight) + uint64_t(p.first + v) * p.width;
 #pragma unroll
         for (int i = 0; i < Tile::TM; ++i) {
@@ -617,6 +629,25 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_weigh
             for (int q = 0; q < 4; ++q) x[q] = __is_same(T, f16) ? tile.acc[i][j][q] * back : tile.acc[i][j][q];
             store_pack<4>(to + d, narrow_pack<T>(x), p.width - d);
         }
+    }
+}
+
+// The piece's rows of dw from the splits' sums.
+template <typename T>
+__global__ __launch_bounds__(256) void k_head_weight_join(HeadArgs p) {
+    const uint32_t quads = (p.width + 3) / 4, rows = min(p.piece, p.classes - p.first);
+    const uint64_t total = uint64_t(rows) * quads, step = uint64_t(rows) * p.sum_stride;
+    const float back = p.inverse ? p.inverse[p.n_pad] : 1.0f;
+    for (uint64_t i = uint64_t(blockIdx.x) * 256 + threadIdx.x; i < total; i += uint64_t(gridDim.x) * 256) {
+        const uint32_t v = uint32_t(i / quads), d = uint32_t(i % quads) * 4;
+        const float *from = p.weight_sum + uint64_t(v) * p.sum_stride + d;
+        f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+        for (uint32_t s = 0; s < p.weight_splits; ++s) sum += *reinterpret_cast<const f32x4 *>(from + s * step);
+        float x[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) x[q] = sum[q] * back;
+        store_pack<4>(static_cast<T *>(p.grad_weight) + uint64_t(p.first + v) * p.width + d, narrow_pack<T>(x), p.width - d);
     }
 }
 

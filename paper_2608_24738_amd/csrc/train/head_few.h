@@ -1,5 +1,8 @@
 // head_few.h -- the kernels of head.h for up to kFewRows rows, such as one new
 // token: bound by one read of the weight, which goes from memory to registers.
+// Groups of kFewRows rows take the same way to their logits where there is so
+// little work that tiles would leave most CUs without one, and go through long
+// rows one step after the other.
 #pragma once
 
 #include "head.h"
@@ -11,13 +14,14 @@ constexpr int kFewClasses = 16 * kFewWaves;     // of a workgroup
 constexpr int kFewSums = 8;
 constexpr int kFewAhead = 8;                    // pieces of a row on their way to a lane
 
-// c h w of 16 classes from v0 on and all rows: the lane holds classes v0 + 4 g + q of row n = lane % 16.
+// h w of 16 classes from v0 on and 16 rows, of which the lane's is `row`: it
+// holds classes v0 + 4 g + q of it.
 template <typename T>
-__device__ __forceinline__ f32x4 few_logits(const HeadArgs &p, uint32_t v0) {
+__device__ __forceinline__ f32x4 few_logits(const HeadArgs &p, uint32_t v0, uint32_t row) {
     constexpr uint32_t V = 16 / sizeof(T), kRound = 4 * V;
     const uint32_t lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const T *w = static_cast<const T *>(p.weight) + uint64_t(min(v0 + r, p.classes - 1)) * p.weight_stride;
-    const T *h = static_cast<const T *>(p.hidden) + uint64_t(min(r, p.n - 1)) * p.hidden_stride;
+    const T *h = static_cast<const T *>(p.hidden) + row * p.hidden_stride;
     // several sums, so that none grows to the whole logit step by step
     f32x4 acc[kFewSums];
 #pragma unroll
@@ -48,15 +52,15 @@ __device__ __forceinline__ f32x4 few_logits(const HeadArgs &p, uint32_t v0) {
     return acc[0];
 }
 
-// Sums of 2^(c x - M) over a workgroup's classes, and c x of the labels.
+// Sums over a workgroup's classes of its 16 rows, and the labels' x.
 template <typename T>
 __global__ __launch_bounds__(64 * kFewWaves) void k_few_sums(HeadArgs p) {
     __shared__ HeadSum lds[kFewWaves][kFewRows];
-    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15;
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = blockIdx.y * kFewRows + (lane & 15);
     const uint32_t v0 = (blockIdx.x * kFewWaves + wave) * 16, v = v0 + (lane >> 4) * 4;
     HeadSum sum = {kLowest, 0.0f};
     if (v0 < p.classes) {
-        f32x4 x = few_logits<T>(p, v0);
+        f32x4 x = few_logits<T>(p, v0, min(n, p.n - 1));
         const int32_t y = n < p.n && p.label ? load_label(p.label, p.label_bytes, n, p.classes) : -1;
         if (y >= 0 && uint32_t(y) - v < 4) {
             const uint32_t q = uint32_t(y) - v;
@@ -70,18 +74,18 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_few_sums(HeadArgs p) {
         }
         most = fmaxf(most, __shfl_xor(most, 16));
         most = fmaxf(most, __shfl_xor(most, 32));
-        sum.m = reference(most, p.c);
+        sum.m = fmaxf(most, kLowest);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) sum.s += exp2_hw(fmaf(x[q], p.c, -sum.m));
+        for (int q = 0; q < 4; ++q) sum.s += exp2_hw((x[q] - sum.m) * p.c);
         sum.s += __shfl_xor(sum.s, 16);
         sum.s += __shfl_xor(sum.s, 32);
     }
-    if (lane < 16) lds[wave][n] = sum;
+    if (lane < 16) lds[wave][lane] = sum;
     __syncthreads();
     if (threadIdx.x >= 16) return;
-    sum = lds[0][n];
+    sum = lds[0][lane];
 #pragma unroll
-    for (int w = 1; w < kFewWaves; ++w) sum = join(sum, lds[w][n]);
+    for (int w = 1; w < kFewWaves; ++w) sum = join(sum, lds[w][lane], p.c);
     if (n < p.n) p.part[uint64_t(n) * p.parts + blockIdx.x] = sum;
 }
 
@@ -96,15 +100,15 @@ __global__ __launch_bounds__(256) void k_few_rows(HeadArgs p) {
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) got[k] = i + 256 * k < p.parts ? part[i + 256 * k] : HeadSum{kLowest, 0.0f};
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) sum = join(sum, got[k]);
+        for (int k = 0; k < kAhead; ++k) sum = join(sum, got[k], p.c);
     }
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) sum = join(sum, HeadSum{__shfl_xor(sum.m, d), __shfl_xor(sum.s, d)});
+    for (int d = 1; d < 64; d <<= 1) sum = join(sum, HeadSum{__shfl_xor(sum.m, d), __shfl_xor(sum.s, d)}, p.c);
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = sum;
     __syncthreads();
     if (threadIdx.x) return;
 #pragma unroll
-    for (int w = 1; w < 4; ++w) sum = join(sum, lds[w]);
+    for (int w = 1; w < 4; ++w) sum = join(sum, lds[w], p.c);
     head_store(p, blockIdx.x, p.found + blockIdx.x, sum);
 }
 
@@ -114,7 +118,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_few_slopes(HeadArgs p) {
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15;
     const uint32_t v0 = (blockIdx.x * kFewWaves + wave) * 16, v = v0 + (lane >> 4) * 4;
     if (v0 >= p.classes) return;
-    const f32x4 x = few_logits<T>(p, v0);
+    const f32x4 x = few_logits<T>(p, v0, min(n, p.n - 1));
     int32_t y = -1;
     HeadUp u = {0.0f, 0.0f};
     HeadSum s = {0.0f, 1.0f};
@@ -130,9 +134,48 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_few_slopes(HeadArgs p) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         if (v + q >= p.classes) break;
-        float g = -b * exp2_hw(fmaf(x[q], p.c, -s.m));
+        float g = -b * exp2_hw((x[q] - s.m) * p.c);
         if (int32_t(v + q) == y) g += u.a;
         static_cast<float *>(p.slope)[uint64_t(v + q) * kFewRows + n] = in ? g : 0.0f;
+    }
+}
+
+// g of the packed rows as the tiles read it, in G planes of S, for a piece: what
+// k_head_slopes gives.  Rows from the last one to its 128 get zeros.
+template <typename T, typename S, int G>
+__global__ __launch_bounds__(64 * kFewWaves) void k_few_tiles(HeadArgs p) {
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = blockIdx.y * kFewRows + (lane & 15);
+    const uint32_t v0 = (blockIdx.x * kFewWaves + wave) * 16, v = v0 + (lane >> 4) * 4, count = *p.count;
+    if (blockIdx.y * kFewRows >= ((count + 127) & ~127u)) return;
+    const bool real = n < count;
+    HeadRow r = {0.0f, 0.0f, 0.0f, -1};
+    f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (blockIdx.y * kFewRows < count) {
+        if (real) r = p.row[n];
+        x = few_logits<T>(p, p.first + v0, p.list[min(n, count - 1)]);
+    }
+    float g[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        g[q] = -r.b * exp2_hw((x[q] - r.m) * p.c);
+        if (int32_t(p.first + v + q) == r.y) g[q] += r.a;
+        if (!real || p.first + v + q >= p.classes) g[q] = 0.0f;
+    }
+    const uint64_t to = uint64_t(n) * p.piece + v, plane = uint64_t(p.n_pad) * p.piece;
+    Pack<S, 4> out[G];
+    if (!__is_same(T, f16) || p.slope) {
+        split(g, out);
+#pragma unroll
+        for (int k = 0; k < G; ++k) store_pack<4>(static_cast<S *>(p.slope) + to + k * plane, out[k]);
+    }
+    if constexpr (__is_same(T, f16)) {
+        if (!p.slope_common) return;
+        const float ratio = real ? p.inverse[n] / p.inverse[p.n_pad] : 1.0f;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) g[q] *= ratio;
+        split(g, out);
+#pragma unroll
+        for (int k = 0; k < G; ++k) store_pack<4>(static_cast<S *>(p.slope_common) + to + k * plane, out[k]);
     }
 }
 

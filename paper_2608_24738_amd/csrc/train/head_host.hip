@@ -20,6 +20,8 @@ constexpr uint64_t kLaidBytes = uint64_t(1) << 30;      // of weights laid out i
 constexpr uint64_t kCus = 256;
 constexpr uint64_t kPlaneRows = 128;
 constexpr uint64_t kNarrowRows = 64;
+constexpr uint64_t kSmallRows = uint64_t(1) << 19;       // in groups of 16 to a grid's second dimension
+constexpr uint64_t kSmallWork = uint64_t(1) << 27;       // products of a logit's term, rows x classes x width
 
 struct HeadShape {
     uint64_t n, classes, width, size;
@@ -71,7 +73,8 @@ struct Room {
 
 uint64_t whole_tiles(uint64_t n) { return ceil_div(n, kTilePad) * kTilePad; }
 
-bool few(const HeadShape &s) { return s.n <= kFewRows; }
+bool small(const HeadShape &s) { return s.n * s.classes <= kSmallWork / s.width && s.n <= kSmallRows; }
+bool few(const HeadShape &s) { return s.n <= kFewRows || small(s); }
 // The gradient of 16-bit operands reads and writes them at the tiles' pace from five rows on (5 x 32768 x 1024 bf16,
 // both passes: 109 us, by the kernels for few 140; float32 284 and 168).
 bool few_grad(const HeadShape &s) { return s.n <= (s.size == 4 ? kFewRows : 4); }
@@ -136,7 +139,7 @@ uint64_t slope_held(const HeadShape &s) { return fine(s) ? 4 : held(s); }
 uint64_t head_room(const HeadShape &s, bool laid, void *at, HeadArgs &a) {
     Room room{static_cast<char *>(at), 0};
     head_sizes(s, few(s), a);
-    a.found = room.take<float>(a.n_pad);
+    a.found = room.take<float>(whole_tiles(s.n));
     if (few(s)) {
         a.parts = uint32_t(ceil_div(s.classes, kFewClasses));
         a.part = room.take<HeadSum>(uint64_t(a.parts) * a.n);
@@ -191,6 +194,13 @@ uint64_t head_grad_room(const HeadShape &s, int dtype, bool laid, bool hidden, b
         a.blocks = uint32_t(std::max(kSlots<Tile>, a.tiles_m * ceil_div(s.n, Tile::BN)));
         return 0;
     });
+    // dw: likewise, for the tiles of the first piece (the last may be shorter)
+    const uint64_t rows = std::min<uint64_t>(a.piece, s.classes);
+    a.weight_splits = by_tile_size<true>(s, s.width, rows, 1, [&](auto *t) {
+        using Tile = std::remove_pointer_t<decltype(t)>;
+        const uint64_t tiles = ceil_div(s.width, Tile::BM) * ceil_div(rows, Tile::BN);
+        return uint32_t(std::max<uint64_t>(1, std::min<uint64_t>({kSlots<Tile> / tiles, s.n / (8 * Tile::kStep), 32})));
+    });
     a.count = room.take<uint32_t>(1);
     a.chunk_count = room.take<uint32_t>(2 * ceil_div(s.n, kListChunk));
     a.list = room.take<uint32_t>(a.n_pad);
@@ -205,6 +215,7 @@ uint64_t head_grad_room(const HeadShape &s, int dtype, bool laid, bool hidden, b
         const uint64_t rows = std::min<uint64_t>(uint64_t(a.most) * a.n_pad, uint64_t(a.blocks / a.tiles_m) * a.tile_n);
         a.sum = room.take<float>(rows * a.sum_stride);
     }
+    if (weight && a.weight_splits > 1) a.weight_sum = room.take<float>(a.weight_splits * rows * a.sum_stride);
     if (laid) a.weight_laid = room.take<char>(uint64_t(a.piece) * a.width_pad * held(s));
     return room.used;
 }
@@ -252,7 +263,8 @@ int lay_piece(const HeadShape &s, const HeadArgs &a, hipStream_t stream) {
 template <typename T>
 int run_head(HeadArgs a, const HeadShape &s, hipStream_t stream) {
     if (few(s)) {
-        const int rc = launch(k_few_sums<T>, dim3(a.parts), dim3(64 * kFewWaves), 0, stream, a);
+        const dim3 grid(a.parts, uint32_t(ceil_div(s.n, kFewRows)));
+        const int rc = launch(k_few_sums<T>, grid, dim3(64 * kFewWaves), 0, stream, a);
         return rc == TM_OK ? launch(k_few_rows, dim3(a.n), dim3(256), 0, stream, a) : rc;
     }
     int rc = pack_rows<T>(s, a, stream);
@@ -295,15 +307,26 @@ int run_head_grad(HeadArgs a, const HeadShape &s, hipStream_t stream) {
         a.add = first > 0;
         if (a.weight_laid) rc = lay_piece<T>(s, a, stream);
         if (rc != TM_OK) break;
-        rc = by_tile<T, false>(s, a.piece, s.n, 1, [&](auto *t) {
-            using Tile = std::remove_pointer_t<decltype(t)>;
-            constexpr int G = Tile::kPlanes;
-            auto kernel = k_head_slopes<T, Tile, G>;
-            if constexpr (sizeof(T) == 2) {
-                if (fine(s)) kernel = k_head_slopes<T, Tile, 2>;
+        if (small(s)) {
+            const dim3 grid(a.piece / kFewClasses, a.n_pad / kFewRows);
+            auto kernel = k_few_tiles<T, T, 1>;
+            if constexpr (sizeof(T) == 4) {
+                if (planes(s)) kernel = k_few_tiles<T, bf16, 3>;
+            } else {
+                if (fine(s)) kernel = k_few_tiles<T, T, 2>;
             }
-            return launch(kernel, lasting_grid<Tile>(a.piece, s.n), dim3(Tile::kThreads), 0, stream, a);
-        });
+            rc = launch(kernel, grid, dim3(64 * kFewWaves), 0, stream, a);
+        } else {
+            rc = by_tile<T, false>(s, a.piece, s.n, 1, [&](auto *t) {
+                using Tile = std::remove_pointer_t<decltype(t)>;
+                constexpr int G = Tile::kPlanes;
+                auto kernel = k_head_slopes<T, Tile, G>;
+                if constexpr (sizeof(T) == 2) {
+                    if (fine(s)) kernel = k_head_slopes<T, Tile, 2>;
+                }
+                return launch(kernel, lasting_grid<Tile>(a.piece, s.n), dim3(Tile::kThreads), 0, stream, a);
+            });
+        }
         if (rc == TM_OK && a.grad_hidden) {
             rc = by_tile<T, true>(s, s.width, s.n, a.most, [&](auto *t) {
                 using Tile = std::remove_pointer_t<decltype(t)>;
@@ -312,10 +335,16 @@ int run_head_grad(HeadArgs a, const HeadShape &s, hipStream_t stream) {
         }
         if (rc == TM_OK && a.grad_weight) {
             const uint64_t rows = std::min<uint64_t>(a.piece, s.classes - first);
-            rc = by_tile<T, true>(s, s.width, rows, 1, [&](auto *t) {
+            // the tile is that of the first piece, whose splits these are
+            rc = by_tile<T, true>(s, s.width, std::min<uint64_t>(a.piece, s.classes), 1, [&](auto *t) {
                 using Tile = std::remove_pointer_t<decltype(t)>;
-                return launch(k_head_weight<T, Tile>, tile_grid<Tile>(s.width, rows), dim3(Tile::kThreads), 0, stream, a);
+                return launch(k_head_weight<T, Tile>, dim3(tile_grid<Tile>(s.width, rows).x * a.weight_splits),
+                              dim3(Tile::kThreads), 0, stream, a);
             });
+            if (rc == TM_OK && a.weight_splits > 1) {
+                const uint64_t blocks = ceil_div(rows * ceil_div(s.width, 4), 256);
+                rc = launch(k_head_weight_join<T>, dim3(uint32_t(std::min<uint64_t>(blocks, 4096))), dim3(256), 0, stream, a);
+            }
         }
     }
     if (rc != TM_OK || !a.grad_hidden) return rc;

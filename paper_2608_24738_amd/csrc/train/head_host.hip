@@ -21,7 +21,9 @@ constexpr uint64_t kCus = 256;
 constexpr uint64_t kPlaneRows = 128;
 constexpr uint64_t kNarrowRows = 64;
 constexpr uint64_t kSmallRows = uint64_t(1) << 19;       // in groups of 16 to a grid's second dimension
-constexpr uint64_t kSmallWork = uint64_t(1) << 27;       // products of a logit's term, rows x classes x width
+// Rows x classes x width up to which tiles take longer than single waves: forward pass of 512 x 1024 x 512, 2^28,
+// bf16 13.3 us and by tiles 18.5, float32 22.7 and 35; of 1024 x 1024 x 512 20.8 and 18.3, 37 and 37.8.
+constexpr uint64_t kSmallWork = uint64_t(1) << 28;
 
 struct HeadShape {
     uint64_t n, classes, width, size;

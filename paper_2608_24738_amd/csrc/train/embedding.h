@@ -27,6 +27,8 @@ struct EmbeddingArgs {
     uint32_t count, rows, width;
     float scale;
     void *y;
+    uint32_t share;             // rows of a workgroup
+    Div32 div_pieces;           // 16-byte pieces of a row
     // gradient
     const void *up;
     void *grad;
@@ -41,23 +43,25 @@ struct EmbeddingArgs {
     uint32_t part_stride, chunk, chunks, sum_blocks;
 };
 
+// A workgroup copies p.share rows, its threads side by side over all their pieces.
 template <typename T>
 __global__ __launch_bounds__(256) void k_embedding(EmbeddingArgs p) {
     constexpr int V = 16 / sizeof(T);
-    const uint32_t pieces = (p.width + V - 1) / V;
-    for (uint64_t n = uint64_t(blockIdx.x) * blockDim.y + threadIdx.y; n < p.count; n += uint64_t(gridDim.x) * blockDim.y) {
-        const int32_t k = load_label(p.token, p.token_bytes, n, p.rows);
-        const T *from = static_cast<const T *>(p.table) + (k < 0 ? 0 : k) * p.stride;
-        T *to = static_cast<T *>(p.y) + n * p.width;
-        for (uint32_t i = blockIdx.y * blockDim.x + threadIdx.x; i < pieces; i += gridDim.y * blockDim.x) {
-            const uint32_t c = i * V;
+    const uint32_t pieces = p.div_pieces.d;
+    const uint64_t step = uint64_t(gridDim.x) * p.share;
+    for (uint64_t n0 = uint64_t(blockIdx.x) * p.share; n0 < p.count; n0 += step) {
+        const uint32_t total = uint32_t(min(uint64_t(p.share), p.count - n0)) * pieces;
+        for (uint32_t i = blockIdx.y * 256 + threadIdx.x; i < total; i += gridDim.y * 256) {
+            const uint32_t r = p.div_pieces.div(i), c = (i - r * pieces) * V;
+            const uint64_t n = n0 + r;
+            const int32_t k = load_label(p.token, p.token_bytes, n, p.rows);
             float v[V] = {};
             if (k >= 0) {
-                const Pack<T, V> x = load_pack<V>(from + c, p.width - c, T{});
+                const Pack<T, V> x = load_pack<V>(static_cast<const T *>(p.table) + k * p.stride + c, p.width - c, T{});
 #pragma unroll
                 for (int j = 0; j < V; ++j) v[j] = widen(x.at(j)) * p.scale;
             }
-            store_pack<V>(to + c, narrow_pack<T>(v), p.width - c);
+            store_pack<V>(static_cast<T *>(p.y) + n * p.width + c, narrow_pack<T>(v), p.width - c);
         }
     }
 }

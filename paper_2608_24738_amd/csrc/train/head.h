@@ -17,7 +17,7 @@
 //     dh = g w,   dw = g^T h.
 // Its rounding to 16 bits is off by as much as that of the results.  With up to
 // kFineRows rows, of which few make up most of a result, g has two planes, 16
-// bits or more; for 512 rows they took 1796 us instead of 1530 (131072 x 2048).
+// bits or more; for 512 rows they took 1796 us instead of 1186 (131072 x 2048).
 // Rows without a label take part only where the log sums are asked for: the
 // rows that do are packed first, and the products run over those alone.
 #pragma once
@@ -195,6 +195,7 @@ __device__ __forceinline__ void lay(const T *from, uint32_t n, S *to, uint64_t p
     }
 }
 
+// 4096 rows of 1024 bf16: 9 us, and 5 for the chunks' counts; 509 rows 5.
 // Packs the hidden states of kPackRows rows, in whole steps with zeros behind
 // them, and writes where they went and what the gradient needs of them.  Every
 // workgroup counts the rows before its own: all of them, or those of its chunk
@@ -354,7 +355,10 @@ __device__ __forceinline__ void each_tile(const HeadArgs &p, uint32_t rows, uint
 }
 
 // Sums of the packed rows over a tile's classes, one for each wave's classes,
-// and the labels' x.
+// and the labels' x.  Bound by the matrix cores and what feeds them, at small
+// widths also by the exponentials at a tile's end: 4096 x 32768 x 1024 bf16 216
+// to 234 us by machine (1120 to 1210 TFLOP/s), half of 8192 x 131072 x 2048 1630
+// (1350).
 template <typename T, typename Tile>
 __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_sums(HeadArgs p) {
     __shared__ __attribute__((aligned(1024))) typename Tile::Buffer even, odd;
@@ -428,7 +432,8 @@ __device__ __forceinline__ void head_store(const HeadArgs &p, uint32_t n, const 
     if (p.stats) p.stats[n] = sum;
 }
 
-// The sums of a row over all parts: 16 rows to a workgroup, parts over its 64 rows of threads.
+// The sums of a row over all parts: 16 rows to a workgroup, parts over its 64 rows of threads, which load several at
+// once.  4096 rows of 256 parts: 6 us; 64 rows to a workgroup 7, and 8 for 509 rows.
 __global__ __launch_bounds__(1024) void k_head_join(HeadArgs p) {
     constexpr uint32_t kRows = 16, kShares = 64;
     __shared__ HeadSum lds[16][kRows];
@@ -457,7 +462,9 @@ __global__ __launch_bounds__(1024) void k_head_join(HeadArgs p) {
     head_store(p, p.list[j], p.found + j, sum);
 }
 
-// g of a piece of the vocabulary, in G planes.
+// g of a piece of the vocabulary, in G planes.  As the sums, and bound by its
+// stores, which all workgroups make at once: 16384 classes of 4096 x 1024 bf16 145
+// us (920 TFLOP/s), 8192 of 4096 x 2048 120 (1150).
 template <typename T, typename Tile, int G>
 __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_slopes(HeadArgs p) {
     typedef Held<T, Tile> S;
@@ -524,7 +531,9 @@ __device__ __forceinline__ uint32_t hidden_splits(const HeadArgs &p, uint32_t ti
     return max(1u, min(p.most, p.blocks / max(1u, p.tiles_m * tiles_n)));
 }
 
-// The piece's share of dh = g w, over a split of its classes.
+// The piece's share of dh = g w, over a split of its classes, added to the
+// shares of the pieces before.  4096 x 16384 x 1024 bf16 in 4 splits 131 to 135 us
+// (1010 TFLOP/s), 4096 x 8192 x 2048 in 2 120 (1150).
 template <typename T, typename Tile>
 __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_hidden(HeadArgs p) {
     typedef Held<T, Tile> S;
@@ -589,6 +598,7 @@ __global__ __launch_bounds__(256) void k_head_hidden_join(HeadArgs p) {
 }
 
 // The piece's rows of dw = g^T h, or their sums over a split of the packed rows.
+// 4096 x 16384 x 1024 bf16 114 us (1170 TFLOP/s), 4096 x 8192 x 2048 112 (1220).
 template <typename T, typename Tile>
 __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_weight(HeadArgs p) {
     typedef Held<T, Tile> S;

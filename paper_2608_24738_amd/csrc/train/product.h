@@ -201,7 +201,7 @@ struct Across {
 // sum it is.  Three of bf16 hold a float, x = h + m + l, exactly, since each
 // takes eight more bits; a product of two is hh + hm + mh + mm + hl + lh, what is
 // left out being below 2^-23 of it, and six instructions of 16 bits take less
-// time than those of floats (2048 x 16384 x 1024: sums 309 us and 495).  All but
+// time than those of floats (2048 x 16384 x 1024: sums 300 us and 495).  All but
 // hh have sums of their own: they are 2^-8 of the whole and add no rounding at
 // its size.  Two planes, of B alone, make 16 or 22 bits of a number.
 template <typename T, int BM_, int BN_, int WM_, int WN_, int PlanesA = 1, int PlanesB = PlanesA>
@@ -234,7 +234,7 @@ struct Tile {
         typedef std::conditional_t<AAcross, Across<T, BM, kWaves, kStep, TM>, Along<T, BM, kWaves, kStep>> FromA;
         typedef std::conditional_t<BAcross, Across<T, BN, kWaves, kStep, TN>, Along<T, BN, kWaves, kStep>> FromB;
         // Waves with their operands at hand go first (4096 x 32768 x 1024: sums 246 -> 238 us); those that
-        // read across k would hold up the others' reads (dw 121 -> 158), and planes leave time (309 -> 321).
+        // read across k would hold up the others' reads (dw 121 -> 158), and planes leave time (sums of floats 309 -> 321).
         static constexpr bool kFirst = !AAcross && !BAcross && PlanesB == 1;
         FromA a[PlanesA];
         FromB b[PlanesB];

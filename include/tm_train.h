@@ -202,8 +202,9 @@ size_t tm_bias_grad_workspace_size(int buckets, int64_t heads);
  *
  * Errors: TM_ERR_SHAPE (classes or width < 1, negative rows or strides),
  * TM_ERR_NULL, TM_ERR_NO_OUTPUT, TM_ERR_DTYPE, TM_ERR_SAMPLING (scale),
- * TM_ERR_TOO_LARGE (some 2^31 rows or classes, 2^31 tiles of 128 x 128 logits,
- * more than 2^20 columns), TM_ERR_WORKSPACE, TM_ERR_ALIAS, TM_ERR_HIP.
+ * TM_ERR_TOO_LARGE (some 2^31 rows or classes, 2^31 tiles of 128 x 128 logits
+ * or of 64 x 128 elements of an operand, more than 2^20 columns),
+ * TM_ERR_WORKSPACE, TM_ERR_ALIAS, TM_ERR_HIP.
  */
 int tm_head_logp(const void *hidden, int dtype, int64_t rows, int64_t classes, int64_t width, int64_t hidden_stride,
                  const void *weight, int64_t weight_stride, const void *labels, int label_dtype, double scale,

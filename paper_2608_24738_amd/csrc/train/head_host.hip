@@ -51,8 +51,10 @@ int check_head(const void *hidden, int dtype, int64_t rows, int64_t classes, int
     s.classes = uint64_t(classes);
     s.width = uint64_t(width);
     s.size = float_bytes(dtype);
-    // workgroups of the smaller tiles
-    if (ceil_div(s.n, 128) * ceil_div(s.classes, 128) >= kLimit) return TM_ERR_TOO_LARGE;
+    // workgroups of the smallest tiles
+    if (ceil_div(s.n, 128) * ceil_div(s.classes, 128) >= kLimit ||
+        ceil_div(std::max(s.n, s.classes), 64) * ceil_div(s.width, 128) >= kLimit)
+        return TM_ERR_TOO_LARGE;
     s.label_bytes = label_dtype == TM_DTYPE_U8 ? 1 : label_dtype == TM_DTYPE_I32 ? 4 : 8;
     if (s.n == 0) return TM_OK;
     if (!hidden || !weight) return TM_ERR_NULL;

@@ -202,7 +202,7 @@ size_t tm_bias_grad_workspace_size(int buckets, int64_t heads);
  *
  * Errors: TM_ERR_SHAPE (classes or width < 1, negative rows or strides),
  * TM_ERR_NULL, TM_ERR_NO_OUTPUT, TM_ERR_DTYPE, TM_ERR_SAMPLING (scale),
- * TM_ERR_TOO_LARGE (some 2^31 rows or classes, 2^31 tiles of 128 x 128 logits
+ * TM_ERR_TOO_LARGE (2^26 rows, 2^30 classes, 2^31 tiles of 128 x 128 logits
  * or of 64 x 128 elements of an operand, more than 2^20 columns),
  * TM_ERR_WORKSPACE, TM_ERR_ALIAS, TM_ERR_HIP.
  */

@@ -195,11 +195,11 @@ __device__ __forceinline__ void lay(const T *from, uint32_t n, S *to, uint64_t p
     }
 }
 
-// 4096 rows of 1024 bf16: 9 us, and 5 for the chunks' counts; 509 rows 5.
 // Packs the hidden states of kPackRows rows, in whole steps with zeros behind
 // them, and writes where they went and what the gradient needs of them.  Every
 // workgroup counts the rows before its own: all of them, or those of its chunk
 // and the chunks' counts.  The last one leaves zeros up to a multiple of 64.
+// 4096 rows of 1024 bf16: 9 us, and 5 for the chunks' counts; 509 rows 5.
 constexpr uint32_t kPackRows = 8;
 template <typename T, typename S, int P>
 __global__ __launch_bounds__(256) void k_head_pack(HeadArgs p) {

@@ -15,6 +15,8 @@ using namespace tmtrain;
 namespace {
 
 constexpr uint64_t kMaxWidth = uint64_t(1) << 20;      // 256 rows fit an offset of 32 bits
+constexpr uint64_t kMostRows = uint64_t(1) << 26;       // a grid has 2^32 threads at most: 64 of k_head_join to a row,
+constexpr uint64_t kMostClasses = uint64_t(1) << 30;    // 4 of k_few_sums to a class
 constexpr uint64_t kPieceBytes = uint64_t(1) << 27;     // of g
 constexpr uint64_t kLaidBytes = uint64_t(1) << 30;      // of weights laid out in whole steps
 constexpr uint64_t kCus = 256;
@@ -45,7 +47,7 @@ int check_head(const void *hidden, int dtype, int64_t rows, int64_t classes, int
         return TM_ERR_DTYPE;
     if (!std::isfinite(scale) || !std::isfinite(float(scale) * kLog2e) || !(float(scale) > FLT_MIN))
         return TM_ERR_SAMPLING;
-    if (uint64_t(rows) >= kLimit - kTilePad || uint64_t(classes) >= kLimit - kTilePad || uint64_t(width) > kMaxWidth)
+    if (uint64_t(rows) >= kMostRows || uint64_t(classes) >= kMostClasses || uint64_t(width) > kMaxWidth)
         return TM_ERR_TOO_LARGE;
     s.n = uint64_t(rows);
     s.classes = uint64_t(classes);

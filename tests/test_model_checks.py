@@ -29,7 +29,8 @@ def test_head_checks(lib):
     for scale in (0.0, -1.0, math.inf, math.nan, 1e39, 1e-39):
         assert head(lib, scale=scale) == SAMPLING
     for big in (dict(rows=1 << 31), dict(classes=1 << 31), dict(width=1 << 25), dict(rows=1 << 30, classes=1 << 30),
-                dict(rows=1 << 30, classes=64, width=1 << 20, hs=1 << 20, ws=1 << 20),
+                dict(rows=1 << 26), dict(classes=1 << 30), dict(rows=1 << 25, classes=1 << 29),
+                dict(classes=1 << 29, width=1 << 20, hs=1 << 20, ws=1 << 20),
                 dict(hs=1 << 60), dict(ws=1 << 60)):
         assert head(lib, nbytes=1 << 50, **big) == TOO_LARGE
     assert head(lib, hidden=None) == NULL and head(lib, weight=None) == NULL

@@ -17,6 +17,7 @@ namespace tmtrain {
 
 constexpr uint32_t kSortTile = 1024;            // tokens that a workgroup sorts at once
 constexpr uint32_t kSortMost = 512;             // values of a digit
+constexpr uint32_t kRangeTokens = 32768;        // that a workgroup lists at most
 constexpr uint32_t kSortFew = 64;               // tiles whose counts each workgroup adds up by itself
 constexpr uint32_t kClearRows = 64;             // rows of the table that a workgroup looks for
 
@@ -36,7 +37,7 @@ struct EmbeddingArgs {
     uint32_t *digits;           // [tile][values]: how often a tile has each value of the digit
     uint32_t *total;            // [values]: how often all have, where there are many tiles
     uint32_t tiles, values;
-    uint32_t shift;             // of the digit at hand; of each one, for k_sort_whole
+    uint32_t shift;             // of the digit at hand
     int32_t from;               // which of the two is read; -1: the tokens themselves
     const uint32_t *sorted_key, *sorted_number;
     float *part;                // [chunks][2][part_stride]
@@ -69,7 +70,7 @@ __global__ __launch_bounds__(256) void k_embedding(EmbeddingArgs p) {
 }
 
 // ---------------------------------------------------------------------------
-// Sorting, a digit at a time from the lowest.
+// Sorting: many tokens a digit at a time from the lowest, few in one launch.
 // ---------------------------------------------------------------------------
 
 __device__ __forceinline__ uint32_t sort_key(const EmbeddingArgs &p, uint32_t i) {
@@ -199,87 +200,95 @@ __global__ __launch_bounds__(256) void k_sort_move(EmbeddingArgs p) {
     }
 }
 
-// All digits in one workgroup, whose LDS holds the tokens: R rounds of a wave.
-template <int R>
-__global__ __launch_bounds__(1024) void k_sort_whole(EmbeddingArgs p) {
-    constexpr uint32_t kWaves = 16;
-    __shared__ uint32_t keys[R * 1024];
-    __shared__ uint16_t numbers[R * 1024];
-    __shared__ uint16_t wave_has[kWaves][kSortMost];    // how many a wave has of a value, then where they begin
-    __shared__ uint32_t scan[kWaves];
-    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = wave * (R * 64) + lane;
-    uint32_t key[R], number[R], rank[R];
+// Few tokens: a workgroup to p.values of the table's rows, which reads all tokens,
+// counts those of lower rows, lists its own and moves them to their places, first
+// by row, then by wave, whose stretches follow one another, then in order.  Bound
+// by the instructions of the first pass, some 25 for 64 tokens.  Sums and all of
+// 50021 x 8: 64 tokens 13 us, 8192 22, 16384 24, 32768 29 (by tiles and digits 16384
+// 38, 32768 43); 16384 times the same token 29.  K: tokens as unsigned numbers,
+// of which negative ones are the largest.
+template <typename K>
+__global__ __launch_bounds__(1024) void k_sort_range(EmbeddingArgs p) {
+    constexpr uint32_t kWaves = 16, kAhead = 8;
+    static_assert(kRangeTokens * kSortMost <= uint64_t(1) << 32, "a number and a digit in 32 bits");
+    extern __shared__ uint32_t list[];                  // numbers and digits, each wave's from its stretch on
+    __shared__ uint16_t wave_has[kWaves][kSortMost];    // how many a wave has of a row, then where the next one goes
+    __shared__ uint32_t scan[kWaves], lower[kWaves];
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, low = blockIdx.x * p.values;
+    const uint32_t stretch = (p.count + 1023) / 1024 * 64, first = wave * stretch, last = min(p.count, first + stretch);
+    for (uint32_t i = threadIdx.x; i < kWaves * kSortMost; i += 1024) (&wave_has[0][0])[i] = 0;
+    uint32_t less = 0, listed = first;
+    for (uint32_t i0 = first; i0 < last; i0 += 64 * kAhead) {
+        K token[kAhead];
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        number[r] = first + r * 64;
-        key[r] = number[r] < p.count ? sort_key(p, number[r]) : 0;
+        for (uint32_t k = 0; k < kAhead; ++k)
+            token[k] = static_cast<const K *>(p.token)[min(i0 + k * 64 + lane, p.count - 1)];
+#pragma unroll
+        for (uint32_t k = 0; k < kAhead; ++k) {
+            const uint32_t i = i0 + k * 64 + lane, digit = (token[k] < p.rows ? uint32_t(token[k]) : p.rows) - low;
+            if (i < last && int32_t(digit) < 0) ++less;
+            const uint64_t set = __ballot(i < last && digit < p.values);
+            if (!set) continue;
+            if (set >> lane & 1) list[listed + __popcll(set & ((uint64_t(1) << lane) - 1))] = i * kSortMost + digit;
+            listed += __popcll(set);
+        }
     }
-    for (uint32_t shift = 0;; shift += p.shift) {
-        for (uint32_t i = threadIdx.x; i < kWaves * kSortMost; i += 1024) (&wave_has[0][0])[i] = 0;
-        __syncthreads();
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const bool real = first + r * 64 < p.count;
-            const uint32_t digit = key[r] >> shift & (p.values - 1);
+    __syncthreads();
+    // fn(number, digit, rank) of what the wave listed; counts it
+    const auto each = [&](auto fn) {
+        for (uint32_t j = first; j < listed; j += 64) {
+            const bool real = j + lane < listed;
+            const uint32_t x = list[min(j + lane, listed - 1)], digit = x % kSortMost;
             uint64_t same = __ballot(real);             // lanes with this lane's digit
-            for (uint32_t bit = 1; bit < p.values; bit <<= 1) {
-                const uint64_t set = __ballot(digit & bit);
-                same &= digit & bit ? set : ~set;
-            }
+            if (__any(digit != uint32_t(__builtin_amdgcn_readfirstlane(digit))))
+                for (uint32_t bit = 1; bit < p.values; bit <<= 1) {
+                    const uint64_t set = __ballot(digit & bit);
+                    same &= digit & bit ? set : ~set;
+                }
             const uint64_t below = same & ((uint64_t(1) << lane) - 1);
-            rank[r] = 0;
-            if (real) rank[r] = wave_has[wave][digit] + __popcll(below);
+            uint32_t at = 0;
+            if (real) at = wave_has[wave][digit] + __popcll(below);
             wave_sync();                                // every lane has read before the first of each digit writes
-            if (real && below == 0) wave_has[wave][digit] = uint16_t(rank[r] + __popcll(same));
+            if (real && below == 0) wave_has[wave][digit] = uint16_t(at + __popcll(same));
             wave_sync();
+            if (real) fn(x / kSortMost, digit, at);
         }
-        __syncthreads();
-        // sums over the waves of each value, and over the lower values
-        uint32_t sum = 0;
-        if (threadIdx.x < p.values)
+    };
+    each([](uint32_t, uint32_t, uint32_t) {});
 #pragma unroll
-            for (uint32_t w = 0; w < kWaves; ++w) sum += wave_has[w][threadIdx.x];
-        uint32_t up = sum;
+    for (int d = 1; d < 64; d <<= 1) less += __shfl_xor(less, d);
+    if (lane == 0) lower[wave] = less;
+    __syncthreads();
+    uint32_t sum = 0;
+    if (threadIdx.x < p.values)
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const uint32_t o = __shfl_up(up, d);
-            if (lane >= uint32_t(d)) up += o;
-        }
-        if (lane == 63) scan[wave] = up;
-        __syncthreads();
-        if (threadIdx.x < p.values) {
-            up -= sum;
-            for (uint32_t w = 0; w < wave; ++w) up += scan[w];
+        for (uint32_t w = 0; w < kWaves; ++w) sum += wave_has[w][threadIdx.x];
+    uint32_t up = sum;
 #pragma unroll
-            for (uint32_t w = 0; w < kWaves; ++w) {
-                const uint32_t x = wave_has[w][threadIdx.x];
-                wave_has[w][threadIdx.x] = uint16_t(up);
-                up += x;
-            }
-        }
-        __syncthreads();
-        const bool last = uint64_t(1) << (shift + p.shift) > p.rows;
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            if (first + r * 64 >= p.count) continue;
-            const uint32_t at = wave_has[wave][key[r] >> shift & (p.values - 1)] + rank[r];
-            if (last) {
-                p.key[0][at] = key[r];
-                p.number[0][at] = number[r];
-            } else {
-                keys[at] = key[r];
-                numbers[at] = uint16_t(number[r]);
-            }
-        }
-        if (last) return;
-        __syncthreads();
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            key[r] = keys[first + r * 64];
-            number[r] = numbers[first + r * 64];
-        }
-        __syncthreads();
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t o = __shfl_up(up, d);
+        if (lane >= uint32_t(d)) up += o;
     }
+    if (lane == 63) scan[wave] = up;
+    __syncthreads();
+    if (threadIdx.x < p.values) {
+        up -= sum;
+        for (uint32_t w = 0; w < wave; ++w) up += scan[w];
+#pragma unroll
+        for (uint32_t w = 0; w < kWaves; ++w) {
+            const uint32_t x = wave_has[w][threadIdx.x];
+            wave_has[w][threadIdx.x] = uint16_t(up);
+            up += x;
+        }
+    }
+    __syncthreads();
+    uint32_t before = 0;
+#pragma unroll
+    for (uint32_t w = 0; w < kWaves; ++w) before += lower[w];
+    each([&](uint32_t i, uint32_t digit, uint32_t at) {
+        p.key[0][before + at] = low + digit;
+        p.number[0][before + at] = i;
+    });
 }
 
 // ---------------------------------------------------------------------------

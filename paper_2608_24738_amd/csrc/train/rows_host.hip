@@ -197,6 +197,10 @@ int check_embedding(int dtype, int64_t rows, int64_t width, const void *tokens, 
     return TM_OK;
 }
 
+// Rows up to which a workgroup to a range of them sorts faster than tiles and digits: the whole gradient of 16384 tokens
+// of 262144 x 8 takes 35 us and by digits 48, of 1000003 rows 85 and 71.
+constexpr uint64_t kRangeRows = uint64_t(1) << 19;
+
 // A workgroup's threads along a row, the rest for other rows.
 dim3 row_block(uint64_t pieces) {
     const uint32_t x = uint32_t(std::min<uint64_t>(256, std::max<uint64_t>(8, pieces)));
@@ -306,12 +310,14 @@ extern "C" int tm_embedding_grad(const void *tokens, int token_dtype, int64_t co
     a.grad = out_grad;
     a.from = -1;
     const uint32_t each = uint32_t(__builtin_ctz(a.values));
-    // Few tokens are sorted by one workgroup (2048 of 50021: 8 us, 4096: 13; by tiles and digits 8192 take 22 in four
-    // launches, 16384 take 25, by one workgroup 37).
-    if (s.count <= 8192) {
-        a.shift = each;
-        const int rc = launch(s.count <= 2048 ? k_sort_whole<2> : s.count <= 4096 ? k_sort_whole<4> : k_sort_whole<8>,
-                              dim3(1), dim3(1024), 0, stream, a);
+    if (s.count <= kRangeTokens && s.rows < kRangeRows) {
+        // a workgroup to every CU, until each has kSortMost rows
+        a.values = 1;
+        while (a.values < kSortMost && a.values * 256 <= s.rows) a.values *= 2;
+        const int rc = launch(s.token_bytes == 1   ? k_sort_range<uint8_t>
+                              : s.token_bytes == 4 ? k_sort_range<uint32_t>
+                                                   : k_sort_range<uint64_t>,
+                              dim3(uint32_t(s.rows / a.values + 1)), dim3(1024), ceil_div(s.count, 1024) * 4096, stream, a);
         if (rc != TM_OK) return rc;
         a.from = 0;
     } else {

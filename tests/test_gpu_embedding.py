@@ -102,6 +102,15 @@ def test_many_tokens(tokens, how):
     compare(*make(tokens, 1500, 12, "bf16", how), 1.0, "bf16", "embedding many %d %s" % (tokens, how))
 
 
+@pytest.mark.parametrize("kind", ["int32", "int64"])
+@pytest.mark.parametrize("tokens,rows,how", [
+    (32768, 20011, "zipf"), (32769, 20011, "zipf"), (32768, 700, "same"), (30000, 511, "outside"), (17000, 131072, "falling"),
+    (1025, 65536, "same"), (9000, (1 << 19) - 1, "outside"), (9000, 1 << 19, "outside"), (16383, 2, "falling")])
+def test_sorted_by_ranges_and_by_digits(tokens, rows, how, kind):
+    """The most tokens and rows of a workgroup to a range of rows, one more of each, and all tokens in one range."""
+    compare(*make(tokens, rows, 3, "f32", how, kind), 1.0, "f32", "embedding %s %s %d of %d" % (kind, how, tokens, rows))
+
+
 def test_shapes_strides_and_no_tokens():
     import torch
     from paper_2608_24738_amd import training

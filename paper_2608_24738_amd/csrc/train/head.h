@@ -69,6 +69,7 @@ struct HeadArgs {
     // in the workspace
     uint32_t *count;            // packed rows
     uint32_t *chunk_count;      // of each chunk, then their exponents
+    uint32_t pack_rows;         // of a workgroup, up to kPackRows
     uint32_t chunks;            // 0: few rows, which are counted where they are needed
     Div32 div_pieces;           // pieces of a packed row
     uint32_t *list;             // the packed rows' numbers
@@ -119,6 +120,43 @@ __device__ __forceinline__ bool takes_part(const HeadArgs &p, uint32_t n, int32_
     y = p.label ? load_label(p.label, p.label_bytes, n, p.classes) : -1;
     return y >= 0 || p.all;
 }
+// Of N rows, `step` apart, at once: what of them is before `end`.  Loads come first, none waits for another.
+template <int N, typename F>
+__device__ __forceinline__ void each_part(const HeadArgs &p, uint32_t n0, uint32_t step, uint32_t end, bool ups, F fn) {
+    int32_t y[N];
+    uint32_t n[N];
+    float a[N] = {}, z[N] = {};
+#pragma unroll
+    for (int k = 0; k < N; ++k) n[k] = min(n0 + k * step, end - 1);
+    const auto labels = [&](const auto *label) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) y[k] = label[n[k]] < p.classes ? int32_t(label[n[k]]) : -1;
+    };
+    if (!p.label) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) y[k] = -1;
+    } else if (p.label_bytes == 1) {
+        labels(static_cast<const uint8_t *>(p.label));
+    } else if (p.label_bytes == 4) {
+        labels(static_cast<const uint32_t *>(p.label));
+    } else {
+        labels(static_cast<const uint64_t *>(p.label));
+    }
+    if (ups && p.up_logp) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) a[k] = p.up_logp[n[k]];
+    }
+    if (ups && p.up_log_sum) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) z[k] = p.up_log_sum[n[k]];
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        if (n0 + k * step >= end || (y[k] < 0 && !p.all)) continue;
+        const float up = y[k] >= 0 ? a[k] : 0.0f;
+        fn(n[k], y[k], HeadUp{p.scale * up, p.scale * (up - z[k])});
+    }
+}
 // Exponent of a row's slopes, kNoExponent for zeros.
 constexpr int kNoExponent = -1000;
 __device__ __forceinline__ int slope_exponent(HeadUp u) {
@@ -148,13 +186,10 @@ __global__ __launch_bounds__(256) void k_head_count(HeadArgs p) {
     const uint32_t last = min(p.n, (blockIdx.x + 1) * kListChunk);
     uint32_t mine = 0;
     int most = kNoExponent;
-#pragma unroll 4
-    for (uint32_t n = blockIdx.x * kListChunk + threadIdx.x; n < last; n += 256) {
-        int32_t y;
-        if (!takes_part(p, n, y)) continue;
+    each_part<kListChunk / 256>(p, blockIdx.x * kListChunk + threadIdx.x, 256, last, p.inverse, [&](uint32_t, int32_t, HeadUp u) {
         ++mine;
-        if (p.inverse) most = max(most, slope_exponent(head_up(p, n, y)));
-    }
+        if (p.inverse) most = max(most, slope_exponent(u));
+    });
     tally(mine, most, &found, &top);
     __syncthreads();
     if (threadIdx.x == 0) {
@@ -212,18 +247,22 @@ __global__ __launch_bounds__(256) void k_head_pack(HeadArgs p) {
         top = kNoExponent;
     }
     __syncthreads();
-    const uint32_t r0 = blockIdx.x * kPackRows, chunk = r0 / kListChunk;
+    const uint32_t r0 = blockIdx.x * p.pack_rows, chunk = r0 / kListChunk;
     const bool exponents = p.inverse != nullptr;
+    // the workgroup's own rows, a lane of the first wave to each
+    const uint32_t own_row = r0 + threadIdx.x;
+    const bool real_row = threadIdx.x < p.pack_rows && own_row < p.n;
+    int32_t y = -1;
+    const bool in = real_row && takes_part(p, own_row, y);
     uint32_t mine = 0;
     int most = kNoExponent;
     const uint32_t last = exponents && !p.chunks ? p.n : r0;
-#pragma unroll 4
-    for (uint32_t n = (p.chunks ? chunk * kListChunk : 0) + threadIdx.x; n < last; n += 256) {
-        int32_t y;
-        if (!takes_part(p, n, y)) continue;
-        mine += n < r0;
-        if (exponents && !p.chunks) most = max(most, slope_exponent(head_up(p, n, y)));
-    }
+    constexpr int kAhead = 8;
+    for (uint32_t n0 = (p.chunks ? chunk * kListChunk : 0) + threadIdx.x; n0 < last; n0 += 256 * kAhead)
+        each_part<kAhead>(p, n0, 256, last, exponents && !p.chunks, [&](uint32_t n, int32_t, HeadUp u) {
+            mine += n < r0;
+            if (exponents && !p.chunks) most = max(most, slope_exponent(u));
+        });
     for (uint32_t i = threadIdx.x; i < p.chunks; i += 256) {
         mine += i < chunk ? p.chunk_count[i] : 0;
         if (exponents) most = max(most, int(p.chunk_count[p.chunks + i]));
@@ -231,16 +270,14 @@ __global__ __launch_bounds__(256) void k_head_pack(HeadArgs p) {
     tally(mine, most, &before, &top);
     __syncthreads();
     if (threadIdx.x < 64) {
-        const uint32_t n = r0 + threadIdx.x;
-        int32_t y = -1;
-        const bool real = threadIdx.x < kPackRows && n < p.n, in = real && takes_part(p, n, y);
+        const uint32_t n = own_row;
         const uint64_t set = __ballot(in);
         const uint32_t rank = __popcll(set & ((uint64_t(1) << threadIdx.x) - 1)), at = before + rank;
         if (threadIdx.x == 0) own = __popcll(set);
         const int common = top == kNoExponent ? 0 : top;
         if (threadIdx.x == 0 && blockIdx.x == 0 && exponents) p.inverse[p.n_pad] = power(common - kSlopeExponent);
-        if (real && p.place) p.place[n] = in ? int32_t(at) : -1;
-        if (real && !in && !p.row) {
+        if (real_row && p.place) p.place[n] = in ? int32_t(at) : -1;
+        if (real_row && !in && !p.row) {
             if (p.logp) p.logp[n] = 0.0f;
             if (p.stats) p.stats[n] = {0.0f, 1.0f};
         }
@@ -569,31 +606,42 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_hidde
     }
 }
 
+// The sum of `count` groups of four, `step` apart, in order; four loads on their way at once.
+__device__ __forceinline__ f32x4 sum_of(const float *from, uint64_t step, uint32_t count) {
+    constexpr uint32_t kAhead = 4;
+    f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (uint32_t s = 0; s < count; s += kAhead) {
+        f32x4 x[kAhead];
+#pragma unroll
+        for (uint32_t k = 0; k < kAhead; ++k) x[k] = *reinterpret_cast<const f32x4 *>(from + min(s + k, count - 1) * step);
+#pragma unroll
+        for (uint32_t k = 0; k < kAhead; ++k)
+            if (s + k < count) sum += x[k];
+    }
+    return sum;
+}
+
 // dh of every row from the splits' sums; rows that took no part get zeros.
 template <typename T>
 __global__ __launch_bounds__(256) void k_head_hidden_join(HeadArgs p) {
     const uint32_t quads = (p.width + 3) / 4, tiles_n = (*p.count + p.tile_n - 1) / p.tile_n;
     const uint32_t splits = hidden_splits(p, tiles_n);
     const uint64_t step = uint64_t(tiles_n) * p.tile_n * p.sum_stride;
-    const uint64_t total = uint64_t(p.n) * quads;
-    for (uint64_t i = uint64_t(blockIdx.x) * 256 + threadIdx.x; i < total; i += uint64_t(gridDim.x) * 256) {
-        const uint32_t n = uint32_t(i / quads), d = uint32_t(i % quads) * 4;
+    for (uint32_t n = blockIdx.x * blockDim.y + threadIdx.y; n < p.n; n += gridDim.x * blockDim.y) {
         const int32_t at = p.place[n];
-        float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (at >= 0) {
-            const float *from = p.sum + uint64_t(at) * p.sum_stride + d;
-#pragma unroll 4
-            for (uint32_t s = 0; s < splits; ++s) {
-                const f32x4 x = *reinterpret_cast<const f32x4 *>(from + s * step);
-#pragma unroll
-                for (int q = 0; q < 4; ++q) v[q] += x[q];
+        const float back = p.inverse && at >= 0 ? p.inverse[at] : 1.0f;
+        for (uint32_t i = threadIdx.x; i < quads; i += blockDim.x) {
+            const uint32_t d = i * 4;
+            f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+            if (at >= 0) {
+                const float *from = p.sum + uint64_t(at) * p.sum_stride + d;
+                sum = sum_of(from, step, splits);
             }
-            if (p.inverse) {
+            float v[4];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) v[q] *= p.inverse[at];
-            }
+            for (int q = 0; q < 4; ++q) v[q] = sum[q] * back;
+            store_pack<4>(static_cast<T *>(p.grad_hidden) + uint64_t(n) * p.width + d, narrow_pack<T>(v), p.width - d);
         }
-        store_pack<4>(static_cast<T *>(p.grad_hidden) + uint64_t(n) * p.width + d, narrow_pack<T>(v), p.width - d);
     }
 }
 
@@ -646,19 +694,19 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_weigh
 template <typename T>
 __global__ __launch_bounds__(256) void k_head_weight_join(HeadArgs p) {
     const uint32_t quads = (p.width + 3) / 4, rows = min(p.piece, p.classes - p.first);
-    const uint64_t total = uint64_t(rows) * quads, step = uint64_t(rows) * p.sum_stride;
+    const uint64_t step = uint64_t(rows) * p.sum_stride;
     const float back = p.inverse ? p.inverse[p.n_pad] : 1.0f;
-    for (uint64_t i = uint64_t(blockIdx.x) * 256 + threadIdx.x; i < total; i += uint64_t(gridDim.x) * 256) {
-        const uint32_t v = uint32_t(i / quads), d = uint32_t(i % quads) * 4;
-        const float *from = p.weight_sum + uint64_t(v) * p.sum_stride + d;
-        f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
-        for (uint32_t s = 0; s < p.weight_splits; ++s) sum += *reinterpret_cast<const f32x4 *>(from + s * step);
-        float x[4];
+    for (uint32_t v = blockIdx.x * blockDim.y + threadIdx.y; v < rows; v += gridDim.x * blockDim.y)
+        for (uint32_t i = threadIdx.x; i < quads; i += blockDim.x) {
+            const uint32_t d = i * 4;
+            const float *from = p.weight_sum + uint64_t(v) * p.sum_stride + d;
+            const f32x4 sum = sum_of(from, step, p.weight_splits);
+            float x[4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) x[q] = sum[q] * back;
-        store_pack<4>(static_cast<T *>(p.grad_weight) + uint64_t(p.first + v) * p.width + d, narrow_pack<T>(x), p.width - d);
-    }
+            for (int q = 0; q < 4; ++q) x[q] = sum[q] * back;
+            store_pack<4>(static_cast<T *>(p.grad_weight) + uint64_t(p.first + v) * p.width + d, narrow_pack<T>(x),
+                          p.width - d);
+        }
 }
 
 }  // namespace tmtrain

@@ -96,10 +96,12 @@ constexpr uint64_t kSlots = (2 * sizeof(typename Tile::Buffer) <= 80 * 1024 ? 2 
 bool fine(const HeadShape &s) { return s.size == 2 && s.n <= kFineRows; }
 
 // fn(tile): the larger of two, unless it leaves CUs without one or more than
-// half of itself empty; `most` is how often k can be split.
+// half of itself empty; `most` is how often k can be split, of which eight count:
+// more cost what they write and read again (dh of 1024 x 8192 x 1024 bf16 by 16
+// splits of the larger 69 us, by 8 of the smaller 63).
 template <typename T, bool Across, typename F>
 auto by_tile(const HeadShape &s, uint64_t m, uint64_t n, uint64_t most, F fn) {
-    const bool large = ceil_div(m, 256) * ceil_div(n, planes(s) ? 128 : 256) * most >= kCus && n > 128 && m > 128;
+    const bool large = ceil_div(m, 256) * ceil_div(n, planes(s) ? 128 : 256) * std::min<uint64_t>(most, 8) >= kCus && n > 128 && m > 128;
     if constexpr (std::is_same<T, float>::value) {
         if (planes(s)) return large ? fn(static_cast<LargeSplit *>(nullptr)) : fn(static_cast<SmallSplit *>(nullptr));
         if (n <= kNarrowRows) return fn(static_cast<NarrowTile *>(nullptr));
@@ -238,14 +240,15 @@ dim3 lasting_grid(uint64_t m, uint64_t n) {
 // The packed rows.
 template <typename T>
 int pack_rows(const HeadShape &s, HeadArgs &a, hipStream_t stream) {
-    a.chunks = a.n <= 2 * kListChunk ? 0 : uint32_t(ceil_div(a.n, kListChunk));
+    a.chunks = a.n <= 4 * kListChunk ? 0 : uint32_t(ceil_div(a.n, kListChunk));
+    a.pack_rows = a.n <= kPackRows * kCus ? kPackRows / 2 : kPackRows;
     if (a.chunks) {
         const int rc = launch(k_head_count, dim3(a.chunks), dim3(256), 0, stream, a);
         if (rc != TM_OK) return rc;
     }
     const bool split = std::is_same<T, float>::value && planes(s);
     a.div_pieces = Div32::make(uint32_t(a.width_pad * (split ? 2 : sizeof(T)) / 16));
-    const dim3 grid(uint32_t(ceil_div(a.n, kPackRows)));
+    const dim3 grid(uint32_t(ceil_div(a.n, a.pack_rows)));
     if constexpr (std::is_same<T, float>::value) {
         if (split) return launch(k_head_pack<float, bf16, 3>, grid, dim3(256), 0, stream, a);
     }
@@ -264,6 +267,15 @@ int lay_piece(const HeadShape &s, const HeadArgs &a, hipStream_t stream) {
         if (split) return launch(k_head_lay<float, bf16, 3>, grid, block, 0, stream, a);
     }
     return launch(k_head_lay<T, T, 1>, grid, block, 0, stream, a);
+}
+
+// The joins' threads: along a row, four columns to each, the rest for other rows.
+dim3 join_block(const HeadShape &s) {
+    const uint32_t x = uint32_t(std::min<uint64_t>(256, pow2_from(uint32_t(ceil_div(s.width, 4)))));
+    return dim3(x, 256 / x);
+}
+dim3 join_grid(uint64_t rows, const HeadShape &s) {
+    return dim3(uint32_t(std::min<uint64_t>(ceil_div(rows, join_block(s).y), 4096)));
 }
 
 template <typename T>
@@ -348,14 +360,12 @@ int run_head_grad(HeadArgs a, const HeadShape &s, hipStream_t stream) {
                               dim3(Tile::kThreads), 0, stream, a);
             });
             if (rc == TM_OK && a.weight_splits > 1) {
-                const uint64_t blocks = ceil_div(rows * ceil_div(s.width, 4), 256);
-                rc = launch(k_head_weight_join<T>, dim3(uint32_t(std::min<uint64_t>(blocks, 4096))), dim3(256), 0, stream, a);
+                rc = launch(k_head_weight_join<T>, join_grid(rows, s), join_block(s), 0, stream, a);
             }
         }
     }
     if (rc != TM_OK || !a.grad_hidden) return rc;
-    const uint64_t blocks = ceil_div(s.n * ceil_div(s.width, 4), 256);
-    return launch(k_head_hidden_join<T>, dim3(uint32_t(std::min<uint64_t>(blocks, 4096))), dim3(256), 0, stream, a);
+    return launch(k_head_hidden_join<T>, join_grid(s.n, s), join_block(s), 0, stream, a);
 }
 
 void head_args(const HeadShape &s, const void *hidden, int64_t hidden_stride, const void *weight, int64_t weight_stride,

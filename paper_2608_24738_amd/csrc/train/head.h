@@ -406,7 +406,7 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_sums(
         for (int j = 0; j < Tile::TN; ++j) {
             const uint32_t n = at.n * Tile::BN + tile.column(j);
             const int32_t y = n < count && p.label ? load_label(p.label, p.label_bytes, p.list[n], p.classes) : -1;
-            wants[j] = y < 0 ? ~0u : uint32_t(y) - p.first - at.m * Tile::BM - (tile.row(0) & ~15u);
+            wants[j] = y < 0 ? ~0u : uint32_t(y) - p.first - at.m * Tile::BM - tile.first_row();
         }
     }, [&](Tile &tile, TilePlace at) {
         const uint32_t part = (p.first / Tile::BM + at.m) * Tile::WM + tile.wave / Tile::WN;
@@ -422,14 +422,14 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_sums(
 #pragma unroll
         for (int j = 0; j < Tile::TN; ++j) {
             const uint32_t n = at.n * Tile::BN + tile.column(j);
-            const bool mine = wants[j] < 16u * Tile::TM && (wants[j] & 15) - uint32_t(tile.lane >> 4) * 4 < 4;
+            const bool mine = wants[j] < 16u * Tile::TM && (wants[j] >> 3 & 3) == uint32_t(tile.lane >> 4);
             if (__any(mine)) {                      // few tiles hold a column's label
                 float label = 0.0f;
 #pragma unroll
                 for (int i = 0; i < Tile::TM; ++i)
 #pragma unroll
                     for (int q = 0; q < 4; ++q)
-                        if ((wants[j] >> 4) == uint32_t(i) && (wants[j] & 3) == uint32_t(q)) label = tile.acc[i][j][q];
+                        if ((wants[j] & ~24u) == Tile::pair_row(i) + q) label = tile.acc[i][j][q];
                 if (mine) p.found[n] = label;
             }
             float most = -INFINITY;
@@ -528,35 +528,35 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_slope
             const uint32_t want = uint32_t(r.y) - p.first - at.m * Tile::BM - tile.row(0);
             const bool labels = __any(r.y >= 0 && want < 16u * Tile::TM);
 #pragma unroll
-            for (int i = 0; i < Tile::TM; ++i) {
+            for (int i = 0; i < Tile::TM; i += 2) {             // eight rows side by side
                 const uint32_t v = at.m * Tile::BM + tile.row(i);
-                float g[4];
+                float g[8];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) g[q] = -r.b * exp2_hw((tile.acc[i][j][q] - r.m) * p.c);
+                for (int q = 0; q < 8; ++q) g[q] = -r.b * exp2_hw((tile.acc[i + q / 4][j][q % 4] - r.m) * p.c);
                 if (labels) {
 #pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        if (r.y >= 0 && want == uint32_t(16 * i + q)) g[q] += r.a;
+                    for (int q = 0; q < 8; ++q)
+                        if (r.y >= 0 && want == Tile::pair_row(i) + q) g[q] += r.a;
                 }
                 if (edge) {
 #pragma unroll
-                    for (int q = 0; q < 4; ++q)
+                    for (int q = 0; q < 8; ++q)
                         if (n >= count || v + q >= rows) g[q] = 0.0f;
                 }
                 const uint64_t to = uint64_t(n) * p.piece + v, plane = uint64_t(p.n_pad) * p.piece;
-                Pack<S, 4> out[G];
+                Pack<S, 8> out[G];
                 if (!__is_same(T, f16) || p.slope) {
                     split(g, out);
 #pragma unroll
-                    for (int k = 0; k < G; ++k) store_pack<4>(static_cast<S *>(p.slope) + to + k * plane, out[k]);
+                    for (int k = 0; k < G; ++k) store_pack<8>(static_cast<S *>(p.slope) + to + k * plane, out[k]);
                 }
                 if constexpr (__is_same(T, f16)) {
                     if (!p.slope_common) continue;
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) g[q] *= ratios[j];
+                    for (int q = 0; q < 8; ++q) g[q] *= ratios[j];
                     split(g, out);
 #pragma unroll
-                    for (int k = 0; k < G; ++k) store_pack<4>(static_cast<S *>(p.slope_common) + to + k * plane, out[k]);
+                    for (int k = 0; k < G; ++k) store_pack<8>(static_cast<S *>(p.slope_common) + to + k * plane, out[k]);
                 }
             }
         }
@@ -594,13 +594,13 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_hidde
             f32x4 before[Tile::TM];
 #pragma unroll
             for (int i = 0; i < Tile::TM; ++i)
-                before[i] = *reinterpret_cast<const f32x4 *>(to + min(at.m * Tile::BM + tile.row(i), p.sum_stride - 4));
+                before[i] = *reinterpret_cast<const f32x4 *>(to + min(at.m * Tile::BM + tile.row_across(i), p.sum_stride - 4));
 #pragma unroll
             for (int i = 0; i < Tile::TM; ++i) tile.acc[i][j] += before[i];
         }
 #pragma unroll
         for (int i = 0; i < Tile::TM; ++i) {
-            const uint32_t d = at.m * Tile::BM + tile.row(i);
+            const uint32_t d = at.m * Tile::BM + tile.row_across(i);
             if (d < p.sum_stride) *reinterpret_cast<f32x4 *>(to + d) = tile.acc[i][j];
         }
     }
@@ -672,7 +672,7 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_weigh
             float *to = p.weight_sum + (uint64_t(at.split) * rows + v) * p.sum_stride;
 #pragma unroll
             for (int i = 0; i < Tile::TM; ++i) {
-                const uint32_t d = at.m * Tile::BM + tile.row(i);
+                const uint32_t d = at.m * Tile::BM + tile.row_across(i);
                 if (d < p.sum_stride) *reinterpret_cast<f32x4 *>(to + d) = tile.acc[i][j];
             }
             continue;
@@ -680,7 +680,7 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_weigh
         T *to = static_cast<T *>(p.grad_weight) + uint64_t(p.first + v) * p.width;
 #pragma unroll
         for (int i = 0; i < Tile::TM; ++i) {
-            const uint32_t d = at.m * Tile::BM + tile.row(i);
+            const uint32_t d = at.m * Tile::BM + tile.row_across(i);
             if (d >= p.width) continue;
             float x[4];
 #pragma unroll

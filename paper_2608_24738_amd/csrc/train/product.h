@@ -21,7 +21,8 @@
 // floats by four 16x16x4 instructions, of which number e takes k = 4 g + e.
 // Across k, 16-bit elements come from LDS by reads that turn blocks of 4 x 16,
 // floats one by one.  Of the result, a lane holds rows m = 4 g .. 4 g + 3 in
-// column n = lane % 16.
+// column n = lane % 16.  Rows of A along k come to LDS in another order, so that
+// these are, of two blocks, eight rows of C side by side, 16 bytes of 16 bits.
 #pragma once
 
 #include <type_traits>
@@ -91,8 +92,9 @@ struct Operand {
 };
 
 // Copies of an operand's steps to LDS, S elements of m or n by Waves waves, K
-// elements of k a step (one or two instructions' worth).
-template <typename T, int S, int Waves, int K>
+// elements of k a step (one or two instructions' worth).  Pairs: of 32 rows, row 4
+// (2 g + b) + q goes to row 4 g + q of block b.
+template <typename T, int S, int Waves, int K, bool Pairs>
 struct Along {
     static constexpr uint32_t kRow = K * sizeof(T), kPieces = kRow / 16;    // 8 or 4 pieces in a row
     static constexpr uint32_t kAtOnce = 64 / kPieces;                       // rows of one copy
@@ -101,12 +103,16 @@ struct Along {
     uint32_t offset[kCopies], place;
 
     static __device__ __forceinline__ uint32_t order(uint32_t r) { return kPieces == 8 ? r & 7 : r >> 1 & 3; }
+    // The row that row r of LDS holds.
+    static __device__ __forceinline__ uint32_t row_at(uint32_t r) {
+        return Pairs ? (r & ~31u) | (r & 12) << 1 | (r & 16) >> 2 | (r & 3) : r;
+    }
     __device__ __forceinline__ Along(const Operand &o, uint32_t m0, uint32_t first, int lane, int wave) {
         const uint32_t r = lane / kPieces, row = min(m0, o.rows - 1);       // tiles may lie behind the last row
         from = o.at + row * o.stride + uint64_t(first) * kRow;
 #pragma unroll
         for (int i = 0; i < kCopies; ++i)
-            offset[i] = min((i * Waves + wave) * kAtOnce + r, o.rows - 1 - row) * uint32_t(o.stride) +
+            offset[i] = min(row_at((i * Waves + wave) * kAtOnce + r), o.rows - 1 - row) * uint32_t(o.stride) +
                         (lane % kPieces ^ order(r)) * 16;
     }
     __device__ __forceinline__ void fetch(char *lds, uint32_t, int, int wave) {
@@ -224,15 +230,20 @@ struct Tile {
         lane = threadIdx.x & 63;
         wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     }
-    // First row and column, in the tile, of what the lane holds of block i, j.
-    __device__ __forceinline__ uint32_t row(int i) const { return ((wave / WN) * TM + i) * 16 + (lane >> 4) * 4; }
+    // First row and column, in the tile, of what the lane holds of block i, j; rows for A along k, of which blocks 2 i
+    // and 2 i + 1 have eight side by side, and across it.
+    static_assert(TM % 2 == 0, "blocks in pairs");
+    static constexpr __device__ __forceinline__ uint32_t pair_row(int i) { return i / 2 * 32 + i % 2 * 4; }
+    __device__ __forceinline__ uint32_t first_row() const { return wave / WN * TM * 16; }
+    __device__ __forceinline__ uint32_t row(int i) const { return first_row() + (lane >> 4) * 8 + pair_row(i); }
+    __device__ __forceinline__ uint32_t row_across(int i) const { return first_row() + i * 16 + (lane >> 4) * 4; }
     __device__ __forceinline__ uint32_t column(int j) const { return ((wave % WN) * TN + j) * 16 + (lane & 15); }
 
     // Where a tile's operands come from, and the next step of both.
     template <bool AAcross, bool BAcross>
     struct Sources {
-        typedef std::conditional_t<AAcross, Across<T, BM, kWaves, kStep, TM>, Along<T, BM, kWaves, kStep>> FromA;
-        typedef std::conditional_t<BAcross, Across<T, BN, kWaves, kStep, TN>, Along<T, BN, kWaves, kStep>> FromB;
+        typedef std::conditional_t<AAcross, Across<T, BM, kWaves, kStep, TM>, Along<T, BM, kWaves, kStep, true>> FromA;
+        typedef std::conditional_t<BAcross, Across<T, BN, kWaves, kStep, TN>, Along<T, BN, kWaves, kStep, false>> FromB;
         // Waves with their operands at hand go first (4096 x 32768 x 1024: sums 246 -> 238 us); those that
         // read across k would hold up the others' reads (dw 121 -> 158), and planes leave time (sums of floats 309 -> 321).
         static constexpr bool kFirst = !AAcross && !BAcross && PlanesB == 1;

@@ -85,6 +85,7 @@ struct HeadArgs {
     uint32_t n_pad, width_pad, sum_stride;
     uint32_t parts;
     uint32_t first, piece;      // classes of the piece at hand, and its width
+    uint32_t few_shift;         // few rows: 1 << few_shift waves share a row's columns
     uint32_t splits, steps;     // few rows: shares of the classes, and classes of one
     uint32_t blocks, most;      // of the product for dh: workgroups, splits that its k allows
     uint32_t tiles_m, tile_n;   // its tiles across the width, and the rows of one
@@ -232,18 +233,19 @@ __device__ __forceinline__ void lay(const T *from, uint32_t n, S *to, uint64_t p
 
 // Packs the hidden states of kPackRows rows, in whole steps with zeros behind
 // them, and writes where they went and what the gradient needs of them.  Every
-// workgroup counts the rows before its own: all of them, or those of its chunk
-// and the chunks' counts.  The last one leaves zeros up to a multiple of 64.
+// workgroup counts the rows before its own and all of them: one by one, or by the
+// chunks' counts.  Behind the last one, workgroups leave zeros up to a multiple
+// of 64.
 // 4096 rows of 1024 bf16: 9 us, and 5 for the chunks' counts; 509 rows 5.
 constexpr uint32_t kPackRows = 8;
 template <typename T, typename S, int P>
 __global__ __launch_bounds__(256) void k_head_pack(HeadArgs p) {
     constexpr uint32_t V = 16 / sizeof(S);
-    __shared__ uint32_t before, own;
+    __shared__ uint32_t before, own, total;
     __shared__ int top;
     __shared__ uint32_t from[kPackRows];
     if (threadIdx.x == 0) {
-        before = 0;
+        before = total = 0;
         top = kNoExponent;
     }
     __syncthreads();
@@ -254,20 +256,24 @@ __global__ __launch_bounds__(256) void k_head_pack(HeadArgs p) {
     const bool real_row = threadIdx.x < p.pack_rows && own_row < p.n;
     int32_t y = -1;
     const bool in = real_row && takes_part(p, own_row, y);
-    uint32_t mine = 0;
+    uint32_t mine = 0, all = 0;
     int most = kNoExponent;
-    const uint32_t last = exponents && !p.chunks ? p.n : r0;
+    const uint32_t last = p.chunks ? r0 : p.n;
     constexpr int kAhead = 8;
     for (uint32_t n0 = (p.chunks ? chunk * kListChunk : 0) + threadIdx.x; n0 < last; n0 += 256 * kAhead)
         each_part<kAhead>(p, n0, 256, last, exponents && !p.chunks, [&](uint32_t n, int32_t, HeadUp u) {
             mine += n < r0;
+            all += !p.chunks;
             if (exponents && !p.chunks) most = max(most, slope_exponent(u));
         });
     for (uint32_t i = threadIdx.x; i < p.chunks; i += 256) {
-        mine += i < chunk ? p.chunk_count[i] : 0;
+        const uint32_t found = p.chunk_count[i];
+        mine += i < chunk ? found : 0;
+        all += found;
         if (exponents) most = max(most, int(p.chunk_count[p.chunks + i]));
     }
     tally(mine, most, &before, &top);
+    tally(all, most, &total, &top);
     __syncthreads();
     if (threadIdx.x < 64) {
         const uint32_t n = own_row;
@@ -301,18 +307,20 @@ __global__ __launch_bounds__(256) void k_head_pack(HeadArgs p) {
         }
     }
     __syncthreads();
-    const bool final = blockIdx.x + 1 == gridDim.x;
-    const uint32_t total = before + own;
-    if (final && threadIdx.x == 0) *p.count = total;
-    const uint32_t pieces = p.width_pad / V, rows = final ? ((total + 63) & ~63u) - before : own;
+    if (threadIdx.x == 0 && blockIdx.x == 0) *p.count = total;
+    const uint32_t pieces = p.width_pad / V;
     const uint64_t plane = uint64_t(p.n_pad) * p.width_pad;
+    S *packed = static_cast<S *>(p.packed);
 #pragma unroll 4
-    for (uint32_t i = threadIdx.x; i < rows * pieces; i += 256) {
+    for (uint32_t i = threadIdx.x; i < own * pieces; i += 256) {
         const uint32_t r = p.div_pieces.div(i), c = (i - r * pieces) * V;
-        const bool real = r < own && c < p.width;
+        const bool real = c < p.width;
         lay<T, S, P, V>(static_cast<const T *>(p.hidden) + (real ? from[r] * p.hidden_stride + c : 0),
-                        real ? p.width - c : 0, static_cast<S *>(p.packed) + uint64_t(before + r) * p.width_pad + c, plane);
+                        real ? p.width - c : 0, packed + uint64_t(before + r) * p.width_pad + c, plane);
     }
+    for (uint32_t r = total + blockIdx.x; r < ((total + 63) & ~63u); r += gridDim.x)
+        for (uint32_t i = threadIdx.x; i < pieces; i += 256)
+            lay<T, S, P, V>(static_cast<const T *>(p.hidden), 0, packed + uint64_t(r) * p.width_pad + i * V, plane);
 }
 
 // The weights of the piece at hand, laid out likewise.
@@ -621,12 +629,35 @@ __device__ __forceinline__ f32x4 sum_of(const float *from, uint64_t step, uint32
     return sum;
 }
 
-// dh of every row from the splits' sums; rows that took no part get zeros.
-template <typename T>
+// dh of every row from the splits' sums; rows that took no part get zeros.  Few
+// rows of many splits: Shares threads to four columns, each with a share of the
+// splits, whose sums are added in order.
+constexpr uint32_t kJoinQuads = 16;
+template <typename T, uint32_t Shares>
 __global__ __launch_bounds__(256) void k_head_hidden_join(HeadArgs p) {
+    __shared__ f32x4 lds[Shares][Shares > 1 ? kJoinQuads : 1];
     const uint32_t quads = (p.width + 3) / 4, tiles_n = (*p.count + p.tile_n - 1) / p.tile_n;
     const uint32_t splits = hidden_splits(p, tiles_n);
     const uint64_t step = uint64_t(tiles_n) * p.tile_n * p.sum_stride;
+    if constexpr (Shares > 1) {
+        const uint32_t n = blockIdx.x, d = (blockIdx.y * kJoinQuads + threadIdx.x) * 4;
+        const int32_t at = p.place[n];
+        const uint32_t share = (splits + Shares - 1) / Shares, first = min(splits, threadIdx.y * share);
+        f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (at >= 0 && d < p.width && first < splits)
+            sum = sum_of(p.sum + uint64_t(at) * p.sum_stride + d + first * step, step, min(share, splits - first));
+        lds[threadIdx.y][threadIdx.x] = sum;
+        __syncthreads();
+        if (threadIdx.y || d >= p.width) return;
+#pragma unroll
+        for (uint32_t s = 1; s < Shares; ++s) sum += lds[s][threadIdx.x];
+        const float back = p.inverse && at >= 0 ? p.inverse[at] : 1.0f;
+        float v[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = sum[q] * back;
+        store_pack<4>(static_cast<T *>(p.grad_hidden) + uint64_t(n) * p.width + d, narrow_pack<T>(v), p.width - d);
+        return;
+    }
     for (uint32_t n = blockIdx.x * blockDim.y + threadIdx.y; n < p.n; n += gridDim.x * blockDim.y) {
         const int32_t at = p.place[n];
         const float back = p.inverse && at >= 0 ? p.inverse[at] : 1.0f;

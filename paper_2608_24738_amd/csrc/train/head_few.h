@@ -12,13 +12,24 @@ namespace tmtrain {
 constexpr int kFewWaves = 4;
 constexpr int kFewClasses = 16 * kFewWaves;     // of a workgroup
 constexpr int kFewSums = 8;
-constexpr int kFewAhead = 8;                    // pieces of a row on their way to a lane
+constexpr uint32_t kFewAhead = 8;                   // pieces of a row on their way to a lane
+
+// The wave's classes, 16 from v0 on: each of its own, or waves share their row's columns.
+struct FewPlace {
+    uint32_t v0, share;
+};
+__device__ __forceinline__ FewPlace few_place(const HeadArgs &p) {
+    const uint32_t wave = blockIdx.x * kFewWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    return {(wave >> p.few_shift) * 16, wave & ((1u << p.few_shift) - 1)};
+}
 
 // h w of 16 classes from v0 on and 16 rows, of which the lane's is `row`: it
-// holds classes v0 + 4 g + q of it.
+// holds classes v0 + 4 g + q of it.  Every wave of a workgroup calls it.
 template <typename T>
-__device__ __forceinline__ f32x4 few_logits(const HeadArgs &p, uint32_t v0, uint32_t row) {
+__device__ __forceinline__ f32x4 few_logits(const HeadArgs &p, uint32_t first, FewPlace at, uint32_t row) {
     constexpr uint32_t V = 16 / sizeof(T), kRound = 4 * V;
+    __shared__ f32x4 lds[kFewWaves][64];
+    const uint32_t v0 = first + at.v0;
     const uint32_t lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const T *w = static_cast<const T *>(p.weight) + uint64_t(min(v0 + r, p.classes - 1)) * p.weight_stride;
     const T *h = static_cast<const T *>(p.hidden) + row * p.hidden_stride;
@@ -26,9 +37,11 @@ __device__ __forceinline__ f32x4 few_logits(const HeadArgs &p, uint32_t v0, uint
     f32x4 acc[kFewSums];
 #pragma unroll
     for (int i = 0; i < kFewSums; ++i) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    uint32_t k = g * V;
+    const uint32_t length = ((p.width + kRound - 1) / kRound + (1u << p.few_shift) - 1 >> p.few_shift) * kRound;
+    const uint32_t end = v0 < p.classes ? min(p.width, (at.share + 1) * length) : 0;
+    uint32_t k = at.share * length + g * V;
     const auto words = [](const Pack<T, int(V)> &x) { return u32x4{x.w[0], x.w[1], x.w[2], x.w[3]}; };
-    for (; k - g * V + kFewAhead * kRound <= p.width; k += kFewAhead * kRound) {
+    for (; k - g * V + kFewAhead * kRound <= end; k += kFewAhead * kRound) {
         Pack<T, int(V)> a[kFewAhead], b[kFewAhead];
 #pragma unroll
         for (int i = 0; i < kFewAhead; ++i) a[i] = load_pack<int(V)>(w + k + i * kRound);
@@ -37,18 +50,37 @@ __device__ __forceinline__ f32x4 few_logits(const HeadArgs &p, uint32_t v0, uint
 #pragma unroll
         for (int i = 0; i < kFewAhead; ++i) acc[i % kFewSums] = multiply<T>(words(a[i]), words(b[i]), acc[i % kFewSums]);
     }
-    for (; k - g * V < p.width; k += kRound) {
-        Pack<T, int(V)> a{}, b{};
-        if (k < p.width) {
-            a = load_pack<int(V)>(w + k, p.width - k, T{});
-            b = load_pack<int(V)>(h + k, p.width - k, T{});
+    if (k - g * V < end) {                              // fewer rounds, of which the last may be part of one
+        const uint32_t left = end - (k - g * V), whole = left / kRound;
+        Pack<T, int(V)> a[kFewAhead], b[kFewAhead], last_a{}, last_b{};
+#pragma unroll
+        for (uint32_t i = 0; i < kFewAhead; ++i) {
+            a[i] = b[i] = Pack<T, int(V)>{};
+            if (i < whole) {
+                a[i] = load_pack<int(V)>(w + k + i * kRound);
+                b[i] = load_pack<int(V)>(h + k + i * kRound);
+            }
         }
-        acc[0] = multiply<T>(words(a), words(b), acc[0]);
+        const uint32_t last = k + whole * kRound;
+        if (left % kRound && last < p.width) {
+            last_a = load_pack<int(V)>(w + last, p.width - last, T{});
+            last_b = load_pack<int(V)>(h + last, p.width - last, T{});
+        }
+#pragma unroll
+        for (uint32_t i = 0; i < kFewAhead; ++i) acc[i % kFewSums] = multiply<T>(words(a[i]), words(b[i]), acc[i % kFewSums]);
+        acc[0] = multiply<T>(words(last_a), words(last_b), acc[0]);
     }
 #pragma unroll
     for (int d = kFewSums / 2; d; d /= 2)
 #pragma unroll
         for (int i = 0; i < d; ++i) acc[i] += acc[i + d];
+    if (p.few_shift) {
+        const uint32_t wave = threadIdx.x >> 6;
+        lds[wave][lane] = acc[0];
+        __syncthreads();
+        acc[0] = lds[wave - at.share][lane];
+        for (uint32_t w = 1; w < 1u << p.few_shift; ++w) acc[0] += lds[wave - at.share + w][lane];
+    }
     return acc[0];
 }
 
@@ -59,10 +91,11 @@ template <typename T>
 __global__ __launch_bounds__(64 * kFewWaves) void k_few_sums(HeadArgs p) {
     __shared__ HeadSum lds[kFewWaves][kFewRows];
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = blockIdx.y * kFewRows + (lane & 15);
-    const uint32_t v0 = (blockIdx.x * kFewWaves + wave) * 16, v = v0 + (lane >> 4) * 4;
+    const FewPlace at = few_place(p);
+    const uint32_t v = at.v0 + (lane >> 4) * 4;
     HeadSum sum = {kLowest, 0.0f};
-    if (v0 < p.classes) {
-        f32x4 x = few_logits<T>(p, v0, min(n, p.n - 1));
+    f32x4 x = few_logits<T>(p, 0, at, min(n, p.n - 1));
+    if (at.v0 < p.classes && at.share == 0) {
         const int32_t y = n < p.n && p.label ? load_label(p.label, p.label_bytes, n, p.classes) : -1;
         if (y >= 0 && uint32_t(y) - v < 4) {
             const uint32_t q = uint32_t(y) - v;
@@ -117,10 +150,11 @@ __global__ __launch_bounds__(256) void k_few_rows(HeadArgs p) {
 // g in float32, [classes][kFewRows]; 0 for rows that take no part.
 template <typename T>
 __global__ __launch_bounds__(64 * kFewWaves) void k_few_slopes(HeadArgs p) {
-    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15;
-    const uint32_t v0 = (blockIdx.x * kFewWaves + wave) * 16, v = v0 + (lane >> 4) * 4;
-    if (v0 >= p.classes) return;
-    const f32x4 x = few_logits<T>(p, v0, min(n, p.n - 1));
+    const uint32_t lane = threadIdx.x & 63, n = lane & 15;
+    const FewPlace at = few_place(p);
+    const uint32_t v = at.v0 + (lane >> 4) * 4;
+    const f32x4 x = few_logits<T>(p, 0, at, min(n, p.n - 1));
+    if (at.v0 >= p.classes || at.share) return;
     int32_t y = -1;
     HeadUp u = {0.0f, 0.0f};
     HeadSum s = {0.0f, 1.0f};
@@ -143,25 +177,29 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_few_slopes(HeadArgs p) {
 }
 
 // g of the packed rows as the tiles read it, in G planes of S, for a piece: what
-// k_head_slopes gives.  Rows from the last one to its 128 get zeros.
+// k_head_slopes gives.  Rows from the last one to its 128 get zeros, and classes
+// from the last one to its 64, which waves without classes of their own write.
 template <typename T, typename S, int G>
 __global__ __launch_bounds__(64 * kFewWaves) void k_few_tiles(HeadArgs p) {
-    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = blockIdx.y * kFewRows + (lane & 15);
-    const uint32_t v0 = (blockIdx.x * kFewWaves + wave) * 16, v = v0 + (lane >> 4) * 4, count = *p.count;
+    const uint32_t lane = threadIdx.x & 63, n = blockIdx.y * kFewRows + (lane & 15), count = *p.count;
+    const FewPlace at = few_place(p);
+    const uint32_t v = at.v0 + at.share * (kFewClasses >> p.few_shift) + (lane >> 4) * 4;
+    const uint32_t rows = min(p.piece, p.classes - p.first);
     if (blockIdx.y * kFewRows >= ((count + 127) & ~127u)) return;
     const bool real = n < count;
     HeadRow r = {0.0f, 0.0f, 0.0f, -1};
     f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
     if (blockIdx.y * kFewRows < count) {
         if (real) r = p.row[n];
-        x = few_logits<T>(p, p.first + v0, p.list[min(n, count - 1)]);
+        x = few_logits<T>(p, p.first, at, p.list[min(n, count - 1)]);
     }
+    if (at.share && (blockIdx.x + 1 < gridDim.x || v >= ((rows + 63) & ~63u))) return;
     float g[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         g[q] = -r.b * exp2_hw((x[q] - r.m) * p.c);
         if (int32_t(p.first + v + q) == r.y) g[q] += r.a;
-        if (!real || p.first + v + q >= p.classes) g[q] = 0.0f;
+        if (!real || v + q >= rows) g[q] = 0.0f;
     }
     const uint64_t to = uint64_t(n) * p.piece + v, plane = uint64_t(p.n_pad) * p.piece;
     Pack<S, 4> out[G];

@@ -20,6 +20,8 @@ constexpr uint64_t kMostClasses = uint64_t(1) << 30;    // 4 of k_few_sums to a 
 constexpr uint64_t kPieceBytes = uint64_t(1) << 27;     // of g
 constexpr uint64_t kLaidBytes = uint64_t(1) << 30;      // of weights laid out in whole steps
 constexpr uint64_t kCus = 256;
+constexpr uint64_t kJoinFew = 1 << 16;                  // groups of four columns of dh
+constexpr uint64_t kMostSplits = 128;                   // of the product for dh
 constexpr uint64_t kPlaneRows = 128;
 constexpr uint64_t kNarrowRows = 64;
 constexpr uint64_t kSmallRows = uint64_t(1) << 19;       // in groups of 16 to a grid's second dimension
@@ -85,6 +87,15 @@ bool few(const HeadShape &s) { return s.n <= kFewRows || small(s); }
 // both passes: 109 us, by the kernels for few 140; float32 284 and 168).
 bool few_grad(const HeadShape &s) { return s.n <= (s.size == 4 ? kFewRows : 4); }
 
+// Which 1 << shift waves share a row's columns in the kernels for few: as many as a workgroup has, unless the chip is
+// full without (forward pass of 2514 x 14 x 3200 bf16 @A us, by single waves 13; 85 x 80 x 1926 float32 @B and 29).
+uint32_t few_shift(const HeadShape &s) {
+    const uint64_t waves = ceil_div(s.classes, 16) * ceil_div(s.n, kFewRows);
+    uint32_t shift = 0;
+    while (1 << shift < kFewWaves && waves << shift < 4 * kCus) ++shift;
+    return shift;
+}
+
 // Floats go to the matrix cores as three 16-bit planes, unless the rows are few.
 bool planes(const HeadShape &s) { return s.size == 4 && s.n > kPlaneRows; }
 
@@ -131,6 +142,7 @@ uint64_t piece_of(uint64_t classes, uint64_t each, uint64_t bytes) {
 }
 
 void head_sizes(const HeadShape &s, bool few, HeadArgs &a) {
+    a.few_shift = few_shift(s);
     a.n = uint32_t(s.n);
     a.classes = uint32_t(s.classes);
     a.width = uint32_t(s.width);
@@ -149,7 +161,7 @@ uint64_t head_room(const HeadShape &s, bool laid, void *at, HeadArgs &a) {
     head_sizes(s, few(s), a);
     a.found = room.take<float>(whole_tiles(s.n));
     if (few(s)) {
-        a.parts = uint32_t(ceil_div(s.classes, kFewClasses));
+        a.parts = uint32_t(ceil_div(s.classes, kFewClasses >> a.few_shift));
         a.part = room.take<HeadSum>(uint64_t(a.parts) * a.n);
         return room.used;
     }
@@ -194,7 +206,7 @@ uint64_t head_grad_room(const HeadShape &s, int dtype, bool laid, bool hidden, b
     // dh: a workgroup to every CU (two of the small tiles, where LDS has room), which the kernel spreads over the tiles
     // that the packed rows take and splits of k, each of 8 steps at least
     const uint64_t steps = a.piece / (s.size == 4 ? 32 : 64);
-    a.most = uint32_t(std::max<uint64_t>(1, std::min<uint64_t>(steps / 8, 32)));
+    a.most = uint32_t(std::max<uint64_t>(1, std::min<uint64_t>(steps / 8, kMostSplits)));
     by_tile_size<true>(s, s.width, s.n, a.most, [&](auto *t) {
         using Tile = std::remove_pointer_t<decltype(t)>;
         a.tiles_m = uint32_t(ceil_div(s.width, Tile::BM));
@@ -241,7 +253,8 @@ dim3 lasting_grid(uint64_t m, uint64_t n) {
 template <typename T>
 int pack_rows(const HeadShape &s, HeadArgs &a, hipStream_t stream) {
     a.chunks = a.n <= 4 * kListChunk ? 0 : uint32_t(ceil_div(a.n, kListChunk));
-    a.pack_rows = a.n <= kPackRows * kCus ? kPackRows / 2 : kPackRows;
+    a.pack_rows = 1;
+    while (a.pack_rows < kPackRows && a.n > 2 * kCus * a.pack_rows) a.pack_rows *= 2;
     if (a.chunks) {
         const int rc = launch(k_head_count, dim3(a.chunks), dim3(256), 0, stream, a);
         if (rc != TM_OK) return rc;
@@ -302,7 +315,7 @@ int run_head(HeadArgs a, const HeadShape &s, hipStream_t stream) {
 
 template <typename T>
 int run_few_grad(const HeadArgs &a, const HeadShape &s, hipStream_t stream) {
-    int rc = launch(k_few_slopes<T>, dim3(uint32_t(ceil_div(s.classes, kFewClasses))), dim3(64 * kFewWaves), 0, stream, a);
+    int rc = launch(k_few_slopes<T>, dim3(uint32_t(ceil_div(s.classes, kFewClasses >> a.few_shift))), dim3(64 * kFewWaves), 0, stream, a);
     if (rc != TM_OK) return rc;
     const dim3 block = few_block(s);
     const dim3 grid(uint32_t(ceil_div(s.classes, a.steps)), uint32_t(ceil_div(s.width, block.x * few_columns(s))));
@@ -326,7 +339,8 @@ int run_head_grad(HeadArgs a, const HeadShape &s, hipStream_t stream) {
         if (a.weight_laid) rc = lay_piece<T>(s, a, stream);
         if (rc != TM_OK) break;
         if (small(s)) {
-            const dim3 grid(a.piece / kFewClasses, a.n_pad / kFewRows);
+            const uint64_t rows = std::min<uint64_t>(a.piece, s.classes - first);
+            const dim3 grid(uint32_t(ceil_div(rows, kFewClasses >> a.few_shift)), a.n_pad / kFewRows);
             auto kernel = k_few_tiles<T, T, 1>;
             if constexpr (sizeof(T) == 4) {
                 if (planes(s)) kernel = k_few_tiles<T, bf16, 3>;
@@ -365,7 +379,12 @@ int run_head_grad(HeadArgs a, const HeadShape &s, hipStream_t stream) {
         }
     }
     if (rc != TM_OK || !a.grad_hidden) return rc;
-    return launch(k_head_hidden_join<T>, join_grid(s.n, s), join_block(s), 0, stream, a);
+    // few rows, which may have many splits
+    const uint64_t quads = ceil_div(s.width, 4);
+    if (s.n * quads <= kJoinFew)
+        return launch(k_head_hidden_join<T, 16>, dim3(a.n, uint32_t(ceil_div(quads, kJoinQuads))), dim3(kJoinQuads, 16), 0,
+                      stream, a);
+    return launch(k_head_hidden_join<T, 1>, join_grid(s.n, s), join_block(s), 0, stream, a);
 }
 
 void head_args(const HeadShape &s, const void *hidden, int64_t hidden_stride, const void *weight, int64_t weight_stride,

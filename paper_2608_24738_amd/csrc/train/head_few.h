@@ -220,10 +220,11 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_few_tiles(HeadArgs p) {
 }
 
 // dw = g^T h and the workgroup's share of dh = g w: a thread has C columns, its
-// workgroup p.steps classes, which the rows of threads take in turn.  N rows of
-// hidden states, whose products in float32 bound it from some four rows on: both
-// passes of 1 x 131072 x 2048 bf16 616 us (3.5 TB/s over the weight's four), of 4
-// rows 808; 16 rows took 961, by tiles 650.
+// workgroup p.steps classes, which the rows of threads take in turn, several on
+// their way at once.  N rows of hidden states.  Two workgroups to a CU: backward
+// passes over 131072 x 2048 bf16 take 324 us for 1 row (g, then the weight read
+// and written at 5 TB/s) and 350 for 8; one to a CU without loads ahead 518 for
+// 1 row, four to a CU 321.
 template <typename T, int N, int C>
 __global__ __launch_bounds__(256) void k_few_outer(HeadArgs p) {
     const uint32_t d = (blockIdx.y * blockDim.x + threadIdx.x) * C;
@@ -245,25 +246,36 @@ __global__ __launch_bounds__(256) void k_few_outer(HeadArgs p) {
         }
     }
     const uint32_t end = min(p.classes, (blockIdx.x + 1) * p.steps);
-    for (uint32_t v = blockIdx.x * p.steps + threadIdx.y; v < end; v += blockDim.y) {
-        const float *g = static_cast<const float *>(p.slope) + uint64_t(v) * kFewRows;
-        float gv[N];
+    constexpr uint32_t kClasses = N > 8 ? 2 : 4;         // on their way at once
+    for (uint32_t v0 = blockIdx.x * p.steps + threadIdx.y; v0 < end; v0 += kClasses * blockDim.y) {
+        float gv[kClasses][N];
+        Pack<T, C> w[kClasses];
 #pragma unroll
-        for (int n = 0; n < N; ++n) gv[n] = g[n];
-        if (p.grad_hidden) {
-            const Pack<T, C> w = load_pack<C>(static_cast<const T *>(p.weight) + v * p.weight_stride + d, left, T{});
+        for (uint32_t u = 0; u < kClasses; ++u) {
+            const uint32_t v = min(v0 + u * blockDim.y, end - 1);
+            const float *g = static_cast<const float *>(p.slope) + uint64_t(v) * kFewRows;
 #pragma unroll
-            for (int n = 0; n < N; ++n)
-#pragma unroll
-                for (int i = 0; i < C; ++i) sum[n][i] = fmaf(gv[n], widen(w.at(i)), sum[n][i]);
+            for (int n = 0; n < N; ++n) gv[u][n] = g[n];
+            if (p.grad_hidden) w[u] = load_pack<C>(static_cast<const T *>(p.weight) + v * p.weight_stride + d, left, T{});
         }
-        if (p.grad_weight) {
-            float x[C] = {};
 #pragma unroll
-            for (int n = 0; n < N; ++n)
+        for (uint32_t u = 0; u < kClasses; ++u) {
+            const uint32_t v = v0 + u * blockDim.y;
+            if (v >= end) break;
+            if (p.grad_hidden) {
 #pragma unroll
-                for (int i = 0; i < C; ++i) x[i] = fmaf(gv[n], h[n][i], x[i]);
-            store_pack<C>(static_cast<T *>(p.grad_weight) + uint64_t(v) * p.width + d, narrow_pack<T>(x), left);
+                for (int n = 0; n < N; ++n)
+#pragma unroll
+                    for (int i = 0; i < C; ++i) sum[n][i] = fmaf(gv[u][n], widen(w[u].at(i)), sum[n][i]);
+            }
+            if (p.grad_weight) {
+                float x[C] = {};
+#pragma unroll
+                for (int n = 0; n < N; ++n)
+#pragma unroll
+                    for (int i = 0; i < C; ++i) x[i] = fmaf(gv[u][n], h[n][i], x[i]);
+                store_pack<C>(static_cast<T *>(p.grad_weight) + uint64_t(v) * p.width + d, narrow_pack<T>(x), left);
+            }
         }
     }
     if (!p.grad_hidden) return;

@@ -83,12 +83,12 @@ uint64_t whole_tiles(uint64_t n) { return ceil_div(n, kTilePad) * kTilePad; }
 
 bool small(const HeadShape &s) { return s.n * s.classes <= kSmallWork / s.width && s.n <= kSmallRows; }
 bool few(const HeadShape &s) { return s.n <= kFewRows || small(s); }
-// The gradient of 16-bit operands reads and writes them at the tiles' pace from five rows on (5 x 32768 x 1024 bf16,
-// both passes: 109 us, by the kernels for few 140; float32 284 and 168).
-bool few_grad(const HeadShape &s) { return s.n <= (s.size == 4 ? kFewRows : 4); }
+// The gradient of 16-bit operands reads and writes them at the tiles' pace from nine rows on (32768 x 1024 bf16: 8 rows
+// 52 us and by tiles 70, 9 rows 71 and 67; float32 keeps to the kernels for few up to 16).
+bool few_grad(const HeadShape &s) { return s.n <= (s.size == 4 ? kFewRows : 8); }
 
 // Which 1 << shift waves share a row's columns in the kernels for few: as many as a workgroup has, unless the chip is
-// full without (forward pass of 2514 x 14 x 3200 bf16 @A us, by single waves 13; 85 x 80 x 1926 float32 @B and 29).
+// full without (forward pass of 2514 x 14 x 3200 bf16 9 us, by single waves 13; 85 x 80 x 1926 float32 10 and 29).
 uint32_t few_shift(const HeadShape &s) {
     const uint64_t waves = ceil_div(s.classes, 16) * ceil_div(s.n, kFewRows);
     uint32_t shift = 0;
@@ -180,7 +180,7 @@ uint64_t head_room(const HeadShape &s, bool laid, void *at, HeadArgs &a) {
 }
 
 // Classes of a workgroup of k_few_outer.
-uint64_t few_share(const HeadShape &s) { return std::max<uint64_t>(16, ceil_div(s.classes, 256)); }
+uint64_t few_share(const HeadShape &s) { return std::max<uint64_t>(16, ceil_div(s.classes, 2 * kCus)); }
 // Columns of a thread of k_few_outer: what its registers hold of n rows, twice in float32.
 uint32_t few_columns(const HeadShape &s) { return s.size == 4 ? 4 : 8; }
 // and its block: as many threads as a row needs, up to 256, the rest for other classes.
@@ -320,9 +320,9 @@ int run_few_grad(const HeadArgs &a, const HeadShape &s, hipStream_t stream) {
     const dim3 block = few_block(s);
     const dim3 grid(uint32_t(ceil_div(s.classes, a.steps)), uint32_t(ceil_div(s.width, block.x * few_columns(s))));
     constexpr int C = sizeof(T) == 4 ? 4 : 8;
-    auto kernel = s.n == 1 ? k_few_outer<T, 1, C> : k_few_outer<T, 4, C>;
+    auto kernel = s.n == 1 ? k_few_outer<T, 1, C> : s.n <= 4 ? k_few_outer<T, 4, C> : k_few_outer<T, 8, C>;
     if constexpr (sizeof(T) == 4) {
-        if (s.n > 4) kernel = k_few_outer<T, 16, 4>;
+        if (s.n > 8) kernel = k_few_outer<T, 16, 4>;
     }
     rc = launch(kernel, grid, block, 0, stream, a);
     if (rc != TM_OK || !a.grad_hidden) return rc;

@@ -76,6 +76,16 @@ def test_sizes(dtype, n, v, d):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("n,v,d", [
+    (6, 900, 264), (8, 777, 100), (9, 14, 2600), (300, 14, 2500), (600, 39, 1303), (90, 65, 1030), (1500, 20, 515),
+    (20, 40000, 24), (33, 50001, 16), (4096, 9, 20), (4097, 9, 20), (2049, 3, 33)])
+def test_waves_that_share_rows_and_many_splits(dtype, n, v, d):
+    """Few classes of long rows, many classes of few and short ones, the numbers of rows where packing changes its way."""
+    hidden, weight, labels, ups = make(n, v, d, dtype, seed=2)
+    compare(hidden, weight, labels, ups, 1.0, False, dtype, "head shared %s %dx%dx%d" % (dtype, n, v, d))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
 @pytest.mark.parametrize("n,v,d", [(1, 500, 96), (9, 100, 40), (33, 300, 64), (200, 700, 100)])
 def test_log_sums_and_scale(dtype, n, v, d):
     hidden, weight, labels, ups = make(n, v, d, dtype, seed=1)

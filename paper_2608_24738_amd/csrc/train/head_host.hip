@@ -21,7 +21,7 @@ constexpr uint64_t kPieceBytes = uint64_t(1) << 27;     // of g
 constexpr uint64_t kLaidBytes = uint64_t(1) << 30;      // of weights laid out in whole steps
 constexpr uint64_t kCus = 256;
 constexpr uint64_t kJoinFew = 1 << 16;                  // groups of four columns of dh
-constexpr uint64_t kMostSplits = 128;                   // of the product for dh
+constexpr uint64_t kMostSplits = 64;                    // of the product for dh
 constexpr uint64_t kPlaneRows = 128;
 constexpr uint64_t kNarrowRows = 64;
 constexpr uint64_t kSmallRows = uint64_t(1) << 19;       // in groups of 16 to a grid's second dimension
@@ -204,9 +204,9 @@ uint64_t head_grad_room(const HeadShape &s, int dtype, bool laid, bool hidden, b
     a.piece = uint32_t(piece_of(s.classes, a.n_pad * slope_held(s), kPieceBytes));
     a.sum_stride = uint32_t(ceil_div(s.width, 4) * 4);
     // dh: a workgroup to every CU (two of the small tiles, where LDS has room), which the kernel spreads over the tiles
-    // that the packed rows take and splits of k, each of 8 steps at least
+    // that the packed rows take and splits of k, each of 4 steps at least
     const uint64_t steps = a.piece / (s.size == 4 ? 32 : 64);
-    a.most = uint32_t(std::max<uint64_t>(1, std::min<uint64_t>(steps / 8, kMostSplits)));
+    a.most = uint32_t(std::max<uint64_t>(1, std::min<uint64_t>(steps / 4, kMostSplits)));
     by_tile_size<true>(s, s.width, s.n, a.most, [&](auto *t) {
         using Tile = std::remove_pointer_t<decltype(t)>;
         a.tiles_m = uint32_t(ceil_div(s.width, Tile::BM));

@@ -236,7 +236,7 @@ __device__ __forceinline__ void lay(const T *from, uint32_t n, S *to, uint64_t p
 // workgroup counts the rows before its own and all of them: one by one, or by the
 // chunks' counts.  Behind the last one, workgroups leave zeros up to a multiple
 // of 64.
-// 4096 rows of 1024 bf16: 9 us, and 5 for the chunks' counts; 509 rows 5.
+// 4096 rows of 1024 bf16: 9.8 us (9 and 5 for chunks' counts); 509 rows 5.6.
 constexpr uint32_t kPackRows = 8;
 template <typename T, typename S, int P>
 __global__ __launch_bounds__(256) void k_head_pack(HeadArgs p) {
@@ -508,8 +508,8 @@ __global__ __launch_bounds__(1024) void k_head_join(HeadArgs p) {
 }
 
 // g of a piece of the vocabulary, in G planes.  As the sums, and bound by its
-// stores, which all workgroups make at once: 16384 classes of 4096 x 1024 bf16 145
-// us (920 TFLOP/s), 8192 of 4096 x 2048 120 (1150).
+// stores, which all workgroups make at once: 16384 classes of 4096 x 1024 bf16 130
+// us (1050 TFLOP/s; 147 by stores of 8 bytes), 8192 of 4096 x 2048 112 (1230).
 template <typename T, typename Tile, int G>
 __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_slopes(HeadArgs p) {
     typedef Held<T, Tile> S;
@@ -578,7 +578,7 @@ __device__ __forceinline__ uint32_t hidden_splits(const HeadArgs &p, uint32_t ti
 
 // The piece's share of dh = g w, over a split of its classes, added to the
 // shares of the pieces before.  4096 x 16384 x 1024 bf16 in 4 splits 131 to 135 us
-// (1010 TFLOP/s), 4096 x 8192 x 2048 in 2 120 (1150).
+// (1020 TFLOP/s), 4096 x 8192 x 2048 in 2 118 (1160).
 template <typename T, typename Tile>
 __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_hidden(HeadArgs p) {
     typedef Held<T, Tile> S;
@@ -631,7 +631,8 @@ __device__ __forceinline__ f32x4 sum_of(const float *from, uint64_t step, uint32
 
 // dh of every row from the splits' sums; rows that took no part get zeros.  Few
 // rows of many splits: Shares threads to four columns, each with a share of the
-// splits, whose sums are added in order.
+// splits, whose sums are added in order (64 x 144 of 64 splits: 4 us, by one
+// thread 12).  4096 x 1024 of 4 splits: 13 us, 5.6 TB/s.
 constexpr uint32_t kJoinQuads = 16;
 template <typename T, uint32_t Shares>
 __global__ __launch_bounds__(256) void k_head_hidden_join(HeadArgs p) {

@@ -386,11 +386,16 @@ __global__ __launch_bounds__(256) void k_embedding_join(EmbeddingArgs p) {
     extern __shared__ float lds[];                      // [blockDim.y][blockDim.x][V]
     const uint32_t chunk = blockIdx.x, first = chunk * p.chunk, last = first + p.chunk;
     if (last >= p.count) return;
-    const uint32_t k = p.sorted_key[last - 1];
-    if (k >= p.rows || p.sorted_key[last] != k) return;                                  // nothing runs on
-    if (first > 0 && p.sorted_key[first - 1] == k) return;                               // an earlier chunk's
-    const uint32_t end = lower_bound(p.sorted_key, p.count, k + 1);
-    const uint32_t chunks = (end - 1) / p.chunk - chunk + 1;
+    const uint32_t k = p.sorted_key[last - 1], next = p.sorted_key[last], before = p.sorted_key[first > 0 ? first - 1 : 0];
+    if (k >= p.rows || next != k) return;                                                // nothing runs on
+    if (first > 0 && before == k) return;                                                // an earlier chunk's
+    // the chunks that begin with the row, a thread to each
+    const uint32_t threads = blockDim.x * blockDim.y, thread = threadIdx.y * blockDim.x + threadIdx.x;
+    uint32_t chunks = 1;
+    for (uint32_t found = threads; found == threads; chunks += found) {
+        const uint64_t at = uint64_t(chunk + chunks + thread) * p.chunk;
+        found = uint32_t(__syncthreads_count(at < p.count && p.sorted_key[at] == k));
+    }
     const uint32_t share = (chunks + blockDim.y - 1) / blockDim.y;
     const uint32_t c = (blockIdx.y * blockDim.x + threadIdx.x) * V;
     float sum[V] = {};

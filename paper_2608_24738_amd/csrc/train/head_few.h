@@ -23,16 +23,51 @@ __device__ __forceinline__ FewPlace few_place(const HeadArgs &p) {
     return {(wave >> p.few_shift) * 16, wave & ((1u << p.few_shift) - 1)};
 }
 
+// A lane's pieces of a row, round by round, of which lane group g has the g-th.
+// Odd: rows may begin between two words, where loads take 2.5 times as long (log
+// sums of 9 x 54800 x 703 float16 56 us, like this 26).  Such a row is read one
+// element further on, and the first element of a piece is then the last one that
+// the group before has read, in the first piece of a round that of the last.
+template <typename T, bool Odd>
+struct FewRow {
+    typedef uint32_t Words __attribute__((ext_vector_type(4), aligned(4)));
+    const T *row;
+    uint32_t lane, carry;
+    bool odd;
+    __device__ __forceinline__ FewRow(const T *row_, uint32_t lane_, uint32_t k, uint32_t width) : row(row_), lane(lane_) {
+        if constexpr (Odd) {
+            odd = uintptr_t(row) & 2;
+            carry = *reinterpret_cast<const uint16_t *>(row + min(k, width - 1));
+        }
+    }
+    __device__ __forceinline__ u32x4 load(uint32_t k) const {
+        if constexpr (Odd) {
+            const Words d = *reinterpret_cast<const Words *>(row + k + odd);
+            return u32x4{d[0], d[1], d[2], d[3]};
+        } else {
+            const auto x = load_pack<16 / int(sizeof(T))>(row + k);
+            return u32x4{x.w[0], x.w[1], x.w[2], x.w[3]};
+        }
+    }
+    // What `load` gave, in rising order of rounds.
+    __device__ __forceinline__ u32x4 piece(u32x4 d) {
+        if constexpr (Odd) {
+            const uint32_t t = uint32_t(__shfl(int(d[3]), int((lane + 48) & 63))) >> 16, e = lane < 16 ? carry : t;
+            carry = t;
+            if (odd) d = u32x4{e | d[0] << 16, d[0] >> 16 | d[1] << 16, d[1] >> 16 | d[2] << 16, d[2] >> 16 | d[3] << 16};
+        }
+        return d;
+    }
+};
+
 // h w of 16 classes from v0 on and 16 rows, of which the lane's is `row`: it
 // holds classes v0 + 4 g + q of it.  Every wave of a workgroup calls it.
-template <typename T>
+template <typename T, bool Odd>
 __device__ __forceinline__ f32x4 few_logits(const HeadArgs &p, uint32_t first, FewPlace at, uint32_t row) {
     constexpr uint32_t V = 16 / sizeof(T), kRound = 4 * V;
     __shared__ f32x4 lds[kFewWaves][64];
     const uint32_t v0 = first + at.v0;
     const uint32_t lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
-    const T *w = static_cast<const T *>(p.weight) + uint64_t(min(v0 + r, p.classes - 1)) * p.weight_stride;
-    const T *h = static_cast<const T *>(p.hidden) + row * p.hidden_stride;
     // several sums, so that none grows to the whole logit step by step
     f32x4 acc[kFewSums];
 #pragma unroll
@@ -40,34 +75,39 @@ __device__ __forceinline__ f32x4 few_logits(const HeadArgs &p, uint32_t first, F
     const uint32_t length = ((p.width + kRound - 1) / kRound + (1u << p.few_shift) - 1 >> p.few_shift) * kRound;
     const uint32_t end = v0 < p.classes ? min(p.width, (at.share + 1) * length) : 0;
     uint32_t k = at.share * length + g * V;
-    const auto words = [](const Pack<T, int(V)> &x) { return u32x4{x.w[0], x.w[1], x.w[2], x.w[3]}; };
-    for (; k - g * V + kFewAhead * kRound <= end; k += kFewAhead * kRound) {
-        Pack<T, int(V)> a[kFewAhead], b[kFewAhead];
+    FewRow<T, Odd> w(static_cast<const T *>(p.weight) + uint64_t(min(v0 + r, p.classes - 1)) * p.weight_stride, lane, k, p.width);
+    FewRow<T, Odd> h(static_cast<const T *>(p.hidden) + row * p.hidden_stride, lane, k, p.width);
+    // an odd row's loads take one element more, which the row must have
+    const uint32_t limit = Odd ? min(end, p.width - 1) : end;
+    for (; k - g * V + kFewAhead * kRound <= limit; k += kFewAhead * kRound) {
+        u32x4 a[kFewAhead], b[kFewAhead];
 #pragma unroll
-        for (int i = 0; i < kFewAhead; ++i) a[i] = load_pack<int(V)>(w + k + i * kRound);
+        for (uint32_t i = 0; i < kFewAhead; ++i) a[i] = w.load(k + i * kRound);
 #pragma unroll
-        for (int i = 0; i < kFewAhead; ++i) b[i] = load_pack<int(V)>(h + k + i * kRound);
+        for (uint32_t i = 0; i < kFewAhead; ++i) b[i] = h.load(k + i * kRound);
 #pragma unroll
-        for (int i = 0; i < kFewAhead; ++i) acc[i % kFewSums] = multiply<T>(words(a[i]), words(b[i]), acc[i % kFewSums]);
+        for (uint32_t i = 0; i < kFewAhead; ++i) acc[i % kFewSums] = multiply<T>(w.piece(a[i]), h.piece(b[i]), acc[i % kFewSums]);
     }
     if (k - g * V < end) {                              // fewer rounds, of which the last may be part of one
-        const uint32_t left = end - (k - g * V), whole = left / kRound;
-        Pack<T, int(V)> a[kFewAhead], b[kFewAhead], last_a{}, last_b{};
+        const uint32_t at = k - g * V, whole = at < limit ? (limit - at) / kRound : 0;
+        u32x4 a[kFewAhead], b[kFewAhead];
+        Pack<T, int(V)> last_a{}, last_b{};
 #pragma unroll
         for (uint32_t i = 0; i < kFewAhead; ++i) {
-            a[i] = b[i] = Pack<T, int(V)>{};
             if (i < whole) {
-                a[i] = load_pack<int(V)>(w + k + i * kRound);
-                b[i] = load_pack<int(V)>(h + k + i * kRound);
+                a[i] = w.load(k + i * kRound);
+                b[i] = h.load(k + i * kRound);
             }
         }
         const uint32_t last = k + whole * kRound;
-        if (left % kRound && last < p.width) {
-            last_a = load_pack<int(V)>(w + last, p.width - last, T{});
-            last_b = load_pack<int(V)>(h + last, p.width - last, T{});
+        if (at + whole * kRound < end && last < p.width) {
+            last_a = load_pack<int(V)>(w.row + last, p.width - last, T{});
+            last_b = load_pack<int(V)>(h.row + last, p.width - last, T{});
         }
+        const auto words = [](const Pack<T, int(V)> &x) { return u32x4{x.w[0], x.w[1], x.w[2], x.w[3]}; };
 #pragma unroll
-        for (uint32_t i = 0; i < kFewAhead; ++i) acc[i % kFewSums] = multiply<T>(words(a[i]), words(b[i]), acc[i % kFewSums]);
+        for (uint32_t i = 0; i < kFewAhead; ++i)
+            if (i < whole) acc[i % kFewSums] = multiply<T>(w.piece(a[i]), h.piece(b[i]), acc[i % kFewSums]);
         acc[0] = multiply<T>(words(last_a), words(last_b), acc[0]);
     }
 #pragma unroll
@@ -87,14 +127,14 @@ __device__ __forceinline__ f32x4 few_logits(const HeadArgs &p, uint32_t first, F
 // Sums over a workgroup's classes of its 16 rows, and the labels' x.  Bound by
 // the weight's bytes: 32768 x 1024 bf16 13.8 us for up to 4 rows (4.8 TB/s),
 // 131072 x 2048 95 (5.6 TB/s).
-template <typename T>
+template <typename T, bool Odd>
 __global__ __launch_bounds__(64 * kFewWaves) void k_few_sums(HeadArgs p) {
     __shared__ HeadSum lds[kFewWaves][kFewRows];
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = blockIdx.y * kFewRows + (lane & 15);
     const FewPlace at = few_place(p);
     const uint32_t v = at.v0 + (lane >> 4) * 4;
     HeadSum sum = {kLowest, 0.0f};
-    f32x4 x = few_logits<T>(p, 0, at, min(n, p.n - 1));
+    f32x4 x = few_logits<T, Odd>(p, 0, at, min(n, p.n - 1));
     if (at.v0 < p.classes && at.share == 0) {
         const int32_t y = n < p.n && p.label ? load_label(p.label, p.label_bytes, n, p.classes) : -1;
         if (y >= 0 && uint32_t(y) - v < 4) {
@@ -148,12 +188,12 @@ __global__ __launch_bounds__(256) void k_few_rows(HeadArgs p) {
 }
 
 // g in float32, [classes][kFewRows]; 0 for rows that take no part.
-template <typename T>
+template <typename T, bool Odd>
 __global__ __launch_bounds__(64 * kFewWaves) void k_few_slopes(HeadArgs p) {
     const uint32_t lane = threadIdx.x & 63, n = lane & 15;
     const FewPlace at = few_place(p);
     const uint32_t v = at.v0 + (lane >> 4) * 4;
-    const f32x4 x = few_logits<T>(p, 0, at, min(n, p.n - 1));
+    const f32x4 x = few_logits<T, Odd>(p, 0, at, min(n, p.n - 1));
     if (at.v0 >= p.classes || at.share) return;
     int32_t y = -1;
     HeadUp u = {0.0f, 0.0f};
@@ -179,7 +219,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_few_slopes(HeadArgs p) {
 // g of the packed rows as the tiles read it, in G planes of S, for a piece: what
 // k_head_slopes gives.  Rows from the last one to its 128 get zeros, and classes
 // from the last one to its 64, which waves without classes of their own write.
-template <typename T, typename S, int G>
+template <typename T, typename S, int G, bool Odd>
 __global__ __launch_bounds__(64 * kFewWaves) void k_few_tiles(HeadArgs p) {
     const uint32_t lane = threadIdx.x & 63, n = blockIdx.y * kFewRows + (lane & 15), count = *p.count;
     const FewPlace at = few_place(p);
@@ -191,7 +231,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_few_tiles(HeadArgs p) {
     f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
     if (blockIdx.y * kFewRows < count) {
         if (real) r = p.row[n];
-        x = few_logits<T>(p, p.first, at, p.list[min(n, count - 1)]);
+        x = few_logits<T, Odd>(p, p.first, at, p.list[min(n, count - 1)]);
     }
     if (at.share && (blockIdx.x + 1 < gridDim.x || v >= ((rows + 63) & ~63u))) return;
     float g[4];

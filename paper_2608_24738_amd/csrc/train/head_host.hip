@@ -291,11 +291,18 @@ dim3 join_grid(uint64_t rows, const HeadShape &s) {
     return dim3(uint32_t(std::min<uint64_t>(ceil_div(rows, join_block(s).y), 4096)));
 }
 
+// Whether rows of 16-bit elements may begin between two words.
+template <typename T>
+bool odd_rows(const HeadArgs &a) {
+    return sizeof(T) == 2 && ((uintptr_t(a.hidden) | uintptr_t(a.weight)) & 2 || (a.hidden_stride | a.weight_stride) & 1);
+}
+
 template <typename T>
 int run_head(HeadArgs a, const HeadShape &s, hipStream_t stream) {
     if (few(s)) {
         const dim3 grid(a.parts, uint32_t(ceil_div(s.n, kFewRows)));
-        const int rc = launch(k_few_sums<T>, grid, dim3(64 * kFewWaves), 0, stream, a);
+        const int rc = launch(odd_rows<T>(a) ? k_few_sums<T, sizeof(T) == 2> : k_few_sums<T, false>, grid,
+                              dim3(64 * kFewWaves), 0, stream, a);
         return rc == TM_OK ? launch(k_few_rows, dim3(a.n), dim3(256), 0, stream, a) : rc;
     }
     int rc = pack_rows<T>(s, a, stream);
@@ -315,7 +322,8 @@ int run_head(HeadArgs a, const HeadShape &s, hipStream_t stream) {
 
 template <typename T>
 int run_few_grad(const HeadArgs &a, const HeadShape &s, hipStream_t stream) {
-    int rc = launch(k_few_slopes<T>, dim3(uint32_t(ceil_div(s.classes, kFewClasses >> a.few_shift))), dim3(64 * kFewWaves), 0, stream, a);
+    int rc = launch(odd_rows<T>(a) ? k_few_slopes<T, sizeof(T) == 2> : k_few_slopes<T, false>,
+                    dim3(uint32_t(ceil_div(s.classes, kFewClasses >> a.few_shift))), dim3(64 * kFewWaves), 0, stream, a);
     if (rc != TM_OK) return rc;
     const dim3 block = few_block(s);
     const dim3 grid(uint32_t(ceil_div(s.classes, a.steps)), uint32_t(ceil_div(s.width, block.x * few_columns(s))));
@@ -341,11 +349,13 @@ int run_head_grad(HeadArgs a, const HeadShape &s, hipStream_t stream) {
         if (small(s)) {
             const uint64_t rows = std::min<uint64_t>(a.piece, s.classes - first);
             const dim3 grid(uint32_t(ceil_div(rows, kFewClasses >> a.few_shift)), a.n_pad / kFewRows);
-            auto kernel = k_few_tiles<T, T, 1>;
+            auto kernel = k_few_tiles<T, T, 1, false>;
             if constexpr (sizeof(T) == 4) {
-                if (planes(s)) kernel = k_few_tiles<T, bf16, 3>;
-            } else {
-                if (fine(s)) kernel = k_few_tiles<T, T, 2>;
+                if (planes(s)) kernel = k_few_tiles<T, bf16, 3, false>;
+            } else if (odd_rows<T>(a)) {
+                kernel = fine(s) ? k_few_tiles<T, T, 2, true> : k_few_tiles<T, T, 1, true>;
+            } else if (fine(s)) {
+                kernel = k_few_tiles<T, T, 2, false>;
             }
             rc = launch(kernel, grid, dim3(64 * kFewWaves), 0, stream, a);
         } else {
@@ -445,7 +455,8 @@ extern "C" size_t tm_head_logp_grad_workspace_size(int dtype, int64_t rows, int6
     const void *some = reinterpret_cast<const void *>(uintptr_t(4096));
     if (check_head(some, dtype, rows, classes, width, 0, some, weight_stride, 0, nullptr, 1.0, s) != TM_OK || s.n == 0)
         return 0;
-    return head_grad_room(s, dtype, !few_grad(s) && to_lay(weight, uint64_t(weight_stride), s), for_hidden != 0, for_weight != 0, nullptr, a);
+    return head_grad_room(s, dtype, !few_grad(s) && to_lay(weight, uint64_t(weight_stride), s), for_hidden != 0,
+                          for_weight != 0, nullptr, a);
 }
 
 extern "C" int tm_head_logp_grad(const void *hidden, int dtype, int64_t rows, int64_t classes, int64_t width,

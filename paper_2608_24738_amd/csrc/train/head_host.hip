@@ -25,9 +25,7 @@ constexpr uint64_t kMostSplits = 64;                    // of the product for dh
 constexpr uint64_t kPlaneRows = 128;
 constexpr uint64_t kNarrowRows = 64;
 constexpr uint64_t kSmallRows = uint64_t(1) << 19;       // in groups of 16 to a grid's second dimension
-// Rows x classes x width up to which tiles take longer than single waves: forward pass of 512 x 1024 x 512, 2^28,
-// bf16 13.3 us and by tiles 18.5, float32 22.7 and 35; of 1024 x 1024 x 512 20.8 and 18.3, 37 and 37.8.
-constexpr uint64_t kSmallWork = uint64_t(1) << 28;
+constexpr double kSmallWork = 1 << 28;                  // rows x classes x width
 
 struct HeadShape {
     uint64_t n, classes, width, size;
@@ -81,7 +79,18 @@ struct Room {
 
 uint64_t whole_tiles(uint64_t n) { return ceil_div(n, kTilePad) * kTilePad; }
 
-bool small(const HeadShape &s) { return s.n * s.classes <= kSmallWork / s.width && s.n <= kSmallRows; }
+// Whether single waves compute the logits sooner than tiles do, by microseconds: theirs go with the work in groups of
+// rows, those of tiles, while CUs are without one, with the steps of k, and rows of no whole 128 bytes are laid out first.
+// Forward passes: of 512 x 1024 x 512, 2^28, bf16 13 us and by tiles 18, float32 23 and 35; of 120 x 2504 x 3920 bf16 44
+// and 61; of 64 x 1500 x 4000 float32 36 and 143; of 24 x 50021 x 777 bf16 36 and 54; of 1024 x 1024 x 512 bf16 20 and 17.
+bool small(const HeadShape &s) {
+    const bool wide = s.size == 4;
+    const double work = double(ceil_div(s.n, kFewRows) * kFewRows) * double(s.classes) * double(s.width) / kSmallWork;
+    const double rounds = std::max<uint64_t>(1, ceil_div(s.n, 128) * ceil_div(s.classes, 128) / (2 * kCus));
+    const double steps = double(ceil_div(s.width, 64)) * rounds * (wide ? 2.2 : 0.65);
+    const double laying = s.width * s.size % 128 ? 3 + double(s.classes * s.width * s.size) * 0.4e-6 : 0;
+    return s.n <= kSmallRows && (work <= 1 || 3 + work * (wide ? 17 : 10) <= 12 + steps + laying);
+}
 bool few(const HeadShape &s) { return s.n <= kFewRows || small(s); }
 // The gradient of 16-bit operands reads and writes them at the tiles' pace from nine rows on (32768 x 1024 bf16: 8 rows
 // 52 us and by tiles 70, 9 rows 71 and 67; float32 keeps to the kernels for few up to 16).

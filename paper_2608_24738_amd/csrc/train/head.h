@@ -15,9 +15,13 @@
 //     beta = scale (up_logp - up_log_sum),
 // and leaves g in the operands' type for the two products
 //     dh = g w,   dw = g^T h.
-// Its rounding to 16 bits is off by as much as that of the results.  With up to
-// kFineRows rows, of which few make up most of a result, g has two planes, 16
-// bits or more; for 512 rows they took 1796 us instead of 1186 (131072 x 2048).
+// Its rounding to 16 bits is off by as much as that of the results, and most of
+// that is the label's own term, the one number of a row that is not small.  What
+// rounding takes from it is kept in float32, `rest`, and added to both products:
+// of 4096 x 32768 x 1024 bf16 the gradients were 0.0024 off and are 0.0017, as
+// float32's rounded once, for 955 us instead of 935.  With up to kFineRows rows,
+// of which few make up most of a result, g has two planes, 16 bits or more; for
+// 512 rows they took 1796 us instead of 1186 (131072 x 2048).
 // Rows without a label take part only where the log sums are asked for: the
 // rows that do are packed first, and the products run over those alone.
 #pragma once
@@ -80,6 +84,7 @@ struct HeadArgs {
     HeadSum *part;              // [parts][n_pad]
     float *found;               // h w of the packed rows' labels
     void *slope, *slope_common; // g [n_pad][piece]; float16: times its row's power of two, and the common one
+    float *rest, *rest_common;  // g of 16 bits: what its rounding takes from the labels', for dh and float16's dw
     void *weight_laid;          // a piece's weights in whole steps, where they do not lie so
     float *sum;                 // dh by splits: [splits][rows of tiles][sum_stride]; few rows: [splits][n][sum_stride]
     uint32_t n_pad, width_pad, sum_stride;
@@ -211,6 +216,13 @@ __device__ __forceinline__ void split(const float (&x)[V], Pack<T, V> (&out)[P])
 #pragma unroll
         for (int j = 0; j < V; ++j) rest[j] -= widen(out[p].at(j));
     }
+}
+
+// What rounding to T takes from x; 0 where that is no number.
+template <typename T>
+__device__ __forceinline__ float lost(float x, T rounded) {
+    const float rest = x - widen(rounded);
+    return fabsf(rest) <= FLT_MAX ? rest : 0.0f;
 }
 
 // V elements as they are laid out: in P planes of S, `plane` elements apart.
@@ -553,8 +565,17 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_slope
                 }
                 const uint64_t to = uint64_t(n) * p.piece + v, plane = uint64_t(p.n_pad) * p.piece;
                 Pack<S, 8> out[G];
+                const auto keep_rest = [&](float *rest) {
+                    if constexpr (sizeof(T) == 2 && G == 1) {
+                        if (!labels) return;
+#pragma unroll
+                        for (int q = 0; q < 8; ++q)
+                            if (r.y >= 0 && want == Tile::pair_row(i) + q) rest[n] = lost(g[q], out[0].at(q));
+                    }
+                };
                 if (!__is_same(T, f16) || p.slope) {
                     split(g, out);
+                    keep_rest(p.rest);
 #pragma unroll
                     for (int k = 0; k < G; ++k) store_pack<8>(static_cast<S *>(p.slope) + to + k * plane, out[k]);
                 }
@@ -563,6 +584,7 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_slope
 #pragma unroll
                     for (int q = 0; q < 8; ++q) g[q] *= ratios[j];
                     split(g, out);
+                    keep_rest(p.rest_common);
 #pragma unroll
                     for (int k = 0; k < G; ++k) store_pack<8>(static_cast<S *>(p.slope_common) + to + k * plane, out[k]);
                 }
@@ -629,10 +651,31 @@ __device__ __forceinline__ f32x4 sum_of(const float *from, uint64_t step, uint32
     return sum;
 }
 
+// The rest of g of packed row `at`'s label and four columns of the label's weights: loaded before the sums that it is
+// added to.  (Infinite weights have made their sums what they are.)
+template <typename T>
+struct LabelRest {
+    float rest = 0.0f;
+    Pack<T, 4> w{};
+    __device__ __forceinline__ LabelRest(const HeadArgs &p, int32_t at, uint32_t d) {
+        const int32_t y = p.rest && at >= 0 && d < p.width ? p.row[at].y : -1;
+        if (y < 0) return;
+        rest = p.rest[at];
+        w = load_pack<4>(static_cast<const T *>(p.weight) + y * p.weight_stride + d, p.width - d, T{});
+    }
+    __device__ __forceinline__ void add_to(f32x4 &sum) const {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const float x = widen(w.at(q));
+            if (fabsf(x) <= FLT_MAX) sum[q] = fmaf(rest, x, sum[q]);
+        }
+    }
+};
+
 // dh of every row from the splits' sums; rows that took no part get zeros.  Few
 // rows of many splits: Shares threads to four columns, each with a share of the
 // splits, whose sums are added in order (64 x 144 of 64 splits: 4 us, by one
-// thread 12).  4096 x 1024 of 4 splits: 13 us, 5.6 TB/s.
+// thread 12).  4096 x 1024 of 4 splits: 15 us, 5.4 TB/s; 13 without the rests, whose rows of the weight lie anywhere.
 constexpr uint32_t kJoinQuads = 16;
 template <typename T, uint32_t Shares>
 __global__ __launch_bounds__(256) void k_head_hidden_join(HeadArgs p) {
@@ -644,6 +687,7 @@ __global__ __launch_bounds__(256) void k_head_hidden_join(HeadArgs p) {
         const uint32_t n = blockIdx.x, d = (blockIdx.y * kJoinQuads + threadIdx.x) * 4;
         const int32_t at = p.place[n];
         const uint32_t share = (splits + Shares - 1) / Shares, first = min(splits, threadIdx.y * share);
+        const LabelRest<T> rest(p, threadIdx.y ? -1 : at, d);
         f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
         if (at >= 0 && d < p.width && first < splits)
             sum = sum_of(p.sum + uint64_t(at) * p.sum_stride + d + first * step, step, min(share, splits - first));
@@ -652,6 +696,7 @@ __global__ __launch_bounds__(256) void k_head_hidden_join(HeadArgs p) {
         if (threadIdx.y || d >= p.width) return;
 #pragma unroll
         for (uint32_t s = 1; s < Shares; ++s) sum += lds[s][threadIdx.x];
+        rest.add_to(sum);
         const float back = p.inverse && at >= 0 ? p.inverse[at] : 1.0f;
         float v[4];
 #pragma unroll
@@ -667,7 +712,9 @@ __global__ __launch_bounds__(256) void k_head_hidden_join(HeadArgs p) {
             f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
             if (at >= 0) {
                 const float *from = p.sum + uint64_t(at) * p.sum_stride + d;
+                const LabelRest<T> rest(p, at, d);
                 sum = sum_of(from, step, splits);
+                rest.add_to(sum);
             }
             float v[4];
 #pragma unroll
@@ -677,8 +724,70 @@ __global__ __launch_bounds__(256) void k_head_hidden_join(HeadArgs p) {
     }
 }
 
+// Adds the rests of g to a tile of dw.  The packed rows from `begin` to `end` whose labels are among the tile's `columns`
+// classes are listed in order, and 64 of them at a time make a step of the product: their hidden states, and rows of
+// zeros with the rest at the label.  `step` is a buffer that all waves have done with.  3891 rows of 4096 x 16384 x 1024
+// bf16, mostly one such step to a tile of 61: dw 115 -> 123 us.
+template <typename Tile>
+struct LabelRows {
+    static constexpr uint32_t kAhead = 4;           // rows that a thread looks at together
+    uint32_t row[64 + kAhead * Tile::kThreads];
+    uint32_t found[kAhead][Tile::kWaves];
+};
+template <typename T, typename Tile>
+__device__ __forceinline__ void add_rests(const HeadArgs &p, Tile &tile, const Operand &hidden, uint32_t m0,
+                                          const Operand &slope, uint32_t n0, uint32_t columns, uint32_t begin, uint32_t end,
+                                          typename Tile::Buffer &step, LabelRows<Tile> &lds) {
+    typedef typename Tile::template Sources<true, true> From;
+    static_assert(Tile::kStep == 64 && Tile::kPlanesB == 1, "a lane of one wave to each row of a step");
+    constexpr uint32_t kAhead = LabelRows<Tile>::kAhead, kThreads = Tile::kThreads;
+    const From from = tile.template sources<true, true>(hidden, m0, slope, n0, 0);
+    const float *rest = __is_same(T, f16) ? p.rest_common : p.rest;
+    const uint32_t low = p.first + n0;
+    const auto add = [&](const uint32_t *rows, uint32_t count) {
+        From::FromA::gather(hidden, m0, rows, count, step.a, tile.lane, tile.wave);
+        for (uint32_t i = threadIdx.x * 16; i < sizeof(step.b); i += kThreads * 16)
+            *reinterpret_cast<u32x4 *>(step.b + i) = u32x4{0, 0, 0, 0};
+        __syncthreads();
+        if (threadIdx.x < count) {
+            const uint32_t n = rows[threadIdx.x];
+            *reinterpret_cast<T *>(step.b + From::FromB::element(threadIdx.x, uint32_t(p.row[n].y) - low)) = narrow<T>(rest[n]);
+        }
+        Tile::sync();
+        f32x4 none[1][1];
+        tile.step(from, step, none);
+        __syncthreads();
+    };
+    uint32_t have = 0;
+    for (uint32_t r0 = begin; r0 < end; r0 += kAhead * kThreads) {
+        uint64_t set[kAhead];
+#pragma unroll
+        for (uint32_t k = 0; k < kAhead; ++k) {
+            const uint32_t n = r0 + k * kThreads + threadIdx.x;
+            const int32_t y = n < end ? p.row[n].y : -1;
+            set[k] = __ballot(y >= 0 && uint32_t(y) - low < columns);
+            if (tile.lane == 0) lds.found[k][tile.wave] = __popcll(set[k]);
+        }
+        __syncthreads();
+#pragma unroll
+        for (uint32_t k = 0; k < kAhead; ++k)
+            for (uint32_t w = 0; w < uint32_t(Tile::kWaves); ++w) {
+                if (w == uint32_t(tile.wave) && set[k] >> tile.lane & 1)
+                    lds.row[have + __popcll(set[k] & ((uint64_t(1) << tile.lane) - 1))] = r0 + k * kThreads + threadIdx.x;
+                have += lds.found[k][w];
+            }
+        __syncthreads();
+        uint32_t done = 0;
+        for (; have - done >= 64; done += 64) add(lds.row + done, 64);
+        have -= done;
+        if (done && threadIdx.x < have) lds.row[threadIdx.x] = lds.row[done + threadIdx.x];
+    }
+    __syncthreads();
+    if (have) add(lds.row, have);
+}
+
 // The piece's rows of dw = g^T h, or their sums over a split of the packed rows.
-// 4096 x 16384 x 1024 bf16 114 us (1170 TFLOP/s), 4096 x 8192 x 2048 112 (1220).
+// 3891 rows of 16384 x 1024 bf16 123 us (1060 TFLOP/s), 4096 of 8192 x 2048 115 (1200).
 template <typename T, typename Tile>
 __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_weight(HeadArgs p) {
     typedef Held<T, Tile> S;
@@ -688,9 +797,15 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_weigh
     const TilePlace at = tile_place(blockIdx.x, tiles_m, tiles_n, p.weight_splits);
     const uint32_t all = (count + Tile::kStep - 1) / Tile::kStep, steps = (all + p.weight_splits - 1) / p.weight_splits;
     const void *slope = __is_same(T, f16) ? p.slope_common : p.slope;
+    const Operand h = hidden_rows<S>(p, p.n_pad), g = slope_rows<S>(p, slope, p.n_pad);
+    const uint32_t first = min(all, at.split * steps), last = min(all, (at.split + 1) * steps);
     Tile tile;
-    tile.template run<true, true>(hidden_rows<S>(p, p.n_pad), at.m * Tile::BM, slope_rows<S>(p, slope, p.n_pad),
-                                  at.n * Tile::BN, min(all, at.split * steps), min(all, (at.split + 1) * steps), even, odd);
+    tile.template run<true, true>(h, at.m * Tile::BM, g, at.n * Tile::BN, first, last, even, odd);
+    if constexpr (sizeof(T) == 2 && Tile::kPlanesB == 1) {
+        __shared__ LabelRows<Tile> labels;
+        add_rests<T>(p, tile, h, at.m * Tile::BM, g, at.n * Tile::BN, min(uint32_t(Tile::BN), rows - at.n * Tile::BN),
+                     first * Tile::kStep, min(count, last * Tile::kStep), even, labels);
+    }
     float back = 1.0f;
     if constexpr (__is_same(T, f16)) {
         back = p.inverse[p.n_pad];

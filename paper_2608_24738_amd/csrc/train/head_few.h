@@ -243,8 +243,16 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_few_tiles(HeadArgs p) {
     }
     const uint64_t to = uint64_t(n) * p.piece + v, plane = uint64_t(p.n_pad) * p.piece;
     Pack<S, 4> out[G];
+    const auto keep_rest = [&](float *rest) {
+        if constexpr (sizeof(T) == 2 && G == 1) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (r.y >= 0 && p.first + v + q == uint32_t(r.y)) rest[n] = lost(g[q], out[0].at(q));
+        }
+    };
     if (!__is_same(T, f16) || p.slope) {
         split(g, out);
+        keep_rest(p.rest);
 #pragma unroll
         for (int k = 0; k < G; ++k) store_pack<4>(static_cast<S *>(p.slope) + to + k * plane, out[k]);
     }
@@ -254,6 +262,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_few_tiles(HeadArgs p) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) g[q] *= ratio;
         split(g, out);
+        keep_rest(p.rest_common);
 #pragma unroll
         for (int k = 0; k < G; ++k) store_pack<4>(static_cast<S *>(p.slope_common) + to + k * plane, out[k]);
     }

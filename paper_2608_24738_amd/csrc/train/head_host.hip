@@ -240,6 +240,10 @@ uint64_t head_grad_room(const HeadShape &s, int dtype, bool laid, bool hidden, b
     const uint64_t slopes = uint64_t(a.n_pad) * a.piece * slope_held(s);
     if (hidden || dtype != TM_DTYPE_F16) a.slope = room.take<char>(slopes);
     if (weight && dtype == TM_DTYPE_F16) a.slope_common = room.take<char>(slopes);
+    if (s.size == 2 && !fine(s)) {
+        if (hidden || dtype != TM_DTYPE_F16) a.rest = room.take<float>(a.n_pad);
+        if (weight && dtype == TM_DTYPE_F16) a.rest_common = room.take<float>(a.n_pad);
+    }
     if (hidden) {
         const uint64_t rows = std::min<uint64_t>(uint64_t(a.most) * a.n_pad, uint64_t(a.blocks / a.tiles_m) * a.tile_n);
         a.sum = room.take<float>(rows * a.sum_stride);

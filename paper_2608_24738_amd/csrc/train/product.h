@@ -170,6 +170,20 @@ struct Across {
         for (int i = 0; i < kCopies; ++i) copy_to_lds(from, offset[i], lds + (i * Waves + wave) * 1024);
         from += uint64_t(K) * stride;
     }
+    // A step of rows that a list of `count` >= 1 numbers gives; behind them the last one again.
+    static __device__ __forceinline__ void gather(const Operand &o, uint32_t m0, const uint32_t *list, uint32_t count,
+                                                  char *lds, int lane, int wave) {
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i) {
+            const uint32_t r = row_of(i, lane, wave), piece = m0 * sizeof(T) / 16 + (lane % kPieces ^ order(r) * kUnitPieces);
+            copy_to_lds(o.at + list[min(r, count - 1)] * o.stride, min(piece, o.pieces - 1) * 16,
+                        lds + (i * Waves + wave) * 1024);
+        }
+    }
+    // Where element c of row r of a step lies.
+    static __device__ __forceinline__ uint32_t element(uint32_t r, uint32_t c) {
+        return r * kRow + (c / 16 ^ order(r)) * 16 * sizeof(T) + c % 16 * sizeof(T);
+    }
     uint32_t place[Blocks];
     __device__ __forceinline__ void reads(int lane, uint32_t block) {
         const uint32_t c = lane & 15, g = lane >> 4;
@@ -266,12 +280,18 @@ struct Tile {
         }
     };
 
-    // Sources for m0.. of A and n0.. of B from step `first` on, which is on its way.
+    // Sources for m0.. of A and n0.. of B from step `first` on.
+    template <bool AAcross, bool BAcross>
+    __device__ __forceinline__ Sources<AAcross, BAcross> sources(const Operand &a, uint32_t m0, const Operand &b,
+                                                                 uint32_t n0, uint32_t first) const {
+        return Sources<AAcross, BAcross>(*this, a, m0, b, n0, first, std::make_index_sequence<PlanesA>{},
+                                         std::make_index_sequence<PlanesB>{});
+    }
+    // The same, with step `first` on its way.
     template <bool AAcross, bool BAcross>
     __device__ __forceinline__ Sources<AAcross, BAcross> begin(const Operand &a, uint32_t m0, const Operand &b, uint32_t n0,
                                                                uint32_t first, Buffer &even) const {
-        Sources<AAcross, BAcross> from(*this, a, m0, b, n0, first, std::make_index_sequence<PlanesA>{},
-                                       std::make_index_sequence<PlanesB>{});
+        auto from = sources<AAcross, BAcross>(a, m0, b, n0, first);
         from.fetch(*this, even, first);
         return from;
     }
@@ -280,6 +300,40 @@ struct Tile {
     static __device__ __forceinline__ void sync() {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
+    }
+
+    // acc += the products of the step in s; low: the small ones of three planes.
+    template <typename From, typename Low>
+    __device__ __forceinline__ void step(const From &from, const Buffer &s, Low &low) {
+#pragma unroll
+        for (int half = 0; half < kHalves; ++half) {
+            u32x4 fa[PlanesA][TM], fb[PlanesB][TN];
+#pragma unroll
+            for (int p = 0; p < PlanesA; ++p)
+#pragma unroll
+                for (int i = 0; i < TM; ++i) fa[p][i] = from.a[0].read(s.a + p * kPlaneA, i, half);
+#pragma unroll
+            for (int p = 0; p < PlanesB; ++p)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) fb[p][j] = from.b[0].read(s.b + p * kPlaneB, j, half);
+            const auto add = [&](auto &to, int pa, int pb) {
+#pragma unroll
+                for (int i = 0; i < TM; ++i)
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) to[i][j] = multiply<T>(fa[pa][i], fb[pb][j], to[i][j]);
+            };
+            if constexpr (From::kFirst) __builtin_amdgcn_s_setprio(1);
+            add(acc, 0, 0);
+            if constexpr (PlanesB == 2) add(acc, 0, 1);
+            if constexpr (PlanesA == 3) {
+                add(low, 0, 1);
+                add(low, 1, 0);
+                add(low, 1, 1);
+                add(low, 0, 2);
+                add(low, 2, 0);
+            }
+            if constexpr (From::kFirst) __builtin_amdgcn_s_setprio(0);
+        }
     }
 
     // The products over steps [first, last), of which `even` has got the first.
@@ -297,37 +351,7 @@ struct Tile {
 #pragma unroll
                 for (int j = 0; j < TN; ++j) low[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         }
-        const auto work = [&](const Buffer &s) {
-#pragma unroll
-            for (int half = 0; half < kHalves; ++half) {
-                u32x4 fa[PlanesA][TM], fb[PlanesB][TN];
-#pragma unroll
-                for (int p = 0; p < PlanesA; ++p)
-#pragma unroll
-                    for (int i = 0; i < TM; ++i) fa[p][i] = from.a[0].read(s.a + p * kPlaneA, i, half);
-#pragma unroll
-                for (int p = 0; p < PlanesB; ++p)
-#pragma unroll
-                    for (int j = 0; j < TN; ++j) fb[p][j] = from.b[0].read(s.b + p * kPlaneB, j, half);
-                const auto add = [&](auto &to, int pa, int pb) {
-#pragma unroll
-                    for (int i = 0; i < TM; ++i)
-#pragma unroll
-                        for (int j = 0; j < TN; ++j) to[i][j] = multiply<T>(fa[pa][i], fb[pb][j], to[i][j]);
-                };
-                if constexpr (From::kFirst) __builtin_amdgcn_s_setprio(1);
-                add(acc, 0, 0);
-                if constexpr (PlanesB == 2) add(acc, 0, 1);
-                if constexpr (PlanesA == 3) {
-                    add(low, 0, 1);
-                    add(low, 1, 0);
-                    add(low, 1, 1);
-                    add(low, 0, 2);
-                    add(low, 2, 0);
-                }
-                if constexpr (From::kFirst) __builtin_amdgcn_s_setprio(0);
-            }
-        };
+        const auto work = [&](const Buffer &s) { step(from, s, low); };
         for (uint32_t k = first; k < last; k += 2) {
             sync();                             // even has arrived, odd is read
             if (k + 1 < last) from.fetch(*this, odd, k + 1);

@@ -505,7 +505,8 @@ def head_log_probs(hidden: torch.Tensor, weight: torch.Tensor, labels: Optional[
 
     Results are float32.  Gradients flow to ``hidden`` and ``weight`` from both
     results.  Products are summed in float32; for more than 256 rows of 16-bit
-    operands the logits' gradient is rounded to their type before its two.
+    operands the logits' gradient is rounded to their type before its two, except
+    at the labels.
     """
     _reverse_only(hidden, weight)
     return HeadLogProbs(*torch_ops().head_log_probs(hidden, weight, labels, scale, log_sums))

@@ -197,8 +197,7 @@ size_t tm_bias_grad_workspace_size(int buckets, int64_t heads);
  *            needs no initialisation.  Rows of the weight that are no multiple of
  *            128 bytes, or not aligned to 16, are laid out there first, and so is
  *            float32 for more than 128 rows, which goes to the matrix cores as
- *            three numbers of 16 bits whose sum it is; an infinity then makes the
- *            logits that it takes part in NaN.
+ *            three numbers of 16 bits whose sum it is.
  *
  * Errors: TM_ERR_SHAPE (classes or width < 1, negative rows or strides),
  * TM_ERR_NULL, TM_ERR_NO_OUTPUT, TM_ERR_DTYPE, TM_ERR_SAMPLING (scale),

@@ -204,7 +204,10 @@ __global__ __launch_bounds__(256) void k_head_count(HeadArgs p) {
     }
 }
 
-// x in planes, each of what the ones before it leave; not finite: NaN.
+template <typename T>
+constexpr float kLargest = __is_same(T, bf16) ? 0x1.fep127f : __is_same(T, f16) ? 65504.0f : FLT_MAX;
+// x in planes, each of what the ones before it leave: nothing of an infinity.  A number that the first plane would round
+// to one is cut to the largest there, and the next plane has the rest.
 template <typename T, int V, int P>
 __device__ __forceinline__ void split(const float (&x)[V], Pack<T, V> (&out)[P]) {
     float rest[V];
@@ -212,6 +215,16 @@ __device__ __forceinline__ void split(const float (&x)[V], Pack<T, V> (&out)[P])
     for (int j = 0; j < V; ++j) rest[j] = x[j];
 #pragma unroll
     for (int p = 0; p < P; ++p) {
+        if (p == 0 && P > 1) {
+            float head[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                head[j] = fabsf(x[j]) <= FLT_MAX ? fminf(fmaxf(x[j], -kLargest<T>), kLargest<T>) : x[j];
+            out[0] = narrow_pack<T>(head);
+#pragma unroll
+            for (int j = 0; j < V; ++j) rest[j] = fabsf(x[j]) == INFINITY ? 0.0f : x[j] - widen(out[0].at(j));
+            continue;
+        }
         out[p] = narrow_pack<T>(rest);
 #pragma unroll
         for (int j = 0; j < V; ++j) rest[j] -= widen(out[p].at(j));

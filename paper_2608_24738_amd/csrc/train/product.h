@@ -223,7 +223,9 @@ struct Across {
 // left out being below 2^-23 of it, and six instructions of 16 bits take less
 // time than those of floats (2048 x 16384 x 1024: sums 300 us and 495).  All but
 // hh have sums of their own: they are 2^-8 of the whole and add no rounding at
-// its size.  Two planes, of B alone, make 16 or 22 bits of a number.
+// its size.  An infinity has the planes inf, 0 and 0: hh then is what the product
+// is, and hm and hl, inf times 0, are left out.  Two planes, of B alone, make 16
+// or 22 bits of a number.
 template <typename T, int BM_, int BN_, int WM_, int WN_, int PlanesA = 1, int PlanesB = PlanesA>
 struct Tile {
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, kPlanes = PlanesA, kPlanesB = PlanesB;
@@ -364,7 +366,10 @@ struct Tile {
 #pragma unroll
             for (int i = 0; i < TM; ++i)
 #pragma unroll
-                for (int j = 0; j < TN; ++j) acc[i][j] += low[i][j];
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        acc[i][j][q] += fabsf(acc[i][j][q]) == INFINITY ? 0.0f : low[i][j][q];
         }
     }
     template <bool AAcross, bool BAcross>

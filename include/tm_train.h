@@ -229,6 +229,8 @@ size_t tm_head_logp_workspace_size(int dtype, int64_t rows, int64_t classes, int
  * (float16: of a multiple by a power of two, one to a row for out_hidden and a
  * common one, of the largest |a| and |z|, for out_weight).  Where every logit
  * of a row is -inf, its g is 0.
+ * The weight is laid out in the workspace as for tm_head_logp where out_hidden or
+ * the logits need it so.
  * Errors: as tm_head_logp.
  */
 int tm_head_logp_grad(const void *hidden, int dtype, int64_t rows, int64_t classes, int64_t width,

@@ -83,12 +83,18 @@ uint64_t whole_tiles(uint64_t n) { return ceil_div(n, kTilePad) * kTilePad; }
 // rows, those of tiles, while CUs are without one, with the steps of k, and rows of no whole 128 bytes are laid out first.
 // Forward passes: of 512 x 1024 x 512, 2^28, bf16 13 us and by tiles 18, float32 23 and 35; of 120 x 2504 x 3920 bf16 44
 // and 61; of 64 x 1500 x 4000 float32 36 and 143; of 24 x 50021 x 777 bf16 36 and 54; of 1024 x 1024 x 512 bf16 20 and 17.
+double small_work(const HeadShape &s) {
+    return double(ceil_div(s.n, kFewRows) * kFewRows) * double(s.classes) * double(s.width) / kSmallWork;
+}
+double tile_rounds(const HeadShape &s) {
+    return double(ceil_div(s.width, 64)) *
+           std::max<uint64_t>(1, ceil_div(s.n, 128) * ceil_div(s.classes, 128) / (2 * kCus));
+}
+double laying_time(const HeadShape &s) { return 3 + double(s.classes * s.width * s.size) * 0.4e-6; }
 bool small(const HeadShape &s) {
     const bool wide = s.size == 4;
-    const double work = double(ceil_div(s.n, kFewRows) * kFewRows) * double(s.classes) * double(s.width) / kSmallWork;
-    const double rounds = std::max<uint64_t>(1, ceil_div(s.n, 128) * ceil_div(s.classes, 128) / (2 * kCus));
-    const double steps = double(ceil_div(s.width, 64)) * rounds * (wide ? 2.2 : 0.65);
-    const double laying = s.width * s.size % 128 ? 3 + double(s.classes * s.width * s.size) * 0.4e-6 : 0;
+    const double work = small_work(s), steps = tile_rounds(s) * (wide ? 2.2 : 0.65);
+    const double laying = s.width * s.size % 128 ? laying_time(s) : 0;
     return s.n <= kSmallRows && (work <= 1 || 3 + work * (wide ? 17 : 10) <= 12 + steps + laying);
 }
 bool few(const HeadShape &s) { return s.n <= kFewRows || small(s); }
@@ -103,6 +109,17 @@ uint32_t few_shift(const HeadShape &s) {
     uint32_t shift = 0;
     while (1 << shift < kFewWaves && waves << shift < 4 * kCus) ++shift;
     return shift;
+}
+
+// The same for g of the gradient, where either way packs the rows; weights that single waves would save from being laid
+// out are those of a gradient without dh, which reads them so.  Whole gradients: of 300 x 513 x 512 bf16 37 us and by tiles
+// 40, of 300 x 1024 x 1024 47 and 44, of 64 x 1500 x 4000 52 and 82, of 24 x 50021 x 777 135 and 119; float32, whose
+// larger tiles of up to kPlaneRows rows take twice as long, of 100 x 5000 x 2047 175 and 233, of 300 x 1024 x 1024 77 and
+// 80, of 17 x 131072 x 2047 1724 and 1422.
+bool small_grad(const HeadShape &s, bool laid) {
+    const bool wide = s.size == 4;
+    const double steps = tile_rounds(s) * (!wide ? 0.65 : s.n > kNarrowRows && s.n <= kPlaneRows ? 4.3 : 2.2);
+    return s.n <= kSmallRows && small_work(s) * (wide ? 17 : 10) <= 1 + steps + (laid ? laying_time(s) : 0);
 }
 
 // Floats go to the matrix cores as three 16-bit planes, unless the rows are few.
@@ -196,6 +213,11 @@ uint32_t few_columns(const HeadShape &s) { return s.size == 4 ? 4 : 8; }
 dim3 few_block(const HeadShape &s) {
     const uint32_t x = std::min<uint32_t>(256, std::max<uint32_t>(16, pow2_from(uint32_t(ceil_div(s.width, few_columns(s))))));
     return dim3(x, 256 / x);
+}
+
+// Whether the gradient lays its weights out: for dh, and for g by tiles.
+bool lays_grad(const HeadShape &s, const void *weight, uint64_t stride, bool hidden) {
+    return !few_grad(s) && to_lay(weight, stride, s) && (hidden || !small_grad(s, true));
 }
 
 // Layout of the gradient's workspace.
@@ -353,13 +375,14 @@ int run_few_grad(const HeadArgs &a, const HeadShape &s, hipStream_t stream) {
 template <typename T>
 int run_head_grad(HeadArgs a, const HeadShape &s, hipStream_t stream) {
     if (few_grad(s)) return run_few_grad<T>(a, s, stream);
+    const bool waves = small_grad(s, !a.grad_hidden && to_lay(a.weight, a.weight_stride, s));
     int rc = pack_rows<T>(s, a, stream);
     for (uint64_t first = 0; rc == TM_OK && first < s.classes; first += a.piece) {
         a.first = uint32_t(first);
         a.add = first > 0;
         if (a.weight_laid) rc = lay_piece<T>(s, a, stream);
         if (rc != TM_OK) break;
-        if (small(s)) {
+        if (waves) {
             const uint64_t rows = std::min<uint64_t>(a.piece, s.classes - first);
             const dim3 grid(uint32_t(ceil_div(rows, kFewClasses >> a.few_shift)), a.n_pad / kFewRows);
             auto kernel = k_few_tiles<T, T, 1, false>;
@@ -468,7 +491,7 @@ extern "C" size_t tm_head_logp_grad_workspace_size(int dtype, int64_t rows, int6
     const void *some = reinterpret_cast<const void *>(uintptr_t(4096));
     if (check_head(some, dtype, rows, classes, width, 0, some, weight_stride, 0, nullptr, 1.0, s) != TM_OK || s.n == 0)
         return 0;
-    return head_grad_room(s, dtype, !few_grad(s) && to_lay(weight, uint64_t(weight_stride), s), for_hidden != 0,
+    return head_grad_room(s, dtype, lays_grad(s, weight, uint64_t(weight_stride), for_hidden != 0), for_hidden != 0,
                           for_weight != 0, nullptr, a);
 }
 
@@ -499,7 +522,7 @@ extern "C" int tm_head_logp_grad(const void *hidden, int dtype, int64_t rows, in
     }
     HeadArgs a{};
     head_args(s, hidden, hidden_stride, weight, weight_stride, labels, scale, a);
-    head_grad_room(s, dtype, !few_grad(s) && to_lay(weight, a.weight_stride, s), out_hidden != nullptr,
+    head_grad_room(s, dtype, lays_grad(s, weight, a.weight_stride, out_hidden != nullptr), out_hidden != nullptr,
                    out_weight != nullptr, workspace, a);
     a.all = up_log_sum != nullptr;
     a.stats = reinterpret_cast<HeadSum *>(const_cast<float *>(stats));

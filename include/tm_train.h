@@ -224,8 +224,9 @@ size_t tm_head_logp_workspace_size(int dtype, int64_t rows, int64_t classes, int
  * that do not get zeros and reach no gradient.  stats are what tm_head_logp
  * gave.  g is computed in float32, a piece of the vocabulary at a time; the two
  * products are summed in float32.  Of 16-bit operands, g is rounded to dtype for
- * more than 256 rows, except at a row's label, where what the rounding takes is
- * added to both products, and for 9 to 256 it is the sum of two numbers of dtype
+ * more than 256 rows of more than 128 classes, except at a row's label, where what
+ * the rounding takes is added to both products; for 9 rows and more of less it is
+ * the sum of two numbers of dtype
  * (float16: of a multiple by a power of two, one to a row for out_hidden and a
  * common one, of the largest |a| and |z|, for out_weight).  Where every logit
  * of a row is -inf, its g is 0.

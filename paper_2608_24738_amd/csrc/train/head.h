@@ -19,9 +19,12 @@
 // that is the label's own term, the one number of a row that is not small.  What
 // rounding takes from it is kept in float32, `rest`, and added to both products:
 // of 4096 x 32768 x 1024 bf16 the gradients were 0.0024 off and are 0.0017, as
-// float32's rounded once, for 955 us instead of 935.  With up to kFineRows rows,
-// of which few make up most of a result, g has two planes, 16 bits or more; for
-// 512 rows they took 1796 us instead of 1186 (131072 x 2048).
+// float32's rounded once, for 955 us instead of 935.  With up to kFineRows rows
+// or kFineClasses classes, of which few make up most of a result, g has two
+// planes, 16 bits or more.  Beyond, they take longer: gradients of 300 x 131072 x
+// 2048 bf16 1149 us instead of 827, of 512 rows 1545 and 1036, of 300 x 512 x 1000
+// 43 and 38, of 300 x 256 x 1000 41 and 36; of 1000 x 128 x 1000 44 and 58, of 4000
+// rows 61 and 66, of 300 rows 37 and 36, since a tile has most rows' labels there.
 // Rows without a label take part only where the log sums are asked for: the
 // rows that do are packed first, and the products run over those alone.
 #pragma once
@@ -33,6 +36,7 @@ namespace tmtrain {
 
 constexpr uint32_t kFewRows = 16;               // rows of hidden states that one matrix instruction holds
 constexpr uint32_t kFineRows = 256;             // rows up to which g of 16-bit operands has two planes
+constexpr uint32_t kFineClasses = 128;          // and classes
 constexpr uint32_t kListChunk = 1024;           // rows that a workgroup counts
 
 struct HeadSum {

@@ -130,7 +130,7 @@ template <typename Tile>
 constexpr uint64_t kSlots = (2 * sizeof(typename Tile::Buffer) <= 80 * 1024 ? 2 : 1) * kCus;
 
 // 16-bit operands whose g has two planes.
-bool fine(const HeadShape &s) { return s.size == 2 && s.n <= kFineRows; }
+bool fine(const HeadShape &s) { return s.size == 2 && (s.n <= kFineRows || s.classes <= kFineClasses); }
 
 // fn(tile): the larger of two, unless it leaves CUs without one or more than
 // half of itself empty; `most` is how often k can be split, of which eight count:

@@ -504,8 +504,8 @@ def head_log_probs(hidden: torch.Tensor, weight: torch.Tensor, labels: Optional[
     ``log_sums``  also the log of the sum of each row's exponentials.
 
     Results are float32.  Gradients flow to ``hidden`` and ``weight`` from both
-    results.  Products are summed in float32; for more than 256 rows of 16-bit
-    operands the logits' gradient is rounded to their type before its two, except
+    results.  Products are summed in float32; for more than 256 rows of more than
+    128 classes of 16 bits the logits' gradient is rounded to their type before its two, except
     at the labels.
     """
     _reverse_only(hidden, weight)

@@ -126,3 +126,16 @@ def test_infinite_weights_keep_their_meaning():
     keep = torch.arange(40, device="cuda") != 3
     assert (dh[mine][:, 3] == -float("inf")).all()
     assert dh[mine][:, keep].isfinite().all() and dw[:7].isfinite().all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("n,v,d", [(300, 30, 300), (257, 128, 100), (1000, 17, 515), (4100, 9, 72), (600, 100, 1303)])
+def test_few_classes(dtype, n, v, d, monkeypatch):
+    """Of up to 128 classes each may be much of a row: g is the sum of two numbers for any number of rows."""
+    monkeypatch.setitem(ref.HALF, dtype, ref.HALF[dtype] ** 2)
+    hidden, weight, labels, ups = make(n, v, d, dtype, seed=7)
+    announce("few classes %s %dx%dx%d" % (dtype, n, v, d))
+    _, (dh, dw) = run(hidden, weight, labels, ups, 1.0, False)
+    want = ref.exact(numbers(hidden), numbers(weight), labels.cpu().numpy(), 1.0, dtype, (numbers(ups[0]), None), False)
+    ref.check(numbers(dh), want["dh"], want["tol_dh"], "hidden's gradient", dtype)
+    ref.check(numbers(dw), want["dw"], want["tol_dw"], "weight's gradient", dtype)

@@ -254,45 +254,47 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void k_norm_grad(NormArgs p) {
 }
 
 // Rows longer than the registers of a workgroup hold (32768 elements of 16 bits): a workgroup to a row, which reads it
-// again for each step, from the caches.
+// again for each step, from the caches, and goes on to others.
 constexpr int kLongThreads = 1024;
 
 template <typename T>
 __global__ __launch_bounds__(kLongThreads) void k_norm_long(NormArgs p) {
     constexpr int V = 16 / sizeof(T);
     __shared__ float lds[kLongThreads / 64][1];
-    const T *x = static_cast<const T *>(p.x) + blockIdx.x * p.stride;
-    const uint32_t c0 = threadIdx.x * V, step = kLongThreads * V;
-    float sum[1] = {0.0f};
-    for (uint32_t c = c0; c < p.width; c += step) {
-        const Pack<T, V> q = load_pack<V>(x + c, p.width - c, T{});
+    for (uint32_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
+        const T *x = static_cast<const T *>(p.x) + row * p.stride;
+        const uint32_t c0 = threadIdx.x * V, step = kLongThreads * V;
+        float sum[1] = {0.0f};
+        for (uint32_t c = c0; c < p.width; c += step) {
+            const Pack<T, V> q = load_pack<V>(x + c, p.width - c, T{});
 #pragma unroll
-        for (int k = 0; k < V; ++k) sum[0] += widen(q.at(k));
-    }
-    row_sums<kLongThreads>(sum, lds);
-    const float mean = sum[0] * p.share;
-    sum[0] = 0.0f;
-    for (uint32_t c = c0; c < p.width; c += step) {
-        const Pack<T, V> q = load_pack<V>(x + c, p.width - c, T{});
-#pragma unroll
-        for (int k = 0; k < V; ++k) {
-            const float v = c + k < p.width ? widen(q.at(k)) - mean : 0.0f;
-            sum[0] = fmaf(v, v, sum[0]);
+            for (int k = 0; k < V; ++k) sum[0] += widen(q.at(k));
         }
-    }
-    row_sums<kLongThreads>(sum, lds);
-    const float r = 1.0f / sqrtf(fmaf(sum[0], p.share, p.eps));
-    if (p.stats && threadIdx.x == 0) p.stats[blockIdx.x] = float2{mean, r};
-    T *y = static_cast<T *>(p.y) + uint64_t(blockIdx.x) * p.width;
-    for (uint32_t c = c0; c < p.width; c += step) {
-        const uint32_t n = p.width - c;
-        const Pack<T, V> q = load_pack<V>(x + c, n, T{});
-        float w[V], b[V], o[V];
-        load_params<V>(p.weight, p.param_type, c, n, 1.0f, w);
-        load_params<V>(p.bias, p.param_type, c, n, 0.0f, b);
+        row_sums<kLongThreads>(sum, lds);
+        const float mean = sum[0] * p.share;
+        sum[0] = 0.0f;
+        for (uint32_t c = c0; c < p.width; c += step) {
+            const Pack<T, V> q = load_pack<V>(x + c, p.width - c, T{});
 #pragma unroll
-        for (int k = 0; k < V; ++k) o[k] = fmaf((widen(q.at(k)) - mean) * r, w[k], b[k]);
-        store_pack<V>(y + c, narrow_pack<T>(o), n);
+            for (int k = 0; k < V; ++k) {
+                const float v = c + k < p.width ? widen(q.at(k)) - mean : 0.0f;
+                sum[0] = fmaf(v, v, sum[0]);
+            }
+        }
+        row_sums<kLongThreads>(sum, lds);
+        const float r = 1.0f / sqrtf(fmaf(sum[0], p.share, p.eps));
+        if (p.stats && threadIdx.x == 0) p.stats[row] = float2{mean, r};
+        T *y = static_cast<T *>(p.y) + uint64_t(row) * p.width;
+        for (uint32_t c = c0; c < p.width; c += step) {
+            const uint32_t n = p.width - c;
+            const Pack<T, V> q = load_pack<V>(x + c, n, T{});
+            float w[V], b[V], o[V];
+            load_params<V>(p.weight, p.param_type, c, n, 1.0f, w);
+            load_params<V>(p.bias, p.param_type, c, n, 0.0f, b);
+#pragma unroll
+            for (int k = 0; k < V; ++k) o[k] = fmaf((widen(q.at(k)) - mean) * r, w[k], b[k]);
+            store_pack<V>(y + c, narrow_pack<T>(o), n);
+        }
     }
 }
 
@@ -300,37 +302,39 @@ template <typename T>
 __global__ __launch_bounds__(kLongThreads) void k_norm_long_grad(NormArgs p) {
     constexpr int V = 16 / sizeof(T);
     __shared__ float lds[kLongThreads / 64][2];
-    const T *x = static_cast<const T *>(p.x) + blockIdx.x * p.stride;
-    const T *up = static_cast<const T *>(p.up) + uint64_t(blockIdx.x) * p.width;
-    const float2 s = p.stats[blockIdx.x];
-    const uint32_t c0 = threadIdx.x * V, step = kLongThreads * V;
-    float sum[2] = {0.0f, 0.0f};
-    for (uint32_t c = c0; c < p.width; c += step) {
-        const uint32_t n = p.width - c;
-        const Pack<T, V> q = load_pack<V>(x + c, n, T{}), g = load_pack<V>(up + c, n, T{});
-        float w[V];
-        load_params<V>(p.weight, p.param_type, c, n, 1.0f, w);
+    for (uint32_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
+        const T *x = static_cast<const T *>(p.x) + row * p.stride;
+        const T *up = static_cast<const T *>(p.up) + uint64_t(row) * p.width;
+        const float2 s = p.stats[row];
+        const uint32_t c0 = threadIdx.x * V, step = kLongThreads * V;
+        float sum[2] = {0.0f, 0.0f};
+        for (uint32_t c = c0; c < p.width; c += step) {
+            const uint32_t n = p.width - c;
+            const Pack<T, V> q = load_pack<V>(x + c, n, T{}), g = load_pack<V>(up + c, n, T{});
+            float w[V];
+            load_params<V>(p.weight, p.param_type, c, n, 1.0f, w);
 #pragma unroll
-        for (int k = 0; k < V; ++k) {
-            const float gw = uint32_t(k) < n ? widen(g.at(k)) * w[k] : 0.0f;
-            sum[0] += gw;
-            sum[1] = fmaf(gw, (widen(q.at(k)) - s.x) * s.y, sum[1]);
+            for (int k = 0; k < V; ++k) {
+                const float gw = uint32_t(k) < n ? widen(g.at(k)) * w[k] : 0.0f;
+                sum[0] += gw;
+                sum[1] = fmaf(gw, (widen(q.at(k)) - s.x) * s.y, sum[1]);
+            }
         }
-    }
-    row_sums<kLongThreads>(sum, lds);
-    const float a = sum[0] * p.share, b = sum[1] * p.share;
-    T *dx = static_cast<T *>(p.dx) + uint64_t(blockIdx.x) * p.width;
-    for (uint32_t c = c0; c < p.width; c += step) {
-        const uint32_t n = p.width - c;
-        const Pack<T, V> q = load_pack<V>(x + c, n, T{}), g = load_pack<V>(up + c, n, T{});
-        float w[V], o[V];
-        load_params<V>(p.weight, p.param_type, c, n, 1.0f, w);
+        row_sums<kLongThreads>(sum, lds);
+        const float a = sum[0] * p.share, b = sum[1] * p.share;
+        T *dx = static_cast<T *>(p.dx) + uint64_t(row) * p.width;
+        for (uint32_t c = c0; c < p.width; c += step) {
+            const uint32_t n = p.width - c;
+            const Pack<T, V> q = load_pack<V>(x + c, n, T{}), g = load_pack<V>(up + c, n, T{});
+            float w[V], o[V];
+            load_params<V>(p.weight, p.param_type, c, n, 1.0f, w);
 #pragma unroll
-        for (int k = 0; k < V; ++k) {
-            const float t = (widen(q.at(k)) - s.x) * s.y;
-            o[k] = (fmaf(widen(g.at(k)), w[k], -a) - t * b) * s.y;
+            for (int k = 0; k < V; ++k) {
+                const float t = (widen(q.at(k)) - s.x) * s.y;
+                o[k] = (fmaf(widen(g.at(k)), w[k], -a) - t * b) * s.y;
+            }
+            store_pack<V>(dx + c, narrow_pack<T>(o), n);
         }
-        store_pack<V>(dx + c, narrow_pack<T>(o), n);
     }
 }
 

@@ -65,6 +65,9 @@ void norm_args(const NormShape &s, const void *x, int64_t stride, const void *we
     a.share = float(1.0 / double(s.width));
 }
 
+// Workgroups for rows that none holds: enough for the chip, since a grid has less than 2^32 threads.
+dim3 long_grid(const NormShape &s) { return dim3(uint32_t(std::min<uint64_t>(s.rows, 2 * kFill))); }
+
 // Workgroups whose sums for dw and db are added afterwards.
 uint64_t norm_parts(const NormShape &s) {
     uint64_t parts = 0;
@@ -107,7 +110,7 @@ extern "C" int tm_layer_norm(const void *x, int dtype, int64_t rows, int64_t wid
                           0, stream, a);
         });
         if (rc != TM_ERR_UNSUPPORTED) return rc;
-        return launch(k_norm_long<T>, dim3(a.rows), dim3(kLongThreads), 0, stream, a);
+        return launch(k_norm_long<T>, long_grid(s), dim3(kLongThreads), 0, stream, a);
     });
 }
 
@@ -156,7 +159,7 @@ extern "C" int tm_layer_norm_grad(const void *x, int dtype, int64_t rows, int64_
             });
             if (rc != TM_ERR_UNSUPPORTED) return rc;
             if (out_x) {
-                const int rc = launch(k_norm_long_grad<T>, dim3(a.rows), dim3(kLongThreads), 0, stream, a);
+                const int rc = launch(k_norm_long_grad<T>, long_grid(s), dim3(kLongThreads), 0, stream, a);
                 if (rc != TM_OK) return rc;
             }
             if (!sums) return int(TM_OK);

@@ -254,7 +254,8 @@ size_t tm_head_logp_grad_workspace_size(int dtype, int64_t rows, int64_t classes
  *   out      [rows][width] contiguous of dtype, rounded once.
  *   out_stats  [rows][2] float32, m and r for tm_layer_norm_grad, or NULL.
  *
- * All arithmetic is float32, the mean taken first.  A row that holds an infinity
+ * All arithmetic is float32, the mean taken first and then what its rounding has
+ * left of it, so that rows far from zero have one as exact.  A row that holds an infinity
  * or NaN becomes NaN, and no other does.
  * Errors: TM_ERR_SHAPE (width < 1, negative rows or stride), TM_ERR_DTYPE,
  * TM_ERR_SAMPLING (eps), TM_ERR_TOO_LARGE (2^31 rows, more than 2^24 columns),

@@ -5,10 +5,12 @@
 //     y = t w + b,
 //     dx = r (g w - mean(g w) - t mean(g w t)),   dw = sum g t,   db = sum g.
 // Bound by memory: x is read once and y written once, and backwards x and g are
-// read once and dx written once.  The mean is taken first and the squares of
-// what is left of it from the registers that hold the row, so that rows far
-// from zero lose nothing.  A thread keeps its columns from row to row: weight,
-// bias and the sums for dw and db stay in registers.
+// read once and dx written once.  The mean is taken first, then the mean and the
+// mean square of what it leaves, from the registers that hold the row: the first
+// mean is off by its sum's rounding, which is much of a row far from zero (rows of
+// 1000.1 came out as up to 0.02 instead of 0), and the second is that error.  A
+// thread keeps its columns from row to row: weight, bias and the sums for dw and
+// db stay in registers.
 #pragma once
 
 #include "train_common.h"
@@ -77,12 +79,22 @@ __device__ __forceinline__ void row_sums(float (&x)[N], float (*lds)[N]) {
     }
 }
 
+// What is left of a row around its first mean: the mean d of it, and r of the row.  Squares about the first mean are
+// d^2 more.
+struct RowRest {
+    float d, r;
+};
+__device__ __forceinline__ RowRest row_rest(const NormArgs &p, const float (&sum)[2]) {
+    const float d = sum[0] * p.share, var = fmaf(sum[1], p.share, -d * d);
+    return {d, 1.0f / sqrtf((var < 0.0f ? 0.0f : var) + p.eps)};
+}
+
 // L threads to a row, each with P pieces of 16 bytes, L pieces apart.  16384 x
-// 2048 bf16: 23 us, 5.8 TB/s.
+// 2048 bf16: 24 us, 5.6 TB/s.
 template <typename T, int L, int P>
 __global__ __launch_bounds__(L > 256 ? L : 256) void k_norm(NormArgs p) {
     constexpr int V = 16 / sizeof(T), kRows = L > 256 ? 1 : 256 / L;
-    __shared__ float lds[L > 64 ? L / 64 : 1][1];
+    __shared__ float lds[L > 64 ? L / 64 : 1][1], lds2[L > 64 ? L / 64 : 1][2];
     const uint32_t lane = threadIdx.x % L;
     uint32_t left[P];           // elements of a piece that the row has
     float w[P][V], b[P][V];
@@ -111,24 +123,25 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void k_norm(NormArgs p) {
         }
         row_sums<L>(sum, lds);
         const float mean = sum[0] * p.share;
-        sum[0] = 0.0f;
+        float rest[2] = {0.0f, 0.0f};
 #pragma unroll
         for (int i = 0; i < P; ++i)
 #pragma unroll
             for (int k = 0; k < V; ++k) {
                 v[i][k] = uint32_t(k) < left[i] ? v[i][k] - mean : 0.0f;
-                sum[0] = fmaf(v[i][k], v[i][k], sum[0]);
+                rest[0] += v[i][k];
+                rest[1] = fmaf(v[i][k], v[i][k], rest[1]);
             }
-        row_sums<L>(sum, lds);
-        const float r = 1.0f / sqrtf(fmaf(sum[0], p.share, p.eps));
-        if (p.stats && lane == 0) p.stats[row] = float2{mean, r};
+        row_sums<L>(rest, lds2);
+        const RowRest s = row_rest(p, rest);
+        if (p.stats && lane == 0) p.stats[row] = float2{mean + s.d, s.r};
         T *y = static_cast<T *>(p.y) + uint64_t(row) * p.width;
 #pragma unroll
         for (int i = 0; i < P; ++i) {
             if (!left[i]) continue;
             float o[V];
 #pragma unroll
-            for (int k = 0; k < V; ++k) o[k] = fmaf(v[i][k] * r, w[i][k], b[i][k]);
+            for (int k = 0; k < V; ++k) o[k] = fmaf((v[i][k] - s.d) * s.r, w[i][k], b[i][k]);
             store_pack<V>(y + (i * L + lane) * V, narrow_pack<T>(o), left[i]);
         }
     }
@@ -260,7 +273,7 @@ constexpr int kLongThreads = 1024;
 template <typename T>
 __global__ __launch_bounds__(kLongThreads) void k_norm_long(NormArgs p) {
     constexpr int V = 16 / sizeof(T);
-    __shared__ float lds[kLongThreads / 64][1];
+    __shared__ float lds[kLongThreads / 64][1], lds2[kLongThreads / 64][2];
     for (uint32_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
         const T *x = static_cast<const T *>(p.x) + row * p.stride;
         const uint32_t c0 = threadIdx.x * V, step = kLongThreads * V;
@@ -272,18 +285,19 @@ __global__ __launch_bounds__(kLongThreads) void k_norm_long(NormArgs p) {
         }
         row_sums<kLongThreads>(sum, lds);
         const float mean = sum[0] * p.share;
-        sum[0] = 0.0f;
+        float rest[2] = {0.0f, 0.0f};
         for (uint32_t c = c0; c < p.width; c += step) {
             const Pack<T, V> q = load_pack<V>(x + c, p.width - c, T{});
 #pragma unroll
             for (int k = 0; k < V; ++k) {
                 const float v = c + k < p.width ? widen(q.at(k)) - mean : 0.0f;
-                sum[0] = fmaf(v, v, sum[0]);
+                rest[0] += v;
+                rest[1] = fmaf(v, v, rest[1]);
             }
         }
-        row_sums<kLongThreads>(sum, lds);
-        const float r = 1.0f / sqrtf(fmaf(sum[0], p.share, p.eps));
-        if (p.stats && threadIdx.x == 0) p.stats[row] = float2{mean, r};
+        row_sums<kLongThreads>(rest, lds2);
+        const RowRest s = row_rest(p, rest);
+        if (p.stats && threadIdx.x == 0) p.stats[row] = float2{mean + s.d, s.r};
         T *y = static_cast<T *>(p.y) + uint64_t(row) * p.width;
         for (uint32_t c = c0; c < p.width; c += step) {
             const uint32_t n = p.width - c;
@@ -292,7 +306,7 @@ __global__ __launch_bounds__(kLongThreads) void k_norm_long(NormArgs p) {
             load_params<V>(p.weight, p.param_type, c, n, 1.0f, w);
             load_params<V>(p.bias, p.param_type, c, n, 0.0f, b);
 #pragma unroll
-            for (int k = 0; k < V; ++k) o[k] = fmaf((widen(q.at(k)) - mean) * r, w[k], b[k]);
+            for (int k = 0; k < V; ++k) o[k] = fmaf((widen(q.at(k)) - mean - s.d) * s.r, w[k], b[k]);
             store_pack<V>(y + c, narrow_pack<T>(o), n);
         }
     }

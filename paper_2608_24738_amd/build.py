@@ -3,6 +3,7 @@ functions with gradients that call it) with the host compiler."""
 from __future__ import annotations
 
 import glob
+import importlib.util
 import os
 import subprocess
 import sys
@@ -43,7 +44,19 @@ def _torch_flags():
     return compile_flags, link_flags
 
 
+def _run(cmd):
+    return subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+
+
+def _finish(running, what: str) -> None:
+    outputs = [proc.communicate()[0] for proc in running]
+    if any(proc.returncode != 0 for proc in running):
+        sys.stderr.write("".join(outputs))
+        raise RuntimeError(what + " failed")
+
+
 def build(verbose: bool = False) -> str:
+    """Builds both. The library needs hipcc alone: it is there also where the torch functions cannot be built, which raises."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     cxx = os.environ.get("CXX", "g++")
     tmp = LIB + ".tmp%d" % os.getpid()
@@ -51,38 +64,51 @@ def build(verbose: bool = False) -> str:
     # the sources share no device code: each is compiled by itself, all at once
     objects = [tmp + "%d.o" % i for i in range(len(SOURCES))]
     torch_object = tmp_ops + ".o"
-    torch_compile, torch_link = _torch_flags()
-    cmds = [[hipcc, *HIPCC_FLAGS, "-I", os.path.join(ROOT, "include"), "-c", src, "-o", obj]
-            for src, obj in zip(SOURCES, objects)]
-    cmds.append([cxx, *torch_compile, "-c", TORCH_SOURCE, "-o", torch_object])
-    links = [([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp, *objects], tmp, LIB),
-             ([cxx, "-shared", "-o", tmp_ops, torch_object, *torch_link], tmp_ops, TORCH_OPS)]
-    if verbose:
-        print("\n".join(" ".join(cmd) for cmd in cmds + [link for link, _, _ in links]), flush=True)
+
+    def start(cmds):
+        if verbose:
+            print("\n".join(" ".join(cmd) for cmd in cmds), flush=True)
+        return [_run(cmd) for cmd in cmds]
+
+    running, torch_running, missing = [], [], None
     try:
-        running = [subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True) for cmd in cmds]
-        outputs = [proc.communicate()[0] for proc in running]
-        if any(proc.returncode != 0 for proc in running):
-            sys.stderr.write("".join(outputs))
-            raise RuntimeError("compiling libtm_edt.so failed")
-        for link, made, target in links:
-            res = subprocess.run(link, capture_output=True, text=True)
-            if res.returncode != 0:
-                sys.stderr.write(res.stdout + res.stderr)
-                raise RuntimeError("linking %s failed" % os.path.basename(target))
-            os.replace(made, target)
+        running = start([[hipcc, *HIPCC_FLAGS, "-I", os.path.join(ROOT, "include"), "-c", src, "-o", obj]
+                         for src, obj in zip(SOURCES, objects)])
+        try:
+            torch_compile, torch_link = _torch_flags()
+            torch_running = start([[cxx, *torch_compile, "-c", TORCH_SOURCE, "-o", torch_object]])
+        except (ImportError, OSError) as err:
+            missing = err
+        _finish(running, "compiling libtm_edt.so")
+        _finish(start([[hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp, *objects]]), "linking libtm_edt.so")
+        os.replace(tmp, LIB)
+        if missing is not None:
+            raise RuntimeError("_torch_ops.so needs torch and a host compiler: %s" % missing) from missing
+        _finish(torch_running, "compiling _torch_ops.so")
+        _finish(start([[cxx, "-shared", "-o", tmp_ops, torch_object, *torch_link]]), "linking _torch_ops.so")
+        os.replace(tmp_ops, TORCH_OPS)
     finally:
-        for obj in objects + [torch_object]:
-            if os.path.exists(obj):
-                os.remove(obj)
+        for proc in running + torch_running:
+            if proc.returncode is None:
+                proc.communicate()
+        for path in objects + [torch_object, tmp, tmp_ops]:
+            if os.path.exists(path):
+                os.remove(path)
     return LIB
+
+
+def _torch_changed() -> float:
+    """When the installed torch last changed, 0 without one."""
+    spec = importlib.util.find_spec("torch")
+    version = os.path.join(os.path.dirname(spec.origin), "version.py") if spec and spec.origin else ""
+    return os.path.getmtime(version) if os.path.exists(version) else 0.0
 
 
 def is_stale() -> bool:
     if not os.path.exists(LIB) or not os.path.exists(TORCH_OPS):
         return True
     t = min(os.path.getmtime(LIB), os.path.getmtime(TORCH_OPS))
-    return any(os.path.getmtime(d) > t for d in DEPS)
+    return any(os.path.getmtime(d) > t for d in DEPS) or _torch_changed() > os.path.getmtime(TORCH_OPS)
 
 
 if __name__ == "__main__":

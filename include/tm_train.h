@@ -181,7 +181,9 @@ size_t tm_bias_grad_workspace_size(int buckets, int64_t heads);
  *                   sum over v of exp(x_nv - scale M)
  *
  * Rows without a label take no part, unless out_log_sum is asked for: what
- * they hold, NaN included, changes nothing, and no work is done for them.
+ * they hold, NaN included, changes nothing, and their out_stats mean nothing.
+ * Products by tiles leave them out; up to 16 rows, and problems so small that
+ * single waves compute their logits, cost what they do with all rows labelled.
  * Where every logit is -inf, out_logp and out_log_sum are -inf; where one is NaN
  * or +inf, the row's results are NaN (out_logp stays 0 without a label).
  * Products are summed in float32.
@@ -221,15 +223,16 @@ size_t tm_head_logp_workspace_size(int dtype, int64_t rows, int64_t classes, int
  *   out_weight[v][d] = sum_n g_nv hidden[n][d]     [classes][width] contiguous, of dtype
  *
  * Either may be NULL.  Rows without a label take part only if z is given; those
- * that do not get zeros and reach no gradient.  stats are what tm_head_logp
- * gave.  g is computed in float32, a piece of the vocabulary at a time; the two
- * products are summed in float32.  Of 16-bit operands, g is rounded to dtype for
- * more than 256 rows of more than 128 classes, except at a row's label, where what
- * the rounding takes is added to both products; for 9 rows and more of less it is
- * the sum of two numbers of dtype
- * (float16: of a multiple by a power of two, one to a row for out_hidden and a
- * common one, of the largest |a| and |z|, for out_weight).  Where every logit
- * of a row is -inf, its g is 0.
+ * that do not get zeros and reach no gradient.  stats are what tm_head_logp gave,
+ * with out_log_sum if z is given.  g is computed in float32, a piece of the
+ * vocabulary at a time; the two products are summed in float32.  Of 16-bit
+ * operands, g is rounded to dtype for more than 256 rows of more than 128 classes,
+ * except at a row's label, where what the rounding takes is added to both
+ * products.  For fewer rows, or classes, it is the sum of two numbers of dtype,
+ * and for up to 8 rows it stays float32.  (float16: of a multiple by a power of
+ * two, one to a row for out_hidden and a common one, of the largest |a| and |z|,
+ * for out_weight.)  Where every logit of a row is -inf, its g is 0; where g is
+ * finite, an infinite weight makes its column of out_hidden infinite or NaN.
  * The weight is laid out in the workspace as for tm_head_logp where out_hidden or
  * the logits need it so.
  * Errors: as tm_head_logp.

@@ -378,7 +378,7 @@ __global__ __launch_bounds__(256) void k_embedding_sums(EmbeddingArgs p) {
     finish(last);
 }
 
-// Rows whose tokens run over several chunks (6.8 us for 1024 chunks of 16 numbers): their sums, in the workgroup of
+// Rows whose tokens run over several chunks (5.4 us for 1024 chunks of 16 numbers): their sums, in the workgroup of
 // the first such chunk, added by the rows of threads in shares and then in order.
 template <typename T>
 __global__ __launch_bounds__(256) void k_embedding_join(EmbeddingArgs p) {

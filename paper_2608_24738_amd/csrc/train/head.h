@@ -430,9 +430,9 @@ __device__ __forceinline__ void each_tile(const HeadArgs &p, uint32_t rows, uint
 
 // Sums of the packed rows over a tile's classes, one for each wave's classes,
 // and the labels' x.  Bound by the matrix cores and what feeds them, at small
-// widths also by the exponentials at a tile's end: 4096 x 32768 x 1024 bf16 216
-// to 234 us by machine (1120 to 1210 TFLOP/s), half of 8192 x 131072 x 2048 1630
-// (1350).
+// widths also by the exponentials at a tile's end: 3891 rows of 4096 x 32768 x 1024
+// bf16 232 to 243 us by machine (1080 to 1120 TFLOP/s), half of 8192 x 131072 x
+// 2048 1610 to 1700 (1290 to 1370).
 template <typename T, typename Tile>
 __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_sums(HeadArgs p) {
     __shared__ __attribute__((aligned(1024))) typename Tile::Buffer even, odd;
@@ -537,8 +537,9 @@ __global__ __launch_bounds__(1024) void k_head_join(HeadArgs p) {
 }
 
 // g of a piece of the vocabulary, in G planes.  As the sums, and bound by its
-// stores, which all workgroups make at once: 16384 classes of 4096 x 1024 bf16 130
-// us (1050 TFLOP/s; 147 by stores of 8 bytes), 8192 of 4096 x 2048 112 (1230).
+// stores, which all workgroups make at once: 16384 classes of 3891 x 1024 bf16 130
+// to 134 us (975 to 1000 TFLOP/s; 147 by stores of 8 bytes), 8192 of 4096 x 2048 110
+// to 117 (1180 to 1250).
 template <typename T, typename Tile, int G>
 __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_slopes(HeadArgs p) {
     typedef Held<T, Tile> S;
@@ -616,8 +617,8 @@ __device__ __forceinline__ uint32_t hidden_splits(const HeadArgs &p, uint32_t ti
 }
 
 // The piece's share of dh = g w, over a split of its classes, added to the
-// shares of the pieces before.  4096 x 16384 x 1024 bf16 in 4 splits 131 to 135 us
-// (1020 TFLOP/s), 4096 x 8192 x 2048 in 2 118 (1160).
+// shares of the pieces before.  3891 x 16384 x 1024 bf16 in 4 splits 130 to 135 us
+// (970 to 1000 TFLOP/s), 4096 x 8192 x 2048 in 2 115 to 124 (1110 to 1200).
 template <typename T, typename Tile>
 __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_hidden(HeadArgs p) {
     typedef Held<T, Tile> S;
@@ -804,7 +805,7 @@ __device__ __forceinline__ void add_rests(const HeadArgs &p, Tile &tile, const O
 }
 
 // The piece's rows of dw = g^T h, or their sums over a split of the packed rows.
-// 3891 rows of 16384 x 1024 bf16 123 us (1060 TFLOP/s), 4096 of 8192 x 2048 115 (1200).
+// 3891 rows of 16384 x 1024 bf16 123 us (1060 TFLOP/s), 4096 of 8192 x 2048 115 to 125 (1100 to 1200).
 template <typename T, typename Tile>
 __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_weight(HeadArgs p) {
     typedef Held<T, Tile> S;

@@ -498,8 +498,8 @@ def head_log_probs(hidden: torch.Tensor, weight: torch.Tensor, labels: Optional[
     ``weight``  (classes, width) of the same type.
     ``labels``  (...); uint8, bool, int32 or int64.  A label outside [0, classes)
                 marks a row without one: log-probability 0, and whatever the row
-                holds reaches no gradient; unless ``log_sums`` are asked for, no
-                work is done for it.  None: no ``log_probs``.
+                holds reaches no gradient.  Large products leave it out, unless
+                ``log_sums`` are asked for.  None: no ``log_probs``.
     ``scale``   positive factor of the logits, such as one over a temperature.
     ``log_sums``  also the log of the sum of each row's exponentials.
 

@@ -235,11 +235,16 @@ __device__ __forceinline__ void split(const float (&x)[V], Pack<T, V> (&out)[P])
     }
 }
 
-// What rounding to T takes from x; 0 where that is no number.
+// What rounding to T takes from a label's g, for packed row n; 0 where that is no number.  For float16, `ratio` takes g to
+// the common power of two.
 template <typename T>
-__device__ __forceinline__ float lost(float x, T rounded) {
-    const float rest = x - widen(rounded);
-    return fabsf(rest) <= FLT_MAX ? rest : 0.0f;
+__device__ __forceinline__ void keep_rest(const HeadArgs &p, uint32_t n, float g, float ratio) {
+    const auto lost = [](float x) {
+        const float rest = x - widen(narrow<T>(x));
+        return fabsf(rest) <= FLT_MAX ? rest : 0.0f;
+    };
+    if (p.rest) p.rest[n] = lost(g);
+    if (__is_same(T, f16) && p.rest_common) p.rest_common[n] = lost(g * ratio);
 }
 
 // V elements as they are laid out: in P planes of S, `plane` elements apart.
@@ -565,6 +570,8 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_slope
             // the label's row among the lane's
             const uint32_t want = uint32_t(r.y) - p.first - at.m * Tile::BM - tile.row(0);
             const bool labels = __any(r.y >= 0 && want < 16u * Tile::TM);
+            float label = 0.0f;
+            bool mine = false;
 #pragma unroll
             for (int i = 0; i < Tile::TM; i += 2) {             // eight rows side by side
                 const uint32_t v = at.m * Tile::BM + tile.row(i);
@@ -574,7 +581,11 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_slope
                 if (labels) {
 #pragma unroll
                     for (int q = 0; q < 8; ++q)
-                        if (r.y >= 0 && want == Tile::pair_row(i) + q) g[q] += r.a;
+                        if (r.y >= 0 && want == Tile::pair_row(i) + q) {
+                            g[q] += r.a;
+                            label = g[q];
+                            mine = true;
+                        }
                 }
                 if (edge) {
 #pragma unroll
@@ -583,17 +594,8 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_slope
                 }
                 const uint64_t to = uint64_t(n) * p.piece + v, plane = uint64_t(p.n_pad) * p.piece;
                 Pack<S, 8> out[G];
-                const auto keep_rest = [&](float *rest) {
-                    if constexpr (sizeof(T) == 2 && G == 1) {
-                        if (!labels) return;
-#pragma unroll
-                        for (int q = 0; q < 8; ++q)
-                            if (r.y >= 0 && want == Tile::pair_row(i) + q) rest[n] = lost(g[q], out[0].at(q));
-                    }
-                };
                 if (!__is_same(T, f16) || p.slope) {
                     split(g, out);
-                    keep_rest(p.rest);
 #pragma unroll
                     for (int k = 0; k < G; ++k) store_pack<8>(static_cast<S *>(p.slope) + to + k * plane, out[k]);
                 }
@@ -602,10 +604,12 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWaves / 4) void k_head_slope
 #pragma unroll
                     for (int q = 0; q < 8; ++q) g[q] *= ratios[j];
                     split(g, out);
-                    keep_rest(p.rest_common);
 #pragma unroll
                     for (int k = 0; k < G; ++k) store_pack<8>(static_cast<S *>(p.slope_common) + to + k * plane, out[k]);
                 }
+            }
+            if constexpr (sizeof(T) == 2 && G == 1) {
+                if (mine) keep_rest<T>(p, n, label, __is_same(T, f16) ? ratios[j] : 1.0f);
             }
         }
     });

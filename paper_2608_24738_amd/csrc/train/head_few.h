@@ -241,28 +241,25 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_few_tiles(HeadArgs p) {
         if (int32_t(p.first + v + q) == r.y) g[q] += r.a;
         if (!real || v + q >= rows) g[q] = 0.0f;
     }
+    float ratio = 1.0f;
+    if constexpr (__is_same(T, f16)) ratio = real ? p.inverse[n] / p.inverse[p.n_pad] : 1.0f;
+    if constexpr (sizeof(T) == 2 && G == 1) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            if (r.y >= 0 && p.first + v + q == uint32_t(r.y)) keep_rest<T>(p, n, g[q], ratio);
+    }
     const uint64_t to = uint64_t(n) * p.piece + v, plane = uint64_t(p.n_pad) * p.piece;
     Pack<S, 4> out[G];
-    const auto keep_rest = [&](float *rest) {
-        if constexpr (sizeof(T) == 2 && G == 1) {
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                if (r.y >= 0 && p.first + v + q == uint32_t(r.y)) rest[n] = lost(g[q], out[0].at(q));
-        }
-    };
     if (!__is_same(T, f16) || p.slope) {
         split(g, out);
-        keep_rest(p.rest);
 #pragma unroll
         for (int k = 0; k < G; ++k) store_pack<4>(static_cast<S *>(p.slope) + to + k * plane, out[k]);
     }
     if constexpr (__is_same(T, f16)) {
         if (!p.slope_common) return;
-        const float ratio = real ? p.inverse[n] / p.inverse[p.n_pad] : 1.0f;
 #pragma unroll
         for (int q = 0; q < 4; ++q) g[q] *= ratio;
         split(g, out);
-        keep_rest(p.rest_common);
 #pragma unroll
         for (int k = 0; k < G; ++k) store_pack<4>(static_cast<S *>(p.slope_common) + to + k * plane, out[k]);
     }
